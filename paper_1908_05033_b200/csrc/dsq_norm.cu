@@ -1,0 +1,639 @@
+// Root-mean-square norm in front of a low-bit linear layer, and its backward pass.
+//
+//   h = x + residual;  rstd = 1/sqrt(mean_k h^2 + eps);  y = h rstd w
+//   8 bits: a = max_k |h w|, q = floor(127 h w / a + 1/2), s = rstd a / 127 (so that
+//   y is about s q): the codes do not depend on rstd, and one pass of reductions
+//   gives the sum of squares and a together.
+//   backward, with g = grad_y w and n = h rstd:
+//   grad_x = rstd (g - n mean_k(g n)) + grad_h,  grad_w = sum_m grad_y n
+//
+// All arithmetic is binary32; outputs are rounded once, to their type.  The sum of the
+// residual is not rounded before it is normalised.
+//
+// Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward).  A row stays in
+// registers between its reduction and its outputs, so every input is read once; the next
+// row of the same threads is on its way meanwhile.  Rows whose length is no multiple of
+// eight start inside a 16-byte vector: the eight-element vectors are counted from the
+// start of the array then, which is the same grid for all arrays of one shape whatever
+// their types, and what a row's first and last vector hold of its neighbours is masked.
+// A thread meets the same columns in all its rows (the weight, and the sums of grad_w,
+// stay in registers): its rows are a multiple of eight apart where rows shift.
+#include <math.h>
+
+#include "dsq_launch.h"
+#include "dsq_ptx.cuh"
+#include "dsq_tc_host.h"
+#include "dsq_types.cuh"
+
+using dsq_ptx::grid_dependency_wait;
+using dsq_ptx::grid_launch_dependents;
+
+namespace {
+
+constexpr int64_t MAX_K = 49152;          // the backward pass keeps a row of sums in shared memory
+
+struct FwdParams {
+    const void *x, *res;
+    const float *w;
+    void *h, *y;
+    int8_t *codes;
+    float *scale, *rstd;
+    int64_t M, total;                     // total: M K
+    int K;
+    float eps, inv_k;
+};
+struct BwdParams {
+    const void *gy, *gh, *h;
+    const float *w, *rstd;
+    void *gx;
+    float *part;                          // [blocks][K], or NULL
+    int64_t M, total;
+    int K;
+    float inv_k;
+};
+
+__host__ __device__ constexpr int block_of(int tpr) { return tpr < 256 ? 256 : tpr; }
+
+template <class T, bool ALIGNED>
+__device__ __forceinline__ DsqRaw8<T> load_vec(const T *p, int64_t at, int64_t total)
+{
+    if constexpr (ALIGNED) {
+        return dsq_load8(p + at);
+    } else {
+        if (at + 8 <= total) return dsq_load8(p + at);
+        // the last vector of the array: nothing behind its end is read
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = at + i < total ? dsq_to_f32(p[at + i]) : 0.f;
+        DsqRaw8<T> r;
+        dsq_pack8(f, r);
+        return r;
+    }
+}
+// f[] of columns outside the row: 0
+template <bool ALIGNED> __device__ __forceinline__ void mask(float (&f)[8], int col, int K)
+{
+    if constexpr (!ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(col + i) >= (unsigned)K) f[i] = 0.f;
+    }
+}
+template <class T, bool ALIGNED>
+__device__ __forceinline__ void store_vec(T *p, int64_t at, int col, int K, const float (&f)[8])
+{
+    if (ALIGNED || (col >= 0 && col + 8 <= K)) {
+        DsqRaw8<T> r;
+        dsq_pack8(f, r);
+        dsq_store8(p + at, r);
+    } else if constexpr (!ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(col + i) < (unsigned)K) p[at + i] = dsq_from_f32<T>(f[i]);
+    }
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void store_codes(int8_t *p, int64_t at, int col, int K, const int (&q)[8])
+{
+    if (ALIGNED || (col >= 0 && col + 8 <= K)) {
+        uint2 v;
+        v.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
+        v.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+        *reinterpret_cast<uint2 *>(p + at) = v;
+    } else if constexpr (!ALIGNED) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if ((unsigned)(col + i) < (unsigned)K) p[at + i] = (int8_t)q[i];
+    }
+}
+template <bool ALIGNED>
+__device__ __forceinline__ void load_weight(const float *w, int col, int K, bool in, float (&f)[8])
+{
+    if (ALIGNED && in) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float4 v = __ldg(reinterpret_cast<const float4 *>(w + col) + i);
+            f[4 * i] = v.x; f[4 * i + 1] = v.y; f[4 * i + 2] = v.z; f[4 * i + 3] = v.w;
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = in && (unsigned)(col + i) < (unsigned)K ? __ldg(w + col + i) : 0.f;
+}
+
+// sum and largest of the TPR threads of a row, to all of them.  `red`: one entry a warp.
+// Every thread of the block calls it.
+template <int TPR>
+__device__ __forceinline__ void reduce_row(float &sum, uint32_t &top, float2 *red)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+    top = __reduce_max_sync(~0u, top);
+    if constexpr (TPR > 32) {
+        constexpr int W = TPR / 32;
+        if (lane == 0) red[warp] = make_float2(sum, __uint_as_float(top));
+        __syncthreads();
+        const float2 v = red[warp / W * W + (lane % W)];
+        sum = v.x;
+#pragma unroll
+        for (int o = W / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        top = __reduce_max_sync(~0u, __float_as_uint(v.y));
+    }
+}
+
+// what a row's reductions give its elements
+struct RowQuant { float rstd, inv, s; };
+__device__ __forceinline__ RowQuant row_quant(float sum, uint32_t top, float inv_k, float eps)
+{
+    RowQuant r;
+    r.rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(sum, inv_k, eps)));
+    const float a = __uint_as_float(top);
+    // (bits above those of infinity: NaN)
+    const bool bad = top >= 0x7F800000u, none = a < 1.5046328e-36f;      // 2^-119: 127 / a is finite
+    r.inv = bad || none ? 0.f : __fdiv_rn(127.f, a);
+    r.s = bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : r.rstd * a * (1.f / 127.f);
+    return r;
+}
+__device__ __forceinline__ int code_of(float hw, float inv)
+{
+    return inv == 0.f ? 0 : __float2int_rd(__fmaf_rn(hw, inv, 0.5f));
+}
+
+template <class T, bool ALIGNED>
+__device__ __forceinline__ void write_outputs(const FwdParams &p, int64_t at, int col, const float (&h)[8],
+                                              const float (&w)[8], const RowQuant &r)
+{
+    if (p.h) store_vec<T, ALIGNED>((T *)p.h, at, col, p.K, h);
+    float y[8];
+    if (p.scale) {
+        int q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            q[i] = code_of(h[i] * w[i], r.inv);
+            y[i] = r.s * (float)q[i];
+        }
+        if (p.codes) store_codes<ALIGNED>(p.codes, at, col, p.K, q);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = h[i] * r.rstd * w[i];
+    }
+    if (p.y) store_vec<T, ALIGNED>((T *)p.y, at, col, p.K, y);
+}
+
+// TPR threads a row, ITEMS vectors of eight a thread
+template <class T, int TPR, int ITEMS, bool ALIGNED>
+__global__ void __launch_bounds__(block_of(TPR)) rmsnorm_fwd_kernel(const FwdParams p)
+{
+    constexpr int RPB = block_of(TPR) / TPR;
+    __shared__ float2 red[2][block_of(TPR) / 32];
+    const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * RPB;          // (a multiple of 8 unless ALIGNED)
+    const int64_t first = (int64_t)blockIdx.x * RPB + sub;
+    const int K = p.K, off = ALIGNED ? 0 : ((int)(first & 7) * (K & 7)) & 7;
+    const int nv = (off + K + 7) >> 3;
+    const T *x = (const T *)p.x, *res = (const T *)p.res;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float w[ITEMS][8];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) load_weight<ALIGNED>(p.w, 8 * (t + i * TPR) - off, K, t + i * TPR < nv, w[i]);
+
+    DsqRaw8<T> xr[ITEMS], rr[ITEMS];
+    auto load = [&](int64_t row) {
+        const int64_t at = row * K - off;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int v = t + i * TPR;
+            if (row < p.M && v < nv) {
+                xr[i] = load_vec<T, ALIGNED>(x, at + 8 * v, p.total);
+                if (res) rr[i] = load_vec<T, ALIGNED>(res, at + 8 * v, p.total);
+            }
+        }
+    };
+    load(first);
+    int buf = 0;
+    for (int64_t base = (int64_t)blockIdx.x * RPB; base < p.M; base += step, buf ^= 1) {
+        const int64_t row = base + sub, at = row * K - off;
+        float h[ITEMS][8];
+        float sum = 0.f;
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int v = t + i * TPR;
+            const bool in = row < p.M && v < nv;
+            dsq_unpack8(xr[i], h[i]);
+            if (res) {
+                float a[8];
+                dsq_unpack8(rr[i], a);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[i][k] += a[k];
+            }
+            mask<ALIGNED>(h[i], 8 * v - off, K);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                if (!in) h[i][k] = 0.f;
+                sum = __fmaf_rn(h[i][k], h[i][k], sum);
+                top = max(top, __float_as_uint(h[i][k] * w[i][k]) & 0x7FFFFFFFu);
+            }
+        }
+        load(row + step);
+        reduce_row<TPR>(sum, top, red[buf]);
+        const RowQuant r = row_quant(sum, top, p.inv_k, p.eps);
+        if (row < p.M) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int v = t + i * TPR;
+                if (v < nv) write_outputs<T, ALIGNED>(p, at + 8 * v, 8 * v - off, h[i], w[i], r);
+            }
+            if (t == 0) {
+                if (p.scale) p.scale[row] = r.s;
+                if (p.rstd) p.rstd[row] = r.rstd;
+            }
+        }
+    }
+}
+
+// rows too long for the registers of a block: read twice, the second time from the caches
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(1024) rmsnorm_fwd_long_kernel(const FwdParams p)
+{
+    __shared__ float2 red[2][32];
+    const T *x = (const T *)p.x, *res = (const T *)p.res;
+    const int K = p.K;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    int buf = 0;
+    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x, buf ^= 1) {
+        const int off = ALIGNED ? 0 : ((int)(row & 7) * (K & 7)) & 7, nv = (off + K + 7) >> 3;
+        const int64_t at = row * K - off;
+        auto value = [&](int v, float (&h)[8], float (&w)[8]) {
+            dsq_unpack8(load_vec<T, ALIGNED>(x, at + 8 * v, p.total), h);
+            if (res) {
+                float a[8];
+                dsq_unpack8(load_vec<T, ALIGNED>(res, at + 8 * v, p.total), a);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) h[k] += a[k];
+            }
+            mask<ALIGNED>(h, 8 * v - off, K);
+            load_weight<ALIGNED>(p.w, 8 * v - off, K, true, w);
+        };
+        float sum = 0.f, h[8], w[8];
+        uint32_t top = 0;
+        for (int v = threadIdx.x; v < nv; v += 1024) {
+            value(v, h, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                sum = __fmaf_rn(h[k], h[k], sum);
+                top = max(top, __float_as_uint(h[k] * w[k]) & 0x7FFFFFFFu);
+            }
+        }
+        reduce_row<1024>(sum, top, red[buf]);
+        const RowQuant r = row_quant(sum, top, p.inv_k, p.eps);
+        for (int v = threadIdx.x; v < nv; v += 1024) {
+            value(v, h, w);
+            write_outputs<T, ALIGNED>(p, at + 8 * v, 8 * v - off, h, w, r);
+        }
+        if (threadIdx.x == 0) {
+            if (p.scale) p.scale[row] = r.s;
+            if (p.rstd) p.rstd[row] = r.rstd;
+        }
+    }
+}
+
+template <class T, int TPR, int ITEMS, bool ALIGNED>
+__global__ void __launch_bounds__(block_of(TPR)) rmsnorm_bwd_kernel(const BwdParams p)
+{
+    constexpr int RPB = block_of(TPR) / TPR;
+    __shared__ float2 red[2][block_of(TPR) / 32];
+    __shared__ float wsum[RPB > 1 ? TPR * ITEMS * 8 : 1];
+    const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
+    const int64_t step = (int64_t)gridDim.x * RPB;          // (a multiple of 8 unless ALIGNED)
+    const int64_t first = (int64_t)blockIdx.x * RPB + sub;
+    const int K = p.K, off = ALIGNED ? 0 : ((int)(first & 7) * (K & 7)) & 7;
+    const int nv = (off + K + 7) >> 3;
+    const T *gy = (const T *)p.gy, *gh = (const T *)p.gh, *hh = (const T *)p.h;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float w[ITEMS][8], gw[ITEMS][8];
+#pragma unroll
+    for (int i = 0; i < ITEMS; ++i) {
+        load_weight<ALIGNED>(p.w, 8 * (t + i * TPR) - off, K, t + i * TPR < nv, w[i]);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) gw[i][k] = 0.f;
+    }
+
+    DsqRaw8<T> yr[ITEMS], hr[ITEMS], gr[ITEMS];
+    float rs = 0.f;
+    auto load = [&](int64_t row) {
+        const int64_t at = row * K - off;
+        if (row < p.M) rs = p.rstd[row];
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int v = t + i * TPR;
+            if (row < p.M && v < nv) {
+                yr[i] = load_vec<T, ALIGNED>(gy, at + 8 * v, p.total);
+                hr[i] = load_vec<T, ALIGNED>(hh, at + 8 * v, p.total);
+                if (gh) gr[i] = load_vec<T, ALIGNED>(gh, at + 8 * v, p.total);
+            }
+        }
+    };
+    load(first);
+    int buf = 0;
+    for (int64_t base = (int64_t)blockIdx.x * RPB; base < p.M; base += step, buf ^= 1) {
+        const int64_t row = base + sub, at = row * K - off;
+        const float rstd = rs;
+        float g[ITEMS][8], n[ITEMS][8];
+        DsqRaw8<T> add[ITEMS];
+        float sum = 0.f;
+        uint32_t none = 0;
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int v = t + i * TPR;
+            const bool in = row < p.M && v < nv;
+            dsq_unpack8(yr[i], g[i]);
+            dsq_unpack8(hr[i], n[i]);
+            add[i] = gr[i];
+            mask<ALIGNED>(g[i], 8 * v - off, K);
+            mask<ALIGNED>(n[i], 8 * v - off, K);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                n[i][k] = in ? n[i][k] * rstd : 0.f;
+                if (!in) g[i][k] = 0.f;
+                gw[i][k] = __fmaf_rn(g[i][k], n[i][k], gw[i][k]);
+                g[i][k] *= w[i][k];
+                sum = __fmaf_rn(g[i][k], n[i][k], sum);
+            }
+        }
+        load(row + step);
+        reduce_row<TPR>(sum, none, red[buf]);
+        const float c = sum * p.inv_k;
+        if (row < p.M) {
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i) {
+                const int v = t + i * TPR;
+                if (v >= nv) continue;
+                float o[8], a[8];
+                if (gh) dsq_unpack8(add[i], a);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    o[k] = rstd * __fmaf_rn(-n[i][k], c, g[i][k]);
+                    if (gh) o[k] += a[k];
+                }
+                store_vec<T, ALIGNED>((T *)p.gx, at + 8 * v, 8 * v - off, K, o);
+            }
+        }
+    }
+    if (!p.part) return;
+    // the block's row of sums: those of its rows' threads in turn
+    float *part = p.part + (int64_t)blockIdx.x * K;
+    if constexpr (RPB == 1) {
+#pragma unroll
+        for (int i = 0; i < ITEMS; ++i) {
+            const int col = 8 * (t + i * TPR) - off;
+            if (t + i * TPR >= nv) continue;
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (ALIGNED || (unsigned)(col + k) < (unsigned)K) part[col + k] = gw[i][k];
+        }
+    } else {
+        for (int s = 0; s < RPB; ++s) {
+            if (sub == s) {
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i) {
+                    const int col = 8 * (t + i * TPR) - off;
+                    if (t + i * TPR >= nv) continue;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        if ((unsigned)(col + k) < (unsigned)K) wsum[col + k] = s ? wsum[col + k] + gw[i][k] : gw[i][k];
+                }
+            }
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < K; c += block_of(TPR)) part[c] = wsum[c];
+    }
+}
+
+// long rows: read twice, the sums of grad_w in shared memory (a column's entry is one
+// thread's alone: the block's rows shift alike, being a multiple of eight apart)
+template <class T, bool ALIGNED>
+__global__ void __launch_bounds__(1024) rmsnorm_bwd_long_kernel(const BwdParams p)
+{
+    extern __shared__ float gw[];
+    __shared__ float2 red[2][32];
+    const T *gy = (const T *)p.gy, *gh = (const T *)p.gh, *hh = (const T *)p.h;
+    const int K = p.K, off = ALIGNED ? 0 : ((int)(blockIdx.x & 7) * (K & 7)) & 7, nv = (off + K + 7) >> 3;
+    for (int c = threadIdx.x; c < K; c += 1024) gw[c] = 0.f;
+    __syncthreads();
+    grid_dependency_wait();
+    grid_launch_dependents();
+    int buf = 0;
+    for (int64_t row = blockIdx.x; row < p.M; row += gridDim.x, buf ^= 1) {
+        const int64_t at = row * K - off;
+        const float rstd = p.rstd[row];
+        auto value = [&](int v, float (&g)[8], float (&n)[8]) {
+            dsq_unpack8(load_vec<T, ALIGNED>(gy, at + 8 * v, p.total), g);
+            dsq_unpack8(load_vec<T, ALIGNED>(hh, at + 8 * v, p.total), n);
+            mask<ALIGNED>(g, 8 * v - off, K);
+            mask<ALIGNED>(n, 8 * v - off, K);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) n[k] *= rstd;
+        };
+        float sum = 0.f, g[8], n[8], w[8];
+        uint32_t none = 0;
+        for (int v = threadIdx.x; v < nv; v += 1024) {
+            value(v, g, n);
+            load_weight<ALIGNED>(p.w, 8 * v - off, K, true, w);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int c = 8 * v - off + k;
+                if (ALIGNED || (unsigned)c < (unsigned)K) gw[c] = __fmaf_rn(g[k], n[k], gw[c]);
+                sum = __fmaf_rn(g[k] * w[k], n[k], sum);
+            }
+        }
+        reduce_row<1024>(sum, none, red[buf]);
+        const float c = sum * p.inv_k;
+        for (int v = threadIdx.x; v < nv; v += 1024) {
+            value(v, g, n);
+            load_weight<ALIGNED>(p.w, 8 * v - off, K, true, w);
+            float a[8], o[8];
+            if (gh) dsq_unpack8(load_vec<T, ALIGNED>(gh, at + 8 * v, p.total), a);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                o[k] = rstd * __fmaf_rn(-n[k], c, g[k] * w[k]);
+                if (gh) o[k] += a[k];
+            }
+            store_vec<T, ALIGNED>((T *)p.gx, at + 8 * v, 8 * v - off, K, o);
+        }
+    }
+    if (!p.part) return;
+    __syncthreads();
+    for (int c = threadIdx.x; c < K; c += 1024) p.part[(int64_t)blockIdx.x * K + c] = gw[c];
+}
+
+// grad_w[k] = sum over the blocks of their sums, in one order
+constexpr int SUM_ROWS = 16;
+__global__ void __launch_bounds__(32 * SUM_ROWS) weight_sum_kernel(const float *part, int rows, int K, float *out)
+{
+    __shared__ float s[SUM_ROWS][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
+    const int col = blockIdx.x * 32 + x;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    float a = 0.f;
+    if (col < K)
+#pragma unroll 4
+        for (int r = y; r < rows; r += SUM_ROWS) a += part[(int64_t)r * K + col];
+    s[y][x] = a;
+    __syncthreads();
+    if (y == 0 && col < K) {
+        a = 0.f;
+#pragma unroll
+        for (int r = 0; r < SUM_ROWS; ++r) a += s[r][x];
+        out[col] = a;
+    }
+}
+
+// threads a row: of K elements (a row that shifts may touch one vector more).  0: too long for registers
+struct Form { int tpr, items; };
+Form fwd_form(int64_t K)
+{
+    const int64_t nv = K % 8 ? K / 8 + 2 : K / 8;
+    if (nv <= 32) return {32, 1};
+    if (nv <= 64) return {32, 2};
+    if (nv <= 128) return {32, 4};
+    if (nv <= 256) return {128, 2};
+    if (nv <= 512) return {256, 2};
+    if (nv <= 1024) return {512, 2};
+    return {0, 0};
+}
+Form bwd_form(int64_t K)
+{
+    const int64_t nv = K % 8 ? K / 8 + 2 : K / 8;
+    if (nv <= 32) return {32, 1};
+    if (nv <= 64) return {32, 2};
+    if (nv <= 128) return {128, 1};
+    if (nv <= 256) return {256, 1};
+    if (nv <= 512) return {512, 1};
+    if (nv <= 1024) return {1024, 1};
+    return {0, 0};
+}
+
+// blocks: what is resident together; a multiple of eight rows where rows shift
+int grid_of(int64_t M, int64_t K, int tpr, int threads_per_sm)
+{
+    const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    const int block = tpr ? block_of(tpr) : 1024, rpb = tpr ? block / tpr : 1;
+    int64_t g = (M + rpb - 1) / rpb;
+    const int64_t most = (int64_t)sms * (threads_per_sm / block > 0 ? threads_per_sm / block : 1);
+    if (g > most) g = most;
+    if (K % 8 && rpb < 8) {
+        const int64_t unit = 8 / rpb;
+        g = (g + unit - 1) / unit * unit;
+    }
+    return (int)g;
+}
+
+template <class T, bool ALIGNED> int fwd_launch(const FwdParams &p, cudaStream_t s)
+{
+    const Form f = fwd_form(p.K);
+    const int pdl = dsq_launch_hooks().pdl;
+    const dim3 grid(grid_of(p.M, p.K, f.tpr, 1024));
+#define FWD(TPR, ITEMS) \
+    if (f.tpr == TPR && f.items == ITEMS) \
+        return dsq_launch(rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
+    FWD(32, 1) FWD(32, 2) FWD(32, 4) FWD(128, 2) FWD(256, 2) FWD(512, 2)
+#undef FWD
+    return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED>, grid, dim3(1024), 0, s, pdl, 0, p);
+}
+
+int bwd_grid(int64_t M, int64_t K) { return grid_of(M, K, bwd_form(K).tpr, 1024); }
+
+template <class T, bool ALIGNED> int bwd_launch(const BwdParams &p, cudaStream_t s)
+{
+    const Form f = bwd_form(p.K);
+    const int pdl = dsq_launch_hooks().pdl;
+    const dim3 grid(bwd_grid(p.M, p.K));
+#define BWD(TPR, ITEMS) \
+    if (f.tpr == TPR && f.items == ITEMS) \
+        return dsq_launch(rmsnorm_bwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
+    BWD(32, 1) BWD(32, 2) BWD(128, 1) BWD(256, 1) BWD(512, 1) BWD(1024, 1)
+#undef BWD
+    static std::atomic<unsigned long long> configured{0};
+    const int st = dsq_allow_smem((const void *)rmsnorm_bwd_long_kernel<T, ALIGNED>, (int)(MAX_K * 4), &configured);
+    if (st) return st;
+    return dsq_launch(rmsnorm_bwd_long_kernel<T, ALIGNED>, grid, dim3(1024), (size_t)p.K * 4, s, pdl, 0, p);
+}
+
+int check_shape(int64_t M, int64_t K, int dtype)
+{
+    if (!dsq_is_float_type(dtype)) return DSQ_ERR_UNSUPPORTED;
+    if (M <= 0 || K <= 0) return DSQ_ERR_SHAPE;
+    if (K > MAX_K || M > (int64_t)1 << 40) return DSQ_ERR_SIZE;
+    return DSQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dsq_rmsnorm_fwd(const void *x, const void *residual, const float *weight, int64_t M, int64_t K,
+                    int dtype, float eps, void *h_out, void *y_out, int8_t *codes_out,
+                    float *scale_out, float *rstd_out, void *stream)
+{
+    if (!x || !weight || (!y_out && !codes_out) || (codes_out && !scale_out)) return DSQ_ERR_NULL;
+    const int st = check_shape(M, K, dtype);
+    if (st) return st;
+    if (!dsq_finite(eps) || eps < 0.f) return DSQ_ERR_RANGE;
+    const void *all[] = {x, residual, weight, h_out, y_out, codes_out, scale_out, rstd_out};
+    for (const void *a : all)
+        if (!dsq_aligned16(a)) return DSQ_ERR_ALIGN;
+    FwdParams p;
+    p.x = x; p.res = residual; p.w = weight;
+    p.h = h_out; p.y = y_out; p.codes = codes_out; p.scale = scale_out; p.rstd = rstd_out;
+    p.M = M; p.total = M * K; p.K = (int)K;
+    p.eps = eps; p.inv_k = (float)(1.0 / (double)K);
+    cudaStream_t s = (cudaStream_t)stream;
+    const bool al = K % 8 == 0;
+    switch (dtype) {
+    case DSQ_F32: return al ? fwd_launch<float, true>(p, s) : fwd_launch<float, false>(p, s);
+    case DSQ_BF16: return al ? fwd_launch<__nv_bfloat16, true>(p, s) : fwd_launch<__nv_bfloat16, false>(p, s);
+    default: return al ? fwd_launch<__half, true>(p, s) : fwd_launch<__half, false>(p, s);
+    }
+}
+
+size_t dsq_rmsnorm_bwd_workspace_bytes(int64_t M, int64_t K)
+{
+    if (M <= 0 || K <= 0 || K > MAX_K) return DSQ_WS_BYTES;
+    return DSQ_WS_BYTES + (size_t)bwd_grid(M, K) * (size_t)K * 4;
+}
+
+int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h, const float *weight,
+                    const float *rstd, int64_t M, int64_t K, int dtype, void *grad_x,
+                    float *grad_weight, void *workspace, size_t ws_bytes, void *stream)
+{
+    if (!grad_y || !h || !weight || !rstd || !grad_x || (grad_weight && !workspace)) return DSQ_ERR_NULL;
+    int st = check_shape(M, K, dtype);
+    if (st) return st;
+    const void *all[] = {grad_y, grad_h, h, weight, rstd, grad_x, grad_weight, workspace};
+    for (const void *a : all)
+        if (!dsq_aligned16(a)) return DSQ_ERR_ALIGN;
+    if (grad_weight && ws_bytes < dsq_rmsnorm_bwd_workspace_bytes(M, K)) return DSQ_ERR_SIZE;
+    BwdParams p;
+    p.gy = grad_y; p.gh = grad_h; p.h = h; p.w = weight; p.rstd = rstd; p.gx = grad_x;
+    p.part = grad_weight ? (float *)((char *)workspace + DSQ_WS_BYTES) : nullptr;
+    p.M = M; p.total = M * K; p.K = (int)K;
+    p.inv_k = (float)(1.0 / (double)K);
+    cudaStream_t s = (cudaStream_t)stream;
+    const bool al = K % 8 == 0;
+    switch (dtype) {
+    case DSQ_F32: st = al ? bwd_launch<float, true>(p, s) : bwd_launch<float, false>(p, s); break;
+    case DSQ_BF16: st = al ? bwd_launch<__nv_bfloat16, true>(p, s) : bwd_launch<__nv_bfloat16, false>(p, s); break;
+    default: st = al ? bwd_launch<__half, true>(p, s) : bwd_launch<__half, false>(p, s); break;
+    }
+    if (st || !grad_weight) return st;
+    return dsq_launch(weight_sum_kernel, dim3((unsigned)((K + 31) / 32)), dim3(32 * SUM_ROWS), 0, s,
+                      dsq_launch_hooks().pdl, 0, p.part, bwd_grid(M, K), (int)K, grad_weight);
+}
+
+}  // extern "C"
