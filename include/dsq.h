@@ -66,6 +66,14 @@ typedef enum dsq_status {
     DSQ_ERR_TIMEOUT = -10     /* a bounded device-side wait ran out           */
 } dsq_status;
 
+/* Storage types, where an entry point takes more than one. */
+typedef enum dsq_dtype {
+    DSQ_F32 = 0,
+    DSQ_BF16 = 1,
+    DSQ_F16 = 2,
+    DSQ_I8 = 3
+} dsq_dtype;
+
 /* Quantiser parameters (b, l, u) of one tensor. */
 typedef struct dsq_quant_t {
     int32_t bits;
@@ -297,6 +305,99 @@ int dsq_wgemm_bf16(const void *X_bf16, const void *W_codes, int64_t M, int64_t N
                    int64_t K, int bits, float w_offset, const float *col_scale,
                    const float *col_bias, float *Y_f32, void *workspace,
                    size_t ws_bytes, void *stream);
+
+/* ---- weights with a scale per group -------------------------------------- */
+
+/* Groups of `group` consecutive weights of a row of K: ceil(K / group); 0 on
+ * invalid arguments.  The last group of a row may be a short one. */
+int64_t dsq_group_count(int64_t K, int64_t group);
+
+/* Algorithm 1 steps 1, 3 on weights [N][K] with the clip range [-a, a] of each
+ * group of `group` consecutive weights of a row, a their largest magnitude:
+ *   q = floor((w + a) / Delta + 1/2),  Delta = 2 a / (2^bits - 1),  c = q - 2^(bits-1)
+ * (a weight on the midpoint between two levels takes the upper code; the codes are
+ * exact, whatever the rounding of Delta).  w stands for scale (2 c + 1), scale = Delta / 2.
+ *   w          [N][K] row-major of `dtype` (DSQ_F32, DSQ_BF16, DSQ_F16)
+ *   bits       4 (1 to 3: DSQ_ERR_UNSUPPORTED)
+ *   group      a multiple of 32 (others: DSQ_ERR_UNSUPPORTED); K or more: one scale a row
+ *   codes_out  packed rows [N][K] of signed codes: dsq_packed_bytes(N, K, bits) bytes
+ *   scales_out fp32 [dsq_group_count(K, group)][N]
+ * A group of zeros gets scale 0 and codes 0.  A group with a NaN or an infinity gets the
+ * scale NaN (what is computed from it is NaN).  K at most 2^20, N at most 2^28
+ * (DSQ_ERR_SIZE).  HBM-bound. */
+int dsq_quantize_groups(const void *w, int64_t N, int64_t K, int dtype, int bits,
+                        int64_t group, void *codes_out, size_t bytes,
+                        float *scales_out, void *stream);
+
+/* Algorithm 1 step 4 on such codes: values_out[n][k] = scale (2 c + 1) with
+ * w_offset = 0.5, scale c with w_offset = 0 (others: DSQ_ERR_UNSUPPORTED), formed in
+ * binary32 and rounded once to `dtype`.  Arguments as above. */
+int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N,
+                          int64_t K, int bits, int64_t group, float w_offset,
+                          int dtype, void *values_out, void *stream);
+
+/* Weight-only product with a scale per group, made for few rows (the linear layers of
+ * a decoder while it serves: one row a request):
+ *   Y[m][n] = row_scale[m] sum_g scale[g][n] sum_{k in g} X[m][k] v[n][k] + bias[n]
+ * with v = 2 c + 1 when w_offset = 0.5 and v = c when w_offset = 0 (others:
+ * DSQ_ERR_UNSUPPORTED).
+ *   X         [M][K] row-major of x_type: DSQ_BF16 or DSQ_F16 (K a multiple of 8), or DSQ_I8
+ *             (K a multiple of 16): rows start on 16-byte boundaries, DSQ_ERR_ALIGN otherwise
+ *   row_scale fp32 [M] with DSQ_I8 (as dsq_rmsnorm_fwd leaves codes and scales), NULL otherwise
+ *   W_codes, scales, bits, group  as dsq_quantize_groups leaves them
+ *   bias      fp32 [N] or NULL
+ *   Y         [M][N] of y_type: DSQ_F32, DSQ_BF16 or DSQ_F16
+ * Any M (up to 64 rows a pass over the weights).  Products are exact; a group's are added by
+ * the tensor core in binary32 (int32 for DSQ_I8: exact, for groups of up to 2^16 weights,
+ * DSQ_ERR_OVERFLOW beyond), groups in binary32 in a fixed order: the same call gives the same
+ * bits.  Y is rounded once.  No workspace. */
+int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,
+                    const void *W_codes, const float *scales, const float *bias,
+                    int64_t M, int64_t N, int64_t K, int bits, int64_t group,
+                    float w_offset, int y_type, void *Y, void *stream);
+
+/* ---- root-mean-square norm ------------------------------------------------ */
+
+/* The norm in front of a quantised linear layer, on rows [M][K]:
+ *   h = x + residual,  rstd = 1 / sqrt(mean_k(h^2) + eps),  y = h rstd weight
+ * and, where scale_out is given, its 8-bit form (Algorithm 1 steps 1, 3, 4 with the range
+ * of each row, 127 steps to its largest magnitude, midpoints upwards):
+ *   scale = max_k |y| / 127,  q = floor(y / scale + 1/2),  y = scale q
+ *   x         [M][K] of `dtype` (DSQ_F32, DSQ_BF16, DSQ_F16)
+ *   residual  like x, or NULL
+ *   weight    fp32 [K]
+ *   h_out     like x, or NULL; may be the buffer of x or of residual
+ *   y_out     like x, or NULL where codes_out is given
+ *   codes_out int8 [M][K] (dense rows), or NULL; needs scale_out
+ *   scale_out fp32 [M], or NULL: no 8-bit form
+ *   rstd_out  fp32 [M], or NULL (dsq_rmsnorm_bwd reads it)
+ * Arithmetic is binary32, outputs are rounded once; h is normalised as it is before its
+ * rounding.  A row with a NaN or an infinity in h weight has scale NaN and codes 0; one whose
+ * |h weight| are all below 2^-119 scale 0 and codes 0.  eps < 0 or not finite:
+ * DSQ_ERR_RANGE.  K at most 49152 (DSQ_ERR_SIZE).  HBM-bound. */
+int dsq_rmsnorm_fwd(const void *x, const void *residual, const float *weight,
+                    int64_t M, int64_t K, int dtype, float eps, void *h_out,
+                    void *y_out, int8_t *codes_out, float *scale_out,
+                    float *rstd_out, void *stream);
+
+/* Back-propagation through it, with g = grad_y weight and n = h rstd:
+ *   grad_x = rstd (g - n mean_k(g n)) + grad_h   (x's gradient, and residual's)
+ *   grad_weight = sum_m grad_y n
+ * The 8-bit form passes gradients straight through (its steps never clip).
+ *   grad_y    [M][K] of `dtype`; grad_h like it or NULL: what reaches h by the residual stream
+ *   h, rstd   as dsq_rmsnorm_fwd leaves them (h: x itself where there is no residual)
+ *   grad_x    like grad_y; may be the buffer of grad_y or of grad_h
+ *   grad_weight  fp32 [K], or NULL
+ *   workspace dsq_rmsnorm_bwd_workspace_bytes(M, K) bytes (DSQ_ERR_SIZE otherwise); not needed
+ *             without grad_weight.  Behind its first dsq_workspace_bytes() bytes it is scratch:
+ *             calls that may overlap on the GPU must not share it.
+ * The sums over rows are binary32, in a fixed order: the same call gives the same bits on the
+ * same GPU.  HBM-bound. */
+size_t dsq_rmsnorm_bwd_workspace_bytes(int64_t M, int64_t K);
+int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h,
+                    const float *weight, const float *rstd, int64_t M, int64_t K,
+                    int dtype, void *grad_x, float *grad_weight, void *workspace,
+                    size_t ws_bytes, void *stream);
 
 /* dsq_gemm for callers that cannot allocate device memory.  (The paper has
  * no counterpart: this is a deployment convenience of the library.)

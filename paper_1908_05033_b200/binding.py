@@ -6,7 +6,7 @@ Two layers, both marshalling only:
   * functions of the same names taking torch CUDA tensors: they check dtypes,
     allocate the output tensors with torch, pass data pointers and the current
     CUDA stream, and raise DsqError on a non-zero status.  Those on the path of
-    a pass (quantise, convolutions, pool, GEMMs, soft quantiser) do that in
+    a pass (quantise, convolutions, pool, GEMMs, soft quantiser, norm) do that in
     native code (_dsq_host.so, csrc/dsq_host.cpp).
 """
 import ctypes as C
@@ -89,6 +89,15 @@ _SIGNATURES = {
     "dsq_wgemm_workspace_bytes": (_sz, [_i64, _i64]),
     "dsq_wgemm_bf16": (_int, [_vp, _vp, _i64, _i64, _i64, _int, C.c_float, _vp, _vp, _vp, _vp,
                               _sz, _vp]),
+    "dsq_group_count": (_i64, [_i64, _i64]),
+    "dsq_quantize_groups": (_int, [_vp, _i64, _i64, _int, _int, _i64, _vp, _sz, _vp, _vp]),
+    "dsq_dequantize_groups": (_int, [_vp, _vp, _i64, _i64, _int, _i64, C.c_float, _int, _vp, _vp]),
+    "dsq_wgemm_group": (_int, [_vp, _int, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _int, _i64,
+                               C.c_float, _int, _vp, _vp]),
+    "dsq_rmsnorm_fwd": (_int, [_vp, _vp, _vp, _i64, _i64, _int, C.c_float, _vp, _vp, _vp, _vp, _vp,
+                               _vp]),
+    "dsq_rmsnorm_bwd_workspace_bytes": (_sz, [_i64, _i64]),
+    "dsq_rmsnorm_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _int, _vp, _vp, _vp, _sz, _vp]),
     "dsq_gemm_static_ws": (_int, [_vp, _vp, _i64, _i64, _i64, _int, _vp, _vp, _vp,
                                   _int, _vp]),
     "dsq_maxpool2x2": (_int, [_vp, C.POINTER(dsq_nhwc_t), _int, _vp, _sz,
@@ -327,6 +336,56 @@ def dsq_wgemm_bf16(X, W, M, N, K, bits, col_scale, col_bias=None, w_offset=0.5, 
         _need(X, torch.bfloat16, "X")
         ws = _sized_workspace(int(lib.dsq_wgemm_workspace_bytes(N, K)), X.device)
     return _host.wgemm(X, W, M, N, K, bits, w_offset, col_scale, col_bias, ws, out)
+
+
+# ---- weights with a scale per group, and the norm in front of them ------------------
+_DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}     # dsq_dtype
+
+
+def dsq_group_count(K, group):
+    return int(lib.dsq_group_count(K, group))
+
+
+def dsq_quantize_groups(w, bits=4, group=128):
+    """w: fp32, bf16 or fp16 [N, K] -> (packed signed codes uint8 [N, pitch], scales fp32
+    [groups, N]); a code c stands for scale * (2 c + 1)."""
+    return _host.quantize_groups(w, bits, group)
+
+
+def dsq_dequantize_groups(codes, scales, N, K, bits=4, group=128, w_offset=0.5,
+                          out_dtype=torch.bfloat16):
+    """The values [N, K] that packed codes with group scales stand for."""
+    return _host.dequantize_groups(codes, scales, N, K, bits, group, w_offset,
+                                   _DTYPES.get(out_dtype, -1))
+
+
+def dsq_wgemm_group(X, W, M, N, K, bits, group, scales, bias=None, row_scale=None, w_offset=0.5,
+                    out_dtype=torch.float32, out=None):
+    """X: bf16 or fp16 [M, K], or int8 [M, K] with row_scale fp32 [M]; W: packed signed codes
+    [N, pitch]; scales fp32 [groups, N].  Returns Y [M, N] of out_dtype (of `out` where given)."""
+    if out is not None:
+        out_dtype = out.dtype
+    return _host.wgemm_group(X, W, M, N, K, bits, group, scales, bias, row_scale, w_offset,
+                             _DTYPES.get(out_dtype, -1), out)
+
+
+def dsq_rmsnorm_fwd(x, weight, eps, residual=None, quantised=False, want_y=True, want_codes=False,
+                    want_rstd=False, out_h=None):
+    """Rows of the last dimension: h = x + residual, y = h / sqrt(mean(h^2) + eps) * weight.
+    quantised: y is what its 8-bit codes stand for.  Returns (h | None, y | None, codes int8 |
+    None, scale fp32 | None, rstd fp32 | None); h where there is a residual or an out_h (which
+    may be x or residual itself)."""
+    return _host.rmsnorm_fwd(x, weight, eps, residual, quantised, want_y, want_codes, want_rstd,
+                             out_h)
+
+
+def dsq_rmsnorm_bwd_workspace_bytes(M, K):
+    return int(lib.dsq_rmsnorm_bwd_workspace_bytes(M, K))
+
+
+def dsq_rmsnorm_bwd(grad_y, h, weight, rstd, grad_h=None, want_weight=True, ws=None):
+    """Returns (grad_x like grad_y, grad_weight fp32 [K] | None)."""
+    return _host.rmsnorm_bwd(grad_y, h, weight, rstd, grad_h, want_weight, ws)
 
 
 def dsq_set_round_k_steps(ks):

@@ -10,6 +10,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAGuard.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -52,6 +53,7 @@ const char *dtype_name(at::ScalarType t)
     case at::kChar: return "torch.int8";
     case at::kFloat: return "torch.float32";
     case at::kBFloat16: return "torch.bfloat16";
+    case at::kHalf: return "torch.float16";
     default: return "another type";
     }
 }
@@ -395,6 +397,237 @@ PyObject *wgemm(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// ---- operators around a low-bit linear layer of a decoder ----------------------
+// They run on the device of their first tensor, whatever the current one, on that device's
+// current stream; the other tensors have to be there too.
+struct OnDevice {
+    c10::Device device;
+    c10::cuda::CUDAGuard guard;
+    explicit OnDevice(const at::Tensor &t) : device(t.device()), guard(t.device()) {}
+    const at::Tensor &operator()(const at::Tensor &t, const char *name) const
+    {
+        if (t.device() != device) {
+            PyErr_Format(PyExc_ValueError, "%s: on another device", name);
+            throw PyFailed();
+        }
+        return t;
+    }
+};
+
+int type_code(at::ScalarType t)
+{
+    switch (t) {
+    case at::kFloat: return DSQ_F32;
+    case at::kBFloat16: return DSQ_BF16;
+    case at::kHalf: return DSQ_F16;
+    case at::kChar: return DSQ_I8;
+    default: return -1;
+    }
+}
+
+// a contiguous CUDA tensor of a floating type
+const at::Tensor &need_float(PyObject *o, const char *name)
+{
+    static const char *const types = "torch.float32, torch.bfloat16 or torch.float16";
+    if (!THPVariable_Check(o)) fail_type(name, types);
+    const at::Tensor &v = THPVariable_Unpack(o);
+    const int t = type_code(v.scalar_type());
+    if (!v.is_cuda() || !v.is_contiguous() || t < 0 || t == DSQ_I8) fail_type(name, types);
+    return v;
+}
+
+at::ScalarType as_type(PyObject *o)
+{
+    const int64_t code = as_int(o);
+    if (code == DSQ_F32) return at::kFloat;
+    if (code == DSQ_BF16) return at::kBFloat16;
+    if (code == DSQ_F16) return at::kHalf;
+    PyErr_SetString(PyExc_TypeError, "out_dtype: want torch.float32, torch.bfloat16 or torch.float16");
+    throw PyFailed();
+}
+
+void want(bool ok, const char *what)
+{
+    if (ok) return;
+    PyErr_SetString(PyExc_ValueError, what);
+    throw PyFailed();
+}
+
+// a tensor like `x`, or None
+const at::Tensor *like_or_none(PyObject *o, const at::Tensor &x, const OnDevice &on, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &t = on(need(o, x.scalar_type(), name), name);
+    want(t.sizes() == x.sizes(), "want tensors of one shape");
+    return &t;
+}
+
+// rows of the last dimension
+void rows_of(const at::Tensor &x, int64_t *M, int64_t *K)
+{
+    want(x.dim() >= 1, "want at least one dimension");
+    *K = x.size(x.dim() - 1);
+    *M = *K ? x.numel() / *K : 0;
+}
+
+void *addr(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+
+// (x, weight, eps, residual | None, quantised, want_y, want_codes, want_rstd, out_h | None)
+// -> (h | None, y | None, codes | None, scale | None, rstd | None)
+PyObject *rmsnorm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 9, [&]() -> PyObject * {
+        const at::Tensor &x = need_float(a[0], "x");
+        const OnDevice on(x);
+        const at::Tensor &w = on(need(a[1], at::kFloat, "weight"), "weight");
+        const float eps = as_float(a[2]);
+        const at::Tensor *res = like_or_none(a[3], x, on, "residual");
+        const bool want_codes = as_bool(a[6]), quantised = as_bool(a[4]) || want_codes;
+        int64_t M, K;
+        rows_of(x, &M, &K);
+        want(w.numel() == K, "weight: want one value a column");
+        at::Tensor h, y, codes, scale, rstd;
+        if (a[8] != Py_None) h = *like_or_none(a[8], x, on, "out_h");
+        else if (res) h = new_tensor(x.sizes(), x.scalar_type(), x);
+        if (as_bool(a[5])) y = new_tensor(x.sizes(), x.scalar_type(), x);
+        if (want_codes) codes = new_tensor(x.sizes(), at::kChar, x);
+        const auto rows = x.sizes().slice(0, x.dim() - 1);
+        if (quantised) scale = new_tensor(rows, at::kFloat, x);
+        if (as_bool(a[7])) rstd = new_tensor(rows, at::kFloat, x);
+        check(enqueue([&](void *s) {
+                  return dsq_rmsnorm_fwd(x.data_ptr(), addr(res), (const float *)w.data_ptr(), M, K,
+                                         type_code(x.scalar_type()), eps, addr(h), addr(y),
+                                         (int8_t *)addr(codes), (float *)addr(scale), (float *)addr(rstd), s);
+              }),
+              "dsq_rmsnorm_fwd");
+        return Py_BuildValue("(NNNNN)", a[8] != Py_None ? Py_NewRef(a[8]) : wrap(h), wrap(y), wrap(codes),
+                             wrap(scale), wrap(rstd));
+    });
+}
+
+// (grad_y, h, weight, rstd, grad_h | None, want_weight, ws | None) -> (grad_x, grad_weight | None)
+PyObject *rmsnorm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 7, [&]() -> PyObject * {
+        const at::Tensor &gy = need_float(a[0], "grad_y");
+        const OnDevice on(gy);
+        const at::Tensor *h = like_or_none(a[1], gy, on, "h");
+        if (!h) fail_type("h", dtype_name(gy.scalar_type()));
+        const at::Tensor &w = on(need(a[2], at::kFloat, "weight"), "weight");
+        const at::Tensor &rstd = on(need(a[3], at::kFloat, "rstd"), "rstd");
+        const at::Tensor *gh = like_or_none(a[4], gy, on, "grad_h");
+        int64_t M, K;
+        rows_of(gy, &M, &K);
+        want(w.numel() == K, "weight: want one value a column");
+        want(rstd.numel() == M, "rstd: want one value a row");
+        at::Tensor gx = new_tensor(gy.sizes(), gy.scalar_type(), gy), gw, ws;
+        if (as_bool(a[5])) {
+            gw = new_tensor(w.sizes(), at::kFloat, gy);
+            if (a[6] != Py_None) ws = on(need(a[6], at::kByte, "ws"), "ws");
+            else ws = new_tensor({(int64_t)dsq_rmsnorm_bwd_workspace_bytes(M, K)}, at::kByte, gy);
+        }
+        check(enqueue([&](void *s) {
+                  return dsq_rmsnorm_bwd(gy.data_ptr(), addr(gh), h->data_ptr(), (const float *)w.data_ptr(),
+                                         (const float *)rstd.data_ptr(), M, K, type_code(gy.scalar_type()),
+                                         gx.data_ptr(), (float *)addr(gw), addr(ws),
+                                         ws.defined() ? (size_t)ws.numel() : 0, s);
+              }),
+              "dsq_rmsnorm_bwd");
+        return Py_BuildValue("(NN)", wrap(gx), wrap(gw));
+    });
+}
+
+// (w, bits, group) -> (codes, scales)
+PyObject *quantize_groups(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&]() -> PyObject * {
+        const at::Tensor &w = need_float(a[0], "w");
+        const OnDevice on(w);
+        const int bits = (int)as_int(a[1]);
+        const int64_t group = as_int(a[2]);
+        want(w.dim() == 2, "w: want [N, K]");
+        const int64_t N = w.size(0), K = w.size(1);
+        at::Tensor codes = new_tensor({N, (int64_t)dsq_row_pitch(K, bits)}, at::kByte, w);
+        at::Tensor scales = new_tensor({dsq_group_count(K, group), N}, at::kFloat, w);
+        check(enqueue([&](void *s) {
+                  return dsq_quantize_groups(w.data_ptr(), N, K, type_code(w.scalar_type()), bits, group,
+                                             codes.data_ptr(), (size_t)codes.numel(), (float *)scales.data_ptr(),
+                                             s);
+              }),
+              "dsq_quantize_groups");
+        return Py_BuildValue("(NN)", wrap(codes), wrap(scales));
+    });
+}
+
+// sizes of codes and scales (sizes that the library refuses are left to it)
+void check_codes(const at::Tensor &codes, const at::Tensor &scales, int64_t N, int64_t K, int bits, int64_t group)
+{
+    if (N <= 0 || K <= 0 || group <= 0) return;
+    want(codes.numel() / N >= (int64_t)dsq_row_pitch(K, bits), "codes: too few bytes");
+    want(scales.numel() / N >= dsq_group_count(K, group), "scales: too few values");
+}
+
+// (codes, scales, N, K, bits, group, w_offset, out type) -> values
+PyObject *dequantize_groups(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 8, [&]() -> PyObject * {
+        const at::Tensor &codes = need(a[0], at::kByte, "codes");
+        const OnDevice on(codes);
+        const at::Tensor &scales = on(need(a[1], at::kFloat, "scales"), "scales");
+        const int64_t N = as_int(a[2]), K = as_int(a[3]), group = as_int(a[5]);
+        const int bits = (int)as_int(a[4]);
+        const float w_offset = as_float(a[6]);
+        const at::ScalarType t = as_type(a[7]);
+        check_codes(codes, scales, N, K, bits, group);
+        want(N >= 0 && K >= 0, "want [N, K]");
+        at::Tensor out = new_tensor({N, K}, t, codes);
+        check(enqueue([&](void *s) {
+                  return dsq_dequantize_groups(codes.data_ptr(), (const float *)scales.data_ptr(), N, K, bits,
+                                               group, w_offset, type_code(t), out.data_ptr(), s);
+              }),
+              "dsq_dequantize_groups");
+        return wrap(out);
+    });
+}
+
+// (X, W, M, N, K, bits, group, scales, bias | None, row_scale | None, w_offset, out type, out | None) -> Y
+PyObject *wgemm_group(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 13, [&]() -> PyObject * {
+        static const char *const types = "torch.bfloat16, torch.float16 or torch.int8";
+        if (!THPVariable_Check(a[0])) fail_type("X", types);
+        const at::Tensor &X = THPVariable_Unpack(a[0]);
+        const int xt = type_code(X.scalar_type());
+        if (!X.is_cuda() || !X.is_contiguous() || xt < 0 || xt == DSQ_F32) fail_type("X", types);
+        const OnDevice on(X);
+        const at::Tensor &W = on(need(a[1], at::kByte, "W"), "W");
+        const int64_t M = as_int(a[2]), N = as_int(a[3]), K = as_int(a[4]), group = as_int(a[6]);
+        const int bits = (int)as_int(a[5]);
+        const at::Tensor &scales = on(need(a[7], at::kFloat, "scales"), "scales");
+        const at::Tensor *bias = nullptr, *rs = nullptr;
+        if (a[8] != Py_None) bias = &on(need(a[8], at::kFloat, "bias"), "bias");
+        if (a[9] != Py_None) rs = &on(need(a[9], at::kFloat, "row_scale"), "row_scale");
+        const float w_offset = as_float(a[10]);
+        const at::ScalarType t = as_type(a[11]);
+        check_codes(W, scales, N, K, bits, group);
+        want(M >= 0 && N >= 0, "want [M, N]");
+        want(K <= 0 || X.numel() / K >= M, "X: too few values");
+        want(!bias || bias->numel() >= N, "bias: too few values");
+        want(!rs || rs->numel() >= M, "row_scale: too few values");
+        at::Tensor store;
+        const at::Tensor &Y = a[12] != Py_None ? on(need(a[12], t, "out"), "out") : (store = new_tensor({M, N}, t, X));
+        want(N <= 0 || Y.numel() / N >= M, "out: too few values");
+        check(enqueue([&](void *s) {
+                  return dsq_wgemm_group(X.data_ptr(), xt, (const float *)addr(rs), W.data_ptr(),
+                                         (const float *)scales.data_ptr(), (const float *)addr(bias), M, N, K,
+                                         bits, group, w_offset, type_code(t), Y.data_ptr(), s);
+              }),
+              "dsq_wgemm_group");
+        if (a[12] != Py_None) return Py_NewRef(a[12]);
+        return wrap(Y);
+    });
+}
+
 // ---- recorded call sequences (dsq_plan.h) -----------------------------------
 // What a plan was recorded from: everything a caller could exchange or change in
 // place between two passes (tensors, ranges, layers).  A plan runs only while all
@@ -569,7 +802,9 @@ PyObject *plan_run(PyObject *, PyObject *const *a, Py_ssize_t n)
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef g_methods[] = {{"set_error_class", set_error_class, METH_O, nullptr},
                            FAST(quantize_act), FAST(conv2d), FAST(maxpool2x2), FAST(soft_fwd),
-                           FAST(soft_bwd), FAST(gemm), FAST(wgemm), FAST(plan_record),
+                           FAST(soft_bwd), FAST(gemm), FAST(wgemm), FAST(rmsnorm_fwd),
+                           FAST(rmsnorm_bwd), FAST(quantize_groups), FAST(dequantize_groups),
+                           FAST(wgemm_group), FAST(plan_record),
                            FAST(plan_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dsq_host", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

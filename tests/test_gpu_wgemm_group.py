@@ -1,0 +1,213 @@
+"""GPU: products of few rows with group-wise 4-bit weights against float64.
+
+Tolerances: products are exact; a group's sum in the tensor core's binary32 and the sum over
+groups take at most K additions, each off by 2^-23 of the terms added so far (the core may cut
+instead of rounding): K 2^-23 sum |x v s|, 2^-22 of that for scale, bias and row scale, half a step
+of the type.  In int8 a group's sum is exact: (groups + 5) 2^-24 of the groups' magnitudes."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+from oracle import groups as G
+from gpu_util import T, N
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def dsq():
+    import paper_1908_05033_b200 as d
+    return d
+
+
+def weights(dsq, n, k, group, seed=0):
+    rng = np.random.default_rng(seed + 31 * n + k)
+    codes = rng.integers(-8, 8, (n, k)).astype(np.int8)
+    scales = (rng.uniform(0.5, 1.5, (-(-k // group), n)) * 0.01).astype(np.float32)
+    bias = rng.normal(size=n).astype(np.float32)
+    return codes, scales, bias, dsq.dsq_pack_codes(T(codes), 4)
+
+
+def check(Y, x, codes, scales, group, bias, off, row_scale=None):
+    k = x.shape[1]
+    ref, mag = G.linear(x, codes, scales, group, bias, row_scale, off)
+    f = torch.finfo(Y.dtype)
+    exact = row_scale is not None
+    tol = ((scales.shape[0] + 5) * U if exact else (k + 2) * 2 * U) * mag + 4 * U * np.abs(ref)
+    tol = tol + f.eps / 2 * np.abs(ref) + f.smallest_normal * f.eps
+    assert np.all(np.abs(N(Y.double()) - ref) <= tol)
+    if Y.dtype == torch.float32 and not exact and k > 512:
+        # errors of single additions do not add up: far inside the bound on average
+        assert np.mean(np.abs(N(Y.double()) - ref)) <= 0.05 * np.mean(tol)
+
+
+SIZES = [(1, 1, 8, 32), (1, 33, 64, 32), (2, 40, 96, 96), (5, 17, 136, 64), (8, 100, 200, 128),
+         (9, 31, 1032, 128), (16, 65, 520, 32), (17, 70, 264, 64), (31, 33, 2056, 256), (32, 8, 128, 64),
+         (33, 96, 776, 32), (64, 130, 1288, 128), (65, 45, 392, 96), (130, 24, 640, 128), (1, 3000, 4104, 160),
+         (3, 4750, 640, 64), (4, 1201, 1288, 1 << 40), (7, 64, 8200, 8224)]
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("size", SIZES)
+def test_floating_rows(dsq, size, t):
+    M, n, k, group = size
+    codes, scales, bias, packed = weights(dsq, n, k, min(group, k))
+    rng = np.random.default_rng(M)
+    x = torch.from_numpy(rng.normal(size=(M, k))).to(t)
+    for off, b, out in ((0.5, bias, torch.float32), (0.0, None, torch.float32), (0.5, None, t),
+                        (0.0, bias, torch.float16)):
+        Y = dsq.dsq_wgemm_group(x.cuda(), packed, M, n, k, 4, group, T(scales),
+                                bias=None if b is None else T(b), w_offset=off, out_dtype=out)
+        assert Y.dtype == out and Y.shape == (M, n)
+        check(Y, x.double().numpy(), codes, scales, min(group, k), b, off)
+
+
+@pytest.mark.parametrize("size", [s for s in SIZES if s[2] % 16 == 0] + [(6, 50, 48, 32), (40, 33, 1040, 64)])
+def test_eight_bit_rows(dsq, size):
+    M, n, k, group = size
+    codes, scales, bias, packed = weights(dsq, n, k, min(group, k), 1)
+    rng = np.random.default_rng(M)
+    x = rng.integers(-128, 128, (M, k)).astype(np.int8)
+    rs = rng.uniform(0.01, 0.02, M).astype(np.float32)
+    for off, b, out in ((0.5, bias, torch.float32), (0.0, None, torch.float32), (0.5, bias, torch.bfloat16)):
+        Y = dsq.dsq_wgemm_group(T(x), packed, M, n, k, 4, group, T(scales), row_scale=T(rs),
+                                bias=None if b is None else T(b), w_offset=off, out_dtype=out)
+        check(Y, x, codes, scales, min(group, k), b, off, rs)
+
+
+@pytest.mark.parametrize("M", [1, 8, 16, 24, 64, 70])
+def test_whole_numbers_are_exact(dsq, M):
+    """Small integers and scales that are powers of two: every sum is exact, any order."""
+    n, k, group = 200, 1000, 64
+    codes, _, _, packed = weights(dsq, n, k, group)
+    rng = np.random.default_rng(M)
+    scales = np.ldexp(1.0, rng.integers(-3, 3, (16, n))).astype(np.float32)
+    x = rng.integers(-4, 5, (M, k)).astype(np.float32)
+    for t in (torch.bfloat16, torch.float16):
+        Y = dsq.dsq_wgemm_group(T(x).to(t), packed, M, n, k, 4, group, T(scales))
+        assert np.array_equal(N(Y), G.linear(x, codes, scales, group)[0])
+
+
+def test_extreme_codes_and_largest_magnitudes(dsq):
+    """Codes and 8-bit activations all at their ends: the largest group sums."""
+    n, k = 40, 1 << 16
+    for c, xv in ((7, 127), (-8, -128), (-8, 127)):
+        codes = np.full((n, k), c, np.int8)
+        packed = dsq.dsq_pack_codes(T(codes), 4)
+        x = np.full((2, k), xv, np.int8)
+        ones = np.ones((1, n), np.float32)
+        Y = dsq.dsq_wgemm_group(T(x), packed, 2, n, k, 4, k, T(ones), row_scale=T(np.ones(2, np.float32)))
+        want = float(k * xv * (2 * c + 1))
+        assert np.all(np.abs(N(Y) - want) <= 6 * U * abs(want))
+
+
+def test_nan_and_infinity_stay_in_their_rows_and_columns(dsq):
+    M, n, k, group = 20, 70, 264, 64
+    codes, scales, _, packed = weights(dsq, n, k, group)
+    x = torch.randn(M, k, device="cuda").bfloat16()
+    x[3, k - 1] = float("inf")
+    x[17, 0] = float("nan")
+    scales[2, 5] = np.nan
+    scales[4, 69] = np.inf
+    Y = N(dsq.dsq_wgemm_group(x, packed, M, n, k, 4, group, T(scales)))
+    bad = ~np.isfinite(Y)
+    want = np.zeros((M, n), bool)
+    want[[3, 17]] = True
+    want[:, [5, 69]] = True
+    assert np.array_equal(bad, want)
+
+
+def test_out_and_rows_behind_it(dsq):
+    M, n, k = 9, 77, 200
+    codes, scales, _, packed = weights(dsq, n, k, 32)
+    x = torch.randn(M + 3, k, device="cuda").bfloat16()
+    x[M:] = float("nan")
+    out = torch.full((M + 3, n), 5.0, device="cuda")
+    assert dsq.dsq_wgemm_group(x, packed, M, n, k, 4, 32, T(scales), out=out) is out
+    assert (out[M:] == 5.0).all()
+    check(out[:M].clone(), N(x[:M].double()), codes, scales, 32, None, 0.5)
+
+
+@pytest.mark.parametrize("M", [1, 16, 64])
+def test_a_call_gives_the_same_bits_again(dsq, M):
+    n, k = 500, 2048
+    codes, scales, bias, packed = weights(dsq, n, k, 128)
+    x = torch.randn(M, k, device="cuda").bfloat16()
+    Y = dsq.dsq_wgemm_group(x, packed, M, n, k, 4, 128, T(scales), bias=T(bias))
+    for _ in range(5):
+        assert torch.equal(Y, dsq.dsq_wgemm_group(x, packed, M, n, k, 4, 128, T(scales), bias=T(bias)))
+
+
+def test_binding_refuses_small_buffers(dsq):
+    codes, scales, bias, packed = weights(dsq, 10, 64, 32)
+    x = torch.randn(2, 64, device="cuda").bfloat16()
+    s = T(scales)
+    bad = [dict(M=3), dict(N=11), dict(K=128), dict(group=16), dict(bias=torch.zeros(9, device="cuda")),
+           dict(out=torch.empty(19, device="cuda"))]
+    for b in bad:
+        a = dict(M=2, N=10, K=64, group=32, bias=None, out=None)
+        a.update(b)
+        with pytest.raises((ValueError, dsq.DsqError)):
+            dsq.dsq_wgemm_group(x, packed, a["M"], a["N"], a["K"], 4, a["group"], s, bias=a["bias"], out=a["out"])
+    with pytest.raises(TypeError):
+        dsq.dsq_wgemm_group(x.float(), packed, 2, 10, 64, 4, 32, s)
+    with pytest.raises(TypeError):
+        dsq.dsq_wgemm_group(x, packed, 2, 10, 64, 4, 32, s, out_dtype=torch.int32)
+    with pytest.raises(dsq.DsqError):
+        dsq.dsq_wgemm_group(x.to(torch.int8), packed, 2, 10, 64, 4, 32, s)
+
+
+def test_layer_front_as_it_serves(dsq):
+    """norm -> 8-bit codes -> product, then the next norm on the stream, eager, on another stream and
+    as a replayed graph: the same numbers, and those of the definition."""
+    M, K, n = 5, 512, 384
+    rng = np.random.default_rng(8)
+    x, r = (torch.from_numpy(rng.normal(size=(M, K))).bfloat16().cuda() for _ in range(2))
+    w1 = T((1 + 0.1 * rng.normal(size=K)).astype(np.float32))
+    w2 = T((1 + 0.1 * rng.normal(size=n)).astype(np.float32))
+    W = torch.from_numpy(rng.normal(size=(n, K)) * 0.05).bfloat16().cuda()
+    codes, scales = dsq.dsq_quantize_groups(W, 4, 64)
+    codes2, scales2 = dsq.dsq_quantize_groups(W.t().contiguous(), 4, 128)
+
+    def front(x, r):
+        h, _, q, s, _ = dsq.dsq_rmsnorm_fwd(x, w1, 1e-5, residual=r, want_y=False, want_codes=True)
+        y = dsq.dsq_wgemm_group(q, codes, M, n, K, 4, 64, scales, row_scale=s, out_dtype=torch.bfloat16)
+        _, z, _, _, _ = dsq.dsq_rmsnorm_fwd(y, w2, 1e-5)
+        return h, y, dsq.dsq_wgemm_group(z, codes2, M, K, n, 4, 128, scales2, out_dtype=torch.bfloat16)
+
+    ref = front(x, r)
+    xd, rd = x.double().cpu().numpy(), r.double().cpu().numpy()
+    from oracle import norm
+    _, Yn, _ = norm.forward(xd, N(w1), 1e-5, rd)
+    V, S = norm.eight_bits(Yn)
+    c1, s1 = G.quantize(N(W.double()), 64)
+    y, mag = G.linear(np.floor(V + 0.5), c1, s1, 64, row_scale=S)
+    # a code may fall on the other side of a border: one step of one activation
+    step = np.max(S) * np.abs(G.values(c1, s1, 64)).max()
+    assert np.all(np.abs(N(ref[1].double()) - y) <= 2.0 ** -8 * np.abs(y) + 1e-5 * mag + 2 * step)
+    _, Z, _ = norm.forward(N(ref[1].double()), N(w2), 1e-5)
+    c2, s2 = G.quantize(N(W.t().double()), 128)
+    y2, mag2 = G.linear(Z, c2, s2, 128)
+    assert np.all(np.abs(N(ref[2].double()) - y2) <= 2.0 ** -8 * np.abs(y2) + (2.0 ** -8 + 1e-5) * mag2)
+
+    other = torch.cuda.Stream()
+    other.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(other):
+        got = front(x, r)
+    other.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(ref, got))
+
+    xs, rs = torch.zeros_like(x), torch.zeros_like(r)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        held = front(xs, rs)
+    for _ in range(3):
+        xs.copy_(x)
+        rs.copy_(r)
+        g.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(ref, held))
+        xs.zero_()
+        g.replay()
