@@ -7,12 +7,15 @@
 //
 // The code is exact: weights kept in 16 bits lie on the border between two codes
 // often (w / a a ratio of small integers), and which side a rounded reciprocal puts
-// them on is chance.  The border nearest to the estimate, w = a (2 b - 16) / 15, is
-// compared with w itself: p = a m and its rounding error e (m = 2 b - 16, an even
-// integer of at most 16 in magnitude) hold a m exactly, and fma(15, w, -p) - e has the
-// sign of 15 w - a m.
+// them on is chance.  With j = rint(7.5 w / a) as far as binary32 gives it, the code is j
+// or j - 1 by the sign of 7.5 w - a j: j is the nearest border, or as near as makes no
+// difference.  For weights of 16 bits a j and the fused difference are exact; for binary32
+// ones the rounding error of a j is taken off too.
 //
-// Bound: memory (bf16 in 2.5 bytes a weight, values out 2.5).
+// Bound: memory (bf16 in 2.5 bytes a weight, values out 2.5), with arithmetic close behind: the
+// conversions between integers and floating point run at an eighth of the other operations' rate,
+// so j is read off the sum with 1.5 2^23, and codes become numbers in the mantissa of 2^23.  A
+// thread's column is the same in all its rows, so that nothing is divided per word.
 #include "dsq_groups.h"
 #include "dsq_ptx.cuh"
 #include "dsq_types.cuh"
@@ -28,37 +31,38 @@ struct QuantParams {
     float *scales;            // [groups][N]
     int64_t N;
     int K, pw;                // pw: 32-bit words of a row (8 codes each)
-    int group_words;          // words of a group
-    int row_words;            // words of a row in whole groups
+    int groups, group_words;  // group_words: words of a group
+    int lanes_log;            // 2^lanes_log threads hold a group
+    int bx_log;               // 2^bx_log threads of a block along a row
 };
 
-// What a group's codes are made with: everything scaled by a power of two that brings a
-// to [1, 2) (smaller for the last subnormal bits, up to 4 at the top of the range), so that
-// nothing below over- or underflows.
+// What a group's codes are made with.  Tiny groups are scaled up (exactly), and the comparison
+// with a border is a sixteenth of it, so that nothing over- or underflows.
 struct Range { float f, a, inv, scale; bool bad; };
 __device__ __forceinline__ Range range_of(uint32_t top)
 {
     Range r;
     const float a = __uint_as_float(top);
     r.bad = top >= 0x7F800000u;                               // an infinity or a NaN in the group
-    const int e = min(max((int)(top >> 23) - 127, -126), 126);
-    r.f = __uint_as_float((uint32_t)(127 - e) << 23);
-    r.a = a * r.f;
-    r.inv = r.bad || a == 0.f ? 0.f : __fdiv_rn(7.5f, r.a);
+    r.f = a < 7.8886e-31f ? 1.2676506e30f : 1.f;              // below 2^-100: times 2^100
+    const float x = a * r.f;
+    r.a = x * 0.0625f;
+    r.inv = r.bad || a == 0.f ? 0.f : __fdiv_rn(7.5f, x);
     r.scale = r.bad ? __uint_as_float(0x7FC00000u) : __fdiv_rn(a, 15.f);
     return r;
 }
-// four bits of the signed code (of a group of zeros: 0; of one that is not finite: -8)
-__device__ __forceinline__ uint32_t code_of(float w, const Range &r)
+constexpr float MAGIC = 12582912.f;                           // 1.5 2^23
+constexpr uint32_t MAGIC_BITS = 0x4B400000u;
+// bits of MAGIC + c, c the signed code (the ends of the range need no clip: |7.5 w| <= 7.5 a)
+template <bool WIDE> __device__ __forceinline__ uint32_t code_bits(float w, const Range &r)
 {
-    if (r.bad) return 8u;
     const float x = w * r.f;
-    const float b = rintf(__fmaf_rn(x, r.inv, 8.f));
-    const float m = __fmaf_rn(2.f, b, -16.f);
-    const float p = __fmul_rn(r.a, m), e = __fmaf_rn(r.a, m, -p);
-    const float d = m == 0.f ? w : __fsub_rn(__fmaf_rn(15.f, x, -p), e);
-    const int q = (int)b - (d >= 0.f ? 0 : 1);
-    return (uint32_t)min(max(q, 0), 15) ^ 8u;
+    const float t = __fmaf_rn(x, r.inv, MAGIC);
+    const float nj = __fsub_rn(MAGIC, t);                     // -j (never -0)
+    const float p = __fmul_rn(r.a, nj);
+    float d = __fmaf_rn(0.46875f, x, p);                      // (7.5 x - a j) / 16
+    if (WIDE) d = __fadd_rn(d, __fmaf_rn(r.a, nj, -p));
+    return __float_as_uint(t) + (uint32_t)((int)__float_as_uint(d) >> 31);
 }
 
 // eight weights from column k of a row; those behind the row's end are 0
@@ -84,71 +88,80 @@ __device__ __forceinline__ uint32_t top_of(const float (&f)[8])
     for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(f[i]) & 0x7FFFFFFFu);
     return t;
 }
+// the word of eight codes; those behind the row's end are 0
+template <bool WIDE>
 __device__ __forceinline__ uint32_t word_of(const float (&f)[8], int k, int K, const Range &r)
 {
     uint32_t v = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v |= (k + i < K ? code_of(f[i], r) : 0u) << (4 * i);
+    for (int i = 7; i >= 0; --i) v = v * 16u + code_bits<WIDE>(f[i], r);
+    // every term stands for MAGIC_BITS + c: codes made positive, summed without carries, and
+    // turned into two's complement nibbles
+    constexpr uint32_t ALL = 0x11111111u;
+    v = (v - MAGIC_BITS * ALL + 8u * ALL) ^ 0x88888888u;
+    if (r.bad) v = 0x88888888u;
+    if (k + 8 > K) v = k >= K ? 0u : v & (0xFFFFFFFFu >> (4 * (8 - (K - k))));
     return v;
 }
 
-// Groups of 32, 64, 128 or 256: 4 to 32 neighbouring threads hold one, a word of codes
-// each (a row's last group, cut short, has idle threads: groups start at lanes that are
-// multiples of their size).
-constexpr int UNROLL = 2;
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) quantize_words_kernel(const QuantParams p)
+// 2^lanes_log neighbouring threads hold a group, up to WORDS words of codes each (0: any number,
+// read twice, the second time from the caches); a thread does ROWS rows.
+template <class T, bool VEC, int WORDS, int ROWS>
+__global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p)
 {
+    constexpr bool WIDE = sizeof(T) == 4;
+    const int lanes = 1 << p.lanes_log, tx = threadIdx.x & ((1 << p.bx_log) - 1), ty = threadIdx.x >> p.bx_log;
+    const int slot = (blockIdx.y << p.bx_log) + tx;
+    const int g = slot >> p.lanes_log, l = slot & (lanes - 1);
+    const int w0 = g * p.group_words + l, w1 = min((g + 1) * p.group_words, p.pw);
+    const int by = 256 >> p.bx_log;
+    const int64_t row0 = (int64_t)blockIdx.x * (by * ROWS) + ty;
+    const bool in = g < p.groups;
+    const T *w = (const T *)p.w;
     grid_dependency_wait();
-    const int64_t base = (int64_t)blockIdx.x * (256 * UNROLL);
-    const int64_t row0 = base / p.row_words;
-    const unsigned rest = (unsigned)(base - row0 * p.row_words) + threadIdx.x;
-    float f[UNROLL][8];
-    int64_t row[UNROLL];
-    int word[UNROLL];
+    if constexpr (WORDS > 0) {
+        float f[ROWS][WORDS][8];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const unsigned i = rest + 256 * u, r = i / (unsigned)p.row_words;
-        row[u] = row0 + r;
-        word[u] = (int)(i - r * (unsigned)p.row_words);
-        load_weights<T, VEC>((const T *)p.w, row[u], row[u] < p.N ? 8 * word[u] : p.K, p.K, f[u]);
-    }
+        for (int u = 0; u < ROWS; ++u)
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        uint32_t top = top_of(f[u]);
-        for (int o = 1; o < p.group_words; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
-        if (row[u] >= p.N || word[u] >= p.pw) continue;
+            for (int i = 0; i < WORDS; ++i) {
+                const int64_t row = row0 + u * by;
+                const int word = w0 + i * lanes;
+                load_weights<T, VEC>(w, row, in && row < p.N && word < w1 ? 8 * word : p.K, p.K, f[u][i]);
+            }
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u) {
+            const int64_t row = row0 + u * by;
+            uint32_t top = 0;
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) top = max(top, top_of(f[u][i]));
+            for (int o = 1; o < lanes; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
+            if (!in || row >= p.N) continue;
+            const Range r = range_of(top);
+#pragma unroll
+            for (int i = 0; i < WORDS; ++i) {
+                const int word = w0 + i * lanes;
+                if (word < w1) p.codes[row * p.pw + word] = word_of<WIDE>(f[u][i], 8 * word, p.K, r);
+            }
+            if (l == 0) p.scales[g * p.N + row] = r.scale;
+        }
+    } else {
+        const int64_t row = row0;
+        float f[8];
+        uint32_t top = 0;
+        const int end = in && row < p.N ? w1 : 0;
+        for (int word = w0; word < end; word += lanes) {
+            load_weights<T, VEC>(w, row, 8 * word, p.K, f);
+            top = max(top, top_of(f));
+        }
+        for (int o = 1; o < lanes; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
         const Range r = range_of(top);
-        p.codes[row[u] * p.pw + word[u]] = word_of(f[u], 8 * word[u], p.K, r);
-        const int g = word[u] / p.group_words;
-        if (word[u] == g * p.group_words) p.scales[g * p.N + row[u]] = r.scale;
+        for (int word = w0; word < end; word += lanes) {
+            load_weights<T, VEC>(w, row, 8 * word, p.K, f);
+            p.codes[row * p.pw + word] = word_of<WIDE>(f, 8 * word, p.K, r);
+        }
+        if (l == 0 && end) p.scales[g * p.N + row] = r.scale;
     }
-}
-
-// Any other multiple of 32: a warp a group, its weights read twice (the second time from
-// the caches).
-template <class T, bool VEC>
-__global__ void __launch_bounds__(256) quantize_group_kernel(const QuantParams p, int groups)
-{
-    grid_dependency_wait();
-    const int lane = threadIdx.x & 31;
-    const int64_t at = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
-    const int64_t row = at / groups;
-    if (row >= p.N) return;
-    const int g = (int)(at - row * groups);
-    const int w0 = g * p.group_words, w1 = min(w0 + p.group_words, p.pw);
-    float f[8];
-    uint32_t top = 0;
-    for (int w = w0 + lane; w < w1; w += 32) {
-        load_weights<T, VEC>((const T *)p.w, row, 8 * w, p.K, f);
-        top = max(top, top_of(f));
-    }
-    const Range r = range_of(__reduce_max_sync(~0u, top));
-    for (int w = w0 + lane; w < w1; w += 32) {
-        load_weights<T, VEC>((const T *)p.w, row, 8 * w, p.K, f);
-        p.codes[row * p.pw + w] = word_of(f, 8 * w, p.K, r);
-    }
-    if (lane == 0) p.scales[g * p.N + row] = r.scale;
 }
 
 struct ValueParams {
@@ -158,78 +171,91 @@ struct ValueParams {
     int64_t N;
     int K, pw, group_words;
     int odd;                  // values 2 c + 1 (else c)
+    int bx_log;
 };
 
 // A thread a word of eight codes: reads and writes of a warp are contiguous.
+constexpr int VALUE_ROWS = 4;
 template <class T, bool VEC>
 __global__ void __launch_bounds__(256) dequantize_kernel(const ValueParams p)
 {
+    const int tx = threadIdx.x & ((1 << p.bx_log) - 1), ty = threadIdx.x >> p.bx_log, by = 256 >> p.bx_log;
+    const int word = (blockIdx.y << p.bx_log) + tx, k = 8 * word;
+    const int64_t row0 = (int64_t)blockIdx.x * (by * VALUE_ROWS) + ty;
+    const float *scales = p.scales + (int64_t)(word / p.group_words) * p.N;
+    T *out = (T *)p.out;
     grid_dependency_wait();
     grid_launch_dependents();
-    const int64_t base = (int64_t)blockIdx.x * (256 * UNROLL);
-    const int64_t row0 = base / p.pw;
-    const unsigned rest = (unsigned)(base - row0 * p.pw) + threadIdx.x;
-    T *out = (T *)p.out;
-    uint32_t v[UNROLL];
-    float s[UNROLL];
-    int64_t row[UNROLL];
-    int word[UNROLL];
+    uint32_t v[VALUE_ROWS];
+    float s[VALUE_ROWS];
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const unsigned i = rest + 256 * u, r = i / (unsigned)p.pw;
-        row[u] = row0 + r;
-        word[u] = (int)(i - r * (unsigned)p.pw);
-        if (row[u] < p.N && 8 * word[u] < p.K) {
-            v[u] = __ldg(p.codes + row[u] * p.pw + word[u]);
-            s[u] = __ldg(p.scales + (int64_t)(word[u] / p.group_words) * p.N + row[u]);
+    for (int u = 0; u < VALUE_ROWS; ++u) {
+        const int64_t row = row0 + u * by;
+        if (row < p.N && k < p.K) {
+            v[u] = __ldg(p.codes + row * p.pw + word);
+            s[u] = __ldg(scales + row);
         }
     }
+    // a nibble at bits 1 to 4 of the mantissa of 2^23: with bit 0, 2^23 + 2 q + 1; else 2^23 + 2 q
+    // (q = c + 8)
+    const uint32_t bits = p.odd ? 0x4B000011u : 0x4B000010u;
+    const float half = p.odd ? 1.f : 0.5f;
 #pragma unroll
-    for (int u = 0; u < UNROLL; ++u) {
-        const int k = 8 * word[u];
-        if (row[u] >= p.N || k >= p.K) continue;
+    for (int u = 0; u < VALUE_ROWS; ++u) {
+        const int64_t row = row0 + u * by;
+        if (row >= p.N || k >= p.K) continue;
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int c = (int)(v[u] << (28 - 4 * i)) >> 28;
-            f[i] = s[u] * (float)(p.odd ? 2 * c + 1 : c);
+            const uint32_t y = i ? v[u] >> (4 * i - 1) : v[u] << 1;
+            f[i] = s[u] * ((__uint_as_float((y & 0x1Eu) ^ bits) - 8388624.f) * half);
         }
         if (VEC) {
             DsqRaw8<T> r;
             dsq_pack8(f, r);
-            dsq_store8(out + row[u] * p.K + k, r);
+            dsq_store8(out + row * p.K + k, r);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < p.K) out[row[u] * p.K + k + i] = dsq_from_f32<T>(f[i]);
+                if (k + i < p.K) out[row * p.K + k + i] = dsq_from_f32<T>(f[i]);
         }
     }
 }
 
-int blocks_of(int64_t words, int per_block, dim3 *grid)
+// A block's threads along a row (a power of two, 32 at least), the rest of them rows; rows along x.
+int block_shape(int64_t N, int64_t across, int rows, int *bx_log, dim3 *grid)
 {
-    const int64_t g = (words + per_block - 1) / per_block;
-    if (g > 0x7FFFFFFF) return DSQ_ERR_SIZE;
-    *grid = dim3((unsigned)g);
+    int log = 5;
+    while (log < 8 && (1 << log) < across) ++log;
+    *bx_log = log;
+    const int64_t per = (int64_t)(256 >> log) * rows, gx = (N + per - 1) / per;
+    const int64_t gy = (across + (1 << log) - 1) >> log;
+    if (gx > 0x7FFFFFFF || gy > 65535) return DSQ_ERR_SIZE;
+    *grid = dim3((unsigned)gx, (unsigned)gy);
     return DSQ_OK;
 }
 
-template <class T, bool VEC> int quantize(const QuantParams &p, int groups, cudaStream_t s)
+template <class T, bool VEC> int quantize(QuantParams p, cudaStream_t s)
 {
+    p.lanes_log = 2;
+    while (p.lanes_log < 5 && (1 << p.lanes_log) < p.group_words) ++p.lanes_log;
+    const int words = (p.group_words + (1 << p.lanes_log) - 1) >> p.lanes_log;      // of a thread
+    const int rows = words == 1 ? 4 : words == 2 ? 2 : 1;
     dim3 grid;
-    const bool words = p.group_words <= 32 && (p.group_words & (p.group_words - 1)) == 0;
-    const int st = words ? blocks_of(p.N * p.row_words, 256 * UNROLL, &grid) : blocks_of(p.N * groups, 8, &grid);
+    const int st = block_shape(p.N, (int64_t)p.groups << p.lanes_log, rows, &p.bx_log, &grid);
     if (st) return st;
     // (what these kernels write are a layer's constants: what follows starts behind them)
-    if (words)
-        return dsq_launch(quantize_words_kernel<T, VEC>, grid, dim3(256), 0, s, dsq_launch_hooks().pdl, 0, p);
-    return dsq_launch(quantize_group_kernel<T, VEC>, grid, dim3(256), 0, s, dsq_launch_hooks().pdl, 0, p, groups);
+    const auto kernel = words == 1   ? quantize_kernel<T, VEC, 1, 4>
+                        : words == 2 ? quantize_kernel<T, VEC, 2, 2>
+                        : words <= 4 ? quantize_kernel<T, VEC, 4, 1>
+                                     : quantize_kernel<T, VEC, 0, 1>;
+    return dsq_launch(kernel, grid, dim3(256), 0, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <class T, bool VEC> int dequantize(const ValueParams &p, cudaStream_t s)
+template <class T, bool VEC> int dequantize(ValueParams p, cudaStream_t s)
 {
     dim3 grid;
-    const int st = blocks_of(p.N * p.pw, 256 * UNROLL, &grid);
+    const int st = block_shape(p.N, p.pw, VALUE_ROWS, &p.bx_log, &grid);
     if (st) return st;
     return dsq_launch(dequantize_kernel<T, VEC>, grid, dim3(256), 0, s, dsq_launch_hooks().pdl, 0, p);
 }
@@ -271,14 +297,15 @@ int dsq_quantize_groups(const void *w, int64_t N, int64_t K, int dtype, int bits
     p.K = (int)K;
     p.pw = (int)(dsq_row_pitch(K, bits) / 4);
     // (a group longer than the row is the row)
-    p.group_words = groups == 1 && group > 256 ? p.pw : (int)(group / 8);
-    p.row_words = groups * p.group_words;
+    p.groups = groups;
+    p.group_words = groups == 1 ? p.pw : (int)(group / 8);
+    p.lanes_log = p.bx_log = 0;
     cudaStream_t s = (cudaStream_t)stream;
     const bool vec = K % 8 == 0;
     switch (dtype) {
-    case DSQ_F32: return vec ? quantize<float, true>(p, groups, s) : quantize<float, false>(p, groups, s);
-    case DSQ_BF16: return vec ? quantize<__nv_bfloat16, true>(p, groups, s) : quantize<__nv_bfloat16, false>(p, groups, s);
-    default: return vec ? quantize<__half, true>(p, groups, s) : quantize<__half, false>(p, groups, s);
+    case DSQ_F32: return vec ? quantize<float, true>(p, s) : quantize<float, false>(p, s);
+    case DSQ_BF16: return vec ? quantize<__nv_bfloat16, true>(p, s) : quantize<__nv_bfloat16, false>(p, s);
+    default: return vec ? quantize<__half, true>(p, s) : quantize<__half, false>(p, s);
     }
 }
 
@@ -300,6 +327,7 @@ int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N, int
     p.pw = (int)(dsq_row_pitch(K, bits) / 4);
     p.group_words = dsq_group_count(K, group) == 1 ? p.pw : (int)(group / 8);
     p.odd = w_offset == 0.5f;
+    p.bx_log = 0;
     cudaStream_t s = (cudaStream_t)stream;
     const bool vec = K % 8 == 0;
     switch (dtype) {
