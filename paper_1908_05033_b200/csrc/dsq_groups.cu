@@ -7,10 +7,13 @@
 //
 // The code is exact: weights kept in 16 bits lie on the border between two codes
 // often (w / a a ratio of small integers), and which side a rounded reciprocal puts
-// them on is chance.  With j = rint(7.5 w / a) as far as binary32 gives it, the code is j
-// or j - 1 by the sign of 7.5 w - a j: j is the nearest border, or as near as makes no
-// difference.  For weights of 16 bits a j and the fused difference are exact; for binary32
-// ones the rounding error of a j is taken off too.
+// them on is chance.  c = floor(v), v = 7.5 w / a:
+//   * 16-bit weights: a v that is no whole number is 2^-15 away from one at least, where it
+//     is above 1 (15 w and 2 a are integers of 15 and 12 bits on one grid, at most three
+//     powers of two apart), and v in binary32 is off by 2^-21 of itself: v (1 +- 2^-19),
+//     upwards, lies on the right side, and its floor is the code;
+//   * binary32 weights: with j = rint(v) as far as binary32 gives it, the code is j or j - 1
+//     by the sign of 7.5 w - a j, in which the rounding error of a j is taken off.
 //
 // Bound: memory (bf16 in 2.5 bytes a weight, values out 2.5), with arithmetic close behind: the
 // conversions between integers and floating point run at an eighth of the other operations' rate,
@@ -47,54 +50,83 @@ __device__ __forceinline__ Range range_of(uint32_t top)
     r.f = a < 7.8886e-31f ? 1.2676506e30f : 1.f;              // below 2^-100: times 2^100
     const float x = a * r.f;
     r.a = x * 0.0625f;
-    r.inv = r.bad || a == 0.f ? 0.f : __fdiv_rn(7.5f, x);
-    r.scale = r.bad ? __uint_as_float(0x7FC00000u) : __fdiv_rn(a, 15.f);
+    // (off by its last bits: what is made of it allows for that; finite for a = 0)
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.inv) : "f"(fmaxf(r.a, 1e-37f)));
+    r.inv *= 0.46875f;
+    // a / 15, rounded once: a quotient, corrected by what is left of a (a division in every
+    // thread took 9 us of 67 at 16384 x 4096 in groups of 128)
+    constexpr float R15 = 1.f / 15.f;
+    const float s = a * R15;
+    r.scale = r.bad ? __uint_as_float(0x7FC00000u) : __fmaf_rn(__fmaf_rn(-15.f, s, a), R15, s);
     return r;
 }
 constexpr float MAGIC = 12582912.f;                           // 1.5 2^23
 constexpr uint32_t MAGIC_BITS = 0x4B400000u;
-// bits of MAGIC + c, c the signed code (the ends of the range need no clip: |7.5 w| <= 7.5 a)
-template <bool WIDE> __device__ __forceinline__ uint32_t code_bits(float w, const Range &r)
+// bits of MAGIC + c, c the signed code (the ends of the range need no clip: |v| <= 7.5)
+template <bool WIDE> __device__ __forceinline__ uint32_t code_bits(float x, const Range &r)
 {
-    const float x = w * r.f;
-    const float t = __fmaf_rn(x, r.inv, MAGIC);
-    const float nj = __fsub_rn(MAGIC, t);                     // -j (never -0)
-    const float p = __fmul_rn(r.a, nj);
-    float d = __fmaf_rn(0.46875f, x, p);                      // (7.5 x - a j) / 16
-    if (WIDE) d = __fadd_rn(d, __fmaf_rn(r.a, nj, -p));
-    return __float_as_uint(t) + (uint32_t)((int)__float_as_uint(d) >> 31);
-}
-
-// eight weights from column k of a row; those behind the row's end are 0
-template <class T, bool VEC>
-__device__ __forceinline__ void load_weights(const T *w, int64_t row, int k, int K, float (&f)[8])
-{
-    if (VEC) {
-        if (k < K) {
-            dsq_unpack8(dsq_load8(w + row * K + k), f);
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = 0.f;
+    if constexpr (WIDE) {
+        const float t = __fmaf_rn(x, r.inv, MAGIC);
+        const float nj = __fsub_rn(MAGIC, t);                 // -j (never -0)
+        const float p = __fmul_rn(r.a, nj);
+        const float d = __fadd_rn(__fmaf_rn(0.46875f, x, p), __fmaf_rn(r.a, nj, -p));   // (7.5 x - a j) / 16
+        return __float_as_uint(t) + (uint32_t)((int)__float_as_uint(d) >> 31);
     } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) f[i] = k + i < K ? dsq_to_f32(w[row * K + k + i]) : 0.f;
+        const float v = __fmul_rn(x, r.inv);
+        return __float_as_uint(__fadd_rd(__fadd_rn(v, __fmul_rn(fabsf(v), 1.9073486e-6f)), MAGIC));
     }
 }
-__device__ __forceinline__ uint32_t top_of(const float (&f)[8])
+
+// eight weights from column k of the row at w; those behind its end are 0
+template <class T, bool VEC>
+__device__ __forceinline__ DsqRaw8<T> load_weights(const T *w, int k, int K)
 {
-    uint32_t t = 0;
+    DsqRaw8<T> r;
+    if (VEC) {
+        if (k < K) return dsq_load8(w + k);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) t = max(t, __float_as_uint(f[i]) & 0x7FFFFFFFu);
-    return t;
+        for (int i = 0; i < (int)(sizeof(r) / 16); ++i) r.v[i] = make_uint4(0u, 0u, 0u, 0u);
+    } else {
+        float f[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = k + i < K ? dsq_to_f32(w[k + i]) : 0.f;
+        dsq_pack8(f, r);
+    }
+    return r;
+}
+// the largest magnitude's bits, in the type's own bits (those of a NaN are above infinity's)
+template <class T> __device__ __forceinline__ uint32_t top_of(const DsqRaw8<T> &r)
+{
+    if constexpr (sizeof(T) == 2) {
+        constexpr uint32_t ABS = 0x7FFF7FFFu;
+        const uint32_t t = __vmaxu2(__vmaxu2(r.v[0].x & ABS, r.v[0].y & ABS), __vmaxu2(r.v[0].z & ABS, r.v[0].w & ABS));
+        return max(t & 0xFFFFu, t >> 16);
+    } else {
+        constexpr uint32_t ABS = 0x7FFFFFFFu;
+        const uint4 a = r.v[0], b = r.v[1];
+        return max(max(max(a.x & ABS, a.y & ABS), max(a.z & ABS, a.w & ABS)),
+                   max(max(b.x & ABS, b.y & ABS), max(b.z & ABS, b.w & ABS)));
+    }
+}
+// such bits as binary32's
+__device__ __forceinline__ uint32_t wide_bits(uint32_t top, float) { return top; }
+__device__ __forceinline__ uint32_t wide_bits(uint32_t top, __nv_bfloat16) { return top << 16; }
+__device__ __forceinline__ uint32_t wide_bits(uint32_t top, __half)
+{
+    return __float_as_uint(__half2float(__ushort_as_half((unsigned short)top))) & 0x7FFFFFFFu;
 }
 // the word of eight codes; those behind the row's end are 0
-template <bool WIDE>
-__device__ __forceinline__ uint32_t word_of(const float (&f)[8], int k, int K, const Range &r)
+template <class T> __device__ __forceinline__ uint32_t word_of(const DsqRaw8<T> &raw, int k, int K, const Range &r)
 {
+    float f[8];
+    dsq_unpack8(raw, f);
+    if (r.f != 1.f) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] *= r.f;
+    }
     uint32_t v = 0;
 #pragma unroll
-    for (int i = 7; i >= 0; --i) v = v * 16u + code_bits<WIDE>(f[i], r);
+    for (int i = 7; i >= 0; --i) v = v * 16u + code_bits<sizeof(T) == 4>(f[i], r);
     // every term stands for MAGIC_BITS + c: codes made positive, summed without carries, and
     // turned into two's complement nibbles
     constexpr uint32_t ALL = 0x11111111u;
@@ -109,7 +141,6 @@ __device__ __forceinline__ uint32_t word_of(const float (&f)[8], int k, int K, c
 template <class T, bool VEC, int WORDS, int ROWS>
 __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p)
 {
-    constexpr bool WIDE = sizeof(T) == 4;
     const int lanes = 1 << p.lanes_log, tx = threadIdx.x & ((1 << p.bx_log) - 1), ty = threadIdx.x >> p.bx_log;
     const int slot = (blockIdx.y << p.bx_log) + tx;
     const int g = slot >> p.lanes_log, l = slot & (lanes - 1);
@@ -120,45 +151,70 @@ __global__ void __launch_bounds__(256) quantize_kernel(const QuantParams p)
     const T *w = (const T *)p.w;
     grid_dependency_wait();
     if constexpr (WORDS > 0) {
-        float f[ROWS][WORDS][8];
+        const int left = (int)min(p.N - row0, (int64_t)ROWS * by);       // rows from row0 on
+        DsqRaw8<T> f[ROWS][WORDS];
+        uint32_t top[ROWS];
+        const T *src = w + row0 * p.K;
 #pragma unroll
-        for (int u = 0; u < ROWS; ++u)
+        for (int u = 0; u < ROWS; ++u, src += (int64_t)by * p.K)
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
-                const int64_t row = row0 + u * by;
                 const int word = w0 + i * lanes;
-                load_weights<T, VEC>(w, row, in && row < p.N && word < w1 ? 8 * word : p.K, p.K, f[u][i]);
+                f[u][i] = load_weights<T, VEC>(src, in && u * by < left && word < w1 ? 8 * word : p.K, p.K);
             }
 #pragma unroll
         for (int u = 0; u < ROWS; ++u) {
-            const int64_t row = row0 + u * by;
-            uint32_t top = 0;
+            top[u] = top_of(f[u][0]);
 #pragma unroll
-            for (int i = 0; i < WORDS; ++i) top = max(top, top_of(f[u][i]));
-            for (int o = 1; o < lanes; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
-            if (!in || row >= p.N) continue;
-            const Range r = range_of(top);
+            for (int i = 1; i < WORDS; ++i) top[u] = max(top[u], top_of(f[u][i]));
+        }
+        if constexpr (sizeof(T) == 2 && ROWS % 2 == 0) {                 // two rows' in a register
+#pragma unroll
+            for (int u = 0; u < ROWS; u += 2) top[u] |= top[u + 1] << 16;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                if (o >= lanes) break;
+#pragma unroll
+                for (int u = 0; u < ROWS; u += 2) top[u] = __vmaxu2(top[u], __shfl_xor_sync(~0u, top[u], o));
+            }
+#pragma unroll
+            for (int u = 0; u < ROWS; u += 2) {
+                top[u + 1] = top[u] >> 16;
+                top[u] &= 0xFFFFu;
+            }
+        } else {
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                if (o >= lanes) break;
+#pragma unroll
+                for (int u = 0; u < ROWS; ++u) top[u] = max(top[u], __shfl_xor_sync(~0u, top[u], o));
+            }
+        }
+        uint32_t *dst = p.codes + row0 * p.pw;
+        float *scale = p.scales + (int64_t)g * p.N + row0;
+#pragma unroll
+        for (int u = 0; u < ROWS; ++u, dst += (int64_t)by * p.pw, scale += by) {
+            if (!in || u * by >= left) continue;
+            const Range r = range_of(wide_bits(top[u], T()));
 #pragma unroll
             for (int i = 0; i < WORDS; ++i) {
                 const int word = w0 + i * lanes;
-                if (word < w1) p.codes[row * p.pw + word] = word_of<WIDE>(f[u][i], 8 * word, p.K, r);
+                if (word < w1) dst[word] = word_of<T>(f[u][i], 8 * word, p.K, r);
             }
-            if (l == 0) p.scales[g * p.N + row] = r.scale;
+            if (l == 0) *scale = r.scale;
         }
     } else {
         const int64_t row = row0;
-        float f[8];
+        const T *src = w + row * p.K;
         uint32_t top = 0;
         const int end = in && row < p.N ? w1 : 0;
         for (int word = w0; word < end; word += lanes) {
-            load_weights<T, VEC>(w, row, 8 * word, p.K, f);
-            top = max(top, top_of(f));
+            top = max(top, top_of(load_weights<T, VEC>(src, 8 * word, p.K)));
         }
         for (int o = 1; o < lanes; o <<= 1) top = max(top, __shfl_xor_sync(~0u, top, o));
-        const Range r = range_of(top);
+        const Range r = range_of(wide_bits(top, T()));
         for (int word = w0; word < end; word += lanes) {
-            load_weights<T, VEC>(w, row, 8 * word, p.K, f);
-            p.codes[row * p.pw + word] = word_of<WIDE>(f, 8 * word, p.K, r);
+            p.codes[row * p.pw + word] = word_of<T>(load_weights<T, VEC>(src, 8 * word, p.K), 8 * word, p.K, r);
         }
         if (l == 0 && end) p.scales[g * p.N + row] = r.scale;
     }
@@ -182,28 +238,27 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const ValueParams p)
     const int tx = threadIdx.x & ((1 << p.bx_log) - 1), ty = threadIdx.x >> p.bx_log, by = 256 >> p.bx_log;
     const int word = (blockIdx.y << p.bx_log) + tx, k = 8 * word;
     const int64_t row0 = (int64_t)blockIdx.x * (by * VALUE_ROWS) + ty;
-    const float *scales = p.scales + (int64_t)(word / p.group_words) * p.N;
-    T *out = (T *)p.out;
+    const float *scales = p.scales + (int64_t)(word / p.group_words) * p.N + row0;
+    const int left = (int)min(p.N - row0, (int64_t)VALUE_ROWS * by);     // rows from row0 on
     grid_dependency_wait();
     grid_launch_dependents();
     uint32_t v[VALUE_ROWS];
     float s[VALUE_ROWS];
+    const uint32_t *src = p.codes + row0 * p.pw + word;
 #pragma unroll
-    for (int u = 0; u < VALUE_ROWS; ++u) {
-        const int64_t row = row0 + u * by;
-        if (row < p.N && k < p.K) {
-            v[u] = __ldg(p.codes + row * p.pw + word);
-            s[u] = __ldg(scales + row);
+    for (int u = 0; u < VALUE_ROWS; ++u, src += (int64_t)by * p.pw)
+        if (u * by < left && k < p.K) {
+            v[u] = __ldg(src);
+            s[u] = __ldg(scales + u * by);
         }
-    }
     // a nibble at bits 1 to 4 of the mantissa of 2^23: with bit 0, 2^23 + 2 q + 1; else 2^23 + 2 q
     // (q = c + 8)
     const uint32_t bits = p.odd ? 0x4B000011u : 0x4B000010u;
     const float half = p.odd ? 1.f : 0.5f;
+    T *out = (T *)p.out + row0 * p.K + k;
 #pragma unroll
-    for (int u = 0; u < VALUE_ROWS; ++u) {
-        const int64_t row = row0 + u * by;
-        if (row >= p.N || k >= p.K) continue;
+    for (int u = 0; u < VALUE_ROWS; ++u, out += (int64_t)by * p.K) {
+        if (u * by >= left || k >= p.K) continue;
         float f[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -213,11 +268,11 @@ __global__ void __launch_bounds__(256) dequantize_kernel(const ValueParams p)
         if (VEC) {
             DsqRaw8<T> r;
             dsq_pack8(f, r);
-            dsq_store8(out + row * p.K + k, r);
+            dsq_store8(out, r);
         } else {
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (k + i < p.K) out[row * p.K + k + i] = dsq_from_f32<T>(f[i]);
+                if (k + i < p.K) out[i] = dsq_from_f32<T>(f[i]);
         }
     }
 }
