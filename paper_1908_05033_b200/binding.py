@@ -123,6 +123,7 @@ _HOOKS = {
     "dsq_set_conv3_window": (_int, [_int]),
     "dsq_set_gemm_two_pass": (_int, [_int]),
     "dsq_set_conv3_expanded_weights": (_int, [_int]),
+    "dsq_set_wgemm_group_form": (_int, [_int]),
 }
 for _name, (_res, _args) in list(_SIGNATURES.items()) + list(_HOOKS.items()):
     _f = getattr(lib, _name)       # AttributeError if a symbol is missing
@@ -394,6 +395,10 @@ def dsq_set_round_k_steps(ks):
 
 def dsq_set_conv3_expanded_weights(on):
     _check(lib.dsq_set_conv3_expanded_weights(int(on)), "dsq_set_conv3_expanded_weights")
+
+
+def dsq_set_wgemm_group_form(form):
+    _check(lib.dsq_set_wgemm_group_form(int(form)), "dsq_set_wgemm_group_form")
 
 
 def dsq_set_gemm_two_pass(on):

@@ -27,22 +27,11 @@
 #include "dsq_ptx.cuh"
 #include "dsq_tc_host.h"
 #include "dsq_types.cuh"
+#include "dsq_wgemm_group.cuh"
 
 using namespace dsq_ptx;
 
 namespace {
-
-struct GvParams {
-    const uint8_t *X, *W;
-    const float *scales, *bias, *row_scale;
-    void *Y;
-    int64_t N;
-    int M, K, pitch;              // pitch: bytes of a row of codes
-    int groups;
-    uint32_t units, units_inv;    // flush units of a group, floor(2^32 / units) + 1
-    int odd;                      // values 2 c + 1 (else c)
-    int y_type;
-};
 
 template <int XT> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
@@ -65,32 +54,9 @@ __device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-// codes i and i + 4 of a word as a pair of 16-bit values
-template <int XT> __device__ __forceinline__ uint32_t value_pair(uint32_t w, int i, uint32_t base)
-{
-    constexpr int AT = XT == DSQ_BF16 ? 3 : 6;                // the field's place in the mantissa
-    constexpr uint32_t MASK = (0xFu << AT) * 0x00010001u;
-    constexpr uint32_t FLIP = ((XT == DSQ_BF16 ? 0x3F80u : 0x3C00u) ^ (8u << AT)) * 0x00010001u;
-    const uint32_t y = 4 * i > AT ? w >> (4 * i - AT) : w << (AT - 4 * i);
-    const uint32_t v = (y & MASK) ^ FLIP;
-    if (XT == DSQ_BF16) {
-        const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v),
-                                         *reinterpret_cast<const __nv_bfloat162 *>(&base));
-        return *reinterpret_cast<const uint32_t *>(&r);
-    }
-    const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&base));
-    return *reinterpret_cast<const uint32_t *>(&r);
-}
-
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ uint32_t lds_32(uint32_t at)
-{
-    uint32_t v;
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-    return v;
 }
 __device__ __forceinline__ uint2 lds_64(uint32_t at)
 {
@@ -110,7 +76,7 @@ template <int XT, int NT, int GP> __host__ __device__ constexpr int stage_bytes(
 
 template <int XT, int MT, int NT, int GP, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32)
-wgemm_group_kernel(const GvParams p)
+wgemm_group_kernel(const DsqGroupGemm p)
 {
     constexpr int TILES = Rows<MT>::TILES, XB = x_bytes<XT>();
     constexpr bool INT = XT == DSQ_I8;
@@ -124,7 +90,7 @@ wgemm_group_kernel(const GvParams p)
     const int turns = warp < chunks ? (chunks - warp - 1) / WARPS + 1 : 0;
     const int stage = stage_bytes<XT, NT, GP>(rows);
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * stage);
-    const uint32_t base = XT == DSQ_BF16 ? (p.odd ? 0x3FBC3FBCu : 0x3FC03FC0u) : (p.odd ? 0x3DE03DE0u : 0x3E003E00u);
+    const uint32_t base = dsq_value_base<XT>(p.odd);
 
     // the copies of this warp's i-th chunk into its stage
     auto issue_w = [&](int i) {
@@ -142,7 +108,7 @@ wgemm_group_kernel(const GvParams p)
 #pragma unroll
         for (int s = lane; s < (4 / GP) * NT * 8; s += 32) {
             const uint32_t unit = (uint32_t)(c * (4 / GP) + s / (8 * NT));
-            const int g = p.units == 1 ? (int)unit : (int)__umulhi(unit, p.units_inv);
+            const int g = p.group_of(unit);
             const int64_t col = n0 + s % (8 * NT);
             const bool in = g < p.groups && col < p.N;
             cp_async_4(at + NT * 512 + s * 4, in ? p.scales + (int64_t)g * p.N + col : p.scales, in ? 4u : 0u);
@@ -248,7 +214,7 @@ wgemm_group_kernel(const GvParams p)
                 } else {
 #pragma unroll
                     for (int s = 0; s < 2; ++s) {
-                        const uint32_t b0 = value_pair<XT>(w, 2 * s, base), b1 = value_pair<XT>(w, 2 * s + 1, base);
+                        const uint32_t b0 = dsq_value_pair<XT>(w, 2 * s, base), b1 = dsq_value_pair<XT>(w, 2 * s + 1, base);
 #pragma unroll
                         for (int m = 0; m < TILES; ++m) mma<XT>(acc[m][t], a[m][s], b0, b1);
                     }
@@ -283,7 +249,7 @@ wgemm_group_kernel(const GvParams p)
             part[(warp * TILES * NT + m * NT + t) * 32 + lane] =
                 make_float4(total[m][t][0], total[m][t][1], total[m][t][2], total[m][t][3]);
     __syncthreads();
-    const float unit = INT ? (p.odd ? 0.125f : 0.0625f) : (p.odd ? 32.f : 16.f);
+    const float unit = dsq_value_unit<XT>(p.odd);
     const float *sums = reinterpret_cast<const float *>(smem);
     for (int e = threadIdx.x; e < TILES * NT * 128; e += WARPS * 32) {
         // element e of the tile in row-major order: 16 TILES rows, 8 NT columns
@@ -294,17 +260,11 @@ wgemm_group_kernel(const GvParams p)
         float s = 0.f;
 #pragma unroll
         for (int w = 0; w < WARPS; ++w) s += sums[((w * TILES * NT + tile) * 32 + l) * 4 + k];
-        s *= unit;
-        if (INT) s *= __ldg(p.row_scale + m0 + row);
-        if (p.bias) s += __ldg(p.bias + n0 + col);
-        const int64_t to = (int64_t)(m0 + row) * p.N + n0 + col;
-        if (p.y_type == DSQ_F32) ((float *)p.Y)[to] = s;
-        else if (p.y_type == DSQ_BF16) ((__nv_bfloat16 *)p.Y)[to] = __float2bfloat16_rn(s);
-        else ((__half *)p.Y)[to] = __float2half_rn(s);
+        p.store(m0 + row, n0 + col, s * unit);
     }
 }
 
-template <int XT, int MT, int NT, int GP, int WARPS, int STAGES> int launch(const GvParams &p, cudaStream_t s)
+template <int XT, int MT, int NT, int GP, int WARPS, int STAGES> int launch(const DsqGroupGemm &p, cudaStream_t s)
 {
     constexpr int ROWS = Rows<MT>::N;
     constexpr int most = WARPS * STAGES * stage_bytes<XT, NT, GP>(ROWS);
@@ -321,25 +281,31 @@ template <int XT, int MT, int NT, int GP, int WARPS, int STAGES> int launch(cons
                       dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int XT, int GP> int pick(GvParams p, cudaStream_t s)
+template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
 {
-    p.units /= 32 * GP;
-    p.units_inv = p.units > 1 ? (uint32_t)((1ull << 32) / p.units + 1) : 0u;
     if (p.M <= 8) return launch<XT, 0, 4, GP, 8, 3>(p, s);
     if (p.M <= 16) return launch<XT, 1, 4, GP, 8, 3>(p, s);
     if (p.M <= 32) return launch<XT, 2, 4, GP, 8, 2>(p, s);
     return launch<XT, 4, 4, GP, 4, 2>(p, s);
 }
 
-template <int XT> int pick_group(const GvParams &p, cudaStream_t s)
+template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
 {
-    // (p.units holds the codes of a group)
-    if (p.units % 128 == 0) return pick<XT, 4>(p, s);
-    if (p.units % 64 == 0) return pick<XT, 2>(p, s);
-    return pick<XT, 1>(p, s);
+    const int gp = dsq_group_pieces(group);
+    p.set_units(group, gp);
+    return gp == 4 ? pick<XT, 4>(p, s) : gp == 2 ? pick<XT, 2>(p, s) : pick<XT, 1>(p, s);
 }
 
 }  // namespace
+
+static std::atomic<int> dsq_group_form{0};
+
+extern "C" int dsq_set_wgemm_group_form(int form)
+{
+    if (form < 0 || form > 2) return DSQ_ERR_SHAPE;
+    dsq_group_form.store(form);
+    return DSQ_OK;
+}
 
 extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale, const void *W_codes,
                                const float *scales, const float *bias, int64_t M, int64_t N, int64_t K,
@@ -361,7 +327,7 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
     // (a group longer than the row is the row; a group's sum of at most 128 * 128 a term stays in int32)
     const int64_t g = dsq_group_count(K, group) == 1 ? (K + 127) / 128 * 128 : group;
     if (x_type == DSQ_I8 && (g < K ? g : K) > (1 << 16)) return DSQ_ERR_OVERFLOW;
-    GvParams p;
+    DsqGroupGemm p;
     p.X = (const uint8_t *)X;
     p.W = (const uint8_t *)W_codes;
     p.scales = scales; p.bias = bias; p.row_scale = row_scale;
@@ -370,14 +336,15 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
     p.M = (int)M; p.K = (int)K;
     p.pitch = (int)dsq_row_pitch(K, 4);
     p.groups = (int)dsq_group_count(K, g);
-    p.units = (uint32_t)g;
-    p.units_inv = 0;
+    p.units = p.units_inv = 0;
     p.odd = w_offset == 0.5f;
     p.y_type = y_type;
     cudaStream_t s = (cudaStream_t)stream;
+    const int form = dsq_group_form.load(std::memory_order_relaxed);
+    if (form == 2 || (form == 0 && N * K > (1 << 21))) return dsq_wgemm_group_tc(p, x_type, g, s);
     switch (x_type) {
-    case DSQ_BF16: return pick_group<DSQ_BF16>(p, s);
-    case DSQ_F16: return pick_group<DSQ_F16>(p, s);
-    default: return pick_group<DSQ_I8>(p, s);
+    case DSQ_BF16: return pick_group<DSQ_BF16>(p, g, s);
+    case DSQ_F16: return pick_group<DSQ_F16>(p, g, s);
+    default: return pick_group<DSQ_I8>(p, g, s);
     }
 }

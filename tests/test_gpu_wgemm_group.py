@@ -211,3 +211,39 @@ def test_layer_front_as_it_serves(dsq):
         assert all(torch.equal(a, b) for a, b in zip(ref, held))
         xs.zero_()
         g.replay()
+
+
+@pytest.fixture(params=[1, 2])
+def form(request, dsq):
+    dsq.dsq_set_wgemm_group_form(request.param)
+    yield request.param
+    dsq.dsq_set_wgemm_group_form(0)
+
+
+# both kernels at every size: columns and rows of a tile and one beyond, chunks of K and their
+# remainders, each number of blocks along K
+FORM_SIZES = [(1, 1, 16, 32), (1, 127, 128, 128), (3, 129, 256, 64), (8, 128, 384, 128), (9, 300, 2064, 32),
+              (16, 257, 4096, 128), (17, 130, 1040, 64), (32, 128, 2048, 128), (33, 200, 3200, 32),
+              (64, 384, 1152, 256), (65, 129, 1296, 64), (150, 140, 528, 96), (2, 1000, 8192, 128),
+              (1, 20000, 1536, 128), (40, 2500, 1040, 128)]
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16, torch.int8])
+@pytest.mark.parametrize("size", FORM_SIZES)
+def test_both_kernels(dsq, form, size, t):
+    M, n, k, group = size
+    codes, scales, bias, packed = weights(dsq, n, k, group, 2)
+    rng = np.random.default_rng(M)
+    rs = None
+    if t == torch.int8:
+        x = torch.from_numpy(rng.integers(-128, 128, (M, k)).astype(np.int8))
+        rs = rng.uniform(0.01, 0.02, M).astype(np.float32)
+    else:
+        x = torch.from_numpy(rng.normal(size=(M, k))).to(t)
+    for off in (0.5, 0.0):
+        Y = dsq.dsq_wgemm_group(x.cuda(), packed, M, n, k, 4, group, T(scales), bias=T(bias),
+                                row_scale=None if rs is None else T(rs), w_offset=off)
+        check(Y, x.double().numpy(), codes, scales, group, bias, off, rs)
+        again = dsq.dsq_wgemm_group(x.cuda(), packed, M, n, k, 4, group, T(scales), bias=T(bias),
+                                    row_scale=None if rs is None else T(rs), w_offset=off)
+        assert torch.equal(Y, again)
