@@ -14,7 +14,7 @@ HOST_SOURCE = "dsq_host.cpp"
 OBJ_DIR = os.path.join(HERE, "_build")
 SOURCES = ["dsq_elementwise.cu", "dsq_dwconv.cu", "dsq_tc.cu", "dsq_conv3.cu", "dsq_pw.cu", "dsq_gemm8.cu",
            "dsq_wgemm_small.cu", "dsq_gemm_small.cu", "dsq_conv_small.cu",
-           "dsq_soft.cu", "dsq_norm.cu", "dsq_groups.cu", "dsq_wgemm_group.cu", "dsq_wgemm_group_tc.cu", "dsq_plan.cu", "dsq_workspace.cu"]
+           "dsq_soft.cu", "dsq_norm.cu", "dsq_groups.cu", "dsq_wgemm_group.cu", "dsq_wgemm_group_tc.cu", "dsq_wgemm_group_few.cu", "dsq_plan.cu", "dsq_workspace.cu"]
 HEADERS = ["dsq_common.cuh", "dsq_conv_rule.h", "dsq_epilogue.cuh", "dsq_fragments.cuh", "dsq_gemm8_rule.h", "dsq_groups.h", "dsq_ptx.cuh", "dsq_tc_common.cuh",
            "dsq_tc_host.h", "dsq_types.cuh", "dsq_wgemm_group.cuh", "dsq_hooks.h", "dsq_launch.h", "dsq_plan.h",
            os.path.join("..", "..", "include", "dsq.h")]

@@ -54,8 +54,8 @@ int dsq_set_conv3_expanded_weights(int on);
  * size (dsq_gemm_workspace_bytes answers accordingly). */
 int dsq_set_gemm_two_pass(int on);
 
-/* dsq_wgemm_group: 0 = the faster kernel (default), 1 = always the mma.sync one, 2 = always the
- * tcgen05 one. */
+/* dsq_wgemm_group: 0 = the faster kernel (default), 1 = always the 16-bit mma.sync one, 2 = always
+ * the tcgen05 one, 3 = always the one of 8-bit digits. */
 int dsq_set_wgemm_group_form(int form);
 
 /* Test hook: in every later launch the thread that issues the TMA copies of

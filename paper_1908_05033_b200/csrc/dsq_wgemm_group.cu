@@ -58,13 +58,6 @@ __device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
-__device__ __forceinline__ uint2 lds_64(uint32_t at)
-{
-    uint2 v;
-    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
-    return v;
-}
-
 // rows: 8 (MT = 0: the lower half of an instruction's rows) or 16 MT
 template <int MT> struct Rows { static constexpr int N = MT ? 16 * MT : 8, TILES = MT ? MT : 1; };
 template <int XT> __host__ __device__ constexpr int x_bytes() { return XT == DSQ_I8 ? 128 : 256; }   // of a row's chunk
@@ -302,7 +295,7 @@ static std::atomic<int> dsq_group_form{0};
 
 extern "C" int dsq_set_wgemm_group_form(int form)
 {
-    if (form < 0 || form > 2) return DSQ_ERR_SHAPE;
+    if (form < 0 || form > 3) return DSQ_ERR_SHAPE;
     dsq_group_form.store(form);
     return DSQ_OK;
 }
@@ -341,6 +334,7 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
     p.y_type = y_type;
     cudaStream_t s = (cudaStream_t)stream;
     const int form = dsq_group_form.load(std::memory_order_relaxed);
+    if (form == 3 || (form == 0 && M <= (x_type == DSQ_I8 ? 16 : 5))) return dsq_wgemm_group_few(p, x_type, g, s);
     if (form == 2 || (form == 0 && N * K > (1 << 21))) return dsq_wgemm_group_tc(p, x_type, g, s);
     switch (x_type) {
     case DSQ_BF16: return pick_group<DSQ_BF16>(p, g, s);

@@ -47,6 +47,7 @@ static inline int dsq_group_pieces(int64_t group) { return group % 128 == 0 ? 4 
 
 // arguments validated; group a multiple of 32
 DSQ_HIDDEN int dsq_wgemm_group_tc(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s);
+DSQ_HIDDEN int dsq_wgemm_group_few(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s);
 
 #ifdef __CUDACC__
 // codes i and i + 4 of a word as a pair of 16-bit values (2 c + 1) / 32 or c / 16: the field in the
@@ -80,6 +81,12 @@ template <int XT> __device__ __forceinline__ float dsq_value_unit(int odd)
 __device__ __forceinline__ uint32_t dsq_idesc_f16(int n)
 {
     return 1u << 4 | (uint32_t)(n >> 3) << 17 | 8u << 24;
+}
+__device__ __forceinline__ uint2 lds_64(uint32_t at)
+{
+    uint2 v;
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(at) : "memory");
+    return v;
 }
 __device__ __forceinline__ uint32_t ld_cluster_32(uint32_t addr)
 {

@@ -213,7 +213,7 @@ def test_layer_front_as_it_serves(dsq):
         g.replay()
 
 
-@pytest.fixture(params=[1, 2])
+@pytest.fixture(params=[1, 2, 3])
 def form(request, dsq):
     dsq.dsq_set_wgemm_group_form(request.param)
     yield request.param
