@@ -4,19 +4,18 @@
 // With a row or two the codes pass through the SM once, and what a code costs in instructions
 // bounds the kernel: as bf16 a word of eight codes takes twelve to unpack and four instructions'
 // worth of mma.sync, as int8 three and one (the field in the upper half of a byte is 16 c as it
-// stands, with bit 3 set 8 (2 c + 1)).  So rows in 16 bits are made integers too: of each 128
+// stands, with bit 3 set 8 (2 c + 1)).  So rows in 16 bits are made integers too: of each 256
 // elements of a row the largest magnitude's exponent gives a power of two that takes it below
 // 2^22, the rounded element is cut into three signed digits of 8 bits, and the digits are three
 // rows of the instruction, whose other rows would be empty anyway.  An element of
-// bf16 (fp16) is exact down to 2^-14 (2^-11) of the largest of its 128, and below that off by at
+// bf16 (fp16) is exact down to 2^-14 (2^-11) of the largest of its 256, and below that off by at
 // most 2^-22 of it.  Sums are exact in int32; they enter the totals times the group's scale and the
 // power of two in binary32.
 //
-//   * A warp takes the chunks of 128 codes of 8 NT columns in turn with the others of its
+//   * A warp takes the chunks of 256 codes of 8 NT columns in turn with the others of its
 //     block, through a ring of stages of its own in shared memory (cp.async, no barrier between
-//     warps).  Lane (n = lane / 4, j = lane & 3) has word j of each of a chunk's four
-//     pieces of 32 codes of column n.
-//   * Rows of X and scales come a chunk ahead into registers.
+//     warps): the chunk's codes, the scales of its groups and its elements of X.  Lane (n = lane / 4,
+//     j = lane & 3) has word j of each of a chunk's eight pieces of 32 codes of column n.
 //   * The warps' totals, and then the digits' ones, are added in a fixed order.
 #include "dsq_groups.h"
 #include "dsq_ptx.cuh"
@@ -36,14 +35,37 @@ __device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
-constexpr int ROW = 160;          // bytes of a row of digits in shared memory (rows meet no bank twice)
+// the same on sums of zero
+__device__ __forceinline__ void mma_i8_first(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%10, %10, %10, %10};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0));
+}
+__device__ __forceinline__ void sts_64(uint32_t at, uint32_t a, uint32_t b)
+{
+    asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
+}
+template <int BYTES> __device__ __forceinline__ void cp_async_small(uint32_t dst, const void *src, uint32_t src_bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes)
+                 : "memory");
+}
 
-// HALF: at most 8 rows of digits (else 16); ROWS of X; GP: pieces of 32 codes that no group's end cuts
+// bytes of a row of digits in shared memory: rows meet no bank twice in 16-byte reads (GP = 4) or in
+// 8-byte ones
+template <int GP> constexpr int row_bytes() { return GP == 4 ? 272 : 288; }
+
+// ROWS of X; GP: pieces of 32 codes that no group's end cuts
 template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> struct Few {
     static constexpr int DIGITS = XT == DSQ_I8 ? 1 : 3;
-    static constexpr bool HALF = ROWS * DIGITS <= 8;
-    static constexpr int W_BYTES = NT * 512;
-    static constexpr int WARP_BYTES = STAGES * W_BYTES + ROWS * DIGITS * ROW;
+    static constexpr bool HALF = ROWS * DIGITS <= 8;              // the lower half of an instruction's rows
+    static constexpr int FLUSHES = 8 / GP;
+    static constexpr int W_BYTES = NT * 1024, S_BYTES = FLUSHES * NT * 32;
+    static constexpr int X_ROW = XT == DSQ_I8 ? 256 : 512;
+    static constexpr int STAGE = W_BYTES + S_BYTES + ROWS * X_ROW;
+    static constexpr int WARP_BYTES = STAGES * STAGE + ROWS * DIGITS * row_bytes<GP>();
     static constexpr int SUMS = WARPS * NT * (HALF ? 64 : 128) * 4;
     static constexpr int BYTES = WARPS * WARP_BYTES > SUMS ? WARPS * WARP_BYTES : SUMS;
     static_assert(ROWS * DIGITS <= 16 && WARP_BYTES % 16 == 0 && BYTES <= 227 * 1024, "shared memory");
@@ -54,184 +76,224 @@ __global__ void __launch_bounds__(WARPS * 32)
 wgemm_group_few_kernel(const DsqGroupGemm p)
 {
     using L = Few<XT, ROWS, NT, GP, WARPS, STAGES>;
-    constexpr int DIGITS = L::DIGITS, FLUSHES = 4 / GP, SLOTS = L::HALF ? 2 : 4;
+    constexpr int DIGITS = L::DIGITS, FLUSHES = L::FLUSHES, HALVES = L::HALF ? 1 : 2;
     constexpr bool INT = XT == DSQ_I8;
+    constexpr int ROW = row_bytes<GP>();
+    constexpr int X_LANE = INT ? 8 : 16;                             // bytes of eight elements
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n = lane >> 2, j = lane & 3;
     const int64_t n0 = (int64_t)blockIdx.x * (8 * NT);
-    const int m0 = blockIdx.y * ROWS, rows = min(p.M - m0, ROWS);
-    const int chunks = (p.K + 127) >> 7;
+    const int m0 = blockIdx.y * ROWS, rows = ROWS == 1 ? 1 : min(p.M - m0, ROWS);
+    const int chunks = (p.K + 255) >> 8;
     const int turns = warp < chunks ? (chunks - warp - 1) / WARPS + 1 : 0;
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * L::WARP_BYTES), digits = ring + STAGES * L::W_BYTES;
-
-    // codes: 16-byte piece j of column n of each eight, where the reads of a piece's words meet no
-    // bank twice
-    const uint8_t *src = p.W + (n0 + n) * p.pitch + warp * 64 + 16 * j;
-    const uint32_t w_to = ring + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
-    const int64_t step = 8 * (int64_t)p.pitch;
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * L::WARP_BYTES), digits = ring + STAGES * L::STAGE;
     const int cols = (int)min((int64_t)8 * NT, p.N - n0);             // of this block
-    int left = p.pitch - warp * 64 - 16 * j;                         // bytes of the rows from src on
-    uint32_t w_stage = 0;
-    auto issue = [&]() {
-        const uint8_t *s = src;
+
+    // Codes: 16-byte piece j of each 64 bytes of column n of each eight, where the reads of a piece's
+    // words meet no bank twice.  (Columns behind the last are the last: their sums are not used.)
+    const uint8_t *src = p.W + n0 * p.pitch;
+    int col_at[NT];
 #pragma unroll
-        for (int t = 0; t < NT; ++t, s += step) {
-            const bool in = left > 0 && 8 * t + n < cols;
-            cp_async_16(w_to + w_stage + t * 512, in ? s : p.W, in ? 16u : 0u);
+    for (int t = 0; t < NT; ++t) col_at[t] = min(8 * t + n, cols - 1) * p.pitch;
+    const uint32_t w_to = n * 64 + ((j ^ (n >> 1)) & 3) * 16;
+    // X: elements 8 lane .. 8 lane + 7 of the chunk
+    const uint8_t *xs = p.X + (int64_t)m0 * p.K * (X_LANE / 8) + lane * X_LANE;
+    const int64_t x_step = (int64_t)p.K * (X_LANE / 8);
+    const bool fours = (p.N & 3) == 0;                               // scales of four columns are aligned
+    uint32_t stage_to = ring;
+    int c_to = warp;                                                 // chunk that is copied next
+    auto issue = [&]() {
+        const int k_at = c_to * 128 + 16 * j;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const bool in = k_at + 64 * h < p.pitch;
+            const uint8_t *s = src + (in ? k_at + 64 * h : 0);
+            const uint32_t bytes = in ? 16u : 0u;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) cp_async_16(stage_to + w_to + (2 * t + h) * 512, s + col_at[t], bytes);
         }
-        src += WARPS * 64;
-        left -= WARPS * 64;
-        w_stage = w_stage == (STAGES - 1) * L::W_BYTES ? 0u : w_stage + L::W_BYTES;
-        cp_async_commit();
-    };
-    // X: elements 4 lane .. 4 lane + 3 of the chunk; scales of columns 8 t + 2 j and + 1
-    uint2 x[ROWS];
-    float2 sc[FLUSHES][NT];
-    const uint8_t *xs = p.X + ((int64_t)m0 * p.K + warp * 128 + 4 * lane) * (INT ? 1 : 2);
-    const bool pairs = (p.N & 1) == 0;
-    auto load = [&](int i) {
-        const int k = (warp + i * WARPS) * 128 + 4 * lane;
+        const uint32_t s_to = stage_to + L::W_BYTES;
+        if (fours) {
+#pragma unroll
+            for (int e = lane; e < FLUSHES * NT * 2; e += 32) {
+                const int f = e / (NT * 2), c = e % (NT * 2) * 4, g = p.group_of((uint32_t)(c_to * FLUSHES + f));
+                const bool in = g < p.groups && c < cols;
+                cp_async_16(s_to + e * 16, in ? p.scales + (int64_t)g * p.N + n0 + c : p.scales, in ? 16u : 0u);
+            }
+        } else {
+#pragma unroll
+            for (int e = lane; e < FLUSHES * NT * 8; e += 32) {
+                const int f = e / (NT * 8), c = e % (NT * 8), g = p.group_of((uint32_t)(c_to * FLUSHES + f));
+                const bool in = g < p.groups && c < cols;
+                cp_async_small<4>(s_to + e * 4, in ? p.scales + (int64_t)g * p.N + n0 + c : p.scales, in ? 4u : 0u);
+            }
+        }
+        const bool x_in = c_to * 256 + 8 * lane < p.K;
+        const uint8_t *xm = xs + (x_in ? c_to * (32 * X_LANE) : 0);
 #pragma unroll
         for (int m = 0; m < ROWS; ++m) {
-            x[m] = make_uint2(0u, 0u);
-            if (i < turns && m < rows && k < p.K) {
-                const uint8_t *at = xs + (int64_t)m * p.K * (INT ? 1 : 2);
-                if (INT) x[m].x = __ldg(reinterpret_cast<const uint32_t *>(at));
-                else x[m] = __ldg(reinterpret_cast<const uint2 *>(at));
-            }
+            const bool in = x_in && m < rows;
+            cp_async_small<X_LANE>(s_to + L::S_BYTES + m * L::X_ROW + lane * X_LANE, in ? xm + m * x_step : p.X,
+                                   in ? X_LANE : 0u);
         }
-        xs += WARPS * 128 * (INT ? 1 : 2);
-#pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) {
-            const int g = p.group_of((uint32_t)((warp + i * WARPS) * FLUSHES + f));
-            const bool in = i < turns && g < p.groups;
-            const float *s = p.scales + (int64_t)g * p.N + n0 + 2 * j;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const int c = 8 * t + 2 * j;
-                sc[f][t] = make_float2(0.f, 0.f);
-                if (pairs) {
-                    if (in && c < cols) sc[f][t] = __ldg(reinterpret_cast<const float2 *>(s + 8 * t));
-                } else {
-                    if (in && c < cols) sc[f][t].x = __ldg(s + 8 * t);
-                    if (in && c + 1 < cols) sc[f][t].y = __ldg(s + 8 * t + 1);
-                }
-            }
-        }
+        c_to += WARPS;
+        stage_to = stage_to == ring + (STAGES - 1) * L::STAGE ? ring : stage_to + L::STAGE;
     };
 
     grid_dependency_wait();
     grid_launch_dependents();
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) issue();
-    load(0);
+    for (int s = 0; s < STAGES - 1; ++s) {
+        if (s < turns) issue();
+        cp_async_commit();
+    }
 
-    float total[NT][SLOTS];
+    float total[NT][2 * HALVES];
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int e = 0; e < SLOTS; ++e) total[t][e] = 0.f;
+        for (int e = 0; e < 2 * HALVES; ++e) total[t][e] = 0.f;
     const uint32_t one = p.odd ? 0x08080808u : 0u;
-    const uint32_t w_at = ring + n * 64 + 4 * j;
-    uint32_t r_stage = 0;
+    const uint32_t w_at = GP == 4 ? w_to : n * 64 + 4 * j;
+    uint32_t at = ring;
 
 #pragma unroll 1
     for (int i = 0; i < turns; ++i) {
         cp_async_wait<STAGES - 2>();
         __syncwarp();             // the stage is here; the last one, and the digits, have been read
-        issue();
-        // digits of X; what this lane's rows of sums (n, n + 8) are multiples of
+        if (i + STAGES - 1 < turns) issue();
+        cp_async_commit();
+        // digits of X, in the order in which codes come out of their words; what this lane's rows of
+        // sums (n, n + 8) are multiples of
         float up[2] = {1.f, 1.f};
-        if (INT) {
+        const uint32_t s_at = at + L::W_BYTES, x_at = s_at + L::S_BYTES + lane * X_LANE;
 #pragma unroll
-            for (int m = 0; m < ROWS; ++m)
-                if (m < rows) sts_32(digits + m * ROW + 4 * lane, x[m].x);
-        } else {
-#pragma unroll
-            for (int m = 0; m < ROWS; ++m) {
-                if (m >= rows) break;
-                float f[4];
+        for (int m = 0; m < ROWS; ++m) {
+            if (m >= rows) break;
+            const uint32_t to = digits + DIGITS * m * ROW + 8 * lane;
+            if constexpr (INT) {
+                const uint2 x = lds_64(x_at + m * L::X_ROW);
+                sts_64(to, __byte_perm(x.x, x.y, 0x6420), __byte_perm(x.x, x.y, 0x7531));
+            } else {
+                const uint4 x = lds_128(x_at + m * L::X_ROW);
+                constexpr uint32_t ABS = 0x7FFF7FFFu, INF = XT == DSQ_BF16 ? 0x7F80u : 0x7C00u;
+                const uint32_t t2 = __vmaxu2(__vmaxu2(x.x & ABS, x.y & ABS), __vmaxu2(x.z & ABS, x.w & ABS));
+                const uint32_t top = __reduce_max_sync(~0u, max(t2 & 0xFFFFu, t2 >> 16));
+                float f[8];
+                DsqRaw8<__half> raw;
+                raw.v[0] = x;
+                uint32_t e;                      // the largest's exponent, as binary32 keeps it
                 if (XT == DSQ_BF16) {
-                    f[0] = __uint_as_float(x[m].x << 16); f[1] = __uint_as_float(x[m].x & 0xFFFF0000u);
-                    f[2] = __uint_as_float(x[m].y << 16); f[3] = __uint_as_float(x[m].y & 0xFFFF0000u);
+                    dsq_unpack8(reinterpret_cast<const DsqRaw8<__nv_bfloat16> &>(raw), f);
+                    e = top >> 7;
                 } else {
-                    const float2 a = __half22float2(*reinterpret_cast<const __half2 *>(&x[m].x));
-                    const float2 b = __half22float2(*reinterpret_cast<const __half2 *>(&x[m].y));
-                    f[0] = a.x; f[1] = a.y; f[2] = b.x; f[3] = b.y;
+                    dsq_unpack8(raw, f);
+                    e = __float_as_uint(__half2float(__ushort_as_half((unsigned short)top))) >> 23;
                 }
-                uint32_t top = 0;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) top = max(top, __float_as_uint(f[e]) & 0x7FFFFFFFu);
-                top = __reduce_max_sync(~0u, top);
-                // 2^(21 - e) of the largest's exponent e, and its inverse (rows with an infinity or a NaN: NaN)
-                const uint32_t e = max(top >> 23, 22u);
+                // times 2^(21 - e), and back (rows with an infinity or a NaN: NaN)
+                e = max(e, 22u);
                 const float scale = __uint_as_float((275u - e) << 23);
-                const float inv = top >= 0x7F800000u ? __uint_as_float(0x7FC00000u) : __uint_as_float((e - 21u) << 23);
-                uint32_t v[4];
+                const float inv = top >= INF ? __uint_as_float(0x7FC00000u) : __uint_as_float((e - 21u) << 23);
+                uint32_t v[8];
 #pragma unroll
-                for (int k = 0; k < 4; ++k)      // the integer plus 0x8080: its low bytes are digits plus 128
+                for (int k = 0; k < 8; ++k)      // the integer plus 0x8080: its low bytes are digits plus 128
                     v[k] = __float_as_uint(__fmaf_rn(f[k], scale, 12582912.f)) + (0x8080u - 0x4B400000u);
-                const uint32_t a = __byte_perm(v[0], v[1], 0x5140), b = __byte_perm(v[2], v[3], 0x5140);
-                const uint32_t to = digits + 3 * m * ROW + 4 * lane;
-                sts_32(to, __byte_perm(__byte_perm(v[0], v[1], 0x0062), __byte_perm(v[2], v[3], 0x0062), 0x5410));
-                sts_32(to + ROW, __byte_perm(a, b, 0x7632) ^ 0x80808080u);
-                sts_32(to + 2 * ROW, __byte_perm(a, b, 0x5410) ^ 0x80808080u);
-                if (n / 3 == m) up[0] = inv;
-                if ((n + 8) / 3 == m) up[1] = inv;
+                uint32_t d[3][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t a = __byte_perm(v[h], v[h + 2], 0x5140), b = __byte_perm(v[h + 4], v[h + 6], 0x5140);
+                    d[0][h] = __byte_perm(__byte_perm(v[h], v[h + 2], 0x0062), __byte_perm(v[h + 4], v[h + 6], 0x0062), 0x5410);
+                    d[1][h] = __byte_perm(a, b, 0x7632) ^ 0x80808080u;
+                    d[2][h] = __byte_perm(a, b, 0x5410) ^ 0x80808080u;
+                }
+#pragma unroll
+                for (int k = 0; k < 3; ++k) sts_64(to + k * ROW, d[k][0], d[k][1]);
+                if (ROWS == 1 || n / 3 == m) up[0] = inv;
+                if (HALVES == 2 && (n + 8) / 3 == m) up[1] = inv;
             }
         }
-        float2 now[FLUSHES][NT];
-#pragma unroll
-        for (int f = 0; f < FLUSHES; ++f)
-#pragma unroll
-            for (int t = 0; t < NT; ++t) now[f][t] = sc[f][t];
-        load(i + 1);
         __syncwarp();
-        int acc[NT][4];
+        // Operands: with groups of whole 128s lane j takes the four words of a 16-byte piece one after the
+        // other (its codes 32 j .. 32 j + 31), else word j of each piece.
+        uint32_t w[2][NT][4], a[8][2 * HALVES];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            if (q % GP == 0) {
-#pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[t][e] = 0;
-            }
-            uint32_t a[4] = {0u, 0u, 0u, 0u};
-#pragma unroll
-            for (int h = 0; h < (L::HALF ? 1 : 2); ++h)
-                if (n + 8 * h < rows * DIGITS) {
-                    const uint2 v = lds_64(digits + (n + 8 * h) * ROW + q * 32 + 8 * j);
-                    a[h] = __byte_perm(v.x, v.y, 0x6420);
-                    a[h + 2] = __byte_perm(v.x, v.y, 0x7531);
-                }
+        for (int h = 0; h < 2; ++h) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const uint32_t w = lds_32(w_at + r_stage + t * 512 + ((q ^ (n >> 1)) & 3) * 16);
-                mma_i8(acc[t], a, ((w << 4) & 0xF0F0F0F0u) | one, (w & 0xF0F0F0F0u) | one);
+                const uint32_t from = at + w_at + (2 * t + h) * 512;
+                if (GP == 4) {
+                    const uint4 v = lds_128(from);
+                    w[h][t][0] = v.x; w[h][t][1] = v.y; w[h][t][2] = v.z; w[h][t][3] = v.w;
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) w[h][t][q] = lds_32(from + ((q ^ (n >> 1)) & 3) * 16);
+                }
+            }
+#pragma unroll
+            for (int r = 0; r < HALVES; ++r) {
+                const uint32_t from = digits + (n + 8 * r) * ROW + 128 * h;
+                const bool in = n + 8 * r < rows * DIGITS;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) a[4 * h + q][2 * r] = a[4 * h + q][2 * r + 1] = 0u;
+                if (GP == 4) {
+#pragma unroll
+                    for (int q = 0; q < 4; q += 2)
+                        if (in) {
+                            const uint4 v = lds_128(from + 32 * j + 8 * q);
+                            a[4 * h + q][2 * r] = v.x; a[4 * h + q][2 * r + 1] = v.y;
+                            a[4 * h + q + 1][2 * r] = v.z; a[4 * h + q + 1][2 * r + 1] = v.w;
+                        }
+                } else {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        if (in) {
+                            const uint2 v = lds_64(from + 32 * q + 8 * j);
+                            a[4 * h + q][2 * r] = v.x; a[4 * h + q][2 * r + 1] = v.y;
+                        }
+                }
+            }
+        }
+        int acc[NT][4];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const uint32_t rows_of[4] = {a[q][0], HALVES == 2 ? a[q][2 * HALVES - 2] : 0u, a[q][1],
+                                         HALVES == 2 ? a[q][2 * HALVES - 1] : 0u};
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const uint32_t c = w[q >> 2][t][q & 3];
+                const uint32_t b0 = ((c << 4) & 0xF0F0F0F0u) | one, b1 = (c & 0xF0F0F0F0u) | one;
+                if (q % GP == 0) mma_i8_first(acc[t], rows_of, b0, b1);
+                else mma_i8(acc[t], rows_of, b0, b1);
             }
             if (q % GP == GP - 1) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const float2 s = now[q / GP][t];
+                    const uint2 sv = lds_64(s_at + ((q / GP) * NT * 8 + 8 * t + 2 * j) * 4);
+                    const float s0 = __uint_as_float(sv.x), s1 = __uint_as_float(sv.y);
 #pragma unroll
-                    for (int h = 0; h < SLOTS / 2; ++h) {
-                        total[t][2 * h] = __fmaf_rn((float)acc[t][2 * h] * up[h], s.x, total[t][2 * h]);
-                        total[t][2 * h + 1] = __fmaf_rn((float)acc[t][2 * h + 1] * up[h], s.y, total[t][2 * h + 1]);
+                    for (int h = 0; h < HALVES; ++h) {
+                        float v0 = (float)acc[t][2 * h], v1 = (float)acc[t][2 * h + 1];
+                        if (!INT) {
+                            v0 *= up[h];
+                            v1 *= up[h];
+                        }
+                        total[t][2 * h] = __fmaf_rn(v0, s0, total[t][2 * h]);
+                        total[t][2 * h + 1] = __fmaf_rn(v1, s1, total[t][2 * h + 1]);
                     }
                 }
             }
         }
-        r_stage = r_stage == (STAGES - 1) * L::W_BYTES ? 0u : r_stage + L::W_BYTES;
+        at = at == ring + (STAGES - 1) * L::STAGE ? ring : at + L::STAGE;
     }
     cp_async_wait<0>();
     __syncthreads();
     float *sums = reinterpret_cast<float *>(smem);          // [WARPS][rows of digits][8 NT columns]
-    constexpr int R = L::HALF ? 8 : 16, C = 8 * NT;
+    constexpr int R = 8 * HALVES, C = 8 * NT;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
 #pragma unroll
-        for (int h = 0; h < SLOTS / 2; ++h)
+        for (int h = 0; h < HALVES; ++h)
             *reinterpret_cast<float2 *>(sums + (warp * R + n + 8 * h) * C + 8 * t + 2 * j) =
                 make_float2(total[t][2 * h], total[t][2 * h + 1]);
     __syncthreads();
@@ -266,12 +328,12 @@ template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> int launch(co
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
 {
     if constexpr (XT == DSQ_I8) {
-        if (p.M <= 8) return launch<XT, 8, 4, GP, 8, 4>(p, s);
-        return launch<XT, 16, 4, GP, 8, 4>(p, s);
+        if (p.M <= 8) return launch<XT, 8, 4, GP, 8, 2>(p, s);
+        return launch<XT, 16, 4, GP, 8, 2>(p, s);
     } else {
-        if (p.M == 1) return launch<XT, 1, 4, GP, 8, 4>(p, s);
-        if (p.M == 2) return launch<XT, 2, 4, GP, 8, 4>(p, s);
-        return launch<XT, 5, 4, GP, 8, 4>(p, s);
+        if (p.M == 1) return launch<XT, 1, 4, GP, 8, 2>(p, s);
+        if (p.M == 2) return launch<XT, 2, 4, GP, 8, 2>(p, s);
+        return launch<XT, 5, 4, GP, 8, 2>(p, s);
     }
 }
 
