@@ -56,25 +56,54 @@ __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[8]) { tmem_ld
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x16(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32(at, r); }
 
-// One instruction (32 bytes of K) with A in tensor memory, issued by one elected lane of a
-// converged warp.
-template <bool INT>
+// COUNT instructions (32 bytes of K each) with A in tensor memory, issued by one elected lane of a
+// converged warp; the first takes the accumulate flag.
+#define DSQ_TS_1(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, pe;\n\t.reg .b64 d0;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 d0, {%2, %3};\n\t" \
+                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+#define DSQ_TS_2(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1;\n\t.reg .b32 l1, a1;\n\t"                    \
+                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\tadd.u32 l1, %2, 2;\n\tadd.u32 a1, %1, 8;\n\t" \
+                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\telect.sync _|pe, 0xffffffff;\n\t"          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+#define DSQ_TS_4(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1, d2, d3;\n\t.reg .b32 l1, l2, l3, a1, a2, a3;\n\t" \
+                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\t"                                       \
+                 "add.u32 l1, %2, 2;\n\tadd.u32 l2, %2, 4;\n\tadd.u32 l3, %2, 6;\n\t"                         \
+                 "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"                       \
+                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\tmov.b64 d2, {l2, %3};\n\tmov.b64 d3, {l3, %3};\n\t" \
+                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a2], d2, %4, q;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a3], d3, %4, q;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+template <bool INT, int COUNT>
 __device__ __forceinline__ void mma_ts_elect(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
                                              uint32_t accumulate)
 {
-    if (INT)
-        asm volatile("{\n\t.reg .pred p, pe;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
-                     "elect.sync _|pe, 0xffffffff;\n\t"
-                     "@pe tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], db, %4, p;\n\t}" ::"r"(d),
-                     "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
-                     : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p, pe;\n\t.reg .b64 db;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 db, {%2, %3};\n\t"
-                     "elect.sync _|pe, 0xffffffff;\n\t"
-                     "@pe tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], db, %4, p;\n\t}" ::"r"(d),
-                     "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)
-                     : "memory");
+    static_assert(COUNT == 1 || COUNT == 2 || COUNT == 4, "instructions of a block");
+    if constexpr (COUNT == 1) {
+        if (INT) DSQ_TS_1("i8");
+        else DSQ_TS_1("f16");
+    } else if constexpr (COUNT == 2) {
+        if (INT) DSQ_TS_2("i8");
+        else DSQ_TS_2("f16");
+    } else {
+        if (INT) DSQ_TS_4("i8");
+        else DSQ_TS_4("f16");
+    }
 }
+#undef DSQ_TS_1
+#undef DSQ_TS_2
+#undef DSQ_TS_4
 
 // once a wait has run out, instructions in flight get this long before their memory is given up
 constexpr unsigned long long DRAIN_NS = 20000000ull;
@@ -157,49 +186,65 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     const uint32_t tmem = lds_32(slot) + team * L::TEAM_COLS;
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);    // this warp's 32 lanes
 
-    // copies of this warp's 32 rows of the team's i-th chunk
-    auto issue_w = [&](int i) {
-        if (i < turns) {
-            const int c = c0 + team + i * TEAMS;
-            const uint32_t at = ring + (uint32_t)(i % STAGES * L::STAGE);
-            const int j = lane & 3;
+    // Copies of this warp's 32 rows of the team's next chunk: 16-byte piece j of a row's 64.  (Rows behind
+    // the last are the last: their sums are not used.)
+    const int j = lane & 3, mine = (warp & 3) * 32 + (lane >> 2);
+    const uint8_t *src = p.W + n0 * p.pitch;
+    const int last = (int)min((int64_t)127, p.N - 1 - n0);
+    int row_at[4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int r = (warp & 3) * 32 + 8 * k + (lane >> 2);
-                const bool in = n0 + r < p.N && c * 64 + 16 * j < p.pitch;
-                cp_async_16(at + r * 64 + ((j ^ (r >> 1)) & 3) * 16,
-                            in ? p.W + (n0 + r) * p.pitch + c * 64 + 16 * j : p.W, in ? 16u : 0u);
-            }
+    for (int k = 0; k < 4; ++k) row_at[k] = min(mine + 8 * k, last) * p.pitch;
+    const uint32_t w_to = mine * 64 + ((j ^ (mine >> 1)) & 3) * 16;
+    int w_left = turns, w_k = (c0 + team) * 64 + 16 * j;
+    uint32_t w_stage = ring;
+    auto issue_w = [&]() {
+        if (w_left > 0) {
+            const bool in = w_k < p.pitch;
+            const uint8_t *s = src + (in ? w_k : 0);
+            const uint32_t bytes = in ? 16u : 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) cp_async_16(w_stage + w_to + k * 512, s + row_at[k], bytes);
         }
+        --w_left;
+        w_k += TEAMS * 64;
+        w_stage = w_stage == ring + (STAGES - 1) * L::STAGE ? ring : w_stage + L::STAGE;
         cp_async_commit();
     };
-    // X of a chunk: 16-byte pieces of its rows, spread over the team
-    constexpr int PIECES = INT ? 8 : 16, XP = (MC * PIECES + 127) / 128;
+    // X of a chunk: 16-byte pieces of its rows, spread over the team: piece pc of rows r0, r0 + RS, ...
+    constexpr int PIECES = INT ? 8 : 16, RS = 128 / PIECES, XP = (MC + RS - 1) / RS;
+    constexpr int ELEMENT = INT ? 1 : 2;
+    const int pc = row % PIECES, r0 = row / PIECES;
+    const uint8_t *xsrc = p.X + ((int64_t)(m0 + r0) * p.K) * ELEMENT + 16 * pc;
+    const int64_t x_step = (int64_t)RS * p.K * ELEMENT;
+    const uint32_t x_to = xbuf + (pc >> 3) * (L::NC * 128) + r0 * 128 + (((pc & 7) ^ (r0 & 7)) << 4);
+    static_assert(RS % 8 == 0, "the swizzle of a thread's rows is one");
     uint4 x[XP];
     float sc[FLUSHES];
-    auto load = [&](int i) {
-        const int c = c0 + team + i * TEAMS;
+    int l_left = turns, l_chunk = c0 + team;
+    auto load = [&]() {
+        const int k_at = l_chunk * (PIECES * 16);                 // bytes into the row
+        const bool in = l_left > 0 && k_at + 16 * pc < p.K * ELEMENT;
+        const uint8_t *s = xsrc + (in ? k_at : 0);
 #pragma unroll
-        for (int k = 0; k < XP; ++k) {
-            const int s = row + 128 * k, r = s / PIECES, pc = s % PIECES;
-            const int at = c * (PIECES * 16) + 16 * pc;           // bytes into the row
+        for (int k = 0; k < XP; ++k, s += x_step) {
             x[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (i < turns && r < rows && at < p.K * (INT ? 1 : 2))
-                x[k] = __ldg(reinterpret_cast<const uint4 *>(p.X + (int64_t)(m0 + r) * p.K * (INT ? 1 : 2) + at));
+            if (in && r0 + k * RS < rows) x[k] = __ldg(reinterpret_cast<const uint4 *>(s));
         }
 #pragma unroll
         for (int f = 0; f < FLUSHES; ++f) {
-            const int g = p.group_of((uint32_t)(c * FLUSHES + f));
+            const int g = p.group_of((uint32_t)(l_chunk * FLUSHES + f));
             sc[f] = 0.f;
-            if (i < turns && g < p.groups && n0 + row < p.N) sc[f] = __ldg(p.scales + (int64_t)g * p.N + n0 + row);
+            if (l_left > 0 && g < p.groups && row <= last) sc[f] = __ldg(p.scales + (int64_t)g * p.N + n0 + row);
         }
+        --l_left;
+        l_chunk += TEAMS;
     };
 
     grid_dependency_wait();
     grid_launch_dependents();
 #pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) issue_w(s);
-    load(0);
+    for (int s = 0; s < STAGES - 1; ++s) issue_w();
+    load();
 
     float total[MC];
 #pragma unroll
@@ -210,6 +255,7 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     bool ok = true;
     uint32_t unit = 0, flush = 0;             // of the team so far
     float pending = 0.f;                      // scale of the sums that wait in D
+    uint32_t r_stage = ring;
 
     // every phase of a barrier is waited for by every thread before the next can end
     auto wait_unit = [&](uint32_t u) {
@@ -235,15 +281,14 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     for (int i = 0; i < turns; ++i) {
         cp_async_wait<STAGES - 2>();
         __syncwarp();             // the chunk's codes are here, and those of the last one have been read
-        issue_w(i + STAGES - 1);
+        issue_w();
         // X: the instructions of the chunk before the last, which read this buffer, are done
         const uint32_t xb = xbuf + (i & 1) * L::XBUF;
 #pragma unroll
         for (int k = 0; k < XP; ++k) {
-            const int s = row + 128 * k, r = s / PIECES, pc = s % PIECES;
-            if (r < rows) {
+            if (r0 + k * RS < rows) {
                 const uint4 v = x[k];
-                const uint32_t to = xb + (pc >> 3) * (L::NC * 128) + r * 128 + (((pc & 7) ^ (r & 7)) << 4);
+                const uint32_t to = x_to + (i & 1) * L::XBUF + k * (RS * 128);
                 if (INT)
                     sts_128(to, __byte_perm(v.x, v.y, 0x6420), __byte_perm(v.x, v.y, 0x7531),
                             __byte_perm(v.z, v.w, 0x6420), __byte_perm(v.z, v.w, 0x7531));
@@ -256,8 +301,9 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
         float now[FLUSHES];
 #pragma unroll
         for (int f = 0; f < FLUSHES; ++f) now[f] = sc[f];
-        load(i + 1);
-        const uint32_t codes = ring + (uint32_t)(i % STAGES * L::STAGE) + row * 64;
+        load();
+        const uint32_t codes = r_stage + row * 64;
+        r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
 #pragma unroll
         for (int u = 0; u < L::UNITS; ++u, ++unit) {
             // the values of this row's codes
@@ -288,10 +334,8 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                 const int at = u * L::UC * (INT ? 1 : 2);         // bytes into the chunk's rows
                 const uint64_t desc = smem_desc_sw128(xb + (at >> 7) * (L::NC * 128) + (at & 127));
                 const uint32_t d = tmem + (flush & 1) * L::NC;
-#pragma unroll
-                for (int k = 0; k < L::AC / 8; ++k)
-                    mma_ts_elect<INT>(d, tmem + L::A_COL + (unit & 1) * L::AC + 8 * k, (uint32_t)desc + 2 * k,
-                                      (uint32_t)(desc >> 32), idesc, (u % L::PER_FLUSH) || k);
+                mma_ts_elect<INT, L::AC / 8>(d, tmem + L::A_COL + (unit & 1) * L::AC, (uint32_t)desc,
+                                             (uint32_t)(desc >> 32), idesc, u % L::PER_FLUSH);
                 mma_commit_elect(bars + 8 * (unit & 1));
                 __syncwarp();
             }
