@@ -62,7 +62,8 @@ template <int XT> __device__ __forceinline__ uint32_t dsq_value_pair(uint32_t w,
     constexpr uint32_t MASK = (0xFu << AT) * 0x00010001u;
     constexpr uint32_t FLIP = ((XT == DSQ_BF16 ? 0x3F80u : 0x3C00u) ^ (8u << AT)) * 0x00010001u;
     const uint32_t y = 4 * i > AT ? w >> (4 * i - AT) : w << (AT - 4 * i);
-    const uint32_t v = (y & MASK) ^ FLIP;
+    uint32_t v;                       // (y & MASK) ^ FLIP: as C, with two constants, it is two instructions
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(v) : "r"(y), "r"(MASK), "r"(FLIP));
     if (XT == DSQ_BF16) {
         const __nv_bfloat162 r = __hsub2(*reinterpret_cast<const __nv_bfloat162 *>(&v),
                                          *reinterpret_cast<const __nv_bfloat162 *>(&base));

@@ -10,14 +10,15 @@
 // traffic through registers: at 8192 x 8192 with bf16 rows mma.sync took 23 us for one row and
 // 64 us for 64, issue-bound.
 //
-//   * Four warps (a team) take a chunk of 128 codes of the block's 128 rows: codes from the
-//     team's ring in shared memory (cp.async, each warp its own 32 rows), X of the chunk
-//     from global memory through registers, permuted to the order in which codes come out of
-//     their words, into the 128-byte swizzle.  A unit of 32 tensor-memory columns (64 codes
-//     as 16-bit values, 128 as int8; less where a group ends sooner) is written while the
-//     instructions of the unit before run: two buffers of A and of D a team.
-//   * Teams of a block take its chunks in turn; blocks of a cluster share K and add their
-//     totals through distributed shared memory.  All sums are in a fixed order.
+//   * TEAMS of four warps take the block's chunks of 128 codes of 128 rows in turn: codes from the team's
+//     ring in shared memory (cp.async, each warp its own 32 rows), X of the chunk from global memory
+//     through registers, permuted to the order in which codes come out of their words, into the
+//     128-byte swizzle.  One warp of the team issues the instructions.
+//   * Four more warps take the sums: a chunk's (a group's, where groups end sooner) lie in one of the
+//     team's places in tensor memory; they read them, give the place back and add.  Making values and
+//     adding sums are both bound by issue slots and by latencies, and with the totals out of the
+//     teams' registers 16 warps fit (two teams that did both took 34 us for 64 rows at 8192 x 8192).
+//   * Blocks of a cluster share K and add their totals through distributed shared memory, in order.
 //   * Exactly one block is on an SM (its shared memory sees to that): blocks of a cluster
 //     wait for one another, and must not wait for tensor memory meanwhile.
 //
@@ -36,12 +37,6 @@ using namespace dsq_ptx;
 
 namespace {
 
-__device__ __forceinline__ void tmem_st_32x8(uint32_t taddr, const uint32_t (&r)[8])
-{
-    asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr),
-                 "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
-                 : "memory");
-}
 __device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8])
 {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
@@ -49,9 +44,6 @@ __device__ __forceinline__ void tmem_ld_32x8(uint32_t taddr, uint32_t (&r)[8])
                  : "r"(taddr)
                  : "memory");
 }
-__device__ __forceinline__ void st_cols(uint32_t at, const uint32_t (&r)[8]) { tmem_st_32x8(at, r); }
-__device__ __forceinline__ void st_cols(uint32_t at, const uint32_t (&r)[16]) { tmem_st_32x16(at, r); }
-__device__ __forceinline__ void st_cols(uint32_t at, const uint32_t (&r)[32]) { tmem_st_32x32(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[8]) { tmem_ld_32x8(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x16(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32(at, r); }
@@ -105,6 +97,20 @@ __device__ __forceinline__ void mma_ts_elect(uint32_t d, uint32_t a, uint32_t b_
 #undef DSQ_TS_2
 #undef DSQ_TS_4
 
+// loads that stay where they stand: a turn ahead of their use
+__device__ __forceinline__ uint4 load_ahead(const uint8_t *p)
+{
+    uint4 v;
+    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    return v;
+}
+__device__ __forceinline__ float load_ahead(const float *p)
+{
+    float v;
+    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
+    return v;
+}
+
 // once a wait has run out, instructions in flight get this long before their memory is given up
 constexpr unsigned long long DRAIN_NS = 20000000ull;
 
@@ -114,7 +120,7 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, unsigned l
     uint64_t t0, t;
     asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t0));
     for (uint32_t it = 1;; ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
+        if (mbar_try_wait(bar, parity, 20u)) return true;
         if ((it & 15u) == 0u) {
             asm volatile("mov.u64 %0, %%globaltimer;" : "=l"(t));
             if (t - t0 > limit_ns) return false;
@@ -123,40 +129,44 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, unsigned l
 }
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
 {
-    bool ok = mbar_try_wait(bar, parity);
+    bool ok = mbar_try_wait(bar, parity, 20u);
     if (!ok) ok = wait_slow(bar, parity, limit_ns);
     return __all_sync(~0u, ok);
 }
 
-// MC: columns of D that are read (rows of X); GP: pieces of 32 codes between two readings of D;
-// TEAMS of four warps; STAGES of a team's ring
+// MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum
 template <int XT, int MC, int GP, int TEAMS, int STAGES> struct Layout {
     static constexpr bool INT = XT == DSQ_I8;
     static constexpr int NC = MC < 16 ? 16 : MC;                  // columns of an instruction
-    static constexpr int UC = INT ? 32 * GP : GP >= 2 ? 64 : 32;  // codes of a unit
-    static constexpr int UNITS = 128 / UC;                        // of a chunk
-    static constexpr int PER_FLUSH = 32 * GP / UC;
-    static constexpr int AC = INT ? UC / 4 : UC / 2;              // tensor-memory columns of a unit
-    static constexpr int A_COL = 2 * NC;                          // behind the two buffers of D
-    static constexpr int TEAM_COLS = (2 * NC + 2 * AC + 31) / 32 * 32;
-    static constexpr int COLS = TEAMS * TEAM_COLS <= 128 ? 128 : TEAMS * TEAM_COLS <= 256 ? 256 : 512;
+    static constexpr int FLUSHES = 4 / GP;                        // sums of a chunk
+    static constexpr int AC = INT ? 32 : 64;                      // tensor-memory columns of a chunk's values
+    // places of a team for its sums (a power of two): the phases of a place's barriers are waited for in
+    // order by the team's issuing warp, so no two teams share one
+    static constexpr int ABUF = TEAMS * (2 * AC + NC) <= 512 ? 2 : 1;         // buffers of a team's values
+    static constexpr int ROOM = (512 - TEAMS * ABUF * AC) / (TEAMS * NC), PLACES = ROOM >= 4 ? 4 : ROOM >= 2 ? 2 : 1;
+    static constexpr int SLOTS = TEAMS * PLACES;
+    static constexpr int A_COL = SLOTS * NC;
+    static constexpr int USED = A_COL + TEAMS * ABUF * AC;
+    static constexpr int COLS = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
     static constexpr int XBUF = NC * (INT ? 128 : 256);
     static constexpr int X_AT = 1024, RING_AT = X_AT + TEAMS * 2 * XBUF;
     static constexpr int STAGE = 128 * 64;
     static constexpr int BYTES = RING_AT + TEAMS * STAGES * STAGE + 1024;    // (its start is aligned to 1024)
-    static constexpr int SUMS = TEAMS * MC * 512;
-    static_assert(TEAMS * TEAM_COLS <= 512, "tensor memory");
+    static constexpr int THREADS = (TEAMS + 1) * 128;
+    // barriers: sums ready and place free of each slot, values read of each team
+    static constexpr int READY = 16, FREE = READY + 8 * SLOTS, READ = FREE + 8 * SLOTS;
+    static_assert(ROOM >= 1 && USED <= 512 && READ + 16 * TEAMS <= X_AT, "tensor memory");
     static_assert(BYTES <= 227 * 1024 && BYTES > 116 * 1024, "one block an SM");
-    static_assert(SUMS <= TEAMS * STAGES * STAGE, "the sums take the rings' place");
+    static_assert(MC * 512 <= TEAMS * STAGES * STAGE, "the totals take the rings' place");
 };
 
 template <int XT, int MC, int GP, int TEAMS, int STAGES>
-__global__ void __launch_bounds__(TEAMS * 128, 1)
+__global__ void __launch_bounds__((TEAMS + 1) * 128, 1)
 wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long long wait_ns)
 {
     using L = Layout<XT, MC, GP, TEAMS, STAGES>;
     constexpr bool INT = L::INT;
-    constexpr int FLUSHES = 4 / GP;
+    constexpr int FLUSHES = L::FLUSHES;
     extern __shared__ uint8_t raw_smem[];
     const uint32_t smem = (smem_u32(raw_smem) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -166,127 +176,104 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     const int m0 = blockIdx.y * MC;
     const int rows = min(p.M - m0, MC);
     const int all = (p.K + 127) >> 7;
-    const int c0 = (int)((int64_t)all * rank / split), c1 = (int)((int64_t)all * (rank + 1) / split);
-    const int turns = c0 + team < c1 ? (c1 - c0 - team - 1) / TEAMS + 1 : 0;
-    const uint32_t bars = smem + 16 + team * 16, slot = smem;
-    const uint32_t xbuf = smem + L::X_AT + team * 2 * L::XBUF;
-    const uint32_t ring = smem + L::RING_AT + team * STAGES * L::STAGE;
+    const int c0 = (int)((int64_t)all * rank / split), chunks = (int)((int64_t)all * (rank + 1) / split) - c0;
+    const int last = (int)min((int64_t)127, p.N - 1 - n0);       // row of weights of this block
 
     if (warp == 0) {
-        tmem_alloc(slot, L::COLS);
+        tmem_alloc(smem, L::COLS);
         tmem_relinquish();
     }
     if (threadIdx.x == 0) {
-        for (int i = 0; i < 2 * TEAMS; ++i) mbar_init(smem + 16 + 8 * i, 1);
+        for (int i = 0; i < L::SLOTS; ++i) {
+            mbar_init(smem + L::READY + 8 * i, 1);
+            mbar_init(smem + L::FREE + 8 * i, 4);
+        }
+        for (int i = 0; i < 2 * TEAMS; ++i) mbar_init(smem + L::READ + 8 * i, 1);
         mbar_init_fence();
     }
     tc_fence_before_sync();
     __syncthreads();
     tc_fence_after_sync();
-    const uint32_t tmem = lds_32(slot) + team * L::TEAM_COLS;
+    const uint32_t tmem = lds_32(smem);
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);    // this warp's 32 lanes
-
-    // Copies of this warp's 32 rows of the team's next chunk: 16-byte piece j of a row's 64.  (Rows behind
-    // the last are the last: their sums are not used.)
-    const int j = lane & 3, mine = (warp & 3) * 32 + (lane >> 2);
-    const uint8_t *src = p.W + n0 * p.pitch;
-    const int last = (int)min((int64_t)127, p.N - 1 - n0);
-    int row_at[4];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) row_at[k] = min(mine + 8 * k, last) * p.pitch;
-    const uint32_t w_to = mine * 64 + ((j ^ (mine >> 1)) & 3) * 16;
-    int w_left = turns, w_k = (c0 + team) * 64 + 16 * j;
-    uint32_t w_stage = ring;
-    auto issue_w = [&]() {
-        if (w_left > 0) {
-            const bool in = w_k < p.pitch;
-            const uint8_t *s = src + (in ? w_k : 0);
-            const uint32_t bytes = in ? 16u : 0u;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) cp_async_16(w_stage + w_to + k * 512, s + row_at[k], bytes);
-        }
-        --w_left;
-        w_k += TEAMS * 64;
-        w_stage = w_stage == ring + (STAGES - 1) * L::STAGE ? ring : w_stage + L::STAGE;
-        cp_async_commit();
-    };
-    // X of a chunk: 16-byte pieces of its rows, spread over the team: piece pc of rows r0, r0 + RS, ...
-    constexpr int PIECES = INT ? 8 : 16, RS = 128 / PIECES, XP = (MC + RS - 1) / RS;
-    constexpr int ELEMENT = INT ? 1 : 2;
-    const int pc = row % PIECES, r0 = row / PIECES;
-    const uint8_t *xsrc = p.X + ((int64_t)(m0 + r0) * p.K) * ELEMENT + 16 * pc;
-    const int64_t x_step = (int64_t)RS * p.K * ELEMENT;
-    const uint32_t x_to = xbuf + (pc >> 3) * (L::NC * 128) + r0 * 128 + (((pc & 7) ^ (r0 & 7)) << 4);
-    static_assert(RS % 8 == 0, "the swizzle of a thread's rows is one");
-    uint4 x[XP];
-    float sc[FLUSHES];
-    int l_left = turns, l_chunk = c0 + team;
-    auto load = [&]() {
-        const int k_at = l_chunk * (PIECES * 16);                 // bytes into the row
-        const bool in = l_left > 0 && k_at + 16 * pc < p.K * ELEMENT;
-        const uint8_t *s = xsrc + (in ? k_at : 0);
-#pragma unroll
-        for (int k = 0; k < XP; ++k, s += x_step) {
-            x[k] = make_uint4(0u, 0u, 0u, 0u);
-            if (in && r0 + k * RS < rows) x[k] = __ldg(reinterpret_cast<const uint4 *>(s));
-        }
-#pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) {
-            const int g = p.group_of((uint32_t)(l_chunk * FLUSHES + f));
-            sc[f] = 0.f;
-            if (l_left > 0 && g < p.groups && row <= last) sc[f] = __ldg(p.scales + (int64_t)g * p.N + n0 + row);
-        }
-        --l_left;
-        l_chunk += TEAMS;
-    };
-
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(smem + bar, parity, ok ? wait_ns : 0) && ok; };
     grid_dependency_wait();
     grid_launch_dependents();
-#pragma unroll
-    for (int s = 0; s < STAGES - 1; ++s) issue_w();
-    load();
 
-    float total[MC];
+    float total[MC];                                             // (of the last team's threads)
 #pragma unroll
     for (int i = 0; i < MC; ++i) total[i] = 0.f;
-    const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
-    const uint32_t base = dsq_value_base<XT>(p.odd);
-    const uint32_t one = p.odd ? 0x08080808u : 0u;
-    bool ok = true;
-    uint32_t unit = 0, flush = 0;             // of the team so far
-    float pending = 0.f;                      // scale of the sums that wait in D
-    uint32_t r_stage = ring;
-
-    // every phase of a barrier is waited for by every thread before the next can end
-    auto wait_unit = [&](uint32_t u) {
-        ok = wait_warp(bars + 8 * (u & 1), (u >> 1) & 1, ok ? wait_ns : 0) && ok;
-    };
-    // D of flush `f`, whose instructions are done: the totals take it
-    auto take = [&](uint32_t f, float s) {
-        tc_fence_after_sync();
-        const uint32_t d = lanes + (f & 1) * L::NC;
-        constexpr int STEP = MC < 32 ? MC : 32;
+    if (team < TEAMS) {
+        const uint32_t xbuf = smem + L::X_AT + team * 2 * L::XBUF;
+        const uint32_t ring = smem + L::RING_AT + team * STAGES * L::STAGE;
+        const int turns = team < chunks ? (chunks - team - 1) / TEAMS + 1 : 0;
+        // Copies of this warp's 32 rows of the team's next chunk: 16-byte piece j of a row's 64.  (Rows
+        // behind the last are the last: their sums are not used.)
+        const int j = lane & 3, mine = (warp & 3) * 32 + (lane >> 2);
+        const uint8_t *src = p.W + n0 * p.pitch;
+        int row_at[4];
 #pragma unroll
-        for (int h = 0; h < MC / STEP; ++h) {
-            uint32_t v[STEP];
-            ld_cols(d + h * STEP, v);
-            tmem_ld_wait();
+        for (int k = 0; k < 4; ++k) row_at[k] = min(mine + 8 * k, last) * p.pitch;
+        const uint32_t w_to = mine * 64 + ((j ^ (mine >> 1)) & 3) * 16;
+        int w_left = turns, w_k = (c0 + team) * 64 + 16 * j;
+        uint32_t w_stage = ring;
+        auto issue_w = [&]() {
+            if (w_left > 0) {
+                const bool in = w_k < p.pitch;
+                const uint8_t *s = src + (in ? w_k : 0);
+                const uint32_t bytes = in ? 16u : 0u;
 #pragma unroll
-            for (int i = 0; i < STEP; ++i)
-                total[h * STEP + i] = __fmaf_rn(INT ? (float)(int)v[i] : __uint_as_float(v[i]), s, total[h * STEP + i]);
-        }
-    };
-
+                for (int k = 0; k < 4; ++k) cp_async_16(w_stage + w_to + k * 512, s + row_at[k], bytes);
+            }
+            --w_left;
+            w_k += TEAMS * 64;
+            w_stage = w_stage == ring + (STAGES - 1) * L::STAGE ? ring : w_stage + L::STAGE;
+            cp_async_commit();
+        };
+        // X of a chunk: 16-byte pieces of its rows, spread over the team: piece pc of rows r0, r0 + RS, ...
+        constexpr int PIECES = INT ? 8 : 16, RS = 128 / PIECES, XP = (MC + RS - 1) / RS;
+        constexpr int ELEMENT = INT ? 1 : 2;
+        const int pc = row % PIECES, r0 = row / PIECES;
+        // (rows behind the last are the last: their columns of D are not read)
+        const uint8_t *xsrc = p.X + (int64_t)m0 * p.K * ELEMENT + 16 * pc;
+        uint32_t x_at[XP];
+#pragma unroll
+        for (int k = 0; k < XP; ++k) x_at[k] = (uint32_t)min(r0 + k * RS, rows - 1) * (uint32_t)(p.K * ELEMENT);
+        const uint32_t x_to = xbuf + (pc >> 3) * (L::NC * 128) + r0 * 128 + (((pc & 7) ^ (r0 & 7)) << 4);
+        static_assert(RS % 8 == 0 && XP * RS <= L::NC, "the swizzle of a thread's rows is one");
+        uint4 x[XP];
+        int l_left = turns, l_k = (c0 + team) * (PIECES * 16);    // bytes into the row
+        auto load_x = [&]() {
+            if (l_left > 0 && l_k + 16 * pc < p.K * ELEMENT) {
+                const uint8_t *s = xsrc + l_k;
+#pragma unroll
+                for (int k = 0; k < XP; ++k) x[k] = load_ahead(s + x_at[k]);
+            } else {
+#pragma unroll
+                for (int k = 0; k < XP; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
+            }
+            --l_left;
+            l_k += TEAMS * (PIECES * 16);
+        };
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) issue_w();
+        load_x();
+        const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
+        const uint32_t base = dsq_value_base<XT>(p.odd), one = p.odd ? 0x08080808u : 0u;
+        // instructions of the team's chunk i have read its values and X
+        auto wait_read = [&](int i) { wait(L::READ + 16 * team + 8 * (i % L::ABUF), (i / L::ABUF) & 1); };
+        uint32_t r_stage = ring;
 #pragma unroll 1
-    for (int i = 0; i < turns; ++i) {
-        cp_async_wait<STAGES - 2>();
-        __syncwarp();             // the chunk's codes are here, and those of the last one have been read
-        issue_w();
-        // X: the instructions of the chunk before the last, which read this buffer, are done
-        const uint32_t xb = xbuf + (i & 1) * L::XBUF;
+        for (int i = 0; i < turns; ++i) {
+            cp_async_wait<STAGES - 2>();
+            __syncwarp();         // the chunk's codes are here, and those of the last one have been read
+            issue_w();
+            // (X has two buffers too: its last chunk but one has been waited for)
+            if (L::ABUF == 2 && i >= 2) wait_read(i - 2);
+            const uint32_t a_col = L::A_COL + (team * L::ABUF + i % L::ABUF) * L::AC;
 #pragma unroll
-        for (int k = 0; k < XP; ++k) {
-            if (r0 + k * RS < rows) {
+            for (int k = 0; k < XP; ++k) {
                 const uint4 v = x[k];
                 const uint32_t to = x_to + (i & 1) * L::XBUF + k * (RS * 128);
                 if (INT)
@@ -296,100 +283,140 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                     sts_128(to, __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
                             __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
             }
-        }
-        fence_proxy_async_smem();
-        float now[FLUSHES];
+            fence_proxy_async_smem();
+            load_x();
+            const uint32_t codes = r_stage + row * 64;
+            r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
+            // the values of this row's codes, 32 columns at a time
 #pragma unroll
-        for (int f = 0; f < FLUSHES; ++f) now[f] = sc[f];
-        load();
-        const uint32_t codes = r_stage + row * 64;
-        r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
+            for (int h = 0; h < L::AC / 32; ++h) {
+                constexpr int P16 = INT ? 4 : 2;                  // 16-byte pieces of the row
+                uint32_t a[32];
 #pragma unroll
-        for (int u = 0; u < L::UNITS; ++u, ++unit) {
-            // the values of this row's codes
-            uint32_t a[L::AC];
+                for (int q = 0; q < P16; ++q) {
+                    const uint4 w4 = lds_128(codes + (((P16 * h + q) ^ (row >> 1)) & 3) * 16);
+                    const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
-            for (int q = 0; q < L::UC / 32; ++q) {
-                const int pc = u * (L::UC / 32) + q;              // 16-byte piece of the row
-                const uint4 w4 = lds_128(codes + ((pc ^ (row >> 1)) & 3) * 16);
-                const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
+                    for (int k = 0; k < 4; ++k) {
+                        if constexpr (INT) {
+                            a[8 * q + 2 * k] = ((w[k] << 4) & 0xF0F0F0F0u) | one;
+                            a[8 * q + 2 * k + 1] = (w[k] & 0xF0F0F0F0u) | one;
+                        } else {
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    if constexpr (INT) {
-                        a[8 * q + 2 * k] = ((w[k] << 4) & 0xF0F0F0F0u) | one;
-                        a[8 * q + 2 * k + 1] = (w[k] & 0xF0F0F0F0u) | one;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) a[16 * q + 4 * k + e] = dsq_value_pair<XT>(w[k], e, base);
+                            for (int e = 0; e < 4; ++e) a[16 * q + 4 * k + e] = dsq_value_pair<XT>(w[k], e, base);
+                        }
                     }
                 }
+                if (L::ABUF == 1 && h == 0 && i > 0) wait_read(i - 1);
+                tmem_st_32x32(lanes + a_col + 32 * h, a);
             }
-            if (unit >= 2) wait_unit(unit - 2);
-            st_cols(lanes + L::A_COL + (unit & 1) * L::AC, a);
             tmem_st_wait();
             tc_fence_before_sync();
             named_barrier_sync(1 + team, 128);
             if ((warp & 3) == 0) {
-                tc_fence_after_sync();
-                const int at = u * L::UC * (INT ? 1 : 2);         // bytes into the chunk's rows
-                const uint64_t desc = smem_desc_sw128(xb + (at >> 7) * (L::NC * 128) + (at & 127));
-                const uint32_t d = tmem + (flush & 1) * L::NC;
-                mma_ts_elect<INT, L::AC / 8>(d, tmem + L::A_COL + (unit & 1) * L::AC, (uint32_t)desc,
-                                             (uint32_t)(desc >> 32), idesc, u % L::PER_FLUSH);
-                mma_commit_elect(bars + 8 * (unit & 1));
+                const uint64_t desc = smem_desc_sw128(xbuf + (i & 1) * L::XBUF);
+                const uint32_t hi = (uint32_t)(desc >> 32);
+#pragma unroll
+                for (int f = 0; f < FLUSHES; ++f) {
+                    const uint32_t use = i * FLUSHES + f, slot = team * L::PLACES + use % L::PLACES;
+                    if (use >= L::PLACES) wait(L::FREE + 8 * slot, ((use / L::PLACES) & 1) ^ 1);
+                    tc_fence_after_sync();
+                    constexpr int COUNT = L::AC / 8 / FLUSHES, BLOCK = COUNT < 4 ? COUNT : 4;
+#pragma unroll
+                    for (int b = 0; b < COUNT / BLOCK; ++b) {
+                        const int at = (f * COUNT + b * BLOCK) * 32;          // bytes into the chunk's rows
+                        mma_ts_elect<INT, BLOCK>(tmem + slot * L::NC, tmem + a_col + (f * COUNT + b * BLOCK) * 8,
+                                                 (uint32_t)desc + (((at >> 7) * (L::NC * 128) + (at & 127)) >> 4), hi, idesc, b);
+                    }
+                    mma_commit_elect(smem + L::READY + 8 * slot);
+                }
+                mma_commit_elect(smem + L::READ + 16 * team + 8 * (i % L::ABUF));
                 __syncwarp();
             }
-            // the sums before this unit's flush, while its instructions run
-            if (u % L::PER_FLUSH == L::PER_FLUSH - 1) {
-                if (flush) {
-                    // (that flush ended PER_FLUSH units ago; two: this unit's A has waited for it)
-                    if (L::PER_FLUSH == 1) wait_unit(unit - 1);
-                    take(flush - 1, pending);
+        }
+        // the last instructions read X and the values to the end
+        for (int i = max(0, turns - L::ABUF); i < turns; ++i) {
+            wait_read(i);
+            if (!ok) wait_warp(smem + L::READ + 16 * team + 8 * (i % L::ABUF), (i / L::ABUF) & 1, DRAIN_NS);
+        }
+    } else {
+        // the scale of a row's sums comes a chunk ahead
+        float sc[FLUSHES];
+        auto load_scales = [&](int c) {
+#pragma unroll
+            for (int f = 0; f < FLUSHES; ++f) {
+                const int g = p.group_of((uint32_t)((c0 + c) * FLUSHES + f));
+                sc[f] = 0.f;
+                if (c < chunks && g < p.groups) sc[f] = load_ahead(p.scales + (int64_t)g * p.N + n0 + min(row, last));
+            }
+        };
+        load_scales(0);
+        uint32_t of = 0, turn = 0;                               // the chunk's team, and its turn
+#pragma unroll 1
+        for (int i = 0; i < chunks; ++i) {
+            float now[FLUSHES];
+#pragma unroll
+            for (int f = 0; f < FLUSHES; ++f) now[f] = sc[f];
+            load_scales(i + 1);
+#pragma unroll
+            for (int f = 0; f < FLUSHES; ++f) {
+                const uint32_t use = turn * FLUSHES + f, slot = of * L::PLACES + use % L::PLACES;
+                wait(L::READY + 8 * slot, (use / L::PLACES) & 1);
+                tc_fence_after_sync();
+                constexpr int STEP = MC < 32 ? MC : 32;
+#pragma unroll
+                for (int h = 0; h < MC / STEP; ++h) {
+                    uint32_t v[STEP];
+                    ld_cols(lanes + slot * L::NC + h * STEP, v);
+                    tmem_ld_wait();
+                    if (h == MC / STEP - 1) {                     // the place is free again
+                        tc_fence_before_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(smem + L::FREE + 8 * slot);
+                    }
+#pragma unroll
+                    for (int e = 0; e < STEP; ++e)
+                        total[h * STEP + e] = __fmaf_rn(INT ? (float)(int)v[e] : __uint_as_float(v[e]), now[f],
+                                                        total[h * STEP + e]);
                 }
-                pending = now[u / L::PER_FLUSH];
-                ++flush;
+            }
+            if (++of == TEAMS) {
+                of = 0;
+                ++turn;
             }
         }
-    }
-    if (flush) {
-        wait_unit(unit - 1);
-        if (!ok) wait_warp(bars + 8 * ((unit - 1) & 1), ((unit - 1) >> 1) & 1, DRAIN_NS);
-        take(flush - 1, pending);
     }
     cp_async_wait<0>();
     tc_fence_before_sync();
     const int failed = __syncthreads_or(!ok);
     if (warp == 0) {
         tc_fence_after_sync();
-        tmem_dealloc(lds_32(slot), L::COLS);
+        tmem_dealloc(lds_32(smem), L::COLS);
     }
-    // the teams' totals, [team][column][row], added in turn; then those of the cluster's blocks
+    if (split == 1) {
+        if (team == TEAMS && row <= last) {
+            const float unit = failed ? __uint_as_float(0x7FC00000u) : dsq_value_unit<XT>(p.odd);
+#pragma unroll
+            for (int m = 0; m < MC; ++m)
+                if (m < rows) p.store(m0 + m, n0 + row, total[m] * unit);
+        }
+        return;
+    }
+    // the totals of the cluster's blocks, [row of X][row of weights], added in their order
     const uint32_t sums = smem + L::RING_AT;
+    if (team == TEAMS) {
 #pragma unroll
-    for (int i = 0; i < MC; ++i)
-        sts_32(sums + ((team * MC + i) * 128 + row) * 4, __float_as_uint(total[i]));
-    __syncthreads();
-    const float unit_value = dsq_value_unit<XT>(p.odd);
-    for (int m = team; m < rows; m += TEAMS) {
+        for (int m = 0; m < MC; ++m)
+            sts_32(sums + (m * 128 + row) * 4, failed ? 0x7FC00000u : __float_as_uint(total[m]));
+    }
+    cluster_sync_all();
+    const float unit = dsq_value_unit<XT>(p.odd);
+    for (int m = rank + team * split; m < rows; m += (TEAMS + 1) * split) {
         float s = 0.f;
-#pragma unroll
-        for (int t = 0; t < TEAMS; ++t) s += __uint_as_float(lds_32(sums + ((t * MC + m) * 128 + row) * 4));
-        if (failed) s = __uint_as_float(0x7FC00000u);
-        if (split == 1) {
-            if (n0 + row < p.N) p.store(m0 + m, n0 + row, s * unit_value);
-        } else {
-            sts_32(sums + (m * 128 + row) * 4, __float_as_uint(s));
-        }
+        for (int r = 0; r < split; ++r) s += __uint_as_float(ld_cluster_32(map_to_cta(sums + (m * 128 + row) * 4, r)));
+        if (row <= last) p.store(m0 + m, n0 + row, s * unit);
     }
-    if (split > 1) {
-        cluster_sync_all();
-        for (int m = rank + team * split; m < rows; m += TEAMS * split) {
-            float s = 0.f;
-            for (int r = 0; r < split; ++r) s += __uint_as_float(ld_cluster_32(map_to_cta(sums + (m * 128 + row) * 4, r)));
-            if (n0 + row < p.N) p.store(m0 + m, n0 + row, s * unit_value);
-        }
-        cluster_sync_all();       // nobody leaves while its sums are read
-    }
+    cluster_sync_all();           // nobody leaves while its sums are read
 }
 
 template <int XT, int MC, int GP, int TEAMS, int STAGES>
@@ -416,16 +443,17 @@ int launch(const DsqGroupGemm &p, cudaStream_t s)
     }
     if (tiles * split > 0x7FFFFFFF || mt > 65535) return DSQ_ERR_SIZE;
     const DsqLaunchHooks h = dsq_launch_hooks();
-    return dsq_launch(kernel, dim3((unsigned)(tiles * split), (unsigned)mt), dim3(TEAMS * 128), (size_t)L::BYTES, s,
+    return dsq_launch(kernel, dim3((unsigned)(tiles * split), (unsigned)mt), dim3(L::THREADS), (size_t)L::BYTES, s,
                       h.pdl, split, p, split, h.wait_ns);
 }
 
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
 {
-    if (p.M <= 8) return launch<XT, 8, GP, 4, 4>(p, s);
-    if (p.M <= 16) return launch<XT, 16, GP, 4, 4>(p, s);
+    constexpr int STAGES = XT == DSQ_I8 ? 5 : 4;
+    if (p.M <= 8) return launch<XT, 8, GP, 3, STAGES>(p, s);
+    if (p.M <= 16) return launch<XT, 16, GP, 3, STAGES>(p, s);
     if (p.M <= 32) return launch<XT, 32, GP, 3, 4>(p, s);
-    return launch<XT, 64, GP, 2, 6>(p, s);
+    return launch<XT, 64, GP, 3, 4>(p, s);
 }
 
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
