@@ -10,8 +10,9 @@
 // traffic through registers: at 8192 x 8192 with bf16 rows mma.sync took 23 us for one row and
 // 64 us for 64, issue-bound.
 //
-//   * TEAMS of four warps take the block's chunks of 128 codes of 128 rows in turn: codes from the team's
-//     ring in shared memory (cp.async, each warp its own 32 rows), X of the chunk from global memory
+//   * TEAMS of four warps take the block's chunks of 128 codes of 128 rows in turn, two at a time: codes
+//     from the team's ring in shared memory (cp.async, each warp its own 32 rows, whole lines of 128
+//     bytes: with 64 of a line at a time memory gave 1.6 TB/s), X of a chunk from global memory
 //     through registers, permuted to the order in which codes come out of their words, into the
 //     128-byte swizzle.  One warp of the team issues the instructions.
 //   * Four more warps take the sums: a chunk's (a group's, where groups end sooner) lie in one of the
@@ -104,11 +105,9 @@ __device__ __forceinline__ uint4 load_ahead(const uint8_t *p)
     asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
     return v;
 }
-__device__ __forceinline__ float load_ahead(const float *p)
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const float *src)
 {
-    float v;
-    asm volatile("ld.global.nc.f32 %0, [%1];" : "=f"(v) : "l"(p));
-    return v;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
 // once a wait has run out, instructions in flight get this long before their memory is given up
@@ -134,6 +133,7 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigne
     return __all_sync(~0u, ok);
 }
 
+constexpr int AHEAD = 8;          // chunks whose scales are on their way
 // MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum
 template <int XT, int MC, int GP, int TEAMS, int STAGES> struct Layout {
     static constexpr bool INT = XT == DSQ_I8;
@@ -150,8 +150,9 @@ template <int XT, int MC, int GP, int TEAMS, int STAGES> struct Layout {
     static constexpr int COLS = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
     static constexpr int XBUF = NC * (INT ? 128 : 256);
     static constexpr int X_AT = 1024, RING_AT = X_AT + TEAMS * 2 * XBUF;
-    static constexpr int STAGE = 128 * 64;
-    static constexpr int BYTES = RING_AT + TEAMS * STAGES * STAGE + 1024;    // (its start is aligned to 1024)
+    static constexpr int STAGE = 128 * 128;                       // two chunks
+    static constexpr int S_AT = RING_AT + TEAMS * STAGES * STAGE, S_STAGE = FLUSHES * 512;    // scales of a chunk
+    static constexpr int BYTES = S_AT + AHEAD * S_STAGE + 1024;              // (its start is aligned to 1024)
     static constexpr int THREADS = (TEAMS + 1) * 128;
     // barriers: sums ready and place free of each slot, values read of each team
     static constexpr int READY = 16, FREE = READY + 8 * SLOTS, READ = FREE + 8 * SLOTS;
@@ -176,7 +177,9 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     const int m0 = blockIdx.y * MC;
     const int rows = min(p.M - m0, MC);
     const int all = (p.K + 127) >> 7;
-    const int c0 = (int)((int64_t)all * rank / split), chunks = (int)((int64_t)all * (rank + 1) / split) - c0;
+    // whole pairs of chunks to a block
+    const int pairs = (all + 1) >> 1, c0 = 2 * (int)((int64_t)pairs * rank / split);
+    const int chunks = min(2 * (int)((int64_t)pairs * (rank + 1) / split), all) - c0;
     const int last = (int)min((int64_t)127, p.N - 1 - n0);       // row of weights of this block
 
     if (warp == 0) {
@@ -207,16 +210,18 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     if (team < TEAMS) {
         const uint32_t xbuf = smem + L::X_AT + team * 2 * L::XBUF;
         const uint32_t ring = smem + L::RING_AT + team * STAGES * L::STAGE;
-        const int turns = team < chunks ? (chunks - team - 1) / TEAMS + 1 : 0;
-        // Copies of this warp's 32 rows of the team's next chunk: 16-byte piece j of a row's 64.  (Rows
+        // the team's chunks: c0 + 2 (team + TEAMS i) and the one behind it
+        const int my_pairs = 2 * team < chunks ? ((chunks + 1) / 2 - team - 1) / TEAMS + 1 : 0;
+        const int turns = my_pairs == 0 ? 0 : 2 * my_pairs - ((chunks & 1) && (chunks / 2) % TEAMS == team);
+        // Copies of this warp's 32 rows of the team's next two chunks: 16-byte piece j of a row's 128.  (Rows
         // behind the last are the last: their sums are not used.)
-        const int j = lane & 3, mine = (warp & 3) * 32 + (lane >> 2);
+        const int j = lane & 7, mine = (warp & 3) * 32 + (lane >> 3);
         const uint8_t *src = p.W + n0 * p.pitch;
-        int row_at[4];
+        int row_at[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) row_at[k] = min(mine + 8 * k, last) * p.pitch;
-        const uint32_t w_to = mine * 64 + ((j ^ (mine >> 1)) & 3) * 16;
-        int w_left = turns, w_k = (c0 + team) * 64 + 16 * j;
+        for (int k = 0; k < 8; ++k) row_at[k] = min(mine + 4 * k, last) * p.pitch;
+        const uint32_t w_to = mine * 128;
+        int w_left = my_pairs, w_k = (c0 + 2 * team) * 64 + 16 * j;
         uint32_t w_stage = ring;
         auto issue_w = [&]() {
             if (w_left > 0) {
@@ -224,10 +229,11 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                 const uint8_t *s = src + (in ? w_k : 0);
                 const uint32_t bytes = in ? 16u : 0u;
 #pragma unroll
-                for (int k = 0; k < 4; ++k) cp_async_16(w_stage + w_to + k * 512, s + row_at[k], bytes);
+                for (int k = 0; k < 8; ++k)
+                    cp_async_16(w_stage + w_to + k * 512 + ((j ^ (mine + 4 * k)) & 7) * 16, s + row_at[k], bytes);
             }
             --w_left;
-            w_k += TEAMS * 64;
+            w_k += TEAMS * 128;
             w_stage = w_stage == ring + (STAGES - 1) * L::STAGE ? ring : w_stage + L::STAGE;
             cp_async_commit();
         };
@@ -243,9 +249,9 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
         const uint32_t x_to = xbuf + (pc >> 3) * (L::NC * 128) + r0 * 128 + (((pc & 7) ^ (r0 & 7)) << 4);
         static_assert(RS % 8 == 0 && XP * RS <= L::NC, "the swizzle of a thread's rows is one");
         uint4 x[XP];
-        int l_left = turns, l_k = (c0 + team) * (PIECES * 16);    // bytes into the row
+        int l_turn = 0, l_k = (c0 + 2 * team) * (PIECES * 16);   // bytes into the row
         auto load_x = [&]() {
-            if (l_left > 0 && l_k + 16 * pc < p.K * ELEMENT) {
+            if (l_turn < turns && l_k + 16 * pc < p.K * ELEMENT) {
                 const uint8_t *s = xsrc + l_k;
 #pragma unroll
                 for (int k = 0; k < XP; ++k) x[k] = load_ahead(s + x_at[k]);
@@ -253,8 +259,8 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
 #pragma unroll
                 for (int k = 0; k < XP; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
             }
-            --l_left;
-            l_k += TEAMS * (PIECES * 16);
+            l_k += (l_turn & 1 ? 2 * TEAMS - 1 : 1) * (PIECES * 16);
+            ++l_turn;
         };
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) issue_w();
@@ -266,9 +272,11 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
         uint32_t r_stage = ring;
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
-            cp_async_wait<STAGES - 2>();
-            __syncwarp();         // the chunk's codes are here, and those of the last one have been read
-            issue_w();
+            if ((i & 1) == 0) {
+                cp_async_wait<STAGES - 2>();
+                __syncwarp();     // the two chunks' codes are here, and those before them have been read
+                issue_w();
+            }
             // (X has two buffers too: its last chunk but one has been waited for)
             if (L::ABUF == 2 && i >= 2) wait_read(i - 2);
             const uint32_t a_col = L::A_COL + (team * L::ABUF + i % L::ABUF) * L::AC;
@@ -285,8 +293,8 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
             }
             fence_proxy_async_smem();
             load_x();
-            const uint32_t codes = r_stage + row * 64;
-            r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
+            const uint32_t codes = r_stage + row * 128;
+            if (i & 1) r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
             // the values of this row's codes, 32 columns at a time
 #pragma unroll
             for (int h = 0; h < L::AC / 32; ++h) {
@@ -294,7 +302,7 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                 uint32_t a[32];
 #pragma unroll
                 for (int q = 0; q < P16; ++q) {
-                    const uint4 w4 = lds_128(codes + (((P16 * h + q) ^ (row >> 1)) & 3) * 16);
+                    const uint4 w4 = lds_128(codes + (((4 * (i & 1) + P16 * h + q) ^ row) & 7) * 16);
                     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -340,24 +348,31 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
             if (!ok) wait_warp(smem + L::READ + 16 * team + 8 * (i % L::ABUF), (i / L::ABUF) & 1, DRAIN_NS);
         }
     } else {
-        // the scale of a row's sums comes a chunk ahead
-        float sc[FLUSHES];
-        auto load_scales = [&](int c) {
+        // A row's scales go through a ring of their own, each thread's copies for itself.  (A chunk ahead, in
+        // registers, the wait for them was the kernel's time: 32 times 0.6 us.)
+        const uint32_t s_ring = smem + L::S_AT + row * 4;
+        const float *scales = p.scales + n0 + min(row, last);
+        auto issue_s = [&](int c) {
+            if (c < chunks) {
 #pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) {
-                const int g = p.group_of((uint32_t)((c0 + c) * FLUSHES + f));
-                sc[f] = 0.f;
-                if (c < chunks && g < p.groups) sc[f] = load_ahead(p.scales + (int64_t)g * p.N + n0 + min(row, last));
+                for (int f = 0; f < FLUSHES; ++f) {
+                    const int g = min(p.group_of((uint32_t)((c0 + c) * FLUSHES + f)), p.groups - 1);
+                    cp_async_4(s_ring + (c % AHEAD) * L::S_STAGE + f * 512, scales + (int64_t)g * p.N);
+                }
             }
+            cp_async_commit();
         };
-        load_scales(0);
-        uint32_t of = 0, turn = 0;                               // the chunk's team, and its turn
+#pragma unroll 1
+        for (int c = 0; c < AHEAD - 1; ++c) issue_s(c);
+        uint32_t of = 0, turn = 0;                               // the chunk's team, and its turn there
 #pragma unroll 1
         for (int i = 0; i < chunks; ++i) {
+            cp_async_wait<AHEAD - 2>();
             float now[FLUSHES];
 #pragma unroll
-            for (int f = 0; f < FLUSHES; ++f) now[f] = sc[f];
-            load_scales(i + 1);
+            for (int f = 0; f < FLUSHES; ++f)
+                now[f] = __uint_as_float(lds_32(s_ring + (i % AHEAD) * L::S_STAGE + f * 512));
+            issue_s(i + AHEAD - 1);
 #pragma unroll
             for (int f = 0; f < FLUSHES; ++f) {
                 const uint32_t use = turn * FLUSHES + f, slot = of * L::PLACES + use % L::PLACES;
@@ -380,9 +395,13 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                                                         total[h * STEP + e]);
                 }
             }
-            if (++of == TEAMS) {
+            if ((i & 1) == 0) {
+                ++turn;
+            } else if (++of == TEAMS) {
                 of = 0;
                 ++turn;
+            } else {
+                --turn;
             }
         }
     }
@@ -433,7 +452,7 @@ int launch(const DsqGroupGemm &p, cudaStream_t s)
     // and the end of a block.
     int split = 1;
     double best = 1e30;
-    for (int c = 1; c <= 8 && c <= chunks; c *= 2) {
+    for (int c = 1; c <= 8 && 2 * c <= chunks + 1; c *= 2) {
         const double waves = (double)((tiles * mt * c + sms - 1) / sms);
         const double t = waves * ((double)((chunks + c - 1) / c + TEAMS - 1) / TEAMS + 6.0 + (c > 1 ? 1.0 : 0.0));
         if (t < best) {
@@ -449,11 +468,10 @@ int launch(const DsqGroupGemm &p, cudaStream_t s)
 
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
 {
-    constexpr int STAGES = XT == DSQ_I8 ? 5 : 4;
-    if (p.M <= 8) return launch<XT, 8, GP, 3, STAGES>(p, s);
-    if (p.M <= 16) return launch<XT, 16, GP, 3, STAGES>(p, s);
-    if (p.M <= 32) return launch<XT, 32, GP, 3, 4>(p, s);
-    return launch<XT, 64, GP, 3, 4>(p, s);
+    if (p.M <= 8) return launch<XT, 8, GP, 3, 3>(p, s);
+    if (p.M <= 16) return launch<XT, 16, GP, 3, 3>(p, s);
+    if (p.M <= 32) return launch<XT, 32, GP, 3, 3>(p, s);
+    return launch<XT, 64, GP, 3, 2>(p, s);
 }
 
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
