@@ -289,6 +289,23 @@ template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
     return gp == 4 ? pick<XT, 4>(p, s) : gp == 2 ? pick<XT, 2>(p, s) : pick<XT, 1>(p, s);
 }
 
+// Estimated time of these kernels: 1.6 us and the turns of a warp, times the blocks an SM has to run, those
+// beyond its first at their share of it (8 rows: 2 and more are resident together) or in waves (one block
+// an SM).  us of a turn, from 1024 x 8192 (one block an SM): 16-bit rows 9.5, 10.7, 15.3 and 32.1 us for 8, 16,
+// 32 and 64 rows, int8 6.2, 7.6, 10.8 and 21.2.
+double estimate_us(const DsqGroupGemm &p, bool i8)
+{
+    const int at = p.M <= 8 ? 0 : p.M <= 16 ? 1 : p.M <= 32 ? 2 : 3;
+    static const double turn[2][4] = {{1.0, 1.15, 1.7, 1.9}, {0.58, 0.75, 1.15, 1.22}};
+    const int warps = at == 3 ? 4 : 8, turns = ((p.K + 127) / 128 + warps - 1) / warps;
+    const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    double load = (double)(((int64_t)p.N + 31) / 32 * ((p.M + 63) / 64)) / sms;
+    const bool waves = i8 ? at == 2 : at != 0;
+    if (load < 1.0) load = 1.0;
+    if (waves) load = (double)(int64_t)(load + 0.999);
+    return load * (1.6 + turns * turn[i8][at]);
+}
+
 }  // namespace
 
 static std::atomic<int> dsq_group_form{0};
@@ -333,9 +350,17 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
     p.odd = w_offset == 0.5f;
     p.y_type = y_type;
     cudaStream_t s = (cudaStream_t)stream;
-    const int form = dsq_group_form.load(std::memory_order_relaxed);
-    if (form == 3 || (form == 0 && M <= (x_type == DSQ_I8 ? 16 : 5))) return dsq_wgemm_group_few(p, x_type, g, s);
-    if (form == 2 || (form == 0 && N * K > (1 << 21))) return dsq_wgemm_group_tc(p, x_type, g, s);
+    int form = dsq_group_form.load(std::memory_order_relaxed);
+    if (form == 3 && (x_type == DSQ_I8 || M > 2)) form = 1;
+    if (form == 0 && x_type != DSQ_I8 && M <= 2) form = 3;
+    if (form == 0) {
+        double tc_us = 0.0;
+        const int st2 = dsq_wgemm_group_tc(p, x_type, g, s, &tc_us);
+        if (st2) return st2;
+        form = tc_us < estimate_us(p, x_type == DSQ_I8) ? 2 : 1;
+    }
+    if (form == 3) return dsq_wgemm_group_few(p, x_type, g, s);
+    if (form == 2) return dsq_wgemm_group_tc(p, x_type, g, s, nullptr);
     switch (x_type) {
     case DSQ_BF16: return pick_group<DSQ_BF16>(p, g, s);
     case DSQ_F16: return pick_group<DSQ_F16>(p, g, s);

@@ -1,5 +1,5 @@
-// What the two kernels for products with group-wise 4-bit weights share
-// (dsq_wgemm_group.cu: mma.sync, small problems; dsq_wgemm_group_tc.cu: tcgen05).
+// What the kernels for products with group-wise 4-bit weights share (dsq_wgemm_group.cu: mma.sync;
+// dsq_wgemm_group_few.cu: mma.sync on digits, one or two rows; dsq_wgemm_group_tc.cu: tcgen05).
 #pragma once
 
 #include <cuda_bf16.h>
@@ -45,8 +45,10 @@ struct DsqGroupGemm {
 // pieces of 32 codes, up to four, that no group's end cuts
 static inline int dsq_group_pieces(int64_t group) { return group % 128 == 0 ? 4 : group % 64 == 0 ? 2 : 1; }
 
-// arguments validated; group a multiple of 32
-DSQ_HIDDEN int dsq_wgemm_group_tc(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s);
+// Arguments validated; group a multiple of 32.
+// tcgen05 (est_us: its estimated time is written there and nothing is launched)
+DSQ_HIDDEN int dsq_wgemm_group_tc(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s, double *est_us);
+// one or two rows in 16 bits
 DSQ_HIDDEN int dsq_wgemm_group_few(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s);
 
 #ifdef __CUDACC__

@@ -47,10 +47,9 @@ __device__ __forceinline__ void sts_64(uint32_t at, uint32_t a, uint32_t b)
 {
     asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(at), "r"(a), "r"(b) : "memory");
 }
-template <int BYTES> __device__ __forceinline__ void cp_async_small(uint32_t dst, const void *src, uint32_t src_bytes)
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
 {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(BYTES), "r"(src_bytes)
-                 : "memory");
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
 }
 
 // bytes of a row of digits in shared memory: rows meet no bank twice in 16-byte reads (GP = 4) or in
@@ -59,16 +58,13 @@ template <int GP> constexpr int row_bytes() { return GP == 4 ? 272 : 288; }
 
 // ROWS of X; GP: pieces of 32 codes that no group's end cuts
 template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> struct Few {
-    static constexpr int DIGITS = XT == DSQ_I8 ? 1 : 3;
-    static constexpr bool HALF = ROWS * DIGITS <= 8;              // the lower half of an instruction's rows
     static constexpr int FLUSHES = 8 / GP;
     static constexpr int W_BYTES = NT * 1024, S_BYTES = FLUSHES * NT * 32;
-    static constexpr int X_ROW = XT == DSQ_I8 ? 256 : 512;
-    static constexpr int STAGE = W_BYTES + S_BYTES + ROWS * X_ROW;
-    static constexpr int WARP_BYTES = STAGES * STAGE + ROWS * DIGITS * row_bytes<GP>();
-    static constexpr int SUMS = WARPS * NT * (HALF ? 64 : 128) * 4;
+    static constexpr int STAGE = W_BYTES + S_BYTES + ROWS * 512;
+    static constexpr int WARP_BYTES = STAGES * STAGE + ROWS * 3 * row_bytes<GP>();
+    static constexpr int SUMS = WARPS * NT * 64 * 4;
     static constexpr int BYTES = WARPS * WARP_BYTES > SUMS ? WARPS * WARP_BYTES : SUMS;
-    static_assert(ROWS * DIGITS <= 16 && WARP_BYTES % 16 == 0 && BYTES <= 227 * 1024, "shared memory");
+    static_assert(ROWS * 3 <= 8 && WARP_BYTES % 16 == 0 && BYTES <= 227 * 1024, "shared memory");
 };
 
 template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES>
@@ -76,10 +72,8 @@ __global__ void __launch_bounds__(WARPS * 32)
 wgemm_group_few_kernel(const DsqGroupGemm p)
 {
     using L = Few<XT, ROWS, NT, GP, WARPS, STAGES>;
-    constexpr int DIGITS = L::DIGITS, FLUSHES = L::FLUSHES, HALVES = L::HALF ? 1 : 2;
-    constexpr bool INT = XT == DSQ_I8;
+    constexpr int FLUSHES = L::FLUSHES;
     constexpr int ROW = row_bytes<GP>();
-    constexpr int X_LANE = INT ? 8 : 16;                             // bytes of eight elements
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n = lane >> 2, j = lane & 3;
@@ -98,8 +92,8 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
     for (int t = 0; t < NT; ++t) col_at[t] = min(8 * t + n, cols - 1) * p.pitch;
     const uint32_t w_to = n * 64 + ((j ^ (n >> 1)) & 3) * 16;
     // X: elements 8 lane .. 8 lane + 7 of the chunk
-    const uint8_t *xs = p.X + (int64_t)m0 * p.K * (X_LANE / 8) + lane * X_LANE;
-    const int64_t x_step = (int64_t)p.K * (X_LANE / 8);
+    const uint8_t *xs = p.X + (int64_t)m0 * p.K * 2 + lane * 16;
+    const int64_t x_step = (int64_t)p.K * 2;
     const bool fours = (p.N & 3) == 0;                               // scales of four columns are aligned
     uint32_t stage_to = ring;
     int c_to = warp;                                                 // chunk that is copied next
@@ -126,16 +120,15 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
             for (int e = lane; e < FLUSHES * NT * 8; e += 32) {
                 const int f = e / (NT * 8), c = e % (NT * 8), g = p.group_of((uint32_t)(c_to * FLUSHES + f));
                 const bool in = g < p.groups && c < cols;
-                cp_async_small<4>(s_to + e * 4, in ? p.scales + (int64_t)g * p.N + n0 + c : p.scales, in ? 4u : 0u);
+                cp_async_4(s_to + e * 4, in ? p.scales + (int64_t)g * p.N + n0 + c : p.scales, in ? 4u : 0u);
             }
         }
         const bool x_in = c_to * 256 + 8 * lane < p.K;
-        const uint8_t *xm = xs + (x_in ? c_to * (32 * X_LANE) : 0);
+        const uint8_t *xm = xs + (x_in ? c_to * 512 : 0);
 #pragma unroll
         for (int m = 0; m < ROWS; ++m) {
             const bool in = x_in && m < rows;
-            cp_async_small<X_LANE>(s_to + L::S_BYTES + m * L::X_ROW + lane * X_LANE, in ? xm + m * x_step : p.X,
-                                   in ? X_LANE : 0u);
+            cp_async_16(s_to + L::S_BYTES + m * 512 + lane * 16, in ? xm + m * x_step : p.X, in ? 16u : 0u);
         }
         c_to += WARPS;
         stage_to = stage_to == ring + (STAGES - 1) * L::STAGE ? ring : stage_to + L::STAGE;
@@ -149,11 +142,9 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
         cp_async_commit();
     }
 
-    float total[NT][2 * HALVES];
+    float total[NT][2];           // of the lower eight rows; the others are empty
 #pragma unroll
-    for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int e = 0; e < 2 * HALVES; ++e) total[t][e] = 0.f;
+    for (int t = 0; t < NT; ++t) total[t][0] = total[t][1] = 0.f;
     const uint32_t one = p.odd ? 0x08080808u : 0u;
     const uint32_t w_at = GP == 4 ? w_to : n * 64 + 4 * j;
     uint32_t at = ring;
@@ -164,59 +155,54 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
         __syncwarp();             // the stage is here; the last one, and the digits, have been read
         if (i + STAGES - 1 < turns) issue();
         cp_async_commit();
-        // digits of X, in the order in which codes come out of their words; what this lane's rows of
-        // sums (n, n + 8) are multiples of
-        float up[2] = {1.f, 1.f};
-        const uint32_t s_at = at + L::W_BYTES, x_at = s_at + L::S_BYTES + lane * X_LANE;
+        // digits of X, in the order in which codes come out of their words; what this lane's row of sums is a
+        // multiple of
+        float up = 1.f;
+        const uint32_t s_at = at + L::W_BYTES, x_at = s_at + L::S_BYTES + lane * 16;
 #pragma unroll
         for (int m = 0; m < ROWS; ++m) {
             if (m >= rows) break;
-            const uint32_t to = digits + DIGITS * m * ROW + 8 * lane;
-            if constexpr (INT) {
-                const uint2 x = lds_64(x_at + m * L::X_ROW);
-                sts_64(to, __byte_perm(x.x, x.y, 0x6420), __byte_perm(x.x, x.y, 0x7531));
+            const uint32_t to = digits + 3 * m * ROW + 8 * lane;
+            const uint4 x = lds_128(x_at + m * 512);
+            constexpr uint32_t ABS = 0x7FFF7FFFu, INF = XT == DSQ_BF16 ? 0x7F80u : 0x7C00u;
+            const uint32_t t2 = __vmaxu2(__vmaxu2(x.x & ABS, x.y & ABS), __vmaxu2(x.z & ABS, x.w & ABS));
+            const uint32_t top = __reduce_max_sync(~0u, max(t2 & 0xFFFFu, t2 >> 16));
+            float f[8];
+            DsqRaw8<__half> raw;
+            raw.v[0] = x;
+            uint32_t e;                      // the largest's exponent, as binary32 keeps it
+            if (XT == DSQ_BF16) {
+                dsq_unpack8(reinterpret_cast<const DsqRaw8<__nv_bfloat16> &>(raw), f);
+                e = top >> 7;
             } else {
-                const uint4 x = lds_128(x_at + m * L::X_ROW);
-                constexpr uint32_t ABS = 0x7FFF7FFFu, INF = XT == DSQ_BF16 ? 0x7F80u : 0x7C00u;
-                const uint32_t t2 = __vmaxu2(__vmaxu2(x.x & ABS, x.y & ABS), __vmaxu2(x.z & ABS, x.w & ABS));
-                const uint32_t top = __reduce_max_sync(~0u, max(t2 & 0xFFFFu, t2 >> 16));
-                float f[8];
-                DsqRaw8<__half> raw;
-                raw.v[0] = x;
-                uint32_t e;                      // the largest's exponent, as binary32 keeps it
-                if (XT == DSQ_BF16) {
-                    dsq_unpack8(reinterpret_cast<const DsqRaw8<__nv_bfloat16> &>(raw), f);
-                    e = top >> 7;
-                } else {
-                    dsq_unpack8(raw, f);
-                    e = __float_as_uint(__half2float(__ushort_as_half((unsigned short)top))) >> 23;
-                }
-                // times 2^(21 - e), and back (rows with an infinity or a NaN: NaN)
-                e = max(e, 22u);
-                const float scale = __uint_as_float((275u - e) << 23);
-                const float inv = top >= INF ? __uint_as_float(0x7FC00000u) : __uint_as_float((e - 21u) << 23);
-                uint32_t v[8];
-#pragma unroll
-                for (int k = 0; k < 8; ++k)      // the integer plus 0x8080: its low bytes are digits plus 128
-                    v[k] = __float_as_uint(__fmaf_rn(f[k], scale, 12582912.f)) + (0x8080u - 0x4B400000u);
-                uint32_t d[3][2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const uint32_t a = __byte_perm(v[h], v[h + 2], 0x5140), b = __byte_perm(v[h + 4], v[h + 6], 0x5140);
-                    d[0][h] = __byte_perm(__byte_perm(v[h], v[h + 2], 0x0062), __byte_perm(v[h + 4], v[h + 6], 0x0062), 0x5410);
-                    d[1][h] = __byte_perm(a, b, 0x7632) ^ 0x80808080u;
-                    d[2][h] = __byte_perm(a, b, 0x5410) ^ 0x80808080u;
-                }
-#pragma unroll
-                for (int k = 0; k < 3; ++k) sts_64(to + k * ROW, d[k][0], d[k][1]);
-                if (ROWS == 1 || n / 3 == m) up[0] = inv;
-                if (HALVES == 2 && (n + 8) / 3 == m) up[1] = inv;
+                dsq_unpack8(raw, f);
+                e = __float_as_uint(__half2float(__ushort_as_half((unsigned short)top))) >> 23;
             }
+            // times 2^(21 - e), and back (rows with an infinity or a NaN: NaN)
+            e = max(e, 22u);
+            const float scale = __uint_as_float((275u - e) << 23);
+            const float inv = top >= INF ? __uint_as_float(0x7FC00000u) : __uint_as_float((e - 21u) << 23);
+            uint32_t v[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)      // the integer plus 0x8080: its low bytes are digits plus 128
+                v[k] = __float_as_uint(__fmaf_rn(f[k], scale, 12582912.f)) + (0x8080u - 0x4B400000u);
+            uint32_t d[3][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t a = __byte_perm(v[h], v[h + 2], 0x5140), b = __byte_perm(v[h + 4], v[h + 6], 0x5140);
+                d[0][h] = __byte_perm(__byte_perm(v[h], v[h + 2], 0x0062), __byte_perm(v[h + 4], v[h + 6], 0x0062), 0x5410);
+                d[1][h] = __byte_perm(a, b, 0x7632) ^ 0x80808080u;
+                d[2][h] = __byte_perm(a, b, 0x5410) ^ 0x80808080u;
+            }
+#pragma unroll
+            for (int k = 0; k < 3; ++k) sts_64(to + k * ROW, d[k][0], d[k][1]);
+            if (ROWS == 1 || n / 3 == m) up = inv;
         }
         __syncwarp();
         // Operands: with groups of whole 128s lane j takes the four words of a 16-byte piece one after the
         // other (its codes 32 j .. 32 j + 31), else word j of each piece.
-        uint32_t w[2][NT][4], a[8][2 * HALVES];
+        uint32_t w[2][NT][4], a[8][2];
+        const bool has_row = n < 3 * rows;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -230,57 +216,43 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
                     for (int q = 0; q < 4; ++q) w[h][t][q] = lds_32(from + ((q ^ (n >> 1)) & 3) * 16);
                 }
             }
+            const uint32_t from = digits + n * ROW + 128 * h;
 #pragma unroll
-            for (int r = 0; r < HALVES; ++r) {
-                const uint32_t from = digits + (n + 8 * r) * ROW + 128 * h;
-                const bool in = n + 8 * r < rows * DIGITS;
+            for (int q = 0; q < 4; ++q) a[4 * h + q][0] = a[4 * h + q][1] = 0u;
+            if (GP == 4) {
 #pragma unroll
-                for (int q = 0; q < 4; ++q) a[4 * h + q][2 * r] = a[4 * h + q][2 * r + 1] = 0u;
-                if (GP == 4) {
+                for (int q = 0; q < 4; q += 2)
+                    if (has_row) {
+                        const uint4 v = lds_128(from + 32 * j + 8 * q);
+                        a[4 * h + q][0] = v.x; a[4 * h + q][1] = v.y;
+                        a[4 * h + q + 1][0] = v.z; a[4 * h + q + 1][1] = v.w;
+                    }
+            } else {
 #pragma unroll
-                    for (int q = 0; q < 4; q += 2)
-                        if (in) {
-                            const uint4 v = lds_128(from + 32 * j + 8 * q);
-                            a[4 * h + q][2 * r] = v.x; a[4 * h + q][2 * r + 1] = v.y;
-                            a[4 * h + q + 1][2 * r] = v.z; a[4 * h + q + 1][2 * r + 1] = v.w;
-                        }
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (in) {
-                            const uint2 v = lds_64(from + 32 * q + 8 * j);
-                            a[4 * h + q][2 * r] = v.x; a[4 * h + q][2 * r + 1] = v.y;
-                        }
-                }
+                for (int q = 0; q < 4; ++q)
+                    if (has_row) {
+                        const uint2 v = lds_64(from + 32 * q + 8 * j);
+                        a[4 * h + q][0] = v.x; a[4 * h + q][1] = v.y;
+                    }
             }
         }
         int acc[NT][4];
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            const uint32_t rows_of[4] = {a[q][0], HALVES == 2 ? a[q][2 * HALVES - 2] : 0u, a[q][1],
-                                         HALVES == 2 ? a[q][2 * HALVES - 1] : 0u};
+            const uint32_t x_rows[4] = {a[q][0], 0u, a[q][1], 0u};
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const uint32_t c = w[q >> 2][t][q & 3];
                 const uint32_t b0 = ((c << 4) & 0xF0F0F0F0u) | one, b1 = (c & 0xF0F0F0F0u) | one;
-                if (q % GP == 0) mma_i8_first(acc[t], rows_of, b0, b1);
-                else mma_i8(acc[t], rows_of, b0, b1);
+                if (q % GP == 0) mma_i8_first(acc[t], x_rows, b0, b1);
+                else mma_i8(acc[t], x_rows, b0, b1);
             }
             if (q % GP == GP - 1) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
                     const uint2 sv = lds_64(s_at + ((q / GP) * NT * 8 + 8 * t + 2 * j) * 4);
-                    const float s0 = __uint_as_float(sv.x), s1 = __uint_as_float(sv.y);
-#pragma unroll
-                    for (int h = 0; h < HALVES; ++h) {
-                        float v0 = (float)acc[t][2 * h], v1 = (float)acc[t][2 * h + 1];
-                        if (!INT) {
-                            v0 *= up[h];
-                            v1 *= up[h];
-                        }
-                        total[t][2 * h] = __fmaf_rn(v0, s0, total[t][2 * h]);
-                        total[t][2 * h + 1] = __fmaf_rn(v1, s1, total[t][2 * h + 1]);
-                    }
+                    total[t][0] = __fmaf_rn((float)acc[t][0] * up, __uint_as_float(sv.x), total[t][0]);
+                    total[t][1] = __fmaf_rn((float)acc[t][1] * up, __uint_as_float(sv.y), total[t][1]);
                 }
             }
         }
@@ -289,28 +261,21 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
     cp_async_wait<0>();
     __syncthreads();
     float *sums = reinterpret_cast<float *>(smem);          // [WARPS][rows of digits][8 NT columns]
-    constexpr int R = 8 * HALVES, C = 8 * NT;
+    constexpr int C = 8 * NT;
 #pragma unroll
     for (int t = 0; t < NT; ++t)
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h)
-            *reinterpret_cast<float2 *>(sums + (warp * R + n + 8 * h) * C + 8 * t + 2 * j) =
-                make_float2(total[t][2 * h], total[t][2 * h + 1]);
+        *reinterpret_cast<float2 *>(sums + (warp * 8 + n) * C + 8 * t + 2 * j) = make_float2(total[t][0], total[t][1]);
     __syncthreads();
     const float unit = dsq_value_unit<DSQ_I8>(p.odd);
     for (int e = threadIdx.x; e < rows * C; e += WARPS * 32) {
         const int m = e / C, col = e % C;
         if (col >= cols) continue;
-        float d[DIGITS];
+        float d[3] = {0.f, 0.f, 0.f};
 #pragma unroll
-        for (int k = 0; k < DIGITS; ++k) {
-            d[k] = 0.f;
+        for (int k = 0; k < 3; ++k)
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) d[k] += sums[(w * R + m * DIGITS + k) * C + col];
-        }
-        float s = d[0];
-        if (DIGITS == 3) s = __fmaf_rn(d[0], 65536.f, __fmaf_rn(d[1 % DIGITS], 256.f, d[2 % DIGITS]));
-        p.store(m0 + m, n0 + col, s * unit);
+            for (int w = 0; w < WARPS; ++w) d[k] += sums[(w * 8 + m * 3 + k) * C + col];
+        p.store(m0 + m, n0 + col, __fmaf_rn(d[0], 65536.f, __fmaf_rn(d[1], 256.f, d[2])) * unit);
     }
 }
 
@@ -327,14 +292,8 @@ template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> int launch(co
 
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
 {
-    if constexpr (XT == DSQ_I8) {
-        if (p.M <= 8) return launch<XT, 8, 4, GP, 8, 2>(p, s);
-        return launch<XT, 16, 4, GP, 8, 2>(p, s);
-    } else {
-        if (p.M == 1) return launch<XT, 1, 4, GP, 8, 2>(p, s);
-        if (p.M == 2) return launch<XT, 2, 4, GP, 8, 2>(p, s);
-        return launch<XT, 5, 4, GP, 8, 2>(p, s);
-    }
+    if (p.M == 1) return launch<XT, 1, 4, GP, 8, 2>(p, s);
+    return launch<XT, 2, 4, GP, 8, 2>(p, s);
 }
 
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
@@ -348,9 +307,5 @@ template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
 
 int dsq_wgemm_group_few(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s)
 {
-    switch (x_type) {
-    case DSQ_BF16: return pick_group<DSQ_BF16>(p, group, s);
-    case DSQ_F16: return pick_group<DSQ_F16>(p, group, s);
-    default: return pick_group<DSQ_I8>(p, group, s);
-    }
+    return x_type == DSQ_BF16 ? pick_group<DSQ_BF16>(p, group, s) : pick_group<DSQ_F16>(p, group, s);
 }

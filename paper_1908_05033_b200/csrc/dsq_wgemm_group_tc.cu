@@ -438,27 +438,61 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     cluster_sync_all();           // nobody leaves while its sums are read
 }
 
+// Clusters of `split` blocks that run at once (a GPC's SMs bound them: of eight blocks fewer than 148 / 8).
+template <class K> int active_clusters(K kernel, int split, int threads, int bytes, std::atomic<int> *cached)
+{
+    int n = cached->load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(split * sms));
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)bytes;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = (unsigned)split;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n <= 0) {
+        cudaGetLastError();
+        n = sms / split;
+    }
+    cached->store(n, std::memory_order_relaxed);
+    return n;
+}
+
+// est_us: the launch's estimated time is written there and nothing is launched
 template <int XT, int MC, int GP, int TEAMS, int STAGES>
-int launch(const DsqGroupGemm &p, cudaStream_t s)
+int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
     using L = Layout<XT, MC, GP, TEAMS, STAGES>;
     static std::atomic<unsigned long long> configured{0};
+    static std::atomic<int> active[4];
     const auto kernel = wgemm_group_tc_kernel<XT, MC, GP, TEAMS, STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, L::BYTES, &configured);
     if (st) return st;
     const int64_t tiles = (p.N + 127) / 128, mt = (p.M + MC - 1) / MC;
-    const int chunks = (p.K + 127) / 128, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
-    // Blocks along K: the time of a wave is its chunks a team and about six more for the start
-    // and the end of a block.
+    const int pairs = ((p.K + 127) / 128 + 1) / 2, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    // Blocks along K.  us of a wave: 3.6 for its start and end, the cluster's sums 1.0, and a turn of a
+    // team: measured at 8192 x 8192 (11 turns): 18.8, 21.7 and 31.8 us for 16, 32 and 64 rows, int8 14.5,
+    // 16.8 and 21.4.
+    constexpr double TURN = XT == DSQ_I8 ? (MC <= 16 ? 0.9 : MC <= 32 ? 1.1 : 1.5) : (MC <= 16 ? 1.3 : MC <= 32 ? 1.55 : 2.5);
     int split = 1;
     double best = 1e30;
-    for (int c = 1; c <= 8 && 2 * c <= chunks + 1; c *= 2) {
-        const double waves = (double)((tiles * mt * c + sms - 1) / sms);
-        const double t = waves * ((double)((chunks + c - 1) / c + TEAMS - 1) / TEAMS + 6.0 + (c > 1 ? 1.0 : 0.0));
+    for (int c = 1, k = 0; c <= 8 && c <= pairs; c *= 2, ++k) {
+        const int64_t at_once = c == 1 ? sms : active_clusters(kernel, c, L::THREADS, L::BYTES, &active[k]);
+        const double waves = (double)((tiles * mt + at_once - 1) / at_once);
+        const int turns = 2 * (((pairs + c - 1) / c + TEAMS - 1) / TEAMS);
+        const double t = waves * (3.6 + TURN * turns + (c > 1 ? 1.0 : 0.0));
         if (t < best) {
             best = t;
             split = c;
         }
+    }
+    if (est_us) {
+        *est_us = best;
+        return DSQ_OK;
     }
     if (tiles * split > 0x7FFFFFFF || mt > 65535) return DSQ_ERR_SIZE;
     const DsqLaunchHooks h = dsq_launch_hooks();
@@ -466,28 +500,28 @@ int launch(const DsqGroupGemm &p, cudaStream_t s)
                       h.pdl, split, p, split, h.wait_ns);
 }
 
-template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
+template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
-    if (p.M <= 8) return launch<XT, 8, GP, 3, 3>(p, s);
-    if (p.M <= 16) return launch<XT, 16, GP, 3, 3>(p, s);
-    if (p.M <= 32) return launch<XT, 32, GP, 3, 3>(p, s);
-    return launch<XT, 64, GP, 3, 2>(p, s);
+    if (p.M <= 8) return launch<XT, 8, GP, 3, 3>(p, s, est_us);
+    if (p.M <= 16) return launch<XT, 16, GP, 3, 3>(p, s, est_us);
+    if (p.M <= 32) return launch<XT, 32, GP, 3, 3>(p, s, est_us);
+    return launch<XT, 64, GP, 3, 2>(p, s, est_us);
 }
 
-template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
+template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s, double *est_us)
 {
     const int gp = dsq_group_pieces(group);
     p.set_units(group, gp);
-    return gp == 4 ? pick<XT, 4>(p, s) : gp == 2 ? pick<XT, 2>(p, s) : pick<XT, 1>(p, s);
+    return gp == 4 ? pick<XT, 4>(p, s, est_us) : gp == 2 ? pick<XT, 2>(p, s, est_us) : pick<XT, 1>(p, s, est_us);
 }
 
 }  // namespace
 
-int dsq_wgemm_group_tc(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s)
+int dsq_wgemm_group_tc(const DsqGroupGemm &p, int x_type, int64_t group, cudaStream_t s, double *est_us)
 {
     switch (x_type) {
-    case DSQ_BF16: return pick_group<DSQ_BF16>(p, group, s);
-    case DSQ_F16: return pick_group<DSQ_F16>(p, group, s);
-    default: return pick_group<DSQ_I8>(p, group, s);
+    case DSQ_BF16: return pick_group<DSQ_BF16>(p, group, s, est_us);
+    case DSQ_F16: return pick_group<DSQ_F16>(p, group, s, est_us);
+    default: return pick_group<DSQ_I8>(p, group, s, est_us);
     }
 }
