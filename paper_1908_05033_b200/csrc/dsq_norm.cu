@@ -70,10 +70,11 @@ __device__ __forceinline__ DsqRaw8<T> load_vec(const T *p, int64_t at, int64_t t
         return r;
     }
 }
-// f[] of columns outside the row: 0
+// f[] of columns outside the row: 0 (only a row's first and last vector have any)
 template <bool ALIGNED> __device__ __forceinline__ void mask(float (&f)[8], int col, int K)
 {
     if constexpr (!ALIGNED) {
+        if (col >= 0 && col + 8 <= K) return;
 #pragma unroll
         for (int i = 0; i < 8; ++i)
             if ((unsigned)(col + i) >= (unsigned)K) f[i] = 0.f;
@@ -128,8 +129,11 @@ __device__ __forceinline__ void reduce_row(float &sum, uint32_t &top, float2 *re
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
-    top = __reduce_max_sync(~0u, top);
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(~0u, sum, o);
+        if (TPR < 32) top = max(top, __shfl_xor_sync(~0u, top, o));
+    }
+    if (TPR >= 32) top = __reduce_max_sync(~0u, top);
     if constexpr (TPR > 32) {
         constexpr int W = TPR / 32;
         if (lane == 0) red[warp] = make_float2(sum, __uint_as_float(top));
@@ -392,9 +396,14 @@ __global__ void __launch_bounds__(block_of(TPR)) rmsnorm_bwd_kernel(const BwdPar
         for (int i = 0; i < ITEMS; ++i) {
             const int col = 8 * (t + i * TPR) - off;
             if (t + i * TPR >= nv) continue;
+            if (ALIGNED && K % 4 == 0) {
+                reinterpret_cast<float4 *>(part + col)[0] = make_float4(gw[i][0], gw[i][1], gw[i][2], gw[i][3]);
+                reinterpret_cast<float4 *>(part + col)[1] = make_float4(gw[i][4], gw[i][5], gw[i][6], gw[i][7]);
+                continue;
+            }
 #pragma unroll
             for (int k = 0; k < 8; ++k)
-                if (ALIGNED || (unsigned)(col + k) < (unsigned)K) part[col + k] = gw[i][k];
+                if ((unsigned)(col + k) < (unsigned)K) part[col + k] = gw[i][k];
         }
     } else {
         for (int s = 0; s < RPB; ++s) {
@@ -471,8 +480,9 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_long_kernel(const BwdParams 
     for (int c = threadIdx.x; c < K; c += 1024) p.part[(int64_t)blockIdx.x * K + c] = gw[c];
 }
 
-// grad_w[k] = sum over the blocks of their sums, in one order
-constexpr int SUM_ROWS = 16;
+// grad_w[k] = sum over the blocks of their sums, in one order: a warp every 32nd row of sums, eight of
+// its loads on their way together
+constexpr int SUM_ROWS = 32;
 __global__ void __launch_bounds__(32 * SUM_ROWS) weight_sum_kernel(const float *part, int rows, int K, float *out)
 {
     __shared__ float s[SUM_ROWS][33];
@@ -482,16 +492,20 @@ __global__ void __launch_bounds__(32 * SUM_ROWS) weight_sum_kernel(const float *
     grid_launch_dependents();
     float a = 0.f;
     if (col < K)
-#pragma unroll 4
-        for (int r = y; r < rows; r += SUM_ROWS) a += part[(int64_t)r * K + col];
+        for (int r = y; r < rows; r += 8 * SUM_ROWS) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = r + i * SUM_ROWS < rows ? __ldcg(part + (int64_t)(r + i * SUM_ROWS) * K + col) : 0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) a += v[i];
+        }
     s[y][x] = a;
     __syncthreads();
-    if (y == 0 && col < K) {
-        a = 0.f;
+    // (column y's sums, over the lanes)
+    a = s[x][y];
 #pragma unroll
-        for (int r = 0; r < SUM_ROWS; ++r) a += s[r][x];
-        out[col] = a;
-    }
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
+    if (x == 0 && blockIdx.x * 32 + y < K) out[blockIdx.x * 32 + y] = a;
 }
 
 // threads a row: of K elements (a row that shifts may touch one vector more).  0: too long for registers
@@ -499,9 +513,11 @@ struct Form { int tpr, items; };
 Form fwd_form(int64_t K)
 {
     const int64_t nv = K % 8 ? K / 8 + 2 : K / 8;
+    if (nv <= 8) return {8, 1};
+    if (nv <= 16) return {16, 1};
     if (nv <= 32) return {32, 1};
-    if (nv <= 64) return {32, 2};
-    if (nv <= 128) return {32, 4};
+    if (nv <= 64) return {64, 1};
+    if (nv <= 128) return {128, 1};
     if (nv <= 256) return {128, 2};
     if (nv <= 512) return {256, 2};
     if (nv <= 1024) return {512, 2};
@@ -510,12 +526,8 @@ Form fwd_form(int64_t K)
 Form bwd_form(int64_t K)
 {
     const int64_t nv = K % 8 ? K / 8 + 2 : K / 8;
-    if (nv <= 32) return {32, 1};
-    if (nv <= 64) return {32, 2};
-    if (nv <= 128) return {128, 1};
-    if (nv <= 256) return {256, 1};
-    if (nv <= 512) return {512, 1};
-    if (nv <= 1024) return {1024, 1};
+    for (int tpr = 8; tpr <= 1024; tpr *= 2)
+        if (nv <= tpr) return {tpr, 1};
     return {0, 0};
 }
 
@@ -542,7 +554,7 @@ template <class T, bool ALIGNED> int fwd_launch(const FwdParams &p, cudaStream_t
 #define FWD(TPR, ITEMS) \
     if (f.tpr == TPR && f.items == ITEMS) \
         return dsq_launch(rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
-    FWD(32, 1) FWD(32, 2) FWD(32, 4) FWD(128, 2) FWD(256, 2) FWD(512, 2)
+    FWD(8, 1) FWD(16, 1) FWD(32, 1) FWD(64, 1) FWD(128, 1) FWD(128, 2) FWD(256, 2) FWD(512, 2)
 #undef FWD
     return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED>, grid, dim3(1024), 0, s, pdl, 0, p);
 }
@@ -557,7 +569,7 @@ template <class T, bool ALIGNED> int bwd_launch(const BwdParams &p, cudaStream_t
 #define BWD(TPR, ITEMS) \
     if (f.tpr == TPR && f.items == ITEMS) \
         return dsq_launch(rmsnorm_bwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
-    BWD(32, 1) BWD(32, 2) BWD(128, 1) BWD(256, 1) BWD(512, 1) BWD(1024, 1)
+    BWD(8, 1) BWD(16, 1) BWD(32, 1) BWD(64, 1) BWD(128, 1) BWD(256, 1) BWD(512, 1) BWD(1024, 1)
 #undef BWD
     static std::atomic<unsigned long long> configured{0};
     const int st = dsq_allow_smem((const void *)rmsnorm_bwd_long_kernel<T, ALIGNED>, (int)(MAX_K * 4), &configured);
