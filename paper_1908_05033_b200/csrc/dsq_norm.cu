@@ -305,8 +305,10 @@ __global__ void __launch_bounds__(1024) rmsnorm_fwd_long_kernel(const FwdParams 
     }
 }
 
+// (16-bit rows: 64 registers, for 1024 threads an SM: 16384 x 1024 36.8 us, so 27.6; binary32 rows
+// would spill: 4096 x 4096 50.8, so 57.8)
 template <class T, int TPR, int ITEMS, bool ALIGNED>
-__global__ void __launch_bounds__(block_of(TPR)) rmsnorm_bwd_kernel(const BwdParams p)
+__global__ void __launch_bounds__(block_of(TPR), sizeof(T) == 2 ? 1024 / block_of(TPR) : 1) rmsnorm_bwd_kernel(const BwdParams p)
 {
     constexpr int RPB = block_of(TPR) / TPR;
     __shared__ float2 red[2][block_of(TPR) / 32];
@@ -513,14 +515,9 @@ struct Form { int tpr, items; };
 Form fwd_form(int64_t K)
 {
     const int64_t nv = K % 8 ? K / 8 + 2 : K / 8;
-    if (nv <= 8) return {8, 1};
-    if (nv <= 16) return {16, 1};
-    if (nv <= 32) return {32, 1};
-    if (nv <= 64) return {64, 1};
-    if (nv <= 128) return {128, 1};
-    if (nv <= 256) return {128, 2};
-    if (nv <= 512) return {256, 2};
-    if (nv <= 1024) return {512, 2};
+    if (K % 8 == 0 && nv > 128 && nv <= 1024) return nv <= 256 ? Form{128, 2} : nv <= 512 ? Form{256, 2} : Form{512, 2};
+    for (int tpr = 8; tpr <= 1024; tpr *= 2)
+        if (nv <= tpr) return {tpr, 1};
     return {0, 0};
 }
 Form bwd_form(int64_t K)
@@ -531,13 +528,14 @@ Form bwd_form(int64_t K)
     return {0, 0};
 }
 
-// blocks: what is resident together; a multiple of eight rows where rows shift
-int grid_of(int64_t M, int64_t K, int tpr, int threads_per_sm)
+// Blocks: what is resident together (per_sm: of the kernel; 0: as many as any takes), a multiple of
+// eight rows where rows shift.
+int grid_of(int64_t M, int64_t K, int tpr, int per_sm)
 {
     const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     const int block = tpr ? block_of(tpr) : 1024, rpb = tpr ? block / tpr : 1;
     int64_t g = (M + rpb - 1) / rpb;
-    const int64_t most = (int64_t)sms * (threads_per_sm / block > 0 ? threads_per_sm / block : 1);
+    const int64_t most = (int64_t)sms * (per_sm > 0 && per_sm < 1024 / block ? per_sm : 1024 / block);
     if (g > most) g = most;
     if (K % 8 && rpb < 8) {
         const int64_t unit = 8 / rpb;
@@ -546,35 +544,60 @@ int grid_of(int64_t M, int64_t K, int tpr, int threads_per_sm)
     return (int)g;
 }
 
+template <class K> int blocks_per_sm(K kernel, int block, std::atomic<int> *cached)
+{
+    int n = cached->load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, block, 0) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        return 0;
+    }
+    cached->store(n, std::memory_order_relaxed);
+    return n;
+}
+
 template <class T, bool ALIGNED> int fwd_launch(const FwdParams &p, cudaStream_t s)
 {
     const Form f = fwd_form(p.K);
     const int pdl = dsq_launch_hooks().pdl;
-    const dim3 grid(grid_of(p.M, p.K, f.tpr, 1024));
 #define FWD(TPR, ITEMS) \
-    if (f.tpr == TPR && f.items == ITEMS) \
-        return dsq_launch(rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
-    FWD(8, 1) FWD(16, 1) FWD(32, 1) FWD(64, 1) FWD(128, 1) FWD(128, 2) FWD(256, 2) FWD(512, 2)
+    if (f.tpr == TPR && f.items == ITEMS) { \
+        static std::atomic<int> fit{0}; \
+        const auto kernel = rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED>; \
+        const dim3 grid(grid_of(p.M, p.K, TPR, blocks_per_sm(kernel, block_of(TPR), &fit))); \
+        return dsq_launch(kernel, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p); \
+    }
+    FWD(8, 1) FWD(16, 1) FWD(32, 1) FWD(64, 1) FWD(128, 1)
+    if constexpr (ALIGNED) {
+        FWD(128, 2) FWD(256, 2) FWD(512, 2)
+    } else {
+        FWD(256, 1) FWD(512, 1) FWD(1024, 1)
+    }
 #undef FWD
-    return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED>, grid, dim3(1024), 0, s, pdl, 0, p);
+    return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED>, dim3(grid_of(p.M, p.K, 0, 1)), dim3(1024), 0, s, pdl, 0, p);
 }
 
-int bwd_grid(int64_t M, int64_t K) { return grid_of(M, K, bwd_form(K).tpr, 1024); }
+// (the workspace is sized for the most blocks that any type takes)
+int bwd_grid(int64_t M, int64_t K) { return grid_of(M, K, bwd_form(K).tpr, 0); }
 
-template <class T, bool ALIGNED> int bwd_launch(const BwdParams &p, cudaStream_t s)
+template <class T, bool ALIGNED> int bwd_launch(const BwdParams &p, cudaStream_t s, int *blocks)
 {
     const Form f = bwd_form(p.K);
     const int pdl = dsq_launch_hooks().pdl;
-    const dim3 grid(bwd_grid(p.M, p.K));
 #define BWD(TPR, ITEMS) \
-    if (f.tpr == TPR && f.items == ITEMS) \
-        return dsq_launch(rmsnorm_bwd_kernel<T, TPR, ITEMS, ALIGNED>, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p);
+    if (f.tpr == TPR && f.items == ITEMS) { \
+        static std::atomic<int> fit{0}; \
+        const auto kernel = rmsnorm_bwd_kernel<T, TPR, ITEMS, ALIGNED>; \
+        *blocks = grid_of(p.M, p.K, TPR, blocks_per_sm(kernel, block_of(TPR), &fit)); \
+        return dsq_launch(kernel, dim3(*blocks), dim3(block_of(TPR)), 0, s, pdl, 0, p); \
+    }
     BWD(8, 1) BWD(16, 1) BWD(32, 1) BWD(64, 1) BWD(128, 1) BWD(256, 1) BWD(512, 1) BWD(1024, 1)
 #undef BWD
     static std::atomic<unsigned long long> configured{0};
     const int st = dsq_allow_smem((const void *)rmsnorm_bwd_long_kernel<T, ALIGNED>, (int)(MAX_K * 4), &configured);
     if (st) return st;
-    return dsq_launch(rmsnorm_bwd_long_kernel<T, ALIGNED>, grid, dim3(1024), (size_t)p.K * 4, s, pdl, 0, p);
+    *blocks = grid_of(p.M, p.K, 0, 1);
+    return dsq_launch(rmsnorm_bwd_long_kernel<T, ALIGNED>, dim3(*blocks), dim3(1024), (size_t)p.K * 4, s, pdl, 0, p);
 }
 
 int check_shape(int64_t M, int64_t K, int dtype)
@@ -638,14 +661,15 @@ int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h, const
     p.inv_k = (float)(1.0 / (double)K);
     cudaStream_t s = (cudaStream_t)stream;
     const bool al = K % 8 == 0;
+    int blocks = 0;
     switch (dtype) {
-    case DSQ_F32: st = al ? bwd_launch<float, true>(p, s) : bwd_launch<float, false>(p, s); break;
-    case DSQ_BF16: st = al ? bwd_launch<__nv_bfloat16, true>(p, s) : bwd_launch<__nv_bfloat16, false>(p, s); break;
-    default: st = al ? bwd_launch<__half, true>(p, s) : bwd_launch<__half, false>(p, s); break;
+    case DSQ_F32: st = al ? bwd_launch<float, true>(p, s, &blocks) : bwd_launch<float, false>(p, s, &blocks); break;
+    case DSQ_BF16: st = al ? bwd_launch<__nv_bfloat16, true>(p, s, &blocks) : bwd_launch<__nv_bfloat16, false>(p, s, &blocks); break;
+    default: st = al ? bwd_launch<__half, true>(p, s, &blocks) : bwd_launch<__half, false>(p, s, &blocks); break;
     }
     if (st || !grad_weight) return st;
     return dsq_launch(weight_sum_kernel, dim3((unsigned)((K + 31) / 32)), dim3(32 * SUM_ROWS), 0, s,
-                      dsq_launch_hooks().pdl, 0, p.part, bwd_grid(M, K), (int)K, grad_weight);
+                      dsq_launch_hooks().pdl, 0, p.part, blocks, (int)K, grad_weight);
 }
 
 }  // extern "C"
