@@ -49,61 +49,20 @@ __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[8]) { tmem_ld
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x16(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32(at, r); }
 
-// COUNT instructions (32 bytes of K each) with A in tensor memory, issued by one elected lane of a
-// converged warp; the first takes the accumulate flag.
-#define DSQ_TS_1(KIND)                                                                                       \
-    asm volatile("{\n\t.reg .pred p, pe;\n\t.reg .b64 d0;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 d0, {%2, %3};\n\t" \
-                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t}" ::"r"(d),          \
-                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
-                 : "memory")
-#define DSQ_TS_2(KIND)                                                                                       \
-    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1;\n\t.reg .b32 l1, a1;\n\t"                    \
-                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\tadd.u32 l1, %2, 2;\n\tadd.u32 a1, %1, 8;\n\t" \
-                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\telect.sync _|pe, 0xffffffff;\n\t"          \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t}" ::"r"(d),          \
-                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
-                 : "memory")
-#define DSQ_TS_4(KIND)                                                                                       \
-    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1, d2, d3;\n\t.reg .b32 l1, l2, l3, a1, a2, a3;\n\t" \
-                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\t"                                       \
-                 "add.u32 l1, %2, 2;\n\tadd.u32 l2, %2, 4;\n\tadd.u32 l3, %2, 6;\n\t"                         \
-                 "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"                       \
-                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\tmov.b64 d2, {l2, %3};\n\tmov.b64 d3, {l3, %3};\n\t" \
-                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t"                     \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a2], d2, %4, q;\n\t"                     \
-                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a3], d3, %4, q;\n\t}" ::"r"(d),          \
-                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
-                 : "memory")
-template <bool INT, int COUNT>
-__device__ __forceinline__ void mma_ts_elect(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
-                                             uint32_t accumulate)
+// D (+)= A B^T with A in tensor memory, by one thread
+template <bool INT>
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
 {
-    static_assert(COUNT == 1 || COUNT == 2 || COUNT == 4, "instructions of a block");
-    if constexpr (COUNT == 1) {
-        if (INT) DSQ_TS_1("i8");
-        else DSQ_TS_1("f16");
-    } else if constexpr (COUNT == 2) {
-        if (INT) DSQ_TS_2("i8");
-        else DSQ_TS_2("f16");
-    } else {
-        if (INT) DSQ_TS_4("i8");
-        else DSQ_TS_4("f16");
-    }
-}
-#undef DSQ_TS_1
-#undef DSQ_TS_2
-#undef DSQ_TS_4
-
-// loads that stay where they stand: a turn ahead of their use
-__device__ __forceinline__ uint4 load_ahead(const uint8_t *p)
-{
-    uint4 v;
-    asm volatile("ld.global.nc.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-    return v;
+    if (INT)
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
+                     "r"(idesc), "r"(accumulate)
+                     : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+                     "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
+                     "r"(idesc), "r"(accumulate)
+                     : "memory");
 }
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const float *src)
 {
@@ -126,6 +85,10 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, unsigned l
         }
     }
 }
+__device__ __forceinline__ bool wait_thread(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
+{
+    return mbar_try_wait(bar, parity, 20u) || wait_slow(bar, parity, limit_ns);
+}
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
 {
     bool ok = mbar_try_wait(bar, parity, 20u);
@@ -133,41 +96,70 @@ __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigne
     return __all_sync(~0u, ok);
 }
 
+// Values of a word's codes 2 b and 2 b + 1 (byte b) as a pair of 16-bit numbers, in that order.  The fields
+// c + 8 stay where the byte has them, in the low half at bit 0 and in the high half at bit 4: as denormal
+// numbers, which two different powers of two make (c + 8) 2^-6 (bf16) or 2^-9 (fp16) of, exactly, in the
+// fused operation that takes 8 or 7.5 of them off.
+template <int XT> __device__ __forceinline__ uint32_t byte_values(uint32_t w, int b, uint32_t less)
+{
+    const uint32_t y = __byte_perm(w, w, 0x1111 * b);
+    uint32_t v;                       // (y & mask) ^ sign bits
+    asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(v) : "r"(y), "r"(0x00F0000Fu), "r"(0x00800008u));
+    if (XT == DSQ_BF16) {
+        const uint32_t scale = 0x7D007F00u;                       // 2^123, 2^127
+        const __nv_bfloat162 r = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&v),
+                                         *reinterpret_cast<const __nv_bfloat162 *>(&scale),
+                                         *reinterpret_cast<const __nv_bfloat162 *>(&less));
+        return *reinterpret_cast<const uint32_t *>(&r);
+    }
+    const uint32_t scale = 0x68007800u;                           // 2^11, 2^15
+    const __half2 r = __hfma2(*reinterpret_cast<const __half2 *>(&v), *reinterpret_cast<const __half2 *>(&scale),
+                              *reinterpret_cast<const __half2 *>(&less));
+    return *reinterpret_cast<const uint32_t *>(&r);
+}
+// -7.5 or -8 units, twice, and what the sums are then multiples of (int8 values are 8 (2 c + 1) or 16 c)
+template <int XT> __device__ __forceinline__ uint32_t byte_less(int odd)
+{
+    return XT == DSQ_BF16 ? (odd ? 0xBDF0BDF0u : 0xBE00BE00u) : (odd ? 0xA380A380u : 0xA400A400u);
+}
+template <int XT> __device__ __forceinline__ float byte_unit(int odd)
+{
+    return XT == DSQ_I8 ? (odd ? 0.125f : 0.0625f) : XT == DSQ_BF16 ? (odd ? 128.f : 64.f) : (odd ? 1024.f : 512.f);
+}
+
 constexpr int AHEAD = 8;          // chunks whose scales are on their way
-// MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum
-template <int XT, int MC, int GP, int TEAMS, int STAGES> struct Layout {
+// MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum; TEAMS, TAKES: of four warps
+template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES> struct Layout {
     static constexpr bool INT = XT == DSQ_I8;
     static constexpr int NC = MC < 16 ? 16 : MC;                  // columns of an instruction
     static constexpr int FLUSHES = 4 / GP;                        // sums of a chunk
     static constexpr int AC = INT ? 32 : 64;                      // tensor-memory columns of a chunk's values
-    // places of a team for its sums (a power of two): the phases of a place's barriers are waited for in
-    // order by the team's issuing warp, so no two teams share one
-    static constexpr int ABUF = TEAMS * (2 * AC + NC) <= 512 ? 2 : 1;         // buffers of a team's values
-    static constexpr int ROOM = (512 - TEAMS * ABUF * AC) / (TEAMS * NC), PLACES = ROOM >= 4 ? 4 : ROOM >= 2 ? 2 : 1;
-    static constexpr int SLOTS = TEAMS * PLACES;
-    static constexpr int A_COL = SLOTS * NC;
-    static constexpr int USED = A_COL + TEAMS * ABUF * AC;
-    static constexpr int COLS = USED <= 128 ? 128 : USED <= 256 ? 256 : 512;
-    static constexpr int XBUF = NC * (INT ? 128 : 256);
-    static constexpr int X_AT = 1024, RING_AT = X_AT + TEAMS * 2 * XBUF;
-    static constexpr int STAGE = 128 * 128;                       // two chunks
-    static constexpr int S_AT = RING_AT + TEAMS * STAGES * STAGE, S_STAGE = FLUSHES * 512;    // scales of a chunk
-    static constexpr int BYTES = S_AT + AHEAD * S_STAGE + 1024;              // (its start is aligned to 1024)
-    static constexpr int THREADS = (TEAMS + 1) * 128;
-    // barriers: sums ready and place free of each slot, values read of each team
-    static constexpr int READY = 16, FREE = READY + 8 * SLOTS, READ = FREE + 8 * SLOTS;
-    static_assert(ROOM >= 1 && USED <= 512 && READ + 16 * TEAMS <= X_AT, "tensor memory");
+    static constexpr int SLOTS = NC > 32 || (NC > 16 && FLUSHES < 4) ? 4 : 8;                 // places for sums
+    static constexpr int A_COL = SLOTS * NC, VALUES = STAGES >= 8 && A_COL + 8 * AC <= 512 ? 8 : 4;         // places for values
+    static constexpr int XBOX = NC * 128, XBOXES = INT ? 2 : 4;   // 128 bytes of K of the rows; of two chunks
+    static constexpr int WBOX = 128 * 128, STAGE = WBOX + XBOXES * XBOX;
+    static constexpr int RING_AT = 1024, S_AT = RING_AT + STAGES * STAGE, S_STAGE = FLUSHES * 512;
+    static constexpr int BYTES = S_AT + TAKES * AHEAD * S_STAGE + 1024;      // (its start is aligned to 1024)
+    static constexpr int ISSUERS = 2 * FLUSHES <= SLOTS ? 2 : 1;  // chunks in turn; each has places of its own
+    static constexpr int WORKERS = (TEAMS + TAKES) * 128, THREADS = WORKERS + 96;
+    // barriers: a stage is full and empty, values made and read, sums ready and place free, all is done
+    static constexpr int FULL = 16, EMPTY = FULL + 8 * STAGES, MADE = EMPTY + 8 * STAGES, READ = MADE + 8 * VALUES;
+    static constexpr int READY = READ + 8 * VALUES, FREE = READY + 8 * SLOTS, DONE = FREE + 8 * SLOTS;
+    static_assert(DONE + 16 <= RING_AT, "barriers");
     static_assert(BYTES <= 227 * 1024 && BYTES > 116 * 1024, "one block an SM");
-    static_assert(MC * 512 <= TEAMS * STAGES * STAGE, "the totals take the rings' place");
+    static_assert(MC * 512 <= STAGES * STAGE, "the totals take the ring's place");
+    // (a team that has seen the values' last use but one read knows all earlier stages full: wait_full)
+    static_assert(TEAMS <= VALUES && VALUES <= 2 * STAGES && A_COL + VALUES * AC <= 512, "phases are waited for in order");
 };
 
-template <int XT, int MC, int GP, int TEAMS, int STAGES>
-__global__ void __launch_bounds__((TEAMS + 1) * 128, 1)
-wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long long wait_ns)
+template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES>
+__global__ void __launch_bounds__((TEAMS + TAKES) * 128 + 96, 1)
+wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
+                      const DsqGroupGemm p, const int split, const unsigned long long wait_ns)
 {
-    using L = Layout<XT, MC, GP, TEAMS, STAGES>;
+    using L = Layout<XT, MC, GP, TEAMS, TAKES, STAGES>;
     constexpr bool INT = L::INT;
-    constexpr int FLUSHES = L::FLUSHES;
+    constexpr int FLUSHES = L::FLUSHES, MCT = MC / TAKES;
     extern __shared__ uint8_t raw_smem[];
     const uint32_t smem = (smem_u32(raw_smem) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -178,20 +170,28 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     const int rows = min(p.M - m0, MC);
     const int all = (p.K + 127) >> 7;
     // whole pairs of chunks to a block
-    const int pairs = (all + 1) >> 1, c0 = 2 * (int)((int64_t)pairs * rank / split);
-    const int chunks = min(2 * (int)((int64_t)pairs * (rank + 1) / split), all) - c0;
+    const int every = (all + 1) >> 1, c0 = 2 * (int)((int64_t)every * rank / split);
+    const int chunks = min(2 * (int)((int64_t)every * (rank + 1) / split), all) - c0, pairs = (chunks + 1) >> 1;
     const int last = (int)min((int64_t)127, p.N - 1 - n0);       // row of weights of this block
 
     if (warp == 0) {
-        tmem_alloc(smem, L::COLS);
+        tmem_alloc(smem, 512);
         tmem_relinquish();
     }
     if (threadIdx.x == 0) {
+        for (int i = 0; i < STAGES; ++i) {
+            mbar_init(smem + L::FULL + 8 * i, 1);
+            mbar_init(smem + L::EMPTY + 8 * i, L::ISSUERS);
+        }
+        for (int i = 0; i < L::VALUES; ++i) {
+            mbar_init(smem + L::MADE + 8 * i, 4);
+            mbar_init(smem + L::READ + 8 * i, 1);
+        }
         for (int i = 0; i < L::SLOTS; ++i) {
             mbar_init(smem + L::READY + 8 * i, 1);
-            mbar_init(smem + L::FREE + 8 * i, 4);
+            mbar_init(smem + L::FREE + 8 * i, 4 * TAKES);
         }
-        for (int i = 0; i < 2 * TEAMS; ++i) mbar_init(smem + L::READ + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) mbar_init(smem + L::DONE + 8 * i, 1);
         mbar_init_fence();
     }
     tc_fence_before_sync();
@@ -199,158 +199,66 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
     tc_fence_after_sync();
     const uint32_t tmem = lds_32(smem);
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);    // this warp's 32 lanes
-    bool ok = true;
-    auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(smem + bar, parity, ok ? wait_ns : 0) && ok; };
+    bool ok = true;               // (a role whose wait ran out stops; the others' waits run out in turn)
+    auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(smem + bar, parity, wait_ns); return ok; };
     grid_dependency_wait();
     grid_launch_dependents();
 
-    float total[MC];                                             // (of the last team's threads)
+    float total[MCT];                                            // (of the takers' threads)
 #pragma unroll
-    for (int i = 0; i < MC; ++i) total[i] = 0.f;
+    for (int i = 0; i < MCT; ++i) total[i] = 0.f;
     if (team < TEAMS) {
-        const uint32_t xbuf = smem + L::X_AT + team * 2 * L::XBUF;
-        const uint32_t ring = smem + L::RING_AT + team * STAGES * L::STAGE;
-        // the team's chunks: c0 + 2 (team + TEAMS i) and the one behind it
-        const int my_pairs = 2 * team < chunks ? ((chunks + 1) / 2 - team - 1) / TEAMS + 1 : 0;
-        const int turns = my_pairs == 0 ? 0 : 2 * my_pairs - ((chunks & 1) && (chunks / 2) % TEAMS == team);
-        // Copies of this warp's 32 rows of the team's next two chunks: 16-byte piece j of a row's 128.  (Rows
-        // behind the last are the last: their sums are not used.)
-        const int j = lane & 7, mine = (warp & 3) * 32 + (lane >> 3);
-        const uint8_t *src = p.W + n0 * p.pitch;
-        int row_at[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k) row_at[k] = min(mine + 4 * k, last) * p.pitch;
-        const uint32_t w_to = mine * 128;
-        int w_left = my_pairs, w_k = (c0 + 2 * team) * 64 + 16 * j;
-        uint32_t w_stage = ring;
-        auto issue_w = [&]() {
-            if (w_left > 0) {
-                const bool in = w_k < p.pitch;
-                const uint8_t *s = src + (in ? w_k : 0);
-                const uint32_t bytes = in ? 16u : 0u;
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    cp_async_16(w_stage + w_to + k * 512 + ((j ^ (mine + 4 * k)) & 7) * 16, s + row_at[k], bytes);
-            }
-            --w_left;
-            w_k += TEAMS * 128;
-            w_stage = w_stage == ring + (STAGES - 1) * L::STAGE ? ring : w_stage + L::STAGE;
-            cp_async_commit();
-        };
-        // X of a chunk: 16-byte pieces of its rows, spread over the team: piece pc of rows r0, r0 + RS, ...
-        constexpr int PIECES = INT ? 8 : 16, RS = 128 / PIECES, XP = (MC + RS - 1) / RS;
-        constexpr int ELEMENT = INT ? 1 : 2;
-        const int pc = row % PIECES, r0 = row / PIECES;
-        // (rows behind the last are the last: their columns of D are not read)
-        const uint8_t *xsrc = p.X + (int64_t)m0 * p.K * ELEMENT + 16 * pc;
-        uint32_t x_at[XP];
-#pragma unroll
-        for (int k = 0; k < XP; ++k) x_at[k] = (uint32_t)min(r0 + k * RS, rows - 1) * (uint32_t)(p.K * ELEMENT);
-        const uint32_t x_to = xbuf + (pc >> 3) * (L::NC * 128) + r0 * 128 + (((pc & 7) ^ (r0 & 7)) << 4);
-        static_assert(RS % 8 == 0 && XP * RS <= L::NC, "the swizzle of a thread's rows is one");
-        uint4 x[XP];
-        int l_turn = 0, l_k = (c0 + 2 * team) * (PIECES * 16);   // bytes into the row
-        auto load_x = [&]() {
-            if (l_turn < turns && l_k + 16 * pc < p.K * ELEMENT) {
-                const uint8_t *s = xsrc + l_k;
-#pragma unroll
-                for (int k = 0; k < XP; ++k) x[k] = load_ahead(s + x_at[k]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < XP; ++k) x[k] = make_uint4(0u, 0u, 0u, 0u);
-            }
-            l_k += (l_turn & 1 ? 2 * TEAMS - 1 : 1) * (PIECES * 16);
-            ++l_turn;
-        };
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) issue_w();
-        load_x();
-        const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
-        const uint32_t base = dsq_value_base<XT>(p.odd), one = p.odd ? 0x08080808u : 0u;
-        // instructions of the team's chunk i have read its values and X
-        auto wait_read = [&](int i) { wait(L::READ + 16 * team + 8 * (i % L::ABUF), (i / L::ABUF) & 1); };
-        uint32_t r_stage = ring;
+        // values of the chunks team, team + TEAMS, ...: a row of 128 codes a thread
+        const uint32_t less = byte_less<XT>(p.odd), one = p.odd ? 0x08080808u : 0u;
+        int v = team, stage = team >> 1;
+        uint32_t v_phase = 1, s_phase = 0;
 #pragma unroll 1
-        for (int i = 0; i < turns; ++i) {
-            if ((i & 1) == 0) {
-                cp_async_wait<STAGES - 2>();
-                __syncwarp();     // the two chunks' codes are here, and those before them have been read
-                issue_w();
-            }
-            // (X has two buffers too: its last chunk but one has been waited for)
-            if (L::ABUF == 2 && i >= 2) wait_read(i - 2);
-            const uint32_t a_col = L::A_COL + (team * L::ABUF + i % L::ABUF) * L::AC;
-#pragma unroll
-            for (int k = 0; k < XP; ++k) {
-                const uint4 v = x[k];
-                const uint32_t to = x_to + (i & 1) * L::XBUF + k * (RS * 128);
-                if (INT)
-                    sts_128(to, __byte_perm(v.x, v.y, 0x6420), __byte_perm(v.x, v.y, 0x7531),
-                            __byte_perm(v.z, v.w, 0x6420), __byte_perm(v.z, v.w, 0x7531));
-                else
-                    sts_128(to, __byte_perm(v.x, v.z, 0x5410), __byte_perm(v.x, v.z, 0x7632),
-                            __byte_perm(v.y, v.w, 0x5410), __byte_perm(v.y, v.w, 0x7632));
-            }
-            fence_proxy_async_smem();
-            load_x();
-            const uint32_t codes = r_stage + row * 128;
-            if (i & 1) r_stage = r_stage == ring + (STAGES - 1) * L::STAGE ? ring : r_stage + L::STAGE;
-            // the values of this row's codes, 32 columns at a time
+        for (int c = team; c < chunks; c += TEAMS) {
+            // (in this order: that the place's last values have been read says that all stages before the
+            // last STAGES are full, without which a phase's parity could be an older one's)
+            if (c >= L::VALUES && !wait(L::READ + 8 * v, v_phase)) break;
+            if (!wait(L::FULL + 8 * stage, s_phase)) break;
+            tc_fence_after_sync();
+            const uint32_t codes = smem + L::RING_AT + stage * L::STAGE + row * 128, to = lanes + L::A_COL + v * L::AC;
 #pragma unroll
             for (int h = 0; h < L::AC / 32; ++h) {
-                constexpr int P16 = INT ? 4 : 2;                  // 16-byte pieces of the row
+                constexpr int P16 = INT ? 4 : 2;                  // 16-byte pieces of the row, 32 columns
                 uint32_t a[32];
 #pragma unroll
                 for (int q = 0; q < P16; ++q) {
-                    const uint4 w4 = lds_128(codes + (((4 * (i & 1) + P16 * h + q) ^ row) & 7) * 16);
+                    const uint4 w4 = lds_128(codes + (((4 * (c & 1) + P16 * h + q) ^ row) & 7) * 16);
                     const uint32_t w[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
                         if constexpr (INT) {
-                            a[8 * q + 2 * k] = ((w[k] << 4) & 0xF0F0F0F0u) | one;
-                            a[8 * q + 2 * k + 1] = (w[k] & 0xF0F0F0F0u) | one;
+                            const uint32_t even = ((w[k] << 4) & 0xF0F0F0F0u) | one, odd = (w[k] & 0xF0F0F0F0u) | one;
+                            a[8 * q + 2 * k] = __byte_perm(even, odd, 0x5140);
+                            a[8 * q + 2 * k + 1] = __byte_perm(even, odd, 0x7362);
                         } else {
 #pragma unroll
-                            for (int e = 0; e < 4; ++e) a[16 * q + 4 * k + e] = dsq_value_pair<XT>(w[k], e, base);
+                            for (int e = 0; e < 4; ++e) a[16 * q + 4 * k + e] = byte_values<XT>(w[k], e, less);
                         }
                     }
                 }
-                if (L::ABUF == 1 && h == 0 && i > 0) wait_read(i - 1);
-                tmem_st_32x32(lanes + a_col + 32 * h, a);
+                tmem_st_32x32(to + 32 * h, a);
             }
             tmem_st_wait();
             tc_fence_before_sync();
-            named_barrier_sync(1 + team, 128);
-            if ((warp & 3) == 0) {
-                const uint64_t desc = smem_desc_sw128(xbuf + (i & 1) * L::XBUF);
-                const uint32_t hi = (uint32_t)(desc >> 32);
-#pragma unroll
-                for (int f = 0; f < FLUSHES; ++f) {
-                    const uint32_t use = i * FLUSHES + f, slot = team * L::PLACES + use % L::PLACES;
-                    if (use >= L::PLACES) wait(L::FREE + 8 * slot, ((use / L::PLACES) & 1) ^ 1);
-                    tc_fence_after_sync();
-                    constexpr int COUNT = L::AC / 8 / FLUSHES, BLOCK = COUNT < 4 ? COUNT : 4;
-#pragma unroll
-                    for (int b = 0; b < COUNT / BLOCK; ++b) {
-                        const int at = (f * COUNT + b * BLOCK) * 32;          // bytes into the chunk's rows
-                        mma_ts_elect<INT, BLOCK>(tmem + slot * L::NC, tmem + a_col + (f * COUNT + b * BLOCK) * 8,
-                                                 (uint32_t)desc + (((at >> 7) * (L::NC * 128) + (at & 127)) >> 4), hi, idesc, b);
-                    }
-                    mma_commit_elect(smem + L::READY + 8 * slot);
-                }
-                mma_commit_elect(smem + L::READ + 16 * team + 8 * (i % L::ABUF));
-                __syncwarp();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(smem + L::MADE + 8 * v);
+            v += TEAMS;
+            if (v >= L::VALUES) {
+                v -= L::VALUES;
+                v_phase ^= 1;
             }
+            stage = ((c + TEAMS) >> 1) % STAGES;
+            s_phase = (((c + TEAMS) >> 1) / STAGES) & 1;
         }
-        // the last instructions read X and the values to the end
-        for (int i = max(0, turns - L::ABUF); i < turns; ++i) {
-            wait_read(i);
-            if (!ok) wait_warp(smem + L::READ + 16 * team + 8 * (i % L::ABUF), (i / L::ABUF) & 1, DRAIN_NS);
-        }
-    } else {
+    } else if (team < TEAMS + TAKES) {
         // A row's scales go through a ring of their own, each thread's copies for itself.  (A chunk ahead, in
         // registers, the wait for them was the kernel's time: 32 times 0.6 us.)
-        const uint32_t s_ring = smem + L::S_AT + row * 4;
+        const uint32_t s_ring = smem + L::S_AT + (team - TEAMS) * (AHEAD * L::S_STAGE) + row * 4;
+        const uint32_t from = lanes + (team - TEAMS) * MCT;
         const float *scales = p.scales + n0 + min(row, last);
         auto issue_s = [&](int c) {
             if (c < chunks) {
@@ -364,9 +272,8 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
         };
 #pragma unroll 1
         for (int c = 0; c < AHEAD - 1; ++c) issue_s(c);
-        uint32_t of = 0, turn = 0;                               // the chunk's team, and its turn there
 #pragma unroll 1
-        for (int i = 0; i < chunks; ++i) {
+        for (int i = 0; i < chunks && ok; ++i) {
             cp_async_wait<AHEAD - 2>();
             float now[FLUSHES];
 #pragma unroll
@@ -375,16 +282,17 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
             issue_s(i + AHEAD - 1);
 #pragma unroll
             for (int f = 0; f < FLUSHES; ++f) {
-                const uint32_t use = turn * FLUSHES + f, slot = of * L::PLACES + use % L::PLACES;
-                wait(L::READY + 8 * slot, (use / L::PLACES) & 1);
+                const uint32_t use = i * FLUSHES + f, slot = use % L::SLOTS;
+                wait(L::READY + 8 * slot, (use / L::SLOTS) & 1);
+                if (!ok) break;
                 tc_fence_after_sync();
-                constexpr int STEP = MC < 32 ? MC : 32;
+                constexpr int STEP = MCT < 32 ? MCT : 32;
 #pragma unroll
-                for (int h = 0; h < MC / STEP; ++h) {
+                for (int h = 0; h < MCT / STEP; ++h) {
                     uint32_t v[STEP];
-                    ld_cols(lanes + slot * L::NC + h * STEP, v);
+                    ld_cols(from + slot * L::NC + h * STEP, v);
                     tmem_ld_wait();
-                    if (h == MC / STEP - 1) {                     // the place is free again
+                    if (h == MCT / STEP - 1) {                    // the place is free again
                         tc_fence_before_sync();
                         __syncwarp();
                         if (lane == 0) mbar_arrive(smem + L::FREE + 8 * slot);
@@ -395,47 +303,120 @@ wgemm_group_tc_kernel(const DsqGroupGemm p, const int split, const unsigned long
                                                         total[h * STEP + e]);
                 }
             }
-            if ((i & 1) == 0) {
-                ++turn;
-            } else if (++of == TEAMS) {
-                of = 0;
-                ++turn;
-            } else {
-                --turn;
+        }
+        cp_async_wait<0>();
+    } else if (warp == L::WORKERS / 32) {
+        // copies: two chunks' codes of 128 rows, whole lines, and X's rows beside them
+        int issued = 0;
+        for (; issued < pairs; ++issued) {
+            const int stage = issued % STAGES;
+            if (issued >= STAGES && !wait(L::EMPTY + 8 * stage, ((issued / STAGES) & 1) ^ 1)) break;
+            if (lane == 0) {
+                const uint32_t to = smem + L::RING_AT + stage * L::STAGE, bar = smem + L::FULL + 8 * stage;
+                const int at = (c0 >> 1) + issued;
+                mbar_arrive_expect_tx(bar, L::STAGE);
+                tma_load_2d(to, &map_w, at * 128, (int)n0, bar);
+#pragma unroll
+                for (int b = 0; b < L::XBOXES; ++b)
+                    tma_load_2d(to + L::WBOX + b * L::XBOX, &map_x, (at * L::XBOXES + b) * 128, m0, bar);
+            }
+            __syncwarp();
+        }
+        // no copy is under way when the block ends
+        for (int i = max(0, issued - STAGES); i < issued; ++i)
+            if (!wait_warp(smem + L::FULL + 8 * (i % STAGES), (i / STAGES) & 1, ok ? wait_ns : DRAIN_NS)) ok = false;
+    } else if (const int q = warp - L::WORKERS / 32 - 1; lane == 0 && q < L::ISSUERS) {
+        // One thread issues, or two that take chunks in turn: what it does lies in every chunk's way (commits and
+        // waits 0.2 us a chunk, instructions 0.03 us each), so places and phases are constants of an unrolled loop.
+        constexpr int IS = L::ISSUERS, COUNT = L::AC / 8 / FLUSHES;
+        constexpr int ROUND = 2 * L::SLOTS / FLUSHES, UNROLL = ROUND > 2 * L::VALUES ? ROUND : 2 * L::VALUES;
+        static_assert(UNROLL * FLUSHES % (2 * L::SLOTS) == 0 && UNROLL <= 2 * STAGES, "constants");
+        const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
+        auto wait1 = [&](uint32_t bar, uint32_t parity) { ok = wait_thread(smem + bar, parity, wait_ns); return ok; };
+        const uint64_t desc = smem_desc_sw128(smem + L::RING_AT + L::WBOX) + (uint32_t)(q * (L::XBOXES / 2) * (L::XBOX >> 4));
+        const uint32_t d0 = tmem + q * FLUSHES * L::NC, a0 = tmem + L::A_COL + q * L::AC, made = L::MADE + 8 * q,
+                       read = L::READ + 8 * q, ready = L::READY + 8 * FLUSHES * q, free = L::FREE + 8 * FLUSHES * q;
+#pragma unroll 1
+        for (int base = q; base < chunks && ok; base += UNROLL) {
+            const int stage0 = (base >> 1) % STAGES;
+            const uint32_t s_phase = ((base >> 1) / STAGES) & 1;
+            const uint64_t x0 = desc + (uint32_t)(stage0 * (L::STAGE >> 4));
+#pragma unroll
+            for (int u = 0; u < UNROLL; u += IS) {
+                const int v = u % L::VALUES;
+                if (base + u >= chunks) break;
+                if ((u & 1) == 0 && !wait1(L::FULL + 8 * (stage0 + u / 2), s_phase)) break;
+                if (!wait1(made + 8 * v, (u / L::VALUES) & 1)) break;
+#pragma unroll
+                for (int f = 0; f < FLUSHES; ++f) {
+                    const int use = u * FLUSHES + f, slot = use % L::SLOTS;
+                    if ((base >= UNROLL || use >= L::SLOTS) && !wait1(free + 8 * slot, ((use / L::SLOTS) & 1) ^ 1)) break;
+                    tc_fence_after_sync();
+#pragma unroll
+                    for (int i = 0; i < COUNT; ++i) {
+                        const int at = (f * COUNT + i) * 32 + (u & 1) * (L::XBOXES / 2) * 128;     // bytes into the pair's rows
+                        mma_ts<INT>(d0 + slot * L::NC, a0 + v * L::AC + (f * COUNT + i) * 8,
+                                    x0 + (uint32_t)((u / 2 * L::STAGE + (at >> 7) * L::XBOX + (at & 127)) >> 4), idesc, i > 0);
+                    }
+                    mma_commit(smem + ready + 8 * slot);
+                }
+                if (!ok) break;
+                mma_commit(smem + read + 8 * v);
+                if (IS == 2 || (u & 1)) mma_commit(smem + L::EMPTY + 8 * (stage0 + u / 2));
             }
         }
+        // no instruction is under way when tensor memory is given up
+        mma_commit(smem + L::DONE + 8 * q);
+        if (!wait_thread(smem + L::DONE + 8 * q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
     }
-    cp_async_wait<0>();
     tc_fence_before_sync();
+    __syncwarp();
     const int failed = __syncthreads_or(!ok);
     if (warp == 0) {
         tc_fence_after_sync();
-        tmem_dealloc(lds_32(smem), L::COLS);
+        tmem_dealloc(lds_32(smem), 512);
     }
+    const bool takes = team >= TEAMS && team < TEAMS + TAKES;
     if (split == 1) {
-        if (team == TEAMS && row <= last) {
-            const float unit = failed ? __uint_as_float(0x7FC00000u) : dsq_value_unit<XT>(p.odd);
+        if (takes && row <= last) {
+            const float unit = failed ? __uint_as_float(0x7FC00000u) : byte_unit<XT>(p.odd);
 #pragma unroll
-            for (int m = 0; m < MC; ++m)
-                if (m < rows) p.store(m0 + m, n0 + row, total[m] * unit);
+            for (int i = 0; i < MCT; ++i) {
+                const int m = (team - TEAMS) * MCT + i;
+                if (m < rows) p.store(m0 + m, n0 + row, total[i] * unit);
+            }
         }
         return;
     }
     // the totals of the cluster's blocks, [row of X][row of weights], added in their order
     const uint32_t sums = smem + L::RING_AT;
-    if (team == TEAMS) {
+    if (takes) {
 #pragma unroll
-        for (int m = 0; m < MC; ++m)
-            sts_32(sums + (m * 128 + row) * 4, failed ? 0x7FC00000u : __float_as_uint(total[m]));
+        for (int i = 0; i < MCT; ++i)
+            sts_32(sums + (((team - TEAMS) * MCT + i) * 128 + row) * 4, failed ? 0x7FC00000u : __float_as_uint(total[i]));
     }
     cluster_sync_all();
-    const float unit = dsq_value_unit<XT>(p.odd);
-    for (int m = rank + team * split; m < rows; m += (TEAMS + 1) * split) {
-        float s = 0.f;
-        for (int r = 0; r < split; ++r) s += __uint_as_float(ld_cluster_32(map_to_cta(sums + (m * 128 + row) * 4, r)));
-        if (row <= last) p.store(m0 + m, n0 + row, s * unit);
-    }
+    const float unit = byte_unit<XT>(p.odd);
+    if (team < TEAMS + TAKES)
+        for (int m = rank + team * split; m < rows; m += (TEAMS + TAKES) * split) {
+            float s = 0.f;
+            for (int r = 0; r < split; ++r) s += __uint_as_float(ld_cluster_32(map_to_cta(sums + (m * 128 + row) * 4, r)));
+            if (row <= last) p.store(m0 + m, n0 + row, s * unit);
+        }
     cluster_sync_all();           // nobody leaves while its sums are read
+}
+
+// rows of bytes, in boxes of 128 of them by box_rows, in the 128-byte swizzle; zeros behind the ends
+int make_map(CUtensorMap *map, const void *base, uint64_t bytes, uint64_t rows, uint64_t pitch, int box_rows)
+{
+    const DsqEncodeTiledFn fn = dsq_encode_tiled_fn();
+    if (!fn) return DSQ_ERR_CUDA;
+    const cuuint64_t dims[2] = {bytes, rows}, strides[1] = {pitch};
+    const cuuint32_t box[2] = {128, (cuuint32_t)box_rows}, step[2] = {1, 1};
+    const CUresult r = fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, step,
+                          CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                          CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DSQ_OK : DSQ_ERR_CUDA;
 }
 
 // Clusters of `split` blocks that run at once (a GPC's SMs bound them: of eight blocks fewer than 148 / 8).
@@ -463,13 +444,13 @@ template <class K> int active_clusters(K kernel, int split, int threads, int byt
 }
 
 // est_us: the launch's estimated time is written there and nothing is launched
-template <int XT, int MC, int GP, int TEAMS, int STAGES>
+template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES>
 int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
-    using L = Layout<XT, MC, GP, TEAMS, STAGES>;
+    using L = Layout<XT, MC, GP, TEAMS, TAKES, STAGES>;
     static std::atomic<unsigned long long> configured{0};
     static std::atomic<int> active[4];
-    const auto kernel = wgemm_group_tc_kernel<XT, MC, GP, TEAMS, STAGES>;
+    const auto kernel = wgemm_group_tc_kernel<XT, MC, GP, TEAMS, TAKES, STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, L::BYTES, &configured);
     if (st) return st;
     const int64_t tiles = (p.N + 127) / 128, mt = (p.M + MC - 1) / MC;
@@ -495,17 +476,23 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
         return DSQ_OK;
     }
     if (tiles * split > 0x7FFFFFFF || mt > 65535) return DSQ_ERR_SIZE;
+    CUtensorMap map_w, map_x;
+    const int row_bytes = p.K * (L::INT ? 1 : 2);
+    int st2 = make_map(&map_w, p.W, (uint64_t)p.pitch, (uint64_t)p.N, (uint64_t)p.pitch, 128);
+    if (!st2) st2 = make_map(&map_x, p.X, (uint64_t)row_bytes, (uint64_t)p.M, (uint64_t)row_bytes, L::NC);
+    if (st2) return st2;
     const DsqLaunchHooks h = dsq_launch_hooks();
     return dsq_launch(kernel, dim3((unsigned)(tiles * split), (unsigned)mt), dim3(L::THREADS), (size_t)L::BYTES, s,
-                      h.pdl, split, p, split, h.wait_ns);
+                      h.pdl, split, map_w, map_x, p, split, h.wait_ns);
 }
 
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
-    if (p.M <= 8) return launch<XT, 8, GP, 3, 3>(p, s, est_us);
-    if (p.M <= 16) return launch<XT, 16, GP, 3, 3>(p, s, est_us);
-    if (p.M <= 32) return launch<XT, 32, GP, 3, 3>(p, s, est_us);
-    return launch<XT, 64, GP, 3, 2>(p, s, est_us);
+    constexpr int MORE = XT == DSQ_I8 ? 1 : 0;                    // (of half the size)
+    if (p.M <= 8) return launch<XT, 8, GP, 3, 1, 8>(p, s, est_us);
+    if (p.M <= 16) return launch<XT, 16, GP, 3, 1, 8>(p, s, est_us);
+    if (p.M <= 32) return launch<XT, 32, GP, 3, 1, 4 + 4 * MORE>(p, s, est_us);
+    return launch<XT, 64, GP, 3, 2, 4>(p, s, est_us);
 }
 
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s, double *est_us)
