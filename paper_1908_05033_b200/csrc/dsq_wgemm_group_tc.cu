@@ -27,6 +27,8 @@
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
+#include <type_traits>
+
 #include "dsq_groups.h"
 #include "dsq_hooks.h"
 #include "dsq_ptx.cuh"
@@ -134,13 +136,15 @@ template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES> struct Layou
     static constexpr int NC = MC < 16 ? 16 : MC;                  // columns of an instruction
     static constexpr int FLUSHES = 4 / GP;                        // sums of a chunk
     static constexpr int AC = INT ? 32 : 64;                      // tensor-memory columns of a chunk's values
-    static constexpr int SLOTS = NC > 32 || (NC > 16 && FLUSHES < 4) ? 4 : 8;                 // places for sums
-    static constexpr int A_COL = SLOTS * NC, VALUES = STAGES >= 8 && A_COL + 8 * AC <= 512 ? 8 : 4;         // places for values
+    static constexpr int VALUES = 6, ROOM = (512 - VALUES * AC) / NC;         // places for values
+    static constexpr int SLOTS = ROOM >= 6 ? 6 : ROOM >= 4 ? 4 : 2, A_COL = SLOTS * NC;     // places for sums
     static constexpr int XBOX = NC * 128, XBOXES = INT ? 2 : 4;   // 128 bytes of K of the rows; of two chunks
     static constexpr int WBOX = 128 * 128, STAGE = WBOX + XBOXES * XBOX;
     static constexpr int RING_AT = 1024, S_AT = RING_AT + STAGES * STAGE, S_STAGE = FLUSHES * 512;
     static constexpr int BYTES = S_AT + TAKES * AHEAD * S_STAGE + 1024;      // (its start is aligned to 1024)
-    static constexpr int ISSUERS = 2 * FLUSHES <= SLOTS ? 2 : 1;  // chunks in turn; each has places of its own
+    // Threads that issue, chunks in turn.  (A thread that issues a chunk's first sum knows that the place's
+    // use before the last is over from its own chunk before, if there are places for a chunk and one more.)
+    static constexpr int ISSUERS = SLOTS > FLUSHES ? 2 : 1;
     static constexpr int WORKERS = (TEAMS + TAKES) * 128, THREADS = WORKERS + 96;
     // barriers: a stage is full and empty, values made and read, sums ready and place free, all is done
     static constexpr int FULL = 16, EMPTY = FULL + 8 * STAGES, MADE = EMPTY + 8 * STAGES, READ = MADE + 8 * VALUES;
@@ -149,7 +153,7 @@ template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES> struct Layou
     static_assert(BYTES <= 227 * 1024 && BYTES > 116 * 1024, "one block an SM");
     static_assert(MC * 512 <= STAGES * STAGE, "the totals take the ring's place");
     // (a team that has seen the values' last use but one read knows all earlier stages full: wait_full)
-    static_assert(TEAMS <= VALUES && VALUES <= 2 * STAGES && A_COL + VALUES * AC <= 512, "phases are waited for in order");
+    static_assert(TEAMS <= VALUES && VALUES <= 2 * STAGES && SLOTS >= 2 && A_COL + VALUES * AC <= 512, "phases are waited for in order");
 };
 
 template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES>
@@ -181,7 +185,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     if (threadIdx.x == 0) {
         for (int i = 0; i < STAGES; ++i) {
             mbar_init(smem + L::FULL + 8 * i, 1);
-            mbar_init(smem + L::EMPTY + 8 * i, L::ISSUERS);
+            mbar_init(smem + L::EMPTY + 8 * i, 2);           // (its two chunks)
         }
         for (int i = 0; i < L::VALUES; ++i) {
             mbar_init(smem + L::MADE + 8 * i, 4);
@@ -325,49 +329,61 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // no copy is under way when the block ends
         for (int i = max(0, issued - STAGES); i < issued; ++i)
             if (!wait_warp(smem + L::FULL + 8 * (i % STAGES), (i / STAGES) & 1, ok ? wait_ns : DRAIN_NS)) ok = false;
-    } else if (const int q = warp - L::WORKERS / 32 - 1; lane == 0 && q < L::ISSUERS) {
-        // One thread issues, or two that take chunks in turn: what it does lies in every chunk's way (commits and
-        // waits 0.2 us a chunk, instructions 0.03 us each), so places and phases are constants of an unrolled loop.
-        constexpr int IS = L::ISSUERS, COUNT = L::AC / 8 / FLUSHES;
-        constexpr int ROUND = 2 * L::SLOTS / FLUSHES, UNROLL = ROUND > 2 * L::VALUES ? ROUND : 2 * L::VALUES;
-        static_assert(UNROLL * FLUSHES % (2 * L::SLOTS) == 0 && UNROLL <= 2 * STAGES, "constants");
-        const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
-        auto wait1 = [&](uint32_t bar, uint32_t parity) { ok = wait_thread(smem + bar, parity, wait_ns); return ok; };
-        const uint64_t desc = smem_desc_sw128(smem + L::RING_AT + L::WBOX) + (uint32_t)(q * (L::XBOXES / 2) * (L::XBOX >> 4));
-        const uint32_t d0 = tmem + q * FLUSHES * L::NC, a0 = tmem + L::A_COL + q * L::AC, made = L::MADE + 8 * q,
-                       read = L::READ + 8 * q, ready = L::READY + 8 * FLUSHES * q, free = L::FREE + 8 * FLUSHES * q;
+    } else if (lane == 0) {
+        // Two threads issue, chunks in turn: what they do lies in every chunk's way (commits and waits 0.2 us a
+        // chunk, instructions 0.013 us each), so places and most phases are constants of an unrolled loop.
+        auto issue = [&](auto which) {
+            constexpr int Q = decltype(which)::value, IS = L::ISSUERS, COUNT = L::AC / 8 / FLUSHES;
+            constexpr int UNROLL = 12;
+            static_assert(UNROLL % L::VALUES == 0 && UNROLL * FLUSHES % L::SLOTS == 0 && UNROLL % IS == 0, "constants");
+            const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
+            auto wait1 = [&](uint32_t bar, uint32_t parity) { ok = wait_thread(smem + bar, parity, wait_ns); return ok; };
+            constexpr uint32_t X_HALF = (L::XBOXES / 2) * (L::XBOX >> 4);
+            const uint64_t x_first = smem_desc_sw128(smem + L::RING_AT + L::WBOX);
+            uint64_t x_at = x_first;
+            uint32_t full = L::FULL, s_phase = 0, odd = 0;        // odd: a round of the loop
 #pragma unroll 1
-        for (int base = q; base < chunks && ok; base += UNROLL) {
-            const int stage0 = (base >> 1) % STAGES;
-            const uint32_t s_phase = ((base >> 1) / STAGES) & 1;
-            const uint64_t x0 = desc + (uint32_t)(stage0 * (L::STAGE >> 4));
+            for (int base = 0; base + Q < chunks && ok; base += UNROLL, odd ^= 1) {
 #pragma unroll
-            for (int u = 0; u < UNROLL; u += IS) {
-                const int v = u % L::VALUES;
-                if (base + u >= chunks) break;
-                if ((u & 1) == 0 && !wait1(L::FULL + 8 * (stage0 + u / 2), s_phase)) break;
-                if (!wait1(made + 8 * v, (u / L::VALUES) & 1)) break;
+                for (int u = Q; u < UNROLL; u += IS) {
+                    const int v = u % L::VALUES;
+                    if (base + u >= chunks) break;
+                    if (!wait1(full, s_phase)) break;
+                    if (!wait1(L::MADE + 8 * v, (u / L::VALUES + odd * (UNROLL / L::VALUES)) & 1)) break;
 #pragma unroll
-                for (int f = 0; f < FLUSHES; ++f) {
-                    const int use = u * FLUSHES + f, slot = use % L::SLOTS;
-                    if ((base >= UNROLL || use >= L::SLOTS) && !wait1(free + 8 * slot, ((use / L::SLOTS) & 1) ^ 1)) break;
-                    tc_fence_after_sync();
+                    for (int f = 0; f < FLUSHES; ++f) {
+                        const int use = u * FLUSHES + f, slot = use % L::SLOTS;
+                        if ((base > 0 || use >= L::SLOTS) &&
+                            !wait1(L::FREE + 8 * slot, (use / L::SLOTS + odd * (UNROLL * FLUSHES / L::SLOTS) + 1) & 1))
+                            break;
+                        tc_fence_after_sync();
 #pragma unroll
-                    for (int i = 0; i < COUNT; ++i) {
-                        const int at = (f * COUNT + i) * 32 + (u & 1) * (L::XBOXES / 2) * 128;     // bytes into the pair's rows
-                        mma_ts<INT>(d0 + slot * L::NC, a0 + v * L::AC + (f * COUNT + i) * 8,
-                                    x0 + (uint32_t)((u / 2 * L::STAGE + (at >> 7) * L::XBOX + (at & 127)) >> 4), idesc, i > 0);
+                        for (int i = 0; i < COUNT; ++i) {
+                            const int at = (f * COUNT + i) * 32;              // bytes into the chunk's rows
+                            mma_ts<INT>(tmem + slot * L::NC, tmem + L::A_COL + v * L::AC + (f * COUNT + i) * 8,
+                                        x_at + ((u & 1) * X_HALF + (((at >> 7) * L::XBOX + (at & 127)) >> 4)), idesc, i > 0);
+                        }
+                        mma_commit(smem + L::READY + 8 * slot);
                     }
-                    mma_commit(smem + ready + 8 * slot);
+                    if (!ok) break;
+                    mma_commit(smem + L::READ + 8 * v);
+                    mma_commit(smem + full + (L::EMPTY - L::FULL));
+                    if (IS == 1 && !(u & 1)) continue;
+                    x_at += L::STAGE >> 4;
+                    full += 8;
+                    if (full == L::FULL + 8 * STAGES) {
+                        full = L::FULL;
+                        x_at = x_first;
+                        s_phase ^= 1;
+                    }
                 }
-                if (!ok) break;
-                mma_commit(smem + read + 8 * v);
-                if (IS == 2 || (u & 1)) mma_commit(smem + L::EMPTY + 8 * (stage0 + u / 2));
             }
-        }
-        // no instruction is under way when tensor memory is given up
-        mma_commit(smem + L::DONE + 8 * q);
-        if (!wait_thread(smem + L::DONE + 8 * q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
+            // no instruction is under way when tensor memory is given up
+            mma_commit(smem + L::DONE + 8 * Q);
+            if (!wait_thread(smem + L::DONE + 8 * Q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
+        };
+        if (warp == L::WORKERS / 32 + 1) issue(std::integral_constant<int, 0>());
+        else if (L::ISSUERS == 2) issue(std::integral_constant<int, 1>());
     }
     tc_fence_before_sync();
     __syncwarp();
