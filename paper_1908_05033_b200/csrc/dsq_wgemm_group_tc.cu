@@ -51,21 +51,55 @@ __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[8]) { tmem_ld
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[16]) { tmem_ld_32x16(at, r); }
 __device__ __forceinline__ void ld_cols(uint32_t at, uint32_t (&r)[32]) { tmem_ld_32x32(at, r); }
 
-// D (+)= A B^T with A in tensor memory, by one thread
-template <bool INT>
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate)
+// COUNT instructions (32 bytes of K each) with A in tensor memory, issued by one elected lane of a
+// converged warp; the first takes the accumulate flag.
+#define DSQ_TS_1(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, pe;\n\t.reg .b64 d0;\n\tsetp.ne.b32 p, %5, 0;\n\tmov.b64 d0, {%2, %3};\n\t" \
+                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+#define DSQ_TS_2(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1;\n\t.reg .b32 l1, a1;\n\t"                    \
+                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\tadd.u32 l1, %2, 2;\n\tadd.u32 a1, %1, 8;\n\t" \
+                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\telect.sync _|pe, 0xffffffff;\n\t"          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+#define DSQ_TS_4(KIND)                                                                                       \
+    asm volatile("{\n\t.reg .pred p, q, pe;\n\t.reg .b64 d0, d1, d2, d3;\n\t.reg .b32 l1, l2, l3, a1, a2, a3;\n\t" \
+                 "setp.ne.b32 p, %5, 0;\n\tsetp.eq.b32 q, %5, %5;\n\t"                                       \
+                 "add.u32 l1, %2, 2;\n\tadd.u32 l2, %2, 4;\n\tadd.u32 l3, %2, 6;\n\t"                         \
+                 "add.u32 a1, %1, 8;\n\tadd.u32 a2, %1, 16;\n\tadd.u32 a3, %1, 24;\n\t"                       \
+                 "mov.b64 d0, {%2, %3};\n\tmov.b64 d1, {l1, %3};\n\tmov.b64 d2, {l2, %3};\n\tmov.b64 d3, {l3, %3};\n\t" \
+                 "elect.sync _|pe, 0xffffffff;\n\t"                                                          \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [%1], d0, %4, p;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a1], d1, %4, q;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a2], d2, %4, q;\n\t"                     \
+                 "@pe tcgen05.mma.cta_group::1.kind::" KIND " [%0], [a3], d3, %4, q;\n\t}" ::"r"(d),          \
+                 "r"(a), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate)                                   \
+                 : "memory")
+template <bool INT, int COUNT>
+__device__ __forceinline__ void mma_ts_elect(uint32_t d, uint32_t a, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                             uint32_t accumulate)
 {
-    if (INT)
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::i8 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
-                     "r"(idesc), "r"(accumulate)
-                     : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-                     "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b),
-                     "r"(idesc), "r"(accumulate)
-                     : "memory");
+    static_assert(COUNT == 1 || COUNT == 2 || COUNT == 4, "instructions of a block");
+    if constexpr (COUNT == 1) {
+        if (INT) DSQ_TS_1("i8");
+        else DSQ_TS_1("f16");
+    } else if constexpr (COUNT == 2) {
+        if (INT) DSQ_TS_2("i8");
+        else DSQ_TS_2("f16");
+    } else {
+        if (INT) DSQ_TS_4("i8");
+        else DSQ_TS_4("f16");
+    }
 }
+#undef DSQ_TS_1
+#undef DSQ_TS_2
+#undef DSQ_TS_4
+
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const float *src)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
@@ -86,10 +120,6 @@ __device__ __noinline__ bool wait_slow(uint32_t bar, uint32_t parity, unsigned l
             if (t - t0 > limit_ns) return false;
         }
     }
-}
-__device__ __forceinline__ bool wait_thread(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
-{
-    return mbar_try_wait(bar, parity, 20u) || wait_slow(bar, parity, limit_ns);
 }
 __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, unsigned long long limit_ns)
 {
@@ -129,15 +159,17 @@ template <int XT> __device__ __forceinline__ float byte_unit(int odd)
     return XT == DSQ_I8 ? (odd ? 0.125f : 0.0625f) : XT == DSQ_BF16 ? (odd ? 128.f : 64.f) : (odd ? 1024.f : 512.f);
 }
 
-constexpr int AHEAD = 8;          // chunks whose scales are on their way
-// MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum; TEAMS, TAKES: of four warps
-template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES> struct Layout {
+// MC: columns of D that are read (rows of X); GP: pieces of 32 codes of a sum; TEAMS: of four warps that
+// make values; COLS, TURNS: teams that take the sums, by columns and by chunks in turn
+template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES> struct Layout {
     static constexpr bool INT = XT == DSQ_I8;
     static constexpr int NC = MC < 16 ? 16 : MC;                  // columns of an instruction
     static constexpr int FLUSHES = 4 / GP;                        // sums of a chunk
     static constexpr int AC = INT ? 32 : 64;                      // tensor-memory columns of a chunk's values
     static constexpr int VALUES = 6, ROOM = (512 - VALUES * AC) / NC;         // places for values
-    static constexpr int SLOTS = ROOM >= 6 ? 6 : ROOM >= 4 ? 4 : 2, A_COL = SLOTS * NC;     // places for sums
+    static constexpr int SLOTS = FLUSHES == 1 ? (ROOM >= 6 ? 6 : ROOM >= 4 ? 4 : 2) : ROOM >= 8 ? 8 : ROOM >= 4 ? 4 : 2;
+    static constexpr int A_COL = SLOTS * NC;                      // (places for sums)
+    static constexpr int TAKES = COLS * TURNS, AHEAD = 8 / TURNS; // a team's chunks whose scales are on their way
     static constexpr int XBOX = NC * 128, XBOXES = INT ? 2 : 4;   // 128 bytes of K of the rows; of two chunks
     static constexpr int WBOX = 128 * 128, STAGE = WBOX + XBOXES * XBOX;
     static constexpr int RING_AT = 1024, S_AT = RING_AT + STAGES * STAGE, S_STAGE = FLUSHES * 512;
@@ -151,19 +183,20 @@ template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES> struct Layou
     static constexpr int READY = READ + 8 * VALUES, FREE = READY + 8 * SLOTS, DONE = FREE + 8 * SLOTS;
     static_assert(DONE + 16 <= RING_AT, "barriers");
     static_assert(BYTES <= 227 * 1024 && BYTES > 116 * 1024, "one block an SM");
-    static_assert(MC * 512 <= STAGES * STAGE, "the totals take the ring's place");
+    static_assert(TURNS * MC * 512 <= STAGES * STAGE, "the totals take the ring's place");
+    static_assert(TURNS == 1 || SLOTS % (2 * FLUSHES) == 0, "a place's sums are one team's and one issuer's");
     // (a team that has seen the values' last use but one read knows all earlier stages full: wait_full)
     static_assert(TEAMS <= VALUES && VALUES <= 2 * STAGES && SLOTS >= 2 && A_COL + VALUES * AC <= 512, "phases are waited for in order");
 };
 
-template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES>
-__global__ void __launch_bounds__((TEAMS + TAKES) * 128 + 96, 1)
+template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES>
+__global__ void __launch_bounds__((TEAMS + COLS * TURNS) * 128 + 96, 1)
 wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
                       const DsqGroupGemm p, const int split, const unsigned long long wait_ns)
 {
-    using L = Layout<XT, MC, GP, TEAMS, TAKES, STAGES>;
+    using L = Layout<XT, MC, GP, TEAMS, COLS, TURNS, STAGES>;
     constexpr bool INT = L::INT;
-    constexpr int FLUSHES = L::FLUSHES, MCT = MC / TAKES;
+    constexpr int FLUSHES = L::FLUSHES, TAKES = L::TAKES, AHEAD = L::AHEAD, MCT = MC / COLS;
     extern __shared__ uint8_t raw_smem[];
     const uint32_t smem = (smem_u32(raw_smem) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -178,6 +211,10 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     const int chunks = min(2 * (int)((int64_t)every * (rank + 1) / split), all) - c0, pairs = (chunks + 1) >> 1;
     const int last = (int)min((int64_t)127, p.N - 1 - n0);       // row of weights of this block
 
+    if (warp == L::WORKERS / 32 && lane == 0) {
+        tma_prefetch_desc(&map_w);
+        tma_prefetch_desc(&map_x);
+    }
     if (warp == 0) {
         tmem_alloc(smem, 512);
         tmem_relinquish();
@@ -193,7 +230,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         }
         for (int i = 0; i < L::SLOTS; ++i) {
             mbar_init(smem + L::READY + 8 * i, 1);
-            mbar_init(smem + L::FREE + 8 * i, 4 * TAKES);
+            mbar_init(smem + L::FREE + 8 * i, 4 * COLS);
         }
         for (int i = 0; i < 2; ++i) mbar_init(smem + L::DONE + 8 * i, 1);
         mbar_init_fence();
@@ -261,23 +298,25 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     } else if (team < TEAMS + TAKES) {
         // A row's scales go through a ring of their own, each thread's copies for itself.  (A chunk ahead, in
         // registers, the wait for them was the kernel's time: 32 times 0.6 us.)
+        const int turn = (team - TEAMS) / COLS;
         const uint32_t s_ring = smem + L::S_AT + (team - TEAMS) * (AHEAD * L::S_STAGE) + row * 4;
-        const uint32_t from = lanes + (team - TEAMS) * MCT;
+        const uint32_t from = lanes + (team - TEAMS) % COLS * MCT;
         const float *scales = p.scales + n0 + min(row, last);
-        auto issue_s = [&](int c) {
+        auto issue_s = [&](int i) {
+            const int c = TURNS * i + turn;
             if (c < chunks) {
 #pragma unroll
                 for (int f = 0; f < FLUSHES; ++f) {
                     const int g = min(p.group_of((uint32_t)((c0 + c) * FLUSHES + f)), p.groups - 1);
-                    cp_async_4(s_ring + (c % AHEAD) * L::S_STAGE + f * 512, scales + (int64_t)g * p.N);
+                    cp_async_4(s_ring + (i % AHEAD) * L::S_STAGE + f * 512, scales + (int64_t)g * p.N);
                 }
             }
             cp_async_commit();
         };
 #pragma unroll 1
-        for (int c = 0; c < AHEAD - 1; ++c) issue_s(c);
+        for (int i = 0; i < AHEAD - 1; ++i) issue_s(i);
 #pragma unroll 1
-        for (int i = 0; i < chunks && ok; ++i) {
+        for (int i = 0; TURNS * i + turn < chunks && ok; ++i) {
             cp_async_wait<AHEAD - 2>();
             float now[FLUSHES];
 #pragma unroll
@@ -286,7 +325,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             issue_s(i + AHEAD - 1);
 #pragma unroll
             for (int f = 0; f < FLUSHES; ++f) {
-                const uint32_t use = i * FLUSHES + f, slot = use % L::SLOTS;
+                const uint32_t use = (TURNS * i + turn) * FLUSHES + f, slot = use % L::SLOTS;
                 wait(L::READY + 8 * slot, (use / L::SLOTS) & 1);
                 if (!ok) break;
                 tc_fence_after_sync();
@@ -329,18 +368,18 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         // no copy is under way when the block ends
         for (int i = max(0, issued - STAGES); i < issued; ++i)
             if (!wait_warp(smem + L::FULL + 8 * (i % STAGES), (i / STAGES) & 1, ok ? wait_ns : DRAIN_NS)) ok = false;
-    } else if (lane == 0) {
-        // Two threads issue, chunks in turn: what they do lies in every chunk's way (commits and waits 0.2 us a
+    } else {
+        // Two warps issue, chunks in turn: what they do lies in every chunk's way (commits and waits 0.2 us a
         // chunk, instructions 0.013 us each), so places and most phases are constants of an unrolled loop.
         auto issue = [&](auto which) {
             constexpr int Q = decltype(which)::value, IS = L::ISSUERS, COUNT = L::AC / 8 / FLUSHES;
             constexpr int UNROLL = 12;
             static_assert(UNROLL % L::VALUES == 0 && UNROLL * FLUSHES % L::SLOTS == 0 && UNROLL % IS == 0, "constants");
             const uint32_t idesc = INT ? idesc_i8(L::NC, true, true) : (XT == DSQ_BF16 ? idesc_bf16(L::NC) : dsq_idesc_f16(L::NC));
-            auto wait1 = [&](uint32_t bar, uint32_t parity) { ok = wait_thread(smem + bar, parity, wait_ns); return ok; };
             constexpr uint32_t X_HALF = (L::XBOXES / 2) * (L::XBOX >> 4);
-            const uint64_t x_first = smem_desc_sw128(smem + L::RING_AT + L::WBOX);
-            uint64_t x_at = x_first;
+            const uint64_t desc = smem_desc_sw128(smem + L::RING_AT + L::WBOX);
+            const uint32_t hi = (uint32_t)(desc >> 32), x_first = (uint32_t)desc;
+            uint32_t x_at = x_first;
             uint32_t full = L::FULL, s_phase = 0, odd = 0;        // odd: a round of the loop
 #pragma unroll 1
             for (int base = 0; base + Q < chunks && ok; base += UNROLL, odd ^= 1) {
@@ -348,26 +387,28 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 for (int u = Q; u < UNROLL; u += IS) {
                     const int v = u % L::VALUES;
                     if (base + u >= chunks) break;
-                    if (!wait1(full, s_phase)) break;
-                    if (!wait1(L::MADE + 8 * v, (u / L::VALUES + odd * (UNROLL / L::VALUES)) & 1)) break;
+                    if (!wait(full, s_phase)) break;
+                    if (!wait(L::MADE + 8 * v, (u / L::VALUES + odd * (UNROLL / L::VALUES)) & 1)) break;
 #pragma unroll
                     for (int f = 0; f < FLUSHES; ++f) {
                         const int use = u * FLUSHES + f, slot = use % L::SLOTS;
                         if ((base > 0 || use >= L::SLOTS) &&
-                            !wait1(L::FREE + 8 * slot, (use / L::SLOTS + odd * (UNROLL * FLUSHES / L::SLOTS) + 1) & 1))
+                            !wait(L::FREE + 8 * slot, (use / L::SLOTS + odd * (UNROLL * FLUSHES / L::SLOTS) + 1) & 1))
                             break;
                         tc_fence_after_sync();
+                        constexpr int BLOCK = COUNT < 4 ? COUNT : 4;
 #pragma unroll
-                        for (int i = 0; i < COUNT; ++i) {
+                        for (int i = 0; i < COUNT; i += BLOCK) {
                             const int at = (f * COUNT + i) * 32;              // bytes into the chunk's rows
-                            mma_ts<INT>(tmem + slot * L::NC, tmem + L::A_COL + v * L::AC + (f * COUNT + i) * 8,
-                                        x_at + ((u & 1) * X_HALF + (((at >> 7) * L::XBOX + (at & 127)) >> 4)), idesc, i > 0);
+                            mma_ts_elect<INT, BLOCK>(tmem + slot * L::NC, tmem + L::A_COL + v * L::AC + (f * COUNT + i) * 8,
+                                                     x_at + ((u & 1) * X_HALF + (((at >> 7) * L::XBOX + (at & 127)) >> 4)), hi,
+                                                     idesc, i);
                         }
-                        mma_commit(smem + L::READY + 8 * slot);
+                        mma_commit_elect(smem + L::READY + 8 * slot);
                     }
                     if (!ok) break;
-                    mma_commit(smem + L::READ + 8 * v);
-                    mma_commit(smem + full + (L::EMPTY - L::FULL));
+                    mma_commit_elect(smem + L::READ + 8 * v);
+                    mma_commit_elect(smem + full + (L::EMPTY - L::FULL));
                     if (IS == 1 && !(u & 1)) continue;
                     x_at += L::STAGE >> 4;
                     full += 8;
@@ -379,47 +420,42 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
                 }
             }
             // no instruction is under way when tensor memory is given up
-            mma_commit(smem + L::DONE + 8 * Q);
-            if (!wait_thread(smem + L::DONE + 8 * Q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
+            mma_commit_elect(smem + L::DONE + 8 * Q);
+            if (!wait_warp(smem + L::DONE + 8 * Q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
         };
         if (warp == L::WORKERS / 32 + 1) issue(std::integral_constant<int, 0>());
         else if (L::ISSUERS == 2) issue(std::integral_constant<int, 1>());
     }
     tc_fence_before_sync();
-    __syncwarp();
     const int failed = __syncthreads_or(!ok);
     if (warp == 0) {
         tc_fence_after_sync();
         tmem_dealloc(lds_32(smem), 512);
     }
-    const bool takes = team >= TEAMS && team < TEAMS + TAKES;
-    if (split == 1) {
-        if (takes && row <= last) {
-            const float unit = failed ? __uint_as_float(0x7FC00000u) : byte_unit<XT>(p.odd);
-#pragma unroll
-            for (int i = 0; i < MCT; ++i) {
-                const int m = (team - TEAMS) * MCT + i;
-                if (m < rows) p.store(m0 + m, n0 + row, total[i] * unit);
-            }
-        }
-        return;
-    }
-    // the totals of the cluster's blocks, [row of X][row of weights], added in their order
+    // the totals of the teams and of the cluster's blocks, [row of X][row of weights], added in their order
     const uint32_t sums = smem + L::RING_AT;
-    if (takes) {
+    const float unit = byte_unit<XT>(p.odd), lost = __uint_as_float(0x7FC00000u);
+    if (team >= TEAMS && team < TEAMS + TAKES) {
+        const int at = (team - TEAMS) / COLS * MC + (team - TEAMS) % COLS * MCT;
 #pragma unroll
-        for (int i = 0; i < MCT; ++i)
-            sts_32(sums + (((team - TEAMS) * MCT + i) * 128 + row) * 4, failed ? 0x7FC00000u : __float_as_uint(total[i]));
+        for (int i = 0; i < MCT; ++i) sts_32(sums + ((at + i) * 128 + row) * 4, __float_as_uint(failed ? lost : total[i]));
     }
-    cluster_sync_all();
-    const float unit = byte_unit<XT>(p.odd);
+    if (split > 1) cluster_sync_all();
+    else __syncthreads();
     if (team < TEAMS + TAKES)
         for (int m = rank + team * split; m < rows; m += (TEAMS + TAKES) * split) {
             float s = 0.f;
-            for (int r = 0; r < split; ++r) s += __uint_as_float(ld_cluster_32(map_to_cta(sums + (m * 128 + row) * 4, r)));
+            for (int r = 0; r < split; ++r) {
+                const uint32_t there = split > 1 ? map_to_cta(sums, r) : sums;
+#pragma unroll
+                for (int t = 0; t < TURNS; ++t) {
+                    const uint32_t at = there + ((t * MC + m) * 128 + row) * 4;
+                    s += __uint_as_float(split > 1 ? ld_cluster_32(at) : lds_32(at));
+                }
+            }
             if (row <= last) p.store(m0 + m, n0 + row, s * unit);
         }
-    cluster_sync_all();           // nobody leaves while its sums are read
+    if (split > 1) cluster_sync_all();    // nobody leaves while its sums are read
 }
 
 // rows of bytes, in boxes of 128 of them by box_rows, in the 128-byte swizzle; zeros behind the ends
@@ -460,13 +496,13 @@ template <class K> int active_clusters(K kernel, int split, int threads, int byt
 }
 
 // est_us: the launch's estimated time is written there and nothing is launched
-template <int XT, int MC, int GP, int TEAMS, int TAKES, int STAGES>
+template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES>
 int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
-    using L = Layout<XT, MC, GP, TEAMS, TAKES, STAGES>;
+    using L = Layout<XT, MC, GP, TEAMS, COLS, TURNS, STAGES>;
     static std::atomic<unsigned long long> configured{0};
     static std::atomic<int> active[4];
-    const auto kernel = wgemm_group_tc_kernel<XT, MC, GP, TEAMS, TAKES, STAGES>;
+    const auto kernel = wgemm_group_tc_kernel<XT, MC, GP, TEAMS, COLS, TURNS, STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, L::BYTES, &configured);
     if (st) return st;
     const int64_t tiles = (p.N + 127) / 128, mt = (p.M + MC - 1) / MC;
@@ -505,10 +541,11 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
     constexpr int MORE = XT == DSQ_I8 ? 1 : 0;                    // (of half the size)
-    if (p.M <= 8) return launch<XT, 8, GP, 3, 1, 8>(p, s, est_us);
-    if (p.M <= 16) return launch<XT, 16, GP, 3, 1, 8>(p, s, est_us);
-    if (p.M <= 32) return launch<XT, 32, GP, 3, 1, 4 + 4 * MORE>(p, s, est_us);
-    return launch<XT, 64, GP, 3, 2, 4>(p, s, est_us);
+    constexpr int TURNS = GP == 1 && XT != DSQ_I8 ? 1 : 2;
+    if (p.M <= 8) return launch<XT, 8, GP, 3, 1, 2, 8>(p, s, est_us);
+    if (p.M <= 16) return launch<XT, 16, GP, 3, 1, 2, 8>(p, s, est_us);
+    if (p.M <= 32) return launch<XT, 32, GP, 3, 1, TURNS, 4 + 4 * MORE>(p, s, est_us);
+    return launch<XT, 64, GP, 3, 2, 1, 4>(p, s, est_us);
 }
 
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s, double *est_us)
