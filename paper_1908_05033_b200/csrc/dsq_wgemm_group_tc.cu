@@ -442,19 +442,37 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     }
     if (split > 1) cluster_sync_all();
     else __syncthreads();
-    if (team < TEAMS + TAKES)
-        for (int m = rank + team * split; m < rows; m += (TEAMS + TAKES) * split) {
-            float s = 0.f;
-            for (int r = 0; r < split; ++r) {
-                const uint32_t there = split > 1 ? map_to_cta(sums, r) : sums;
+    if (team < TEAMS + TAKES) {
+        // (eight loads on their way together: rows', or blocks' where there are few rows)
+        constexpr int ROWS = MC <= 16 ? 1 : 4, BLOCKS = MC <= 16 ? 8 : 2;
+        const int step = (TEAMS + TAKES) * split;
+        for (int m = rank + team * split; m < rows; m += ROWS * step) {
+            float s[ROWS] = {};
+            for (int r0 = 0; r0 < split; r0 += BLOCKS) {
+                uint32_t v[BLOCKS][TURNS][ROWS];
 #pragma unroll
-                for (int t = 0; t < TURNS; ++t) {
-                    const uint32_t at = there + ((t * MC + m) * 128 + row) * 4;
-                    s += __uint_as_float(split > 1 ? ld_cluster_32(at) : lds_32(at));
+                for (int r = 0; r < BLOCKS; ++r) {
+                    const uint32_t there = (split > 1 ? map_to_cta(sums, min(r0 + r, split - 1)) : sums) + row * 4;
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j)
+#pragma unroll
+                        for (int t = 0; t < TURNS; ++t) {
+                            const uint32_t at = there + (t * MC + m + j * step) * 512;
+                            v[r][t][j] = m + j * step >= rows || r0 + r >= split ? 0u : split > 1 ? ld_cluster_32(at) : lds_32(at);
+                        }
                 }
+#pragma unroll
+                for (int r = 0; r < BLOCKS; ++r)
+#pragma unroll
+                    for (int j = 0; j < ROWS; ++j)
+#pragma unroll
+                        for (int t = 0; t < TURNS; ++t) s[j] += __uint_as_float(v[r][t][j]);
             }
-            if (row <= last) p.store(m0 + m, n0 + row, s * unit);
+#pragma unroll
+            for (int j = 0; j < ROWS; ++j)
+                if (m + j * step < rows && row <= last) p.store(m0 + m + j * step, n0 + row, s[j] * unit);
         }
+    }
     if (split > 1) cluster_sync_all();    // nobody leaves while its sums are read
 }
 
