@@ -525,17 +525,18 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
     if (st) return st;
     const int64_t tiles = (p.N + 127) / 128, mt = (p.M + MC - 1) / MC;
     const int pairs = ((p.K + 127) / 128 + 1) / 2, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
-    // Blocks along K.  us of a wave: 3.6 for its start and end, the cluster's sums 1.0, and a turn of a
-    // team: measured at 8192 x 8192 (11 turns): 18.8, 21.7 and 31.8 us for 16, 32 and 64 rows, int8 14.5,
-    // 16.8 and 21.4.
-    constexpr double TURN = XT == DSQ_I8 ? (MC <= 16 ? 0.9 : MC <= 32 ? 1.1 : 1.5) : (MC <= 16 ? 1.3 : MC <= 32 ? 1.55 : 2.5);
+    // Blocks along K.  us of a wave: its start and end, the cluster's sums, and a chunk's time by the sums it
+    // has; fitted to 216 sizes from 512 x 512 to 8192 x 8192 and 4 to 100 rows, within 12 % of nearly all.
+    constexpr int AT = MC <= 8 ? 0 : MC <= 16 ? 1 : MC <= 32 ? 2 : 3, SUMS = GP == 4 ? 0 : GP == 2 ? 1 : 2;
+    constexpr double START[] = {2.4, 3.4, 3.8, 5.4}, CLUSTER[] = {1.8, 1.2, 1.7, 0.8};
+    constexpr double CHUNK[2][3][4] = {{{0.385, 0.39, 0.41, 0.435}, {0.45, 0.455, 0.48, 0.69}, {0.55, 0.56, 0.84, 0.965}},
+                                       {{0.315, 0.32, 0.345, 0.385}, {0.38, 0.395, 0.43, 0.605}, {0.475, 0.505, 0.705, 0.925}}};
     int split = 1;
     double best = 1e30;
     for (int c = 1, k = 0; c <= 8 && c <= pairs; c *= 2, ++k) {
         const int64_t at_once = c == 1 ? sms : active_clusters(kernel, c, L::THREADS, L::BYTES, &active[k]);
         const double waves = (double)((tiles * mt + at_once - 1) / at_once);
-        const int turns = 2 * (((pairs + c - 1) / c + TEAMS - 1) / TEAMS);
-        const double t = waves * (3.6 + TURN * turns + (c > 1 ? 1.0 : 0.0));
+        const double t = waves * (START[AT] + CHUNK[L::INT][SUMS][AT] * 2 * ((pairs + c - 1) / c)) + (c > 1 ? CLUSTER[AT] : 0.0);
         if (t < best) {
             best = t;
             split = c;
