@@ -10,8 +10,9 @@
 // them on is chance.  c = floor(v), v = 7.5 w / a:
 //   * 16-bit weights: a v that is no whole number is 2^-15 away from one at least, where it
 //     is above 1 (15 w and 2 a are integers of 15 and 12 bits on one grid, at most three
-//     powers of two apart), and v in binary32 is off by 2^-21 of itself: v (1 +- 2^-19),
-//     upwards, lies on the right side, and its floor is the code;
+//     powers of two apart), and 7.5 / a in binary32 is off by 2^-21 of itself: v (1 +- 2^-19),
+//     upwards, lies on the right side, and its floor is the code.  Both signs' v are made and rounded
+//     down to a whole number in one fused operation each, and the larger one is the upper one;
 //   * binary32 weights: with j = rint(v) as far as binary32 gives it, the code is j or j - 1
 //     by the sign of 7.5 w - a j, in which the rounding error of a j is taken off.
 //
@@ -41,7 +42,7 @@ struct QuantParams {
 
 // What a group's codes are made with.  Tiny groups are scaled up (exactly), and the comparison
 // with a border is a sixteenth of it, so that nothing over- or underflows.
-struct Range { float f, a, inv, scale; bool bad; };
+struct Range { float f, a, inv, up, down, scale; bool bad; };      // up, down: inv (1 +- 2^-19)
 __device__ __forceinline__ Range range_of(uint32_t top)
 {
     Range r;
@@ -53,6 +54,8 @@ __device__ __forceinline__ Range range_of(uint32_t top)
     // (off by its last bits: what is made of it allows for that; finite for a = 0)
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r.inv) : "f"(fmaxf(r.a, 1e-37f)));
     r.inv *= 0.46875f;
+    r.up = r.inv * (1.f + 1.9073486e-6f);
+    r.down = r.inv * (1.f - 1.9073486e-6f);
     // a / 15, rounded once: a quotient, corrected by what is left of a (a division in every
     // thread took 9 us of 67 at 16384 x 4096 in groups of 128)
     constexpr float R15 = 1.f / 15.f;
@@ -69,11 +72,11 @@ template <bool WIDE> __device__ __forceinline__ uint32_t code_bits(float x, cons
         const float t = __fmaf_rn(x, r.inv, MAGIC);
         const float nj = __fsub_rn(MAGIC, t);                 // -j (never -0)
         const float p = __fmul_rn(r.a, nj);
-        const float d = __fadd_rn(__fmaf_rn(0.46875f, x, p), __fmaf_rn(r.a, nj, -p));   // (7.5 x - a j) / 16
+        // (7.5 x - a j) / 16, rounded down: that of the smallest negative x stays below 0
+        const float d = __fadd_rn(__fmaf_rd(0.46875f, x, p), __fmaf_rn(r.a, nj, -p));
         return __float_as_uint(t) + (uint32_t)((int)__float_as_uint(d) >> 31);
     } else {
-        const float v = __fmul_rn(x, r.inv);
-        return __float_as_uint(__fadd_rd(__fadd_rn(v, __fmul_rn(fabsf(v), 1.9073486e-6f)), MAGIC));
+        return __float_as_uint(fmaxf(__fmaf_rd(x, r.up, MAGIC), __fmaf_rd(x, r.down, MAGIC)));
     }
 }
 
@@ -292,17 +295,20 @@ int block_shape(int64_t N, int64_t across, int rows, int *bx_log, dim3 *grid)
 
 template <class T, bool VEC> int quantize(QuantParams p, cudaStream_t s)
 {
-    p.lanes_log = 2;
-    while (p.lanes_log < 5 && (1 << p.lanes_log) < p.group_words) ++p.lanes_log;
+    // Words of a thread: with more of them a group's magnitude and reciprocal are fewer threads' work, with
+    // fewer lanes a warp's accesses are shorter pieces.  16384 x 4096 in bf16, us, one, two and four words: groups
+    // of 128 43.0, 36.7, 34.0; of 64 42.6, 36.8, 38.7; of 32 42.6, 38.0, 43.7.  4096 x 4096 in binary32, of 64:
+    // 16.8, 14.9, 16.6.
+    const int most = sizeof(T) == 2 && p.group_words >= 16 ? 4 : 2;
+    p.lanes_log = 0;
+    while (p.lanes_log < 5 && (most << p.lanes_log) < p.group_words) ++p.lanes_log;
     const int words = (p.group_words + (1 << p.lanes_log) - 1) >> p.lanes_log;      // of a thread
-    const int rows = words == 1 ? 4 : words == 2 ? 2 : 1;
     dim3 grid;
-    const int st = block_shape(p.N, (int64_t)p.groups << p.lanes_log, rows, &p.bx_log, &grid);
+    const int st = block_shape(p.N, (int64_t)p.groups << p.lanes_log, words <= 4 ? 2 : 1, &p.bx_log, &grid);
     if (st) return st;
     // (what these kernels write are a layer's constants: what follows starts behind them)
-    const auto kernel = words == 1   ? quantize_kernel<T, VEC, 1, 4>
-                        : words == 2 ? quantize_kernel<T, VEC, 2, 2>
-                        : words <= 4 ? quantize_kernel<T, VEC, 4, 1>
+    const auto kernel = words <= 2   ? quantize_kernel<T, VEC, 2, 2>
+                        : words <= 4 ? quantize_kernel<T, VEC, 4, 2>
                                      : quantize_kernel<T, VEC, 0, 1>;
     return dsq_launch(kernel, grid, dim3(256), 0, s, dsq_launch_hooks().pdl, 0, p);
 }

@@ -88,3 +88,24 @@ def test_more_than_2_to_the_31_weights(dsq):
     v = dsq.dsq_dequantize_groups(codes, scales, n, k, 4, 128)
     assert torch.equal(v[-3:], dsq.dsq_dequantize_groups(c, s, 3, k, 4, 128))
     assert not v[:-3].any()
+
+
+@pytest.mark.parametrize("t", TYPES)
+def test_weights_far_below_the_largest(dsq, t):
+    """Below zero, by however little beside the group's largest, is code -1; zero and above is 0."""
+    f = torch.finfo(t)
+    least = f.smallest_normal * f.eps
+    small = torch.tensor([-least, least, -f.smallest_normal, f.smallest_normal, -0.0, 0.0, -3 * least, 5 * least],
+                         dtype=torch.float64)
+    for top in (f.max, 1.0, 2.0 ** -13):
+        w = torch.zeros(2, 64, dtype=torch.float64)
+        w[:, 8:16] = small
+        w[:, 40:48] = small
+        w[:, 0] = torch.tensor([top, -top], dtype=torch.float64)
+        w[:, 63] = -top
+        w = w.to(t)
+        C, S = G.quantize(w.double().numpy(), 32)
+        codes, scales = dsq.dsq_quantize_groups(w.cuda(), 4, 32)
+        assert np.array_equal(unpacked(dsq, codes, 2, 64), C)
+        if top >= 1.0:        # (fp16's smallest normal number is half of 2^-13)
+            assert (C[:, 8:16] == [-1, 0, -1, 0, 0, 0, -1, 0]).all()
