@@ -347,10 +347,15 @@ int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N,
  *   W_codes, scales, bits, group  as dsq_quantize_groups leaves them
  *   bias      fp32 [N] or NULL
  *   Y         [M][N] of y_type: DSQ_F32, DSQ_BF16 or DSQ_F16
- * Any M (up to 64 rows a pass over the weights).  Products are exact; a group's are added by
- * the tensor core in binary32 (int32 for DSQ_I8: exact, for groups of up to 2^16 weights,
- * DSQ_ERR_OVERFLOW beyond), groups in binary32 in a fixed order: the same call gives the same
- * bits.  Y is rounded once.  No workspace. */
+ * Any M up to 64 * 65535 (DSQ_ERR_SIZE beyond; up to 64 rows a pass over the weights).  With
+ * three rows or more products are exact, and a group's are added by the tensor core in binary32.
+ * One or two rows of 16 bits are made integers first: an element is exact down to 2^-14 (DSQ_BF16)
+ * or 2^-11 (DSQ_F16) of the largest of its 256 neighbours (k / 256), and below that off by at
+ * most 2^-22 of that largest; a group's sums are then exact.  With DSQ_I8 a group's sums are exact
+ * in int32 (groups of up to 2^16 weights, DSQ_ERR_OVERFLOW beyond).  Groups are added in binary32 in
+ * a fixed order: the same call gives the same bits on the same GPU.  Y is rounded once.  A row with an
+ * infinity or a NaN gives what such terms give, or NaN; other rows do not see it.  Device-side waits
+ * are bounded: outputs that one is given up for are NaN (there is no workspace to hold a status). */
 int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,
                     const void *W_codes, const float *scales, const float *bias,
                     int64_t M, int64_t N, int64_t K, int bits, int64_t group,

@@ -2,28 +2,35 @@
 // tensor cores (dsq_wgemm_group.cu states the product and holds the kernel of small problems).
 //
 // The weights are the rows of an instruction, X its columns: D[128 weights' rows][rows of X]
-// = A B^T with A the values 2 c + 1 (or c) of 128 rows of codes, made in registers and put
-// into tensor memory, and B a few rows of X in shared memory.  A row of codes belongs to one
-// thread, which makes its values, reads its sums of a group back and adds them, times the
-// group's scale, to its totals in binary32 (one scale a thread and group).  An instruction of
-// 128 x 16 x 16 does for 16 rows what 16 x 8 mma.sync tiles do with 16 times the operands'
-// traffic through registers: at 8192 x 8192 with bf16 rows mma.sync took 23 us for one row and
-// 64 us for 64, issue-bound.
+// = A B^T with A the values of 128 rows of codes, made in registers and put into tensor memory,
+// and B a few rows of X in shared memory.  A row of codes belongs to one thread of those that make
+// values and to one of those that read its sums of a group back and add them, times the group's
+// scale, to its totals in binary32.  An instruction of 128 x 16 x 16 does for 16 rows what 16 x 8
+// mma.sync tiles do with 16 times the operands' traffic through registers: at 8192 x 8192 with bf16
+// rows mma.sync takes 16.5 us for 8 rows, 21 for 16, 31 for 32 and 64 for 64.
 //
-//   * TEAMS of four warps take the block's chunks of 128 codes of 128 rows in turn, two at a time: codes
-//     from the team's ring in shared memory (cp.async, each warp its own 32 rows, whole lines of 128
-//     bytes: with 64 of a line at a time memory gave 1.6 TB/s), X of a chunk from global memory
-//     through registers, permuted to the order in which codes come out of their words, into the
-//     128-byte swizzle.  One warp of the team issues the instructions.
-//   * Four more warps take the sums: a chunk's (a group's, where groups end sooner) lie in one of the
-//     team's places in tensor memory; they read them, give the place back and add.  Making values and
-//     adding sums are both bound by issue slots and by latencies, and with the totals out of the
-//     teams' registers 16 warps fit (two teams that did both took 34 us for 64 rows at 8192 x 8192).
+//   * One warp copies: a stage of the ring is two chunks of 128 codes of 128 rows (whole lines of 128
+//     bytes) and X's elements for them, both by TMA into the 128-byte swizzle; zeros behind the ends.
+//   * TEAMS of four warps make values, chunks in turn: 64 columns of tensor memory a chunk for 16-bit
+//     rows, 32 for 8-bit ones.  Three operations for two 16-bit values, in the order of X.  (With pairs as
+//     they come out of a word, codes i and i + 4, X had to be permuted on its way, in the same warps:
+//     that cost 64 rows 31.8 us where they now take 20.1.)
+//   * Two warps issue the instructions, chunks in turn, with an elected lane.  (One thread in a branch of its
+//     own took 75 cycles an instruction and 200 a commit, an elected lane of a whole warp 30 and 40: 8 rows
+//     17.4 against 15.4 us.  One issuing warp instead of two: 22.)
+//   * One, two or four teams more take the sums: a chunk's (a group's, where groups end sooner) lie in
+//     one of the places in tensor memory; they read them, give the place back and add.
 //   * Blocks of a cluster share K and add their totals through distributed shared memory, in order.
 //   * Exactly one block is on an SM (its shared memory sees to that): blocks of a cluster
 //     wait for one another, and must not wait for tensor memory meanwhile.
 //
-// Every wait for the tensor core is bounded; where one runs out the outputs are NaN.
+// Bound at 8192 x 8192, 16 rows of bf16 (16.4 us; codes alone 5.3 us at the copy's rate): 3.8 us of
+// launch, set-up and the cluster's sums, 7 for the copies and the roles' signals to one another with no
+// work between them, the rest unpacking and instructions, of which no pipe is full (issue slots 47 %,
+// ALU 44 %, tensor 6 %).  8-bit rows 12.8 us; 64 rows 20.1 and 18.4; groups of 32 instead of 128, 16 rows:
+// 21.7 us, four sums a chunk.
+//
+// Every wait is bounded; where one runs out the outputs of the cluster are NaN.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -105,7 +112,7 @@ __device__ __forceinline__ void cp_async_4(uint32_t dst, const float *src)
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// once a wait has run out, instructions in flight get this long before their memory is given up
+// copies and instructions in flight get this long at least before their memory is given up
 constexpr unsigned long long DRAIN_NS = 20000000ull;
 
 // Bounded wait of all lanes of a warp; false where it ran out.
@@ -192,7 +199,7 @@ template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES> st
 template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES>
 __global__ void __launch_bounds__((TEAMS + COLS * TURNS) * 128 + 96, 1)
 wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_constant__ CUtensorMap map_x,
-                      const DsqGroupGemm p, const int split, const unsigned long long wait_ns)
+                      const DsqGroupGemm p, const int split, const unsigned long long wait_ns, const int skip)
 {
     using L = Layout<XT, MC, GP, TEAMS, COLS, TURNS, STAGES>;
     constexpr bool INT = L::INT;
@@ -240,6 +247,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
     tc_fence_after_sync();
     const uint32_t tmem = lds_32(smem);
     const uint32_t lanes = tmem + ((uint32_t)((warp & 3) * 32) << 16);    // this warp's 32 lanes
+    const unsigned long long drain_ns = wait_ns > DRAIN_NS ? wait_ns : DRAIN_NS;
     bool ok = true;               // (a role whose wait ran out stops; the others' waits run out in turn)
     auto wait = [&](uint32_t bar, uint32_t parity) { ok = wait_warp(smem + bar, parity, wait_ns); return ok; };
     grid_dependency_wait();
@@ -354,7 +362,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         for (; issued < pairs; ++issued) {
             const int stage = issued % STAGES;
             if (issued >= STAGES && !wait(L::EMPTY + 8 * stage, ((issued / STAGES) & 1) ^ 1)) break;
-            if (lane == 0) {
+            if (lane == 0 && issued != skip) {
                 const uint32_t to = smem + L::RING_AT + stage * L::STAGE, bar = smem + L::FULL + 8 * stage;
                 const int at = (c0 >> 1) + issued;
                 mbar_arrive_expect_tx(bar, L::STAGE);
@@ -367,7 +375,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
         }
         // no copy is under way when the block ends
         for (int i = max(0, issued - STAGES); i < issued; ++i)
-            if (!wait_warp(smem + L::FULL + 8 * (i % STAGES), (i / STAGES) & 1, ok ? wait_ns : DRAIN_NS)) ok = false;
+            if (i != skip && !wait_warp(smem + L::FULL + 8 * (i % STAGES), (i / STAGES) & 1, drain_ns)) ok = false;
     } else {
         // Two warps issue, chunks in turn: what they do lies in every chunk's way (commits and waits 0.2 us a
         // chunk, instructions 0.013 us each), so places and most phases are constants of an unrolled loop.
@@ -421,7 +429,7 @@ wgemm_group_tc_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_co
             }
             // no instruction is under way when tensor memory is given up
             mma_commit_elect(smem + L::DONE + 8 * Q);
-            if (!wait_warp(smem + L::DONE + 8 * Q, 0, ok ? wait_ns : DRAIN_NS)) ok = false;
+            if (!wait_warp(smem + L::DONE + 8 * Q, 0, drain_ns)) ok = false;
         };
         if (warp == L::WORKERS / 32 + 1) issue(std::integral_constant<int, 0>());
         else if (L::ISSUERS == 2) issue(std::integral_constant<int, 1>());
@@ -554,7 +562,7 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
     if (st2) return st2;
     const DsqLaunchHooks h = dsq_launch_hooks();
     return dsq_launch(kernel, dim3((unsigned)(tiles * split), (unsigned)mt), dim3(L::THREADS), (size_t)L::BYTES, s,
-                      h.pdl, split, map_w, map_x, p, split, h.wait_ns);
+                      h.pdl, split, map_w, map_x, p, split, h.wait_ns, h.skip_b_round);
 }
 
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)

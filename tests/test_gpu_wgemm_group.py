@@ -247,3 +247,36 @@ def test_both_kernels(dsq, form, size, t):
         again = dsq.dsq_wgemm_group(x.cuda(), packed, M, n, k, 4, group, T(scales), bias=T(bias),
                                     row_scale=None if rs is None else T(rs), w_offset=off)
         assert torch.equal(Y, again)
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.int8])
+@pytest.mark.parametrize("size", [(8, 128, 4096), (20, 300, 1024), (64, 4750, 256)])
+def test_bounded_wait_runs_out_and_the_next_call_is_clean(dsq, size, t):
+    """A wait that nothing satisfies: the test hook makes the copying warp leave out one stage, so the
+    warps that wait for it run into the limit (3 ms here).  The kernel must come back by itself, with
+    NaN where a block had that stage (each has a first one; blocks of a cluster and blocks on their
+    own), and the same call with the hook off must be right."""
+    M, n, k = size
+    codes, scales, bias, packed = weights(dsq, n, k, 128)
+    rng = np.random.default_rng(k)
+    x = rng.integers(-20, 21, (M, k))
+    xt = torch.from_numpy(x).to(t).cuda()
+    rs = torch.ones(M, device="cuda") if t == torch.int8 else None
+    args = (xt, packed, M, n, k, 4, 128, T(scales))
+    dsq.dsq_set_wgemm_group_form(2)
+    try:
+        for skip in (0, 1):
+            dsq.dsq_set_wait_limit_ns(3_000_000)
+            dsq.dsq_set_test_skip_b_round(skip)
+            bad = dsq.dsq_wgemm_group(*args, row_scale=rs)
+            torch.cuda.synchronize()       # the kernel came back
+            dsq.dsq_set_test_skip_b_round(-1)
+            dsq.dsq_set_wait_limit_ns(0)
+            if skip == 0:
+                assert bad.isnan().all()
+            Y = dsq.dsq_wgemm_group(*args, row_scale=rs)
+            check(Y, x.astype(np.float64), codes, scales, 128, None, 0.5, None if rs is None else N(rs))
+    finally:
+        dsq.dsq_set_test_skip_b_round(-1)
+        dsq.dsq_set_wait_limit_ns(0)
+        dsq.dsq_set_wgemm_group_form(0)
