@@ -182,3 +182,57 @@ def test_nothing_outside_the_rows_is_written(dsq):
                                         out_h=pad[:M * K].view(M, K))
     assert (pad[M * K:] == 7.0).all()
     assert torch.equal(pad[:M * K].view(M, K), (x.float() + res.view(M, K).float()).bfloat16())
+
+
+@pytest.mark.parametrize("K", [4096, 49152])
+def test_more_than_2_to_the_31_elements(dsq, K):
+    M = 2 ** 31 // K + 40
+    base = torch.randn(64, K, device="cuda").bfloat16()
+    x = torch.empty(M, K, device="cuda", dtype=torch.bfloat16)
+    x[:] = 1.0
+    x[-64:] = base
+    w = 1 + 0.1 * torch.randn(K, device="cuda")
+    alone = dsq.dsq_rmsnorm_fwd(base, w, 1e-5, quantised=True, want_codes=True, want_rstd=True)
+    _, y, codes, scale, rstd = dsq.dsq_rmsnorm_fwd(x, w, 1e-5, quantised=True, want_codes=True, want_rstd=True)
+    for a, b in zip((y, codes, scale, rstd), alone[1:]):
+        assert torch.equal(a[-64:], b)
+    del y, codes
+    gx, _ = dsq.dsq_rmsnorm_bwd(x, x, w, rstd, want_weight=False)
+    want, _ = dsq.dsq_rmsnorm_bwd(base, base, w, alone[4], want_weight=False)
+    assert torch.equal(gx[-64:], want)
+
+
+def test_captured_backward_passes_beside_one_another(dsq):
+    """Two captured steps with a workspace each, replayed at once on two streams, with new inputs."""
+    M, K = 700, 2048
+    w = 1 + 0.1 * torch.randn(K, device="cuda")
+    def inputs(seed):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        return [torch.randn(M, K, device="cuda", generator=g).bfloat16() for _ in range(3)]
+
+    def step(x, r, gy, ws):
+        h, y, _, _, rstd = dsq.dsq_rmsnorm_fwd(x, w, 1e-5, residual=r, want_rstd=True)
+        return (y,) + tuple(dsq.dsq_rmsnorm_bwd(gy, h, w, rstd, grad_h=gy, ws=ws))
+
+    size = dsq.dsq_rmsnorm_bwd_workspace_bytes(M, K)
+    held = []
+    for i in range(2):
+        a, ws = inputs(50 + i), torch.empty(size, dtype=torch.uint8, device="cuda")
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step(*a, ws)
+        held.append((g, a, ws, out, torch.cuda.Stream()))
+    for seed in range(4):
+        new = [inputs(2 * seed + i) for i in range(2)]
+        ref = [step(*a, None) for a in new]
+        for (g, a, _, _, _), n in zip(held, new):
+            for t, v in zip(a, n):
+                t.copy_(v)
+        torch.cuda.synchronize()
+        for _ in range(3):
+            for g, _, _, _, s in held:
+                with torch.cuda.stream(s):
+                    g.replay()
+        torch.cuda.synchronize()
+        for (_, _, _, out, _), r in zip(held, ref):
+            assert all(torch.equal(a, b) for a, b in zip(out, r))

@@ -280,3 +280,61 @@ def test_bounded_wait_runs_out_and_the_next_call_is_clean(dsq, size, t):
         dsq.dsq_set_test_skip_b_round(-1)
         dsq.dsq_set_wait_limit_ns(0)
         dsq.dsq_set_wgemm_group_form(0)
+
+
+@pytest.mark.parametrize("M", [1, 8, 40])
+def test_codes_of_more_than_2_to_the_31_bytes(dsq, form, M):
+    n, k, group = 262144 + 40, 16384, 128
+    if form == 3 and M > 2:
+        pytest.skip("one or two rows")
+    packed = torch.randint(0, 256, (n, k // 2), dtype=torch.uint8, device="cuda")
+    scales = torch.rand(k // group, n, device="cuda")
+    x = torch.randn(M, k, device="cuda").bfloat16()
+    Y = dsq.dsq_wgemm_group(x, packed, M, n, k, 4, group, scales)
+    for part in (slice(0, 64), slice(262144 - 64, 262144 + 40)):
+        codes = N(dsq.dsq_unpack(packed[part].contiguous(), part.stop - part.start, k, 4, True)).astype(np.int64)
+        check(Y[:, part], N(x.double()), codes, N(scales[:, part]), group, None, 0.5)
+
+
+def test_two_streams_and_two_graphs_at_once(dsq):
+    """Calls that overlap on the GPU share nothing: kernels of each form beside one another."""
+    sizes = [(1, 4096, 4096, torch.bfloat16), (8, 2048, 2048, torch.bfloat16), (64, 1024, 4096, torch.bfloat16),
+             (16, 1500, 4096, torch.int8), (40, 4096, 1024, torch.float16)]
+    calls = []
+    for M, n, k, t in sizes:
+        codes, scales, _, packed = weights(dsq, n, k, 128)
+        x = torch.randint(-90, 91, (M, k), device="cuda").to(t)
+        rs = torch.rand(M, device="cuda") if t == torch.int8 else None
+        calls.append((x, packed, M, n, k, T(scales), rs))
+
+    def run(c, out=None):
+        return dsq.dsq_wgemm_group(c[0], c[1], c[2], c[3], c[4], 4, 128, c[5], row_scale=c[6], out=out)
+
+    ref = [run(c) for c in calls]
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    outs = [[torch.empty_like(r) for r in ref] for _ in streams]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                for j in range(len(calls)):
+                    run(calls[(j + i) % len(calls)], outs[i][(j + i) % len(calls)])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o in outs for a, b in zip(o, ref))
+
+    graphs = []
+    for i in range(2):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            for c, o in zip(calls, outs[i]):
+                run(c, o)
+        graphs.append(g)
+        for o in outs[i]:
+            o.zero_()
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for o in outs[:2] for a, b in zip(o, ref))
