@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(block_of(TPR), sizeof(T) == 2 ? 1024 / block_o
 {
     constexpr int RPB = block_of(TPR) / TPR, ONES = Singles<TPR, ALIGNED>::N, SLOTS = ONES ? ONES : 1;
     __shared__ float2 red[2][block_of(TPR) / 32];
-    __shared__ float wsum[RPB > 1 ? TPR * ITEMS * 8 + 16 : 1];
+    __shared__ float wsum[RPB > 1 || !ALIGNED ? TPR * ITEMS * 8 + 16 : 1];
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * RPB;          // (a multiple of 8 unless ALIGNED)
     const int64_t first = (int64_t)blockIdx.x * RPB + sub;
@@ -442,22 +442,14 @@ __global__ void __launch_bounds__(block_of(TPR), sizeof(T) == 2 ? 1024 / block_o
     if (!p.part) return;
     // the block's row of sums: those of its rows' threads in turn
     float *part = p.part + (int64_t)blockIdx.x * K;
-    if constexpr (RPB == 1) {
+    if constexpr (RPB == 1 && ALIGNED) {
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
-            const int col = cut.head + 8 * (t + i * TPR);
+            const int col = 8 * (t + i * TPR);
             if (t + i * TPR >= cut.nv) continue;
-            if (ALIGNED) {
-                reinterpret_cast<float4 *>(part + col)[0] = make_float4(gw[i][0], gw[i][1], gw[i][2], gw[i][3]);
-                reinterpret_cast<float4 *>(part + col)[1] = make_float4(gw[i][4], gw[i][5], gw[i][6], gw[i][7]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) part[col + k] = gw[i][k];
-            }
+            reinterpret_cast<float4 *>(part + col)[0] = make_float4(gw[i][0], gw[i][1], gw[i][2], gw[i][3]);
+            reinterpret_cast<float4 *>(part + col)[1] = make_float4(gw[i][4], gw[i][5], gw[i][6], gw[i][7]);
         }
-#pragma unroll
-        for (int i = 0; i < ONES; ++i)
-            if (t + i * TPR < cut.singles) part[single_of(cut, t + i * TPR)] = gw1[i];
     } else {
         for (int s = 0; s < RPB; ++s) {
             if (sub == s) {
@@ -577,12 +569,12 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_long_kernel(const BwdParams 
 
 // grad_w[k] = sum over the blocks of their sums, in one order: a warp every 32nd row of sums, eight of
 // its loads on their way together
-constexpr int SUM_ROWS = 32;
-__global__ void __launch_bounds__(32 * SUM_ROWS) weight_sum_kernel(const float *part, int rows, int K, float *out)
+constexpr int SUM_ROWS = 64, SUM_COLS = 16;
+__global__ void __launch_bounds__(SUM_COLS * SUM_ROWS) weight_sum_kernel(const float *part, int rows, int K, float *out)
 {
-    __shared__ float s[SUM_ROWS][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5;
-    const int col = blockIdx.x * 32 + x;
+    __shared__ float s[SUM_ROWS][SUM_COLS + 1];
+    const int x = threadIdx.x % SUM_COLS, y = threadIdx.x / SUM_COLS;
+    const int col = blockIdx.x * SUM_COLS + x;
     grid_dependency_wait();
     grid_launch_dependents();
     float a = 0.f;
@@ -596,11 +588,15 @@ __global__ void __launch_bounds__(32 * SUM_ROWS) weight_sum_kernel(const float *
         }
     s[y][x] = a;
     __syncthreads();
-    // (column y's sums, over the lanes)
-    a = s[x][y];
+    // (a column's sums, over the lanes of a warp)
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp >= SUM_COLS) return;
+    a = 0.f;
+#pragma unroll
+    for (int i = 0; i < SUM_ROWS / 32; ++i) a += s[lane + 32 * i][warp];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
-    if (x == 0 && blockIdx.x * 32 + y < K) out[blockIdx.x * 32 + y] = a;
+    if (lane == 0 && blockIdx.x * SUM_COLS + warp < K) out[blockIdx.x * SUM_COLS + warp] = a;
 }
 
 // threads a row and vectors a thread, of K elements (eight threads take up to 14 single ones).  0: too
@@ -763,7 +759,7 @@ int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h, const
     default: st = al ? bwd_launch<__half, true>(p, s, &blocks) : bwd_launch<__half, false>(p, s, &blocks); break;
     }
     if (st || !grad_weight) return st;
-    return dsq_launch(weight_sum_kernel, dim3((unsigned)((K + 31) / 32)), dim3(32 * SUM_ROWS), 0, s,
+    return dsq_launch(weight_sum_kernel, dim3((unsigned)((K + SUM_COLS - 1) / SUM_COLS)), dim3(SUM_COLS * SUM_ROWS), 0, s,
                       dsq_launch_hooks().pdl, 0, p.part, blocks, (int)K, grad_weight);
 }
 
