@@ -6,6 +6,10 @@
     python -m paper_1908_05033_b200.cases quant --mb 1024 --bits 4
     python -m paper_1908_05033_b200.cases dw --c 192 --hw 56 --batch 64
     python -m paper_1908_05033_b200.cases soft --mb 1024 --bits 4
+    python -m paper_1908_05033_b200.cases norm --m 8192 --size 4096          (forward, 8-bit output)
+    python -m paper_1908_05033_b200.cases normbwd --m 8192 --size 4096
+    python -m paper_1908_05033_b200.cases groups --n 16384 --k 4096 --group 128
+    python -m paper_1908_05033_b200.cases glinear --m 64 --size 8192 --group 128 --type bf16
 
 Each runs the named kernel `--iters` times on seeded synthetic inputs (an L2
 flush between launches) and prints the median CUDA-event time with the
@@ -40,12 +44,15 @@ def _timeit(fn, iters, flush):
 
 def main(argv=None):
     ap = argparse.ArgumentParser()
-    ap.add_argument("case", choices=["gemm", "bgemm", "wgemm", "conv", "quant", "dw", "soft"])
+    ap.add_argument("case", choices=["gemm", "bgemm", "wgemm", "conv", "quant", "dw", "soft",
+                                     "norm", "normbwd", "groups", "glinear"])
     ap.add_argument("--size", type=int, default=4096)
     ap.add_argument("--m", type=int, default=0, help="rows of a GEMM's result (0: --size)")
     ap.add_argument("--n", type=int, default=0, help="its columns")
     ap.add_argument("--k", type=int, default=0, help="its inner extent")
     ap.add_argument("--bits", type=int, default=4)
+    ap.add_argument("--group", type=int, default=128, help="weights that share a scale")
+    ap.add_argument("--type", choices=["f32", "bf16", "f16", "i8"], default="bf16", help="rows of norm and glinear")
     ap.add_argument("--iters", type=int, default=5)
     ap.add_argument("--cin", type=int, default=64)
     ap.add_argument("--cout", type=int, default=64)
@@ -110,6 +117,40 @@ def main(argv=None):
         ms, all_ms = _timeit(lambda: B.dsq_wgemm_bf16(X, W, m, n, k, bits, sc, ws=ws, out=Y),
                              a.iters, flush)
         out.update(size=[m, n, k], ms=ms, tflops=2.0 * m * n * k / (ms * 1e-3) / 1e12, all_ms=all_ms)
+    elif a.case in ("norm", "normbwd"):
+        t = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[a.type]
+        x, r, g = (torch.randn((m, k), device=dev, generator=gen).to(t) for _ in range(3))
+        w = torch.rand(k, device=dev, generator=gen) + 0.5
+        if a.case == "norm":
+            ms, all_ms = _timeit(lambda: B.dsq_rmsnorm_fwd(x, w, 1e-5, residual=r, quantised=True, want_y=False,
+                                                           want_codes=True), a.iters, flush)
+            nbytes = x.numel() * (3 * x.element_size() + 1)
+        else:
+            rstd = torch.ones(m, device=dev)
+            ms, all_ms = _timeit(lambda: B.dsq_rmsnorm_bwd(x, r, w, rstd, grad_h=g), a.iters, flush)
+            nbytes = x.numel() * 4 * x.element_size()
+        out.update(size=[m, k], ms=ms, gbs=nbytes / (ms * 1e-3) / 1e9, all_ms=all_ms)
+    elif a.case == "groups":
+        # weights to codes and scales, and back to values
+        w = torch.randn((n, k), device=dev, generator=gen).to(torch.bfloat16)
+        codes, scales = B.dsq_quantize_groups(w, 4, a.group)
+        ms, all_ms = _timeit(lambda: B.dsq_quantize_groups(w, 4, a.group), a.iters, flush)
+        msv, all_v = _timeit(lambda: B.dsq_dequantize_groups(codes, scales, n, k, 4, a.group), a.iters, flush)
+        nbytes = w.numel() * 2 + codes.numel() + scales.numel() * 4
+        out.update(size=[n, k], group=a.group, ms=ms, gbs=nbytes / (ms * 1e-3) / 1e9, values_ms=msv,
+                   values_gbs=nbytes / (msv * 1e-3) / 1e9, all_ms=all_ms + all_v)
+    elif a.case == "glinear":
+        # rows [m, k] x 4-bit weights [n, k] with a scale per group
+        X = torch.randn((m, k), device=dev, generator=gen)
+        rs = torch.ones(m, device=dev) if a.type == "i8" else None
+        X = {"i8": (30 * X).to(torch.int8), "bf16": X.bfloat16(), "f16": X.half()}[a.type]
+        W = packed(n, 4)
+        sc = torch.rand((B.dsq_group_count(k, a.group), n), device=dev, generator=gen)
+        Y = torch.empty((m, n), dtype=torch.bfloat16, device=dev)
+        ms, all_ms = _timeit(lambda: B.dsq_wgemm_group(X, W, m, n, k, 4, a.group, sc, row_scale=rs,
+                                                       out_dtype=torch.bfloat16, out=Y), a.iters, flush)
+        out.update(size=[m, n, k], group=a.group, ms=ms, gbs=(W.numel() + 4 * sc.numel()) / (ms * 1e-3) / 1e9,
+                   tflops=2.0 * m * n * k / (ms * 1e-3) / 1e12, all_ms=all_ms)
     elif a.case == "conv":
         shape = (a.batch, a.hw, a.hw, a.cin)
         pitch = B.dsq_row_pitch(a.cin, bits)

@@ -16,8 +16,8 @@
 //   * binary32 weights: with j = rint(v) as far as binary32 gives it, the code is j or j - 1
 //     by the sign of 7.5 w - a j, in which the rounding error of a j is taken off.
 //
-// Bound: memory (bf16 in 2.5 bytes a weight, values out 2.5), with arithmetic close behind: the
-// conversions between integers and floating point run at an eighth of the other operations' rate,
+// Bound: memory (bf16 in 2.5 bytes a weight, values out 2.5), with arithmetic close behind (16384 x
+// 4096 in groups of 128: codes 31 us, values 30, at the copy's rate 26): the conversions between integers and floating point run at an eighth of the other operations' rate,
 // so j is read off the sum with 1.5 2^23, and codes become numbers in the mantissa of 2^23.  A
 // thread's column is the same in all its rows, so that nothing is divided per word.
 #include "dsq_groups.h"

@@ -10,7 +10,9 @@
 // All arithmetic is binary32; outputs are rounded once, to their type.  The sum of the
 // residual is not rounded before it is normalised.
 //
-// Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward).  A row stays in
+// Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward): 8192 x 4096 in bf16 takes
+// 46 us forward with fake-quantised output (0.89 of the copy's rate) and 49 backward (0.84; 45 without
+// grad_w, whose sums over the blocks are a kernel of their own).  A row stays in
 // registers between its reduction and its outputs, so every input is read once; the next
 // row of the same threads is on its way meanwhile.  Rows whose length is no multiple of
 // eight start inside a 16-byte vector: the eight-element vectors are counted from the

@@ -3,11 +3,17 @@
 //   Y[m][n] = row_scale[m] sum_g scale[g][n] sum_{k in g} X[m][k] v[n][k] + bias[n],
 // v = 2 c + 1 or c, X bf16, fp16 (row_scale = 1) or int8.
 //
-// With few rows the codes are read once and used once, so a warp takes them from global
-// memory to tensor-core operands in registers (mma.sync; tcgen05 wants its operands in shared
-// memory as whole tiles of 128 rows, of which M would be real: one more pass over every
-// weight).  The sums of a group are kept apart (its products are exact in the tensor core's
-// binary32, or int32, sums) and enter the total with the group's scale in binary32.
+// Three kernels: one or two rows of 16 bits as digits of 8 (dsq_wgemm_group_few.cu); this one, on
+// mma.sync, where there is little work; tcgen05 where there is more (dsq_wgemm_group_tc.cu), by
+// their estimated times.  (us of this one and of tcgen05: bf16, 8 rows, 4096 x 4096 6.0 and 8.0,
+// 8192 x 8192 16.5 and 16.2; 64 rows 18 and 10.4, 64 and 20; int8, 8 rows, 8192 x 8192 10.2 and 13.4,
+// 32 rows 22 and 15.7.)
+//
+// Here the codes are read once and used once: a warp takes them from global memory to tensor-core
+// operands in registers, with one launch's latency and no hand-over between warps but at the
+// end.  The sums of a group are kept apart (its products are exact in the tensor core's
+// binary32, or int32, sums) and enter the total with the group's scale in binary32.  Bound: issue
+// slots, of unpacking and of mma.sync whose 16 rows are M real ones.
 //
 //   * K is cut into chunks of 128 codes, a chunk into four pieces of 32 that never cross
 //     a group.  Of a piece a lane (n = lane / 4, j = lane & 3) has word j of column n:

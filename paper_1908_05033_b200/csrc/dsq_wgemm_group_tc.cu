@@ -181,9 +181,10 @@ template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES> st
     static constexpr int WBOX = 128 * 128, STAGE = WBOX + XBOXES * XBOX;
     static constexpr int RING_AT = 1024, S_AT = RING_AT + STAGES * STAGE, S_STAGE = FLUSHES * 512;
     static constexpr int BYTES = S_AT + TAKES * AHEAD * S_STAGE + 1024;      // (its start is aligned to 1024)
-    // Threads that issue, chunks in turn.  (A thread that issues a chunk's first sum knows that the place's
-    // use before the last is over from its own chunk before, if there are places for a chunk and one more.)
-    static constexpr int ISSUERS = SLOTS > FLUSHES ? 2 : 1;
+    // Warps that issue, chunks in turn: two where a place's sums are always the same one's.  (A warp knows a
+    // place's use before the last to be over only from its own wait for it; else a phase's parity could be
+    // an older one's.)
+    static constexpr int ISSUERS = SLOTS % (2 * FLUSHES) == 0 ? 2 : 1;
     static constexpr int WORKERS = (TEAMS + TAKES) * 128, THREADS = WORKERS + 96;
     // barriers: a stage is full and empty, values made and read, sums ready and place free, all is done
     static constexpr int FULL = 16, EMPTY = FULL + 8 * STAGES, MADE = EMPTY + 8 * STAGES, READ = MADE + 8 * VALUES;
@@ -191,9 +192,10 @@ template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES> st
     static_assert(DONE + 16 <= RING_AT, "barriers");
     static_assert(BYTES <= 227 * 1024 && BYTES > 116 * 1024, "one block an SM");
     static_assert(TURNS * MC * 512 <= STAGES * STAGE, "the totals take the ring's place");
-    static_assert(TURNS == 1 || SLOTS % (2 * FLUSHES) == 0, "a place's sums are one team's and one issuer's");
-    // (a team that has seen the values' last use but one read knows all earlier stages full: wait_full)
-    static_assert(TEAMS <= VALUES && VALUES <= 2 * STAGES && SLOTS >= 2 && A_COL + VALUES * AC <= 512, "phases are waited for in order");
+    static_assert(TURNS == 1 || SLOTS % (2 * FLUSHES) == 0, "a place's sums are one team's");
+    static_assert(VALUES % TEAMS == 0 && VALUES % 2 == 0, "a place's values are one team's, and one issuer's");
+    // (a chunk whose place has been read tells its team that all stages up to its own were full)
+    static_assert(VALUES <= 2 * STAGES && A_COL + VALUES * AC <= 512, "phases are waited for in order");
 };
 
 template <int XT, int MC, int GP, int TEAMS, int COLS, int TURNS, int STAGES>
@@ -565,13 +567,15 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
                       h.pdl, split, map_w, map_x, p, split, h.wait_ns, h.skip_b_round);
 }
 
+// Three teams make values (8192 x 8192, 16 rows, us: two 18.5, three 18.0, four 18.3; 64 rows 22.4, 23.1,
+// 24.4).  Two take sums in turn where places allow (groups of 32, one row 25.0 -> 22.0); with 64 rows two
+// share the columns instead, for the registers.
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
-    constexpr int MORE = XT == DSQ_I8 ? 1 : 0;                    // (of half the size)
-    constexpr int TURNS = GP == 1 && XT != DSQ_I8 ? 1 : 2;
+    constexpr bool INT = XT == DSQ_I8;
     if (p.M <= 8) return launch<XT, 8, GP, 3, 1, 2, 8>(p, s, est_us);
     if (p.M <= 16) return launch<XT, 16, GP, 3, 1, 2, 8>(p, s, est_us);
-    if (p.M <= 32) return launch<XT, 32, GP, 3, 1, TURNS, 4 + 4 * MORE>(p, s, est_us);
+    if (p.M <= 32) return launch<XT, 32, GP, 3, 1, GP == 1 && !INT ? 1 : 2, INT ? 8 : 4>(p, s, est_us);
     return launch<XT, 64, GP, 3, 2, 1, 4>(p, s, est_us);
 }
 
