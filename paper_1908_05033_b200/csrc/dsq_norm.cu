@@ -621,12 +621,16 @@ Form bwd_form(int64_t K)
 }
 
 // Blocks: what is resident together (per_sm: of the kernel; 0: as many as any takes), a multiple of
-// eight rows where rows shift.
-int grid_of(int64_t M, int64_t K, int tpr, int per_sm)
+// eight rows where rows shift; of long rows `rows` a block at least beyond one block an SM: each block
+// leaves a row of sums (backward, us, one, two, three and four rows: 1000 x 2048 9.7, 7.7, 8.4, 8.0; 1111 x
+// 1777 10.4, 9.9, 9.5, 9.0; 600 x 2000 8.6, 6.4, 6.8, 7.0; 1500 x 1500 10.9, 11.0, 9.2, 10.1; without grad_w
+// one is best: 1111 x 1777 4.9, four 5.5).
+int grid_of(int64_t M, int64_t K, int tpr, int per_sm, int rows = 1)
 {
     const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     const int block = tpr ? block_of(tpr) : 1024, rpb = tpr ? block / tpr : 1;
     int64_t g = (M + rpb - 1) / rpb;
+    if (rpb == 1 && g > sms) g = (M + rows - 1) / rows > sms ? (M + rows - 1) / rows : sms;
     const int64_t most = (int64_t)sms * (tpr == 0 ? per_sm : per_sm > 0 && per_sm < 1024 / block ? per_sm : 1024 / block);
     if (g > most) g = most;
     if (K % 8 && rpb < 8) {
@@ -681,7 +685,7 @@ template <class T, bool ALIGNED> int bwd_launch(const BwdParams &p, cudaStream_t
     if (f.tpr == TPR && f.items == ITEMS) { \
         static std::atomic<int> fit{0}; \
         const auto kernel = rmsnorm_bwd_kernel<T, TPR, ITEMS, ALIGNED>; \
-        *blocks = grid_of(p.M, p.K, TPR, blocks_per_sm(kernel, block_of(TPR), &fit)); \
+        *blocks = grid_of(p.M, p.K, TPR, blocks_per_sm(kernel, block_of(TPR), &fit), p.part ? 3 : 1); \
         return dsq_launch(kernel, dim3(*blocks), dim3(block_of(TPR)), 0, s, pdl, 0, p); \
     }
     BWD(8, 1) BWD(16, 1) BWD(32, 1) BWD(64, 1) BWD(128, 1) BWD(256, 1) BWD(512, 1) BWD(1024, 1)
