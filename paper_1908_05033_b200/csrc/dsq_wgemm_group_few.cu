@@ -18,8 +18,8 @@
 //     j = lane & 3) has word j of each of a chunk's eight pieces of 32 codes of column n.
 //   * The warps' totals, and then the digits' ones, are added in a fixed order.
 //
-// One row of bf16, us (at the copy's rate the codes and scales take): 4096 x 4096 4.6 (1.4), 8192 x 8192
-// 10.3 (5.5), 16384 x 8192 19.3 (10.9).  Bound: latency of 16 warps an SM (issue slots 45 %, memory 40 %):
+// One row of bf16, us (at the copy's rate the codes and scales take): 4096 x 4096 4.7 (1.4), 8192 x 8192
+// 10.1 (5.5), 16384 x 8192 18.6 (11.1).  Bound: latency of 16 warps an SM (issue slots 45 %, memory 40 %):
 // their registers allow two blocks, and a third stage, fewer or more columns or warps were slower
 // (8192 x 8192: three stages 12.3, two or eight words of columns 11.8 and 11.7, 16 warps 13.0).
 #include "dsq_groups.h"
@@ -61,8 +61,12 @@ __device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32
 // 8-byte ones
 template <int GP> constexpr int row_bytes() { return GP == 4 ? 272 : 288; }
 
-// ROWS of X; GP: pieces of 32 codes that no group's end cuts
-template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> struct Few {
+// Rows of X, one of them or both.  (One alone, known when compiling, is ordered worse by the compiler:
+// 8192 x 8192 11.3 us against 10.1.)
+constexpr int ROWS = 2;
+
+// GP: pieces of 32 codes that no group's end cuts
+template <int XT, int NT, int GP, int WARPS, int STAGES> struct Few {
     static constexpr int FLUSHES = 8 / GP;
     static constexpr int W_BYTES = NT * 1024, S_BYTES = FLUSHES * NT * 32;
     static constexpr int STAGE = W_BYTES + S_BYTES + ROWS * 512;
@@ -72,18 +76,18 @@ template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> struct Few {
     static_assert(ROWS * 3 <= 8 && WARP_BYTES % 16 == 0 && BYTES <= 227 * 1024, "shared memory");
 };
 
-template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES>
+template <int XT, int NT, int GP, int WARPS, int STAGES>
 __global__ void __launch_bounds__(WARPS * 32)
 wgemm_group_few_kernel(const DsqGroupGemm p)
 {
-    using L = Few<XT, ROWS, NT, GP, WARPS, STAGES>;
+    using L = Few<XT, NT, GP, WARPS, STAGES>;
     constexpr int FLUSHES = L::FLUSHES;
     constexpr int ROW = row_bytes<GP>();
     extern __shared__ __align__(128) uint8_t smem[];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int n = lane >> 2, j = lane & 3;
     const int64_t n0 = (int64_t)blockIdx.x * (8 * NT);
-    const int m0 = blockIdx.y * ROWS, rows = ROWS == 1 ? 1 : min(p.M - m0, ROWS);
+    const int m0 = blockIdx.y * ROWS, rows = min(p.M - m0, ROWS);
     const int chunks = (p.K + 255) >> 8;
     const int turns = warp < chunks ? (chunks - warp - 1) / WARPS + 1 : 0;
     const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * L::WARP_BYTES), digits = ring + STAGES * L::STAGE;
@@ -201,7 +205,7 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
             }
 #pragma unroll
             for (int k = 0; k < 3; ++k) sts_64(to + k * ROW, d[k][0], d[k][1]);
-            if (ROWS == 1 || n / 3 == m) up = inv;
+            if (n / 3 == m) up = inv;
         }
         __syncwarp();
         // Operands: with groups of whole 128s lane j takes the four words of a 16-byte piece one after the
@@ -284,28 +288,22 @@ wgemm_group_few_kernel(const DsqGroupGemm p)
     }
 }
 
-template <int XT, int ROWS, int NT, int GP, int WARPS, int STAGES> int launch(const DsqGroupGemm &p, cudaStream_t s)
+template <int XT, int NT, int GP, int WARPS, int STAGES> int launch(const DsqGroupGemm &p, cudaStream_t s)
 {
-    using L = Few<XT, ROWS, NT, GP, WARPS, STAGES>;
+    using L = Few<XT, NT, GP, WARPS, STAGES>;
     static std::atomic<unsigned long long> configured{0};
-    const auto kernel = wgemm_group_few_kernel<XT, ROWS, NT, GP, WARPS, STAGES>;
+    const auto kernel = wgemm_group_few_kernel<XT, NT, GP, WARPS, STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, L::BYTES, &configured);
     if (st) return st;
     const dim3 grid((unsigned)((p.N + 8 * NT - 1) / (8 * NT)), (unsigned)((p.M + ROWS - 1) / ROWS));
     return dsq_launch(kernel, grid, dim3(WARPS * 32), (size_t)L::BYTES, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s)
-{
-    if (p.M == 1) return launch<XT, 1, 4, GP, 8, 2>(p, s);
-    return launch<XT, 2, 4, GP, 8, 2>(p, s);
-}
-
 template <int XT> int pick_group(DsqGroupGemm p, int64_t group, cudaStream_t s)
 {
     const int gp = dsq_group_pieces(group);
     p.set_units(group, gp);
-    return gp == 4 ? pick<XT, 4>(p, s) : gp == 2 ? pick<XT, 2>(p, s) : pick<XT, 1>(p, s);
+    return gp == 4 ? launch<XT, 4, 4, 8, 2>(p, s) : gp == 2 ? launch<XT, 4, 2, 8, 2>(p, s) : launch<XT, 4, 1, 8, 2>(p, s);
 }
 
 }  // namespace
