@@ -368,6 +368,8 @@ int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,
  * and, where scale_out is given, its 8-bit form (Algorithm 1 steps 1, 3, 4 with the range
  * of each row, 127 steps to its largest magnitude, midpoints upwards):
  *   scale = max_k |y| / 127,  q = floor(y / scale + 1/2),  y = scale q
+ * (the codes are exact for h in binary32, whatever the roundings of rstd, y and scale: rstd
+ * cancels, and which side of a border h weight lies on is decided without rounding)
  *   x         [M][K] of `dtype` (DSQ_F32, DSQ_BF16, DSQ_F16)
  *   residual  like x, or NULL
  *   weight    fp32 [K]

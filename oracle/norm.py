@@ -34,3 +34,19 @@ def backward(grad_y, h, w, rstd, grad_h=None):
         gx = gx + np.asarray(grad_h, np.float64)
         mag = mag + np.abs(np.asarray(grad_h, np.float64))
     return gx, (gy * n).sum(0), mag, np.abs(gy * n).sum(0)
+
+
+def exact_codes(h, w):
+    """floor(127 h w / a + 1/2), a = max |h w| of a row, of binary32 values h [M, K] and w [K]: decided
+    exactly, by 254 h w >= (2 q - 1) a.  (A product of two binary32 numbers fits float64; with a number of
+    eight bits more it fits the 64 bits of a long double.)  Rows of zeros: codes 0."""
+    hw = np.asarray(h, np.float64) * np.asarray(w, np.float64)
+    a = np.abs(hw).max(1, keepdims=True)
+    safe = np.where(a > 0, a, 1.0)
+    q = np.floor(127.0 * (hw / safe) + 0.5)
+    wide = np.longdouble
+    assert np.finfo(wide).nmant >= 63
+    x, a = wide(254) * hw.astype(wide), safe.astype(wide)
+    q -= x < (2 * q - 1).astype(wide) * a
+    q += x >= (2 * q + 1).astype(wide) * a
+    return q.astype(np.int64)

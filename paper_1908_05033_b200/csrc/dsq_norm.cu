@@ -3,7 +3,11 @@
 //   h = x + residual;  rstd = 1/sqrt(mean_k h^2 + eps);  y = h rstd w
 //   8 bits: a = max_k |h w|, q = floor(127 h w / a + 1/2), s = rstd a / 127 (so that
 //   y is about s q): the codes do not depend on rstd, and one pass of reductions
-//   gives the sum of squares and a together.
+//   gives the sum of squares and a together.  Codes are exact for the h and w that binary32
+//   holds: a code on the wrong side of a border changes every output of the product behind it.
+//   The reductions bring what the rounding of a lost as well, and elements next to a border
+//   are decided with what theirs lost (rows of 4096 in bf16: 2 % of the time; of 1024 and less,
+//   where instructions bind, up to a fifth).
 //   backward, with g = grad_y w and n = h rstd:
 //   grad_x = rstd (g - n mean_k(g n)) + grad_h,  grad_w = sum_m grad_y n
 //
@@ -11,7 +15,7 @@
 // residual is not rounded before it is normalised.
 //
 // Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward): 8192 x 4096 in bf16 takes
-// 46 us forward with fake-quantised output (0.89 of the copy's rate) and 49 backward (0.84; 45 without
+// 47.5 us forward with fake-quantised output (0.87 of the copy's rate) and 49 backward (0.84; 45 without
 // grad_w, whose sums over the blocks are a kernel of their own).  A row stays in
 // registers between its reduction and its outputs, so every input is read once; the next
 // row of the same threads is on its way meanwhile.  Rows whose length is no multiple of
@@ -23,6 +27,8 @@
 // A thread meets the same columns in all its rows (the weight, and the sums of grad_w,
 // stay in registers): its rows are a multiple of eight apart where rows shift.
 #include <math.h>
+
+#include <type_traits>
 
 #include "dsq_launch.h"
 #include "dsq_ptx.cuh"
@@ -71,11 +77,13 @@ template <bool ALIGNED> __device__ __forceinline__ Cut cut_of(int64_t row, int K
 // column of single element j
 __device__ __forceinline__ int single_of(const Cut &c, int j) { return j < c.head ? j : j + 8 * c.nv; }
 
-__device__ __forceinline__ void store_codes(int8_t *p, const int (&q)[8])
+// the low bytes of eight numbers
+__device__ __forceinline__ void store_codes(int8_t *p, const float (&f)[8])
 {
     uint2 v;
-    v.x = __byte_perm(__byte_perm(q[0], q[1], 0x0040), __byte_perm(q[2], q[3], 0x0040), 0x5410);
-    v.y = __byte_perm(__byte_perm(q[4], q[5], 0x0040), __byte_perm(q[6], q[7], 0x0040), 0x5410);
+    const auto u = [&](int i) { return __float_as_uint(f[i]); };
+    v.x = __byte_perm(__byte_perm(u(0), u(1), 0x0040), __byte_perm(u(2), u(3), 0x0040), 0x5410);
+    v.y = __byte_perm(__byte_perm(u(4), u(5), 0x0040), __byte_perm(u(6), u(7), 0x0040), 0x5410);
     *reinterpret_cast<uint2 *>(p) = v;
 }
 template <class T> __device__ __forceinline__ void store_vec(T *p, const float (&f)[8])
@@ -123,54 +131,183 @@ __device__ __forceinline__ void reduce_row(float &sum, uint32_t &top, float2 *re
     }
 }
 
+// What the rounding of the largest |h w| lost: the largest |h w| - top, exactly (times 2^60 where top is so small that
+// some of it would lie below binary32's smallest number), as bits that order like numbers and are never 0.
+constexpr float SMALL = 8.6736174e-19f, UP = 1.1529215e18f;     // 2^-60, 2^60
+// the largest of three, NaN where one is
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
+template <bool TINY> __device__ __forceinline__ float above(float most, float h, float w, float top)
+{
+    if (!TINY) return max3(most, __fmaf_rn(h, w, -top), __fmaf_rn(-h, w, -top));
+    const float ah = fabsf(h), aw = fabsf(w);
+    return fmaxf(most, __fmaf_rn(fminf(ah, aw) * UP, fmaxf(ah, aw), -top * UP));
+}
+// largest |h w| of N elements and `most`
+template <int N> __device__ __forceinline__ float largest(float most, const float (&h)[N], const float (&w)[N])
+{
+#pragma unroll
+    for (int k = 0; k + 1 < N; k += 2) most = max3(most, fabsf(h[k] * w[k]), fabsf(h[k + 1] * w[k + 1]));
+    if (N % 2) most = max3(most, most, fabsf(h[N - 1] * w[N - 1]));
+    return most;
+}
+__device__ __forceinline__ uint32_t ordered(float v)
+{
+    const uint32_t bits = __float_as_uint(v);
+    return bits ^ ((uint32_t)((int)bits >> 31) | 0x80000000u);
+}
+
+__device__ __forceinline__ float from_ordered(uint32_t v) { return __uint_as_float((int)v < 0 ? v ^ 0x80000000u : ~v); }
+template <int N> __device__ __forceinline__ uint32_t low_of(const float (&h)[N], const float (&w)[N], float own)
+{
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = own >= SMALL ? above<false>(most, h[i], w[i], own) : above<true>(most, h[i], w[i], own);
+    return ordered(most);
+}
+
+// The same for the forward pass, where the largest is wanted for rows in 8 bits alone, and with it what its rounding lost:
+// the largest `low` of the threads that have it.
+template <int TPR, bool EIGHT>
+__device__ __forceinline__ void reduce_row_low(float &sum, uint32_t &top, uint32_t &low, float4 *red)
+{
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    [[maybe_unused]] const uint32_t own = top;
+#pragma unroll
+    for (int o = (TPR < 32 ? TPR : 32) / 2; o > 0; o >>= 1) {
+        sum += __shfl_xor_sync(~0u, sum, o);
+        if (EIGHT && TPR < 32) top = max(top, __shfl_xor_sync(~0u, top, o));
+    }
+    if constexpr (EIGHT) {
+        if (TPR >= 32) top = __reduce_max_sync(~0u, top);
+        low = own == top ? low : 0u;
+        if (TPR >= 32) {
+            low = __reduce_max_sync(~0u, low);
+        } else {
+#pragma unroll
+            for (int o = TPR / 2; o > 0; o >>= 1) low = max(low, __shfl_xor_sync(~0u, low, o));
+        }
+    }
+    if constexpr (TPR > 32) {
+        constexpr int W = TPR / 32;
+        if (lane == 0) red[warp] = make_float4(sum, __uint_as_float(top), __uint_as_float(low), 0.f);
+        __syncthreads();
+        const float4 v = red[warp / W * W + (lane % W)];
+        sum = v.x;
+#pragma unroll
+        for (int o = W / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        if constexpr (EIGHT) {
+            top = __reduce_max_sync(~0u, __float_as_uint(v.y));
+            low = __reduce_max_sync(~0u, __float_as_uint(v.y) == top ? __float_as_uint(v.z) : 0u);
+        }
+    }
+}
+
 // what a row's reductions give its elements
-struct RowQuant { float rstd, inv, s; };
-__device__ __forceinline__ RowQuant row_quant(float sum, uint32_t top, float inv_k, float eps)
+struct RowQuant { float rstd, inv, up, s; uint32_t top, low; };      // inv, up: 127 / a, less and more a small part of it
+__device__ __forceinline__ RowQuant row_quant(float sum, uint32_t top, uint32_t low, float inv_k, float eps)
 {
     RowQuant r;
     r.rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(sum, inv_k, eps)));
     const float a = __uint_as_float(top);
     // (bits above those of infinity: NaN)
     const bool bad = top >= 0x7F800000u, none = a < 1.5046328e-36f;      // 2^-119: 127 / a is finite
-    r.inv = bad || none ? 0.f : __fdiv_rn(127.f, a);
+    // 127 / (a and what its rounding lost), rounded once
+    const float quot = __fdiv_rn(127.f, a), low_part = from_ordered(low) * (a < SMALL ? 1.f / UP : 1.f);
+    const float inv = __fmaf_rn(-quot, low_part * quot * (1.f / 127.f), quot);
+    const float part = a < SMALL ? 3.8146973e-6f : 2.3841858e-7f;       // 2^-18 (products lose more bits there), 2^-22
+    r.inv = bad || none ? 0.f : inv * (1.f - part);
+    r.up = inv * (1.f + part);
     r.s = bad ? __uint_as_float(0x7FC00000u) : none ? 0.f : r.rstd * a * (1.f / 127.f);
+    r.top = top;
+    r.low = low;
     return r;
 }
-__device__ __forceinline__ int code_of(float hw, float inv)
+
+// The code of an element so near to the border between two codes that rounded products do not tell on which side it lies:
+// the sign of 254 h w - b a, b twice the border.  Both products are sums of two numbers, p + e and top + low (all of
+// them times a power of two where they are tiny or huge), and what is left of 254 p - b top, of e's and of low's
+// products are exact sums.
+__device__ __noinline__ float exact_code(float h, float w, float b, uint32_t top_bits, uint32_t low_bits)
 {
-    return inv == 0.f ? 0 : __float2int_rd(__fmaf_rn(hw, inv, 0.5f));
+    float top = __uint_as_float(top_bits), low = from_ordered(low_bits);
+    if (top < SMALL || top > 1.f / SMALL) {
+        const bool first = (fabsf(h) < fabsf(w)) == (top < SMALL);       // whose range bears it
+        const float f = top < SMALL ? UP : 1.f / UP;
+        h *= first ? f : 1.f;
+        w *= first ? 1.f : f;
+        if (top > 1.f) low *= f;
+        top *= f;
+    }
+    const float p = h * w, e = __fmaf_rn(h, w, -p);
+    const float u = b * top, t = __fsub_rn(__fmaf_rn(254.f, p, -u), __fmaf_rn(b, top, -u));
+    const float x = 254.f * e, y = b * low, v = __fsub_rn(x, y), z = __fsub_rn(v, x);
+    const float vl = __fsub_rn(__fsub_rn(x, __fsub_rn(v, z)), __fadd_rn(y, z));          // x - y = v + vl
+    const float rest = __fadd_rn(vl, __fsub_rn(__fmaf_rn(254.f, e, -x), __fmaf_rn(b, low, -y)));
+    const float off = __fadd_rn(__fadd_rn(t, v), rest);
+    return 0.5f * b + (off < 0.f ? -0.5f : 0.5f);
+}
+// Codes floor(127 h w / a + 1/2) of N elements, as MAGIC and the code (whose low byte is the code's).  The rounded product
+// times the rounded 127 / a is off by 2^-23 of itself (and 2^-46 of it): times 1 +- 2^-22 it gives the code twice.  Where
+// it does not, the element lies next to a border (one in 60000; rows of small integers meet borders often), and its
+// code is found exactly.
+constexpr float MAGIC = 12582912.f;                            // 1.5 2^23
+template <int N> __device__ __forceinline__ void codes_of(const float (&h)[N], const float (&w)[N], const RowQuant &r, float (&t)[N])
+{
+    if (r.inv == 0.f) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) t[i] = MAGIC;
+        return;
+    }
+    uint32_t open = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float p = h[i] * w[i];
+        t[i] = __fmaf_rn(p, r.inv, MAGIC);
+        open |= __float_as_uint(t[i]) ^ __float_as_uint(__fmaf_rn(p, r.up, MAGIC));
+    }
+    if (!open) return;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float up = __fmaf_rn(h[i] * w[i], r.up, MAGIC);
+        if (t[i] != up) t[i] = MAGIC + exact_code(h[i], w[i], __fadd_rn(__fsub_rn(t[i], MAGIC), __fsub_rn(up, MAGIC)), r.top, r.low);
+    }
 }
 
 // outputs of eight elements at flat index `at`, and of one
-template <class T>
+template <class T, bool EIGHT>
 __device__ __forceinline__ void write_outputs(const FwdParams &p, int64_t at, const float (&h)[8], const float (&w)[8],
                                               const RowQuant &r)
 {
     if (p.h) store_vec((T *)p.h + at, h);
     float y[8];
-    if (p.scale) {
-        int q[8];
+    if constexpr (EIGHT) {
+        codes_of<8>(h, w, r, y);
+        if (p.codes) store_codes(p.codes + at, y);
+        if (!p.y) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            q[i] = code_of(h[i] * w[i], r.inv);
-            y[i] = r.s * (float)q[i];
-        }
-        if (p.codes) store_codes(p.codes + at, q);
+        for (int i = 0; i < 8; ++i) y[i] = r.s * __fsub_rn(y[i], MAGIC);
     } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = h[i] * r.rstd * w[i];
     }
     if (p.y) store_vec((T *)p.y + at, y);
 }
-template <class T>
+template <class T, bool EIGHT>
 __device__ __forceinline__ void write_output(const FwdParams &p, int64_t at, float h, float w, const RowQuant &r)
 {
     if (p.h) ((T *)p.h)[at] = dsq_from_f32<T>(h);
     float y = h * r.rstd * w;
-    if (p.scale) {
-        const int q = code_of(h * w, r.inv);
-        y = r.s * (float)q;
-        if (p.codes) p.codes[at] = (int8_t)q;
+    if constexpr (EIGHT) {
+        const float h1[1] = {h}, w1[1] = {w};
+        float code[1];
+        codes_of<1>(h1, w1, r, code);
+        y = r.s * __fsub_rn(code[0], MAGIC);
+        if (p.codes) p.codes[at] = (int8_t)__float_as_uint(code[0]);
     }
     if (p.y) ((T *)p.y)[at] = dsq_from_f32<T>(y);
 }
@@ -178,12 +315,21 @@ __device__ __forceinline__ void write_output(const FwdParams &p, int64_t at, flo
 // single elements of a row a thread takes (14 at most)
 template <int TPR, bool ALIGNED> struct Singles { static constexpr int N = ALIGNED ? 0 : TPR >= 16 ? 1 : 2; };
 
+// Blocks an SM that rows in 8 bits are given registers for.  (Left to the compiler the path of exact codes takes 90 to 125
+// for rows of one vector a thread: 16384 x 1024 in bf16 29.3 us, 27.4 with three blocks of 256; with four it spills, 29.0.)
+__host__ __device__ constexpr int fwd_blocks(int size, int tpr, int items, bool eight)
+{
+    if (!eight) return 1;
+    if (items == 2) return 512 / block_of(tpr);
+    return tpr >= 512 ? (size == 2 ? 1024 : 512) / block_of(tpr) + (tpr == 1024 && size == 4) : 3;
+}
+
 // TPR threads a row, ITEMS vectors of eight a thread
-template <class T, int TPR, int ITEMS, bool ALIGNED>
-__global__ void __launch_bounds__(block_of(TPR)) rmsnorm_fwd_kernel(const FwdParams p)
+template <class T, int TPR, int ITEMS, bool ALIGNED, bool EIGHT>
+__global__ void __launch_bounds__(block_of(TPR), fwd_blocks(sizeof(T), TPR, ITEMS, EIGHT)) rmsnorm_fwd_kernel(const FwdParams p)
 {
     constexpr int RPB = block_of(TPR) / TPR, ONES = Singles<TPR, ALIGNED>::N, SLOTS = ONES ? ONES : 1;
-    __shared__ float2 red[2][block_of(TPR) / 32];
+    __shared__ float4 red[2][block_of(TPR) / 32];
     const int sub = threadIdx.x / TPR, t = threadIdx.x % TPR;
     const int64_t step = (int64_t)gridDim.x * RPB;          // (a multiple of 8 unless ALIGNED)
     const int64_t first = (int64_t)blockIdx.x * RPB + sub;
@@ -224,8 +370,7 @@ __global__ void __launch_bounds__(block_of(TPR)) rmsnorm_fwd_kernel(const FwdPar
     for (int64_t base = (int64_t)blockIdx.x * RPB; base < p.M; base += step, buf ^= 1) {
         const int64_t row = base + sub, at = row * K + cut.head;
         float h[ITEMS][8], one[SLOTS];
-        float sum = 0.f;
-        uint32_t top = 0;
+        float sum = 0.f, most = 0.f;
 #pragma unroll
         for (int i = 0; i < ITEMS; ++i) {
             const bool in = row < p.M && t + i * TPR < cut.nv;
@@ -240,29 +385,45 @@ __global__ void __launch_bounds__(block_of(TPR)) rmsnorm_fwd_kernel(const FwdPar
             for (int k = 0; k < 8; ++k) {
                 if (!in) h[i][k] = 0.f;
                 sum = __fmaf_rn(h[i][k], h[i][k], sum);
-                top = max(top, __float_as_uint(h[i][k] * w[i][k]) & 0x7FFFFFFFu);
             }
+            if (EIGHT) most = largest<8>(most, h[i], w[i]);
         }
 #pragma unroll
         for (int i = 0; i < ONES; ++i) {
             one[i] = row < p.M && t + i * TPR < cut.singles ? dsq_to_f32(x1[i]) + (res ? dsq_to_f32(r1[i]) : 0.f) : 0.f;
             sum = __fmaf_rn(one[i], one[i], sum);
-            top = max(top, __float_as_uint(one[i] * w1[i]) & 0x7FFFFFFFu);
+            if (EIGHT) most = max3(most, most, fabsf(one[i] * w1[i]));
         }
         load(row + step);
-        reduce_row<TPR>(sum, top, red[buf]);
-        const RowQuant r = row_quant(sum, top, p.inv_k, p.eps);
+        uint32_t top = __float_as_uint(most), low = 0;
+        if constexpr (EIGHT) {
+            const float own = most;
+            most = -INFINITY;
+            auto each = [&](auto tiny) {
+#pragma unroll
+                for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) most = above<decltype(tiny)::value>(most, h[i][k], w[i][k], own);
+#pragma unroll
+                for (int i = 0; i < ONES; ++i) most = above<decltype(tiny)::value>(most, one[i], w1[i], own);
+            };
+            if (own >= SMALL || own == 0.f) each(std::false_type());
+            else each(std::true_type());
+            low = ordered(most);
+        }
+        reduce_row_low<TPR, EIGHT>(sum, top, low, red[buf]);
+        const RowQuant r = row_quant(sum, top, low, p.inv_k, p.eps);
         if (row < p.M) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
                 const int v = t + i * TPR;
-                if (v < cut.nv) write_outputs<T>(p, at + 8 * v, h[i], w[i], r);
+                if (v < cut.nv) write_outputs<T, EIGHT>(p, at + 8 * v, h[i], w[i], r);
             }
 #pragma unroll
             for (int i = 0; i < ONES; ++i)
-                if (t + i * TPR < cut.singles) write_output<T>(p, row * K + single_of(cut, t + i * TPR), one[i], w1[i], r);
+                if (t + i * TPR < cut.singles) write_output<T, EIGHT>(p, row * K + single_of(cut, t + i * TPR), one[i], w1[i], r);
             if (t == 0) {
-                if (p.scale) p.scale[row] = r.s;
+                if (EIGHT) p.scale[row] = r.s;
                 if (p.rstd) p.rstd[row] = r.rstd;
             }
         }
@@ -270,10 +431,12 @@ __global__ void __launch_bounds__(block_of(TPR)) rmsnorm_fwd_kernel(const FwdPar
 }
 
 // rows too long for the registers of a block: read twice, the second time from the caches
-template <class T, bool ALIGNED>
+template <class T, bool ALIGNED, bool EIGHT>
 __global__ void __launch_bounds__(1024, 2) rmsnorm_fwd_long_kernel(const FwdParams p)
 {
     __shared__ float2 red[2][32];
+    __shared__ uint32_t lows[2];
+    if (EIGHT && threadIdx.x < 2) lows[threadIdx.x] = 0;
     const T *x = (const T *)p.x, *res = (const T *)p.res;
     const int K = p.K;
     grid_dependency_wait();
@@ -296,32 +459,46 @@ __global__ void __launch_bounds__(1024, 2) rmsnorm_fwd_long_kernel(const FwdPara
             }
             load_weight<ALIGNED>(p.w + cut.head + 8 * v, true, w);
         };
-        float sum = 0.f, h[8], w[8], h1 = 0.f, w1 = 0.f;
-        uint32_t top = 0;
+        float sum = 0.f, most = 0.f, h[8], w[8], h1[1] = {0.f}, w1[1] = {0.f};
         if (single) {
-            h1 = dsq_to_f32(x[one]);
-            if (res) h1 += dsq_to_f32(res[one]);
-            w1 = __ldg(p.w + single_of(cut, threadIdx.x));
-            sum = h1 * h1;
-            top = __float_as_uint(h1 * w1) & 0x7FFFFFFFu;
+            h1[0] = dsq_to_f32(x[one]);
+            if (res) h1[0] += dsq_to_f32(res[one]);
+            w1[0] = __ldg(p.w + single_of(cut, threadIdx.x));
+            sum = h1[0] * h1[0];
+            if (EIGHT) most = largest<1>(most, h1, w1);
         }
         for (int v = threadIdx.x; v < cut.nv; v += 1024) {
             value(v, h, w);
 #pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                sum = __fmaf_rn(h[k], h[k], sum);
-                top = max(top, __float_as_uint(h[k] * w[k]) & 0x7FFFFFFFu);
-            }
+            for (int k = 0; k < 8; ++k) sum = __fmaf_rn(h[k], h[k], sum);
+            if (EIGHT) most = largest<8>(most, h, w);
         }
+        uint32_t top = __float_as_uint(most);
         reduce_row<1024>(sum, top, red[buf]);
-        const RowQuant r = row_quant(sum, top, p.inv_k, p.eps);
+        uint32_t low = 0;
+        if constexpr (EIGHT) {
+            // (by the few threads that hold it, which read their part of the row once more: kept by each thread along with
+            // its largest product it takes registers, 2048 x 16384 112 us)
+            if (__float_as_uint(most) == top) {
+                if (single) low = low_of<1>(h1, w1, most);
+                for (int v = threadIdx.x; v < cut.nv; v += 1024) {
+                    value(v, h, w);
+                    low = max(low, low_of<8>(h, w, most));
+                }
+                atomicMax(&lows[buf], low);
+            }
+            __syncthreads();
+            low = lows[buf];
+            if (threadIdx.x == 0) lows[buf ^ 1] = 0;
+        }
+        const RowQuant r = row_quant(sum, top, low, p.inv_k, p.eps);
         for (int v = threadIdx.x; v < cut.nv; v += 1024) {
             value(v, h, w);
-            write_outputs<T>(p, at + 8 * v, h, w, r);
+            write_outputs<T, EIGHT>(p, at + 8 * v, h, w, r);
         }
-        if (single) write_output<T>(p, one, h1, w1, r);
+        if (single) write_output<T, EIGHT>(p, one, h1[0], w1[0], r);
         if (threadIdx.x == 0) {
-            if (p.scale) p.scale[row] = r.s;
+            if (EIGHT) p.scale[row] = r.s;
             if (p.rstd) p.rstd[row] = r.rstd;
         }
     }
@@ -653,14 +830,14 @@ template <class K> int blocks_per_sm(K kernel, int block, std::atomic<int> *cach
     return n;
 }
 
-template <class T, bool ALIGNED> int fwd_launch(const FwdParams &p, cudaStream_t s)
+template <class T, bool ALIGNED, bool EIGHT> int fwd_launch(const FwdParams &p, cudaStream_t s)
 {
     const Form f = fwd_form(p.K);
     const int pdl = dsq_launch_hooks().pdl;
 #define FWD(TPR, ITEMS) \
     if (f.tpr == TPR && f.items == ITEMS) { \
         static std::atomic<int> fit{0}; \
-        const auto kernel = rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED>; \
+        const auto kernel = rmsnorm_fwd_kernel<T, TPR, ITEMS, ALIGNED, EIGHT>; \
         const dim3 grid(grid_of(p.M, p.K, TPR, blocks_per_sm(kernel, block_of(TPR), &fit))); \
         return dsq_launch(kernel, grid, dim3(block_of(TPR)), 0, s, pdl, 0, p); \
     }
@@ -671,7 +848,14 @@ template <class T, bool ALIGNED> int fwd_launch(const FwdParams &p, cudaStream_t
         FWD(256, 1) FWD(512, 1) FWD(1024, 1)
     }
 #undef FWD
-    return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED>, dim3(grid_of(p.M, p.K, 0, 2)), dim3(1024), 0, s, pdl, 0, p);
+    return dsq_launch(rmsnorm_fwd_long_kernel<T, ALIGNED, EIGHT>, dim3(grid_of(p.M, p.K, 0, 2)), dim3(1024), 0, s, pdl, 0, p);
+}
+
+template <class T> int fwd_pick(const FwdParams &p, cudaStream_t s)
+{
+    const bool al = p.K % 8 == 0;
+    if (p.scale) return al ? fwd_launch<T, true, true>(p, s) : fwd_launch<T, false, true>(p, s);
+    return al ? fwd_launch<T, true, false>(p, s) : fwd_launch<T, false, false>(p, s);
 }
 
 // (the workspace is sized for the most blocks that any type takes)
@@ -726,11 +910,10 @@ int dsq_rmsnorm_fwd(const void *x, const void *residual, const float *weight, in
     p.M = M; p.K = (int)K;
     p.eps = eps; p.inv_k = (float)(1.0 / (double)K);
     cudaStream_t s = (cudaStream_t)stream;
-    const bool al = K % 8 == 0;
     switch (dtype) {
-    case DSQ_F32: return al ? fwd_launch<float, true>(p, s) : fwd_launch<float, false>(p, s);
-    case DSQ_BF16: return al ? fwd_launch<__nv_bfloat16, true>(p, s) : fwd_launch<__nv_bfloat16, false>(p, s);
-    default: return al ? fwd_launch<__half, true>(p, s) : fwd_launch<__half, false>(p, s);
+    case DSQ_F32: return fwd_pick<float>(p, s);
+    case DSQ_BF16: return fwd_pick<__nv_bfloat16>(p, s);
+    default: return fwd_pick<__half>(p, s);
     }
 }
 
