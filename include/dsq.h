@@ -347,11 +347,9 @@ int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N,
  *   W_codes, scales, bits, group  as dsq_quantize_groups leaves them
  *   bias      fp32 [N] or NULL
  *   Y         [M][N] of y_type: DSQ_F32, DSQ_BF16 or DSQ_F16
- * Any M up to 64 * 65535 (DSQ_ERR_SIZE beyond; up to 64 rows a pass over the weights).  With
- * three rows or more products are exact, and a group's are added by the tensor core in binary32.
- * One or two rows of 16 bits are made integers first: an element is exact down to 2^-14 (DSQ_BF16)
- * or 2^-11 (DSQ_F16) of the largest of its 256 neighbours (k / 256), and below that off by at
- * most 2^-22 of that largest; a group's sums are then exact.  With DSQ_I8 a group's sums are exact
+ * Any M up to 64 * 65535 (DSQ_ERR_SIZE beyond; up to 64 rows a pass over the weights).  Products
+ * X v are exact.  With three rows of 16 bits or more a group's are added by the tensor core in
+ * binary32; with one or two, sums of up to 128 are exact.  With DSQ_I8 a group's sums are exact
  * in int32 (groups of up to 2^16 weights, DSQ_ERR_OVERFLOW beyond).  Groups are added in binary32 in
  * a fixed order: the same call gives the same bits on the same GPU.  Y is rounded once.  A row with an
  * infinity or a NaN gives what such terms give, or NaN; other rows do not see it.  Device-side waits
