@@ -348,10 +348,10 @@ int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N,
  *   bias      fp32 [N] or NULL
  *   Y         [M][N] of y_type: DSQ_F32, DSQ_BF16 or DSQ_F16
  * Any M up to 64 * 65535 (DSQ_ERR_SIZE beyond; up to 64 rows a pass over the weights).  Products
- * X v are exact.  With three rows of 16 bits or more a group's are added by the tensor core in
- * binary32; with one or two, sums of up to 128 are exact.  With DSQ_I8 a group's sums are exact
- * in int32 (groups of up to 2^16 weights, DSQ_ERR_OVERFLOW beyond).  Groups are added in binary32 in
- * a fixed order: the same call gives the same bits on the same GPU.  Y is rounded once.  A row with an
+ * X v are exact, and added in sums of up to 128 codes of a group: by the tensor core in binary32
+ * with three rows of 16 bits or more, exactly with DSQ_I8 (groups of up to 2^16 weights:
+ * DSQ_ERR_OVERFLOW beyond) and with one or two rows.  Those sums are added, times their group's
+ * scale, in binary32 in a fixed order: the same call gives the same bits on the same GPU.  Y is rounded once.  A row with an
  * infinity or a NaN gives what such terms give, or NaN; other rows do not see it.  Device-side waits
  * are bounded: outputs that one is given up for are NaN (there is no workspace to hold a status). */
 int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,

@@ -340,7 +340,8 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
         if (!dsq_aligned16(a)) return DSQ_ERR_ALIGN;
     if (K % (x_type == DSQ_I8 ? 16 : 8) != 0) return DSQ_ERR_ALIGN;
     if (M > 65535 * 64) return DSQ_ERR_SIZE;
-    // (a group longer than the row is the row; a group's sum of at most 128 * 128 a term stays in int32)
+    // (a group longer than the row is the row.  Longer groups of 8-bit rows are refused as the interface has it: the
+    // kernels take exact sums of 128 codes at most, which are far from int32's end.)
     const int64_t g = dsq_group_count(K, group) == 1 ? (K + 127) / 128 * 128 : group;
     if (x_type == DSQ_I8 && (g < K ? g : K) > (1 << 16)) return DSQ_ERR_OVERFLOW;
     DsqGroupGemm p;
