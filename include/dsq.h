@@ -377,7 +377,9 @@ int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,
  *   scale_out fp32 [M], or NULL: no 8-bit form
  *   rstd_out  fp32 [M], or NULL (dsq_rmsnorm_bwd reads it)
  * Arithmetic is binary32, outputs are rounded once; h is normalised as it is before its
- * rounding.  A row with a NaN or an infinity in h weight has scale NaN and codes 0; one whose
+ * rounding.  Rows whose squares are outside binary32's range are scaled by a power of two first;
+ * rstd is binary32's largest number where it would be above it, and 0 for a row of zeros with
+ * eps = 0 (y: 0).  A row with a NaN or an infinity in h weight has scale NaN and codes 0; one whose
  * |h weight| are all below 2^-119 scale 0 and codes 0.  eps < 0 or not finite:
  * DSQ_ERR_RANGE.  K at most 49152 (DSQ_ERR_SIZE).  HBM-bound. */
 int dsq_rmsnorm_fwd(const void *x, const void *residual, const float *weight,

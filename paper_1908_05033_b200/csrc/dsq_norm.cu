@@ -6,16 +6,17 @@
 //   gives the sum of squares and a together.  Codes are exact for the h and w that binary32
 //   holds: a code on the wrong side of a border changes every output of the product behind it.
 //   The reductions bring what the rounding of a lost as well, and elements next to a border
-//   are decided with what theirs lost (rows of 4096 in bf16: 2 % of the time; of 1024 and less,
-//   where instructions bind, up to a fifth).
+//   are decided with what theirs lost (8192 x 4096 in bf16: 2 % of the time; shorter and
+//   unaligned rows, where instructions bind, up to a quarter: 16384 x 1024 23.7 -> 29.9 us).
 //   backward, with g = grad_y w and n = h rstd:
 //   grad_x = rstd (g - n mean_k(g n)) + grad_h,  grad_w = sum_m grad_y n
 //
 // All arithmetic is binary32; outputs are rounded once, to their type.  The sum of the
-// residual is not rounded before it is normalised.
+// residual is not rounded before it is normalised.  Rows whose squares overflow, or vanish beside
+// a tiny eps, take a second reduction of the row times a power of two.
 //
 // Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward): 8192 x 4096 in bf16 takes
-// 47.5 us forward with fake-quantised output (0.87 of the copy's rate) and 49 backward (0.84; 45 without
+// 47.4 us forward with fake-quantised output (0.87 of the copy's rate) and 49 backward (0.84; 45 without
 // grad_w, whose sums over the blocks are a kernel of their own).  A row stays in
 // registers between its reduction and its outputs, so every input is read once; the next
 // row of the same threads is on its way meanwhile.  Rows whose length is no multiple of
@@ -170,10 +171,14 @@ template <int N> __device__ __forceinline__ uint32_t low_of(const float (&h)[N],
     return ordered(most);
 }
 
+// Whether a mean of squares (and eps) has left binary32's range, or is so small that squares below it count.
+__device__ __forceinline__ bool out_of_range(float mean) { return !(mean < 3.0e38f) || mean < 8.2718061e-25f; }     // 2^-80
+
 // The same for the forward pass, where the largest is wanted for rows in 8 bits alone, and with it what its rounding lost:
-// the largest `low` of the threads that have it.
+// the largest `low` of the threads that have it.  True, for all threads that share a barrier, where the sum of one of their
+// rows is out of range.
 template <int TPR, bool EIGHT>
-__device__ __forceinline__ void reduce_row_low(float &sum, uint32_t &top, uint32_t &low, float4 *red)
+__device__ __forceinline__ bool reduce_row_low(float &sum, uint32_t &top, uint32_t &low, float4 *red, float inv_k, float eps)
 {
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     [[maybe_unused]] const uint32_t own = top;
@@ -192,27 +197,48 @@ __device__ __forceinline__ void reduce_row_low(float &sum, uint32_t &top, uint32
             for (int o = TPR / 2; o > 0; o >>= 1) low = max(low, __shfl_xor_sync(~0u, low, o));
         }
     }
+    bool far;
     if constexpr (TPR > 32) {
-        constexpr int W = TPR / 32;
+        constexpr int W = TPR / 32, ALL = block_of(TPR) / 32;        // warps of a row, of the block
         if (lane == 0) red[warp] = make_float4(sum, __uint_as_float(top), __uint_as_float(low), 0.f);
         __syncthreads();
-        const float4 v = red[warp / W * W + (lane % W)];
+        const float4 v = red[lane % ALL];
+        const bool mine = ALL == W || lane % ALL / W == warp / W;
         sum = v.x;
 #pragma unroll
         for (int o = W / 2; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
+        far = __any_sync(~0u, out_of_range(__fmaf_rn(sum, inv_k, eps)));
+        if (ALL > W) sum = __shfl_sync(~0u, sum, warp / W * W);
         if constexpr (EIGHT) {
-            top = __reduce_max_sync(~0u, __float_as_uint(v.y));
-            low = __reduce_max_sync(~0u, __float_as_uint(v.y) == top ? __float_as_uint(v.z) : 0u);
+            top = __reduce_max_sync(~0u, mine ? __float_as_uint(v.y) : 0u);
+            low = __reduce_max_sync(~0u, mine && __float_as_uint(v.y) == top ? __float_as_uint(v.z) : 0u);
         }
+    } else {
+        far = __any_sync(~0u, out_of_range(__fmaf_rn(sum, inv_k, eps)));
     }
+    return far;
+}
+
+// 1 / sqrt(mean + eps) of a row whose sum is out of range, from the sum of squares times f^2: 2^-80 where squares are too large, 2^90
+// where they are too small.
+__device__ __forceinline__ float far_factor(float sum, float inv_k, float eps)
+{
+    return __fmaf_rn(sum, inv_k, eps) < 1.f ? 1.2379401e27f : 8.2718061e-25f;
+}
+__device__ __forceinline__ float far_rstd(float sum, float f, float inv_k, float eps)
+{
+    const float mean = __fmaf_rn(sum, inv_k, eps * f * f);
+    // (a row of zeros with eps = 0: 0, so that its outputs are)
+    const float r = mean == 0.f ? 0.f : __fdiv_rn(f, __fsqrt_rn(mean));
+    return r > 3.4028235e38f ? 3.4028235e38f : r;            // (NaN stays)
 }
 
 // what a row's reductions give its elements
 struct RowQuant { float rstd, inv, up, s; uint32_t top, low; };      // inv, up: 127 / a, less and more a small part of it
-__device__ __forceinline__ RowQuant row_quant(float sum, uint32_t top, uint32_t low, float inv_k, float eps)
+__device__ __forceinline__ RowQuant row_quant(float rstd, uint32_t top, uint32_t low)
 {
     RowQuant r;
-    r.rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(sum, inv_k, eps)));
+    r.rstd = rstd;
     const float a = __uint_as_float(top);
     // (bits above those of infinity: NaN)
     const bool bad = top >= 0x7F800000u, none = a < 1.5046328e-36f;      // 2^-119: 127 / a is finite
@@ -315,18 +341,19 @@ __device__ __forceinline__ void write_output(const FwdParams &p, int64_t at, flo
 // single elements of a row a thread takes (14 at most)
 template <int TPR, bool ALIGNED> struct Singles { static constexpr int N = ALIGNED ? 0 : TPR >= 16 ? 1 : 2; };
 
-// Blocks an SM that rows in 8 bits are given registers for.  (Left to the compiler the path of exact codes takes 90 to 125
-// for rows of one vector a thread: 16384 x 1024 in bf16 29.3 us, 27.4 with three blocks of 256; with four it spills, 29.0.)
-__host__ __device__ constexpr int fwd_blocks(int size, int tpr, int items, bool eight)
+// Blocks an SM that are given registers for: what the usual path needs.  (Left to the compiler the paths of exact codes and of
+// rows out of range take more, for rows of one vector a thread: 16384 x 1024 in bf16 to 8 bits 29.3 us, 27.4 with three
+// blocks of 256; with four it spills, 29.0.)
+__host__ __device__ constexpr int fwd_blocks(int size, int tpr, int items, bool aligned, bool eight)
 {
-    if (!eight) return 1;
-    if (items == 2) return 512 / block_of(tpr);
-    return tpr >= 512 ? (size == 2 ? 1024 : 512) / block_of(tpr) + (tpr == 1024 && size == 4) : 3;
+    if (items == 2) return eight ? 512 / block_of(tpr) : 1;
+    if (tpr >= 512) return (size == 2 || !eight ? 1024 : 512) / block_of(tpr) + (tpr == 1024 && size == 4 && eight);
+    return size == 2 && aligned && !eight ? 4 : 3;
 }
 
 // TPR threads a row, ITEMS vectors of eight a thread
 template <class T, int TPR, int ITEMS, bool ALIGNED, bool EIGHT>
-__global__ void __launch_bounds__(block_of(TPR), fwd_blocks(sizeof(T), TPR, ITEMS, EIGHT)) rmsnorm_fwd_kernel(const FwdParams p)
+__global__ void __launch_bounds__(block_of(TPR), fwd_blocks(sizeof(T), TPR, ITEMS, ALIGNED, EIGHT)) rmsnorm_fwd_kernel(const FwdParams p)
 {
     constexpr int RPB = block_of(TPR) / TPR, ONES = Singles<TPR, ALIGNED>::N, SLOTS = ONES ? ONES : 1;
     __shared__ float4 red[2][block_of(TPR) / 32];
@@ -411,8 +438,23 @@ __global__ void __launch_bounds__(block_of(TPR), fwd_blocks(sizeof(T), TPR, ITEM
             else each(std::true_type());
             low = ordered(most);
         }
-        reduce_row_low<TPR, EIGHT>(sum, top, low, red[buf]);
-        const RowQuant r = row_quant(sum, top, low, p.inv_k, p.eps);
+        const bool far = reduce_row_low<TPR, EIGHT>(sum, top, low, red[buf], p.inv_k, p.eps);
+        float rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(sum, p.inv_k, p.eps)));
+        if (far) {                // (rows in range beside one that is not keep theirs)
+            const float f = far_factor(sum, p.inv_k, p.eps);
+            float again = 0.f;
+#pragma unroll
+            for (int i = 0; i < ITEMS; ++i)
+#pragma unroll
+                for (int k = 0; k < 8; ++k) again = __fmaf_rn(h[i][k] * f, h[i][k] * f, again);
+#pragma unroll
+            for (int i = 0; i < ONES; ++i) again = __fmaf_rn(one[i] * f, one[i] * f, again);
+            if (TPR > 32) __syncthreads();                   // red[buf] has been read
+            uint32_t none = 0, none2 = 0;
+            reduce_row_low<TPR, false>(again, none, none2, red[buf], 1.f, 1.f);
+            if (out_of_range(__fmaf_rn(sum, p.inv_k, p.eps))) rstd = far_rstd(again, f, p.inv_k, p.eps);
+        }
+        const RowQuant r = row_quant(rstd, top, low);
         if (row < p.M) {
 #pragma unroll
             for (int i = 0; i < ITEMS; ++i) {
@@ -491,7 +533,21 @@ __global__ void __launch_bounds__(1024, 2) rmsnorm_fwd_long_kernel(const FwdPara
             low = lows[buf];
             if (threadIdx.x == 0) lows[buf ^ 1] = 0;
         }
-        const RowQuant r = row_quant(sum, top, low, p.inv_k, p.eps);
+        float rstd = __fdiv_rn(1.f, __fsqrt_rn(__fmaf_rn(sum, p.inv_k, p.eps)));
+        if (out_of_range(__fmaf_rn(sum, p.inv_k, p.eps))) {
+            const float f = far_factor(sum, p.inv_k, p.eps);
+            float again = single ? h1[0] * f * (h1[0] * f) : 0.f;
+            for (int v = threadIdx.x; v < cut.nv; v += 1024) {
+                value(v, h, w);
+#pragma unroll
+                for (int k = 0; k < 8; ++k) again = __fmaf_rn(h[k] * f, h[k] * f, again);
+            }
+            __syncthreads();                                 // red[buf] has been read
+            uint32_t none = 0;
+            reduce_row<1024>(again, none, red[buf]);
+            rstd = far_rstd(again, f, p.inv_k, p.eps);
+        }
+        const RowQuant r = row_quant(rstd, top, low);
         for (int v = threadIdx.x; v < cut.nv; v += 1024) {
             value(v, h, w);
             write_outputs<T, EIGHT>(p, at + 8 * v, h, w, r);
