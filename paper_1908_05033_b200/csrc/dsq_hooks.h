@@ -2,8 +2,9 @@
  * dsq_hooks.h - process-wide tuning and test hooks of the tensor-core kernels.
  * Not part of the public interface (include/dsq.h): profiling tools and the
  * test-suite use them to force a tiling or a pipeline, or to make a bounded
- * wait run out.  Each hook sets one atomic integer that later dsq_conv2d /
- * dsq_gemm calls read; results never depend on the tuning hooks.
+ * wait run out.  Each hook sets one atomic integer that later calls
+ * read.  Results never depend on the tuning hooks, but for the order in which
+ * dsq_wgemm_bf16 and dsq_wgemm_group add in binary32.
  */
 #ifndef DSQ_HOOKS_H_
 #define DSQ_HOOKS_H_
@@ -54,8 +55,8 @@ int dsq_set_conv3_expanded_weights(int on);
  * size (dsq_gemm_workspace_bytes answers accordingly). */
 int dsq_set_gemm_two_pass(int on);
 
-/* dsq_wgemm_group: 0 = the faster kernel (default), 1 = always the 16-bit mma.sync one, 2 = always
- * the tcgen05 one, 3 = always the one of 8-bit digits. */
+/* dsq_wgemm_group: 0 = the faster kernel (default), 1 = always the mma.sync one on the rows as they are, 2 =
+ * always the tcgen05 one, 3 = the one of 8-bit digits wherever it applies (one or two rows of 16 bits; else 1). */
 int dsq_set_wgemm_group_form(int form);
 
 /* Test hook: in every later launch the thread that issues the TMA copies of
@@ -65,7 +66,10 @@ int dsq_set_wgemm_group_form(int form);
  * records DSQ_ERR_TIMEOUT in the workspace, every role leaves its loop,
  * copies and MMAs already in flight are allowed to finish, tensor memory is
  * freed and the kernel returns.  Nothing faults and nothing waits longer
- * than the limit; the outputs of such a launch are undefined. */
+ * than the limit; the outputs of such a launch are undefined.
+ * dsq_wgemm_group's tcgen05 kernel, which has no workspace: the copying warp leaves out the stage
+ * (codes and rows of two chunks) `round` of its block and goes on with those behind it as their
+ * places come free; where a block has that stage, all outputs of its cluster are NaN. */
 int dsq_set_test_skip_b_round(int round);
 
 #ifdef __cplusplus

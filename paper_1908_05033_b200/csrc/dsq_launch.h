@@ -23,6 +23,7 @@ struct DsqLaunchHooks {
     int skip_b_round;           // test hook, -1 = off
     int window3;                // dsq_set_conv3_window
     int w8;                     // dsq_set_conv3_expanded_weights
+    int group_form;             // dsq_set_wgemm_group_form
 };
 DSQ_HIDDEN DsqLaunchHooks dsq_launch_hooks();
 // a number that changes whenever a hook is set

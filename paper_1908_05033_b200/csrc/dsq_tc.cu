@@ -1446,6 +1446,7 @@ std::atomic<unsigned long long> g_wait_ns{WAIT_LIMIT_NS};   // dsq_set_wait_limi
 std::atomic<int> g_skip_b_round{-1};  // dsq_set_test_skip_b_round
 std::atomic<int> g_window3{1};        // dsq_set_conv3_window
 std::atomic<int> g_two_pass{1};       // dsq_set_gemm_two_pass
+std::atomic<int> g_group_form{0};     // dsq_set_wgemm_group_form
 std::atomic<int> g_w8{1};             // dsq_set_conv3_expanded_weights
 std::atomic<unsigned> g_generation{0}; // moves with every change of a hook
 
@@ -1599,6 +1600,7 @@ DsqLaunchHooks dsq_launch_hooks()
     h.pdl = g_pdl.load();
     h.wait_ns = g_wait_ns.load();
     h.skip_b_round = g_skip_b_round.load();
+    h.group_form = g_group_form.load();
     h.window3 = g_window3.load();
     h.w8 = g_w8.load();
     return h;
@@ -1733,6 +1735,14 @@ int dsq_set_gemm_two_pass(int on)
 {
     if (on < 0 || on > 2) return DSQ_ERR_SHAPE;
     g_two_pass = on;
+    ++g_generation;
+    return DSQ_OK;
+}
+
+int dsq_set_wgemm_group_form(int form)
+{
+    if (form < 0 || form > 3) return DSQ_ERR_SHAPE;
+    g_group_form = form;
     ++g_generation;
     return DSQ_OK;
 }

@@ -314,15 +314,6 @@ double estimate_us(const DsqGroupGemm &p, bool i8)
 
 }  // namespace
 
-static std::atomic<int> dsq_group_form{0};
-
-extern "C" int dsq_set_wgemm_group_form(int form)
-{
-    if (form < 0 || form > 3) return DSQ_ERR_SHAPE;
-    dsq_group_form.store(form);
-    return DSQ_OK;
-}
-
 extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale, const void *W_codes,
                                const float *scales, const float *bias, int64_t M, int64_t N, int64_t K,
                                int bits, int64_t group, float w_offset, int y_type, void *Y, void *stream)
@@ -357,7 +348,7 @@ extern "C" int dsq_wgemm_group(const void *X, int x_type, const float *row_scale
     p.odd = w_offset == 0.5f;
     p.y_type = y_type;
     cudaStream_t s = (cudaStream_t)stream;
-    int form = dsq_group_form.load(std::memory_order_relaxed);
+    int form = dsq_launch_hooks().group_form;
     if (form == 3 && (x_type == DSQ_I8 || M > 2)) form = 1;
     if (form == 0 && x_type != DSQ_I8 && M <= 2) form = 3;
     if (form == 0) {
