@@ -559,10 +559,12 @@ PyObject *quantize_groups(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
-// sizes of codes and scales (sizes that the library refuses are left to it)
+// sizes of codes and scales (sizes that the library refuses are left to it): matrices as they are laid out, or flat
 void check_codes(const at::Tensor &codes, const at::Tensor &scales, int64_t N, int64_t K, int bits, int64_t group)
 {
     if (N <= 0 || K <= 0 || group <= 0) return;
+    want(bits != 4 || codes.dim() != 2 || codes.size(1) == (int64_t)dsq_row_pitch(K, bits), "codes: want [N, row pitch]");
+    want(scales.dim() != 2 || scales.size(1) == N, "scales: want [groups, N]");
     want(codes.numel() / N >= (int64_t)dsq_row_pitch(K, bits), "codes: too few bytes");
     want(scales.numel() / N >= dsq_group_count(K, group), "scales: too few values");
 }
