@@ -6,8 +6,8 @@
 //   gives the sum of squares and a together.  Codes are exact for the h and w that binary32
 //   holds: a code on the wrong side of a border changes every output of the product behind it.
 //   The reductions bring what the rounding of a lost as well, and elements next to a border
-//   are decided with what theirs lost (8192 x 4096 in bf16: 2 % of the time; shorter and
-//   unaligned rows, where instructions bind, up to a quarter: 16384 x 1024 23.7 -> 29.9 us).
+//   are decided with what theirs lost (nothing at 8192 x 4096 in bf16, where memory
+//   binds; of shorter and unaligned rows, where instructions do, up to a quarter: 16384 x 1024 23.7 -> 29.9 us).
 //   backward, with g = grad_y w and n = h rstd:
 //   grad_x = rstd (g - n mean_k(g n)) + grad_h,  grad_w = sum_m grad_y n
 //
@@ -16,7 +16,7 @@
 // a tiny eps, take a second reduction of the row times a power of two.
 //
 // Bound: memory (bf16: 8 bytes an element forward with residual, 8 backward): 8192 x 4096 in bf16 takes
-// 47.4 us forward with fake-quantised output (0.87 of the copy's rate) and 49 backward (0.84; 45 without
+// 44.4 us forward with fake-quantised output (0.93 of the copy's rate) and 49 backward (0.84; 45 without
 // grad_w, whose sums over the blocks are a kernel of their own).  A row stays in
 // registers between its reduction and its outputs, so every input is read once; the next
 // row of the same threads is on its way meanwhile.  Rows whose length is no multiple of
@@ -343,10 +343,11 @@ template <int TPR, bool ALIGNED> struct Singles { static constexpr int N = ALIGN
 
 // Blocks an SM that are given registers for: what the usual path needs.  (Left to the compiler the paths of exact codes and of
 // rows out of range take more, for rows of one vector a thread: 16384 x 1024 in bf16 to 8 bits 29.3 us, 27.4 with three
-// blocks of 256; with four it spills, 29.0.)
+// blocks of 256; with four it spills, 29.0.  Of two vectors: 8192 x 4096 47.4 with two blocks, 44.4 with three; rows of 2048, which
+// spill then, 25.3 and 36.5.)
 __host__ __device__ constexpr int fwd_blocks(int size, int tpr, int items, bool aligned, bool eight)
 {
-    if (items == 2) return eight ? 512 / block_of(tpr) : 1;
+    if (items == 2) return !eight ? 1 : size == 2 && tpr == 256 ? 3 : 512 / block_of(tpr);
     if (tpr >= 512) return (size == 2 || !eight ? 1024 : 512) / block_of(tpr) + (tpr == 1024 && size == 4 && eight);
     return size == 2 && aligned && !eight ? 4 : 3;
 }
