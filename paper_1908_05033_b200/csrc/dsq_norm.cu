@@ -803,8 +803,8 @@ __global__ void __launch_bounds__(1024) rmsnorm_bwd_long_kernel(const BwdParams 
     if (single) part[single_of(cut, threadIdx.x)] = gw1;
 }
 
-// grad_w[k] = sum over the blocks of their sums, in one order: a warp every 32nd row of sums, eight of
-// its loads on their way together
+// grad_w[k] = sum over the blocks of their sums, in one order: 16 threads a row of sums, 64 rows at a time, eight
+// loads of a thread on their way together
 constexpr int SUM_ROWS = 64, SUM_COLS = 16;
 __global__ void __launch_bounds__(SUM_COLS * SUM_ROWS) weight_sum_kernel(const float *part, int rows, int K, float *out)
 {

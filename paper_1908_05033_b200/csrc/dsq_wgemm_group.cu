@@ -5,9 +5,9 @@
 //
 // Three kernels: one or two rows of 16 bits as digits of 8 (dsq_wgemm_group_few.cu); this one, on
 // mma.sync, where there is little work; tcgen05 where there is more (dsq_wgemm_group_tc.cu), by
-// their estimated times.  (us of this one and of tcgen05: bf16, 8 rows, 4096 x 4096 6.0 and 8.0,
-// 8192 x 8192 16.5 and 16.2; 64 rows 18 and 10.4, 64 and 20; int8, 8 rows, 8192 x 8192 10.2 and 13.4,
-// 32 rows 22 and 15.7.)
+// their estimated times.  (us of this one and of tcgen05: bf16, 8 rows, 4096 x 4096 5.9 and 7.9,
+// 8192 x 8192 16.0 and 15.4; 64 rows 18 and 10.4, 64 and 20; int8, 8 rows, 8192 x 8192 9.8 and 12.9,
+// 32 rows 21.5 and 15.0.)
 //
 // Here the codes are read once and used once: a warp takes them from global memory to tensor-core
 // operands in registers, with one launch's latency and no hand-over between warps but at the

@@ -22,8 +22,9 @@
 //   * The warps' totals, and then the digits' ones, are added in a fixed order.
 //
 // One row of bf16, us (at the copy's rate the codes and scales take): 4096 x 4096 4.8 (1.4), 8192 x 8192
-// 10.6 (5.5), 16384 x 8192 19.5 (11.1); with three digits, which lost what lies 2^-22 below a chunk's largest, 4.7,
-// 10.1 and 18.6.  Bound: latency of 16 warps an SM.  Registers and shared memory allow two blocks; a third stage leaves room
+// 10.6 (5.5), 16384 x 8192 19.4 (11.1), launches in a row with the weights from HBM; from L2 0.4 to 1.2 less, a launch by itself
+// behind a flush of L2 22.5 at 16384 x 8192.  With three digits, which lost what lies 2^-22 below a chunk's largest, 4.7,
+// 10.1 and 18.6.  Two rows of 8192 x 8192 12.2.  Bound: latency of 16 warps an SM (issue slots 54 %, memory 39 %).  Registers and shared memory allow two blocks; a third stage leaves room
 // for one, and fewer or more columns or warps were slower (three digits, 8192 x 8192: three stages with one block 12.3, two or
 // eight words of columns 11.8 and 11.7, 16 warps 13.0).
 #include "dsq_groups.h"

@@ -7,7 +7,7 @@
 // values and to one of those that read its sums of a group back and add them, times the group's
 // scale, to its totals in binary32.  An instruction of 128 x 16 x 16 does for 16 rows what 16 x 8
 // mma.sync tiles do with 16 times the operands' traffic through registers: at 8192 x 8192 with bf16
-// rows mma.sync takes 16.5 us for 8 rows, 21 for 16, 31 for 32 and 64 for 64.
+// rows mma.sync takes 16.0 us for 8 rows, 21 for 16, 30 for 32 and 64 for 64.
 //
 //   * One warp copies: a stage of the ring is two chunks of 128 codes of 128 rows (whole lines of 128
 //     bytes) and X's elements for them, both by TMA into the 128-byte swizzle; zeros behind the ends.
@@ -27,8 +27,9 @@
 // Bound at 8192 x 8192, 16 rows of bf16 (16.4 us; codes alone 5.3 us at the copy's rate): 3.8 us of
 // launch, set-up and the cluster's sums, 7 for the copies and the roles' signals to one another with no
 // work between them, the rest unpacking and instructions, of which no pipe is full (issue slots 47 %,
-// ALU 44 %, tensor 6 %).  8-bit rows 12.8 us; 64 rows 20.1 and 18.4; groups of 32 instead of 128, 16 rows:
-// 21.7 us, four sums a chunk.
+// ALU 44 %, tensor 6 %).  64 rows 20.2, in 8 bits 18.5; 8 rows 15.4 and 12.9; groups of 32 instead of 128, 16 rows:
+// 21.6 us, four sums a chunk.  (Launches in a row, weights from HBM; from L2 as much.  A launch by itself behind a
+// flush of L2 takes 25 us for 64 rows.)
 //
 // Every wait is bounded; where one runs out the outputs of the cluster are NaN.
 #include <cuda_bf16.h>
@@ -567,9 +568,9 @@ int launch(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
                       h.pdl, split, map_w, map_x, p, split, h.wait_ns, h.skip_b_round);
 }
 
-// Three teams make values (8192 x 8192, 16 rows, us: two 18.5, three 18.0, four 18.3; 64 rows 22.4, 23.1,
-// 24.4).  Two take sums in turn where places allow (groups of 32, one row 25.0 -> 22.0); with 64 rows two
-// share the columns instead, for the registers.
+// Three teams make values (8192 x 8192, us, two and three: 16 rows 17.0 and 16.4, 64 rows 20.5 and 20.2).  Two take sums in
+// turn where places allow (groups of 32, 8 rows, one and two: 24.8 and 20.6); with 64 rows two share the columns
+// instead, for the registers.
 template <int XT, int GP> int pick(const DsqGroupGemm &p, cudaStream_t s, double *est_us)
 {
     constexpr bool INT = XT == DSQ_I8;
