@@ -351,9 +351,10 @@ int dsq_dequantize_groups(const void *codes, const float *scales, int64_t N,
  * X v are exact, and added in sums of up to 128 codes of a group: by the tensor core in binary32
  * with three rows of 16 bits or more, exactly with DSQ_I8 (groups of up to 2^16 weights:
  * DSQ_ERR_OVERFLOW beyond) and with one or two rows.  Those sums are added, times their group's
- * scale, in binary32 in a fixed order: the same call gives the same bits on the same GPU.  Y is rounded once.  A row with an
- * infinity or a NaN gives what such terms give, or NaN; other rows do not see it.  Device-side waits
- * are bounded: outputs that one is given up for are NaN (there is no workspace to hold a status). */
+ * scale, in binary32 in a fixed order: the same call gives the same bits on the same GPU.  Y is
+ * rounded once.  A row with an infinity or a NaN gives what such terms give, or NaN; other rows do
+ * not see it.  Device-side waits are bounded: outputs that one is given up for are NaN (there is no
+ * workspace to hold a status). */
 int dsq_wgemm_group(const void *X, int x_type, const float *row_scale,
                     const void *W_codes, const float *scales, const float *bias,
                     int64_t M, int64_t N, int64_t K, int bits, int64_t group,

@@ -10,8 +10,9 @@
 // rows of the instruction, whose other rows would be empty anyway.  An element of bf16 (fp16) is
 // whole down to 2^-22 (2^-19) of the largest of its 256.  Where one is not, what the digits leave
 // of it goes through the same again, on a grid of its own, until nothing is left: whatever stands
-// beside an element, its product is exact, as in the kernels for more rows.  (256 normal elements with
-// one 12 times as large take the second time in 2 chunks of a thousand, with one of 2^10 in 5 of a hundred.)
+// beside an element, its product is exact, as in the kernels for more rows.  (Of chunks of normal elements with
+// one 12 times as large 3 in ten thousand take a second time, with one of 2^10 3 in a hundred, of 2^14 41: 8192 x 8192 with
+// such an element in every chunk 10.7, 11.3 and 13.9 us.)
 // Sums of up to 128 codes are exact in int32; they enter the totals times the group's scale and the
 // power of two in binary32.
 //
@@ -22,11 +23,12 @@
 //   * The warps' totals, and then the digits' ones, are added in a fixed order.
 //
 // One row of bf16, us (at the copy's rate the codes and scales take): 4096 x 4096 4.8 (1.4), 8192 x 8192
-// 10.6 (5.5), 16384 x 8192 19.4 (11.1), launches in a row with the weights from HBM; from L2 0.4 to 1.2 less, a launch by itself
-// behind a flush of L2 22.5 at 16384 x 8192.  With three digits, which lost what lies 2^-22 below a chunk's largest, 4.7,
-// 10.1 and 18.6.  Two rows of 8192 x 8192 12.2.  Bound: latency of 16 warps an SM (issue slots 54 %, memory 39 %).  Registers and shared memory allow two blocks; a third stage leaves room
-// for one, and fewer or more columns or warps were slower (three digits, 8192 x 8192: three stages with one block 12.3, two or
-// eight words of columns 11.8 and 11.7, 16 warps 13.0).
+// 10.6 (5.5), 16384 x 8192 19.4 (11.1), launches in a row with the weights from HBM; from L2 0.4 to 1.2
+// less, a launch by itself behind a flush of L2 22.5 at 16384 x 8192.  Two rows of 8192 x 8192 12.2.  (With three
+// digits, which lost what lies 2^-22 below a chunk's largest, one row 4.7, 10.1 and 18.6.)  Bound: latency of 16
+// warps an SM (issue slots 54 %, memory 39 %).  Registers and shared memory allow two blocks; a third stage
+// leaves room for one, and fewer or more columns or warps were slower (three digits, 8192 x 8192: three stages
+// with one block 12.3, two or eight words of columns 11.8 and 11.7, 16 warps 13.0).
 #include "dsq_groups.h"
 #include "dsq_ptx.cuh"
 #include "dsq_tc_host.h"
