@@ -407,6 +407,65 @@ int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h,
                     int dtype, void *grad_x, float *grad_weight, void *workspace,
                     size_t ws_bytes, void *stream);
 
+/* ---- norms of queries' and keys' heads, with the position rotation --------- */
+
+/* Positions of tokens and what they turn.  Of a head of head_dim elements the first rot_dim are
+ * pairs (i, i + rot_dim / 2) or, interleaved, (2 i, 2 i + 1); pair i turns by the angle
+ * positions[axis[i]][token] inv_freq[i].
+ *   positions  int64 [axes][tokens] (one position a token, or one for time, height and width ...)
+ *   inv_freq   fp32 [rot_dim / 2]
+ *   axis       uint8 [rot_dim / 2], below axes (a pair with another one is NaN); NULL: all 0
+ * Angles are formed and reduced in binary64, cosines and sines are binary32. */
+typedef struct dsq_rotary_t {
+    const int64_t *positions;
+    const float *inv_freq;
+    const uint8_t *axis;
+    int32_t head_dim, rot_dim, axes, interleaved;
+} dsq_rotary_t;
+
+/* Heads [tokens][heads][head_dim] with strides in elements (of the token and of the head; the
+ * elements of a head lie side by side): a part of a row of q, k and v is one. */
+typedef struct dsq_heads_t {
+    const void *x;
+    void *y;                  /* may be the buffer of x, with its strides */
+    const float *weight;      /* fp32 [head_dim], or NULL: ones */
+    int64_t heads, x_token, x_head, y_token, y_head;
+} dsq_heads_t;
+
+/* For every head of q and of k (NULL: q alone), in one launch:
+ *   n = x rstd weight,  rstd = 1 / sqrt(mean(x^2) + eps)     (norm = 0: n = x, no weight)
+ *   y = n with its pairs (n1, n2) turned: (n1 cos - n2 sin, n2 cos + n1 sin)
+ * Types DSQ_F32, DSQ_BF16, DSQ_F16, the same for q and k; arithmetic is binary32, outputs are rounded
+ * once.  A head whose squares leave binary32's range is normalised in binary64; one of zeros with
+ * eps = 0 gives zeros; a NaN or an infinity stays in its head.  Data need the alignment of their
+ * elements only (this and the next function; 16 bytes and strides that are multiples of 16 bytes
+ * are the fast case).  head_dim even, at most 512; heads at most 4096 (DSQ_ERR_SIZE); heads of y that
+ * overlap: DSQ_ERR_SHAPE; weight with norm = 0, odd head_dim: DSQ_ERR_UNSUPPORTED.  HBM-bound. */
+int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
+                     const dsq_rotary_t *rotary, int norm, float eps, int dtype,
+                     void *stream);
+
+/* Back-propagation through it: with g = grad_y turned back and n = x rstd
+ *   grad_x = rstd (g weight - n mean(g weight n)),  grad_weight = sum over tokens and heads of g n
+ *   x            the forward pass's input (not needed with norm = 0)
+ *   grad_x       may be the buffer of grad_y or of x, with its strides
+ *   grad_weight  fp32 [head_dim] or NULL
+ *   workspace    dsq_headnorm_bwd_workspace_bytes(head_dim) bytes (DSQ_ERR_SIZE otherwise); not
+ *                needed without grad_weight.  Scratch: calls that may overlap must not share it.
+ * Sums are binary32 in a fixed order: the same call gives the same bits on the same GPU. */
+typedef struct dsq_heads_grad_t {
+    const void *grad_y, *x;
+    const float *weight;
+    void *grad_x;
+    float *grad_weight;
+    int64_t heads, gy_token, gy_head, x_token, x_head, gx_token, gx_head;
+} dsq_heads_grad_t;
+
+size_t dsq_headnorm_bwd_workspace_bytes(int64_t head_dim);
+int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64_t tokens,
+                     const dsq_rotary_t *rotary, int norm, float eps, int dtype,
+                     void *workspace, size_t ws_bytes, void *stream);
+
 /* dsq_gemm for callers that cannot allocate device memory.  (The paper has
  * no counterpart: this is a deployment convenience of the library.)
  *

@@ -61,6 +61,23 @@ class dsq_epilogue_t(C.Structure):
                 ("residual_q", dsq_quant_t), ("requant", dsq_quant_t)]
 
 
+class dsq_rotary_t(C.Structure):
+    _fields_ = [("positions", C.c_void_p), ("inv_freq", C.c_void_p), ("axis", C.c_void_p),
+                ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("axes", C.c_int32),
+                ("interleaved", C.c_int32)]
+
+
+class dsq_heads_t(C.Structure):
+    _fields_ = [("x", C.c_void_p), ("y", C.c_void_p), ("weight", C.c_void_p)] + [
+        (n, C.c_int64) for n in ("heads", "x_token", "x_head", "y_token", "y_head")]
+
+
+class dsq_heads_grad_t(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("grad_y", "x", "weight", "grad_x", "grad_weight")] + [
+        (n, C.c_int64) for n in ("heads", "gy_token", "gy_head", "x_token", "x_head", "gx_token",
+                                 "gx_head")]
+
+
 _vp, _i64, _int, _sz = C.c_void_p, C.c_int64, C.c_int, C.c_size_t
 _SIGNATURES = {
     "dsq_row_pitch": (_sz, [_i64, _int]),
@@ -98,6 +115,11 @@ _SIGNATURES = {
                                _vp]),
     "dsq_rmsnorm_bwd_workspace_bytes": (_sz, [_i64, _i64]),
     "dsq_rmsnorm_bwd": (_int, [_vp, _vp, _vp, _vp, _vp, _i64, _i64, _int, _vp, _vp, _vp, _sz, _vp]),
+    "dsq_headnorm_fwd": (_int, [C.POINTER(dsq_heads_t), C.POINTER(dsq_heads_t), _i64,
+                                C.POINTER(dsq_rotary_t), _int, C.c_float, _int, _vp]),
+    "dsq_headnorm_bwd_workspace_bytes": (_sz, [_i64]),
+    "dsq_headnorm_bwd": (_int, [C.POINTER(dsq_heads_grad_t), C.POINTER(dsq_heads_grad_t), _i64,
+                                C.POINTER(dsq_rotary_t), _int, C.c_float, _int, _vp, _sz, _vp]),
     "dsq_gemm_static_ws": (_int, [_vp, _vp, _i64, _i64, _i64, _int, _vp, _vp, _vp,
                                   _int, _vp]),
     "dsq_maxpool2x2": (_int, [_vp, C.POINTER(dsq_nhwc_t), _int, _vp, _sz,
@@ -387,6 +409,29 @@ def dsq_rmsnorm_bwd_workspace_bytes(M, K):
 def dsq_rmsnorm_bwd(grad_y, h, weight, rstd, grad_h=None, want_weight=True, ws=None):
     """Returns (grad_x like grad_y, grad_weight fp32 [K] | None)."""
     return _host.rmsnorm_bwd(grad_y, h, weight, rstd, grad_h, want_weight, ws)
+
+
+# ---- heads of queries and keys -------------------------------------------------------
+def dsq_headnorm_fwd(q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6, norm=True,
+                     axis=None, interleaved=False, out_q=None, out_k=None):
+    """q [tokens, heads, head_dim], k likewise or None (fp32, bf16 or fp16; any strides of tokens and
+    heads): each head normalised (norm=False: not) and its first 2 * len(inv_freq) elements rotated.
+    positions: int64 [tokens] or [axes, tokens]; axis: uint8, the axis of each pair.  Returns (q, k | None);
+    out_q and out_k may be q and k themselves."""
+    return _host.headnorm_fwd(q, k, positions, inv_freq, q_weight, k_weight, eps, norm, axis,
+                              interleaved, out_q, out_k)
+
+
+def dsq_headnorm_bwd_workspace_bytes(head_dim):
+    return int(lib.dsq_headnorm_bwd_workspace_bytes(head_dim))
+
+
+def dsq_headnorm_bwd(grad_q, grad_k, q, k, positions, inv_freq, q_weight=None, k_weight=None, eps=1e-6,
+                     norm=True, axis=None, interleaved=False, want_weight=True, ws=None):
+    """Returns (grad_q, grad_k | None, grad_q_weight | None, grad_k_weight | None): gradients of the
+    inputs of dsq_headnorm_fwd, fp32 ones of the weights that are given."""
+    return _host.headnorm_bwd(grad_q, grad_k, q, k, positions, inv_freq, q_weight, k_weight, eps, norm,
+                              axis, interleaved, want_weight, ws)
 
 
 def dsq_set_round_k_steps(ks):

@@ -14,6 +14,7 @@
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <algorithm>
 #include <cstring>
 #include <memory>
 #include <string>
@@ -630,6 +631,139 @@ PyObject *wgemm_group(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// heads [tokens, heads, head_dim] of a floating type, the elements of a head side by side
+const at::Tensor &need_heads(PyObject *o, const char *name)
+{
+    static const char *const types = "torch.float32, torch.bfloat16 or torch.float16";
+    if (!THPVariable_Check(o)) fail_type(name, types);
+    const at::Tensor &v = THPVariable_Unpack(o);
+    const int t = type_code(v.scalar_type());
+    if (!v.is_cuda() || t < 0 || t == DSQ_I8 || (v.dim() == 3 && v.size(2) > 1 && v.stride(2) != 1)) {
+        PyErr_Format(PyExc_TypeError, "%s: want a CUDA tensor of %s whose last dimension is contiguous", name, types);
+        throw PyFailed();
+    }
+    want(v.dim() == 3, "want [tokens, heads, head_dim]");
+    return v;
+}
+
+// the same, like `x`
+const at::Tensor &heads_like(PyObject *o, const at::Tensor &x, const OnDevice &on, const char *name)
+{
+    const at::Tensor &t = on(need_heads(o, name), name);
+    want(t.scalar_type() == x.scalar_type() && t.sizes() == x.sizes(), "want tensors of one type and shape");
+    return t;
+}
+
+// (positions, inv_freq, axis | None, interleaved) beside heads `x`
+dsq_rotary_t as_rotary(PyObject *pos, PyObject *freq, PyObject *axis, PyObject *interleaved, const at::Tensor &x,
+                       const OnDevice &on)
+{
+    dsq_rotary_t r = {};
+    if (!THPVariable_Check(pos) || !THPVariable_Unpack(pos).is_cuda() || !THPVariable_Unpack(pos).is_contiguous() ||
+        THPVariable_Unpack(pos).scalar_type() != at::kLong)
+        fail_type("positions", "torch.int64");
+    const at::Tensor &p = on(THPVariable_Unpack(pos), "positions"), &f = on(need(freq, at::kFloat, "inv_freq"), "inv_freq");
+    want((p.dim() == 1 || p.dim() == 2) && p.size(p.dim() - 1) == x.size(0), "positions: want [tokens] or [axes, tokens]");
+    want(x.size(2) <= 1 << 20 && 2 * f.numel() <= x.size(2), "inv_freq: want one value a rotated pair");
+    r.positions = (const int64_t *)p.data_ptr();
+    r.inv_freq = (const float *)f.data_ptr();
+    r.head_dim = (int32_t)x.size(2);
+    r.rot_dim = (int32_t)(2 * f.numel());
+    r.axes = p.dim() == 2 ? (int32_t)std::min<int64_t>(p.size(0), 1 << 20) : 1;
+    r.interleaved = as_bool(interleaved);
+    if (axis != Py_None) {
+        const at::Tensor &a = on(need(axis, at::kByte, "axis"), "axis");
+        want(a.numel() == f.numel(), "axis: want one value a rotated pair");
+        r.axis = (const uint8_t *)a.data_ptr();
+    }
+    return r;
+}
+
+const float *head_weight(PyObject *o, const at::Tensor &x, const OnDevice &on, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor &w = on(need(o, at::kFloat, name), name);
+    want(w.numel() == x.size(2), "weight: want one value an element of a head");
+    return (const float *)w.data_ptr();
+}
+
+// (q, k | None, positions, inv_freq, q_weight | None, k_weight | None, eps, norm, axis | None, interleaved,
+// out_q | None, out_k | None) -> (q, k | None)
+PyObject *headnorm_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 12, [&]() -> PyObject * {
+        const at::Tensor &q = need_heads(a[0], "q");
+        const OnDevice on(q);
+        const dsq_rotary_t r = as_rotary(a[2], a[3], a[8], a[9], q, on);
+        const float eps = as_float(a[6]);
+        const bool norm = as_bool(a[7]);
+        const at::Tensor *in[2] = {&q, nullptr};
+        at::Tensor out[2];
+        dsq_heads_t h[2] = {};
+        want(a[1] != Py_None || a[11] == Py_None, "out_k: there is no k");
+        for (int i = 0; i < 2; ++i) {
+            if (i && a[1] == Py_None) break;
+            if (i) {
+                const at::Tensor &k = on(need_heads(a[1], "k"), "k");
+                want(k.scalar_type() == q.scalar_type() && k.size(0) == q.size(0) && k.size(2) == q.size(2),
+                     "k: want the type, tokens and head_dim of q");
+                in[1] = &k;
+            }
+            const at::Tensor &x = *in[i];
+            if (a[10 + i] != Py_None) out[i] = heads_like(a[10 + i], x, on, i ? "out_k" : "out_q");
+            else out[i] = new_tensor(x.sizes(), x.scalar_type(), x);
+            h[i] = {x.data_ptr(), out[i].data_ptr(), head_weight(a[4 + i], x, on, i ? "k_weight" : "q_weight"),
+                    x.size(1), x.stride(0), x.stride(1), out[i].stride(0), out[i].stride(1)};
+        }
+        check(enqueue([&](void *s) {
+                  return dsq_headnorm_fwd(&h[0], in[1] ? &h[1] : nullptr, q.size(0), &r, norm, eps,
+                                          type_code(q.scalar_type()), s);
+              }),
+              "dsq_headnorm_fwd");
+        return Py_BuildValue("(NN)", a[10] != Py_None ? Py_NewRef(a[10]) : wrap(out[0]),
+                             a[11] != Py_None ? Py_NewRef(a[11]) : wrap(out[1]));
+    });
+}
+
+// (grad_q, grad_k | None, q, k, positions, inv_freq, q_weight | None, k_weight | None, eps, norm, axis | None,
+// interleaved, want_weight, ws | None) -> (grad_q, grad_k | None, grad_q_weight | None, grad_k_weight | None)
+PyObject *headnorm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 14, [&]() -> PyObject * {
+        const at::Tensor &gq = need_heads(a[0], "grad_q");
+        const OnDevice on(gq);
+        const dsq_rotary_t r = as_rotary(a[4], a[5], a[10], a[11], gq, on);
+        const float eps = as_float(a[8]);
+        const bool norm = as_bool(a[9]), want_weight = as_bool(a[12]);
+        at::Tensor out[2], gw[2], ws;
+        dsq_heads_grad_t h[2] = {};
+        const bool with_k = a[1] != Py_None;
+        for (int i = 0; i < (with_k ? 2 : 1); ++i) {
+            const at::Tensor &g = i ? on(need_heads(a[1], "grad_k"), "grad_k") : gq;
+            want(g.scalar_type() == gq.scalar_type() && g.size(0) == gq.size(0) && g.size(2) == gq.size(2),
+                 "grad_k: want the type, tokens and head_dim of grad_q");
+            const at::Tensor *x = nullptr;
+            if (norm || a[2 + i] != Py_None) x = &heads_like(a[2 + i], g, on, i ? "k" : "q");
+            out[i] = new_tensor(g.sizes(), g.scalar_type(), g);
+            const float *w = head_weight(a[6 + i], g, on, i ? "k_weight" : "q_weight");
+            if (w && want_weight) gw[i] = new_tensor({g.size(2)}, at::kFloat, g);
+            h[i] = {g.data_ptr(), addr(x), w, out[i].data_ptr(), (float *)addr(gw[i]), g.size(1), g.stride(0),
+                    g.stride(1), x ? x->stride(0) : 0, x ? x->stride(1) : 0, out[i].stride(0), out[i].stride(1)};
+        }
+        if (gw[0].defined() || gw[1].defined()) {
+            if (a[13] != Py_None) ws = on(need(a[13], at::kByte, "ws"), "ws");
+            else ws = new_tensor({(int64_t)dsq_headnorm_bwd_workspace_bytes(r.head_dim)}, at::kByte, gq);
+        }
+        check(enqueue([&](void *s) {
+                  return dsq_headnorm_bwd(&h[0], with_k ? &h[1] : nullptr, gq.size(0), &r, norm, eps,
+                                          type_code(gq.scalar_type()), addr(ws),
+                                          ws.defined() ? (size_t)ws.numel() : 0, s);
+              }),
+              "dsq_headnorm_bwd");
+        return Py_BuildValue("(NNNN)", wrap(out[0]), wrap(out[1]), wrap(gw[0]), wrap(gw[1]));
+    });
+}
+
 // ---- recorded call sequences (dsq_plan.h) -----------------------------------
 // What a plan was recorded from: everything a caller could exchange or change in
 // place between two passes (tensors, ranges, layers).  A plan runs only while all
@@ -806,7 +940,7 @@ PyMethodDef g_methods[] = {{"set_error_class", set_error_class, METH_O, nullptr}
                            FAST(quantize_act), FAST(conv2d), FAST(maxpool2x2), FAST(soft_fwd),
                            FAST(soft_bwd), FAST(gemm), FAST(wgemm), FAST(rmsnorm_fwd),
                            FAST(rmsnorm_bwd), FAST(quantize_groups), FAST(dequantize_groups),
-                           FAST(wgemm_group), FAST(plan_record),
+                           FAST(wgemm_group), FAST(headnorm_fwd), FAST(headnorm_bwd), FAST(plan_record),
                            FAST(plan_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dsq_host", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};
