@@ -466,6 +466,78 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
                      const dsq_rotary_t *rotary, int norm, float eps, int dtype,
                      void *workspace, size_t ws_bytes, void *stream);
 
+/* ---- log probabilities of tokens -------------------------------------------- */
+
+/* Of rows of logits [M][V] (row m at logits + m ld elements, ld >= V), z = scale logits:
+ *   lse = log sum_j e^z_j,  logp = z_t - lse,  entropy = -sum_j p_j log p_j,  p_j = e^(z_j - lse)
+ * and the `top` largest of a row in order, equal ones by index, the lowest first.
+ *   dtype     DSQ_F32, DSQ_BF16 or DSQ_F16
+ *   targets   int64 [M] (needed for logp): a negative one is none (logp 0), one of V or more gives NaN
+ *   scale     positive and finite (an inverse temperature), DSQ_ERR_RANGE otherwise
+ *   top       0 to 32 (DSQ_ERR_UNSUPPORTED beyond) and at most V; 0 just where top_ids and top_logp
+ *             are NULL (DSQ_ERR_SHAPE)
+ *   logp, entropy, lse  fp32 [M], top_ids int64 [M][top], top_logp fp32 [M][top]: any may be NULL
+ * Logits of -infinity are masked: they have no probability and add nothing.  A row of nothing else has
+ * lse -infinity, entropy 0 and log probabilities -infinity.  A NaN or +infinity makes its row's numbers
+ * NaN; top_ids takes NaN to be below all.  Arithmetic is binary32.  Data need the alignment of their
+ * elements only (this and the next function).  V at most 2^30, M at most 2^28 (DSQ_ERR_SIZE).
+ * HBM-bound: the logits are read once. */
+int dsq_logprob_fwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dtype,
+                    const int64_t *targets, float scale, int top, float *logp,
+                    float *entropy, float *lse, int64_t *top_ids, float *top_logp,
+                    void *stream);
+
+/* Back-propagation of gradients of logp (grad_logp fp32 [M] or NULL) and of the entropy (grad_entropy
+ * fp32 [M] or NULL; entropy is needed with it), with lse and entropy as the forward pass leaves them:
+ *   grad_logits_j = scale (grad_logp ([j = t] - p_j) - grad_entropy p_j (log p_j + entropy))
+ * grad_logits [M][V] of `dtype`, rows grad_ld elements apart; may be the buffer of logits where ld is the same.
+ * A row whose gradients are both 0 (a negative target has none of logp), or whose logits are all masked,
+ * gets zeros whatever its logits; a target of V or more with a gradient makes its row NaN.  HBM-bound. */
+int dsq_logprob_bwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dtype,
+                    const int64_t *targets, float scale, const float *lse,
+                    const float *entropy, const float *grad_logp,
+                    const float *grad_entropy, void *grad_logits, int64_t grad_ld,
+                    void *stream);
+
+/* ---- a layer of experts for few tokens ---------------------------------------- */
+
+/* The router's choice: of each row of logits fp32 [T][E] the k largest, in order (equal ones by index, the
+ * lowest first; NaN below all), and their weights: with `renormalise` the softmax over the chosen,
+ * without it the probabilities that the softmax over all E gives them.
+ *   ids int32 [T][k], weights fp32 [T][k]
+ * E at most 2^20, k at most 32 (DSQ_ERR_SIZE) and E (DSQ_ERR_SHAPE).  Logits of -infinity are masked: weight 0;
+ * in a row of nothing else all weights are 0.  A NaN or +infinity among those summed makes a row's weights NaN. */
+int dsq_moe_route(const float *logits, int64_t T, int64_t E, int k, int renormalise,
+                  int32_t *ids, float *weights, void *stream);
+
+/* activations of the gate */
+typedef enum dsq_activation { DSQ_SILU = 0, DSQ_GELU_TANH = 1 } dsq_activation;
+
+/* The chosen experts' layers on weights with group scales:
+ *   mid = act(x W_gate[e]^T) * (x W_up[e]^T),   Y_t = residual_t + sum_s weights[t][s] mid_ts W_out[e]^T
+ * with e = ids[t][s], act(g) = g / (1 + e^-g) or g (1 + tanh(sqrt(2/pi) (g + 0.044715 g^3))) / 2.
+ *   X         [T][H] of x_type: DSQ_BF16 or DSQ_F16 (H a multiple of 8, DSQ_ERR_ALIGN otherwise)
+ *   ids       int32 [T][k]: an id outside 0 .. E - 1 adds nothing; one that comes twice counts twice
+ *   weights   fp32 [T][k]
+ *   W_in      codes and scales as dsq_quantize_groups leaves them of the matrix [E 2 I][H]: of each expert
+ *             the I rows of its gate, then the I rows of its other half; scales fp32 [groups][E 2 I]
+ *   W_out     the same of the matrix [E H][I]
+ *   bits, group, w_offset  as in dsq_wgemm_group
+ *   residual  [T][H] of y_type, or NULL;  Y [T][H] of y_type: DSQ_F32, DSQ_BF16 or DSQ_F16 (may be the residual)
+ *   workspace dsq_moe_workspace_bytes(T, I, k) bytes (DSQ_ERR_SIZE otherwise).  Scratch: calls that may
+ *             overlap must not share it.
+ * Made for few tokens: up to 64 share a pass over the weights of the experts they chose; more take several.
+ * Sums are binary32 in a fixed order: the same call gives the same bits on the same GPU; mid is kept to
+ * 16 bits of mantissa; Y is rounded once.  A token with a NaN or an infinity does not touch the others.
+ * k at most 32, E at most 1024, H and I at most 2^20, T at most 2^20 (DSQ_ERR_SIZE). */
+size_t dsq_moe_workspace_bytes(int64_t T, int64_t I, int k);
+int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *weights,
+                  const void *W_in, const float *scales_in, const void *W_out,
+                  const float *scales_out, int64_t T, int64_t H, int64_t I, int64_t E,
+                  int k, int bits, int64_t group, float w_offset, int activation,
+                  const void *residual, int y_type, void *Y, void *workspace,
+                  size_t ws_bytes, void *stream);
+
 /* dsq_gemm for callers that cannot allocate device memory.  (The paper has
  * no counterpart: this is a deployment convenience of the library.)
  *

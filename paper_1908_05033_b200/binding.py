@@ -120,6 +120,14 @@ _SIGNATURES = {
     "dsq_headnorm_bwd_workspace_bytes": (_sz, [_i64]),
     "dsq_headnorm_bwd": (_int, [C.POINTER(dsq_heads_grad_t), C.POINTER(dsq_heads_grad_t), _i64,
                                 C.POINTER(dsq_rotary_t), _int, C.c_float, _int, _vp, _sz, _vp]),
+    "dsq_logprob_fwd": (_int, [_vp, _i64, _i64, _i64, _int, _vp, C.c_float, _int, _vp, _vp, _vp, _vp, _vp,
+                               _vp]),
+    "dsq_logprob_bwd": (_int, [_vp, _i64, _i64, _i64, _int, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp, _i64,
+                               _vp]),
+    "dsq_moe_route": (_int, [_vp, _i64, _i64, _int, _int, _vp, _vp, _vp]),
+    "dsq_moe_workspace_bytes": (_sz, [_i64, _i64, _int]),
+    "dsq_moe_group": (_int, [_vp, _int] + [_vp] * 6 + [_i64] * 4 + [_int, _int, _i64, C.c_float, _int, _vp, _int,
+                             _vp, _vp, _sz, _vp]),
     "dsq_gemm_static_ws": (_int, [_vp, _vp, _i64, _i64, _i64, _int, _vp, _vp, _vp,
                                   _int, _vp]),
     "dsq_maxpool2x2": (_int, [_vp, C.POINTER(dsq_nhwc_t), _int, _vp, _sz,
@@ -432,6 +440,47 @@ def dsq_headnorm_bwd(grad_q, grad_k, q, k, positions, inv_freq, q_weight=None, k
     inputs of dsq_headnorm_fwd, fp32 ones of the weights that are given."""
     return _host.headnorm_bwd(grad_q, grad_k, q, k, positions, inv_freq, q_weight, k_weight, eps, norm,
                               axis, interleaved, want_weight, ws)
+
+
+# ---- log probabilities of tokens -------------------------------------------------------
+def dsq_logprob_fwd(logits, targets=None, scale=1.0, top=0, want_entropy=True):
+    """logits [rows, vocabulary] (fp32, bf16 or fp16; rows may lie further apart), targets int64 [rows] or
+    None.  Returns (logp | None, entropy | None, lse, top_ids int64 [rows, top] | None, top_logp | None)
+    of the softmax of scale * logits; numbers are fp32."""
+    return _host.logprob_fwd(logits, targets, scale, top, want_entropy)
+
+
+def dsq_logprob_bwd(logits, targets, lse, grad_logp, entropy=None, grad_entropy=None, scale=1.0, out=None):
+    """The gradient of the logits (like them; `out` may be the logits themselves)."""
+    return _host.logprob_bwd(logits, targets, lse, grad_logp, entropy, grad_entropy, scale, out)
+
+
+# ---- a layer of experts ------------------------------------------------------------------
+_ACTIVATIONS = {"silu": 0, "gelu_tanh": 1}                            # dsq_activation
+
+
+def dsq_moe_route(logits, k, renormalise=True):
+    """logits fp32 [tokens, experts] -> (ids int32 [tokens, k], weights fp32 [tokens, k])."""
+    return _host.moe_route(logits, k, renormalise)
+
+
+def dsq_moe_workspace_bytes(T, I, k):
+    return int(lib.dsq_moe_workspace_bytes(T, I, k))
+
+
+def dsq_moe_group(X, ids, weights, W_in, scales_in, W_out, scales_out, experts, width, bits=4, group=128,
+                  activation="silu", w_offset=0.5, residual=None, out_dtype=None, out=None, ws=None):
+    """X: bf16 or fp16 [tokens, hidden]; ids int32 and weights fp32 [tokens, k]; W_in, scales_in: codes and
+    group scales of [experts * 2 * width, hidden] (of each expert its gate's rows, then the others), W_out,
+    scales_out of [experts * hidden, width], as dsq_quantize_groups leaves them.  Returns residual + the
+    experts' weighted sum, of out_dtype (X's where not given)."""
+    if out is not None:
+        out_dtype = out.dtype
+    if activation not in _ACTIVATIONS:
+        raise ValueError(f"activation: want one of {sorted(_ACTIVATIONS)}")
+    return _host.moe_group(X, ids, weights, W_in, scales_in, W_out, scales_out, experts, width, bits, group,
+                           _ACTIVATIONS[activation], w_offset, residual,
+                           -1 if out_dtype is None else _DTYPES.get(out_dtype, 99), out, ws)
 
 
 def dsq_set_round_k_steps(ks):

@@ -764,6 +764,174 @@ PyObject *headnorm_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
     });
 }
 
+// rows of logits [rows, vocabulary], the elements of a row side by side
+const at::Tensor &need_logits(PyObject *o, const char *name)
+{
+    static const char *const types = "torch.float32, torch.bfloat16 or torch.float16";
+    if (!THPVariable_Check(o)) fail_type(name, types);
+    const at::Tensor &v = THPVariable_Unpack(o);
+    const int t = type_code(v.scalar_type());
+    if (!v.is_cuda() || t < 0 || t == DSQ_I8 || (v.dim() == 2 && v.size(1) > 1 && v.stride(1) != 1)) {
+        PyErr_Format(PyExc_TypeError, "%s: want a CUDA tensor of %s whose last dimension is contiguous", name, types);
+        throw PyFailed();
+    }
+    want(v.dim() == 2, "want [rows, vocabulary]");
+    return v;
+}
+
+int64_t row_stride(const at::Tensor &v) { return v.size(0) > 1 ? v.stride(0) : v.size(1); }
+
+// one value a row, or None
+const at::Tensor *a_row_each(PyObject *o, at::ScalarType t, const at::Tensor &rows, const OnDevice &on, const char *name)
+{
+    if (o == Py_None) return nullptr;
+    if (!THPVariable_Check(o) || !THPVariable_Unpack(o).is_cuda() || THPVariable_Unpack(o).scalar_type() != t ||
+        !THPVariable_Unpack(o).is_contiguous())
+        fail_type(name, t == at::kLong ? "torch.int64" : dtype_name(t));
+    const at::Tensor &v = on(THPVariable_Unpack(o), name);
+    if (v.numel() != rows.size(0)) {
+        PyErr_Format(PyExc_ValueError, "%s: want one value a row", name);
+        throw PyFailed();
+    }
+    return &v;
+}
+
+// (logits, targets | None, scale, top, want_entropy) -> (logp | None, entropy | None, lse, top_ids | None, top_logp | None)
+PyObject *logprob_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 5, [&]() -> PyObject * {
+        const at::Tensor &x = need_logits(a[0], "logits");
+        const OnDevice on(x);
+        const at::Tensor *targets = a_row_each(a[1], at::kLong, x, on, "targets");
+        const float scale = as_float(a[2]);
+        const int64_t top = as_int(a[3]), M = x.size(0);
+        want(top >= 0 && top <= 1 << 20, "top: want a number of alternatives");
+        at::Tensor logp, entropy, lse = new_tensor({M}, at::kFloat, x), ids, top_logp;
+        if (targets) logp = new_tensor({M}, at::kFloat, x);
+        if (as_bool(a[4])) entropy = new_tensor({M}, at::kFloat, x);
+        if (top > 0) {
+            ids = new_tensor({M, top}, at::kLong, x);
+            top_logp = new_tensor({M, top}, at::kFloat, x);
+        }
+        check(enqueue([&](void *s) {
+                  return dsq_logprob_fwd(x.data_ptr(), row_stride(x), M, x.size(1), type_code(x.scalar_type()),
+                                         (const int64_t *)addr(targets), scale, (int)top, (float *)addr(logp),
+                                         (float *)addr(entropy), (float *)addr(lse), (int64_t *)addr(ids),
+                                         (float *)addr(top_logp), s);
+              }),
+              "dsq_logprob_fwd");
+        return Py_BuildValue("(NNNNN)", wrap(logp), wrap(entropy), wrap(lse), wrap(ids), wrap(top_logp));
+    });
+}
+
+// (logits, targets | None, lse, grad_logp | None, entropy | None, grad_entropy | None, scale, out | None) -> grad_logits
+PyObject *logprob_bwd(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 8, [&]() -> PyObject * {
+        const at::Tensor &x = need_logits(a[0], "logits");
+        const OnDevice on(x);
+        const at::Tensor *targets = a_row_each(a[1], at::kLong, x, on, "targets");
+        const at::Tensor *lse = a_row_each(a[2], at::kFloat, x, on, "lse"), *g = a_row_each(a[3], at::kFloat, x, on, "grad_logp");
+        const at::Tensor *h = a_row_each(a[4], at::kFloat, x, on, "entropy");
+        const at::Tensor *gh = a_row_each(a[5], at::kFloat, x, on, "grad_entropy");
+        const float scale = as_float(a[6]);
+        at::Tensor out;
+        if (a[7] != Py_None) {
+            out = on(need_logits(a[7], "out"), "out");
+            want(out.scalar_type() == x.scalar_type() && out.sizes() == x.sizes(), "out: want the type and shape of logits");
+        } else {
+            out = new_tensor(x.sizes(), x.scalar_type(), x);
+        }
+        check(enqueue([&](void *s) {
+                  return dsq_logprob_bwd(x.data_ptr(), row_stride(x), x.size(0), x.size(1), type_code(x.scalar_type()),
+                                         (const int64_t *)addr(targets), scale, (const float *)addr(lse),
+                                         (const float *)addr(h), (const float *)addr(g), (const float *)addr(gh),
+                                         out.data_ptr(), row_stride(out), s);
+              }),
+              "dsq_logprob_bwd");
+        if (a[7] != Py_None) return Py_NewRef(a[7]);
+        return wrap(out);
+    });
+}
+
+// (logits, k, renormalise) -> (ids, weights)
+PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 3, [&]() -> PyObject * {
+        const at::Tensor &x = need(a[0], at::kFloat, "logits");
+        const OnDevice on(x);
+        want(x.dim() == 2, "logits: want [tokens, experts]");
+        const int64_t k = as_int(a[1]);
+        const bool renormalise = as_bool(a[2]);
+        want(k >= 0 && k <= 1 << 20, "k: want a number of experts");
+        at::Tensor ids = new_tensor({x.size(0), k}, at::kInt, x), weights = new_tensor({x.size(0), k}, at::kFloat, x);
+        check(enqueue([&](void *s) {
+                  return dsq_moe_route((const float *)x.data_ptr(), x.size(0), x.size(1), (int)k, renormalise,
+                                       (int32_t *)ids.data_ptr(), (float *)weights.data_ptr(), s);
+              }),
+              "dsq_moe_route");
+        return Py_BuildValue("(NN)", wrap(ids), wrap(weights));
+    });
+}
+
+// (X, ids, weights, W_in, scales_in, W_out, scales_out, E, I, bits, group, activation, w_offset, residual | None,
+// out type | -1, out | None, ws | None) -> Y
+PyObject *moe_group(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    return guarded(n, 17, [&]() -> PyObject * {
+        static const char *const types = "torch.bfloat16 or torch.float16";
+        if (!THPVariable_Check(a[0])) fail_type("X", types);
+        const at::Tensor &X = THPVariable_Unpack(a[0]);
+        const int xt = type_code(X.scalar_type());
+        if (!X.is_cuda() || !X.is_contiguous() || (xt != DSQ_BF16 && xt != DSQ_F16)) fail_type("X", types);
+        const OnDevice on(X);
+        want(X.dim() == 2, "X: want [tokens, hidden]");
+        const int64_t T = X.size(0), H = X.size(1), E = as_int(a[7]), I = as_int(a[8]), group = as_int(a[10]);
+        const int bits = (int)as_int(a[9]);
+        if (!THPVariable_Check(a[1]) || !THPVariable_Unpack(a[1]).is_cuda() || !THPVariable_Unpack(a[1]).is_contiguous() ||
+            THPVariable_Unpack(a[1]).scalar_type() != at::kInt)
+            fail_type("ids", "torch.int32");
+        const at::Tensor &ids = on(THPVariable_Unpack(a[1]), "ids");
+        const at::Tensor &weights = on(need(a[2], at::kFloat, "weights"), "weights");
+        want(ids.dim() == 2 && ids.size(0) == T && weights.sizes() == ids.sizes(), "ids, weights: want [tokens, k]");
+        const at::Tensor &w_in = on(need(a[3], at::kByte, "W_in"), "W_in"), &s_in = on(need(a[4], at::kFloat, "scales_in"), "scales_in");
+        const at::Tensor &w_out = on(need(a[5], at::kByte, "W_out"), "W_out");
+        const at::Tensor &s_out = on(need(a[6], at::kFloat, "scales_out"), "scales_out");
+        want(E <= 1 << 20 && I <= 1 << 20 && H <= 1 << 20 && ids.size(1) <= 1 << 20, "sizes: too large");
+        if (E > 0 && I > 0) {
+            check_codes(w_in, s_in, E * 2 * I, H, bits, group);
+            check_codes(w_out, s_out, E * H, I, bits, group);
+        }
+        const float w_offset = as_float(a[12]);
+        const at::ScalarType t = as_int(a[14]) < 0 ? X.scalar_type() : as_type(a[14]);
+        const at::Tensor *residual = nullptr;
+        if (a[13] != Py_None) {
+            residual = &on(need(a[13], t, "residual"), "residual");
+            want(residual->sizes() == X.sizes(), "residual: want the shape of X");
+        }
+        at::Tensor Y, ws;
+        if (a[15] != Py_None) {
+            Y = on(need(a[15], t, "out"), "out");
+            want(Y.sizes() == X.sizes(), "out: want the shape of X");
+        } else {
+            Y = new_tensor(X.sizes(), t, X);
+        }
+        const int k = (int)ids.size(1);
+        if (a[16] != Py_None) ws = on(need(a[16], at::kByte, "ws"), "ws");
+        else ws = new_tensor({(int64_t)dsq_moe_workspace_bytes(T, I, k)}, at::kByte, X);
+        const int act = (int)as_int(a[11]);
+        check(enqueue([&](void *s) {
+                  return dsq_moe_group(X.data_ptr(), xt, (const int32_t *)ids.data_ptr(), (const float *)weights.data_ptr(),
+                                       w_in.data_ptr(), (const float *)s_in.data_ptr(), w_out.data_ptr(),
+                                       (const float *)s_out.data_ptr(), T, H, I, E, k, bits, group, w_offset, act,
+                                       addr(residual), type_code(t), Y.data_ptr(), ws.data_ptr(), (size_t)ws.numel(), s);
+              }),
+              "dsq_moe_group");
+        if (a[15] != Py_None) return Py_NewRef(a[15]);
+        return wrap(Y);
+    });
+}
+
 // ---- recorded call sequences (dsq_plan.h) -----------------------------------
 // What a plan was recorded from: everything a caller could exchange or change in
 // place between two passes (tensors, ranges, layers).  A plan runs only while all
@@ -940,7 +1108,8 @@ PyMethodDef g_methods[] = {{"set_error_class", set_error_class, METH_O, nullptr}
                            FAST(quantize_act), FAST(conv2d), FAST(maxpool2x2), FAST(soft_fwd),
                            FAST(soft_bwd), FAST(gemm), FAST(wgemm), FAST(rmsnorm_fwd),
                            FAST(rmsnorm_bwd), FAST(quantize_groups), FAST(dequantize_groups),
-                           FAST(wgemm_group), FAST(headnorm_fwd), FAST(headnorm_bwd), FAST(plan_record),
+                           FAST(wgemm_group), FAST(headnorm_fwd), FAST(headnorm_bwd), FAST(logprob_fwd),
+                           FAST(logprob_bwd), FAST(moe_route), FAST(moe_group), FAST(plan_record),
                            FAST(plan_run), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "_dsq_host", nullptr, -1, g_methods,
                         nullptr, nullptr, nullptr, nullptr};

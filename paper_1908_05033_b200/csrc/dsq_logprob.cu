@@ -1,0 +1,618 @@
+// Log probabilities of given tokens with entropy and the most probable alternatives of rows of
+// logits, and the logits' gradient (what stands behind a decoder's last product).
+//
+//   z = scale x,  lse = m + log s,  s = sum e^(z - m),  logp = z_t - lse,
+//   H = log s - t / s,  t = sum (z - m) e^(z - m)
+//   grad_j = scale (g ([j = t] - p_j) - g_H p_j (log p_j + H)),  p = e^(z - lse)
+//
+// HBM-bound: the forward kernel reads the logits once, the backward one reads and writes them once.
+//   * Forward: a row goes to a block or, where there are few, to a cluster of up to eight, whose first
+//     block joins the parts.  A thread keeps m, s and t of its elements in one pass; four vectors are
+//     on their way together.
+//   * Alternatives: a thread's m says all there is to know of its elements but their order.  The block's
+//     threads form 128 groups; the top-th of the groups' largest elements bounds from below what can be among the
+//     first `top`, and only threads with an m above the bound read theirs again (from L2) and leave
+//     what passes in shared memory, where ranks are counted.  Order and ties are those of (value, lowest
+//     index), as one 64-bit key.
+#include "dsq_launch.h"
+#include "dsq_ptx.cuh"
+#include "dsq_types.cuh"
+
+using namespace dsq_ptx;
+
+namespace {
+
+constexpr int THREADS = 512, GROUPS = 128, MAX_TOP = 32, MAX_CLUSTER = 8, AHEAD = 4;
+constexpr int ROOM = 1088;        // of candidates: 128 threads' vectors where fewer groups than `top` have any
+constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+// what e^x of a lower power of two is zero
+constexpr float NOTHING = -1000.f;
+
+struct FwdParams {
+    const void *x;
+    const int64_t *targets;
+    float *logp, *entropy, *lse, *top_logp;
+    int64_t *top_ids;
+    int64_t ld;
+    int V, top, cluster;
+    float scale;
+};
+
+struct BwdParams {
+    const void *x;
+    const int64_t *targets;
+    const float *lse, *entropy, *g_logp, *g_entropy;
+    void *grad;
+    int64_t ld, grad_ld;
+    int V, segments;
+    float scale;
+};
+
+__device__ __forceinline__ float ex2(float v)
+{
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(v));
+    return r;
+}
+// (a NaN stays one)
+__device__ __forceinline__ float max_nan(float a, float b)
+{
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+typedef unsigned long long f2;        // two binary32 values
+__device__ __forceinline__ f2 pack2(float a, float b)
+{
+    f2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpack2(f2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f2 add2(f2 a, f2 b)
+{
+    f2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 mul2(f2 a, f2 b)
+{
+    f2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
+{
+    f2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
+template <class T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
+
+__device__ __forceinline__ uint4 load_16(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+template <class T> __device__ __forceinline__ void values(const uint4 &r, float (&f)[vec_of<T>()])
+{
+    if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(r.x); f[1] = __uint_as_float(r.y);
+        f[2] = __uint_as_float(r.z); f[3] = __uint_as_float(r.w);
+    } else {
+        DsqRaw8<T> raw;
+        raw.v[0] = r;
+        dsq_unpack8(raw, f);
+    }
+}
+// -infinity in every place
+template <class T> __device__ __forceinline__ uint4 nothing()
+{
+    const uint32_t w = sizeof(T) == 4 ? 0xFF800000u : std::is_same<T, __half>::value ? 0xFC00FC00u : 0xFF80FF80u;
+    return make_uint4(w, w, w, w);
+}
+// the largest element, NaN left out (of nothing but NaN: NaN)
+template <class T> __device__ __forceinline__ float largest(const uint4 (&r)[AHEAD])
+{
+    if constexpr (sizeof(T) == 4) {
+        float m = __uint_as_float(r[0].x);
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i)
+            m = fmaxf(fmaxf(fmaxf(m, __uint_as_float(r[i].x)), __uint_as_float(r[i].y)),
+                      fmaxf(__uint_as_float(r[i].z), __uint_as_float(r[i].w)));
+        return m;
+    } else {
+        typedef typename std::conditional<std::is_same<T, __half>::value, __half2, __nv_bfloat162>::type T2;
+        const T2 *v = reinterpret_cast<const T2 *>(r);
+        T2 m = v[0];
+#pragma unroll
+        for (int i = 1; i < 4 * AHEAD; ++i) m = __hmax2(m, v[i]);
+        return fmaxf(dsq_to_f32(m.x), dsq_to_f32(m.y));
+    }
+}
+
+// Key of an element: by value, equal ones by index, the lowest first; NaN below all, nothing at all 0.
+__device__ __forceinline__ unsigned long long key_of(float v, int index)
+{
+    const uint32_t u = __float_as_uint(v + 0.f);              // (-0 is 0)
+    uint32_t k = (int)u < 0 ? ~u : u | 0x80000000u;
+    if (v != v) k = 0u;
+    return (unsigned long long)k << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ float value_of(unsigned long long key)
+{
+    const uint32_t k = (uint32_t)(key >> 32);
+    if (k == 0u) return __uint_as_float(0x7FC00000u);
+    return __uint_as_float((int)k < 0 ? k & 0x7FFFFFFFu : ~k);
+}
+__device__ __forceinline__ int index_of(unsigned long long key) { return (int)~(uint32_t)key; }
+
+// sums of elements less m, in powers of two: s, and t of the exponents' products
+struct Sums { float m, s, t; };
+__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
+{
+    Sums r;
+    r.m = fmaxf(a.m, b.m);
+    const float da = max_nan((a.m - r.m) * c, NOTHING), db = max_nan((b.m - r.m) * c, NOTHING);
+    const float ea = ex2(da), eb = ex2(db);
+    r.s = __fmaf_rn(a.s, ea, b.s * eb);
+    r.t = __fmaf_rn(__fmaf_rn(a.s, da, a.t), ea, __fmaf_rn(b.s, db, b.t) * eb);
+    return r;
+}
+
+// Where a row's whole vectors lie: `head` single elements, nv vectors, `tail` single ones.
+template <class T> struct Cut {
+    const T *row;
+    int head, nv, tail;
+    __device__ __forceinline__ Cut(const T *r, int V) : row(r)
+    {
+        head = min(V, (int)((16 - (reinterpret_cast<uintptr_t>(r) & 15)) & 15) / (int)sizeof(T));
+        nv = (V - head) / vec_of<T>();
+        tail = V - head - nv * vec_of<T>();
+    }
+    __device__ __forceinline__ int index(int v) const { return head + v * vec_of<T>(); }
+    __device__ __forceinline__ int single(int i) const { return i < head ? i : i + nv * vec_of<T>(); }
+};
+
+// Ranks of n keys, all different: f(rank, key) for each.
+template <class F> __device__ __forceinline__ void ranked(const unsigned long long *keys, int n, F f)
+{
+    for (int i = threadIdx.x; i < n; i += THREADS) {
+        const unsigned long long mine = keys[i];
+        int rank = 0;
+        for (int j = 0; j < n; ++j) rank += keys[j] > mine;
+        f(rank, mine);
+    }
+}
+
+__device__ __forceinline__ void st_cluster_64(uint32_t addr, unsigned long long v)
+{
+    asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+template <class T, bool TOP>
+__global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_constant__ FwdParams p)
+{
+    constexpr int VEC = vec_of<T>();
+    __shared__ Sums warp_sums[THREADS / 32];
+    __shared__ Sums block_sums[MAX_CLUSTER];
+    __shared__ unsigned long long lists[TOP ? MAX_CLUSTER * MAX_TOP : 1];      // of the first block: all blocks' first `top`
+    __shared__ unsigned long long bests[TOP ? GROUPS : 1], found[TOP ? ROOM : 1], bound_key;
+    __shared__ int count;
+    const int rank = p.cluster > 1 ? (int)cluster_ctarank() : 0;
+    const int64_t row = blockIdx.x / p.cluster;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    // (the first block's shared memory is written from the others once it has started)
+    if (p.cluster > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");
+    const Cut<T> cut((const T *)p.x + row * p.ld, p.V);
+    const int v0 = (int)((int64_t)cut.nv * rank / p.cluster), v1 = (int)((int64_t)cut.nv * (rank + 1) / p.cluster);
+    const int singles = rank == 0 ? cut.head + cut.tail : 0;
+    const float c = p.scale * LOG2E;
+    const T *vecs = cut.row + cut.head;
+    float wanted = 0.f;                                        // the target's logit
+    int64_t target = -1;
+    if (rank == 0 && tid == 0 && p.logp) {
+        target = p.targets[row];
+        if (target >= 0 && target < p.V) wanted = dsq_to_f32(cut.row[target]);
+    }
+
+    // one pass: m, s, t of this thread's elements, and in which turn m came
+    auto load = [&](int turn, uint4 (&r)[AHEAD]) {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int v = v0 + (turn * AHEAD + j) * THREADS + tid;
+            r[j] = v < v1 ? load_16(vecs + (int64_t)v * VEC) : nothing<T>();
+        }
+    };
+    const int turns = (v1 - v0 + THREADS * AHEAD - 1) / (THREADS * AHEAD);
+    float m = LOWEST;
+    int best_turn = -1;
+    f2 s2 = 0ull, t2 = 0ull;
+    const f2 c2 = pack2(c, c);
+    uint4 next[AHEAD];
+    if (turns > 0) load(0, next);
+#pragma unroll 1
+    for (int turn = 0; turn < turns; ++turn) {
+        uint4 r[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) r[j] = next[j];
+        if (turn + 1 < turns) load(turn + 1, next);
+        const float most = largest<T>(r);
+        if (TOP && best_turn < 0 && v0 + turn * AHEAD * THREADS + tid < v1) best_turn = turn;     // (lowest or less: the first turn)
+        if (most > m) {
+            const float d = max_nan((m - most) * c, NOTHING), e = ex2(d);
+            const f2 e2 = pack2(e, e);
+            t2 = mul2(fma2(s2, pack2(d, d), t2), e2);
+            s2 = mul2(s2, e2);
+            m = most;
+            best_turn = turn;
+        }
+        const f2 less = pack2(-m, -m);
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            float f[VEC];
+            values<T>(r[j], f);
+#pragma unroll
+            for (int i = 0; i < VEC; i += 2) {
+                const f2 d = mul2(add2(pack2(f[i], f[i + 1]), less), c2);
+                float d0, d1;
+                unpack2(d, d0, d1);
+                d0 = max_nan(d0, NOTHING);
+                d1 = max_nan(d1, NOTHING);
+                const f2 e = pack2(ex2(d0), ex2(d1));
+                s2 = add2(s2, e);
+                t2 = fma2(pack2(d0, d1), e, t2);
+            }
+        }
+    }
+    Sums sum;
+    {
+        float a, b;
+        unpack2(s2, a, b);
+        sum.s = a + b;
+        unpack2(t2, a, b);
+        sum.t = a + b;
+        sum.m = m;
+    }
+    if (tid < singles) {
+        const float v = dsq_to_f32(cut.row[cut.single(tid)]);
+        // (-infinity and NaN as in the loop: less LOWEST nothing, and NaN)
+        Sums one = {fmaxf(v, LOWEST), 1.f, 0.f};
+        const float d = max_nan((v - one.m) * c, NOTHING);
+        one.s = ex2(d);
+        one.t = d * one.s;
+        sum = joined(sum, one, c);
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+        const Sums other = {__shfl_xor_sync(~0u, sum.m, o), __shfl_xor_sync(~0u, sum.s, o), __shfl_xor_sync(~0u, sum.t, o)};
+        // (the lower lane's first, so that both lanes have the same)
+        sum = lane & o ? joined(other, sum, c) : joined(sum, other, c);
+    }
+    if (lane == 0) warp_sums[warp] = sum;
+    if (TOP) {
+        if (tid == 0) {
+            count = 0;
+            bound_key = 0ull;
+        }
+        // the largest of a group, its index no lower than it is
+        unsigned long long best = 0ull;
+        if (best_turn >= 0) {
+            const int first = v0 + best_turn * AHEAD * THREADS + tid, last = first + min(AHEAD - 1, (v1 - 1 - first) / THREADS) * THREADS;
+            // (m is LOWEST where all are -infinity, NaN or LOWEST: below them all, then, but above what is not there)
+            best = m > LOWEST ? key_of(m, cut.index(last) + VEC - 1) : (unsigned long long)(uint32_t)~(cut.index(last) + VEC - 1);
+        }
+#pragma unroll
+        for (int o = 1; o < THREADS / GROUPS; o <<= 1) {
+            const unsigned long long other = __shfl_xor_sync(~0u, best, o);
+            best = best > other ? best : other;
+        }
+        if (tid % (THREADS / GROUPS) == 0) bests[tid / (THREADS / GROUPS)] = best;
+        __syncthreads();
+        // the `top`-th of them
+        {
+            constexpr int SHARE = THREADS / GROUPS;
+            int above = 0;
+#pragma unroll 4
+            for (int j = tid % SHARE; j < GROUPS; j += SHARE) above += bests[j] > best;
+#pragma unroll
+            for (int o = 1; o < SHARE; o <<= 1) above += __shfl_xor_sync(~0u, above, o);
+            if (tid % SHARE == 0 && above == p.top - 1 && best != 0ull) bound_key = best;
+        }
+        __syncthreads();
+        const unsigned long long bound = bound_key;
+        auto keep = [&](float v, int index) {
+            const unsigned long long key = key_of(v, index);
+            if (key < bound) return;
+            const int at = atomicAdd(&count, 1);
+            if (at < ROOM) found[at] = key;
+        };
+        if (tid < singles) keep(dsq_to_f32(cut.row[cut.single(tid)]), cut.single(tid));
+        const bool some = best_turn >= 0 && (m > LOWEST ? key_of(m, cut.index(v0 + best_turn * AHEAD * THREADS + tid)) >= bound
+                                                        : true);
+        if (some && (m > LOWEST || key_of(LOWEST, 0) >= bound)) {
+#pragma unroll 1
+            for (int turn = 0; turn < turns; ++turn) {
+                uint4 r[AHEAD];
+                load(turn, r);
+                if (bound >> 32 && !(largest<T>(r) >= value_of(bound))) continue;
+#pragma unroll 1
+                for (int j = 0; j < AHEAD; ++j) {
+                    const int v = v0 + (turn * AHEAD + j) * THREADS + tid;
+                    if (v >= v1) break;
+                    float f[VEC];
+                    values<T>(r[j], f);
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) keep(f[i], cut.index(v) + i);
+                }
+            }
+        }
+    }
+    __syncthreads();
+    if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (tid < 32) {
+        Sums all = warp_sums[tid & (THREADS / 32 - 1)];
+        for (int o = THREADS / 64; o > 0; o >>= 1) {
+            const Sums other = {__shfl_xor_sync(~0u, all.m, o), __shfl_xor_sync(~0u, all.s, o), __shfl_xor_sync(~0u, all.t, o)};
+            all = lane & o ? joined(other, all, c) : joined(all, other, c);
+        }
+        if (tid == 0) {
+            if (p.cluster == 1) block_sums[0] = all;
+            else {
+                const uint32_t at = map_to_cta(smem_u32(&block_sums[rank]), 0);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at), "f"(all.m) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 4), "f"(all.s) : "memory");
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(at + 8), "f"(all.t) : "memory");
+            }
+        }
+    }
+    if (TOP) {
+        const uint32_t list = p.cluster == 1 ? smem_u32(lists) : map_to_cta(smem_u32(lists + rank * p.top), 0);
+        auto put = [&](int at, unsigned long long key) {
+            if (p.cluster == 1) lists[at] = key;
+            else st_cluster_64(list + 8 * at, key);
+        };
+        const int n = count;
+        // (fewer than `top`: the rest of the list is nothing)
+        for (int i = tid; i < p.top; i += THREADS)
+            if (i >= n) put(i, 0ull);
+        if (n <= ROOM) {
+            ranked(found, n, [&](int at, unsigned long long key) {
+                if (at < p.top) put(at, key);
+            });
+        } else {
+            // More than there is room for (many large elements, and all with the same few threads): one after
+            // the other, the largest below the one before.
+            unsigned long long last = ~0ull;
+            for (int i = 0; i < p.top; ++i) {
+                unsigned long long best = 0ull;
+                auto take = [&](float v, int index) {
+                    const unsigned long long key = key_of(v, index);
+                    if (key < last && key > best) best = key;
+                };
+                if (tid < singles) take(dsq_to_f32(cut.row[cut.single(tid)]), cut.single(tid));
+#pragma unroll 1
+                for (int v = v0 + tid; v < v1; v += THREADS) {
+                    float f[VEC];
+                    values<T>(load_16(vecs + (int64_t)v * VEC), f);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) take(f[e], cut.index(v) + e);
+                }
+                for (int o = 16; o > 0; o >>= 1) {
+                    const unsigned long long other = __shfl_xor_sync(~0u, best, o);
+                    best = best > other ? best : other;
+                }
+                __syncthreads();
+                if (lane == 0) bests[warp] = best;
+                __syncthreads();
+                for (int w = 0; w < THREADS / 32; ++w) best = best > bests[w] ? best : bests[w];
+                if (tid == 0) put(i, best);
+                last = best;
+            }
+        }
+    }
+    if (p.cluster > 1) cluster_sync_all();
+    else __syncthreads();
+    if (rank != 0) return;
+    Sums all = block_sums[0];
+    for (int i = 1; i < p.cluster; ++i) all = joined(all, block_sums[i], c);
+    const float log_s = logf(all.s);
+    // (a row without any: everything is improbable, and there is nothing to be uncertain about)
+    const bool empty = all.s == 0.f;
+    const float none = __uint_as_float(0xFF800000u), nan = __uint_as_float(0x7FC00000u);
+    auto logp_of = [&](float v) { return empty ? none : (v - all.m) * p.scale - log_s; };
+    if (tid == 0) {
+        if (p.logp) p.logp[row] = target < 0 ? 0.f : target >= p.V ? nan : logp_of(wanted);
+        if (p.entropy) {
+            const float h = log_s - all.t * LN2 / all.s;
+            p.entropy[row] = empty || h < 0.f ? 0.f : h;
+        }
+        if (p.lse) p.lse[row] = empty ? none : __fmaf_rn(all.m, p.scale, log_s);
+    }
+    if (TOP)
+        ranked(lists, p.cluster * p.top, [&](int at, unsigned long long key) {
+            if (at >= p.top || key == 0ull) return;
+            if (p.top_ids) p.top_ids[row * p.top + at] = index_of(key);
+            if (p.top_logp) p.top_logp[row * p.top + at] = logp_of(value_of(key));
+        });
+}
+
+constexpr int BWD_THREADS = 256, BWD_AHEAD = 2;
+template <class T> constexpr int bwd_segment() { return BWD_THREADS * BWD_AHEAD * vec_of<T>() * 4; }   // elements, four turns
+
+// SAME: logits and gradients lie alike in their vectors
+template <class T, bool SAME>
+__global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_kernel(const __grid_constant__ BwdParams p)
+{
+    constexpr int VEC = vec_of<T>();
+    const int64_t row = blockIdx.x / p.segments;
+    const int segment = (int)(blockIdx.x - row * p.segments);
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const T *x = (const T *)p.x + row * p.ld;
+    T *grad = (T *)p.grad + row * p.grad_ld;
+    const int64_t target = p.targets ? p.targets[row] : -1;
+    float g = p.g_logp && target >= 0 ? p.g_logp[row] : 0.f;
+    const float ge = p.g_entropy ? p.g_entropy[row] : 0.f;
+    if (g != 0.f && target >= p.V) g = __uint_as_float(0x7FC00000u);
+    const float lse = p.lse[row], h = p.entropy ? p.entropy[row] : 0.f;
+    // rows that nothing comes back to, and rows without any probability
+    const int at_target = target >= 0 && target < p.V ? (int)target : -1;
+    const bool zero = (g == 0.f && ge == 0.f) || lse == __uint_as_float(0xFF800000u);
+    const float a = g * p.scale, b = ge * p.scale;
+    // -p (a + b (log p + H)) of z = scale x
+    auto of = [&](float v) {
+        const float l = __fmaf_rn(v, p.scale, -lse), l2 = max_nan(l * LOG2E, NOTHING);
+        return -(ex2(l2) * __fmaf_rn(b, max_nan(l, NOTHING) + h, a));
+    };
+    auto one = [&](int i) {
+        float v = 0.f;
+        if (!zero) {
+            v = of(dsq_to_f32(x[i]));
+            if (i == at_target) v += a;
+        }
+        grad[i] = dsq_from_f32<T>(v);
+    };
+    if constexpr (!SAME) {
+        const int from = segment * bwd_segment<T>(), to = min(p.V, from + bwd_segment<T>());
+        for (int i = from + threadIdx.x; i < to; i += BWD_THREADS) one(i);
+    } else {
+        const Cut<T> cut(x, p.V);
+        if (segment == 0 && threadIdx.x < cut.head + cut.tail) one(cut.single(threadIdx.x));
+        constexpr int PER = bwd_segment<T>() / VEC;
+        const int from = segment * PER, to = min(cut.nv, from + PER);
+        const T *xv = x + cut.head;
+        T *gv = grad + cut.head;
+#pragma unroll 1
+        for (int v0 = from + threadIdx.x; v0 < to; v0 += BWD_THREADS * BWD_AHEAD) {
+            uint4 r[BWD_AHEAD];
+#pragma unroll
+            for (int j = 0; j < BWD_AHEAD; ++j)
+                if (!zero && v0 + j * BWD_THREADS < to) r[j] = load_16(xv + (int64_t)(v0 + j * BWD_THREADS) * VEC);
+#pragma unroll
+            for (int j = 0; j < BWD_AHEAD; ++j) {
+                const int v = v0 + j * BWD_THREADS;
+                if (v >= to) break;
+                float f[VEC];
+                values<T>(r[j], f);
+                const int off = at_target - cut.index(v);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    f[i] = of(f[i]);
+                    if (off == i) f[i] += a;
+                    if (zero) f[i] = 0.f;
+                }
+                if constexpr (sizeof(T) == 4)
+                    *reinterpret_cast<float4 *>(gv + (int64_t)v * VEC) = make_float4(f[0], f[1], f[2], f[3]);
+                else {
+                    DsqRaw8<T> out;
+                    dsq_pack8(f, out);
+                    dsq_store8(gv + (int64_t)v * VEC, out);
+                }
+            }
+        }
+    }
+}
+
+// blocks of a row: as many as leave each a turn's work and the SMs no more than one each
+int cluster_of(int64_t M, int64_t V, int vec)
+{
+    const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    int c = 1;
+    while (c < MAX_CLUSTER && M * c * 2 <= sms && V >= (int64_t)THREADS * vec * 2 * c) c *= 2;
+    return c;
+}
+
+template <class T> int fwd_launch(FwdParams &p, int64_t M, cudaStream_t s)
+{
+    p.cluster = cluster_of(M, p.V, vec_of<T>());
+    const auto kernel = p.top > 0 ? logprob_fwd_kernel<T, true> : logprob_fwd_kernel<T, false>;
+    return dsq_launch(kernel, dim3((unsigned)(M * p.cluster)), dim3(THREADS), 0, s, dsq_launch_hooks().pdl, p.cluster, p);
+}
+
+template <class T> int bwd_launch(BwdParams &p, int64_t M, cudaStream_t s)
+{
+    const uintptr_t x = (uintptr_t)p.x, g = (uintptr_t)p.grad;
+    const bool same = (x & 15) == (g & 15) && (p.ld - p.grad_ld) % vec_of<T>() == 0;
+    p.segments = (p.V + bwd_segment<T>() - 1) / bwd_segment<T>();
+    if (M * p.segments > 0x7FFFFFFF) return DSQ_ERR_SIZE;
+    const dim3 grid((unsigned)(M * p.segments));
+    const int pdl = dsq_launch_hooks().pdl;
+    return same ? dsq_launch(logprob_bwd_kernel<T, true>, grid, dim3(BWD_THREADS), 0, s, pdl, 0, p)
+                : dsq_launch(logprob_bwd_kernel<T, false>, grid, dim3(BWD_THREADS), 0, s, pdl, 0, p);
+}
+
+bool aligned_to(const void *p, int size) { return (reinterpret_cast<uintptr_t>(p) & (uintptr_t)(size - 1)) == 0; }
+
+int check_rows(int64_t M, int64_t V, int64_t ld, int dtype, float scale)
+{
+    if (!dsq_is_float_type(dtype)) return DSQ_ERR_UNSUPPORTED;
+    if (M <= 0 || V <= 0 || ld < V) return DSQ_ERR_SHAPE;
+    if (V > 1 << 30 || M > 1 << 28) return DSQ_ERR_SIZE;
+    if (!dsq_finite(scale) || scale <= 0.f) return DSQ_ERR_RANGE;
+    return DSQ_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dsq_logprob_fwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dtype, const int64_t *targets,
+                    float scale, int top, float *logp, float *entropy, float *lse, int64_t *top_ids,
+                    float *top_logp, void *stream)
+{
+    if (!logits || (!logp && !entropy && !lse && !top_ids && !top_logp) || (logp && !targets)) return DSQ_ERR_NULL;
+    const int st = check_rows(M, V, ld, dtype, scale);
+    if (st) return st;
+    if (top < 0 || top > V || (top == 0) != (!top_ids && !top_logp)) return DSQ_ERR_SHAPE;
+    if (top > MAX_TOP) return DSQ_ERR_UNSUPPORTED;
+    if (!aligned_to(logits, dtype == DSQ_F32 ? 4 : 2) || !aligned_to(targets, 8) || !aligned_to(top_ids, 8) ||
+        !aligned_to(logp, 4) || !aligned_to(entropy, 4) || !aligned_to(lse, 4) || !aligned_to(top_logp, 4))
+        return DSQ_ERR_ALIGN;
+    FwdParams p;
+    p.x = logits; p.targets = targets;
+    p.logp = logp; p.entropy = entropy; p.lse = lse; p.top_logp = top_logp; p.top_ids = top_ids;
+    p.ld = ld;
+    p.V = (int)V; p.top = top; p.cluster = 1;
+    p.scale = scale;
+    cudaStream_t s = (cudaStream_t)stream;
+    switch (dtype) {
+    case DSQ_F32: return fwd_launch<float>(p, M, s);
+    case DSQ_BF16: return fwd_launch<__nv_bfloat16>(p, M, s);
+    default: return fwd_launch<__half>(p, M, s);
+    }
+}
+
+int dsq_logprob_bwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dtype, const int64_t *targets,
+                    float scale, const float *lse, const float *entropy, const float *grad_logp,
+                    const float *grad_entropy, void *grad_logits, int64_t grad_ld, void *stream)
+{
+    if (!logits || !lse || !grad_logits || (!grad_logp && !grad_entropy) || (grad_logp && !targets) ||
+        (grad_entropy && !entropy))
+        return DSQ_ERR_NULL;
+    const int st = check_rows(M, V, ld, dtype, scale);
+    if (st) return st;
+    if (grad_ld < V) return DSQ_ERR_SHAPE;
+    const int size = dtype == DSQ_F32 ? 4 : 2;
+    if (!aligned_to(logits, size) || !aligned_to(grad_logits, size) || !aligned_to(targets, 8) || !aligned_to(lse, 4) ||
+        !aligned_to(entropy, 4) || !aligned_to(grad_logp, 4) || !aligned_to(grad_entropy, 4))
+        return DSQ_ERR_ALIGN;
+    BwdParams p;
+    p.x = logits; p.targets = targets;
+    p.lse = lse; p.entropy = entropy; p.g_logp = grad_logp; p.g_entropy = grad_entropy;
+    p.grad = grad_logits;
+    p.ld = ld; p.grad_ld = grad_ld;
+    p.V = (int)V; p.segments = 1;
+    p.scale = scale;
+    cudaStream_t s = (cudaStream_t)stream;
+    switch (dtype) {
+    case DSQ_F32: return bwd_launch<float>(p, M, s);
+    case DSQ_BF16: return bwd_launch<__nv_bfloat16>(p, M, s);
+    default: return bwd_launch<__half>(p, M, s);
+    }
+}
+
+}  // extern "C"
