@@ -24,9 +24,9 @@ def act(g, kind):
 
 
 def layer(x, ids, weights, c_in, s_in, c_out, s_out, E, I, group, kind="silu", w_offset=0.5, residual=None,
-          eps_in=0.0, eps_out=0.0, eps_mid=0.0):
+          eps_in=0.0, eps_out=0.0, eps_mid=0.0, digits=0.0):
     """(y, bound): the bound takes sums of the first products to be off by eps_in of their terms' magnitudes, mid
-    by eps_mid of itself, sums of the second by eps_out.  c_in: codes [E 2 I, H], c_out [E H, I]."""
+    by eps_mid of itself, sums of the second by eps_out, and x and mid by `digits` of the largest element of a row.  c_in: codes [E 2 I, H], c_out [E H, I]."""
     x = np.asarray(x, np.float64)
     T, H = x.shape
     y = np.zeros((T, H)) if residual is None else np.array(residual, np.float64)
@@ -40,10 +40,11 @@ def layer(x, ids, weights, c_in, s_in, c_out, s_out, E, I, group, kind="silu", w
         rows = slice(e * H, (e + 1) * H)
         w2 = groups.values(c_out[rows], s_out[:, rows], group, w_offset)
         for t, s in hit:
-            both, mag = w1 @ x[t], np.abs(w1) @ np.abs(x[t]) * eps_in
+            both, mag = w1 @ x[t], np.abs(w1) @ (np.abs(x[t]) * eps_in + digits * np.abs(x[t]).max())
             g, u = both[:I], both[I:]
             mid = act(g, kind) * u
             off = 1.13 * mag[:I] * (np.abs(u) + mag[I:]) + np.abs(act(g, kind)) * mag[I:] + eps_mid * np.abs(mid)
+            off = off + digits * np.abs(mid).max()
             y[t] += weights[t, s] * (w2 @ mid)
             bound[t] += abs(weights[t, s]) * (np.abs(w2) @ off * (1 + eps_out) + eps_out * (np.abs(w2) @ np.abs(mid)))
     return y, bound

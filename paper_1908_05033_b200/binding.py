@@ -125,7 +125,7 @@ _SIGNATURES = {
     "dsq_logprob_bwd": (_int, [_vp, _i64, _i64, _i64, _int, _vp, C.c_float, _vp, _vp, _vp, _vp, _vp, _i64,
                                _vp]),
     "dsq_moe_route": (_int, [_vp, _i64, _i64, _int, _int, _vp, _vp, _vp]),
-    "dsq_moe_workspace_bytes": (_sz, [_i64, _i64, _int]),
+    "dsq_moe_workspace_bytes": (_sz, [_i64, _i64, _i64, _int]),
     "dsq_moe_group": (_int, [_vp, _int] + [_vp] * 6 + [_i64] * 4 + [_int, _int, _i64, C.c_float, _int, _vp, _int,
                              _vp, _vp, _sz, _vp]),
     "dsq_gemm_static_ws": (_int, [_vp, _vp, _i64, _i64, _i64, _int, _vp, _vp, _vp,
@@ -464,8 +464,8 @@ def dsq_moe_route(logits, k, renormalise=True):
     return _host.moe_route(logits, k, renormalise)
 
 
-def dsq_moe_workspace_bytes(T, I, k):
-    return int(lib.dsq_moe_workspace_bytes(T, I, k))
+def dsq_moe_workspace_bytes(T, H, I, k):
+    return int(lib.dsq_moe_workspace_bytes(T, H, I, k))
 
 
 def dsq_moe_group(X, ids, weights, W_in, scales_in, W_out, scales_out, experts, width, bits=4, group=128,

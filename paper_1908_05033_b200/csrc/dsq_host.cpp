@@ -918,7 +918,7 @@ PyObject *moe_group(PyObject *, PyObject *const *a, Py_ssize_t n)
         }
         const int k = (int)ids.size(1);
         if (a[16] != Py_None) ws = on(need(a[16], at::kByte, "ws"), "ws");
-        else ws = new_tensor({(int64_t)dsq_moe_workspace_bytes(T, I, k)}, at::kByte, X);
+        else ws = new_tensor({(int64_t)dsq_moe_workspace_bytes(T, H, I, k)}, at::kByte, X);
         const int act = (int)as_int(a[11]);
         check(enqueue([&](void *s) {
                   return dsq_moe_group(X.data_ptr(), xt, (const int32_t *)ids.data_ptr(), (const float *)weights.data_ptr(),

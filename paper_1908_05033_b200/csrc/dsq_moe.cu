@@ -3,24 +3,28 @@
 //
 //   mid = act(x W_gate^T) * (x W_up^T),   y_t = residual_t + sum_s weight_ts mid_ts W_out^T
 //
-// Two kernels behind one another, both bound by the bytes of the experts that anything goes to:
-//   * A slot is a token's s-th choice.  Every block sorts the slots by expert (stable, in shared memory) and cuts
-//     each expert's into groups of up to ROWS, the rows of a tensor-core tile.
-//   * moe_in_kernel: a block has 16 columns of a group's gate and the same 16 of its other half; its
-//     warps split K in chunks of 128 codes, each through a ring of stages of its own (cp.async, no
-//     barrier between warps); their sums are added in a fixed order, and the activation makes mid
-//     of them.
-//   * moe_out_kernel: a block (or a cluster, where there are few columns) has 32 columns of all tokens; the
-//     chunks of all groups, one behind the other, are cut evenly among the warps, so that every
-//     block has the same work however the tokens are spread.  A warp adds a group's sums, times the tokens'
-//     weights, to rows of its own in shared memory; at the end the warps' and the cluster's are added in a fixed
-//     order: no atomics, no partial results in memory, no third launch.  Its first weights are on their
-//     way while the kernel ahead still runs.
-//   * Codes become bf16 or fp16 pairs in registers as in dsq_wgemm_group.cu; products are exact and
-//     added in binary32.  mid goes as two bf16 numbers, hi + lo (16 bits of mantissa: bf16 alone would
-//     add as much again to the error as rounding y does), as the upper and lower eight rows of a tile,
-//     which for eight slots costs the tensor core nothing.
-//   * Rows of x and mid come from L2 straight into the operands' registers, a chunk ahead.
+// Bound by the bytes of the experts that anything goes to, read once: 128 bytes of codes that a warp reads
+// may cost it some 18 instructions at 6 TB/s, and unpacking them to bf16 is 12 (dsq_wgemm_group.cu).
+// So everything is 8-bit integers, as in dsq_wgemm_group_few.cu: a word of eight codes takes 3 instructions,
+// a row of x or mid is four signed digits of 8 bits, on a grid of its own for each chunk of 128 elements
+// (2^-30 of the largest's power of two), and four slots' digits are the 16 rows of an instruction.
+//
+//   * A slot is a token's s-th choice.  moe_prepare_kernel sorts the slots by expert (stable), cuts each
+//     expert's into groups of up to eight, and makes digits of x.
+//   * moe_in_kernel: a block has columns of a group's gate and the same ones of its other half; warps
+//     split columns and K in chunks of 128 codes, each through a ring of stages of its own (cp.async,
+//     no barrier between warps); their sums are added in a fixed order, and the activation makes
+//     mid of them, in binary32.  moe_mid_kernel makes digits of it.
+//   * moe_out_kernel: a cluster has columns of all tokens; the chunks of all groups, one behind the
+//     other, are cut evenly among its warps, so that all have the same work however the tokens
+//     are spread.  A warp adds a group's sums, times the tokens' weights, to rows of its own in shared memory;
+//     at the end the warps' and the cluster's are added in a fixed order: no atomics, no partial results in
+//     memory.  Its first codes are on their way while the kernels ahead still run.
+//   * Sums of up to 128 codes are exact in int32; they enter the totals in binary32.  Digits leave of an
+//     element what is below 2^-31 of the largest of its 128: for the codes' grid Delta (c + 1/2),
+//     which has no 0, that is below the rounding of the sums.  For the grid Delta c, whose 0 can make the largest
+//     element vanish, a token that digits are not all of goes through the tensor core as bf16 or fp16 (exact products,
+//     twice the instructions).
 #include "dsq_groups.h"
 #include "dsq_ptx.cuh"
 #include "dsq_tc_host.h"
@@ -31,8 +35,7 @@ using namespace dsq_ptx;
 
 namespace {
 
-constexpr int WARPS = 8, THREADS = WARPS * 32, PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;
-constexpr int MAX_SLOTS = PASS_TOKENS * MAX_TOP;
+constexpr int ROWS = 8, PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;
 
 // ---- the router's choice ---------------------------------------------------------------
 // A warp a token: the largest key among those below the last, k times.  ITEMS logits a lane in
@@ -111,105 +114,191 @@ template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const R
     }
 }
 
-// ---- slots by expert ---------------------------------------------------------------------
+// ---- preparation: slots by expert, digits ---------------------------------------------------
 struct Group {
     int expert, first, n;             // slots first .. first + n - 1 of the sorted ones
 };
-struct Slots {
-    uint16_t sorted[MAX_SLOTS];
-    uint32_t packed[MAX_SLOTS];       // groups: expert | first << 10 | (n - 1) << 22
-    int start[MAX_EXPERTS];           // (counts, then where the next slot of an expert goes)
-    int groups;
-    __device__ __forceinline__ Group group(int i) const
-    {
-        const uint32_t v = packed[i];
-        return {(int)(v & 1023), (int)(v >> 10 & 4095), (int)(v >> 22) + 1};
-    }
+// what lies in the workspace
+struct Work {
+    int *groups;                      // how many
+    uint32_t *packed;                 // groups: expert | first << 10 | (n - 1) << 22
+    uint16_t *sorted;                 // slots by expert
+    uint8_t *lost;                    // [T][chunks_in]: digits are not all of x's chunk
+    float *x_step, *mid_step;         // [T][chunks_in], [slots][chunks_out]: what the lowest digit stands for
+    uint8_t *x_digits, *mid_digits;   // [T][4][128 chunks_in], [slots][4][128 chunks_out], the highest digit first
+    float *mid;                       // [slots][128 chunks_out]
 };
-
-// Sorts the slots whose expert there is; groups of up to `rows`.  All threads; ends with a barrier.
-__device__ __forceinline__ void sort_slots(Slots &s, const int32_t *ids, int n, int E, int rows)
-{
-    const int lane = threadIdx.x & 31;
-    for (int e = threadIdx.x; e < E; e += THREADS) s.start[e] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const int id = ids[i];
-        if (id >= 0 && id < E) atomicAdd(&s.start[id], 1);
-    }
-    __syncthreads();
-    if (threadIdx.x < 32) {
-        int slots = 0, groups = 0;    // so far
-        for (int e0 = 0; e0 < E; e0 += 32) {
-            const int e = e0 + lane, count = e < E ? s.start[e] : 0, parts = (count + rows - 1) / rows;
-            int a = count, b = parts;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int u = __shfl_up_sync(~0u, a, o), v = __shfl_up_sync(~0u, b, o);
-                if (lane >= o) {
-                    a += u;
-                    b += v;
-                }
-            }
-            const int first = slots + a - count, g = groups + b - parts;
-            if (e < E) s.start[e] = first;
-            for (int i = 0; i < parts; ++i)
-                s.packed[g + i] = (uint32_t)e | (uint32_t)(first + i * rows) << 10 | (uint32_t)(min(rows, count - i * rows) - 1) << 22;
-            slots += __shfl_sync(~0u, a, 31);
-            groups += __shfl_sync(~0u, b, 31);
-        }
-        if (lane == 0) s.groups = groups;
-        __syncwarp();
-        for (int i0 = 0; i0 < n; i0 += 32) {
-            int id = i0 + lane < n ? ids[i0 + lane] : -1;
-            if (id < 0 || id >= E) id = -1;
-            const uint32_t same = __match_any_sync(~0u, id);
-            int at = id >= 0 ? s.start[id] : 0;
-            __syncwarp();
-            if (id >= 0) {
-                s.sorted[at + __popc(same & ((1u << lane) - 1))] = (uint16_t)(i0 + lane);
-                if (lane == 31 - __clz(same)) s.start[id] = at + __popc(same);
-            }
-            __syncwarp();
-        }
-    }
-    __syncthreads();
-}
-
-// ---- products ------------------------------------------------------------------------------
 struct MoeParams {
+    Work w;
     const uint8_t *X, *W_in, *W_out;
     const float *s_in, *s_out, *weights;
     const int32_t *ids;
-    uint16_t *mid;                    // hi rows of all slots, then lo rows, of pitch_mid bf16 each
     const void *residual;
     void *Y;
     int T, H, I, E, k, slots;
-    int pitch_in, pitch_out, pitch_mid;      // bytes of a row of codes; elements
+    int pitch_in, pitch_out;                 // bytes of a row of codes
+    int chunks_in, chunks_out;               // of 128 codes in a row
     int groups_in, groups_out;               // scales of a row
     uint32_t units_in, units_in_inv, units_out, units_out_inv;
     int odd, act, y_type;
 };
+__device__ __forceinline__ Group group_at(const Work &w, int i)
+{
+    const uint32_t v = w.packed[i];
+    return {(int)(v & 1023), (int)(v >> 10 & 4095), (int)(v >> 22) + 1};
+}
 
+// Sorts the slots whose expert there is, and cuts them into groups.  A block; `start`: MAX_EXPERTS values.
+__device__ __forceinline__ void sort_slots(const MoeParams &p, int *start)
+{
+    const int lane = threadIdx.x & 31, E = p.E, n = p.slots;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) start[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int id = p.ids[i];
+        if (id >= 0 && id < E) atomicAdd(&start[id], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    int slots = 0, groups = 0;        // so far
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane, count = e < E ? start[e] : 0, parts = (count + ROWS - 1) / ROWS;
+        int a = count, b = parts;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int u = __shfl_up_sync(~0u, a, o), v = __shfl_up_sync(~0u, b, o);
+            if (lane >= o) {
+                a += u;
+                b += v;
+            }
+        }
+        const int first = slots + a - count, g = groups + b - parts;
+        if (e < E) start[e] = first;
+        for (int i = 0; i < parts; ++i)
+            p.w.packed[g + i] = (uint32_t)e | (uint32_t)(first + i * ROWS) << 10 | (uint32_t)(min(ROWS, count - i * ROWS) - 1) << 22;
+        slots += __shfl_sync(~0u, a, 31);
+        groups += __shfl_sync(~0u, b, 31);
+    }
+    if (lane == 0) *p.w.groups = groups;
+    __syncwarp();
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        int id = i0 + lane < n ? p.ids[i0 + lane] : -1;
+        if (id < 0 || id >= E) id = -1;
+        const uint32_t same = __match_any_sync(~0u, id);
+        const int at = id >= 0 ? start[id] : 0;
+        __syncwarp();
+        if (id >= 0) {
+            p.w.sorted[at + __popc(same & ((1u << lane) - 1))] = (uint16_t)(i0 + lane);
+            if (lane == 31 - __clz(same)) start[id] = at + __popc(same);
+        }
+        __syncwarp();
+    }
+}
+
+// The four digits of a chunk of 128 elements, by a warp: f holds elements 4 lane .. 4 lane + 3.  Stored as an instruction's
+// operand wants them: lane j's 32 bytes of a chunk are four words' codes 0, 2, 4, 6, 1, 3, 5, 7, the words being 4 j .. 4 j
+// + 3 where no group's end cuts the chunk (WHOLE), else j, j + 4, j + 8, j + 12.  Returns the step; *lost: something is
+// left of the elements.
+template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (&f)[4], uint8_t *to, int64_t plane, bool *lost)
+{
+    const int lane = threadIdx.x & 31;
+    float most = 0.f;
+    bool bad = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        most = fmaxf(most, fabsf(f[i]));
+        bad = bad || !(fabsf(f[i]) <= 3.402823466e38f);
+    }
+    const uint32_t e = __reduce_max_sync(~0u, __float_as_uint(most) >> 23);
+    // step = 2^(e - 156), 2^-149 at least: the largest is below 2^30 of it
+    const int up = 156 - (int)max(e, 7u), up1 = min(up, 126);
+    const float a = __uint_as_float((uint32_t)(127 + up1) << 23), b = __uint_as_float((uint32_t)(127 + up - up1) << 23);
+    uint32_t v[4];
+    bool rest = false;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float u = f[i] * b * a, w = rintf(u);
+        rest = rest || w != u || (u == 0.f && f[i] != 0.f);
+        v[i] = (uint32_t)__float2int_rn(u) + 0x808080u;
+    }
+    // bytes of elements 0, 2 and 1, 3: the lower three plus 128
+    const int block = lane >> 1, half = lane & 1;
+    const int word = WHOLE ? block : (block & 3) * 4 + (block >> 2);
+    uint8_t *at = to + word * 8 + half * 2;
+#pragma unroll
+    for (int d = 0; d < 4; ++d) {
+        const uint32_t flip = d == 0 ? 0u : 0x8080u;
+        const uint32_t sel = (3 - d) | (7 - d) << 4;
+        *reinterpret_cast<uint16_t *>(at + d * plane) = (uint16_t)(__byte_perm(v[0], v[2], sel) ^ flip);
+        *reinterpret_cast<uint16_t *>(at + d * plane + 4) = (uint16_t)(__byte_perm(v[1], v[3], sel) ^ flip);
+    }
+    *lost = __any_sync(~0u, rest);
+    if (__any_sync(~0u, bad)) return __uint_as_float(0x7FC00000u);
+    return up <= 126 ? __uint_as_float((uint32_t)(127 - up) << 23) : __uint_as_float(1u << (149 - up));
+}
+
+constexpr int PREPARE_WARPS = 8;
+// block 0: the slots; the others' warps a chunk of a token each
+template <int XT, bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_prepare_kernel(const __grid_constant__ MoeParams p)
+{
+    __shared__ int start[MAX_EXPERTS];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (blockIdx.x == 0) {
+        sort_slots(p, start);
+        return;
+    }
+    const int i = (blockIdx.x - 1) * PREPARE_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    if (i >= p.T * p.chunks_in) return;
+    const int t = i / p.chunks_in, c = i - t * p.chunks_in, k = c * 128 + 4 * lane;
+    float f[4] = {};
+    if (k < p.H) {                    // (H is a multiple of 8)
+        const uint2 v = *reinterpret_cast<const uint2 *>(p.X + ((int64_t)t * p.H + k) * 2);
+        const uint32_t w[2] = {v.x, v.y};
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            if (XT == DSQ_BF16) {
+                f[2 * h] = __uint_as_float(w[h] << 16);
+                f[2 * h + 1] = __uint_as_float(w[h] & 0xFFFF0000u);
+            } else {
+                const float2 u = __half22float2(*reinterpret_cast<const __half2 *>(&w[h]));
+                f[2 * h] = u.x;
+                f[2 * h + 1] = u.y;
+            }
+        }
+    }
+    bool lost;
+    const int64_t plane = (int64_t)p.chunks_in * 128;
+    const float step = make_digits<WHOLE>(f, p.w.x_digits + t * 4 * plane + c * 128, plane, &lost);
+    if (lane == 0) {
+        p.w.x_step[i] = step;
+        p.w.lost[i] = lost;
+    }
+}
+
+// mid's digits, a warp a chunk of a slot (of slots without an expert: of whatever lies there)
+template <bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_mid_kernel(const __grid_constant__ MoeParams p)
+{
+    const int i = blockIdx.x * PREPARE_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (i >= p.slots * p.chunks_out) return;
+    const int s = i / p.chunks_out, c = i - s * p.chunks_out;
+    const int64_t plane = (int64_t)p.chunks_out * 128;
+    const float4 v = *reinterpret_cast<const float4 *>(p.w.mid + s * plane + c * 128 + 4 * lane);
+    const float f[4] = {v.x, v.y, v.z, v.w};
+    bool lost;
+    const float step = make_digits<WHOLE>(f, p.w.mid_digits + s * 4 * plane + c * 128, plane, &lost);
+    if (lane == 0) p.w.mid_step[i] = step;
+}
+
+// ---- products ------------------------------------------------------------------------------
 // group of scales of a unit (dsq_wgemm_group.cuh)
 __device__ __forceinline__ int scale_of(uint32_t unit, uint32_t units, uint32_t inv)
 {
     return units == 1 ? (int)unit : (int)__umulhi(unit, inv);
 }
 
-template <int XT> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if (XT == DSQ_BF16)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-            "{%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-            "{%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
@@ -248,62 +337,123 @@ __device__ __forceinline__ void copy_chunk(uint32_t at, const uint8_t *W, int pi
     }
 }
 
-// A lane's rows of a tile's operand: 16 bytes of each of a chunk's four pieces, of rows n and n + 8 of each tile.
-template <int TILES> struct Rows { uint4 x[TILES][2][4]; };
+// ---- digits
+__device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%0, %1, %2, %3};"
+        : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// The same on sums of 1.5 2^23 as binary32 keeps it: a sum below 2^22 (128 codes of 128 at most, digits of 128: 2^21)
+// is then a binary32 number, 1.5 2^23 and itself.
+constexpr float MAGIC = 12582912.f;
+__device__ __forceinline__ void mma_i8_first(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+        "{%8, %9}, {%10, %10, %10, %10};"
+        : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0x4B400000));
+}
 
-// Sums of a chunk: total += scale (sum of x v).  `refill(tile, half, piece)`: what is loaded where a piece was.
-template <int XT, int TILES, int NT, int GP, class Refill>
-__device__ __forceinline__ void multiply(uint32_t at, uint32_t base, Rows<TILES> &r, float (&total)[TILES][NT][4], Refill refill)
+// What a lane has of a chunk's rows: row n (and n + 8) of a tile is digit n & 3 of its slot n / 4 (and 2 + n / 4); 32 bytes
+// of each, and the slots' steps.
+template <int TILES> struct Digits {
+    uint4 x[TILES][2][2];
+    float step[TILES][2];
+};
+
+// total += scale step (sum of digits times codes) of a chunk
+template <int TILES, int NT, int GP>
+__device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const Digits<TILES> &r, float (&total)[TILES][NT][4])
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES;
-    float acc[TILES][NT][4];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+        uint32_t w[4];
+        if (GP == 4) {
+            const uint4 v = lds_128(at + t * 512 + n * 64 + ((j ^ (n >> 1)) & 3) * 16);
+            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
+        } else {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = lds_32(at + t * 512 + n * 64 + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
+        }
+        int acc[TILES][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+            const uint32_t b0 = ((w[q] << 4) & 0xF0F0F0F0u) | one, b1 = (w[q] & 0xF0F0F0F0u) | one;
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) {
+                const uint4 u = r.x[m][0][q >> 1], v = r.x[m][1][q >> 1];
+                const uint32_t a[4] = {q & 1 ? u.z : u.x, q & 1 ? v.z : v.x, q & 1 ? u.w : u.y, q & 1 ? v.w : v.y};
+                if (q % GP == 0) mma_i8_first(acc[m], a, b0, b1);
+                else mma_i8(acc[m], a, b0, b1);
+            }
+            if (q % GP == GP - 1) {
+                const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
+                const float s0 = __uint_as_float(sv.x), s1 = __uint_as_float(sv.y);
+#pragma unroll
+                for (int m = 0; m < TILES; ++m)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const float up = r.step[m][h];
+                        float &u = total[m][t][2 * h], &v = total[m][t][2 * h + 1];
+                        u = __fmaf_rn((__int_as_float(acc[m][2 * h]) - MAGIC) * up, s0, u);
+                        v = __fmaf_rn((__int_as_float(acc[m][2 * h + 1]) - MAGIC) * up, s1, v);
+                    }
+            }
+        }
+    }
+}
+
+// ---- bf16 and fp16
+template <int XT> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
+{
+    if (XT == DSQ_BF16)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+            "{%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+            "{%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// total[t][0 .. 1] += scale (sum of x v) of a chunk: x, a row of 16-bit elements of the chunk (row n of a tile whose
+// upper half is empty), k elements of it
+template <int XT, int NT, int GP>
+__device__ __forceinline__ void multiply_16(uint32_t at, uint32_t base, const uint8_t *x, int k, float (&total)[NT][4])
+{
+    const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+    const uint32_t as = at + Stage<NT, GP>::W_BYTES;
+    float acc[NT][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
         if (q % GP == 0) {
 #pragma unroll
-            for (int m = 0; m < TILES; ++m)
+            for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) acc[m][t][e] = 0.f;
+                for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
         }
-        uint32_t a[TILES][2][4];
-#pragma unroll
-        for (int m = 0; m < TILES; ++m) {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const uint4 v = r.x[m][h][q];
-                // elements (2 s, 2 s + 4) and (2 s + 1, 2 s + 5), as the codes come out of their words
-                a[m][0][h] = __byte_perm(v.x, v.z, 0x5410);
-                a[m][0][h + 2] = __byte_perm(v.x, v.z, 0x7632);
-                a[m][1][h] = __byte_perm(v.y, v.w, 0x5410);
-                a[m][1][h + 2] = __byte_perm(v.y, v.w, 0x7632);
-                refill(m, h, q);
-            }
-        }
+        const uint4 v = x && 32 * q + 8 * j < k ? *reinterpret_cast<const uint4 *>(x + 64 * q + 16 * j) : make_uint4(0u, 0u, 0u, 0u);
+        // elements (2 s, 2 s + 4) and (2 s + 1, 2 s + 5), as the codes come out of their words
+        const uint32_t a[2][4] = {{__byte_perm(v.x, v.z, 0x5410), 0u, __byte_perm(v.x, v.z, 0x7632), 0u},
+                                  {__byte_perm(v.y, v.w, 0x5410), 0u, __byte_perm(v.y, v.w, 0x7632), 0u}};
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
             const uint32_t w = lds_32(at + t * 512 + n * 64 + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
 #pragma unroll
-            for (int s = 0; s < 2; ++s) {
-                const uint32_t b0 = dsq_value_pair<XT>(w, 2 * s, base), b1 = dsq_value_pair<XT>(w, 2 * s + 1, base);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) mma<XT>(acc[m][t], a[m][s], b0, b1);
-            }
+            for (int s = 0; s < 2; ++s)
+                mma<XT>(acc[t], a[s], dsq_value_pair<XT>(w, 2 * s, base), dsq_value_pair<XT>(w, 2 * s + 1, base));
         }
         if (q % GP == GP - 1) {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
-                const float s0 = __uint_as_float(sv.x), s1 = __uint_as_float(sv.y);
-#pragma unroll
-                for (int m = 0; m < TILES; ++m) {
-                    total[m][t][0] = __fmaf_rn(acc[m][t][0], s0, total[m][t][0]);
-                    total[m][t][1] = __fmaf_rn(acc[m][t][1], s1, total[m][t][1]);
-                    total[m][t][2] = __fmaf_rn(acc[m][t][2], s0, total[m][t][2]);
-                    total[m][t][3] = __fmaf_rn(acc[m][t][3], s1, total[m][t][3]);
-                }
+                total[t][0] = __fmaf_rn(acc[t][0], __uint_as_float(sv.x), total[t][0]);
+                total[t][1] = __fmaf_rn(acc[t][1], __uint_as_float(sv.y), total[t][1]);
             }
         }
     }
@@ -316,116 +466,209 @@ __device__ __forceinline__ float activated(float g, int act)
     return 0.5f * g * (1.f + tanhf(u));
 }
 
-// HALF: groups of up to 8 slots (the lower half of a tile), else 16
-template <int XT, bool HALF, int GP, int STAGES>
-__global__ void __launch_bounds__(THREADS, 2) moe_in_kernel(const __grid_constant__ MoeParams p)
-{
-    constexpr int NT = 4, ROWS = HALF ? 8 : 16, COLS = 16;
+constexpr int NT = 4;                 // tiles of eight columns that a warp has
+constexpr int IN_WARPS = 8, OUT_WARPS = 4;
+
+// What is behind a warp's sums of a group, shared by both forms: WC warps side by side on 16 columns of gate and
+// other half each, IN_WARPS / WC along K.
+template <int XT, int GP, int WC, int STAGES> struct In {
     using S = Stage<NT, GP>;
-    extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ Slots slots;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-    const int c0 = blockIdx.x * COLS;
-    const int chunks = (p.H + 127) >> 7, turns = warp < chunks ? (chunks - warp - 1) / WARPS + 1 : 0;
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES), base = dsq_value_base<XT>(p.odd);
-    grid_dependency_wait();
-    grid_launch_dependents();
-    sort_slots(slots, p.ids, p.slots, p.E, ROWS);
-    for (int gi = blockIdx.y; gi < slots.groups; gi += gridDim.y) {
-        const Group g = slots.group(gi);
-        const int64_t row0 = (int64_t)g.expert * 2 * p.I + c0;
-        auto row = [&](int c) { return c0 + (c & 15) < p.I ? row0 + (c & 15) + (c < 16 ? 0 : p.I) : (int64_t)-1; };
-        auto issue = [&](int i) {
-            if (i < turns)
-                copy_chunk<NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), p.W_in, p.pitch_in, p.s_in, (int64_t)p.E * 2 * p.I,
-                                   p.groups_in, p.units_in, p.units_in_inv, warp + i * WARPS, row);
-            cp_async_commit();
+    static constexpr int KW = IN_WARPS / WC, RING = IN_WARPS * STAGES * S::BYTES, SUMS = IN_WARPS * 2 * NT * 512;
+    static constexpr int BYTES = RING > SUMS ? RING : SUMS;
+
+    const MoeParams &p;
+    const Group g;
+    uint8_t *smem;
+    int warp, lane, n, j, wk, c0, turns, to_turn, issued;
+    uint32_t ring;
+    const uint8_t *src[NT];           // 16-byte piece j of the next chunk of this lane's columns
+    int col;                          // the scale that this lane copies is of this row (negative: none)
+    int64_t rows;
+
+    __device__ __forceinline__ In(const MoeParams &p_, const Group &g_, uint8_t *smem_) : p(p_), g(g_), smem(smem_)
+    {
+        warp = threadIdx.x >> 5; lane = threadIdx.x & 31; n = lane >> 2; j = lane & 3;
+        wk = warp / WC;
+        c0 = (blockIdx.x * WC + warp % WC) * 16;
+        turns = wk < p.chunks_in && (int)blockIdx.x * WC * 16 < p.I ? (p.chunks_in - wk - 1) / KW + 1 : 0;
+        ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES);
+        rows = (int64_t)p.E * 2 * p.I;
+        issued = 0;
+    }
+    // row of the matrix of codes that column c of the 32 is
+    __device__ __forceinline__ int64_t row(int c) const
+    {
+        return c0 + (c & 15) < p.I ? (int64_t)g.expert * 2 * p.I + c0 + (c & 15) + (c < 16 ? 0 : p.I) : (int64_t)-1;
+    }
+    __device__ __forceinline__ void issue()
+    {
+        if (issued < turns)
+            copy_chunk<NT, GP>(ring + (uint32_t)(issued % STAGES * S::BYTES), p.W_in, p.pitch_in, p.s_in, rows, p.groups_in, p.units_in,
+                               p.units_in_inv, wk + issued * KW, [&](int c) { return row(c); });
+        ++issued;
+        cp_async_commit();
+    }
+    // mid of (slot r of the group, column c of the block): gate and up are sums
+    __device__ __forceinline__ void put(int r, int c, float gate, float up) const
+    {
+        const int at = blockIdx.x * WC * 16 + c;
+        if (at >= p.chunks_out * 128) return;
+        // (columns behind the last are zeros up to the end of the chunk)
+        p.w.mid[(int64_t)p.w.sorted[g.first + r] * p.chunks_out * 128 + at] = at < p.I ? activated(gate, p.act) * up : 0.f;
+    }
+
+    template <int TILES> __device__ __forceinline__ void digits()
+    {
+        const uint32_t one = p.odd ? 0x08080808u : 0u;
+        const uint8_t *x[TILES][2];
+        const float *step[TILES][2];
+        const int64_t plane = (int64_t)p.chunks_in * 128;
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 4 * m + 2 * h + (n >> 2);
+                const int token = r < g.n ? p.w.sorted[g.first + r] / p.k : -1;
+                x[m][h] = token < 0 ? nullptr : p.w.x_digits + (token * 4 + (n & 3)) * plane + 32 * j;
+                step[m][h] = p.w.x_step + (token < 0 ? 0 : token) * p.chunks_in;
+            }
+        Digits<TILES> d;
+        auto load = [&](int chunk) {
+#pragma unroll
+            for (int m = 0; m < TILES; ++m)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const bool on = x[m][h] && chunk < p.chunks_in;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) d.x[m][h][i] = on ? load_16(x[m][h] + chunk * 128 + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+                    d.step[m][h] = on ? step[m][h][chunk] : 0.f;
+                }
         };
-#pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) issue(s);
-        const uint8_t *x[2];
-        bool has[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            has[h] = n + 8 * h < g.n;
-            x[h] = p.X + (has[h] ? (int64_t)(slots.sorted[g.first + n + 8 * h] / p.k) * p.H * 2 : 0) + 16 * j;
-        }
-        Rows<1> r;
-        auto load = [&](int i, int h, int q) {
-            const int at = (warp + i * WARPS) * 256 + 64 * q;
-            r.x[0][h][q] = has[h] && i < turns && at + 16 * j < 2 * p.H ? load_16(x[h] + at) : make_uint4(0u, 0u, 0u, 0u);
-        };
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) load(0, h, q);
-        float total[1][NT][4] = {};
+        load(wk);
+        float total[TILES][NT][4] = {};
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
             cp_async_wait<STAGES - 2>();
             __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
-            issue(i + STAGES - 1);
-            multiply<XT, 1, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), base, r, total,
-                                    [&](int, int h, int q) { load(i + 1, h, q); });
+            issue();
+            multiply_digits<TILES, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), one, d, total);
+            load(wk + (i + 1) * KW);
         }
         // the warps' sums, added in a fixed order
         cp_async_wait<0>();
         __syncthreads();
-        float4 *part = reinterpret_cast<float4 *>(smem);        // [WARPS][NT][32]
+        float4 *part = reinterpret_cast<float4 *>(smem);        // [IN_WARPS][TILES][NT][32]
 #pragma unroll
-        for (int t = 0; t < NT; ++t)
-            part[(warp * NT + t) * 32 + lane] = make_float4(total[0][t][0], total[0][t][1], total[0][t][2], total[0][t][3]);
+        for (int m = 0; m < TILES; ++m)
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+                part[((warp * TILES + m) * NT + t) * 32 + lane] = make_float4(total[m][t][0], total[m][t][1], total[m][t][2], total[m][t][3]);
         __syncthreads();
-        const float unit = dsq_value_unit<XT>(p.odd);
+        const float unit = dsq_value_unit<DSQ_I8>(p.odd);
         const float *sums = reinterpret_cast<const float *>(smem);
-        for (int e = threadIdx.x; e < ROWS * COLS; e += THREADS) {
-            const int rr = e / COLS, c = e % COLS;
-            if (rr >= g.n) break;
-            const int at = ((c >> 3) * 32 + (rr & 7) * 4 + ((c & 7) >> 1)) * 4 + 2 * (rr >> 3) + (c & 1);
-            float gate = 0.f, up = 0.f;
+        for (int e = threadIdx.x; e < g.n * WC * 16; e += IN_WARPS * 32) {
+            const int r = e / (WC * 16), c = e % (WC * 16), wc = c / 16;
+            float both[2];
 #pragma unroll
-            for (int w = 0; w < WARPS; ++w) {
-                gate += sums[w * NT * 128 + at];
-                up += sums[w * NT * 128 + 2 * 128 + at];
+            for (int u = 0; u < 2; ++u) {
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int l = ((r & 1) * 4 + k) * 4 + ((c & 7) >> 1);
+                    const int at = (((r >> 2) * NT + 2 * u + ((c >> 3) & 1)) * 32 + l) * 4 + (r & 2) + (c & 1);
+                    v[k] = 0.f;
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) v[k] += sums[(w * WC + wc) * TILES * NT * 128 + at];
+                }
+                both[u] = __fmaf_rn(v[0], 16777216.f * unit, __fmaf_rn(v[1], 65536.f * unit, __fmaf_rn(v[2], 256.f * unit, v[3] * unit)));
             }
-            // (columns behind the last are zeros up to the row's pitch)
-            float v = c0 + c < p.I ? activated(gate * unit, p.act) * (up * unit) : 0.f;
-            const __nv_bfloat16 hi = __float2bfloat16_rn(v);
-            const float rest = v - __bfloat162float(hi);
-            // (an infinity or a NaN has no rest)
-            const __nv_bfloat16 lo = __float2bfloat16_rn(rest == rest ? rest : 0.f);
-            const int64_t to = (int64_t)slots.sorted[g.first + rr] * p.pitch_mid + c0 + c;
-            p.mid[to] = __bfloat16_as_ushort(hi);
-            p.mid[to + (int64_t)p.slots * p.pitch_mid] = __bfloat16_as_ushort(lo);
+            put(r, c, both[0], both[1]);
         }
         __syncthreads();
     }
+
+    __device__ __forceinline__ void sixteen()
+    {
+        const uint32_t base = dsq_value_base<XT>(p.odd);
+        const uint8_t *x = n < g.n ? p.X + (int64_t)(p.w.sorted[g.first + n] / p.k) * p.H * 2 : nullptr;
+        float total[NT][4] = {};
+#pragma unroll 1
+        for (int i = 0; i < turns; ++i) {
+            cp_async_wait<STAGES - 2>();
+            __syncwarp();
+            issue();
+            const int chunk = wk + i * KW;
+            multiply_16<XT, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), base, x ? x + chunk * 256 : nullptr, p.H - chunk * 128, total);
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+        float2 *part = reinterpret_cast<float2 *>(smem);        // [IN_WARPS][NT][32]
+#pragma unroll
+        for (int t = 0; t < NT; ++t) part[(warp * NT + t) * 32 + lane] = make_float2(total[t][0], total[t][1]);
+        __syncthreads();
+        const float unit = dsq_value_unit<XT>(p.odd);
+        const float *sums = reinterpret_cast<const float *>(smem);
+        for (int e = threadIdx.x; e < g.n * WC * 16; e += IN_WARPS * 32) {
+            const int r = e / (WC * 16), c = e % (WC * 16), wc = c / 16;
+            float both[2] = {0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int w = 0; w < KW; ++w)
+                    both[u] += sums[(w * WC + wc) * NT * 64 + ((2 * u + ((c >> 3) & 1)) * 32 + r * 4 + ((c & 7) >> 1)) * 2 + (c & 1)];
+            put(r, c, both[0] * unit, both[1] * unit);
+        }
+        __syncthreads();
+    }
+};
+
+template <int XT, int GP, int WC, int STAGES>
+__global__ void __launch_bounds__(IN_WARPS * 32, 2) moe_in_kernel(const __grid_constant__ MoeParams p)
+{
+    using L = In<XT, GP, WC, STAGES>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    grid_dependency_wait();
+    grid_launch_dependents();
+    const int groups = *p.w.groups;
+    for (int i = blockIdx.y; i < groups; i += gridDim.y) {
+        L l(p, group_at(p.w, i), smem);
+#pragma unroll
+        for (int s = 0; s < STAGES - 1; ++s) l.issue();
+        bool lost = false;
+        if (!p.odd)
+            for (int e = threadIdx.x; e < l.g.n * p.chunks_in; e += IN_WARPS * 32)
+                lost = lost || p.w.lost[p.w.sorted[l.g.first + e / p.chunks_in] / p.k * p.chunks_in + e % p.chunks_in];
+        if (!p.odd && __syncthreads_or(lost)) l.sixteen();
+        else if (l.g.n <= 4) l.template digits<1>();
+        else l.template digits<2>();
+    }
 }
 
-template <int TILES, int GP, int STAGES>
-__global__ void __launch_bounds__(THREADS, TILES == 1 ? 2 : 1) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
+// WC warps side by side on 32 columns each, OUT_WARPS / WC (and the cluster's blocks) along the chunks
+template <int GP, int WC, int STAGES>
+__global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
 {
-    constexpr int NT = 4, ROWS = 8 * TILES, COLS = 8 * NT;
+    constexpr int KW = OUT_WARPS / WC, WIDE = 8 * NT, COLS = WC * WIDE, THREADS = OUT_WARPS * 32;
     using S = Stage<NT, GP>;
     extern __shared__ __align__(128) uint8_t smem[];
-    __shared__ Slots slots;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
-    const int64_t c0 = (int64_t)(blockIdx.x / cluster) * COLS;
-    const int chunks = (p.I + 127) >> 7;
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES), base = dsq_value_base<DSQ_BF16>(p.odd);
-    // [WARPS][T][COLS]; the warp's own
-    float *sums = reinterpret_cast<float *>(smem + WARPS * STAGES * S::BYTES), *mine = sums + warp * p.T * COLS;
-    // Ahead of the wait: ids, codes and scales are older than the kernel ahead (moe_in_kernel, which
-    // waited for all that was in front of it before it let this one start).
-    sort_slots(slots, p.ids, p.slots, p.E, ROWS);
+    const int64_t b0 = (int64_t)(blockIdx.x / cluster) * COLS, c0 = b0 + warp % WC * WIDE;
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES), one = p.odd ? 0x08080808u : 0u;
+    // [OUT_WARPS][T][WIDE]; the warp's own
+    float *sums = reinterpret_cast<float *>(smem + OUT_WARPS * STAGES * S::BYTES), *mine = sums + warp * p.T * WIDE;
+    for (int i = lane; i < p.T * WIDE; i += 32) mine[i] = 0.f;
+    // Ahead of the wait: the slots, codes and scales are older than the kernel ahead (moe_mid_kernel; moe_in_kernel,
+    // which moe_mid_kernel waits for before it lets this one start, waited for all that was in front of it).
+    const int groups = *p.w.groups, chunks = p.chunks_out;
     // this warp's share of the chunks of all groups
-    const int64_t all = (int64_t)slots.groups * chunks, share = rank * WARPS + warp, shares = cluster * WARPS;
+    const int64_t all = (int64_t)groups * chunks;
+    const int share = rank * KW + warp / WC, shares = cluster * KW;
     const int q0 = (int)(all * share / shares), q1 = (int)(all * (share + 1) / shares);
     int ig = q0 / chunks, ic = q0 - ig * chunks;                // of the next copy
     auto issue = [&](int i) {
         if (i < q1) {
-            const int64_t row0 = (int64_t)(slots.packed[ig] & 1023) * p.H + c0;
+            const int64_t row0 = (int64_t)(p.w.packed[ig] & 1023) * p.H + c0;
             copy_chunk<NT, GP>(ring + (uint32_t)((i - q0) % STAGES * S::BYTES), p.W_out, p.pitch_out, p.s_out, (int64_t)p.E * p.H,
                                p.groups_out, p.units_out, p.units_out_inv, ic,
                                [&](int c) { return c0 + c < p.H ? row0 + c : (int64_t)-1; });
@@ -438,100 +681,134 @@ __global__ void __launch_bounds__(THREADS, TILES == 1 ? 2 : 1) moe_out_kernel(co
     };
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(q0 + s);
-    for (int i = lane; i < p.T * COLS; i += 32) mine[i] = 0.f;
     __syncwarp();
     grid_dependency_wait();
     grid_launch_dependents();
 
-    // rows of the chunk that is loaded next
-    int lg = q0 / chunks, lc = q0 - lg * chunks;
-    const uint16_t *x[TILES];
-    bool has[TILES];
-    const int64_t lo = (int64_t)p.slots * p.pitch_mid;
-    auto rows_of = [&]() {
-        if (lg >= slots.groups) return;
-        const Group g = slots.group(lg);
+    Group g = {};
+    const uint8_t *x[2][2];
+    const float *step[2][2];
+    const int64_t plane = (int64_t)chunks * 128;
+    int cg = q0 / chunks, cc = q0 - cg * chunks;                // of the chunk at hand
+    auto rows_of = [&](int i) {
+        g = group_at(p.w, i);
 #pragma unroll
-        for (int m = 0; m < TILES; ++m) {
-            has[m] = n + 8 * m < g.n;
-            x[m] = p.mid + (has[m] ? (int64_t)slots.sorted[g.first + n + 8 * m] * p.pitch_mid : 0) + 8 * j;
-        }
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = 4 * m + 2 * h + (n >> 2);
+                const int slot = r < g.n ? p.w.sorted[g.first + r] : -1;
+                x[m][h] = slot < 0 ? nullptr : p.w.mid_digits + (slot * 4 + (n & 3)) * plane + 32 * j;
+                step[m][h] = p.w.mid_step + (slot < 0 ? 0 : slot) * chunks;
+            }
     };
-    Rows<TILES> r;
-    auto load = [&](bool on, int m, int h, int q) {
-        const int at = lc * 128 + 32 * q;
-        r.x[m][h][q] = on && has[m] && at + 8 * j < p.pitch_mid ? load_16(x[m] + (h ? lo : 0) + at) : make_uint4(0u, 0u, 0u, 0u);
+    Digits<2> d;
+    auto load = [&](int chunk) {
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i)
+                    d.x[m][h][i] = x[m][h] ? load_16(x[m][h] + chunk * 128 + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
+                d.step[m][h] = x[m][h] ? step[m][h][chunk] : 0.f;
+            }
     };
-    rows_of();
-#pragma unroll
-    for (int m = 0; m < TILES; ++m)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) load(q0 < q1, m, h, q);
-    float total[TILES][NT][4] = {};
-    int cg = lg, cc = lc;                                       // of the chunk at hand
+    if (q0 < q1) {
+        rows_of(cg);
+        load(cc);
+    }
+    float total[2][NT][4] = {};
+    // what a row's digit stands for
+    const float place = (n & 3) == 0 ? 16777216.f : (n & 3) == 1 ? 65536.f : (n & 3) == 2 ? 256.f : 1.f;
 #pragma unroll 1
     for (int i = q0; i < q1; ++i) {
         cp_async_wait<STAGES - 2>();
         __syncwarp();
         issue(i + STAGES - 1);
-        if (++lc == chunks) {
-            lc = 0;
-            ++lg;
-            rows_of();
-        }
-        multiply<DSQ_BF16, TILES, NT, GP>(ring + (uint32_t)((i - q0) % STAGES * S::BYTES), base, r, total,
-                                          [&](int m, int h, int q) { load(i + 1 < q1, m, h, q); });
-        if (++cc < chunks && i + 1 < q1) continue;
-        // the group's sums to the tokens' rows, one slot after the other (two may be the same token's)
-        const Group g = slots.group(cg);
+        const uint32_t at = ring + (uint32_t)((i - q0) % STAGES * S::BYTES);
+        if (g.n <= 4) {
+            Digits<1> d1;
 #pragma unroll
-        for (int m = 0; m < TILES; ++m)
-            for (int rr = 0; rr < 8 && 8 * m + rr < g.n; ++rr) {
-                if (n == rr) {
-                    const int slot = slots.sorted[g.first + 8 * m + rr], token = slot / p.k;
+            for (int h = 0; h < 2; ++h) {
+                d1.x[0][h][0] = d.x[0][h][0];
+                d1.x[0][h][1] = d.x[0][h][1];
+                d1.step[0][h] = d.step[0][h];
+            }
+            multiply_digits<1, NT, GP>(at, one, d1, reinterpret_cast<float (&)[1][NT][4]>(total));
+        } else {
+            multiply_digits<2, NT, GP>(at, one, d, total);
+        }
+        if (++cc < chunks && i + 1 < q1) {
+            load(cc);
+            continue;
+        }
+        // the group's sums to the tokens' rows, one slot after the other (two may be the same token's)
+#pragma unroll
+        for (int m = 0; m < 2; ++m) {
+            if (4 * m >= g.n) break;
+#pragma unroll
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = total[m][t][e] * place;
+                    v += __shfl_xor_sync(~0u, v, 4);
+                    v += __shfl_xor_sync(~0u, v, 8);
+                    total[m][t][e] = v;
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (4 * m + r >= g.n) break;
+                if (n == (r & 1) * 4) {
+                    const int slot = p.w.sorted[g.first + 4 * m + r], token = slot / p.k;
                     const float w = p.weights[slot];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
-                        float2 *to = reinterpret_cast<float2 *>(mine + token * COLS + 8 * t + 2 * j);
+                        float2 *to = reinterpret_cast<float2 *>(mine + token * WIDE + 8 * t + 2 * j);
                         float2 v = *to;
-                        v.x = __fmaf_rn(total[m][t][0] + total[m][t][2], w, v.x);
-                        v.y = __fmaf_rn(total[m][t][1] + total[m][t][3], w, v.y);
+                        v.x = __fmaf_rn(total[m][t][(r & 2)], w, v.x);
+                        v.y = __fmaf_rn(total[m][t][(r & 2) + 1], w, v.y);
                         *to = v;
                     }
                 }
                 __syncwarp();
             }
 #pragma unroll
-        for (int m = 0; m < TILES; ++m)
-#pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) total[m][t][e] = 0.f;
-        cc = 0;
-        ++cg;
+        }
+        if (cc == chunks) {
+            cc = 0;
+            ++cg;
+        }
+        if (i + 1 < q1) {
+            rows_of(cg);
+            load(cc);
+        }
     }
     cp_async_wait<0>();
     __syncthreads();
-    // the warps' rows, into the first one's place
+    // the sums of the warps along the chunks, into the first one's place
     for (int e = threadIdx.x; e < p.T * COLS; e += THREADS) {
         float s = 0.f;
 #pragma unroll
-        for (int w = 0; w < WARPS; ++w) s += sums[w * p.T * COLS + e];
-        sums[e] = s;
+        for (int w = 0; w < KW; ++w) s += sums[w * p.T * COLS + e];
+        if (KW > 1) sums[e] = s;
     }
     if (cluster > 1) cluster_sync_all();
     else __syncthreads();
-    const float unit = dsq_value_unit<DSQ_BF16>(p.odd);
+    const float unit = dsq_value_unit<DSQ_I8>(p.odd);
     for (int e = rank * THREADS + threadIdx.x; e < p.T * COLS; e += cluster * THREADS) {
         float s = 0.f;
         if (cluster == 1) s = sums[e];
         else
             for (int c = 0; c < cluster; ++c) s += __uint_as_float(ld_cluster_32(map_to_cta(smem_u32(sums + e), c)));
-        const int64_t col = c0 + e % COLS;
+        // (a row of 32 columns of each of the warps side by side)
+        const int wc = e / (p.T * WIDE), token = e / WIDE - wc * p.T;
+        const int64_t col = b0 + wc * WIDE + e % WIDE;
         if (col >= p.H) continue;
-        const int64_t to = (int64_t)(e / COLS) * p.H + col;
+        const int64_t to = (int64_t)token * p.H + col;
         s *= unit;
         if (p.y_type == DSQ_F32) {
             if (p.residual) s += ((const float *)p.residual)[to];
@@ -548,48 +825,81 @@ __global__ void __launch_bounds__(THREADS, TILES == 1 ? 2 : 1) moe_out_kernel(co
 }
 
 // ---- host ------------------------------------------------------------------------------------
-constexpr int IN_STAGES = 4, OUT_STAGES = 3;
+constexpr int IN_STAGES = 4, OUT_STAGES = 4;
 
-template <int XT, int GP> int launch_in(const MoeParams &p, cudaStream_t s)
+// from how many tokens on warps lie side by side, so that they share rows of digits in L1
+constexpr int WIDE_FROM = 9;
+
+template <int XT, int GP> int launch_prepare(const MoeParams &p, cudaStream_t s)
 {
-    using S = Stage<4, GP>;
-    constexpr int bytes = WARPS * IN_STAGES * S::BYTES;
-    static_assert(bytes >= WARPS * 4 * 512 && bytes <= 100 * 1024, "shared memory");
-    const dim3 grid((unsigned)((p.I + 15) / 16), (unsigned)(p.slots < p.E ? p.slots : p.E));
-    const bool half = p.T <= 8;
-    static std::atomic<unsigned long long> configured[2];
-    const auto kernel = half ? moe_in_kernel<XT, true, GP, IN_STAGES> : moe_in_kernel<XT, false, GP, IN_STAGES>;
-    const int st = dsq_allow_smem((const void *)kernel, bytes, &configured[half]);
-    if (st) return st;
-    return dsq_launch(kernel, grid, dim3(THREADS), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
+    const int blocks = 1 + (p.T * p.chunks_in + PREPARE_WARPS - 1) / PREPARE_WARPS;
+    return dsq_launch(moe_prepare_kernel<XT, GP == 4>, dim3(blocks), dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int TILES, int GP> int launch_out(const MoeParams &p, cudaStream_t s)
+template <int XT, int GP, int WC> int launch_in(const MoeParams &p, cudaStream_t s)
 {
-    using S = Stage<4, GP>;
-    constexpr int ring = WARPS * OUT_STAGES * S::BYTES, row = WARPS * 32 * 4, most = ring + PASS_TOKENS * row;
-    static_assert(most <= 200 * 1024, "shared memory");
-    static std::atomic<unsigned long long> configured;
-    const auto kernel = moe_out_kernel<TILES, GP, OUT_STAGES>;
-    const int st = dsq_allow_smem((const void *)kernel, most, &configured);
+    constexpr int bytes = In<XT, GP, WC, IN_STAGES>::BYTES;
+    static_assert(bytes <= 112 * 1024, "shared memory");
+    static std::atomic<unsigned long long> configured{0};
+    const auto kernel = moe_in_kernel<XT, GP, WC, IN_STAGES>;
+    const int st = dsq_allow_smem((const void *)kernel, bytes, &configured);
     if (st) return st;
-    const int tiles = (p.H + 31) / 32, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    // (to the end of the last chunk: zeros)
+    const dim3 grid((unsigned)((p.chunks_out * 128 + WC * 16 - 1) / (WC * 16)), (unsigned)(p.slots < p.E ? p.slots : p.E));
+    return dsq_launch(kernel, grid, dim3(IN_WARPS * 32), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
+}
+
+template <int GP, int WC> int launch_out(const MoeParams &p, cudaStream_t s)
+{
+    constexpr int ring = OUT_WARPS * OUT_STAGES * Stage<NT, GP>::BYTES, row = OUT_WARPS * 8 * NT * 4, cols = WC * 8 * NT;
+    static_assert(ring + PASS_TOKENS * row <= 200 * 1024, "shared memory");
+    static std::atomic<unsigned long long> configured{0};
+    const auto kernel = moe_out_kernel<GP, WC, OUT_STAGES>;
+    const int st = dsq_allow_smem((const void *)kernel, ring + PASS_TOKENS * row, &configured);
+    if (st) return st;
+    const int tiles = (p.H + cols - 1) / cols, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     int cluster = 1;
-    while (cluster < 8 && tiles * cluster * 2 <= 2 * sms) cluster *= 2;
-    return dsq_launch(kernel, dim3((unsigned)(tiles * cluster)), dim3(THREADS), (size_t)(ring + p.T * row), s,
+    while (cluster < 8 && tiles * cluster * 2 <= 3 * sms) cluster *= 2;
+    return dsq_launch(kernel, dim3((unsigned)(tiles * cluster)), dim3(OUT_WARPS * 32), (size_t)(ring + p.T * row), s,
                       dsq_launch_hooks().pdl, cluster, p, cluster);
 }
 
-template <int GP_IN> int pick_in(const MoeParams &p, int x_type, cudaStream_t s)
+template <int XT, int GP> int pick_in(const MoeParams &p, cudaStream_t s)
 {
-    return x_type == DSQ_BF16 ? launch_in<DSQ_BF16, GP_IN>(p, s) : launch_in<DSQ_F16, GP_IN>(p, s);
+    const int st = launch_prepare<XT, GP>(p, s);
+    if (st) return st;
+    return p.T < WIDE_FROM ? launch_in<XT, GP, 1>(p, s) : launch_in<XT, GP, 4>(p, s);
 }
 template <int GP> int pick_out(const MoeParams &p, cudaStream_t s)
 {
-    return p.T <= 8 ? launch_out<1, GP>(p, s) : launch_out<2, GP>(p, s);
+    const int st = dsq_launch(moe_mid_kernel<GP == 4>, dim3((p.slots * p.chunks_out + PREPARE_WARPS - 1) / PREPARE_WARPS),
+                              dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
+    if (st) return st;
+    return p.T < WIDE_FROM ? launch_out<GP, 1>(p, s) : launch_out<GP, 4>(p, s);
 }
 
-int pitch_of_mid(int64_t I) { return (int)((I + 15) / 16 * 16); }
+int chunks_of(int64_t K) { return (int)((K + 127) / 128); }
+
+// Lays the workspace out behind its first bytes; returns its size.
+size_t lay_out(Work &w, char *base, int T, int slots, int chunks_in, int chunks_out)
+{
+    size_t at = DSQ_WS_BYTES;
+    auto take = [&](size_t bytes) {
+        char *p = base + at;
+        at += (bytes + 255) / 256 * 256;
+        return p;
+    };
+    w.groups = (int *)take(4);
+    w.packed = (uint32_t *)take((size_t)slots * 4);
+    w.sorted = (uint16_t *)take((size_t)slots * 2);
+    w.lost = (uint8_t *)take((size_t)T * chunks_in);
+    w.x_step = (float *)take((size_t)T * chunks_in * 4);
+    w.mid_step = (float *)take((size_t)slots * chunks_out * 4);
+    w.x_digits = (uint8_t *)take((size_t)T * chunks_in * 512);
+    w.mid_digits = (uint8_t *)take((size_t)slots * chunks_out * 512);
+    w.mid = (float *)take((size_t)slots * chunks_out * 512);
+    return at;
+}
 
 // a group longer than the row is the row
 int64_t group_of_row(int64_t K, int64_t group) { return dsq_group_count(K, group) == 1 ? (K + 127) / 128 * 128 : group; }
@@ -618,10 +928,12 @@ int dsq_moe_route(const float *logits, int64_t T, int64_t E, int k, int renormal
     return dsq_launch(kernel, dim3((unsigned)((T + 3) / 4)), dim3(128), 0, (cudaStream_t)stream, dsq_launch_hooks().pdl, 0, p);
 }
 
-size_t dsq_moe_workspace_bytes(int64_t T, int64_t I, int k)
+size_t dsq_moe_workspace_bytes(int64_t T, int64_t H, int64_t I, int k)
 {
-    if (T <= 0 || I <= 0 || I > 1 << 24 || k <= 0 || k > MAX_TOP) return DSQ_WS_BYTES;
-    return DSQ_WS_BYTES + (size_t)(T < PASS_TOKENS ? T : PASS_TOKENS) * (size_t)k * (size_t)pitch_of_mid(I) * 4;
+    if (T <= 0 || H <= 0 || H > DSQ_GROUPS_MAX_K || I <= 0 || I > DSQ_GROUPS_MAX_K || k <= 0 || k > MAX_TOP) return DSQ_WS_BYTES;
+    const int tokens = (int)(T < PASS_TOKENS ? T : PASS_TOKENS);
+    Work w;
+    return lay_out(w, nullptr, tokens, tokens * k, chunks_of(H), chunks_of(I));
 }
 
 int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *weights, const void *W_in,
@@ -643,15 +955,15 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
     for (const void *a : aligned)
         if (!dsq_aligned16(a)) return DSQ_ERR_ALIGN;
     if (H % 8 != 0) return DSQ_ERR_ALIGN;
-    if (ws_bytes < dsq_moe_workspace_bytes(T, I, k)) return DSQ_ERR_SIZE;
+    if (ws_bytes < dsq_moe_workspace_bytes(T, H, I, k)) return DSQ_ERR_SIZE;
     const int64_t g_in = group_of_row(H, group), g_out = group_of_row(I, group);
     const int gp_in = dsq_group_pieces(g_in), gp_out = dsq_group_pieces(g_out);
     MoeParams p;
     p.W_in = (const uint8_t *)W_in; p.W_out = (const uint8_t *)W_out;
     p.s_in = scales_in; p.s_out = scales_out;
-    p.mid = (uint16_t *)((char *)workspace + DSQ_WS_BYTES);
     p.H = (int)H; p.I = (int)I; p.E = (int)E; p.k = k;
-    p.pitch_in = (int)dsq_row_pitch(H, 4); p.pitch_out = (int)dsq_row_pitch(I, 4); p.pitch_mid = pitch_of_mid(I);
+    p.pitch_in = (int)dsq_row_pitch(H, 4); p.pitch_out = (int)dsq_row_pitch(I, 4);
+    p.chunks_in = chunks_of(H); p.chunks_out = chunks_of(I);
     p.groups_in = (int)dsq_group_count(H, g_in); p.groups_out = (int)dsq_group_count(I, g_out);
     set_units(g_in, gp_in, &p.units_in, &p.units_in_inv);
     set_units(g_out, gp_out, &p.units_out, &p.units_out_inv);
@@ -661,11 +973,15 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
     for (int64_t t = 0; t < T; t += PASS_TOKENS) {
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
+        lay_out(p.w, (char *)workspace, p.T, p.slots, p.chunks_in, p.chunks_out);
         p.X = (const uint8_t *)X + t * H * 2;
         p.ids = ids + t * k; p.weights = weights + t * k;
         p.residual = residual ? (const char *)residual + t * H * y_size : nullptr;
         p.Y = (char *)Y + t * H * y_size;
-        st = gp_in == 4 ? pick_in<4>(p, x_type, s) : gp_in == 2 ? pick_in<2>(p, x_type, s) : pick_in<1>(p, x_type, s);
+        if (x_type == DSQ_BF16)
+            st = gp_in == 4 ? pick_in<DSQ_BF16, 4>(p, s) : gp_in == 2 ? pick_in<DSQ_BF16, 2>(p, s) : pick_in<DSQ_BF16, 1>(p, s);
+        else
+            st = gp_in == 4 ? pick_in<DSQ_F16, 4>(p, s) : gp_in == 2 ? pick_in<DSQ_F16, 2>(p, s) : pick_in<DSQ_F16, 1>(p, s);
         if (!st) st = gp_out == 4 ? pick_out<4>(p, s) : gp_out == 2 ? pick_out<2>(p, s) : pick_out<1>(p, s);
         if (st) return st;
     }

@@ -4,7 +4,9 @@ Tolerances, in units u = 2^-24 of binary32, of the magnitudes of the terms:
   first sums    products are exact; a tensor-core instruction adds 16 of them to its sums within 8 u of their
                 magnitudes, eight of which make up to 128 codes: 64 u; K / 32 fused sums with scales, 8 warps' sums:
                 eps_in = (64 + K / 32 + 12) u
-  mid           activation and product 16 u, hi + lo 2^-18 = 64 u: eps_mid = 80 u
+  mid           activation and product 16 u: eps_mid = 20 u
+  digits        x and mid are kept to half a step, 2^-31 of the power of two above the largest of 128 elements:
+                2^-30 of the largest of a row at most
   second sums   the same of I codes, k slots' sums and weights, 8 warps of 8 blocks: eps_out = (64 + I / 32 +
                 2 k + 20) u
   y             the residual's addition u, then half a step of the type
@@ -55,7 +57,7 @@ class Layer:
         H, I, k = self.x.shape[1], self.I, self.ids.shape[1]
         ref, bound = moe.layer(self.x.double().numpy(), self.ids, self.w, self.c_in, self.s_in, self.c_out, self.s_out,
                                self.E, I, self.group, kind, w_offset, self.residual.double().numpy() if residual else None,
-                               eps_in=(76 + H / 32) * U, eps_out=(84 + I / 32 + 2 * k) * U, eps_mid=80 * U)
+                               eps_in=(76 + H / 32) * U, eps_out=(84 + I / 32 + 2 * k) * U, eps_mid=20 * U, digits=2.0 ** -30)
         f = torch.finfo(y.dtype)
         tol = bound + U * np.abs(ref) + (f.eps / 2 * (np.abs(ref) + bound) + f.smallest_normal * f.eps)
         err = np.abs(N(y.double()) - ref)
@@ -90,7 +92,7 @@ def test_forms(dsq, T):
             a.check(a.run(dsq, activation=kind, w_offset=off), kind, off)
     for t in (torch.float32, torch.float16):
         a.check(a.run(dsq, residual=None, out_dtype=t), residual=False)
-    ws = torch.full((dsq.dsq_moe_workspace_bytes(T, 100, 3),), 255, dtype=torch.uint8, device="cuda")
+    ws = torch.full((dsq.dsq_moe_workspace_bytes(T, 264, 100, 3),), 255, dtype=torch.uint8, device="cuda")
     y = a.residual.cuda()
     assert a.run(dsq, residual=y, out=y, ws=ws) is y
     assert torch.equal(y, a.run(dsq))
@@ -128,6 +130,30 @@ def test_not_a_number_and_infinity_stay_with_their_token(dsq, T):
     a.w[2] = INF
     got = a.run(dsq)
     assert not got[2].isfinite().any() and got[[0, 1]].isfinite().all()
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("off", [0.5, 0.0])
+@pytest.mark.parametrize("T", [1, 7, 30])
+def test_outliers(dsq, T, t, off):
+    """Elements far above the rest of their row; on the grid with a 0, behind weights that make them vanish."""
+    a = Layer(dsq, T, 512, 96, 3, 2, 64, t=t, seed=6)
+    big = 6e4 if t == torch.float16 else 1e30
+    a.x[:, 5::128] = big
+    a.x[:, 77] = 2.0 ** -20
+    if off == 0.0:
+        a.c_in[:, 5::128] = 0
+        a.weights[0] = dsq.dsq_pack_codes(torch.from_numpy(a.c_in).cuda(), 4)
+        y = a.run(dsq, w_offset=off, residual=None, out_dtype=torch.float32)
+        b = Layer.__new__(Layer)
+        b.__dict__.update(a.__dict__)
+        b.x = a.x.clone()
+        b.x[:, 5::128] = 0
+        b.check(y, w_offset=off, residual=False)       # what is left is as exact as ever
+    elif t == torch.float16:
+        a.s_in *= 1e-3
+        a.weights[1] = torch.from_numpy(a.s_in).cuda()
+        a.check(a.run(dsq, out_dtype=torch.float32, residual=None), residual=False)
 
 
 def test_large_values(dsq):
@@ -225,14 +251,14 @@ def test_two_graphs_and_streams(dsq):
     calls, graphs = [], []
     for a in sets:
         args = [a.x.cuda(), torch.from_numpy(a.ids).cuda(), torch.from_numpy(a.w).cuda()]
-        ws = torch.empty(dsq.dsq_moe_workspace_bytes(len(a.x), a.I, a.ids.shape[1]), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(dsq.dsq_moe_workspace_bytes(*a.x.shape, a.I, a.ids.shape[1]), dtype=torch.uint8, device="cuda")
         call = lambda a=a, args=args, ws=ws: dsq.dsq_moe_group(*args, *a.weights, ws=ws)
         want = call().clone()
         torch.cuda.synchronize()
         graph = torch.cuda.CUDAGraph()
         with torch.cuda.graph(graph):
             y = call()
-        calls.append((want, y))
+        calls.append((want, y, call))              # (a graph does not hold its inputs)
         graphs.append(graph)
     streams = [torch.cuda.Stream() for _ in sets]
     for _ in range(30):
@@ -240,5 +266,5 @@ def test_two_graphs_and_streams(dsq):
             with torch.cuda.stream(s):
                 graph.replay()
     torch.cuda.synchronize()
-    for want, y in calls:
+    for want, y, _ in calls:
         assert torch.equal(want, y)

@@ -32,17 +32,19 @@ def layer(X=P, xt=1, ids=P, w=P, wi=P, si=P, wo=P, so=P, T=4, H=64, I=48, E=8, k
     (layer, dict(bits=5), -3), (layer, dict(bits=3), -8), (layer, dict(group=48), -8), (layer, dict(group=0), -4),
     (layer, dict(off=NAN), -6), (layer, dict(off=0.25), -8), (layer, dict(act=2), -8), (layer, dict(xt=0), -8),
     (layer, dict(xt=3), -8), (layer, dict(yt=3), -8), (layer, dict(H=60), -2), (layer, dict(X=ODD), -2),
-    (layer, dict(res=ODD), -2), (layer, dict(ws=ODD), -2), (layer, dict(nbytes=256 + 4 * 2 * 48 * 4 - 1), -5),
+    (layer, dict(res=ODD), -2), (layer, dict(ws=ODD), -2), (layer, dict(nbytes=4 * 2 * 128 * 8), -5),
 ])
 def test_status(call, args, status):
     assert call(**args) == status
 
 
 def test_sizes():
-    assert dsq.dsq_moe_workspace_bytes(4, 48, 2) == 256 + 4 * 2 * 48 * 4
-    assert dsq.dsq_moe_workspace_bytes(1, 1, 1) == 256 + 16 * 4
-    assert dsq.dsq_moe_workspace_bytes(64, 100, 3) == dsq.dsq_moe_workspace_bytes(1 << 19, 100, 3)
-    assert dsq.dsq_moe_workspace_bytes(0, 1, 1) == dsq.dsq_workspace_bytes()
+    # digits of four bytes an element of x, eight bytes an element of mid, in chunks of 128
+    need = 4 * 64 * 4 + 4 * 2 * 128 * 8
+    assert need <= dsq.dsq_moe_workspace_bytes(4, 64, 48, 2) <= 256 + 2 * need + 9 * 256
+    assert dsq.dsq_moe_workspace_bytes(64, 64, 100, 3) == dsq.dsq_moe_workspace_bytes(1 << 19, 64, 100, 3)
+    for bad in ((0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1, 1, 1, 33), (1, 1 << 21, 1, 1)):
+        assert dsq.dsq_moe_workspace_bytes(*bad) == dsq.dsq_workspace_bytes()
 
 
 def test_the_binding_refuses_other_tensors():
