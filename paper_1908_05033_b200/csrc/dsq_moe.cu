@@ -124,8 +124,8 @@ struct Work {
     uint32_t *packed;                 // groups: expert | first << 10 | (n - 1) << 22
     uint16_t *sorted;                 // slots by expert
     uint8_t *lost;                    // [T][chunks_in]: digits are not all of x's chunk
-    float *x_step, *mid_step;         // [T][chunks_in], [slots][chunks_out]: what the lowest digit stands for
-    uint8_t *x_digits, *mid_digits;   // [T][4][128 chunks_in], [slots][4][128 chunks_out], the highest digit first
+    float *x_step, *mid_step;         // [T][chunks_in], [slots][chunks_out]: what the highest digit stands for
+    uint8_t *x_digits, *mid_digits;   // [T][chunks_in][512], [slots][chunks_out][512]
     float *mid;                       // [slots][128 chunks_out]
 };
 struct MoeParams {
@@ -195,11 +195,13 @@ __device__ __forceinline__ void sort_slots(const MoeParams &p, int *start)
     }
 }
 
-// The four digits of a chunk of 128 elements, by a warp: f holds elements 4 lane .. 4 lane + 3.  Stored as an instruction's
-// operand wants them: lane j's 32 bytes of a chunk are four words' codes 0, 2, 4, 6, 1, 3, 5, 7, the words being 4 j .. 4 j
-// + 3 where no group's end cuts the chunk (WHOLE), else j, j + 4, j + 8, j + 12.  Returns the step; *lost: something is
-// left of the elements.
-template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (&f)[4], uint8_t *to, int64_t plane, bool *lost)
+// The four digits of a chunk of 128 elements, by a warp: f holds elements 4 lane .. 4 lane + 3.  512 bytes, as an
+// instruction's rows want them: a lane of row n (and n + 8) has digits d = n & 1 (and d + 2) of a slot, and of each of its
+// four words of codes 16 bytes: codes 0, 2, 4, 6 in digit d, in digit d + 2, codes 1, 3, 5, 7 in digit d, in digit d + 2; the
+// words of lane j are 4 j .. 4 j + 3 where no group's end cuts the chunk (WHOLE), else j, j + 4, j + 8, j + 12.  The
+// 16 bytes of word q of lane j and digit d lie at 128 q + 64 d + 16 j.  Returns what the highest digit (0) stands for; *lost:
+// something is left of the elements.
+template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (&f)[4], uint8_t *to, bool *lost)
 {
     const int lane = threadIdx.x & 31;
     float most = 0.f;
@@ -210,7 +212,7 @@ template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (
         bad = bad || !(fabsf(f[i]) <= 3.402823466e38f);
     }
     const uint32_t e = __reduce_max_sync(~0u, __float_as_uint(most) >> 23);
-    // step = 2^(e - 156), 2^-149 at least: the largest is below 2^30 of it
+    // the lowest digit stands for 2^(e - 156), 2^-149 at least: the largest is below 2^30 of it
     const int up = 156 - (int)max(e, 7u), up1 = min(up, 126);
     const float a = __uint_as_float((uint32_t)(127 + up1) << 23), b = __uint_as_float((uint32_t)(127 + up - up1) << 23);
     uint32_t v[4];
@@ -219,22 +221,22 @@ template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (
     for (int i = 0; i < 4; ++i) {
         const float u = f[i] * b * a, w = rintf(u);
         rest = rest || w != u || (u == 0.f && f[i] != 0.f);
-        v[i] = (uint32_t)__float2int_rn(u) + 0x808080u;
+        v[i] = (uint32_t)__float2int_rn(u) + 0x808080u;       // its lower bytes are digits plus 128
     }
-    // bytes of elements 0, 2 and 1, 3: the lower three plus 128
     const int block = lane >> 1, half = lane & 1;
-    const int word = WHOLE ? block : (block & 3) * 4 + (block >> 2);
-    uint8_t *at = to + word * 8 + half * 2;
+    const int j = WHOLE ? block >> 2 : block & 3, q = WHOLE ? block & 3 : block >> 2;
+    uint8_t *at = to + q * 128 + j * 16 + half * 2;
 #pragma unroll
     for (int d = 0; d < 4; ++d) {
         const uint32_t flip = d == 0 ? 0u : 0x8080u;
         const uint32_t sel = (3 - d) | (7 - d) << 4;
-        *reinterpret_cast<uint16_t *>(at + d * plane) = (uint16_t)(__byte_perm(v[0], v[2], sel) ^ flip);
-        *reinterpret_cast<uint16_t *>(at + d * plane + 4) = (uint16_t)(__byte_perm(v[1], v[3], sel) ^ flip);
+        uint8_t *digit = at + (d & 1) * 64 + (d >> 1) * 4;
+        *reinterpret_cast<uint16_t *>(digit) = (uint16_t)(__byte_perm(v[0], v[2], sel) ^ flip);
+        *reinterpret_cast<uint16_t *>(digit + 8) = (uint16_t)(__byte_perm(v[1], v[3], sel) ^ flip);
     }
     *lost = __any_sync(~0u, rest);
     if (__any_sync(~0u, bad)) return __uint_as_float(0x7FC00000u);
-    return up <= 126 ? __uint_as_float((uint32_t)(127 - up) << 23) : __uint_as_float(1u << (149 - up));
+    return __uint_as_float((uint32_t)(151 - up) << 23);       // 2^(24 - up)
 }
 
 constexpr int PREPARE_WARPS = 8;
@@ -268,8 +270,7 @@ template <int XT, bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 
         }
     }
     bool lost;
-    const int64_t plane = (int64_t)p.chunks_in * 128;
-    const float step = make_digits<WHOLE>(f, p.w.x_digits + t * 4 * plane + c * 128, plane, &lost);
+    const float step = make_digits<WHOLE>(f, p.w.x_digits + (int64_t)i * 512, &lost);
     if (lane == 0) {
         p.w.x_step[i] = step;
         p.w.lost[i] = lost;
@@ -283,14 +284,14 @@ template <bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_
     grid_dependency_wait();
     grid_launch_dependents();
     if (i >= p.slots * p.chunks_out) return;
-    const int s = i / p.chunks_out, c = i - s * p.chunks_out;
-    const int64_t plane = (int64_t)p.chunks_out * 128;
-    const float4 v = *reinterpret_cast<const float4 *>(p.w.mid + s * plane + c * 128 + 4 * lane);
+    const float4 v = *reinterpret_cast<const float4 *>(p.w.mid + (int64_t)i * 128 + 4 * lane);
     const float f[4] = {v.x, v.y, v.z, v.w};
     bool lost;
-    const float step = make_digits<WHOLE>(f, p.w.mid_digits + s * 4 * plane + c * 128, plane, &lost);
+    const float step = make_digits<WHOLE>(f, p.w.mid_digits + (int64_t)i * 512, &lost);
     if (lane == 0) p.w.mid_step[i] = step;
 }
+
+constexpr int NT = 4;                 // tiles of eight columns that a warp has
 
 // ---- products ------------------------------------------------------------------------------
 // group of scales of a unit (dsq_wgemm_group.cuh)
@@ -315,27 +316,26 @@ template <int NT, int GP> struct Stage {
     static constexpr int W_BYTES = NT * 512, S_BYTES = (4 / GP) * NT * 32, BYTES = W_BYTES + S_BYTES;
 };
 
-// Copies of a chunk: column c of the stage is row(c) of the matrix of codes (negative: none).
-template <int NT, int GP, class Row>
-__device__ __forceinline__ void copy_chunk(uint32_t at, const uint8_t *W, int pitch, const float *scales, int64_t rows, int groups,
-                                           uint32_t units, uint32_t inv, int chunk, Row row)
-{
-    const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-    const int k_at = chunk * 64 + 16 * j;
+// A warp's copies of codes and scales, chunk by chunk.  (Columns behind the last are the last: their sums are not used.)
+template <int NT, int GP> struct Copies {
+    const uint8_t *w[NT];             // 16-byte piece j of this lane's columns, from the first chunk on
+    const float *scale;               // of the column whose scales this lane copies
+    __device__ __forceinline__ void operator()(uint32_t at, int chunk, int pitch, int64_t rows, int groups, uint32_t units, uint32_t inv) const
+    {
+        const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+        const uint32_t to = at + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
+        const int64_t from = chunk * 64;
+        const uint32_t bytes = chunk * 64 + 16 * j < pitch ? 16u : 0u;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        const int64_t r = row(8 * t + n);
-        const bool in = r >= 0 && k_at < pitch;
-        cp_async_16(at + t * 512 + n * 64 + ((j ^ (n >> 1)) & 3) * 16, in ? W + r * pitch + k_at : W, in ? 16u : 0u);
-    }
+        for (int t = 0; t < NT; ++t) cp_async_16(to + t * 512, bytes ? w[t] + from : w[t], bytes);
 #pragma unroll
-    for (int s = lane; s < (4 / GP) * NT * 8; s += 32) {
-        const int g = scale_of((uint32_t)(chunk * (4 / GP) + s / (8 * NT)), units, inv);
-        const int64_t r = row(s % (8 * NT));
-        const bool in = r >= 0 && g < groups;
-        cp_async_4(at + Stage<NT, GP>::W_BYTES + s * 4, in ? scales + (int64_t)g * rows + r : scales, in ? 4u : 0u);
+        for (int u = 0; u < 4 / GP; ++u) {
+            const int g = scale_of((uint32_t)(chunk * (4 / GP) + u), units, inv);
+            cp_async_4(at + Stage<NT, GP>::W_BYTES + u * NT * 32 + lane * 4, scale + (g < groups ? g * rows : 0), g < groups ? 4u : 0u);
+        }
     }
-}
+};
+static_assert(8 * NT == 32, "a lane a column's scales");
 
 // ---- digits
 __device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -356,11 +356,44 @@ __device__ __forceinline__ void mma_i8_first(int (&d)[4], const uint32_t (&a)[4]
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0x4B400000));
 }
 
-// What a lane has of a chunk's rows: row n (and n + 8) of a tile is digit n & 3 of its slot n / 4 (and 2 + n / 4); 32 bytes
-// of each, and the slots' steps.
+// What a lane has of a chunk's rows, a tile being four slots: digits n & 1 and (n & 1) + 2 of slot n / 2, and the step.
 template <int TILES> struct Digits {
-    uint4 x[TILES][2][2];
-    float step[TILES][2];
+    uint4 x[TILES][4];
+    float step[TILES];
+};
+// where they are: slot r of a group has its chunks of digits and steps at `digits` and `steps`, from the lane's place on
+template <int TILES> struct Sources {
+    const uint8_t *digits[TILES];
+    const float *steps[TILES];
+    __device__ __forceinline__ void set(int m, const uint8_t *d, const float *s)
+    {
+        const int lane = threadIdx.x & 31;
+        digits[m] = d ? d + (lane >> 2 & 1) * 64 + (lane & 3) * 16 : nullptr;
+        steps[m] = s;
+    }
+    // (rows of no slot stay zeros)
+    __device__ __forceinline__ void load(int chunk, Digits<TILES> &r) const
+    {
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+            if (digits[m]) {
+                const uint8_t *at = digits[m] + (int64_t)chunk * 512;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) r.x[m][q] = load_16(at + 128 * q);
+                r.step[m] = steps[m][chunk];
+            }
+    }
+    // Brings a chunk into L1, a line a lane of eight (the loads behind would wait for L2 with every register taken).
+    __device__ __forceinline__ void touch(int chunk) const
+    {
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+            if (digits[m]) {
+                const int lane = threadIdx.x & 31;
+                uint32_t none;
+                asm volatile("ld.global.u32 %0, [%1];" : "=r"(none) : "l"(digits[m] + (int64_t)chunk * 512 + (lane & 3) * 112));
+            }
+    }
 };
 
 // total += scale step (sum of digits times codes) of a chunk
@@ -385,23 +418,19 @@ __device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const
             const uint32_t b0 = ((w[q] << 4) & 0xF0F0F0F0u) | one, b1 = (w[q] & 0xF0F0F0F0u) | one;
 #pragma unroll
             for (int m = 0; m < TILES; ++m) {
-                const uint4 u = r.x[m][0][q >> 1], v = r.x[m][1][q >> 1];
-                const uint32_t a[4] = {q & 1 ? u.z : u.x, q & 1 ? v.z : v.x, q & 1 ? u.w : u.y, q & 1 ? v.w : v.y};
+                const uint32_t a[4] = {r.x[m][q].x, r.x[m][q].y, r.x[m][q].z, r.x[m][q].w};
                 if (q % GP == 0) mma_i8_first(acc[m], a, b0, b1);
                 else mma_i8(acc[m], a, b0, b1);
             }
             if (q % GP == GP - 1) {
                 const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
-                const float s0 = __uint_as_float(sv.x), s1 = __uint_as_float(sv.y);
 #pragma unroll
-                for (int m = 0; m < TILES; ++m)
+                for (int m = 0; m < TILES; ++m) {
+                    const float s0 = __uint_as_float(sv.x) * r.step[m], s1 = __uint_as_float(sv.y) * r.step[m];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float up = r.step[m][h];
-                        float &u = total[m][t][2 * h], &v = total[m][t][2 * h + 1];
-                        u = __fmaf_rn((__int_as_float(acc[m][2 * h]) - MAGIC) * up, s0, u);
-                        v = __fmaf_rn((__int_as_float(acc[m][2 * h + 1]) - MAGIC) * up, s1, v);
-                    }
+                    for (int e = 0; e < 4; ++e)
+                        total[m][t][e] = __fmaf_rn(__int_as_float(acc[m][e]) - MAGIC, e & 1 ? s1 : s0, total[m][t][e]);
+                }
             }
         }
     }
@@ -466,7 +495,6 @@ __device__ __forceinline__ float activated(float g, int act)
     return 0.5f * g * (1.f + tanhf(u));
 }
 
-constexpr int NT = 4;                 // tiles of eight columns that a warp has
 constexpr int IN_WARPS = 8, OUT_WARPS = 4;
 
 // What is behind a warp's sums of a group, shared by both forms: WC warps side by side on 16 columns of gate and
@@ -481,9 +509,7 @@ template <int XT, int GP, int WC, int STAGES> struct In {
     uint8_t *smem;
     int warp, lane, n, j, wk, c0, turns, to_turn, issued;
     uint32_t ring;
-    const uint8_t *src[NT];           // 16-byte piece j of the next chunk of this lane's columns
-    int col;                          // the scale that this lane copies is of this row (negative: none)
-    int64_t rows;
+    Copies<NT, GP> copies;
 
     __device__ __forceinline__ In(const MoeParams &p_, const Group &g_, uint8_t *smem_) : p(p_), g(g_), smem(smem_)
     {
@@ -492,19 +518,18 @@ template <int XT, int GP, int WC, int STAGES> struct In {
         c0 = (blockIdx.x * WC + warp % WC) * 16;
         turns = wk < p.chunks_in && (int)blockIdx.x * WC * 16 < p.I ? (p.chunks_in - wk - 1) / KW + 1 : 0;
         ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES);
-        rows = (int64_t)p.E * 2 * p.I;
         issued = 0;
-    }
-    // row of the matrix of codes that column c of the 32 is
-    __device__ __forceinline__ int64_t row(int c) const
-    {
-        return c0 + (c & 15) < p.I ? (int64_t)g.expert * 2 * p.I + c0 + (c & 15) + (c < 16 ? 0 : p.I) : (int64_t)-1;
+        // columns 0 .. 15 are the gate's, 16 .. 31 the other half's
+        auto row = [&](int c) { return (int64_t)g.expert * 2 * p.I + min(c0 + (c & 15), p.I - 1) + (c < 16 ? 0 : p.I); };
+#pragma unroll
+        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_in + row(8 * t + n) * p.pitch_in + 16 * j;
+        copies.scale = p.s_in + row(lane);
     }
     __device__ __forceinline__ void issue()
     {
         if (issued < turns)
-            copy_chunk<NT, GP>(ring + (uint32_t)(issued % STAGES * S::BYTES), p.W_in, p.pitch_in, p.s_in, rows, p.groups_in, p.units_in,
-                               p.units_in_inv, wk + issued * KW, [&](int c) { return row(c); });
+            copies(ring + (uint32_t)(issued % STAGES * S::BYTES), wk + issued * KW, p.pitch_in, (int64_t)p.E * 2 * p.I, p.groups_in,
+                   p.units_in, p.units_in_inv);
         ++issued;
         cp_async_commit();
     }
@@ -520,31 +545,17 @@ template <int XT, int GP, int WC, int STAGES> struct In {
     template <int TILES> __device__ __forceinline__ void digits()
     {
         const uint32_t one = p.odd ? 0x08080808u : 0u;
-        const uint8_t *x[TILES][2];
-        const float *step[TILES][2];
-        const int64_t plane = (int64_t)p.chunks_in * 128;
+        Sources<TILES> from;
+        Digits<TILES> d = {};
 #pragma unroll
-        for (int m = 0; m < TILES; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = 4 * m + 2 * h + (n >> 2);
-                const int token = r < g.n ? p.w.sorted[g.first + r] / p.k : -1;
-                x[m][h] = token < 0 ? nullptr : p.w.x_digits + (token * 4 + (n & 3)) * plane + 32 * j;
-                step[m][h] = p.w.x_step + (token < 0 ? 0 : token) * p.chunks_in;
-            }
-        Digits<TILES> d;
-        auto load = [&](int chunk) {
-#pragma unroll
-            for (int m = 0; m < TILES; ++m)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const bool on = x[m][h] && chunk < p.chunks_in;
-#pragma unroll
-                    for (int i = 0; i < 2; ++i) d.x[m][h][i] = on ? load_16(x[m][h] + chunk * 128 + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
-                    d.step[m][h] = on ? step[m][h][chunk] : 0.f;
-                }
-        };
-        load(wk);
+        for (int m = 0; m < TILES; ++m) {
+            const int r = 4 * m + (n >> 1);
+            const int token = r < g.n ? p.w.sorted[g.first + r] / p.k : -1;
+            if (token < 0) from.set(m, nullptr, nullptr);
+            else from.set(m, p.w.x_digits + (int64_t)token * p.chunks_in * 512, p.w.x_step + (int64_t)token * p.chunks_in);
+        }
+        if (turns > 0) from.load(wk, d);
+        if (turns > 1) from.touch(wk + KW);
         float total[TILES][NT][4] = {};
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
@@ -552,7 +563,8 @@ template <int XT, int GP, int WC, int STAGES> struct In {
             __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
             issue();
             multiply_digits<TILES, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), one, d, total);
-            load(wk + (i + 1) * KW);
+            if (i + 1 < turns) from.load(wk + (i + 1) * KW, d);
+            if (i + 2 < turns) from.touch(wk + (i + 2) * KW);
         }
         // the warps' sums, added in a fixed order
         cp_async_wait<0>();
@@ -573,14 +585,14 @@ template <int XT, int GP, int WC, int STAGES> struct In {
             for (int u = 0; u < 2; ++u) {
                 float v[4];
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int l = ((r & 1) * 4 + k) * 4 + ((c & 7) >> 1);
-                    const int at = (((r >> 2) * NT + 2 * u + ((c >> 3) & 1)) * 32 + l) * 4 + (r & 2) + (c & 1);
+                for (int k = 0; k < 4; ++k) {                  // digit k
+                    const int l = ((r & 3) * 2 + (k & 1)) * 4 + ((c & 7) >> 1);
+                    const int at = (((r >> 2) * NT + 2 * u + ((c >> 3) & 1)) * 32 + l) * 4 + (k & 2) + (c & 1);
                     v[k] = 0.f;
 #pragma unroll
                     for (int w = 0; w < KW; ++w) v[k] += sums[(w * WC + wc) * TILES * NT * 128 + at];
                 }
-                both[u] = __fmaf_rn(v[0], 16777216.f * unit, __fmaf_rn(v[1], 65536.f * unit, __fmaf_rn(v[2], 256.f * unit, v[3] * unit)));
+                both[u] = __fmaf_rn(v[3], 0x1p-24f, __fmaf_rn(v[2], 0x1p-16f, __fmaf_rn(v[1], 0x1p-8f, v[0]))) * unit;
             }
             put(r, c, both[0], both[1]);
         }
@@ -666,19 +678,25 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
     const int share = rank * KW + warp / WC, shares = cluster * KW;
     const int q0 = (int)(all * share / shares), q1 = (int)(all * (share + 1) / shares);
     int ig = q0 / chunks, ic = q0 - ig * chunks;                // of the next copy
+    Copies<NT, GP> copies;
+    auto columns_of = [&](int i) {
+        const int64_t row0 = (int64_t)(p.w.packed[i] & 1023) * p.H;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_out + (row0 + min(c0 + 8 * t + n, (int64_t)p.H - 1)) * p.pitch_out + 16 * j;
+        copies.scale = p.s_out + row0 + min(c0 + lane, (int64_t)p.H - 1);
+    };
     auto issue = [&](int i) {
         if (i < q1) {
-            const int64_t row0 = (int64_t)(p.w.packed[ig] & 1023) * p.H + c0;
-            copy_chunk<NT, GP>(ring + (uint32_t)((i - q0) % STAGES * S::BYTES), p.W_out, p.pitch_out, p.s_out, (int64_t)p.E * p.H,
-                               p.groups_out, p.units_out, p.units_out_inv, ic,
-                               [&](int c) { return c0 + c < p.H ? row0 + c : (int64_t)-1; });
+            copies(ring + (uint32_t)((i - q0) % STAGES * S::BYTES), ic, p.pitch_out, (int64_t)p.E * p.H, p.groups_out, p.units_out,
+                   p.units_out_inv);
             if (++ic == chunks) {
                 ic = 0;
-                ++ig;
+                if (i + 1 < q1) columns_of(++ig);
             }
         }
         cp_async_commit();
     };
+    if (q0 < q1) columns_of(ig);
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(q0 + s);
     __syncwarp();
@@ -686,41 +704,27 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
     grid_launch_dependents();
 
     Group g = {};
-    const uint8_t *x[2][2];
-    const float *step[2][2];
-    const int64_t plane = (int64_t)chunks * 128;
+    Sources<2> from;
+    Digits<2> d = {};
     int cg = q0 / chunks, cc = q0 - cg * chunks;                // of the chunk at hand
     auto rows_of = [&](int i) {
         g = group_at(p.w, i);
+        d = {};
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = 4 * m + 2 * h + (n >> 2);
-                const int slot = r < g.n ? p.w.sorted[g.first + r] : -1;
-                x[m][h] = slot < 0 ? nullptr : p.w.mid_digits + (slot * 4 + (n & 3)) * plane + 32 * j;
-                step[m][h] = p.w.mid_step + (slot < 0 ? 0 : slot) * chunks;
-            }
-    };
-    Digits<2> d;
-    auto load = [&](int chunk) {
-#pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-#pragma unroll
-                for (int i = 0; i < 2; ++i)
-                    d.x[m][h][i] = x[m][h] ? load_16(x[m][h] + chunk * 128 + 16 * i) : make_uint4(0u, 0u, 0u, 0u);
-                d.step[m][h] = x[m][h] ? step[m][h][chunk] : 0.f;
-            }
+        for (int m = 0; m < 2; ++m) {
+            const int r = 4 * m + (n >> 1);
+            const int slot = r < g.n ? p.w.sorted[g.first + r] : -1;
+            if (slot < 0) from.set(m, nullptr, nullptr);
+            else from.set(m, p.w.mid_digits + (int64_t)slot * chunks * 512, p.w.mid_step + (int64_t)slot * chunks);
+        }
     };
     if (q0 < q1) {
         rows_of(cg);
-        load(cc);
+        from.load(cc, d);
     }
     float total[2][NT][4] = {};
-    // what a row's digit stands for
-    const float place = (n & 3) == 0 ? 16777216.f : (n & 3) == 1 ? 65536.f : (n & 3) == 2 ? 256.f : 1.f;
+    // what a lane's digits n & 1 and (n & 1) + 2 stand for, in steps
+    const float high = n & 1 ? 0x1p-8f : 1.f, low = n & 1 ? 0x1p-24f : 0x1p-16f;
 #pragma unroll 1
     for (int i = q0; i < q1; ++i) {
         cp_async_wait<STAGES - 2>();
@@ -730,17 +734,15 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
         if (g.n <= 4) {
             Digits<1> d1;
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                d1.x[0][h][0] = d.x[0][h][0];
-                d1.x[0][h][1] = d.x[0][h][1];
-                d1.step[0][h] = d.step[0][h];
-            }
+            for (int q = 0; q < 4; ++q) d1.x[0][q] = d.x[0][q];
+            d1.step[0] = d.step[0];
             multiply_digits<1, NT, GP>(at, one, d1, reinterpret_cast<float (&)[1][NT][4]>(total));
         } else {
             multiply_digits<2, NT, GP>(at, one, d, total);
         }
         if (++cc < chunks && i + 1 < q1) {
-            load(cc);
+            from.load(cc, d);
+            if (cc + 1 < chunks && i + 2 < q1) from.touch(cc + 1);
             continue;
         }
         // the group's sums to the tokens' rows, one slot after the other (two may be the same token's)
@@ -750,24 +752,22 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = total[m][t][e] * place;
-                    v += __shfl_xor_sync(~0u, v, 4);
-                    v += __shfl_xor_sync(~0u, v, 8);
-                    total[m][t][e] = v;
+                for (int e = 0; e < 2; ++e) {
+                    const float v = __fmaf_rn(total[m][t][e + 2], low, total[m][t][e] * high);
+                    total[m][t][e] = v + __shfl_xor_sync(~0u, v, 4);
                 }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (4 * m + r >= g.n) break;
-                if (n == (r & 1) * 4) {
+                if (n == 2 * r) {
                     const int slot = p.w.sorted[g.first + 4 * m + r], token = slot / p.k;
                     const float w = p.weights[slot];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         float2 *to = reinterpret_cast<float2 *>(mine + token * WIDE + 8 * t + 2 * j);
                         float2 v = *to;
-                        v.x = __fmaf_rn(total[m][t][(r & 2)], w, v.x);
-                        v.y = __fmaf_rn(total[m][t][(r & 2) + 1], w, v.y);
+                        v.x = __fmaf_rn(total[m][t][0], w, v.x);
+                        v.y = __fmaf_rn(total[m][t][1], w, v.y);
                         *to = v;
                     }
                 }
@@ -784,7 +784,8 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
         }
         if (i + 1 < q1) {
             rows_of(cg);
-            load(cc);
+            from.load(cc, d);
+            if (cc + 1 < chunks && i + 2 < q1) from.touch(cc + 1);
         }
     }
     cp_async_wait<0>();
