@@ -16,6 +16,7 @@
 //     gradient) of its own unit in registers.
 //   * Heads or strides that are no multiple of a vector go element by element, 32 lanes a head.
 #include "dsq_launch.h"
+#include "dsq_pairs.cuh"
 #include "dsq_ptx.cuh"
 #include "dsq_tc_host.h"
 #include "dsq_types.cuh"
@@ -44,19 +45,29 @@ struct Params {
     int64_t tokens;
     int q_blocks, k_blocks;
     int D, R, axes, norm, lanes, units;
+    uint32_t half_inv;            // floor(2^32 / (R / 2)) + 1
     float eps, inv_d;
 };
 
-// cosine and sine of pos f
+// Cosine and sine of pos f: the angle and what it is beyond a whole number of quarter turns in binary64 (that number
+// below 2^51), then the two series at most pi / 4 away from 0, whose first terms left out are below 2^-29.
 __device__ __forceinline__ float2 turn_of(int64_t pos, float f)
 {
-    const double a = (double)pos * (double)f;
-    const double k = rint(a * 0.6366197723675814);           // quarter turns
+    constexpr double WHOLE = 6755399441055744.0;              // 1.5 2^52: the sum's low bits are the whole number
+    const double a = (double)pos * (double)f, k1 = fma(a, 0.6366197723675814, WHOLE), k = k1 - WHOLE;
     // pi / 2 in two parts
-    const double r = fma(-k, 6.123233995736766e-17, fma(-k, 1.5707963267948966, a));
-    float s, c;
-    sincosf((float)r, &s, &c);
-    const int q = (int)(fma(-4.0, floor(k * 0.25), k));       // k mod 4
+    const float r = (float)fma(-k, 6.123233995736766e-17, fma(-k, 1.5707963267948966, a));
+    const int q = __double2loint(k1) & 3;
+    const float x = r * r;
+    float c = __fmaf_rn(x, -1.f / 3628800.f, 1.f / 40320.f);
+    c = __fmaf_rn(x, c, -1.f / 720.f);
+    c = __fmaf_rn(x, c, 1.f / 24.f);
+    c = __fmaf_rn(x, c, -0.5f);
+    c = __fmaf_rn(x, c, 1.f);
+    float s = __fmaf_rn(x, 1.f / 362880.f, -1.f / 5040.f);
+    s = __fmaf_rn(x, s, 1.f / 120.f);
+    s = __fmaf_rn(x, s, -1.f / 6.f);
+    s = __fmaf_rn(x * r, s, r);
     float2 t;
     t.x = q & 1 ? s : c;
     t.y = q & 1 ? c : s;
@@ -65,45 +76,66 @@ __device__ __forceinline__ float2 turn_of(int64_t pos, float f)
     return t;
 }
 
-// Where pair i's turn lies among a token's: units' pairs 2 q, 2 q + 1 side by side over the units, so that the lanes
-// of a head read consecutive 16 bytes.
+// Where pair i's cosine lies among a token's values, and how far behind it the sine: of a unit's pairs 2 q, 2 q + 1 cosines and
+// sines side by side, units beside units, so that the lanes of a head read consecutive 16 bytes.
 template <int VEC> __device__ __forceinline__ int turn_at(int i, int units)
 {
-    return VEC == 1 ? i : ((i % VEC) / 2 * units + i / VEC) * 2 + (i & 1);
+    return VEC == 1 ? 2 * i : ((i % VEC) / 2 * units + i / VEC) * 4 + (i & 1);
 }
+template <int VEC> constexpr int SINE = VEC == 1 ? 1 : 2;
 
 // the turns of `n` tokens from token0 on
-template <int VEC> __device__ __forceinline__ void make_turns(const Params &p, int64_t token0, int n, float2 *turns)
+template <int VEC> __device__ __forceinline__ void make_turns(const Params &p, int64_t token0, int n, float *turns)
 {
     const int half = p.R / 2, units = half / VEC;
     for (int e = threadIdx.x; e < n * half; e += BLOCK) {
-        const int t = e / half, i = e - t * half;
+        const int t = half == 1 ? e : (int)__umulhi((uint32_t)e, p.half_inv), i = e - t * half;
         const int axis = p.axis ? p.axis[i] : 0;
         float2 v = make_float2(__int_as_float(0x7FC00000), __int_as_float(0x7FC00000));   // (no such axis: NaN)
         if (axis < p.axes) v = turn_of(p.pos[axis * p.tokens + token0 + t], p.freq[i]);
-        turns[t * half + turn_at<VEC>(i, units)] = v;
+        float *to = turns + t * p.R + turn_at<VEC>(i, units);
+        to[0] = v.x;
+        to[SINE<VEC>] = v.y;
     }
 }
 
-template <class T, int VEC> __device__ __forceinline__ void load_vec(const T *p, T (&v)[VEC])
+// a vector as it lies in memory, its elements two by two, and back
+template <class T, int VEC> struct Raw { uint4 v; };
+template <class T> struct Raw<T, 1> { T v; };
+template <class T, int VEC> __device__ __forceinline__ void load_vec(const T *p, Raw<T, VEC> &r)
 {
-    if constexpr (VEC == 1) v[0] = *p;
-    else {
-        uint4 r;
+    if constexpr (VEC == 1) r.v = *p;
+    else
         asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
-                     : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-        *reinterpret_cast<uint4 *>(v) = r;
+                     : "=r"(r.v.x), "=r"(r.v.y), "=r"(r.v.z), "=r"(r.v.w) : "l"(p));
+}
+template <class T, int VEC> __device__ __forceinline__ void clear(Raw<T, VEC> &r)
+{
+    if constexpr (VEC == 1) r.v = dsq_from_f32<T>(0.f);
+    else r.v = make_uint4(0u, 0u, 0u, 0u);
+}
+template <class T, int VEC> __device__ __forceinline__ void unpack(const Raw<T, VEC> &r, float *f)
+{
+    if constexpr (VEC == 1) f[0] = dsq_to_f32(r.v);
+    else if constexpr (sizeof(T) == 4) {
+        f[0] = __uint_as_float(r.v.x); f[1] = __uint_as_float(r.v.y);
+        f[2] = __uint_as_float(r.v.z); f[3] = __uint_as_float(r.v.w);
+    } else {
+        DsqRaw8<T> raw;
+        raw.v[0] = r.v;
+        float v[8];
+        dsq_unpack8(raw, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f[i] = v[i];
     }
 }
 template <class T, int VEC> __device__ __forceinline__ void store_vec(T *p, const float *f)
 {
     if constexpr (VEC == 1) *p = dsq_from_f32<T>(f[0]);
-    else {
-        alignas(16) T v[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) v[i] = dsq_from_f32<T>(f[i]);
-        *reinterpret_cast<uint4 *>(p) = *reinterpret_cast<const uint4 *>(v);
-    }
+    else if constexpr (sizeof(T) == 4) *reinterpret_cast<float4 *>(p) = make_float4(f[0], f[1], f[2], f[3]);
+    else
+        *reinterpret_cast<uint4 *>(p) = make_uint4(dsq_pair(f[0], f[1], T()), dsq_pair(f[2], f[3], T()),
+                                                   dsq_pair(f[4], f[5], T()), dsq_pair(f[6], f[7], T()));
 }
 
 // where the two vectors of unit u start; which of them exist, whether it is rotated
@@ -125,9 +157,15 @@ template <int VEC, bool INTER> __device__ __forceinline__ Unit unit_of(const Par
     return r;
 }
 
-__device__ __forceinline__ float lanes_sum(float v, int lanes)
+template <int L> __device__ __forceinline__ int lanes_of(const Params &p) { return L ? L : p.lanes; }
+template <int L> __device__ __forceinline__ float lanes_sum(float v, int lanes)
 {
-    for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (L) {
+#pragma unroll
+        for (int o = L >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    } else {
+        for (int o = lanes >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    }
     return v;
 }
 // heads of a tile (tile_of), a bit each
@@ -207,80 +245,108 @@ template <class T, bool BACK> __device__ __forceinline__ void wide_heads(const P
     }
 }
 
-// A lane's part of a head: U units, element i of vector v of unit u at (2 u + v) VEC + i.
-template <class T, int VEC, int U, bool INTER> struct Lane {
-    static constexpr int N = 2 * U * VEC;
+// A lane's part of a head: U units, element i of vector v of unit u at (2 u + v) VEC + i, two by two.
+// L: lanes of a head, each with all its units and all of them turned; 0: p.lanes, any.
+template <class T, int VEC, int U, bool INTER, int L> struct Lane {
+    static constexpr int N = 2 * U * VEC, P = N / 2;
     Unit unit[U];
-    float w[N];
+    DsqPair w[P];
     __device__ __forceinline__ void init(const Params &p, const Tensor &t, int lane)
     {
+        float v[N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            unit[u] = unit_of<VEC, INTER>(p, lane + u * p.lanes);
-            if (lane + u * p.lanes >= p.units) unit[u].has_a = unit[u].has_b = unit[u].turned = false;
+            unit[u] = unit_of<VEC, INTER>(p, lane + u * lanes_of<L>(p));
+            if (L) unit[u].has_a = unit[u].has_b = unit[u].turned = true;
+            else if (lane + u * p.lanes >= p.units) unit[u].has_a = unit[u].has_b = unit[u].turned = false;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                w[2 * u * VEC + i] = t.w && unit[u].has_a ? __ldg(t.w + unit[u].a + i) : 1.f;
-                w[(2 * u + 1) * VEC + i] = t.w && unit[u].has_b ? __ldg(t.w + unit[u].b + i) : 1.f;
+                v[2 * u * VEC + i] = t.w && unit[u].has_a ? __ldg(t.w + unit[u].a + i) : 1.f;
+                v[(2 * u + 1) * VEC + i] = t.w && unit[u].has_b ? __ldg(t.w + unit[u].b + i) : 1.f;
             }
         }
+#pragma unroll
+        for (int i = 0; i < P; ++i) w[i] = dsq_pair_of(v[2 * i], v[2 * i + 1]);
     }
     // (what does not exist is zero)
-    __device__ __forceinline__ void load(const T *row, bool on, T (&r)[U][2][VEC]) const
+    __device__ __forceinline__ void load(const T *row, bool on, Raw<T, VEC> (&r)[U][2]) const
     {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-#pragma unroll
-            for (int i = 0; i < VEC; ++i) r[u][0][i] = r[u][1][i] = dsq_from_f32<T>(0.f);
-            if (on && unit[u].has_a) load_vec<T, VEC>(row + unit[u].a, r[u][0]);
-            if (on && unit[u].has_b) load_vec<T, VEC>(row + unit[u].b, r[u][1]);
-        }
-    }
-    __device__ __forceinline__ static void values(const T (&r)[U][2][VEC], float (&f)[N])
-    {
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = dsq_to_f32(r[i / (2 * VEC)][i / VEC % 2][i % VEC]);
-    }
-    __device__ __forceinline__ void store(T *row, const float (&f)[N]) const
-    {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (unit[u].has_a) store_vec<T, VEC>(row + unit[u].a, f + 2 * u * VEC);
-            if (unit[u].has_b) store_vec<T, VEC>(row + unit[u].b, f + (2 * u + 1) * VEC);
-        }
-    }
-    // turns the pairs, forwards (dir = 1) or back (-1)
-    __device__ __forceinline__ void turn(float (&f)[N], const float2 *turns, int lane, const Params &p, float dir) const
-    {
-        const int turned = p.R / (2 * VEC);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (!unit[u].turned) continue;
-            const int at = lane + u * p.lanes;
-#pragma unroll
-            for (int j = 0; j < VEC; j += 2) {
-                float2 t[2];
-                if constexpr (VEC == 1) t[0] = turns[at];
-                else {
-                    const float4 v = *reinterpret_cast<const float4 *>(turns + (j / 2 * turned + at) * 2);
-                    t[0] = make_float2(v.x, v.y);
-                    t[1] = make_float2(v.z, v.w);
+            if (L) {                                           // (rows behind the last: whatever is there is not used)
+                if (on) {
+                    load_vec(row + unit[u].a, r[u][0]);
+                    load_vec(row + unit[u].b, r[u][1]);
                 }
+                continue;
+            }
+            clear(r[u][0]);
+            clear(r[u][1]);
+            if (on && unit[u].has_a) load_vec(row + unit[u].a, r[u][0]);
+            if (on && unit[u].has_b) load_vec(row + unit[u].b, r[u][1]);
+        }
+    }
+    __device__ __forceinline__ static void values(const Raw<T, VEC> (&r)[U][2], DsqPair (&f)[P])
+    {
+        float v[N];
 #pragma unroll
-                for (int h = 0; h < (VEC == 1 ? 1 : 2); ++h) {
-                    const int i = j + h;                       // the unit's i-th pair
-                    float &f1 = f[2 * u * VEC + (INTER ? 2 * i : i)];
-                    float &f2 = f[2 * u * VEC + (INTER ? 2 * i + 1 : VEC + i)];
-                    const float c = t[h].x, s = t[h].y * dir, a = f1, b = f2;
-                    f1 = __fmaf_rn(a, c, -(b * s));
-                    f2 = __fmaf_rn(b, c, a * s);
+        for (int i = 0; i < 2 * U; ++i) unpack(r[i / 2][i % 2], v + i * VEC);
+#pragma unroll
+        for (int i = 0; i < P; ++i) f[i] = dsq_pair_of(v[2 * i], v[2 * i + 1]);
+    }
+    __device__ __forceinline__ void store(T *row, const DsqPair (&f)[P]) const
+    {
+        float v[N];
+#pragma unroll
+        for (int i = 0; i < P; ++i) dsq_halves(f[i], v[2 * i], v[2 * i + 1]);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (L || unit[u].has_a) store_vec<T, VEC>(row + unit[u].a, v + 2 * u * VEC);
+            if (L || unit[u].has_b) store_vec<T, VEC>(row + unit[u].b, v + (2 * u + 1) * VEC);
+        }
+    }
+    // turns the pairs, forwards or back; turns: the token's
+    template <bool BACK> __device__ __forceinline__ void turn(DsqPair (&f)[P], const float *turns, int lane, const Params &p) const
+    {
+        const int turned = L ? L * U : p.R / (2 * VEC);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (!L && !unit[u].turned) continue;
+            const int at = lane + u * lanes_of<L>(p);
+            if constexpr (VEC == 1) {                          // f[u] is the unit's pair
+                float a, b;
+                dsq_halves(f[u], a, b);
+                const float2 t = *reinterpret_cast<const float2 *>(turns + 2 * at);
+                const float s = BACK ? -t.y : t.y;
+                f[u] = dsq_pair_of(__fmaf_rn(a, t.x, -(b * s)), __fmaf_rn(b, t.x, a * s));
+            } else {
+#pragma unroll
+                for (int j = 0; j < VEC; j += 2) {
+                    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(turns + (j / 2 * turned + at) * 4);
+                    const DsqPair c = v.x, s = BACK ? dsq_pair_neg(v.y) : v.y;
+                    if constexpr (INTER) {                     // f[u VEC + j], f[u VEC + j + 1]: pairs j and j + 1
+                        float a0, b0, a1, b1;
+                        dsq_halves(f[u * VEC + j], a0, b0);
+                        dsq_halves(f[u * VEC + j + 1], a1, b1);
+                        const DsqPair a = dsq_pair_of(a0, a1), b = dsq_pair_of(b0, b1);
+                        const DsqPair y1 = dsq_pair_fma(a, c, dsq_pair_neg(dsq_pair_mul(b, s)));
+                        const DsqPair y2 = dsq_pair_fma(b, c, dsq_pair_mul(a, s));
+                        dsq_halves(y1, a0, a1);
+                        dsq_halves(y2, b0, b1);
+                        f[u * VEC + j] = dsq_pair_of(a0, b0);
+                        f[u * VEC + j + 1] = dsq_pair_of(a1, b1);
+                    } else {                                   // first and second elements VEC / 2 pairs apart
+                        const DsqPair a = f[u * VEC + j / 2], b = f[u * VEC + VEC / 2 + j / 2];
+                        f[u * VEC + j / 2] = dsq_pair_fma(a, c, dsq_pair_neg(dsq_pair_mul(b, s)));
+                        f[u * VEC + VEC / 2 + j / 2] = dsq_pair_fma(b, c, dsq_pair_mul(a, s));
+                    }
                 }
             }
         }
     }
 };
 
-// The heads of a tile of tokens, a head to L lanes: which one a thread has, and the next.
+// The heads of a tile of tokens, a head to L lanes: which one a thread has, and the next, `step` heads on.
 struct Place {
     int row, token, head;
     __device__ __forceinline__ void to(const Tensor &t, int r)
@@ -290,135 +356,177 @@ struct Place {
         head = r - token * t.heads;
     }
 };
-
-template <class T, int VEC, int U, bool INTER>
-__global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 2 : 4) heads_fwd_kernel(const __grid_constant__ Params p)
+// an address that goes with it
+template <class T> struct Walk {
+    T *at;
+    int64_t go, back;                 // for `step` heads on; more where that passes a token's last head
+    __device__ __forceinline__ Walk(T *base, int64_t token0, const Place &l, const Place &step, int heads, int64_t token, int64_t head)
+    {
+        at = base + (token0 + l.token) * token + l.head * head;
+        go = step.token * token + step.head * head;
+        back = token - heads * head;
+    }
+    __device__ __forceinline__ void next(bool over) { at += over ? go + back : go; }
+};
+__device__ __forceinline__ bool advance(Place &l, const Place &step, int heads)
 {
-    using L = Lane<T, VEC, U, INTER>;
-    extern __shared__ __align__(16) float2 turns[];
+    l.row += step.row;
+    l.token += step.token;
+    l.head += step.head;
+    const bool over = l.head >= heads;
+    if (over) {
+        l.head -= heads;
+        ++l.token;
+    }
+    return over;
+}
+__device__ __forceinline__ float sum_of(DsqPair v)
+{
+    float a, b;
+    dsq_halves(v, a, b);
+    return a + b;
+}
+
+template <class T, int VEC, int U, bool INTER, int L_>
+__global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 2 : 3) heads_fwd_kernel(const __grid_constant__ Params p)
+{
+    using L = Lane<T, VEC, U, INTER, L_>;
+    extern __shared__ __align__(16) float turns[];
     __shared__ uint32_t marks[MARKS];
     const bool second = (int)blockIdx.x >= p.q_blocks;
     const Tensor &t = p.t[second];
     const int64_t token0 = (int64_t)(blockIdx.x - (second ? p.q_blocks : 0)) * t.tile;
     const int n = (int)min((int64_t)t.tile, p.tokens - token0), rows = n * t.heads;
-    const int lane = threadIdx.x & (p.lanes - 1), step = BLOCK / p.lanes;
+    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), step = BLOCK / lanes;
     grid_dependency_wait();
     grid_launch_dependents();
     L l;
     l.init(p, t, lane);
-    Place at = {};
-    T next[U][2][VEC];
-    auto load = [&]() {
-        l.load((const T *)t.x + (token0 + at.token) * t.x_token + at.head * t.x_head, at.row < rows, next);
-    };
-    at.to(t, threadIdx.x / p.lanes);
-    load();
+    Place at, by;
+    at.to(t, threadIdx.x / lanes);
+    by.to(t, step);
+    Walk<const T> x((const T *)t.x, token0, at, by, t.heads, t.x_token, t.x_head);
+    Walk<T> y((T *)t.y, token0, at, by, t.heads, t.y_token, t.y_head);
+    Raw<T, VEC> next[U][2];
+    l.load(x.at, at.row < rows, next);
     bool any = false;
     for (int i = threadIdx.x; i < MARKS; i += BLOCK) marks[i] = 0u;
     make_turns<VEC>(p, token0, n, turns);
     __syncthreads();
     // (a warp's lanes go round together: the sums are over lanes)
-    for (int first = (threadIdx.x & ~31) / p.lanes; first < rows; first += step) {
-        float f[L::N];
+    for (int first = (threadIdx.x & ~31) / lanes; first < rows; first += step) {
+        DsqPair f[L::P];
         L::values(next, f);
-        const Place here = at;
-        bool on = here.row < rows;
-        at.to(t, at.row + step);
-        load();
+        const int row = at.row;
+        const float *turn = turns + at.token * (L_ ? 2 * L_ * U * VEC : p.R);
+        T *to = y.at;
+        bool on = row < rows;
+        const bool over = advance(at, by, t.heads);
+        x.next(over);
+        y.next(over);
+        l.load(x.at, at.row < rows, next);
         if (p.norm) {
-            float sum = 0.f;
+            DsqPair sum = 0ull;
 #pragma unroll
-            for (int i = 0; i < L::N; ++i) sum = __fmaf_rn(f[i], f[i], sum);
-            const float mean = __fmaf_rn(lanes_sum(sum, p.lanes), p.inv_d, p.eps);
-            const float rstd = 1.f / sqrtf(mean);
+            for (int i = 0; i < L::P; ++i) sum = dsq_pair_fma(f[i], f[i], sum);
+            const float mean = __fmaf_rn(lanes_sum<L_>(sum_of(sum), p.lanes), p.inv_d, p.eps);
+            const float rstd = rsqrtf(mean);
             const bool bad = on && !in_range(mean);
             if (bad) {
-                if (lane == 0) atomicOr(&marks[here.row >> 5], 1u << (here.row & 31));
+                if (lane == 0) atomicOr(&marks[row >> 5], 1u << (row & 31));
                 on = false;
                 any = true;
             }
+            const DsqPair r = dsq_pair_of(rstd, rstd);
 #pragma unroll
-            for (int i = 0; i < L::N; ++i) f[i] = f[i] * rstd * l.w[i];
+            for (int i = 0; i < L::P; ++i) f[i] = dsq_pair_mul(dsq_pair_mul(f[i], r), l.w[i]);
         }
         if (on) {
-            l.turn(f, turns + here.token * (p.R / 2), lane, p, 1.f);
-            l.store((T *)t.y + (token0 + here.token) * t.y_token + here.head * t.y_head, f);
+            l.template turn<false>(f, turn, lane, p);
+            l.store(to, f);
         }
     }
     if (__syncthreads_or(any)) wide_heads<T, false>(p, t, token0, rows, marks, INTER, nullptr);
 }
 
-template <class T, int VEC, int U, bool INTER>
+template <class T, int VEC, int U, bool INTER, int L_>
 __global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 1 : 2) heads_bwd_kernel(const __grid_constant__ Params p)
 {
-    using L = Lane<T, VEC, U, INTER>;
-    extern __shared__ __align__(16) float2 turns[];
+    using L = Lane<T, VEC, U, INTER, L_>;
+    extern __shared__ __align__(16) float turns[];
     __shared__ float sums[BLOCK / 32][MAX_DIM];
     __shared__ uint32_t marks[MARKS];
     const bool second = (int)blockIdx.x >= p.q_blocks;
     const Tensor &t = p.t[second];
     const int block = blockIdx.x - (second ? p.q_blocks : 0), blocks = second ? p.k_blocks : p.q_blocks;
-    const int lane = threadIdx.x & (p.lanes - 1), step = BLOCK / p.lanes;
+    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), step = BLOCK / lanes;
     grid_dependency_wait();
     grid_launch_dependents();
     L l;
     l.init(p, t, lane);
-    float gw[L::N];
+    DsqPair gw[L::P];
 #pragma unroll
-    for (int i = 0; i < L::N; ++i) gw[i] = 0.f;
+    for (int i = 0; i < L::P; ++i) gw[i] = 0ull;
     for (int c = threadIdx.x & 31; c < p.D; c += 32) sums[threadIdx.x >> 5][c] = 0.f;
     for (int i = threadIdx.x; i < MARKS; i += BLOCK) marks[i] = 0u;
     __syncthreads();
 
     for (int64_t token0 = (int64_t)block * t.tile; token0 < p.tokens; token0 += (int64_t)blocks * t.tile) {
         const int n = (int)min((int64_t)t.tile, p.tokens - token0), rows = n * t.heads;
-        Place at = {};
-        T next_x[U][2][VEC], next_g[U][2][VEC];
-        auto load = [&]() {
-            l.load((const T *)t.gy + (token0 + at.token) * t.g_token + at.head * t.g_head, at.row < rows, next_g);
-            l.load((const T *)t.x + (token0 + at.token) * t.x_token + at.head * t.x_head, p.norm && at.row < rows, next_x);
-        };
-        at.to(t, threadIdx.x / p.lanes);
-        load();
+        Place at, by;
+        at.to(t, threadIdx.x / lanes);
+        by.to(t, step);
+        Walk<const T> gy((const T *)t.gy, token0, at, by, t.heads, t.g_token, t.g_head);
+        Walk<const T> in((const T *)t.x, token0, at, by, t.heads, t.x_token, t.x_head);
+        Walk<T> out((T *)t.y, token0, at, by, t.heads, t.y_token, t.y_head);
+        Raw<T, VEC> next_x[U][2], next_g[U][2];
+        l.load(gy.at, at.row < rows, next_g);
+        l.load(in.at, p.norm && at.row < rows, next_x);
         bool any = false;
         make_turns<VEC>(p, token0, n, turns);
         __syncthreads();
-        for (int first = (threadIdx.x & ~31) / p.lanes; first < rows; first += step) {
-            float g[L::N], x[L::N];
+        for (int first = (threadIdx.x & ~31) / lanes; first < rows; first += step) {
+            DsqPair g[L::P], x[L::P];
             L::values(next_g, g);
             L::values(next_x, x);
-            const Place here = at;
-            bool on = here.row < rows;
-            at.to(t, at.row + step);
-            load();
-            if (on) l.turn(g, turns + here.token * (p.R / 2), lane, p, -1.f);
+            const int row = at.row;
+            const float *turn = turns + at.token * (L_ ? 2 * L_ * U * VEC : p.R);
+            T *to = out.at;
+            bool on = row < rows;
+            const bool over = advance(at, by, t.heads);
+            gy.next(over);
+            in.next(over);
+            out.next(over);
+            l.load(gy.at, at.row < rows, next_g);
+            l.load(in.at, p.norm && at.row < rows, next_x);
+            if (on) l.template turn<true>(g, turn, lane, p);
             if (p.norm) {
-                float sum = 0.f, dot = 0.f;
+                DsqPair sum2 = 0ull, dot2 = 0ull;
 #pragma unroll
-                for (int i = 0; i < L::N; ++i) {
-                    sum = __fmaf_rn(x[i], x[i], sum);
-                    dot = __fmaf_rn(g[i] * l.w[i], x[i], dot);
+                for (int i = 0; i < L::P; ++i) {
+                    sum2 = dsq_pair_fma(x[i], x[i], sum2);
+                    dot2 = dsq_pair_fma(dsq_pair_mul(g[i], l.w[i]), x[i], dot2);
                 }
-                sum = lanes_sum(sum, p.lanes);
-                dot = lanes_sum(dot, p.lanes);
-                const float mean = __fmaf_rn(sum, p.inv_d, p.eps), rstd = 1.f / sqrtf(mean);
+                const float sum = lanes_sum<L_>(sum_of(sum2), p.lanes), dot = lanes_sum<L_>(sum_of(dot2), p.lanes);
+                const float mean = __fmaf_rn(sum, p.inv_d, p.eps), rstd = rsqrtf(mean);
                 const bool bad = on && !in_range(mean);
                 if (bad) {
-                    if (lane == 0) atomicOr(&marks[here.row >> 5], 1u << (here.row & 31));
+                    if (lane == 0) atomicOr(&marks[row >> 5], 1u << (row & 31));
                     on = false;
                     any = true;
                 }
                 if (on) {
                     const float c = dot * rstd * p.inv_d;
+                    const DsqPair r = dsq_pair_of(rstd, rstd), less = dsq_pair_of(-c, -c);
 #pragma unroll
-                    for (int i = 0; i < L::N; ++i) {
-                        const float m = x[i] * rstd;
-                        gw[i] = __fmaf_rn(g[i], m, gw[i]);
-                        g[i] = rstd * __fmaf_rn(-m, c, g[i] * l.w[i]);
+                    for (int i = 0; i < L::P; ++i) {
+                        const DsqPair m = dsq_pair_mul(x[i], r);
+                        gw[i] = dsq_pair_fma(g[i], m, gw[i]);
+                        g[i] = dsq_pair_mul(r, dsq_pair_fma(m, less, dsq_pair_mul(g[i], l.w[i])));
                     }
                 }
             }
-            if (on) l.store((T *)t.y + (token0 + here.token) * t.y_token + here.head * t.y_head, g);
+            if (on) l.store(to, g);
         }
         // (and the turns have been read)
         if (__syncthreads_or(any)) wide_heads<T, true>(p, t, token0, rows, marks, INTER, sums[threadIdx.x >> 5]);
@@ -428,11 +536,13 @@ __global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 1 : 2) heads_bwd_kernel(c
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < L::N; ++i) {
-        float s = gw[i];
-        for (int o = 16; o >= p.lanes; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
+        float half[2];
+        dsq_halves(gw[i / 2], half[0], half[1]);
+        float s = half[i % 2];
+        for (int o = 16; o >= lanes; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
         const Unit &u = l.unit[i / (2 * VEC)];
         const bool b = i / VEC % 2;
-        if ((threadIdx.x & 31) < p.lanes && (b ? u.has_b : u.has_a)) sums[threadIdx.x >> 5][(b ? u.b : u.a) + i % VEC] += s;
+        if ((threadIdx.x & 31) < lanes && (b ? u.has_b : u.has_a)) sums[threadIdx.x >> 5][(b ? u.b : u.a) + i % VEC] += s;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.D; c += BLOCK) {
@@ -510,15 +620,6 @@ int check_rotary(const dsq_rotary_t *r, int64_t tokens, int dtype, float eps)
 
 template <class T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
 
-// Fills in what depends on the vectors' length.
-void set_lanes(Params &p, int vec)
-{
-    const int turned = p.R / (2 * vec), rest = (p.D - p.R + 2 * vec - 1) / (2 * vec);
-    p.units = turned + rest;
-    p.lanes = 1;
-    while (p.lanes < p.units && p.lanes < 32) p.lanes *= 2;
-}
-
 // Tokens of a tile: `passes` rounds of a block's lanes, as far as their turns have room.
 int tile_of(const Params &p, int64_t heads, int passes)
 {
@@ -538,12 +639,12 @@ size_t turn_bytes(const Params &p)
 
 constexpr int SUM_BLOCKS_PER_SM = 4;
 
-template <class T, int VEC, int U, bool INTER> int launch(Params &p, bool back, cudaStream_t s)
+template <class T, int VEC, int U, bool INTER, int L, bool BACK> int launch(Params &p, cudaStream_t s)
 {
     const int pdl = dsq_launch_hooks().pdl;
     const int64_t sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     const int64_t rows = p.tokens * (p.t[0].heads + p.t[1].heads), round = BLOCK / p.lanes;
-    if (!back) {
+    if constexpr (!BACK) {
         // as many rounds a block as leave some blocks for every place on an SM
         int passes = (int)(rows / (round * sms * 16));
         passes = passes < 1 ? 1 : passes > MAX_PASSES ? MAX_PASSES : passes;
@@ -556,49 +657,63 @@ template <class T, int VEC, int U, bool INTER> int launch(Params &p, bool back, 
         if (blocks[0] + blocks[1] > 0x7FFFFFFF) return DSQ_ERR_SIZE;
         p.q_blocks = (int)blocks[0];
         p.k_blocks = (int)blocks[1];
-        return dsq_launch(heads_fwd_kernel<T, VEC, U, INTER>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
+        return dsq_launch(heads_fwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
+                          turn_bytes(p), s, pdl, 0, p);
+    } else {
+        // what is resident together, shared among q and k as their rows are
+        int64_t most = sms * SUM_BLOCKS_PER_SM, blocks[2] = {0, 0};
+        for (int i = 0; i < 2; ++i) {
+            if (!p.t[i].heads) continue;
+            p.t[i].tile = tile_of(p, p.t[i].heads, 2);
+            const int64_t tiles = (p.tokens + p.t[i].tile - 1) / p.t[i].tile;
+            int64_t share = most * p.t[i].heads / (p.t[0].heads + p.t[1].heads);
+            if (share < 1) share = 1;
+            blocks[i] = tiles < share ? tiles : share;
+        }
+        p.q_blocks = (int)blocks[0];
+        p.k_blocks = (int)blocks[1];
+        if (p.t[1].part) p.t[1].part = p.t[0].part + blocks[0] * p.D;
+        return dsq_launch(heads_bwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
                           turn_bytes(p), s, pdl, 0, p);
     }
-    // what is resident together, shared among q and k as their rows are
-    int64_t most = sms * SUM_BLOCKS_PER_SM, blocks[2] = {0, 0};
-    for (int i = 0; i < 2; ++i) {
-        if (!p.t[i].heads) continue;
-        p.t[i].tile = tile_of(p, p.t[i].heads, 2);
-        const int64_t tiles = (p.tokens + p.t[i].tile - 1) / p.t[i].tile;
-        int64_t share = most * p.t[i].heads / (p.t[0].heads + p.t[1].heads);
-        if (share < 1) share = 1;
-        blocks[i] = tiles < share ? tiles : share;
-    }
-    p.q_blocks = (int)blocks[0];
-    p.k_blocks = (int)blocks[1];
-    if (p.t[1].part) p.t[1].part = p.t[0].part + blocks[0] * p.D;
-    return dsq_launch(heads_bwd_kernel<T, VEC, U, INTER>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
-                      turn_bytes(p), s, pdl, 0, p);
 }
 
-template <class T> int pick(Params &p, bool back, bool vectors, bool inter, cudaStream_t s)
+// Fills in what depends on the vectors' length and the units of a lane.
+void set_lanes(Params &p, int vec, int per_lane)
 {
-    constexpr int V = vec_of<T>();
-    set_lanes(p, vectors ? V : 1);
-    const int per_lane = (p.units + p.lanes - 1) / p.lanes;
-#define FORM(VEC, U) return inter ? launch<T, VEC, U, true>(p, back, s) : launch<T, VEC, U, false>(p, back, s)
-    if (vectors) {
-        if constexpr (V == 4) {
-            if (per_lane == 2) FORM(V, 2);
-        }
-        FORM(V, 1);
-    }
-    if (per_lane <= 2) FORM(1, 2);
-    FORM(1, 8);
-#undef FORM
+    const int turned = p.R / (2 * vec), rest = (p.D - p.R + 2 * vec - 1) / (2 * vec);
+    p.units = turned + rest;
+    p.lanes = 1;
+    while (p.lanes * per_lane < p.units && p.lanes < 32) p.lanes *= 2;
 }
 
-int start(Params &p, bool back, bool vectors, bool inter, int dtype, cudaStream_t s)
+// Two units a lane forwards and one back (where sums of the weights' gradient take their registers), or as
+// many as 32 lanes need.
+template <class T, bool INTER, bool BACK> int pick(Params &p, bool vectors, cudaStream_t s)
+{
+    constexpr int V = vec_of<T>(), U = BACK ? 1 : 2;
+    if (!vectors) {
+        set_lanes(p, 1, 1);
+        return p.units <= 64 ? launch<T, 1, 2, INTER, 0, BACK>(p, s) : launch<T, 1, 8, INTER, 0, BACK>(p, s);
+    }
+    set_lanes(p, V, U);
+    if (p.R == p.D && p.lanes * U == p.units) {
+        if (p.lanes == 16 / U) return launch<T, V, U, INTER, 16 / U, BACK>(p, s);
+        if (p.lanes == 8 / U) return launch<T, V, U, INTER, 8 / U, BACK>(p, s);
+        if (p.lanes == 4 / U) return launch<T, V, U, INTER, 4 / U, BACK>(p, s);
+    }
+    if constexpr (BACK && V == 4) {
+        if (p.units > 32) return launch<T, V, 2, INTER, 0, BACK>(p, s);
+    }
+    return launch<T, V, U, INTER, 0, BACK>(p, s);
+}
+
+template <bool BACK> int start(Params &p, bool vectors, bool inter, int dtype, cudaStream_t s)
 {
     switch (dtype) {
-    case DSQ_F32: return pick<float>(p, back, vectors, inter, s);
-    case DSQ_BF16: return pick<__nv_bfloat16>(p, back, vectors, inter, s);
-    default: return pick<__half>(p, back, vectors, inter, s);
+    case DSQ_F32: return inter ? pick<float, true, BACK>(p, vectors, s) : pick<float, false, BACK>(p, vectors, s);
+    case DSQ_BF16: return inter ? pick<__nv_bfloat16, true, BACK>(p, vectors, s) : pick<__nv_bfloat16, false, BACK>(p, vectors, s);
+    default: return inter ? pick<__half, true, BACK>(p, vectors, s) : pick<__half, false, BACK>(p, vectors, s);
     }
 }
 
@@ -608,6 +723,7 @@ void fill(Params &p, const dsq_rotary_t *r, int64_t tokens, int norm, float eps)
     p.pos = r->positions; p.freq = r->inv_freq; p.axis = r->axis;
     p.tokens = tokens;
     p.D = r->head_dim; p.R = r->rot_dim; p.axes = r->axes;
+    p.half_inv = p.R > 2 ? (uint32_t)((1ull << 32) / (uint64_t)(p.R / 2) + 1) : 0u;
     p.norm = norm != 0;
     p.eps = eps; p.inv_d = (float)(1.0 / r->head_dim);
 }
@@ -652,7 +768,7 @@ int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
         vectors = vectors && in_vectors(h->x, h->x_token, h->x_head, vec, size) &&
                   in_vectors(h->y, h->y_token, h->y_head, vec, size);
     }
-    return start(p, false, vectors, rotary->interleaved != 0, dtype, (cudaStream_t)stream);
+    return start<false>(p, vectors, rotary->interleaved != 0, dtype, (cudaStream_t)stream);
 }
 
 size_t dsq_headnorm_bwd_workspace_bytes(int64_t head_dim)
@@ -707,7 +823,7 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
     }
     if (sums && !dsq_aligned16(workspace)) return DSQ_ERR_ALIGN;
     if (sums && ws_bytes < dsq_headnorm_bwd_workspace_bytes(p.D)) return DSQ_ERR_SIZE;
-    st = start(p, true, vectors, rotary->interleaved != 0, dtype, (cudaStream_t)stream);
+    st = start<true>(p, vectors, rotary->interleaved != 0, dtype, (cudaStream_t)stream);
     if (st || !sums) return st;
     for (int i = 0; i < 2; ++i) sp.part[i] = p.t[i].part;
     sp.blocks[0] = p.q_blocks; sp.blocks[1] = p.k_blocks;

@@ -8,13 +8,17 @@
 // HBM-bound: the forward kernel reads the logits once, the backward one reads and writes them once.
 //   * Forward: a row goes to a block or, where there are few, to a cluster of up to eight, whose first
 //     block joins the parts.  A thread keeps m, s and t of its elements in one pass; four vectors are
-//     on their way together.
+//     on their way together.  The exponents are powers of two, x c - M with c = scale log2 e and M = m c as
+//     binary32 rounds it: one fused operation, the rounding of M being the same in s, t and the target's
+//     exponent.  Four instructions an element in all; where an element is -infinity, or M is large enough for its
+//     rounding to matter, (x - m) c instead, held above -1000 (six).
 //   * Alternatives: a thread's m says all there is to know of its elements but their order.  The block's
 //     threads form 128 groups; the top-th of the groups' largest elements bounds from below what can be among the
 //     first `top`, and only threads with an m above the bound read theirs again (from L2) and leave
 //     what passes in shared memory, where ranks are counted.  Order and ties are those of (value, lowest
 //     index), as one 64-bit key.
 #include "dsq_launch.h"
+#include "dsq_pairs.cuh"
 #include "dsq_ptx.cuh"
 #include "dsq_types.cuh"
 
@@ -22,11 +26,13 @@ using namespace dsq_ptx;
 
 namespace {
 
-constexpr int THREADS = 512, GROUPS = 128, MAX_TOP = 32, MAX_CLUSTER = 8, AHEAD = 4;
+constexpr int MAX_TOP = 32, MAX_CLUSTER = 8, AHEAD = 4, SHARE = 4;      // SHARE: threads of a group
 constexpr int ROOM = 1088;        // of candidates: 128 threads' vectors where fewer groups than `top` have any
 constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
-// what e^x of a lower power of two is zero
+// 2^x of what is lower is zero
 constexpr float NOTHING = -1000.f;
+// M is taken below this: its rounding is at most 2^-8 then
+constexpr float FAR = 65536.f;
 
 struct FwdParams {
     const void *x;
@@ -61,33 +67,6 @@ __device__ __forceinline__ float max_nan(float a, float b)
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-typedef unsigned long long f2;        // two binary32 values
-__device__ __forceinline__ f2 pack2(float a, float b)
-{
-    f2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpack2(f2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f2 add2(f2 a, f2 b)
-{
-    f2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 mul2(f2 a, f2 b)
-{
-    f2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ f2 fma2(f2 a, f2 b, f2 c)
-{
-    f2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 template <class T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
 
 __device__ __forceinline__ uint4 load_16(const void *p)
@@ -149,13 +128,27 @@ __device__ __forceinline__ float value_of(unsigned long long key)
 }
 __device__ __forceinline__ int index_of(unsigned long long key) { return (int)~(uint32_t)key; }
 
-// sums of elements less m, in powers of two: s, and t of the exponents' products
+// Sums of powers of two: s of 2^d, t of d 2^d, d = x c - M with M = m c rounded; where that is far, d = (x - m) c.
+// Sums are joined on the larger m.
 struct Sums { float m, s, t; };
+// what d of m' is less beside m: m' c - m c, each product as it is taken
+__device__ __forceinline__ float between(float from, float to, float c)
+{
+    const float F = from * c, T = to * c;
+    const bool f = fabsf(F) < FAR, t = fabsf(T) < FAR;
+    return max_nan(f ? (t ? F - T : __fmaf_rn(-to, c, F)) : t ? __fmaf_rn(from, c, -T) : (from - to) * c, NOTHING);
+}
+// the exponent of x beside m
+__device__ __forceinline__ float exponent(float x, float m, float c)
+{
+    const float M = m * c;
+    return max_nan(fabsf(M) < FAR ? __fmaf_rn(x, c, -M) : (x - m) * c, NOTHING);
+}
 __device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
 {
     Sums r;
     r.m = fmaxf(a.m, b.m);
-    const float da = max_nan((a.m - r.m) * c, NOTHING), db = max_nan((b.m - r.m) * c, NOTHING);
+    const float da = between(a.m, r.m, c), db = between(b.m, r.m, c);
     const float ea = ex2(da), eb = ex2(db);
     r.s = __fmaf_rn(a.s, ea, b.s * eb);
     r.t = __fmaf_rn(__fmaf_rn(a.s, da, a.t), ea, __fmaf_rn(b.s, db, b.t) * eb);
@@ -176,14 +169,15 @@ template <class T> struct Cut {
     __device__ __forceinline__ int single(int i) const { return i < head ? i : i + nv * vec_of<T>(); }
 };
 
-// Ranks of n keys, all different: f(rank, key) for each.
-template <class F> __device__ __forceinline__ void ranked(const unsigned long long *keys, int n, F f)
+// Ranks of n keys, all different: f(rank, key) for each, by one lane of the warp that counts.
+template <int THREADS, class F> __device__ __forceinline__ void ranked(const unsigned long long *keys, int n, F f)
 {
-    for (int i = threadIdx.x; i < n; i += THREADS) {
+    const int lane = threadIdx.x & 31;
+    for (int i = threadIdx.x >> 5; i < n; i += THREADS / 32) {
         const unsigned long long mine = keys[i];
         int rank = 0;
-        for (int j = 0; j < n; ++j) rank += keys[j] > mine;
-        f(rank, mine);
+        for (int j = 0; j < n; j += 32) rank += __popc(__ballot_sync(~0u, j + lane < n && keys[j + lane] > mine));
+        if (lane == 0) f(rank, mine);
     }
 }
 
@@ -192,10 +186,11 @@ __device__ __forceinline__ void st_cluster_64(uint32_t addr, unsigned long long 
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
 
-template <class T, bool TOP>
-__global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_constant__ FwdParams p)
+template <class T, bool TOP, int THREADS>
+__global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(const __grid_constant__ FwdParams p)
 {
-    constexpr int VEC = vec_of<T>();
+    constexpr int VEC = vec_of<T>(), GROUPS = THREADS / SHARE;
+    static_assert(GROUPS >= MAX_TOP, "a group for each of the first");
     __shared__ Sums warp_sums[THREADS / 32];
     __shared__ Sums block_sums[MAX_CLUSTER];
     __shared__ unsigned long long lists[TOP ? MAX_CLUSTER * MAX_TOP : 1];      // of the first block: all blocks' first `top`
@@ -228,53 +223,91 @@ __global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_co
             r[j] = v < v1 ? load_16(vecs + (int64_t)v * VEC) : nothing<T>();
         }
     };
-    const int turns = (v1 - v0 + THREADS * AHEAD - 1) / (THREADS * AHEAD);
+    const int turns = (v1 - v0 + THREADS * AHEAD - 1) / (THREADS * AHEAD), full = (v1 - v0) / (THREADS * AHEAD);
     float m = LOWEST;
     int best_turn = -1;
-    f2 s2 = 0ull, t2 = 0ull;
-    const f2 c2 = pack2(c, c);
+    DsqPair s2 = 0ull, t2 = 0ull;
+    const DsqPair c2 = dsq_pair_of(c, c);
+    // (x - m) c above NOTHING: any element
+    auto any_vector = [&](const uint4 &r) {
+        const bool near = fabsf(m * c) < FAR;
+        const DsqPair less = dsq_pair_of(-m, -m), lessM = dsq_pair_of(-(m * c), -(m * c));
+        float f[VEC];
+        values<T>(r, f);
+#pragma unroll
+        for (int i = 0; i < VEC; i += 2) {
+            const DsqPair x = dsq_pair_of(f[i], f[i + 1]);
+            const DsqPair d = near ? dsq_pair_fma(x, c2, lessM) : dsq_pair_mul(dsq_pair_add(x, less), c2);
+            float d0, d1;
+            dsq_halves(d, d0, d1);
+            d0 = max_nan(d0, NOTHING);
+            d1 = max_nan(d1, NOTHING);
+            const DsqPair e = dsq_pair_of(ex2(d0), ex2(d1));
+            s2 = dsq_pair_add(s2, e);
+            t2 = dsq_pair_fma(dsq_pair_of(d0, d1), e, t2);
+        }
+    };
+    // m of all so far
+    auto raise = [&](float most, int turn) {
+        if (!(most > m)) return;
+        const float d = between(m, most, c), e = ex2(d);
+        const DsqPair e2 = dsq_pair_of(e, e);
+        t2 = dsq_pair_mul(dsq_pair_fma(s2, dsq_pair_of(d, d), t2), e2);
+        s2 = dsq_pair_mul(s2, e2);
+        m = most;
+        best_turn = turn;
+    };
+    if (TOP && v0 + tid < v1) best_turn = 0;                   // (where m stays LOWEST: the first turn)
+    bool general = false;                                      // elements of -infinity have been seen
     uint4 next[AHEAD];
     if (turns > 0) load(0, next);
 #pragma unroll 1
-    for (int turn = 0; turn < turns; ++turn) {
+    for (int turn = 0; turn < full; ++turn) {
         uint4 r[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) r[j] = next[j];
         if (turn + 1 < turns) load(turn + 1, next);
-        const float most = largest<T>(r);
-        if (TOP && best_turn < 0 && v0 + turn * AHEAD * THREADS + tid < v1) best_turn = turn;     // (lowest or less: the first turn)
-        if (most > m) {
-            const float d = max_nan((m - most) * c, NOTHING), e = ex2(d);
-            const f2 e2 = pack2(e, e);
-            t2 = mul2(fma2(s2, pack2(d, d), t2), e2);
-            s2 = mul2(s2, e2);
-            m = most;
-            best_turn = turn;
-        }
-        const f2 less = pack2(-m, -m);
+        raise(largest<T>(r), turn);
+        const float M = m * c;
+        if (!general && fabsf(M) < FAR) {
+            const DsqPair s0 = s2, t0 = t2, less = dsq_pair_of(-M, -M);
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            float f[VEC];
-            values<T>(r[j], f);
+            for (int j = 0; j < AHEAD; ++j) {
+                float f[VEC];
+                values<T>(r[j], f);
 #pragma unroll
-            for (int i = 0; i < VEC; i += 2) {
-                const f2 d = mul2(add2(pack2(f[i], f[i + 1]), less), c2);
-                float d0, d1;
-                unpack2(d, d0, d1);
-                d0 = max_nan(d0, NOTHING);
-                d1 = max_nan(d1, NOTHING);
-                const f2 e = pack2(ex2(d0), ex2(d1));
-                s2 = add2(s2, e);
-                t2 = fma2(pack2(d0, d1), e, t2);
+                for (int i = 0; i < VEC; i += 2) {
+                    const DsqPair d = dsq_pair_fma(dsq_pair_of(f[i], f[i + 1]), c2, less);
+                    float d0, d1;
+                    dsq_halves(d, d0, d1);
+                    const DsqPair e = dsq_pair_of(ex2(d0), ex2(d1));
+                    s2 = dsq_pair_add(s2, e);
+                    t2 = dsq_pair_fma(d, e, t2);
+                }
             }
+            float a, b;
+            dsq_halves(t2, a, b);
+            if (a + b == a + b) continue;
+            // (-infinity times 0, or a NaN of the row's: once more)
+            s2 = s0;
+            t2 = t0;
+            general = true;
         }
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) any_vector(r[j]);
+    }
+    if (full < turns) {
+        raise(largest<T>(next), full);                         // (what is not there is -infinity)
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (v0 + (full * AHEAD + j) * THREADS + tid < v1) any_vector(next[j]);
     }
     Sums sum;
     {
         float a, b;
-        unpack2(s2, a, b);
+        dsq_halves(s2, a, b);
         sum.s = a + b;
-        unpack2(t2, a, b);
+        dsq_halves(t2, a, b);
         sum.t = a + b;
         sum.m = m;
     }
@@ -282,7 +315,7 @@ __global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_co
         const float v = dsq_to_f32(cut.row[cut.single(tid)]);
         // (-infinity and NaN as in the loop: less LOWEST nothing, and NaN)
         Sums one = {fmaxf(v, LOWEST), 1.f, 0.f};
-        const float d = max_nan((v - one.m) * c, NOTHING);
+        const float d = exponent(v, one.m, c);
         one.s = ex2(d);
         one.t = d * one.s;
         sum = joined(sum, one, c);
@@ -306,15 +339,14 @@ __global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_co
             best = m > LOWEST ? key_of(m, cut.index(last) + VEC - 1) : (unsigned long long)(uint32_t)~(cut.index(last) + VEC - 1);
         }
 #pragma unroll
-        for (int o = 1; o < THREADS / GROUPS; o <<= 1) {
+        for (int o = 1; o < SHARE; o <<= 1) {
             const unsigned long long other = __shfl_xor_sync(~0u, best, o);
             best = best > other ? best : other;
         }
-        if (tid % (THREADS / GROUPS) == 0) bests[tid / (THREADS / GROUPS)] = best;
+        if (tid % SHARE == 0) bests[tid / SHARE] = best;
         __syncthreads();
         // the `top`-th of them
         {
-            constexpr int SHARE = THREADS / GROUPS;
             int above = 0;
 #pragma unroll 4
             for (int j = tid % SHARE; j < GROUPS; j += SHARE) above += bests[j] > best;
@@ -380,7 +412,7 @@ __global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_co
         for (int i = tid; i < p.top; i += THREADS)
             if (i >= n) put(i, 0ull);
         if (n <= ROOM) {
-            ranked(found, n, [&](int at, unsigned long long key) {
+            ranked<THREADS>(found, n, [&](int at, unsigned long long key) {
                 if (at < p.top) put(at, key);
             });
         } else {
@@ -419,21 +451,28 @@ __global__ void __launch_bounds__(THREADS, 2) logprob_fwd_kernel(const __grid_co
     if (rank != 0) return;
     Sums all = block_sums[0];
     for (int i = 1; i < p.cluster; ++i) all = joined(all, block_sums[i], c);
-    const float log_s = logf(all.s);
+    const float log_s = log2f(all.s);
     // (a row without any: everything is improbable, and there is nothing to be uncertain about)
     const bool empty = all.s == 0.f;
     const float none = __uint_as_float(0xFF800000u), nan = __uint_as_float(0x7FC00000u);
-    auto logp_of = [&](float v) { return empty ? none : (v - all.m) * p.scale - log_s; };
+    auto logp_of = [&](float v) {
+        const float M = all.m * c;
+        if (empty) return none;
+        return fabsf(M) < FAR && fabsf(v * c) < FAR ? (__fmaf_rn(v, c, -M) - log_s) * LN2 : (v - all.m) * p.scale - log_s * LN2;
+    };
     if (tid == 0) {
         if (p.logp) p.logp[row] = target < 0 ? 0.f : target >= p.V ? nan : logp_of(wanted);
         if (p.entropy) {
-            const float h = log_s - all.t * LN2 / all.s;
+            const float h = (log_s - all.t / all.s) * LN2;
             p.entropy[row] = empty || h < 0.f ? 0.f : h;
         }
-        if (p.lse) p.lse[row] = empty ? none : __fmaf_rn(all.m, p.scale, log_s);
+        if (p.lse) {
+            const float M = all.m * c;
+            p.lse[row] = empty ? none : fabsf(M) < FAR ? __fmaf_rn(M, LN2, log_s * LN2) : __fmaf_rn(all.m, p.scale, log_s * LN2);
+        }
     }
     if (TOP)
-        ranked(lists, p.cluster * p.top, [&](int at, unsigned long long key) {
+        ranked<THREADS>(lists, p.cluster * p.top, [&](int at, unsigned long long key) {
             if (at >= p.top || key == 0ull) return;
             if (p.top_ids) p.top_ids[row * p.top + at] = index_of(key);
             if (p.top_logp) p.top_logp[row * p.top + at] = logp_of(value_of(key));
@@ -518,19 +557,26 @@ __global__ void __launch_bounds__(BWD_THREADS) logprob_bwd_kernel(const __grid_c
 }
 
 // blocks of a row: as many as leave each a turn's work and the SMs no more than one each
-int cluster_of(int64_t M, int64_t V, int vec)
+int cluster_of(int64_t M, int64_t V, int threads, int vec)
 {
     const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     int c = 1;
-    while (c < MAX_CLUSTER && M * c * 2 <= sms && V >= (int64_t)THREADS * vec * 2 * c) c *= 2;
+    while (c < MAX_CLUSTER && M * c * 2 <= sms && V >= (int64_t)threads * vec * 2 * c) c *= 2;
     return c;
 }
 
-template <class T> int fwd_launch(FwdParams &p, int64_t M, cudaStream_t s)
+template <class T, int THREADS> int fwd_launch(FwdParams &p, int64_t M, cudaStream_t s)
 {
-    p.cluster = cluster_of(M, p.V, vec_of<T>());
-    const auto kernel = p.top > 0 ? logprob_fwd_kernel<T, true> : logprob_fwd_kernel<T, false>;
+    const auto kernel = p.top > 0 ? logprob_fwd_kernel<T, true, THREADS> : logprob_fwd_kernel<T, false, THREADS>;
     return dsq_launch(kernel, dim3((unsigned)(M * p.cluster)), dim3(THREADS), 0, s, dsq_launch_hooks().pdl, p.cluster, p);
+}
+
+// Small blocks where there are rows enough to fill the SMs with them: some are between their passes while others read.
+template <class T> int fwd_pick(FwdParams &p, int64_t M, cudaStream_t s)
+{
+    const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
+    p.cluster = cluster_of(M, p.V, 512, vec_of<T>());
+    return M >= 2 * sms ? fwd_launch<T, 256>(p, M, s) : fwd_launch<T, 512>(p, M, s);
 }
 
 template <class T> int bwd_launch(BwdParams &p, int64_t M, cudaStream_t s)
@@ -580,9 +626,9 @@ int dsq_logprob_fwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dt
     p.scale = scale;
     cudaStream_t s = (cudaStream_t)stream;
     switch (dtype) {
-    case DSQ_F32: return fwd_launch<float>(p, M, s);
-    case DSQ_BF16: return fwd_launch<__nv_bfloat16>(p, M, s);
-    default: return fwd_launch<__half>(p, M, s);
+    case DSQ_F32: return fwd_pick<float>(p, M, s);
+    case DSQ_BF16: return fwd_pick<__nv_bfloat16>(p, M, s);
+    default: return fwd_pick<__half>(p, M, s);
     }
 }
 

@@ -118,7 +118,7 @@ def test_ties(dsq, t, M):
 
 
 @pytest.mark.parametrize("t", [torch.float32, torch.bfloat16])
-@pytest.mark.parametrize("M", [1, 200])
+@pytest.mark.parametrize("M", [1, 200, 300])
 def test_large_elements_with_the_same_threads(dsq, t, M):
     """More candidates than a block has room for: a block's stride of large elements, in sorted order."""
     V = 128000
@@ -127,7 +127,7 @@ def test_large_elements_with_the_same_threads(dsq, t, M):
     # all elements of the vectors of the first few threads, whatever block a row is cut into
     v = torch.arange(V) // vec
     part = V // vec // 8
-    for period in (512,):
+    for period in (512 if M < 296 else 256,):
         here = ((v - 0) % period < 70) | ((v % part) % period < 70)
         x[:, here] = (torch.arange(int(here.sum())) % 977).float() * 0.0625
     check(dsq, x.to(t), torch.zeros(M, dtype=torch.long), 1.0, 32)
