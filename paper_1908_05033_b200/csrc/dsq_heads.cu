@@ -8,12 +8,15 @@
 //
 // HBM-bound: a head is read once and written once, everything between is in registers.
 //   * A unit is 32 bytes of a head (two 16-byte vectors): the first and second elements of the same
-//     pairs, so that a turn needs no other lane; L lanes (a power of two) share a head and two sums.
-//   * A block takes the heads of some tokens; their cosines and sines are made once a block, in
-//     shared memory, one angle for all heads.  An angle is formed and reduced to a quarter turn in
-//     binary64 (a position of 2^20 leaves 2^-4 of an angle in binary32).
-//   * Blocks of q and blocks of k are apart: a lane keeps the weights (and the sums of their
-//     gradient) of its own unit in registers.
+//     pairs, so that a turn needs no other lane; L lanes (a power of two), a team, share a head and two sums.
+//   * A team takes a token's heads one after the other (all of them, or a part where there are few
+//     tokens): a lane has the same pairs of all of them, makes their cosines and sines itself and
+//     keeps them in registers; nothing goes through shared memory and no team waits for another.
+//     (With a table a block in shared memory, for all heads: 16384 tokens of 32 + 8 heads of 128 in bf16 67 us.)
+//     An angle is formed and reduced to a quarter turn in binary64 (a position of 2^20 leaves 2^-4 of
+//     an angle in binary32).
+//   * Backwards teams take either heads of q or of k, and a lane keeps the sums of the weights' gradient of its
+//     pairs in registers; blocks leave theirs in the workspace, a second kernel adds them in one order.
 //   * Heads or strides that are no multiple of a vector go element by element, 32 lanes a head.
 #include "dsq_launch.h"
 #include "dsq_pairs.cuh"
@@ -25,7 +28,7 @@ using namespace dsq_ptx;
 
 namespace {
 
-constexpr int BLOCK = 256, MAX_DIM = 512, MAX_HEADS = 4096, TURN_BYTES = 16384;
+constexpr int BLOCK = 128, MAX_DIM = 512, MAX_HEADS = 4096;
 
 struct Tensor {
     const void *x, *gy;           // (gy: backward)
@@ -33,8 +36,8 @@ struct Tensor {
     const float *w;
     float *part;                  // sums of the weight's gradient, [blocks][D]
     int64_t x_token, x_head, y_token, y_head, g_token, g_head;
-    int heads, tile;              // tokens of a tile
-    uint32_t heads_inv;           // floor(2^32 / heads) + 1
+    int heads;
+    int parts, per_part;          // of a token's heads (forward: of q's and k's together, in t[0])
 };
 
 struct Params {
@@ -45,7 +48,6 @@ struct Params {
     int64_t tokens;
     int q_blocks, k_blocks;
     int D, R, axes, norm, lanes, units;
-    uint32_t half_inv;            // floor(2^32 / (R / 2)) + 1
     float eps, inv_d;
 };
 
@@ -74,29 +76,6 @@ __device__ __forceinline__ float2 turn_of(int64_t pos, float f)
     if (q == 1 || q == 2) t.x = -t.x;
     if (q >= 2) t.y = -t.y;
     return t;
-}
-
-// Where pair i's cosine lies among a token's values, and how far behind it the sine: of a unit's pairs 2 q, 2 q + 1 cosines and
-// sines side by side, units beside units, so that the lanes of a head read consecutive 16 bytes.
-template <int VEC> __device__ __forceinline__ int turn_at(int i, int units)
-{
-    return VEC == 1 ? 2 * i : ((i % VEC) / 2 * units + i / VEC) * 4 + (i & 1);
-}
-template <int VEC> constexpr int SINE = VEC == 1 ? 1 : 2;
-
-// the turns of `n` tokens from token0 on
-template <int VEC> __device__ __forceinline__ void make_turns(const Params &p, int64_t token0, int n, float *turns)
-{
-    const int half = p.R / 2, units = half / VEC;
-    for (int e = threadIdx.x; e < n * half; e += BLOCK) {
-        const int t = half == 1 ? e : (int)__umulhi((uint32_t)e, p.half_inv), i = e - t * half;
-        const int axis = p.axis ? p.axis[i] : 0;
-        float2 v = make_float2(__int_as_float(0x7FC00000), __int_as_float(0x7FC00000));   // (no such axis: NaN)
-        if (axis < p.axes) v = turn_of(p.pos[axis * p.tokens + token0 + t], p.freq[i]);
-        float *to = turns + t * p.R + turn_at<VEC>(i, units);
-        to[0] = v.x;
-        to[SINE<VEC>] = v.y;
-    }
 }
 
 // a vector as it lies in memory, its elements two by two, and back
@@ -168,14 +147,12 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v, int lanes)
     }
     return v;
 }
-// heads of a tile (tile_of), a bit each
-constexpr int MAX_PASSES = 8, MARKS = (MAX_HEADS > BLOCK * MAX_PASSES ? MAX_HEADS : BLOCK * MAX_PASSES) / 32;
 // squares, and what is divided by their root, are inside binary32's range
 __device__ __forceinline__ bool in_range(float mean) { return mean > 1e-28f && mean < 1e36f; }
 
-// A head whose squares are not (found in the loop, done behind it): by a whole warp in binary64, element by element.  `sums`: the warp's
+// A head whose squares are not: by a whole warp in binary64, element by element.  `sums`: the warp's
 // sums of the weight's gradient.  Every pair is read and written by one lane.
-template <class T, bool BACK> __device__ __noinline__ void wide_head(const Params &p, const Tensor &t, int64_t token, int head,
+template <class T, bool BACK> __device__ __forceinline__ void wide_head(const Params &p, const Tensor &t, int64_t token, int head,
                                                                      bool inter, float *sums)
 {
     const T *x = (const T *)t.x + token * t.x_token + head * t.x_head;
@@ -228,45 +205,96 @@ template <class T, bool BACK> __device__ __noinline__ void wide_head(const Param
         if (j >= 0) y[j] = dsq_from_f32<T>((float)o2);
     });
 }
-// the marked heads of a tile, a warp each; marks are cleared
-template <class T, bool BACK> __device__ __forceinline__ void wide_heads(const Params &p, const Tensor &t, int64_t token0, int rows,
-                                                                         uint32_t *marks, bool inter, float *sums)
+// Heads that are done behind the loop, a bit each, a row of words a team.  A row's heads are those of a team's part.
+constexpr int MARKS = 2048;
+__device__ __forceinline__ uint32_t *marks_of(uint32_t *marks, int lanes, int per_part)
 {
-    const int warp = threadIdx.x >> 5;
-    for (int w = warp; 32 * w < rows; w += BLOCK / 32) {
-        uint32_t mask = marks[w];
-        while (mask) {
-            const int row = 32 * w + __ffs(mask) - 1;
-            wide_head<T, BACK>(p, t, token0 + row / t.heads, row % t.heads, inter, sums);
-            mask &= mask - 1;
+    return marks + threadIdx.x / lanes * ((per_part + 31) >> 5);
+}
+// the marked heads of a warp's teams, whose parts begin at (token, first); clears the marks
+template <class T, bool BACK> __device__ __noinline__ void wide_heads(const Params &p, const Tensor &t, uint32_t *marks, int lanes,
+                                                                      int per_part, int64_t token, int first, bool inter, float *sums)
+{
+    const int words = (per_part + 31) >> 5;
+    __syncwarp();
+    for (int from = 0; from < 32; from += lanes) {
+        const int64_t tk = __shfl_sync(~0u, token, from);
+        const int h0 = __shfl_sync(~0u, first, from);
+        uint32_t *row = marks + ((threadIdx.x & ~31) + from) / lanes * words;
+        for (int w = 0; w < words; ++w) {
+            uint32_t mask = row[w];
+            while (mask) {
+                const int h = h0 + 32 * w + __ffs(mask) - 1;
+                // (forward: of q, then of k)
+                const bool second = !BACK && h >= p.t[0].heads;
+                wide_head<T, BACK>(p, BACK ? t : p.t[second], tk, second ? h - p.t[0].heads : h, inter, sums);
+                mask &= mask - 1;
+            }
+            __syncwarp();
+            if ((threadIdx.x & 31) == 0) row[w] = 0u;
         }
-        __syncwarp();
-        if ((threadIdx.x & 31) == 0) marks[w] = 0u;
     }
+    __syncwarp();
 }
 
-// A lane's part of a head: U units, element i of vector v of unit u at (2 u + v) VEC + i, two by two.
 // L: lanes of a head, each with all its units and all of them turned; 0: p.lanes, any.
 template <class T, int VEC, int U, bool INTER, int L> struct Lane {
     static constexpr int N = 2 * U * VEC, P = N / 2;
     Unit unit[U];
     DsqPair w[P];
-    __device__ __forceinline__ void init(const Params &p, const Tensor &t, int lane)
+    // cosines and sines of the pairs (not turned: 1 and 0), two by two where a unit has more than one
+    float c[P], s[P];
+    __device__ __forceinline__ void init(const Params &p, int lane)
     {
-        float v[N];
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             unit[u] = unit_of<VEC, INTER>(p, lane + u * lanes_of<L>(p));
             if (L) unit[u].has_a = unit[u].has_b = unit[u].turned = true;
             else if (lane + u * p.lanes >= p.units) unit[u].has_a = unit[u].has_b = unit[u].turned = false;
+        }
+    }
+    __device__ __forceinline__ void weights(const float *from)
+    {
+        float v[N];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
-                v[2 * u * VEC + i] = t.w && unit[u].has_a ? __ldg(t.w + unit[u].a + i) : 1.f;
-                v[(2 * u + 1) * VEC + i] = t.w && unit[u].has_b ? __ldg(t.w + unit[u].b + i) : 1.f;
+                v[2 * u * VEC + i] = from && unit[u].has_a ? __ldg(from + unit[u].a + i) : 1.f;
+                v[(2 * u + 1) * VEC + i] = from && unit[u].has_b ? __ldg(from + unit[u].b + i) : 1.f;
             }
-        }
 #pragma unroll
         for (int i = 0; i < P; ++i) w[i] = dsq_pair_of(v[2 * i], v[2 * i + 1]);
+    }
+    __device__ __forceinline__ float2 turn_at(const Params &p, int64_t token, int lane, int u, int i) const
+    {
+        if (!unit[u].turned) return make_float2(1.f, 0.f);
+        const int pair = (lane + u * lanes_of<L>(p)) * VEC + i, axis = p.axis ? __ldg(p.axis + pair) : 0;
+        if (axis < p.axes) return turn_of(__ldg(p.pos + axis * p.tokens + token), __ldg(p.freq + pair));
+        return make_float2(__int_as_float(0x7FC00000), __int_as_float(0x7FC00000));       // (no such axis)
+    }
+    // SHARED: all teams of the warp have the token, and each makes its share of the turns
+    template <bool SHARED> __device__ __forceinline__ void turns(const Params &p, int64_t token, int lane)
+    {
+        constexpr int TEAMS = L ? 32 / L : 1, BY = SHARED ? (TEAMS < VEC ? TEAMS : VEC) : 1;
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < VEC; i += BY) {
+                if constexpr (BY == 1) {
+                    const float2 t = turn_at(p, token, lane, u, i);
+                    c[u * VEC + i] = t.x;
+                    s[u * VEC + i] = t.y;
+                } else {
+                    const int team = (threadIdx.x & 31) / L;
+                    const float2 t = turn_at(p, token, lane, u, i + team % BY);
+#pragma unroll
+                    for (int k = 0; k < BY; ++k) {
+                        c[u * VEC + i + k] = __shfl_sync(~0u, t.x, k * L + lane);
+                        s[u * VEC + i + k] = __shfl_sync(~0u, t.y, k * L + lane);
+                    }
+                }
+            }
     }
     // (what does not exist is zero)
     __device__ __forceinline__ void load(const T *row, bool on, Raw<T, VEC> (&r)[U][2]) const
@@ -305,81 +333,37 @@ template <class T, int VEC, int U, bool INTER, int L> struct Lane {
             if (L || unit[u].has_b) store_vec<T, VEC>(row + unit[u].b, v + (2 * u + 1) * VEC);
         }
     }
-    // turns the pairs, forwards or back; turns: the token's
-    template <bool BACK> __device__ __forceinline__ void turn(DsqPair (&f)[P], const float *turns, int lane, const Params &p) const
+    // turns the pairs, forwards or back
+    template <bool BACK> __device__ __forceinline__ void turn(DsqPair (&f)[P]) const
     {
-        const int turned = L ? L * U : p.R / (2 * VEC);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
             if (!L && !unit[u].turned) continue;
-            const int at = lane + u * lanes_of<L>(p);
-            if constexpr (VEC == 1) {                          // f[u] is the unit's pair
-                float a, b;
-                dsq_halves(f[u], a, b);
-                const float2 t = *reinterpret_cast<const float2 *>(turns + 2 * at);
-                const float s = BACK ? -t.y : t.y;
-                f[u] = dsq_pair_of(__fmaf_rn(a, t.x, -(b * s)), __fmaf_rn(b, t.x, a * s));
-            } else {
+            if constexpr (VEC == 1 || INTER) {                 // f[i] is a pair
 #pragma unroll
-                for (int j = 0; j < VEC; j += 2) {
-                    const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(turns + (j / 2 * turned + at) * 4);
-                    const DsqPair c = v.x, s = BACK ? dsq_pair_neg(v.y) : v.y;
-                    if constexpr (INTER) {                     // f[u VEC + j], f[u VEC + j + 1]: pairs j and j + 1
-                        float a0, b0, a1, b1;
-                        dsq_halves(f[u * VEC + j], a0, b0);
-                        dsq_halves(f[u * VEC + j + 1], a1, b1);
-                        const DsqPair a = dsq_pair_of(a0, a1), b = dsq_pair_of(b0, b1);
-                        const DsqPair y1 = dsq_pair_fma(a, c, dsq_pair_neg(dsq_pair_mul(b, s)));
-                        const DsqPair y2 = dsq_pair_fma(b, c, dsq_pair_mul(a, s));
-                        dsq_halves(y1, a0, a1);
-                        dsq_halves(y2, b0, b1);
-                        f[u * VEC + j] = dsq_pair_of(a0, b0);
-                        f[u * VEC + j + 1] = dsq_pair_of(a1, b1);
-                    } else {                                   // first and second elements VEC / 2 pairs apart
-                        const DsqPair a = f[u * VEC + j / 2], b = f[u * VEC + VEC / 2 + j / 2];
-                        f[u * VEC + j / 2] = dsq_pair_fma(a, c, dsq_pair_neg(dsq_pair_mul(b, s)));
-                        f[u * VEC + VEC / 2 + j / 2] = dsq_pair_fma(b, c, dsq_pair_mul(a, s));
-                    }
+                for (int i = u * VEC; i < (u + 1) * VEC; ++i) {
+                    float a, b;
+                    dsq_halves(f[i], a, b);
+                    const float sn = BACK ? -s[i] : s[i];
+                    f[i] = dsq_pair_of(__fmaf_rn(a, c[i], -(b * sn)), __fmaf_rn(b, c[i], a * sn));
+                }
+            } else {                                           // first and second elements VEC / 2 of these apart
+#pragma unroll
+                for (int i = 0; i < VEC; i += 2) {
+                    float a0, a1, b0, b1;
+                    DsqPair &x = f[u * VEC + i / 2], &y = f[u * VEC + VEC / 2 + i / 2];
+                    dsq_halves(x, a0, a1);
+                    dsq_halves(y, b0, b1);
+                    const int k = u * VEC + i;
+                    const float s0 = BACK ? -s[k] : s[k], s1 = BACK ? -s[k + 1] : s[k + 1];
+                    x = dsq_pair_of(__fmaf_rn(a0, c[k], -(b0 * s0)), __fmaf_rn(a1, c[k + 1], -(b1 * s1)));
+                    y = dsq_pair_of(__fmaf_rn(b0, c[k], a0 * s0), __fmaf_rn(b1, c[k + 1], a1 * s1));
                 }
             }
         }
     }
 };
 
-// The heads of a tile of tokens, a head to L lanes: which one a thread has, and the next, `step` heads on.
-struct Place {
-    int row, token, head;
-    __device__ __forceinline__ void to(const Tensor &t, int r)
-    {
-        row = r;
-        token = t.heads == 1 ? r : (int)__umulhi((uint32_t)r, t.heads_inv);
-        head = r - token * t.heads;
-    }
-};
-// an address that goes with it
-template <class T> struct Walk {
-    T *at;
-    int64_t go, back;                 // for `step` heads on; more where that passes a token's last head
-    __device__ __forceinline__ Walk(T *base, int64_t token0, const Place &l, const Place &step, int heads, int64_t token, int64_t head)
-    {
-        at = base + (token0 + l.token) * token + l.head * head;
-        go = step.token * token + step.head * head;
-        back = token - heads * head;
-    }
-    __device__ __forceinline__ void next(bool over) { at += over ? go + back : go; }
-};
-__device__ __forceinline__ bool advance(Place &l, const Place &step, int heads)
-{
-    l.row += step.row;
-    l.token += step.token;
-    l.head += step.head;
-    const bool over = l.head >= heads;
-    if (over) {
-        l.head -= heads;
-        ++l.token;
-    }
-    return over;
-}
 __device__ __forceinline__ float sum_of(DsqPair v)
 {
     float a, b;
@@ -387,152 +371,213 @@ __device__ __forceinline__ float sum_of(DsqPair v)
     return a + b;
 }
 
-template <class T, int VEC, int U, bool INTER, int L_>
-__global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 2 : 3) heads_fwd_kernel(const __grid_constant__ Params p)
+// rows on their way ahead of the one at hand
+constexpr int AHEAD = 2;
+
+// WARP: the teams of a warp take a token's heads in turn (they lie side by side in memory), else each team has
+// a token's of its own.
+template <class T, int VEC, int U, bool INTER, int L_, bool WARP>
+__global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 3 : 5) heads_fwd_kernel(const __grid_constant__ Params p)
 {
     using L = Lane<T, VEC, U, INTER, L_>;
-    extern __shared__ __align__(16) float turns[];
     __shared__ uint32_t marks[MARKS];
-    const bool second = (int)blockIdx.x >= p.q_blocks;
-    const Tensor &t = p.t[second];
-    const int64_t token0 = (int64_t)(blockIdx.x - (second ? p.q_blocks : 0)) * t.tile;
-    const int n = (int)min((int64_t)t.tile, p.tokens - token0), rows = n * t.heads;
-    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), step = BLOCK / lanes;
+    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), by = WARP ? 32 / lanes : 1;
+    const int64_t thread = (int64_t)blockIdx.x * BLOCK + threadIdx.x, item = WARP ? thread >> 5 : thread / lanes;
+    const int parts = p.t[0].parts, per_part = p.t[0].per_part, q_heads = p.t[0].heads, heads = q_heads + p.t[1].heads;
+    const int64_t token = parts == 1 ? item : item / parts;
+    const int begin = parts == 1 ? 0 : (int)(item - token * parts) * per_part;
+    const int last = token < p.tokens ? min(begin + per_part, heads) : begin, first = begin + (WARP ? (threadIdx.x & 31) / lanes : 0);
+    uint32_t *bad_heads = marks_of(marks, lanes, per_part);
+    bool any = false;
+    for (int w = lane; 32 * w < per_part; w += lanes) bad_heads[w] = 0u;
+    __syncwarp();
     grid_dependency_wait();
     grid_launch_dependents();
     L l;
-    l.init(p, t, lane);
-    Place at, by;
-    at.to(t, threadIdx.x / lanes);
-    by.to(t, step);
-    Walk<const T> x((const T *)t.x, token0, at, by, t.heads, t.x_token, t.x_head);
-    Walk<T> y((T *)t.y, token0, at, by, t.heads, t.y_token, t.y_head);
-    Raw<T, VEC> next[U][2];
-    l.load(x.at, at.row < rows, next);
-    bool any = false;
-    for (int i = threadIdx.x; i < MARKS; i += BLOCK) marks[i] = 0u;
-    make_turns<VEC>(p, token0, n, turns);
-    __syncthreads();
-    // (a warp's lanes go round together: the sums are over lanes)
-    for (int first = (threadIdx.x & ~31) / lanes; first < rows; first += step) {
-        DsqPair f[L::P];
-        L::values(next, f);
-        const int row = at.row;
-        const float *turn = turns + at.token * (L_ ? 2 * L_ * U * VEC : p.R);
-        T *to = y.at;
-        bool on = row < rows;
-        const bool over = advance(at, by, t.heads);
-        x.next(over);
-        y.next(over);
-        l.load(x.at, at.row < rows, next);
-        if (p.norm) {
-            DsqPair sum = 0ull;
-#pragma unroll
-            for (int i = 0; i < L::P; ++i) sum = dsq_pair_fma(f[i], f[i], sum);
-            const float mean = __fmaf_rn(lanes_sum<L_>(sum_of(sum), p.lanes), p.inv_d, p.eps);
-            const float rstd = rsqrtf(mean);
-            const bool bad = on && !in_range(mean);
-            if (bad) {
-                if (lane == 0) atomicOr(&marks[row >> 5], 1u << (row & 31));
-                on = false;
-                any = true;
-            }
-            const DsqPair r = dsq_pair_of(rstd, rstd);
-#pragma unroll
-            for (int i = 0; i < L::P; ++i) f[i] = dsq_pair_mul(dsq_pair_mul(f[i], r), l.w[i]);
+    l.init(p, lane);
+    Raw<T, VEC> next[AHEAD][U][2];
+    // the head whose load is next and the one at hand, those of k behind those of q
+    int ahead = first, head = first;
+    const T *x;
+    T *y;
+    auto x_of = [&]() {
+        const Tensor &t = p.t[ahead >= q_heads];
+        x = (const T *)t.x + token * t.x_token + (ahead >= q_heads ? ahead - q_heads : ahead) * t.x_head;
+    };
+    auto y_of = [&]() {
+        const Tensor &t = p.t[head >= q_heads];
+        y = (T *)t.y + token * t.y_token + (head >= q_heads ? head - q_heads : head) * t.y_head;
+        l.weights(t.w);
+    };
+    if (first < last) {
+        x_of();
+        y_of();
+    }
+    auto load = [&](Raw<T, VEC> (&r)[U][2]) {
+        l.load(x, ahead < last, r);
+        const bool of_q = ahead < q_heads;
+        ahead += by;
+        if (of_q && ahead >= q_heads) {
+            if (ahead < last) x_of();
+        } else {
+            x += by * p.t[!of_q].x_head;
         }
-        if (on) {
-            l.template turn<false>(f, turn, lane, p);
-            l.store(to, f);
+    };
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) load(next[a]);
+    if (WARP || first < last) l.template turns<WARP>(p, token < p.tokens ? token : 0, lane);
+    // (a warp's teams go round together: the sums are over lanes)
+    for (int i = 0; i < per_part; i += AHEAD * by) {
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (i + a * by >= per_part) break;
+            DsqPair f[L::P];
+            L::values(next[a], f);
+            load(next[a]);
+            bool on = head < last;
+            if (p.norm) {
+                DsqPair sum = 0ull;
+#pragma unroll
+                for (int k = 0; k < L::P; ++k) sum = dsq_pair_fma(f[k], f[k], sum);
+                const float mean = __fmaf_rn(lanes_sum<L_>(sum_of(sum), lanes), p.inv_d, p.eps);
+                const float rstd = rsqrtf(mean);
+                const bool bad = on && !in_range(mean);
+                if (bad) {
+                    if (lane == 0) bad_heads[(head - begin) >> 5] |= 1u << ((head - begin) & 31);
+                    any = true;
+                    on = false;
+                }
+                const DsqPair r = dsq_pair_of(rstd, rstd);
+#pragma unroll
+                for (int k = 0; k < L::P; ++k) f[k] = dsq_pair_mul(dsq_pair_mul(f[k], r), l.w[k]);
+            }
+            if (on) {
+                l.template turn<false>(f);
+                l.store(y, f);
+            }
+            const bool of_q = head < q_heads;
+            head += by;
+            if (of_q && head >= q_heads) {
+                if (head < last) y_of();
+            } else {
+                y += by * p.t[!of_q].y_head;
+            }
         }
     }
-    if (__syncthreads_or(any)) wide_heads<T, false>(p, t, token0, rows, marks, INTER, nullptr);
+    if (__any_sync(~0u, any)) wide_heads<T, false>(p, p.t[0], marks, lanes, per_part, token, begin, INTER, nullptr);
 }
 
 template <class T, int VEC, int U, bool INTER, int L_>
-__global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 1 : 2) heads_bwd_kernel(const __grid_constant__ Params p)
+__global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_kernel(const __grid_constant__ Params p)
 {
     using L = Lane<T, VEC, U, INTER, L_>;
-    extern __shared__ __align__(16) float turns[];
     __shared__ float sums[BLOCK / 32][MAX_DIM];
     __shared__ uint32_t marks[MARKS];
     const bool second = (int)blockIdx.x >= p.q_blocks;
     const Tensor &t = p.t[second];
     const int block = blockIdx.x - (second ? p.q_blocks : 0), blocks = second ? p.k_blocks : p.q_blocks;
-    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), step = BLOCK / lanes;
+    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1);
+    const int64_t items = p.tokens * t.parts, teams = (int64_t)blocks * BLOCK / lanes;
     grid_dependency_wait();
     grid_launch_dependents();
     L l;
-    l.init(p, t, lane);
+    l.init(p, lane);
+    l.weights(t.w);
     DsqPair gw[L::P];
 #pragma unroll
     for (int i = 0; i < L::P; ++i) gw[i] = 0ull;
-    for (int c = threadIdx.x & 31; c < p.D; c += 32) sums[threadIdx.x >> 5][c] = 0.f;
-    for (int i = threadIdx.x; i < MARKS; i += BLOCK) marks[i] = 0u;
-    __syncthreads();
+    float *mine = sums[threadIdx.x >> 5];
+    for (int c = threadIdx.x & 31; c < p.D; c += 32) mine[c] = 0.f;
+    uint32_t *bad_heads = marks_of(marks, lanes, t.per_part);
+    for (int w = lane; 32 * w < t.per_part; w += lanes) bad_heads[w] = 0u;
+    __syncwarp();
 
-    for (int64_t token0 = (int64_t)block * t.tile; token0 < p.tokens; token0 += (int64_t)blocks * t.tile) {
-        const int n = (int)min((int64_t)t.tile, p.tokens - token0), rows = n * t.heads;
-        Place at, by;
-        at.to(t, threadIdx.x / lanes);
-        by.to(t, step);
-        Walk<const T> gy((const T *)t.gy, token0, at, by, t.heads, t.g_token, t.g_head);
-        Walk<const T> in((const T *)t.x, token0, at, by, t.heads, t.x_token, t.x_head);
-        Walk<T> out((T *)t.y, token0, at, by, t.heads, t.y_token, t.y_head);
-        Raw<T, VEC> next_x[U][2], next_g[U][2];
-        l.load(gy.at, at.row < rows, next_g);
-        l.load(in.at, p.norm && at.row < rows, next_x);
+    // A team's heads, item by item: where the loads are, and where the work is
+    int64_t item = ((int64_t)block * BLOCK + threadIdx.x) / lanes;
+    const int64_t rounds = (items - (((int64_t)block * BLOCK + (threadIdx.x & ~31)) / lanes) + teams - 1) / teams;   // of the warp's first team
+    struct At { int64_t item, token; int head, last; };
+    auto start = [&](At &a, int64_t i) {
+        a.item = i;
+        a.token = t.parts == 1 ? i : i / t.parts;
+        a.head = t.parts == 1 ? 0 : (int)(i - a.token * t.parts) * t.per_part;
+        a.last = i < items ? min(a.head + t.per_part, t.heads) : a.head;
+    };
+    At in, at;
+    int left = t.per_part;
+    start(in, item);
+    start(at, item);
+    const T *gy, *x;
+    T *y;
+    auto from = [&]() {
+        gy = (const T *)t.gy + in.token * t.g_token + in.head * t.g_head;
+        x = (const T *)t.x + in.token * t.x_token + in.head * t.x_head;
+    };
+    auto to = [&]() { y = (T *)t.y + at.token * t.y_token + at.head * t.y_head; };
+    from();
+    to();
+    Raw<T, VEC> next_x[U][2], next_g[U][2];
+    auto load = [&]() {
+        const bool on = in.head < in.last;
+        l.load(gy, on, next_g);
+        l.load(x, p.norm && on, next_x);
+        ++in.head;
+        if (--left == 0) {
+            left = t.per_part;
+            start(in, in.item + teams);
+            from();
+        } else {
+            gy += t.g_head;
+            x += t.x_head;
+        }
+    };
+    load();
+    for (int64_t round = 0; round < rounds; ++round) {
+        if (at.head < at.last) l.template turns<false>(p, at.token, lane);
+        const int first = at.head;
         bool any = false;
-        make_turns<VEC>(p, token0, n, turns);
-        __syncthreads();
-        for (int first = (threadIdx.x & ~31) / lanes; first < rows; first += step) {
-            DsqPair g[L::P], x[L::P];
+        for (int i = 0; i < t.per_part; ++i) {
+            DsqPair g[L::P], v[L::P];
             L::values(next_g, g);
-            L::values(next_x, x);
-            const int row = at.row;
-            const float *turn = turns + at.token * (L_ ? 2 * L_ * U * VEC : p.R);
-            T *to = out.at;
-            bool on = row < rows;
-            const bool over = advance(at, by, t.heads);
-            gy.next(over);
-            in.next(over);
-            out.next(over);
-            l.load(gy.at, at.row < rows, next_g);
-            l.load(in.at, p.norm && at.row < rows, next_x);
-            if (on) l.template turn<true>(g, turn, lane, p);
+            L::values(next_x, v);
+            load();
+            bool on = at.head < at.last;
+            if (on) l.template turn<true>(g);
             if (p.norm) {
                 DsqPair sum2 = 0ull, dot2 = 0ull;
 #pragma unroll
-                for (int i = 0; i < L::P; ++i) {
-                    sum2 = dsq_pair_fma(x[i], x[i], sum2);
-                    dot2 = dsq_pair_fma(dsq_pair_mul(g[i], l.w[i]), x[i], dot2);
+                for (int k = 0; k < L::P; ++k) {
+                    sum2 = dsq_pair_fma(v[k], v[k], sum2);
+                    dot2 = dsq_pair_fma(dsq_pair_mul(g[k], l.w[k]), v[k], dot2);
                 }
-                const float sum = lanes_sum<L_>(sum_of(sum2), p.lanes), dot = lanes_sum<L_>(sum_of(dot2), p.lanes);
+                const float sum = lanes_sum<L_>(sum_of(sum2), lanes), dot = lanes_sum<L_>(sum_of(dot2), lanes);
                 const float mean = __fmaf_rn(sum, p.inv_d, p.eps), rstd = rsqrtf(mean);
                 const bool bad = on && !in_range(mean);
                 if (bad) {
-                    if (lane == 0) atomicOr(&marks[row >> 5], 1u << (row & 31));
-                    on = false;
+                    if (lane == 0) bad_heads[i >> 5] |= 1u << (i & 31);
                     any = true;
+                    on = false;
                 }
                 if (on) {
                     const float c = dot * rstd * p.inv_d;
                     const DsqPair r = dsq_pair_of(rstd, rstd), less = dsq_pair_of(-c, -c);
 #pragma unroll
-                    for (int i = 0; i < L::P; ++i) {
-                        const DsqPair m = dsq_pair_mul(x[i], r);
-                        gw[i] = dsq_pair_fma(g[i], m, gw[i]);
-                        g[i] = dsq_pair_mul(r, dsq_pair_fma(m, less, dsq_pair_mul(g[i], l.w[i])));
+                    for (int k = 0; k < L::P; ++k) {
+                        const DsqPair m = dsq_pair_mul(v[k], r);
+                        gw[k] = dsq_pair_fma(g[k], m, gw[k]);
+                        g[k] = dsq_pair_mul(r, dsq_pair_fma(m, less, dsq_pair_mul(g[k], l.w[k])));
                     }
                 }
             }
-            if (on) l.store(to, g);
+            if (on) l.store(y, g);
+            ++at.head;
+            y += t.y_head;
         }
-        // (and the turns have been read)
-        if (__syncthreads_or(any)) wide_heads<T, true>(p, t, token0, rows, marks, INTER, sums[threadIdx.x >> 5]);
+        if (__any_sync(~0u, any)) wide_heads<T, true>(p, t, marks, lanes, t.per_part, at.token, first, INTER, mine);
+        start(at, at.item + teams);
+        to();
     }
     if (!t.part) return;
-    // the block's sums: over the heads of a warp, then the warps, in one order
+    // the block's sums: over the teams of a warp, then the warps, in one order
     __syncwarp();
 #pragma unroll
     for (int i = 0; i < L::N; ++i) {
@@ -542,7 +587,7 @@ __global__ void __launch_bounds__(BLOCK, U * VEC > 8 ? 1 : 2) heads_bwd_kernel(c
         for (int o = 16; o >= lanes; o >>= 1) s += __shfl_xor_sync(~0u, s, o);
         const Unit &u = l.unit[i / (2 * VEC)];
         const bool b = i / VEC % 2;
-        if ((threadIdx.x & 31) < lanes && (b ? u.has_b : u.has_a)) sums[threadIdx.x >> 5][(b ? u.b : u.a) + i % VEC] += s;
+        if ((threadIdx.x & 31) < lanes && (b ? u.has_b : u.has_a)) mine[(b ? u.b : u.a) + i % VEC] += s;
     }
     __syncthreads();
     for (int c = threadIdx.x; c < p.D; c += BLOCK) {
@@ -620,61 +665,54 @@ int check_rotary(const dsq_rotary_t *r, int64_t tokens, int dtype, float eps)
 
 template <class T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
 
-// Tokens of a tile: `passes` rounds of a block's lanes, as far as their turns have room.
-int tile_of(const Params &p, int64_t heads, int passes)
+// Parts of a token's heads: the fewest (each makes the token's turns) that give the resident teams two and a half
+// each (a whole number and a bit of rounds are paid as the next), eight heads a part at least; where there are few
+// tokens down to one.  Marks have room for MARKS words a block.
+void set_parts(Tensor &t, int64_t tokens, int heads, int64_t teams, int per_block)
 {
-    const int rows = BLOCK / p.lanes * passes;
-    int64_t tile = rows / heads;
-    const int64_t room = p.R > 0 ? TURN_BYTES / (p.R * 4) : tile;
-    if (tile > room) tile = room;
-    if (tile > p.tokens) tile = p.tokens;
-    return tile < 1 ? 1 : (int)tile;
+    int64_t parts = (teams * 5 / 2 + tokens - 1) / tokens;
+    const int64_t most = tokens * 2 >= teams ? (heads + 7) / 8 : heads;
+    if (parts > most) parts = most;
+    if (parts < 1) parts = 1;
+    t.per_part = (int)((heads + parts - 1) / parts);
+    if (t.per_part > MARKS / per_block * 32) t.per_part = MARKS / per_block * 32;
+    t.parts = (heads + t.per_part - 1) / t.per_part;
 }
 
-size_t turn_bytes(const Params &p)
-{
-    const int tile = p.t[0].tile > p.t[1].tile ? p.t[0].tile : p.t[1].tile;
-    return (size_t)tile * p.R * 4 + 16;
-}
-
+// (of the backward kernel: as many as are resident)
 constexpr int SUM_BLOCKS_PER_SM = 4;
 
 template <class T, int VEC, int U, bool INTER, int L, bool BACK> int launch(Params &p, cudaStream_t s)
 {
     const int pdl = dsq_launch_hooks().pdl;
-    const int64_t sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
-    const int64_t rows = p.tokens * (p.t[0].heads + p.t[1].heads), round = BLOCK / p.lanes;
+    const int64_t sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148, per_block = BLOCK / p.lanes;
     if constexpr (!BACK) {
-        // as many rounds a block as leave some blocks for every place on an SM
-        int passes = (int)(rows / (round * sms * 16));
-        passes = passes < 1 ? 1 : passes > MAX_PASSES ? MAX_PASSES : passes;
+        // heads enough for the teams of a warp to share a token's
+        const int heads = p.t[0].heads + p.t[1].heads;
+        const bool warp = L && heads >= 2 * (32 / p.lanes);
+        const int64_t items = warp ? BLOCK / 32 : per_block;
+        set_parts(p.t[0], p.tokens, heads, sms * 5 * items, (int)per_block);
+        const int64_t blocks = (p.tokens * p.t[0].parts + items - 1) / items;
+        if (blocks > 0x7FFFFFFF) return DSQ_ERR_SIZE;
+        const auto kernel = warp ? heads_fwd_kernel<T, VEC, U, INTER, L, L != 0> : heads_fwd_kernel<T, VEC, U, INTER, L, false>;
+        return dsq_launch(kernel, dim3((unsigned)blocks), dim3(BLOCK), 0, s, pdl, 0, p);
+    } else {
+        // what is resident together, shared among q and k as their heads are
+        const int64_t most = sms * (2 * U * VEC > 16 ? 2 : SUM_BLOCKS_PER_SM);
         int64_t blocks[2] = {0, 0};
         for (int i = 0; i < 2; ++i) {
-            if (!p.t[i].heads) continue;
-            p.t[i].tile = tile_of(p, p.t[i].heads, passes);
-            blocks[i] = (p.tokens + p.t[i].tile - 1) / p.t[i].tile;
-        }
-        if (blocks[0] + blocks[1] > 0x7FFFFFFF) return DSQ_ERR_SIZE;
-        p.q_blocks = (int)blocks[0];
-        p.k_blocks = (int)blocks[1];
-        return dsq_launch(heads_fwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
-                          turn_bytes(p), s, pdl, 0, p);
-    } else {
-        // what is resident together, shared among q and k as their rows are
-        int64_t most = sms * SUM_BLOCKS_PER_SM, blocks[2] = {0, 0};
-        for (int i = 0; i < 2; ++i) {
-            if (!p.t[i].heads) continue;
-            p.t[i].tile = tile_of(p, p.t[i].heads, 2);
-            const int64_t tiles = (p.tokens + p.t[i].tile - 1) / p.t[i].tile;
-            int64_t share = most * p.t[i].heads / (p.t[0].heads + p.t[1].heads);
+            Tensor &t = p.t[i];
+            if (!t.heads) continue;
+            int64_t share = most * t.heads / (p.t[0].heads + p.t[1].heads);
             if (share < 1) share = 1;
-            blocks[i] = tiles < share ? tiles : share;
+            set_parts(t, p.tokens, t.heads, share * per_block, (int)per_block);
+            const int64_t need = (p.tokens * t.parts + per_block - 1) / per_block;
+            blocks[i] = need < share ? need : share;
         }
         p.q_blocks = (int)blocks[0];
         p.k_blocks = (int)blocks[1];
         if (p.t[1].part) p.t[1].part = p.t[0].part + blocks[0] * p.D;
-        return dsq_launch(heads_bwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK),
-                          turn_bytes(p), s, pdl, 0, p);
+        return dsq_launch(heads_bwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK), 0, s, pdl, 0, p);
     }
 }
 
@@ -687,11 +725,10 @@ void set_lanes(Params &p, int vec, int per_lane)
     while (p.lanes * per_lane < p.units && p.lanes < 32) p.lanes *= 2;
 }
 
-// Two units a lane forwards and one back (where sums of the weights' gradient take their registers), or as
-// many as 32 lanes need.
+// One unit a lane, or as many as 32 lanes need.
 template <class T, bool INTER, bool BACK> int pick(Params &p, bool vectors, cudaStream_t s)
 {
-    constexpr int V = vec_of<T>(), U = BACK ? 1 : 2;
+    constexpr int V = vec_of<T>(), U = 1;
     if (!vectors) {
         set_lanes(p, 1, 1);
         return p.units <= 64 ? launch<T, 1, 2, INTER, 0, BACK>(p, s) : launch<T, 1, 8, INTER, 0, BACK>(p, s);
@@ -702,7 +739,7 @@ template <class T, bool INTER, bool BACK> int pick(Params &p, bool vectors, cuda
         if (p.lanes == 8 / U) return launch<T, V, U, INTER, 8 / U, BACK>(p, s);
         if (p.lanes == 4 / U) return launch<T, V, U, INTER, 4 / U, BACK>(p, s);
     }
-    if constexpr (BACK && V == 4) {
+    if constexpr (V == 4) {
         if (p.units > 32) return launch<T, V, 2, INTER, 0, BACK>(p, s);
     }
     return launch<T, V, U, INTER, 0, BACK>(p, s);
@@ -723,7 +760,6 @@ void fill(Params &p, const dsq_rotary_t *r, int64_t tokens, int norm, float eps)
     p.pos = r->positions; p.freq = r->inv_freq; p.axis = r->axis;
     p.tokens = tokens;
     p.D = r->head_dim; p.R = r->rot_dim; p.axes = r->axes;
-    p.half_inv = p.R > 2 ? (uint32_t)((1ull << 32) / (uint64_t)(p.R / 2) + 1) : 0u;
     p.norm = norm != 0;
     p.eps = eps; p.inv_d = (float)(1.0 / r->head_dim);
 }
@@ -764,7 +800,6 @@ int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
         t.x = h->x; t.y = h->y; t.w = h->weight;
         t.x_token = h->x_token; t.x_head = h->x_head; t.y_token = h->y_token; t.y_head = h->y_head;
         t.heads = (int)h->heads;
-        t.heads_inv = h->heads > 1 ? (uint32_t)((1ull << 32) / (uint64_t)h->heads + 1) : 0u;
         vectors = vectors && in_vectors(h->x, h->x_token, h->x_head, vec, size) &&
                   in_vectors(h->y, h->y_token, h->y_head, vec, size);
     }
@@ -813,7 +848,6 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
         t.g_token = h->gy_token; t.g_head = h->gy_head;
         t.x_token = h->x_token; t.x_head = h->x_head; t.y_token = h->gx_token; t.y_head = h->gx_head;
         t.heads = (int)h->heads;
-        t.heads_inv = h->heads > 1 ? (uint32_t)((1ull << 32) / (uint64_t)h->heads + 1) : 0u;
         // (sums of both are made where either is wanted)
         t.part = sums ? (float *)((char *)workspace + DSQ_WS_BYTES) : nullptr;
         sp.out[i] = h->grad_weight;
