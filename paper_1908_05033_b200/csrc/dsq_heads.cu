@@ -276,7 +276,7 @@ template <class T, int VEC, int U, bool INTER, int L> struct Lane {
     // SHARED: all teams of the warp have the token, and each makes its share of the turns
     template <bool SHARED> __device__ __forceinline__ void turns(const Params &p, int64_t token, int lane)
     {
-        constexpr int TEAMS = L ? 32 / L : 1, BY = SHARED ? (TEAMS < VEC ? TEAMS : VEC) : 1;
+        constexpr int TEAMS = L ? 32 / L : 2, BY = SHARED ? (TEAMS < VEC ? TEAMS : VEC) : 1;   // (any: two teams at least)
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
@@ -286,12 +286,12 @@ template <class T, int VEC, int U, bool INTER, int L> struct Lane {
                     c[u * VEC + i] = t.x;
                     s[u * VEC + i] = t.y;
                 } else {
-                    const int team = (threadIdx.x & 31) / L;
+                    const int lanes = lanes_of<L>(p), team = (threadIdx.x & 31) / lanes;
                     const float2 t = turn_at(p, token, lane, u, i + team % BY);
 #pragma unroll
                     for (int k = 0; k < BY; ++k) {
-                        c[u * VEC + i + k] = __shfl_sync(~0u, t.x, k * L + lane);
-                        s[u * VEC + i + k] = __shfl_sync(~0u, t.y, k * L + lane);
+                        c[u * VEC + i + k] = __shfl_sync(~0u, t.x, k * lanes + lane);
+                        s[u * VEC + i + k] = __shfl_sync(~0u, t.y, k * lanes + lane);
                     }
                 }
             }
@@ -371,8 +371,8 @@ __device__ __forceinline__ float sum_of(DsqPair v)
     return a + b;
 }
 
-// rows on their way ahead of the one at hand
-constexpr int AHEAD = 2;
+// rows on their way ahead of the one at hand; resident blocks of the backward kernel
+constexpr int AHEAD = 2, BACK_BLOCKS = 3;
 
 // WARP: the teams of a warp take a token's heads in turn (they lie side by side in memory), else each team has
 // a token's of its own.
@@ -467,8 +467,8 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 3 : 5) heads_fwd_ker
     if (__any_sync(~0u, any)) wide_heads<T, false>(p, p.t[0], marks, lanes, per_part, token, begin, INTER, nullptr);
 }
 
-template <class T, int VEC, int U, bool INTER, int L_>
-__global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_kernel(const __grid_constant__ Params p)
+template <class T, int VEC, int U, bool INTER, int L_, bool WARP>
+__global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : BACK_BLOCKS) heads_bwd_kernel(const __grid_constant__ Params p)
 {
     using L = Lane<T, VEC, U, INTER, L_>;
     __shared__ float sums[BLOCK / 32][MAX_DIM];
@@ -476,8 +476,14 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
     const bool second = (int)blockIdx.x >= p.q_blocks;
     const Tensor &t = p.t[second];
     const int block = blockIdx.x - (second ? p.q_blocks : 0), blocks = second ? p.k_blocks : p.q_blocks;
-    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1);
-    const int64_t items = p.tokens * t.parts, teams = (int64_t)blocks * BLOCK / lanes;
+    const int lanes = lanes_of<L_>(p), lane = threadIdx.x & (lanes - 1), by = WARP ? 32 / lanes : 1;
+    const int of_warp = WARP ? (threadIdx.x & 31) / lanes : 0, per_item = WARP ? 32 : lanes;
+    const int64_t items = p.tokens * t.parts, step = (int64_t)blocks * BLOCK / per_item;
+    float *mine = sums[threadIdx.x >> 5];
+    for (int c = threadIdx.x & 31; c < p.D; c += 32) mine[c] = 0.f;
+    uint32_t *bad_heads = marks_of(marks, lanes, t.per_part);
+    for (int w = lane; 32 * w < t.per_part; w += lanes) bad_heads[w] = 0u;
+    __syncwarp();
     grid_dependency_wait();
     grid_launch_dependents();
     L l;
@@ -486,26 +492,24 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
     DsqPair gw[L::P];
 #pragma unroll
     for (int i = 0; i < L::P; ++i) gw[i] = 0ull;
-    float *mine = sums[threadIdx.x >> 5];
-    for (int c = threadIdx.x & 31; c < p.D; c += 32) mine[c] = 0.f;
-    uint32_t *bad_heads = marks_of(marks, lanes, t.per_part);
-    for (int w = lane; 32 * w < t.per_part; w += lanes) bad_heads[w] = 0u;
-    __syncwarp();
 
-    // A team's heads, item by item: where the loads are, and where the work is
-    int64_t item = ((int64_t)block * BLOCK + threadIdx.x) / lanes;
-    const int64_t rounds = (items - (((int64_t)block * BLOCK + (threadIdx.x & ~31)) / lanes) + teams - 1) / teams;   // of the warp's first team
-    struct At { int64_t item, token; int head, last; };
+    // Item by item (a part of a token's heads): where the loads are, and where the work is.
+    const int64_t item = ((int64_t)block * BLOCK + threadIdx.x) / per_item;
+    const int64_t lowest = ((int64_t)block * BLOCK + (threadIdx.x & ~31)) / per_item;         // of the warp
+    const int64_t rounds = lowest < items ? (items - lowest + step - 1) / step : 0;
+    struct At { int64_t item, token; int begin, head, last; };
     auto start = [&](At &a, int64_t i) {
         a.item = i;
         a.token = t.parts == 1 ? i : i / t.parts;
-        a.head = t.parts == 1 ? 0 : (int)(i - a.token * t.parts) * t.per_part;
-        a.last = i < items ? min(a.head + t.per_part, t.heads) : a.head;
+        a.begin = t.parts == 1 ? 0 : (int)(i - a.token * t.parts) * t.per_part;
+        a.head = a.begin + of_warp;
+        a.last = i < items ? min(a.begin + t.per_part, t.heads) : a.begin;
     };
     At in, at;
-    int left = t.per_part;
+    const int turns = (t.per_part + by - 1) / by;              // of an item
+    int left = turns;
     start(in, item);
-    start(at, item);
+    at = in;
     const T *gy, *x;
     T *y;
     auto from = [&]() {
@@ -520,22 +524,21 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
         const bool on = in.head < in.last;
         l.load(gy, on, next_g);
         l.load(x, p.norm && on, next_x);
-        ++in.head;
+        in.head += by;
         if (--left == 0) {
-            left = t.per_part;
-            start(in, in.item + teams);
+            left = turns;
+            start(in, in.item + step);
             from();
         } else {
-            gy += t.g_head;
-            x += t.x_head;
+            gy += by * t.g_head;
+            x += by * t.x_head;
         }
     };
     load();
     for (int64_t round = 0; round < rounds; ++round) {
-        if (at.head < at.last) l.template turns<false>(p, at.token, lane);
-        const int first = at.head;
+        if (WARP || at.head < at.last) l.template turns<WARP>(p, at.item < items ? at.token : 0, lane);
         bool any = false;
-        for (int i = 0; i < t.per_part; ++i) {
+        for (int i = 0; i < turns; ++i) {
             DsqPair g[L::P], v[L::P];
             L::values(next_g, g);
             L::values(next_x, v);
@@ -553,7 +556,7 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
                 const float mean = __fmaf_rn(sum, p.inv_d, p.eps), rstd = rsqrtf(mean);
                 const bool bad = on && !in_range(mean);
                 if (bad) {
-                    if (lane == 0) bad_heads[i >> 5] |= 1u << (i & 31);
+                    if (lane == 0) bad_heads[(at.head - at.begin) >> 5] |= 1u << ((at.head - at.begin) & 31);
                     any = true;
                     on = false;
                 }
@@ -569,11 +572,11 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
                 }
             }
             if (on) l.store(y, g);
-            ++at.head;
-            y += t.y_head;
+            at.head += by;
+            y += by * t.y_head;
         }
-        if (__any_sync(~0u, any)) wide_heads<T, true>(p, t, marks, lanes, t.per_part, at.token, first, INTER, mine);
-        start(at, at.item + teams);
+        if (__any_sync(~0u, any)) wide_heads<T, true>(p, t, marks, lanes, t.per_part, at.token, at.begin, INTER, mine);
+        start(at, at.item + step);
         to();
     }
     if (!t.part) return;
@@ -598,16 +601,18 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : 4) heads_bwd_ker
     }
 }
 
-// grad_w[c] = sum over the blocks of their sums, in one order: a warp a column, of q (blockIdx.y = 0) or k
+// grad_w[c] = sum over the blocks of their sums, in one order, of q (blockIdx.y = 0) or k: 128 threads a column, eight
+// columns, four loads of a thread on their way together
 struct SumParams {
     const float *part[2];
     float *out[2];
     int blocks[2], D;
 };
-__global__ void __launch_bounds__(1024) heads_sum_kernel(const SumParams p)
+constexpr int SUM_COLS = 8, SUM_ROWS = 128;
+__global__ void __launch_bounds__(SUM_COLS * SUM_ROWS) heads_sum_kernel(const SumParams p)
 {
-    __shared__ float s[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, col = blockIdx.x * 32 + x;
+    __shared__ float s[SUM_ROWS / 4][SUM_COLS + 1];
+    const int x = threadIdx.x % SUM_COLS, y = threadIdx.x / SUM_COLS, col = blockIdx.x * SUM_COLS + x;
     const float *part = p.part[blockIdx.y];
     const int rows = p.blocks[blockIdx.y];
     grid_dependency_wait();
@@ -615,19 +620,23 @@ __global__ void __launch_bounds__(1024) heads_sum_kernel(const SumParams p)
     if (!p.out[blockIdx.y]) return;
     float a = 0.f;
     if (col < p.D)
-        for (int r = y; r < rows; r += 256) {
-            float v[8];
+        for (int r = y; r < rows; r += 4 * SUM_ROWS) {
+            float v[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = r + 32 * i < rows ? __ldcg(part + (int64_t)(r + 32 * i) * p.D + col) : 0.f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) a += v[i];
+            for (int i = 0; i < 4; ++i) v[i] = r + SUM_ROWS * i < rows ? __ldcg(part + (int64_t)(r + SUM_ROWS * i) * p.D + col) : 0.f;
+            a += (v[0] + v[1]) + (v[2] + v[3]);
         }
-    s[y][x] = a;
+    // (a warp has four rows of the eight columns)
+    a += __shfl_xor_sync(~0u, a, 8);
+    a += __shfl_xor_sync(~0u, a, 16);
+    if ((threadIdx.x & 31) < SUM_COLS) s[threadIdx.x >> 5][x] = a;
     __syncthreads();
-    a = s[x][y];
+    if (threadIdx.x >= 32 * SUM_COLS) return;
+    const int c = threadIdx.x >> 5;
+    a = s[threadIdx.x & 31][c];
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(~0u, a, o);
-    if (x == 0 && blockIdx.x * 32 + y < p.D) p.out[blockIdx.y][blockIdx.x * 32 + y] = a;
+    if ((threadIdx.x & 31) == 0 && blockIdx.x * SUM_COLS + c < p.D) p.out[blockIdx.y][blockIdx.x * SUM_COLS + c] = a;
 }
 
 // ---- host ----------------------------------------------------------------------------
@@ -665,22 +674,24 @@ int check_rotary(const dsq_rotary_t *r, int64_t tokens, int dtype, float eps)
 
 template <class T> constexpr int vec_of() { return 16 / (int)sizeof(T); }
 
-// Parts of a token's heads: the fewest (each makes the token's turns) that give the resident teams two and a half
-// each (a whole number and a bit of rounds are paid as the next), eight heads a part at least; where there are few
-// tokens down to one.  Marks have room for MARKS words a block.
-void set_parts(Tensor &t, int64_t tokens, int heads, int64_t teams, int per_block)
+// Parts of a token's heads.  `resident` takers of parts go round together, as often as there are parts for them, and a
+// part costs its turns (as much as three heads, less than two where a warp shares them) and its heads, `by`
+// at a time: the cheapest. 
+// Marks have room for MARKS words a block.
+void set_parts(Tensor &t, int64_t tokens, int heads, int64_t resident, int by, int per_block)
 {
-    int64_t parts = (teams * 5 / 2 + tokens - 1) / tokens;
-    const int64_t most = tokens * 2 >= teams ? (heads + 7) / 8 : heads;
-    if (parts > most) parts = most;
-    if (parts < 1) parts = 1;
-    t.per_part = (int)((heads + parts - 1) / parts);
-    if (t.per_part > MARKS / per_block * 32) t.per_part = MARKS / per_block * 32;
+    int64_t best = -1;
+    const int most = heads < 64 ? heads : 64;
+    for (int parts = 1; parts <= most; ++parts) {
+        const int per_part = (heads + parts - 1) / parts;
+        if (per_part > MARKS / per_block * 32) continue;
+        const int64_t rounds = (tokens * parts + resident - 1) / resident, cost = rounds * ((by > 1 ? 2 : 3) + (per_part + by - 1) / by);
+        if (best >= 0 && cost >= best) continue;
+        best = cost;
+        t.per_part = per_part;
+    }
     t.parts = (heads + t.per_part - 1) / t.per_part;
 }
-
-// (of the backward kernel: as many as are resident)
-constexpr int SUM_BLOCKS_PER_SM = 4;
 
 template <class T, int VEC, int U, bool INTER, int L, bool BACK> int launch(Params &p, cudaStream_t s)
 {
@@ -689,30 +700,37 @@ template <class T, int VEC, int U, bool INTER, int L, bool BACK> int launch(Para
     if constexpr (!BACK) {
         // heads enough for the teams of a warp to share a token's
         const int heads = p.t[0].heads + p.t[1].heads;
-        const bool warp = L && heads >= 2 * (32 / p.lanes);
+        const bool warp = p.lanes < 32 && heads >= 2 * (32 / p.lanes);
         const int64_t items = warp ? BLOCK / 32 : per_block;
-        set_parts(p.t[0], p.tokens, heads, sms * 5 * items, (int)per_block);
+        set_parts(p.t[0], p.tokens, heads, sms * 5 * items, warp ? 32 / p.lanes : 1, (int)per_block);
         const int64_t blocks = (p.tokens * p.t[0].parts + items - 1) / items;
         if (blocks > 0x7FFFFFFF) return DSQ_ERR_SIZE;
-        const auto kernel = warp ? heads_fwd_kernel<T, VEC, U, INTER, L, L != 0> : heads_fwd_kernel<T, VEC, U, INTER, L, false>;
+        const auto kernel = warp ? heads_fwd_kernel<T, VEC, U, INTER, L, true> : heads_fwd_kernel<T, VEC, U, INTER, L, false>;
         return dsq_launch(kernel, dim3((unsigned)blocks), dim3(BLOCK), 0, s, pdl, 0, p);
     } else {
-        // what is resident together, shared among q and k as their heads are
-        const int64_t most = sms * (2 * U * VEC > 16 ? 2 : SUM_BLOCKS_PER_SM);
+        // what is resident together, shared among q and k as their tokens' costs are (set_parts)
+        const int64_t most = sms * (2 * U * VEC > 16 ? 2 : BACK_BLOCKS);
         int64_t blocks[2] = {0, 0};
+        // (where not all units are turned a warp's sharing gains nothing: 8192 tokens of 8 + 8 heads of 96, half of each
+        // turned, 36.8 us with it, 31.1 without)
+        const int teams = 32 / p.lanes;
+        const bool warp = L && p.t[0].heads >= teams && (!p.t[1].heads || p.t[1].heads >= teams);
+        const int64_t of_block = warp ? BLOCK / 32 : per_block;
         for (int i = 0; i < 2; ++i) {
             Tensor &t = p.t[i];
             if (!t.heads) continue;
-            int64_t share = most * t.heads / (p.t[0].heads + p.t[1].heads);
+            auto cost = [&](int heads) { return heads ? (warp ? 2 + (heads + teams - 1) / teams : 3 + heads) : 0; };
+            int64_t share = most * cost(t.heads) / (cost(p.t[0].heads) + cost(p.t[1].heads));
             if (share < 1) share = 1;
-            set_parts(t, p.tokens, t.heads, share * per_block, (int)per_block);
-            const int64_t need = (p.tokens * t.parts + per_block - 1) / per_block;
+            set_parts(t, p.tokens, t.heads, share * of_block, warp ? teams : 1, (int)per_block);
+            const int64_t need = (p.tokens * t.parts + of_block - 1) / of_block;
             blocks[i] = need < share ? need : share;
         }
         p.q_blocks = (int)blocks[0];
         p.k_blocks = (int)blocks[1];
         if (p.t[1].part) p.t[1].part = p.t[0].part + blocks[0] * p.D;
-        return dsq_launch(heads_bwd_kernel<T, VEC, U, INTER, L>, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK), 0, s, pdl, 0, p);
+        const auto kernel = warp ? heads_bwd_kernel<T, VEC, U, INTER, L, true> : heads_bwd_kernel<T, VEC, U, INTER, L, false>;
+        return dsq_launch(kernel, dim3((unsigned)(blocks[0] + blocks[1])), dim3(BLOCK), 0, s, pdl, 0, p);
     }
 }
 
@@ -810,7 +828,7 @@ size_t dsq_headnorm_bwd_workspace_bytes(int64_t head_dim)
 {
     if (head_dim <= 0 || head_dim > MAX_DIM) return DSQ_WS_BYTES;
     const int sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
-    return DSQ_WS_BYTES + (size_t)(sms * SUM_BLOCKS_PER_SM + 2) * (size_t)head_dim * 4;
+    return DSQ_WS_BYTES + (size_t)(sms * BACK_BLOCKS + 2) * (size_t)head_dim * 4;
 }
 
 int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64_t tokens,
@@ -862,7 +880,7 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
     for (int i = 0; i < 2; ++i) sp.part[i] = p.t[i].part;
     sp.blocks[0] = p.q_blocks; sp.blocks[1] = p.k_blocks;
     sp.D = p.D;
-    return dsq_launch(heads_sum_kernel, dim3((unsigned)((p.D + 31) / 32), 2), dim3(1024), 0, (cudaStream_t)stream,
+    return dsq_launch(heads_sum_kernel, dim3((unsigned)((p.D + SUM_COLS - 1) / SUM_COLS), 2), dim3(SUM_COLS * SUM_ROWS), 0, (cudaStream_t)stream,
                       dsq_launch_hooks().pdl, 0, sp);
 }
 
