@@ -12,11 +12,11 @@
 //     binary32 rounds it: one fused operation, the rounding of M being the same in s, t and the target's
 //     exponent.  Four instructions an element in all; where an element is -infinity, or M is large enough for its
 //     rounding to matter, (x - m) c instead, held above -1000 (six).
-//   * Alternatives: a thread's m says all there is to know of its elements but their order.  The block's
-//     threads form 128 groups; the top-th of the groups' largest elements bounds from below what can be among the
-//     first `top`, and only threads with an m above the bound read theirs again (from L2) and leave
-//     what passes in shared memory, where ranks are counted.  Order and ties are those of (value, lowest
-//     index), as one 64-bit key.
+//   * Alternatives: a thread leaves the largest element of each turn of its loop in shared memory.  Fours of
+//     threads form groups; the top-th of the groups' largest elements bounds from below what can be among the
+//     first `top`, and only turns whose largest is above the bound are read again (from L2), by as many threads as
+//     they have vectors; what passes goes to shared memory, where ranks are counted.  Order and ties are those of
+//     (value, lowest index), as one 64-bit key.
 #include "dsq_launch.h"
 #include "dsq_pairs.cuh"
 #include "dsq_ptx.cuh"
@@ -28,6 +28,7 @@ namespace {
 
 constexpr int MAX_TOP = 32, MAX_CLUSTER = 8, AHEAD = 4, SHARE = 4;      // SHARE: threads of a group
 constexpr int ROOM = 1088;        // of candidates: 128 threads' vectors where fewer groups than `top` have any
+constexpr int SLOTS = 16, HITS = 512;      // turns that are told apart, and how many may be read again
 constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // 2^x of what is lower is zero
 constexpr float NOTHING = -1000.f;
@@ -144,15 +145,26 @@ __device__ __forceinline__ float exponent(float x, float m, float c)
     const float M = m * c;
     return max_nan(fabsf(M) < FAR ? __fmaf_rn(x, c, -M) : (x - m) * c, NOTHING);
 }
-__device__ __forceinline__ Sums joined(const Sums &a, const Sums &b, float c)
+__device__ __forceinline__ void move_to(Sums &v, float m, float c)
 {
-    Sums r;
-    r.m = fmaxf(a.m, b.m);
-    const float da = between(a.m, r.m, c), db = between(b.m, r.m, c);
-    const float ea = ex2(da), eb = ex2(db);
-    r.s = __fmaf_rn(a.s, ea, b.s * eb);
-    r.t = __fmaf_rn(__fmaf_rn(a.s, da, a.t), ea, __fmaf_rn(b.s, db, b.t) * eb);
-    return r;
+    const float d = between(v.m, m, c), e = ex2(d);
+    v.t = __fmaf_rn(v.s, d, v.t) * e;
+    v.s *= e;
+    v.m = m;
+}
+// of the lanes of a warp, the same in all
+__device__ __forceinline__ Sums joined(Sums v, float c)
+{
+    float m = v.m;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    move_to(v, m, c);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) {
+        v.s += __shfl_xor_sync(~0u, v.s, o);
+        v.t += __shfl_xor_sync(~0u, v.t, o);
+    }
+    return v;
 }
 
 // Where a row's whole vectors lie: `head` single elements, nv vectors, `tail` single ones.
@@ -195,7 +207,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
     __shared__ Sums block_sums[MAX_CLUSTER];
     __shared__ unsigned long long lists[TOP ? MAX_CLUSTER * MAX_TOP : 1];      // of the first block: all blocks' first `top`
     __shared__ unsigned long long bests[TOP ? GROUPS : 1], found[TOP ? ROOM : 1], bound_key;
-    __shared__ int count;
+    __shared__ float slot_most[TOP ? SLOTS * THREADS : 1];
+    __shared__ uint32_t hit[TOP ? HITS : 1];                   // thread, slot
+    __shared__ int count, hits;
     const int rank = p.cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t row = blockIdx.x / p.cluster;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
@@ -259,6 +273,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
     };
     if (TOP && v0 + tid < v1) best_turn = 0;                   // (where m stays LOWEST: the first turn)
     bool general = false;                                      // elements of -infinity have been seen
+    // a slot's turns, its largest element so far
+    const int per_slot = (turns + SLOTS - 1) / SLOTS;
+    int slot = 0, in_slot = 0;
+    float so_far = 0.f;
+    auto note = [&](float most) {
+        if (!TOP) return;
+        so_far = in_slot == 0 ? most : fmaxf(so_far, most);
+        slot_most[slot * THREADS + tid] = so_far;
+        if (++in_slot == per_slot) {
+            in_slot = 0;
+            ++slot;
+        }
+    };
     uint4 next[AHEAD];
     if (turns > 0) load(0, next);
 #pragma unroll 1
@@ -267,7 +294,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) r[j] = next[j];
         if (turn + 1 < turns) load(turn + 1, next);
-        raise(largest<T>(r), turn);
+        const float most = largest<T>(r);
+        note(most);
+        raise(most, turn);
         const float M = m * c;
         if (!general && fabsf(M) < FAR) {
             const DsqPair s0 = s2, t0 = t2, less = dsq_pair_of(-M, -M);
@@ -297,7 +326,9 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
         for (int j = 0; j < AHEAD; ++j) any_vector(r[j]);
     }
     if (full < turns) {
-        raise(largest<T>(next), full);                         // (what is not there is -infinity)
+        const float most = largest<T>(next);                   // (what is not there is -infinity)
+        note(most);
+        raise(most, full);
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j)
             if (v0 + (full * AHEAD + j) * THREADS + tid < v1) any_vector(next[j]);
@@ -314,21 +345,19 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
     if (tid < singles) {
         const float v = dsq_to_f32(cut.row[cut.single(tid)]);
         // (-infinity and NaN as in the loop: less LOWEST nothing, and NaN)
-        Sums one = {fmaxf(v, LOWEST), 1.f, 0.f};
-        const float d = exponent(v, one.m, c);
-        one.s = ex2(d);
-        one.t = d * one.s;
-        sum = joined(sum, one, c);
+        const float one_m = fmaxf(v, LOWEST), d = exponent(v, one_m, c), e = ex2(d);
+        Sums one = {one_m, e, d * e};
+        const float both = fmaxf(sum.m, one_m);
+        move_to(sum, both, c);
+        move_to(one, both, c);
+        sum.s += one.s;
+        sum.t += one.t;
     }
-    for (int o = 16; o > 0; o >>= 1) {
-        const Sums other = {__shfl_xor_sync(~0u, sum.m, o), __shfl_xor_sync(~0u, sum.s, o), __shfl_xor_sync(~0u, sum.t, o)};
-        // (the lower lane's first, so that both lanes have the same)
-        sum = lane & o ? joined(other, sum, c) : joined(sum, other, c);
-    }
+    sum = joined(sum, c);
     if (lane == 0) warp_sums[warp] = sum;
     if (TOP) {
         if (tid == 0) {
-            count = 0;
+            count = hits = 0;
             bound_key = 0ull;
         }
         // the largest of a group, its index no lower than it is
@@ -363,34 +392,36 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
             if (at < ROOM) found[at] = key;
         };
         if (tid < singles) keep(dsq_to_f32(cut.row[cut.single(tid)]), cut.single(tid));
-        const bool some = best_turn >= 0 && (m > LOWEST ? key_of(m, cut.index(v0 + best_turn * AHEAD * THREADS + tid)) >= bound
-                                                        : true);
-        if (some && (m > LOWEST || key_of(LOWEST, 0) >= bound)) {
-#pragma unroll 1
-            for (int turn = 0; turn < turns; ++turn) {
-                uint4 r[AHEAD];
-                load(turn, r);
-                if (bound >> 32 && !(largest<T>(r) >= value_of(bound))) continue;
-#pragma unroll 1
-                for (int j = 0; j < AHEAD; ++j) {
-                    const int v = v0 + (turn * AHEAD + j) * THREADS + tid;
-                    if (v >= v1) break;
-                    float f[VEC];
-                    values<T>(r[j], f);
+        // turns that may have some, and their vectors, a thread each
+        const bool any_value = bound >> 32 == 0ull;
+        const float least = value_of(bound);
+        for (int i = 0; i * per_slot < turns; ++i) {
+            if (v0 + i * per_slot * AHEAD * THREADS + tid >= v1) break;
+            if (!any_value && !(slot_most[i * THREADS + tid] >= least)) continue;
+            const int at = atomicAdd(&hits, 1);
+            if (at < HITS) hit[at] = (uint32_t)tid | (uint32_t)i << 16;
+        }
+        __syncthreads();
+        const int per_hit = per_slot * AHEAD, n_hits = hits;
+        if (n_hits > HITS) {
+            if (tid == 0) count = ROOM + 1;                    // (more than there is room for)
+        } else {
+            for (int64_t w = tid; w < (int64_t)n_hits * per_hit; w += THREADS) {
+                const int h = (int)(w / per_hit), k = (int)(w - (int64_t)h * per_hit);
+                const int64_t v = v0 + ((int64_t)(hit[h] >> 16) * per_hit + k) * THREADS + (hit[h] & 0xFFFFu);
+                if (v >= v1) continue;
+                float f[VEC];
+                values<T>(load_16(vecs + v * VEC), f);
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) keep(f[i], cut.index(v) + i);
-                }
+                for (int i = 0; i < VEC; ++i) keep(f[i], cut.index((int)v) + i);
             }
         }
     }
     __syncthreads();
     if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     if (tid < 32) {
-        Sums all = warp_sums[tid & (THREADS / 32 - 1)];
-        for (int o = THREADS / 64; o > 0; o >>= 1) {
-            const Sums other = {__shfl_xor_sync(~0u, all.m, o), __shfl_xor_sync(~0u, all.s, o), __shfl_xor_sync(~0u, all.t, o)};
-            all = lane & o ? joined(other, all, c) : joined(all, other, c);
-        }
+        const Sums nothing_yet = {LOWEST, 0.f, 0.f};
+        const Sums all = joined(tid < THREADS / 32 ? warp_sums[tid] : nothing_yet, c);
         if (tid == 0) {
             if (p.cluster == 1) block_sums[0] = all;
             else {
@@ -449,8 +480,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
     if (p.cluster > 1) cluster_sync_all();
     else __syncthreads();
     if (rank != 0) return;
-    Sums all = block_sums[0];
-    for (int i = 1; i < p.cluster; ++i) all = joined(all, block_sums[i], c);
+    const Sums nothing_yet = {LOWEST, 0.f, 0.f};
+    const Sums all = joined(lane < p.cluster ? block_sums[lane] : nothing_yet, c);
     const float log_s = log2f(all.s);
     // (a row without any: everything is improbable, and there is nothing to be uncertain about)
     const bool empty = all.s == 0.f;
