@@ -230,12 +230,11 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
     }
 
     // one pass: m, s, t of this thread's elements, and in which turn m came
-    auto load = [&](int turn, uint4 (&r)[AHEAD]) {
+    const T *at = vecs + ((int64_t)v0 + tid) * VEC;            // of the next turn
+    auto load = [&](uint4 (&r)[AHEAD]) {
 #pragma unroll
-        for (int j = 0; j < AHEAD; ++j) {
-            const int v = v0 + (turn * AHEAD + j) * THREADS + tid;
-            r[j] = v < v1 ? load_16(vecs + (int64_t)v * VEC) : nothing<T>();
-        }
+        for (int j = 0; j < AHEAD; ++j) r[j] = load_16(at + j * THREADS * VEC);
+        at += AHEAD * THREADS * VEC;
     };
     const int turns = (v1 - v0 + THREADS * AHEAD - 1) / (THREADS * AHEAD), full = (v1 - v0) / (THREADS * AHEAD);
     float m = LOWEST;
@@ -287,13 +286,21 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
         }
     };
     uint4 next[AHEAD];
-    if (turns > 0) load(0, next);
+    // the last turn's vectors, as far as there are any
+    auto load_rest = [&]() {
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            next[j] = v0 + (full * AHEAD + j) * THREADS + tid < v1 ? load_16(at + j * THREADS * VEC) : nothing<T>();
+    };
+    if (full > 0) load(next);
+    else load_rest();
 #pragma unroll 1
     for (int turn = 0; turn < full; ++turn) {
         uint4 r[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) r[j] = next[j];
-        if (turn + 1 < turns) load(turn + 1, next);
+        if (turn + 1 < full) load(next);
+        else load_rest();
         const float most = largest<T>(r);
         note(most);
         raise(most, turn);
