@@ -26,6 +26,7 @@
 //     element vanish, a token that digits are not all of goes through the tensor core as bf16 or fp16 (exact products,
 //     twice the instructions).
 #include "dsq_groups.h"
+#include "dsq_pairs.cuh"
 #include "dsq_ptx.cuh"
 #include "dsq_tc_host.h"
 #include "dsq_types.cuh"
@@ -35,7 +36,7 @@ using namespace dsq_ptx;
 
 namespace {
 
-constexpr int ROWS = 8, PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;
+constexpr int PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;
 
 // ---- the router's choice ---------------------------------------------------------------
 // A warp a token: the largest key among those below the last, k times.  ITEMS logits a lane in
@@ -115,14 +116,15 @@ template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const R
 }
 
 // ---- preparation: slots by expert, digits ---------------------------------------------------
-struct Group {
-    int expert, first, n;             // slots first .. first + n - 1 of the sorted ones
+// a group as the kernels read it, in one access
+struct alignas(32) Group {
+    int expert, n, unused[2];
+    uint16_t slot[8];
 };
 // what lies in the workspace
 struct Work {
     int *groups;                      // how many
-    uint32_t *packed;                 // groups: expert | first << 10 | (n - 1) << 22
-    uint16_t *sorted;                 // slots by expert
+    Group *group;                     // by expert, the slots of an expert in their order
     uint8_t *lost;                    // [T][chunks_in]: digits are not all of x's chunk
     float *x_step, *mid_step;         // [T][chunks_in], [slots][chunks_out]: what the highest digit stands for
     uint8_t *x_digits, *mid_digits;   // [T][chunks_in][512], [slots][chunks_out][512]
@@ -141,42 +143,61 @@ struct MoeParams {
     int groups_in, groups_out;               // scales of a row
     uint32_t units_in, units_in_inv, units_out, units_out_inv;
     int odd, act, y_type;
+    int rows;                                // slots of a group, 4 or 8
 };
-__device__ __forceinline__ Group group_at(const Work &w, int i)
+__device__ __forceinline__ uint4 load_16(const void *p)
 {
-    const uint32_t v = w.packed[i];
-    return {(int)(v & 1023), (int)(v >> 10 & 4095), (int)(v >> 22) + 1};
+    uint4 r;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+// expert, n; and slots, all of them (behind the n-th: anything)
+struct Members {
+    int expert, n;
+    uint4 slots;
+    __device__ __forceinline__ int slot(int r) const
+    {
+        const uint32_t w = r & 4 ? (r & 2 ? slots.w : slots.z) : r & 2 ? slots.y : slots.x;
+        return (int)(r & 1 ? w >> 16 : w & 0xFFFFu);
+    }
+};
+__device__ __forceinline__ Members members_of(const Work &w, int i)
+{
+    const uint4 a = load_16(w.group + i), b = load_16(w.group[i].slot);
+    return {(int)a.x, (int)a.y, b};
 }
 
-// Sorts the slots whose expert there is, and cuts them into groups.  A block; `start`: MAX_EXPERTS values.
-__device__ __forceinline__ void sort_slots(const MoeParams &p, int *start)
+// Sorts the slots whose expert there is, and cuts them into groups.  A block.
+struct Sorting { int count[MAX_EXPERTS], group[MAX_EXPERTS]; };
+__device__ __forceinline__ void sort_slots(const MoeParams &p, Sorting &s)
 {
-    const int lane = threadIdx.x & 31, E = p.E, n = p.slots;
-    for (int e = threadIdx.x; e < E; e += blockDim.x) start[e] = 0;
+    const int lane = threadIdx.x & 31, E = p.E, n = p.slots, rows = p.rows, shift = rows == 8 ? 3 : 2;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) s.count[e] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
         const int id = p.ids[i];
-        if (id >= 0 && id < E) atomicAdd(&start[id], 1);
+        if (id >= 0 && id < E) atomicAdd(&s.count[id], 1);
     }
     __syncthreads();
     if (threadIdx.x >= 32) return;
-    int slots = 0, groups = 0;        // so far
+    int groups = 0;                   // so far
     for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane, count = e < E ? start[e] : 0, parts = (count + ROWS - 1) / ROWS;
-        int a = count, b = parts;
+        const int e = e0 + lane, count = e < E ? s.count[e] : 0, parts = (count + rows - 1) >> shift;
+        int b = parts;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int u = __shfl_up_sync(~0u, a, o), v = __shfl_up_sync(~0u, b, o);
-            if (lane >= o) {
-                a += u;
-                b += v;
-            }
+            const int v = __shfl_up_sync(~0u, b, o);
+            if (lane >= o) b += v;
         }
-        const int first = slots + a - count, g = groups + b - parts;
-        if (e < E) start[e] = first;
-        for (int i = 0; i < parts; ++i)
-            p.w.packed[g + i] = (uint32_t)e | (uint32_t)(first + i * ROWS) << 10 | (uint32_t)(min(ROWS, count - i * ROWS) - 1) << 22;
-        slots += __shfl_sync(~0u, a, 31);
+        const int g = groups + b - parts;
+        if (e < E) {
+            s.count[e] = 0;
+            s.group[e] = g;
+        }
+        for (int i = 0; i < parts; ++i) {
+            p.w.group[g + i].expert = e;
+            p.w.group[g + i].n = min(rows, count - i * rows);
+        }
         groups += __shfl_sync(~0u, b, 31);
     }
     if (lane == 0) *p.w.groups = groups;
@@ -185,11 +206,12 @@ __device__ __forceinline__ void sort_slots(const MoeParams &p, int *start)
         int id = i0 + lane < n ? p.ids[i0 + lane] : -1;
         if (id < 0 || id >= E) id = -1;
         const uint32_t same = __match_any_sync(~0u, id);
-        const int at = id >= 0 ? start[id] : 0;
+        const int at = id >= 0 ? s.count[id] : 0;
         __syncwarp();
         if (id >= 0) {
-            p.w.sorted[at + __popc(same & ((1u << lane) - 1))] = (uint16_t)(i0 + lane);
-            if (lane == 31 - __clz(same)) start[id] = at + __popc(same);
+            const int pos = at + __popc(same & ((1u << lane) - 1));
+            p.w.group[s.group[id] + (pos >> shift)].slot[pos & (rows - 1)] = (uint16_t)(i0 + lane);
+            if (lane == 31 - __clz(same)) s.count[id] = at + __popc(same);
         }
         __syncwarp();
     }
@@ -243,11 +265,11 @@ constexpr int PREPARE_WARPS = 8;
 // block 0: the slots; the others' warps a chunk of a token each
 template <int XT, bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_prepare_kernel(const __grid_constant__ MoeParams p)
 {
-    __shared__ int start[MAX_EXPERTS];
+    __shared__ Sorting sorting;
     grid_dependency_wait();
     grid_launch_dependents();
     if (blockIdx.x == 0) {
-        sort_slots(p, start);
+        sort_slots(p, sorting);
         return;
     }
     const int i = (blockIdx.x - 1) * PREPARE_WARPS + (threadIdx.x >> 5), lane = threadIdx.x & 31;
@@ -303,12 +325,6 @@ __device__ __forceinline__ int scale_of(uint32_t unit, uint32_t units, uint32_t 
 __device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-__device__ __forceinline__ uint4 load_16(const void *p)
-{
-    uint4 r;
-    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
 }
 
 // Codes of 8 NT columns and the scales of a chunk's 4 / GP units, as dsq_wgemm_group.cu keeps them.
@@ -398,7 +414,7 @@ template <int TILES> struct Sources {
 
 // total += scale step (sum of digits times codes) of a chunk
 template <int TILES, int NT, int GP>
-__device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const Digits<TILES> &r, float (&total)[TILES][NT][4])
+__device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const Digits<TILES> &r, DsqPair (&total)[TILES][NT][2])
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES;
@@ -424,12 +440,14 @@ __device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const
             }
             if (q % GP == GP - 1) {
                 const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
+                const DsqPair scales = dsq_pair_of(__uint_as_float(sv.x), __uint_as_float(sv.y)), less = dsq_pair_of(-MAGIC, -MAGIC);
 #pragma unroll
                 for (int m = 0; m < TILES; ++m) {
-                    const float s0 = __uint_as_float(sv.x) * r.step[m], s1 = __uint_as_float(sv.y) * r.step[m];
+                    const DsqPair by = dsq_pair_mul(scales, dsq_pair_of(r.step[m], r.step[m]));
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        total[m][t][e] = __fmaf_rn(__int_as_float(acc[m][e]) - MAGIC, e & 1 ? s1 : s0, total[m][t][e]);
+                    for (int e = 0; e < 2; ++e)
+                        total[m][t][e] = dsq_pair_fma(dsq_pair_add(dsq_pair_of(__int_as_float(acc[m][2 * e]), __int_as_float(acc[m][2 * e + 1])), less),
+                                                      by, total[m][t][e]);
                 }
             }
         }
@@ -499,19 +517,19 @@ constexpr int IN_WARPS = 8, OUT_WARPS = 4;
 
 // What is behind a warp's sums of a group, shared by both forms: WC warps side by side on 16 columns of gate and
 // other half each, IN_WARPS / WC along K.
-template <int XT, int GP, int WC, int STAGES> struct In {
+template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
     using S = Stage<NT, GP>;
-    static constexpr int KW = IN_WARPS / WC, RING = IN_WARPS * STAGES * S::BYTES, SUMS = IN_WARPS * 2 * NT * 512;
+    static constexpr int KW = IN_WARPS / WC, RING = IN_WARPS * STAGES * S::BYTES, SUMS = IN_WARPS * MOST * NT * 512;
     static constexpr int BYTES = RING > SUMS ? RING : SUMS;
 
     const MoeParams &p;
-    const Group g;
+    const Members g;
     uint8_t *smem;
     int warp, lane, n, j, wk, c0, turns, to_turn, issued;
     uint32_t ring;
     Copies<NT, GP> copies;
 
-    __device__ __forceinline__ In(const MoeParams &p_, const Group &g_, uint8_t *smem_) : p(p_), g(g_), smem(smem_)
+    __device__ __forceinline__ In(const MoeParams &p_, const Members &g_, uint8_t *smem_) : p(p_), g(g_), smem(smem_)
     {
         warp = threadIdx.x >> 5; lane = threadIdx.x & 31; n = lane >> 2; j = lane & 3;
         wk = warp / WC;
@@ -539,7 +557,7 @@ template <int XT, int GP, int WC, int STAGES> struct In {
         const int at = blockIdx.x * WC * 16 + c;
         if (at >= p.chunks_out * 128) return;
         // (columns behind the last are zeros up to the end of the chunk)
-        p.w.mid[(int64_t)p.w.sorted[g.first + r] * p.chunks_out * 128 + at] = at < p.I ? activated(gate, p.act) * up : 0.f;
+        p.w.mid[(int64_t)g.slot(r) * p.chunks_out * 128 + at] = at < p.I ? activated(gate, p.act) * up : 0.f;
     }
 
     template <int TILES> __device__ __forceinline__ void digits()
@@ -550,13 +568,13 @@ template <int XT, int GP, int WC, int STAGES> struct In {
 #pragma unroll
         for (int m = 0; m < TILES; ++m) {
             const int r = 4 * m + (n >> 1);
-            const int token = r < g.n ? p.w.sorted[g.first + r] / p.k : -1;
+            const int token = r < g.n ? g.slot(r) / p.k : -1;
             if (token < 0) from.set(m, nullptr, nullptr);
             else from.set(m, p.w.x_digits + (int64_t)token * p.chunks_in * 512, p.w.x_step + (int64_t)token * p.chunks_in);
         }
         if (turns > 0) from.load(wk, d);
         if (turns > 1) from.touch(wk + KW);
-        float total[TILES][NT][4] = {};
+        DsqPair total[TILES][NT][2] = {};
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
             cp_async_wait<STAGES - 2>();
@@ -574,7 +592,7 @@ template <int XT, int GP, int WC, int STAGES> struct In {
         for (int m = 0; m < TILES; ++m)
 #pragma unroll
             for (int t = 0; t < NT; ++t)
-                part[((warp * TILES + m) * NT + t) * 32 + lane] = make_float4(total[m][t][0], total[m][t][1], total[m][t][2], total[m][t][3]);
+                reinterpret_cast<ulonglong2 *>(part)[((warp * TILES + m) * NT + t) * 32 + lane] = make_ulonglong2(total[m][t][0], total[m][t][1]);
         __syncthreads();
         const float unit = dsq_value_unit<DSQ_I8>(p.odd);
         const float *sums = reinterpret_cast<const float *>(smem);
@@ -602,7 +620,7 @@ template <int XT, int GP, int WC, int STAGES> struct In {
     __device__ __forceinline__ void sixteen()
     {
         const uint32_t base = dsq_value_base<XT>(p.odd);
-        const uint8_t *x = n < g.n ? p.X + (int64_t)(p.w.sorted[g.first + n] / p.k) * p.H * 2 : nullptr;
+        const uint8_t *x = n < g.n ? p.X + (int64_t)(g.slot(n) / p.k) * p.H * 2 : nullptr;
         float total[NT][4] = {};
 #pragma unroll 1
         for (int i = 0; i < turns; ++i) {
@@ -634,31 +652,34 @@ template <int XT, int GP, int WC, int STAGES> struct In {
     }
 };
 
-template <int XT, int GP, int WC, int STAGES>
-__global__ void __launch_bounds__(IN_WARPS * 32, 2) moe_in_kernel(const __grid_constant__ MoeParams p)
+// MOST: tiles of four slots of a group, 1 or 2 (fewer registers, more warps)
+template <int XT, int GP, int WC, int MOST, int STAGES>
+__global__ void __launch_bounds__(IN_WARPS * 32, MOST == 1 ? 3 : 2) moe_in_kernel(const __grid_constant__ MoeParams p)
 {
-    using L = In<XT, GP, WC, STAGES>;
+    using L = In<XT, GP, WC, MOST, STAGES>;
     extern __shared__ __align__(128) uint8_t smem[];
     grid_dependency_wait();
     grid_launch_dependents();
+    // (what is there of a group that is not is not used)
+    Members g = members_of(p.w, blockIdx.y);
     const int groups = *p.w.groups;
-    for (int i = blockIdx.y; i < groups; i += gridDim.y) {
-        L l(p, group_at(p.w, i), smem);
+    for (int i = blockIdx.y; i < groups; i += gridDim.y, g = members_of(p.w, min(i, groups - 1))) {
+        L l(p, g, smem);
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) l.issue();
         bool lost = false;
         if (!p.odd)
             for (int e = threadIdx.x; e < l.g.n * p.chunks_in; e += IN_WARPS * 32)
-                lost = lost || p.w.lost[p.w.sorted[l.g.first + e / p.chunks_in] / p.k * p.chunks_in + e % p.chunks_in];
+                lost = lost || p.w.lost[l.g.slot(e / p.chunks_in) / p.k * p.chunks_in + e % p.chunks_in];
         if (!p.odd && __syncthreads_or(lost)) l.sixteen();
-        else if (l.g.n <= 4) l.template digits<1>();
-        else l.template digits<2>();
+        else if (MOST == 1 || l.g.n <= 4) l.template digits<1>();
+        else l.template digits<MOST>();
     }
 }
 
 // WC warps side by side on 32 columns each, OUT_WARPS / WC (and the cluster's blocks) along the chunks
-template <int GP, int WC, int STAGES>
-__global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
+template <int GP, int WC, int MOST, int STAGES>
+__global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
 {
     constexpr int KW = OUT_WARPS / WC, WIDE = 8 * NT, COLS = WC * WIDE, THREADS = OUT_WARPS * 32;
     using S = Stage<NT, GP>;
@@ -680,7 +701,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
     int ig = q0 / chunks, ic = q0 - ig * chunks;                // of the next copy
     Copies<NT, GP> copies;
     auto columns_of = [&](int i) {
-        const int64_t row0 = (int64_t)(p.w.packed[i] & 1023) * p.H;
+        const int64_t row0 = (int64_t)p.w.group[i].expert * p.H;
 #pragma unroll
         for (int t = 0; t < NT; ++t) copies.w[t] = p.W_out + (row0 + min(c0 + 8 * t + n, (int64_t)p.H - 1)) * p.pitch_out + 16 * j;
         copies.scale = p.s_out + row0 + min(c0 + lane, (int64_t)p.H - 1);
@@ -703,17 +724,17 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
     grid_dependency_wait();
     grid_launch_dependents();
 
-    Group g = {};
-    Sources<2> from;
-    Digits<2> d = {};
+    Members g = {};
+    Sources<MOST> from;
+    Digits<MOST> d = {};
     int cg = q0 / chunks, cc = q0 - cg * chunks;                // of the chunk at hand
     auto rows_of = [&](int i) {
-        g = group_at(p.w, i);
+        g = members_of(p.w, i);
         d = {};
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+        for (int m = 0; m < MOST; ++m) {
             const int r = 4 * m + (n >> 1);
-            const int slot = r < g.n ? p.w.sorted[g.first + r] : -1;
+            const int slot = r < g.n ? g.slot(r) : -1;
             if (slot < 0) from.set(m, nullptr, nullptr);
             else from.set(m, p.w.mid_digits + (int64_t)slot * chunks * 512, p.w.mid_step + (int64_t)slot * chunks);
         }
@@ -722,7 +743,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
         rows_of(cg);
         from.load(cc, d);
     }
-    float total[2][NT][4] = {};
+    DsqPair total[MOST][NT][2] = {};
     // what a lane's digits n & 1 and (n & 1) + 2 stand for, in steps
     const float high = n & 1 ? 0x1p-8f : 1.f, low = n & 1 ? 0x1p-24f : 0x1p-16f;
 #pragma unroll 1
@@ -731,14 +752,18 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
         __syncwarp();
         issue(i + STAGES - 1);
         const uint32_t at = ring + (uint32_t)((i - q0) % STAGES * S::BYTES);
-        if (g.n <= 4) {
-            Digits<1> d1;
+        if constexpr (MOST == 2) {
+            if (g.n <= 4) {
+                Digits<1> d1;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) d1.x[0][q] = d.x[0][q];
-            d1.step[0] = d.step[0];
-            multiply_digits<1, NT, GP>(at, one, d1, reinterpret_cast<float (&)[1][NT][4]>(total));
+                for (int q = 0; q < 4; ++q) d1.x[0][q] = d.x[0][q];
+                d1.step[0] = d.step[0];
+                multiply_digits<1, NT, GP>(at, one, d1, reinterpret_cast<DsqPair (&)[1][NT][2]>(total));
+            } else {
+                multiply_digits<2, NT, GP>(at, one, d, total);
+            }
         } else {
-            multiply_digits<2, NT, GP>(at, one, d, total);
+            multiply_digits<1, NT, GP>(at, one, d, total);
         }
         if (++cc < chunks && i + 1 < q1) {
             from.load(cc, d);
@@ -747,27 +772,33 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
         }
         // the group's sums to the tokens' rows, one slot after the other (two may be the same token's)
 #pragma unroll
-        for (int m = 0; m < 2; ++m) {
+        for (int m = 0; m < MOST; ++m) {
             if (4 * m >= g.n) break;
 #pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const float v = __fmaf_rn(total[m][t][e + 2], low, total[m][t][e] * high);
-                    total[m][t][e] = v + __shfl_xor_sync(~0u, v, 4);
-                }
+            for (int t = 0; t < NT; ++t) {
+                float h0, h1, l0, l1;
+                dsq_halves(total[m][t][0], h0, h1);
+                dsq_halves(total[m][t][1], l0, l1);
+                h0 = __fmaf_rn(l0, low, h0 * high);
+                h1 = __fmaf_rn(l1, low, h1 * high);
+                h0 += __shfl_xor_sync(~0u, h0, 4);
+                h1 += __shfl_xor_sync(~0u, h1, 4);
+                total[m][t][0] = dsq_pair_of(h0, h1);
+            }
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
                 if (4 * m + r >= g.n) break;
                 if (n == 2 * r) {
-                    const int slot = p.w.sorted[g.first + 4 * m + r], token = slot / p.k;
+                    const int slot = g.slot(4 * m + r), token = slot / p.k;
                     const float w = p.weights[slot];
 #pragma unroll
                     for (int t = 0; t < NT; ++t) {
                         float2 *to = reinterpret_cast<float2 *>(mine + token * WIDE + 8 * t + 2 * j);
                         float2 v = *to;
-                        v.x = __fmaf_rn(total[m][t][0], w, v.x);
-                        v.y = __fmaf_rn(total[m][t][1], w, v.y);
+                        float h0, h1;
+                        dsq_halves(total[m][t][0], h0, h1);
+                        v.x = __fmaf_rn(h0, w, v.x);
+                        v.y = __fmaf_rn(h1, w, v.y);
                         *to = v;
                     }
                 }
@@ -776,7 +807,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
 #pragma unroll
             for (int t = 0; t < NT; ++t)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) total[m][t][e] = 0.f;
+                for (int e = 0; e < 2; ++e) total[m][t][e] = 0ull;
         }
         if (cc == chunks) {
             cc = 0;
@@ -826,10 +857,8 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 3) moe_out_kernel(const __grid
 }
 
 // ---- host ------------------------------------------------------------------------------------
-constexpr int IN_STAGES = 4, OUT_STAGES = 4;
-
-// from how many tokens on warps lie side by side, so that they share rows of digits in L1
-constexpr int WIDE_FROM = 9;
+template <int MOST> constexpr int IN_STAGES = MOST == 1 ? 3 : 4;
+constexpr int OUT_STAGES = 4;
 
 template <int XT, int GP> int launch_prepare(const MoeParams &p, cudaStream_t s)
 {
@@ -837,12 +866,12 @@ template <int XT, int GP> int launch_prepare(const MoeParams &p, cudaStream_t s)
     return dsq_launch(moe_prepare_kernel<XT, GP == 4>, dim3(blocks), dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int XT, int GP, int WC> int launch_in(const MoeParams &p, cudaStream_t s)
+template <int XT, int GP, int WC, int MOST> int launch_in(const MoeParams &p, cudaStream_t s)
 {
-    constexpr int bytes = In<XT, GP, WC, IN_STAGES>::BYTES;
-    static_assert(bytes <= 112 * 1024, "shared memory");
+    constexpr int bytes = In<XT, GP, WC, MOST, IN_STAGES<MOST>>::BYTES;
+    static_assert(bytes <= (MOST == 1 ? 74 : 112) * 1024, "shared memory");
     static std::atomic<unsigned long long> configured{0};
-    const auto kernel = moe_in_kernel<XT, GP, WC, IN_STAGES>;
+    const auto kernel = moe_in_kernel<XT, GP, WC, MOST, IN_STAGES<MOST>>;
     const int st = dsq_allow_smem((const void *)kernel, bytes, &configured);
     if (st) return st;
     // (to the end of the last chunk: zeros)
@@ -850,17 +879,17 @@ template <int XT, int GP, int WC> int launch_in(const MoeParams &p, cudaStream_t
     return dsq_launch(kernel, grid, dim3(IN_WARPS * 32), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int GP, int WC> int launch_out(const MoeParams &p, cudaStream_t s)
+template <int GP, int WC, int MOST> int launch_out(const MoeParams &p, cudaStream_t s)
 {
     constexpr int ring = OUT_WARPS * OUT_STAGES * Stage<NT, GP>::BYTES, row = OUT_WARPS * 8 * NT * 4, cols = WC * 8 * NT;
     static_assert(ring + PASS_TOKENS * row <= 200 * 1024, "shared memory");
     static std::atomic<unsigned long long> configured{0};
-    const auto kernel = moe_out_kernel<GP, WC, OUT_STAGES>;
+    const auto kernel = moe_out_kernel<GP, WC, MOST, OUT_STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, ring + PASS_TOKENS * row, &configured);
     if (st) return st;
     const int tiles = (p.H + cols - 1) / cols, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
     int cluster = 1;
-    while (cluster < 8 && tiles * cluster * 2 <= 3 * sms) cluster *= 2;
+    while (cluster < 8 && tiles * cluster * 2 <= (MOST == 1 ? 4 : 3) * sms) cluster *= 2;
     return dsq_launch(kernel, dim3((unsigned)(tiles * cluster)), dim3(OUT_WARPS * 32), (size_t)(ring + p.T * row), s,
                       dsq_launch_hooks().pdl, cluster, p, cluster);
 }
@@ -869,14 +898,14 @@ template <int XT, int GP> int pick_in(const MoeParams &p, cudaStream_t s)
 {
     const int st = launch_prepare<XT, GP>(p, s);
     if (st) return st;
-    return p.T < WIDE_FROM ? launch_in<XT, GP, 1>(p, s) : launch_in<XT, GP, 4>(p, s);
+    return p.rows == 4 ? launch_in<XT, GP, 1, 1>(p, s) : launch_in<XT, GP, 4, 2>(p, s);
 }
 template <int GP> int pick_out(const MoeParams &p, cudaStream_t s)
 {
     const int st = dsq_launch(moe_mid_kernel<GP == 4>, dim3((p.slots * p.chunks_out + PREPARE_WARPS - 1) / PREPARE_WARPS),
                               dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
     if (st) return st;
-    return p.T < WIDE_FROM ? launch_out<GP, 1>(p, s) : launch_out<GP, 4>(p, s);
+    return p.rows == 4 ? launch_out<GP, 1, 1>(p, s) : launch_out<GP, 4, 2>(p, s);
 }
 
 int chunks_of(int64_t K) { return (int)((K + 127) / 128); }
@@ -891,8 +920,7 @@ size_t lay_out(Work &w, char *base, int T, int slots, int chunks_in, int chunks_
         return p;
     };
     w.groups = (int *)take(4);
-    w.packed = (uint32_t *)take((size_t)slots * 4);
-    w.sorted = (uint16_t *)take((size_t)slots * 2);
+    w.group = (Group *)take((size_t)slots * sizeof(Group));
     w.lost = (uint8_t *)take((size_t)T * chunks_in);
     w.x_step = (float *)take((size_t)T * chunks_in * 4);
     w.mid_step = (float *)take((size_t)slots * chunks_out * 4);
@@ -974,6 +1002,9 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
     for (int64_t t = 0; t < T; t += PASS_TOKENS) {
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
+        // Groups of four where few experts can be expected to have more; else of eight, whose warps lie side by side and
+        // share the rows of digits in L1.
+        p.rows = p.T <= 4 || p.slots <= 3 * p.E ? 4 : 8;
         lay_out(p.w, (char *)workspace, p.T, p.slots, p.chunks_in, p.chunks_out);
         p.X = (const uint8_t *)X + t * H * 2;
         p.ids = ids + t * k; p.weights = weights + t * k;
