@@ -418,36 +418,54 @@ __device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES;
+    // (SIDE tiles of columns together: an instruction's sums are 20 clocks away from the next one's)
+    constexpr int SIDE = 2;
 #pragma unroll
-    for (int t = 0; t < NT; ++t) {
-        uint32_t w[4];
-        if (GP == 4) {
-            const uint4 v = lds_128(at + t * 512 + n * 64 + ((j ^ (n >> 1)) & 3) * 16);
-            w[0] = v.x; w[1] = v.y; w[2] = v.z; w[3] = v.w;
-        } else {
+    for (int t0 = 0; t0 < NT; t0 += SIDE) {
+        uint32_t w[SIDE][4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) w[q] = lds_32(at + t * 512 + n * 64 + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
+        for (int s = 0; s < SIDE; ++s) {
+            const uint32_t from = at + (t0 + s) * 512 + n * 64;
+            if (GP == 4) {
+                const uint4 v = lds_128(from + ((j ^ (n >> 1)) & 3) * 16);
+                w[s][0] = v.x; w[s][1] = v.y; w[s][2] = v.z; w[s][3] = v.w;
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) w[s][q] = lds_32(from + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
+            }
         }
-        int acc[TILES][4];
+        int acc[SIDE][TILES][4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-            const uint32_t b0 = ((w[q] << 4) & 0xF0F0F0F0u) | one, b1 = (w[q] & 0xF0F0F0F0u) | one;
+            uint32_t b[SIDE][2];
 #pragma unroll
-            for (int m = 0; m < TILES; ++m) {
-                const uint32_t a[4] = {r.x[m][q].x, r.x[m][q].y, r.x[m][q].z, r.x[m][q].w};
-                if (q % GP == 0) mma_i8_first(acc[m], a, b0, b1);
-                else mma_i8(acc[m], a, b0, b1);
+            for (int s = 0; s < SIDE; ++s) {
+                b[s][0] = ((w[s][q] << 4) & 0xF0F0F0F0u) | one;
+                b[s][1] = (w[s][q] & 0xF0F0F0F0u) | one;
             }
+#pragma unroll
+            for (int m = 0; m < TILES; ++m)
+#pragma unroll
+                for (int s = 0; s < SIDE; ++s) {
+                    const uint32_t a[4] = {r.x[m][q].x, r.x[m][q].y, r.x[m][q].z, r.x[m][q].w};
+                    if (q % GP == 0) mma_i8_first(acc[s][m], a, b[s][0], b[s][1]);
+                    else mma_i8(acc[s][m], a, b[s][0], b[s][1]);
+                }
             if (q % GP == GP - 1) {
-                const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
-                const DsqPair scales = dsq_pair_of(__uint_as_float(sv.x), __uint_as_float(sv.y)), less = dsq_pair_of(-MAGIC, -MAGIC);
 #pragma unroll
-                for (int m = 0; m < TILES; ++m) {
-                    const DsqPair by = dsq_pair_mul(scales, dsq_pair_of(r.step[m], r.step[m]));
+                for (int s = 0; s < SIDE; ++s) {
+                    const int t = t0 + s;
+                    const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
+                    const DsqPair scales = dsq_pair_of(__uint_as_float(sv.x), __uint_as_float(sv.y)), less = dsq_pair_of(-MAGIC, -MAGIC);
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        total[m][t][e] = dsq_pair_fma(dsq_pair_add(dsq_pair_of(__int_as_float(acc[m][2 * e]), __int_as_float(acc[m][2 * e + 1])), less),
-                                                      by, total[m][t][e]);
+                    for (int m = 0; m < TILES; ++m) {
+                        const DsqPair by = dsq_pair_mul(scales, dsq_pair_of(r.step[m], r.step[m]));
+#pragma unroll
+                        for (int e = 0; e < 2; ++e)
+                            total[m][t][e] = dsq_pair_fma(
+                                dsq_pair_add(dsq_pair_of(__int_as_float(acc[s][m][2 * e]), __int_as_float(acc[s][m][2 * e + 1])), less), by,
+                                total[m][t][e]);
+                    }
                 }
             }
         }
@@ -898,7 +916,7 @@ template <int XT, int GP> int pick_in(const MoeParams &p, cudaStream_t s)
 {
     const int st = launch_prepare<XT, GP>(p, s);
     if (st) return st;
-    return p.rows == 4 ? launch_in<XT, GP, 1, 1>(p, s) : launch_in<XT, GP, 4, 2>(p, s);
+    return p.rows == 4 ? launch_in<XT, GP, 2, 1>(p, s) : launch_in<XT, GP, 4, 2>(p, s);
 }
 template <int GP> int pick_out(const MoeParams &p, cudaStream_t s)
 {
