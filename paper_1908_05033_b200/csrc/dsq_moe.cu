@@ -22,21 +22,13 @@
 //     memory.  Its first codes are on their way while the kernels ahead still run.
 //   * Sums of up to 128 codes are exact in int32; they enter the totals in binary32.  Digits leave of an
 //     element what is below 2^-31 of the largest of its 128: for the codes' grid Delta (c + 1/2),
-//     which has no 0, that is below the rounding of the sums.  For the grid Delta c, whose 0 can make the largest
-//     element vanish, a token that digits are not all of goes through the tensor core as bf16 or fp16 (exact products,
-//     twice the instructions).
-#include "dsq_groups.h"
-#include "dsq_pairs.cuh"
-#include "dsq_ptx.cuh"
-#include "dsq_tc_host.h"
-#include "dsq_types.cuh"
-#include "dsq_wgemm_group.cuh"
+//     which has no 0, that is below the rounding of the sums.  The grid Delta c, whose 0 can make the largest
+//     element vanish, and experts with more slots go on 16 bits (dsq_moe_wide.cu).
+#include "dsq_moe.cuh"
 
-using namespace dsq_ptx;
+using namespace dsq_moe;
 
 namespace {
-
-constexpr int PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;
 
 // ---- the router's choice ---------------------------------------------------------------
 // A warp a token: the largest key among those below the last, k times.  ITEMS logits a lane in
@@ -115,115 +107,29 @@ template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const R
     }
 }
 
-// ---- preparation: slots by expert, digits ---------------------------------------------------
-// a group as the kernels read it, in one access
-struct alignas(32) Group {
-    int expert, n, unused[2];
-    uint16_t slot[8];
-};
-// what lies in the workspace
-struct Work {
-    int *groups;                      // how many
-    Group *group;                     // by expert, the slots of an expert in their order
-    uint8_t *lost;                    // [T][chunks_in]: digits are not all of x's chunk
-    float *x_step, *mid_step;         // [T][chunks_in], [slots][chunks_out]: what the highest digit stands for
-    uint8_t *x_digits, *mid_digits;   // [T][chunks_in][512], [slots][chunks_out][512]
-    float *mid;                       // [slots][128 chunks_out]
-};
-struct MoeParams {
-    Work w;
-    const uint8_t *X, *W_in, *W_out;
-    const float *s_in, *s_out, *weights;
-    const int32_t *ids;
-    const void *residual;
-    void *Y;
-    int T, H, I, E, k, slots;
-    int pitch_in, pitch_out;                 // bytes of a row of codes
-    int chunks_in, chunks_out;               // of 128 codes in a row
-    int groups_in, groups_out;               // scales of a row
-    uint32_t units_in, units_in_inv, units_out, units_out_inv;
-    int odd, act, y_type;
-    int rows;                                // slots of a group, 4 or 8
-};
-__device__ __forceinline__ uint4 load_16(const void *p)
-{
-    uint4 r;
-    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
-    return r;
-}
-// expert, n; and slots, all of them (behind the n-th: anything)
+// ---- preparation ---------------------------------------------------------------------------
+// expert, n and the slots of a group of up to four
 struct Members {
     int expert, n;
-    uint4 slots;
+    uint2 slots;
     __device__ __forceinline__ int slot(int r) const
     {
-        const uint32_t w = r & 4 ? (r & 2 ? slots.w : slots.z) : r & 2 ? slots.y : slots.x;
+        const uint32_t w = r & 2 ? slots.y : slots.x;
         return (int)(r & 1 ? w >> 16 : w & 0xFFFFu);
     }
 };
 __device__ __forceinline__ Members members_of(const Work &w, int i)
 {
     const uint4 a = load_16(w.group + i), b = load_16(w.group[i].slot);
-    return {(int)a.x, (int)a.y, b};
-}
-
-// Sorts the slots whose expert there is, and cuts them into groups.  A block.
-struct Sorting { int count[MAX_EXPERTS], group[MAX_EXPERTS]; };
-__device__ __forceinline__ void sort_slots(const MoeParams &p, Sorting &s)
-{
-    const int lane = threadIdx.x & 31, E = p.E, n = p.slots, rows = p.rows, shift = rows == 8 ? 3 : 2;
-    for (int e = threadIdx.x; e < E; e += blockDim.x) s.count[e] = 0;
-    __syncthreads();
-    for (int i = threadIdx.x; i < n; i += blockDim.x) {
-        const int id = p.ids[i];
-        if (id >= 0 && id < E) atomicAdd(&s.count[id], 1);
-    }
-    __syncthreads();
-    if (threadIdx.x >= 32) return;
-    int groups = 0;                   // so far
-    for (int e0 = 0; e0 < E; e0 += 32) {
-        const int e = e0 + lane, count = e < E ? s.count[e] : 0, parts = (count + rows - 1) >> shift;
-        int b = parts;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(~0u, b, o);
-            if (lane >= o) b += v;
-        }
-        const int g = groups + b - parts;
-        if (e < E) {
-            s.count[e] = 0;
-            s.group[e] = g;
-        }
-        for (int i = 0; i < parts; ++i) {
-            p.w.group[g + i].expert = e;
-            p.w.group[g + i].n = min(rows, count - i * rows);
-        }
-        groups += __shfl_sync(~0u, b, 31);
-    }
-    if (lane == 0) *p.w.groups = groups;
-    __syncwarp();
-    for (int i0 = 0; i0 < n; i0 += 32) {
-        int id = i0 + lane < n ? p.ids[i0 + lane] : -1;
-        if (id < 0 || id >= E) id = -1;
-        const uint32_t same = __match_any_sync(~0u, id);
-        const int at = id >= 0 ? s.count[id] : 0;
-        __syncwarp();
-        if (id >= 0) {
-            const int pos = at + __popc(same & ((1u << lane) - 1));
-            p.w.group[s.group[id] + (pos >> shift)].slot[pos & (rows - 1)] = (uint16_t)(i0 + lane);
-            if (lane == 31 - __clz(same)) s.count[id] = at + __popc(same);
-        }
-        __syncwarp();
-    }
+    return {(int)a.x, (int)a.y, make_uint2(b.x, b.y)};
 }
 
 // The four digits of a chunk of 128 elements, by a warp: f holds elements 4 lane .. 4 lane + 3.  512 bytes, as an
 // instruction's rows want them: a lane of row n (and n + 8) has digits d = n & 1 (and d + 2) of a slot, and of each of its
 // four words of codes 16 bytes: codes 0, 2, 4, 6 in digit d, in digit d + 2, codes 1, 3, 5, 7 in digit d, in digit d + 2; the
 // words of lane j are 4 j .. 4 j + 3 where no group's end cuts the chunk (WHOLE), else j, j + 4, j + 8, j + 12.  The
-// 16 bytes of word q of lane j and digit d lie at 128 q + 64 d + 16 j.  Returns what the highest digit (0) stands for; *lost:
-// something is left of the elements.
-template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (&f)[4], uint8_t *to, bool *lost)
+// 16 bytes of word q of lane j and digit d lie at 128 q + 64 d + 16 j.  Returns what the highest digit (0) stands for.
+template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (&f)[4], uint8_t *to)
 {
     const int lane = threadIdx.x & 31;
     float most = 0.f;
@@ -238,12 +144,9 @@ template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (
     const int up = 156 - (int)max(e, 7u), up1 = min(up, 126);
     const float a = __uint_as_float((uint32_t)(127 + up1) << 23), b = __uint_as_float((uint32_t)(127 + up - up1) << 23);
     uint32_t v[4];
-    bool rest = false;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float u = f[i] * b * a, w = rintf(u);
-        rest = rest || w != u || (u == 0.f && f[i] != 0.f);
-        v[i] = (uint32_t)__float2int_rn(u) + 0x808080u;       // its lower bytes are digits plus 128
+        v[i] = (uint32_t)__float2int_rn(f[i] * b * a) + 0x808080u;       // its lower bytes are digits plus 128
     }
     const int block = lane >> 1, half = lane & 1;
     const int j = WHOLE ? block >> 2 : block & 3, q = WHOLE ? block & 3 : block >> 2;
@@ -256,7 +159,6 @@ template <bool WHOLE> __device__ __forceinline__ float make_digits(const float (
         *reinterpret_cast<uint16_t *>(digit) = (uint16_t)(__byte_perm(v[0], v[2], sel) ^ flip);
         *reinterpret_cast<uint16_t *>(digit + 8) = (uint16_t)(__byte_perm(v[1], v[3], sel) ^ flip);
     }
-    *lost = __any_sync(~0u, rest);
     if (__any_sync(~0u, bad)) return __uint_as_float(0x7FC00000u);
     return __uint_as_float((uint32_t)(151 - up) << 23);       // 2^(24 - up)
 }
@@ -291,12 +193,8 @@ template <int XT, bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 
             }
         }
     }
-    bool lost;
-    const float step = make_digits<WHOLE>(f, p.w.x_digits + (int64_t)i * 512, &lost);
-    if (lane == 0) {
-        p.w.x_step[i] = step;
-        p.w.lost[i] = lost;
-    }
+    const float step = make_digits<WHOLE>(f, p.w.x + (int64_t)i * 512);
+    if (lane == 0) p.w.x_step[i] = step;
 }
 
 // mid's digits, a warp a chunk of a slot (of slots without an expert: of whatever lies there)
@@ -308,50 +206,9 @@ template <bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_
     if (i >= p.slots * p.chunks_out) return;
     const float4 v = *reinterpret_cast<const float4 *>(p.w.mid + (int64_t)i * 128 + 4 * lane);
     const float f[4] = {v.x, v.y, v.z, v.w};
-    bool lost;
-    const float step = make_digits<WHOLE>(f, p.w.mid_digits + (int64_t)i * 512, &lost);
+    const float step = make_digits<WHOLE>(f, p.w.mid_rows + (int64_t)i * 512);
     if (lane == 0) p.w.mid_step[i] = step;
 }
-
-constexpr int NT = 4;                 // tiles of eight columns that a warp has
-
-// ---- products ------------------------------------------------------------------------------
-// group of scales of a unit (dsq_wgemm_group.cuh)
-__device__ __forceinline__ int scale_of(uint32_t unit, uint32_t units, uint32_t inv)
-{
-    return units == 1 ? (int)unit : (int)__umulhi(unit, inv);
-}
-
-__device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
-{
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
-}
-
-// Codes of 8 NT columns and the scales of a chunk's 4 / GP units, as dsq_wgemm_group.cu keeps them.
-template <int NT, int GP> struct Stage {
-    static constexpr int W_BYTES = NT * 512, S_BYTES = (4 / GP) * NT * 32, BYTES = W_BYTES + S_BYTES;
-};
-
-// A warp's copies of codes and scales, chunk by chunk.  (Columns behind the last are the last: their sums are not used.)
-template <int NT, int GP> struct Copies {
-    const uint8_t *w[NT];             // 16-byte piece j of this lane's columns, from the first chunk on
-    const float *scale;               // of the column whose scales this lane copies
-    __device__ __forceinline__ void operator()(uint32_t at, int chunk, int pitch, int64_t rows, int groups, uint32_t units, uint32_t inv) const
-    {
-        const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-        const uint32_t to = at + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
-        const int64_t from = chunk * 64;
-        const uint32_t bytes = chunk * 64 + 16 * j < pitch ? 16u : 0u;
-#pragma unroll
-        for (int t = 0; t < NT; ++t) cp_async_16(to + t * 512, bytes ? w[t] + from : w[t], bytes);
-#pragma unroll
-        for (int u = 0; u < 4 / GP; ++u) {
-            const int g = scale_of((uint32_t)(chunk * (4 / GP) + u), units, inv);
-            cp_async_4(at + Stage<NT, GP>::W_BYTES + u * NT * 32 + lane * 4, scale + (g < groups ? g * rows : 0), g < groups ? 4u : 0u);
-        }
-    }
-};
-static_assert(8 * NT == 32, "a lane a column's scales");
 
 // ---- digits
 __device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
@@ -414,10 +271,11 @@ template <int TILES> struct Sources {
 
 // total += scale step (sum of digits times codes) of a chunk
 template <int TILES, int NT, int GP>
-__device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const Digits<TILES> &r, DsqPair (&total)[TILES][NT][2])
+__device__ __forceinline__ void multiply_digits(uint32_t at, const Digits<TILES> &r, DsqPair (&total)[TILES][NT][2])
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES;
+    constexpr uint32_t one = 0x08080808u;                     // codes 2 c + 1 (times 8)
     // (SIDE tiles of columns together: an instruction's sums are 20 clocks away from the next one's)
     constexpr int SIDE = 2;
 #pragma unroll
@@ -472,74 +330,15 @@ __device__ __forceinline__ void multiply_digits(uint32_t at, uint32_t one, const
     }
 }
 
-// ---- bf16 and fp16
-template <int XT> __device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
-{
-    if (XT == DSQ_BF16)
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-            "{%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    else
-        asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-            "{%8, %9}, {%0, %1, %2, %3};"
-            : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-            : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
-// total[t][0 .. 1] += scale (sum of x v) of a chunk: x, a row of 16-bit elements of the chunk (row n of a tile whose
-// upper half is empty), k elements of it
-template <int XT, int NT, int GP>
-__device__ __forceinline__ void multiply_16(uint32_t at, uint32_t base, const uint8_t *x, int k, float (&total)[NT][4])
-{
-    const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-    const uint32_t as = at + Stage<NT, GP>::W_BYTES;
-    float acc[NT][4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-        if (q % GP == 0) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) acc[t][e] = 0.f;
-        }
-        const uint4 v = x && 32 * q + 8 * j < k ? *reinterpret_cast<const uint4 *>(x + 64 * q + 16 * j) : make_uint4(0u, 0u, 0u, 0u);
-        // elements (2 s, 2 s + 4) and (2 s + 1, 2 s + 5), as the codes come out of their words
-        const uint32_t a[2][4] = {{__byte_perm(v.x, v.z, 0x5410), 0u, __byte_perm(v.x, v.z, 0x7632), 0u},
-                                  {__byte_perm(v.y, v.w, 0x5410), 0u, __byte_perm(v.y, v.w, 0x7632), 0u}};
-#pragma unroll
-        for (int t = 0; t < NT; ++t) {
-            const uint32_t w = lds_32(at + t * 512 + n * 64 + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
-#pragma unroll
-            for (int s = 0; s < 2; ++s)
-                mma<XT>(acc[t], a[s], dsq_value_pair<XT>(w, 2 * s, base), dsq_value_pair<XT>(w, 2 * s + 1, base));
-        }
-        if (q % GP == GP - 1) {
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
-                total[t][0] = __fmaf_rn(acc[t][0], __uint_as_float(sv.x), total[t][0]);
-                total[t][1] = __fmaf_rn(acc[t][1], __uint_as_float(sv.y), total[t][1]);
-            }
-        }
-    }
-}
-
-__device__ __forceinline__ float activated(float g, int act)
-{
-    if (act == DSQ_SILU) return g / (1.f + expf(-g));
-    const float u = 0.7978845608028654f * __fmaf_rn(0.044715f * g * g, g, g);
-    return 0.5f * g * (1.f + tanhf(u));
-}
-
 constexpr int IN_WARPS = 8, OUT_WARPS = 4;
 
-// What is behind a warp's sums of a group, shared by both forms: WC warps side by side on 16 columns of gate and
-// other half each, IN_WARPS / WC along K.
-template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
+// A block's sums of a group: WC warps side by side on 16 columns of gate and other half each, IN_WARPS / WC along K.
+template <int GP, int WC, int STAGES> struct In {
     using S = Stage<NT, GP>;
-    static constexpr int KW = IN_WARPS / WC, RING = IN_WARPS * STAGES * S::BYTES, SUMS = IN_WARPS * MOST * NT * 512;
+    static constexpr int KW = IN_WARPS / WC, RING = IN_WARPS * STAGES * S::BYTES, SUMS = IN_WARPS * NT * 512;
     static constexpr int BYTES = RING > SUMS ? RING : SUMS;
 
+    static constexpr int TILES = 1;
     const MoeParams &p;
     const Members g;
     uint8_t *smem;
@@ -578,9 +377,8 @@ template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
         p.w.mid[(int64_t)g.slot(r) * p.chunks_out * 128 + at] = at < p.I ? activated(gate, p.act) * up : 0.f;
     }
 
-    template <int TILES> __device__ __forceinline__ void digits()
+    __device__ __forceinline__ void run()
     {
-        const uint32_t one = p.odd ? 0x08080808u : 0u;
         Sources<TILES> from;
         Digits<TILES> d = {};
 #pragma unroll
@@ -588,7 +386,7 @@ template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
             const int r = 4 * m + (n >> 1);
             const int token = r < g.n ? g.slot(r) / p.k : -1;
             if (token < 0) from.set(m, nullptr, nullptr);
-            else from.set(m, p.w.x_digits + (int64_t)token * p.chunks_in * 512, p.w.x_step + (int64_t)token * p.chunks_in);
+            else from.set(m, p.w.x + (int64_t)token * p.chunks_in * 512, p.w.x_step + (int64_t)token * p.chunks_in);
         }
         if (turns > 0) from.load(wk, d);
         if (turns > 1) from.touch(wk + KW);
@@ -598,7 +396,7 @@ template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
             cp_async_wait<STAGES - 2>();
             __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
             issue();
-            multiply_digits<TILES, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), one, d, total);
+            multiply_digits<TILES, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), d, total);
             if (i + 1 < turns) from.load(wk + (i + 1) * KW, d);
             if (i + 2 < turns) from.touch(wk + (i + 2) * KW);
         }
@@ -612,7 +410,7 @@ template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
             for (int t = 0; t < NT; ++t)
                 reinterpret_cast<ulonglong2 *>(part)[((warp * TILES + m) * NT + t) * 32 + lane] = make_ulonglong2(total[m][t][0], total[m][t][1]);
         __syncthreads();
-        const float unit = dsq_value_unit<DSQ_I8>(p.odd);
+        const float unit = dsq_value_unit<DSQ_I8>(1);
         const float *sums = reinterpret_cast<const float *>(smem);
         for (int e = threadIdx.x; e < g.n * WC * 16; e += IN_WARPS * 32) {
             const int r = e / (WC * 16), c = e % (WC * 16), wc = c / 16;
@@ -634,47 +432,11 @@ template <int XT, int GP, int WC, int MOST, int STAGES> struct In {
         }
         __syncthreads();
     }
-
-    __device__ __forceinline__ void sixteen()
-    {
-        const uint32_t base = dsq_value_base<XT>(p.odd);
-        const uint8_t *x = n < g.n ? p.X + (int64_t)(g.slot(n) / p.k) * p.H * 2 : nullptr;
-        float total[NT][4] = {};
-#pragma unroll 1
-        for (int i = 0; i < turns; ++i) {
-            cp_async_wait<STAGES - 2>();
-            __syncwarp();
-            issue();
-            const int chunk = wk + i * KW;
-            multiply_16<XT, NT, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), base, x ? x + chunk * 256 : nullptr, p.H - chunk * 128, total);
-        }
-        cp_async_wait<0>();
-        __syncthreads();
-        float2 *part = reinterpret_cast<float2 *>(smem);        // [IN_WARPS][NT][32]
-#pragma unroll
-        for (int t = 0; t < NT; ++t) part[(warp * NT + t) * 32 + lane] = make_float2(total[t][0], total[t][1]);
-        __syncthreads();
-        const float unit = dsq_value_unit<XT>(p.odd);
-        const float *sums = reinterpret_cast<const float *>(smem);
-        for (int e = threadIdx.x; e < g.n * WC * 16; e += IN_WARPS * 32) {
-            const int r = e / (WC * 16), c = e % (WC * 16), wc = c / 16;
-            float both[2] = {0.f, 0.f};
-#pragma unroll
-            for (int u = 0; u < 2; ++u)
-#pragma unroll
-                for (int w = 0; w < KW; ++w)
-                    both[u] += sums[(w * WC + wc) * NT * 64 + ((2 * u + ((c >> 3) & 1)) * 32 + r * 4 + ((c & 7) >> 1)) * 2 + (c & 1)];
-            put(r, c, both[0] * unit, both[1] * unit);
-        }
-        __syncthreads();
-    }
 };
 
-// MOST: tiles of four slots of a group, 1 or 2 (fewer registers, more warps)
-template <int XT, int GP, int WC, int MOST, int STAGES>
-__global__ void __launch_bounds__(IN_WARPS * 32, MOST == 1 ? 3 : 2) moe_in_kernel(const __grid_constant__ MoeParams p)
+template <int GP, int WC, int STAGES>
+__global__ void __launch_bounds__(IN_WARPS * 32, 3) moe_in_kernel(const __grid_constant__ MoeParams p)
 {
-    using L = In<XT, GP, WC, MOST, STAGES>;
     extern __shared__ __align__(128) uint8_t smem[];
     grid_dependency_wait();
     grid_launch_dependents();
@@ -682,22 +444,16 @@ __global__ void __launch_bounds__(IN_WARPS * 32, MOST == 1 ? 3 : 2) moe_in_kerne
     Members g = members_of(p.w, blockIdx.y);
     const int groups = *p.w.groups;
     for (int i = blockIdx.y; i < groups; i += gridDim.y, g = members_of(p.w, min(i, groups - 1))) {
-        L l(p, g, smem);
+        In<GP, WC, STAGES> in(p, g, smem);
 #pragma unroll
-        for (int s = 0; s < STAGES - 1; ++s) l.issue();
-        bool lost = false;
-        if (!p.odd)
-            for (int e = threadIdx.x; e < l.g.n * p.chunks_in; e += IN_WARPS * 32)
-                lost = lost || p.w.lost[l.g.slot(e / p.chunks_in) / p.k * p.chunks_in + e % p.chunks_in];
-        if (!p.odd && __syncthreads_or(lost)) l.sixteen();
-        else if (MOST == 1 || l.g.n <= 4) l.template digits<1>();
-        else l.template digits<MOST>();
+        for (int s = 0; s < STAGES - 1; ++s) in.issue();
+        in.run();
     }
 }
 
 // WC warps side by side on 32 columns each, OUT_WARPS / WC (and the cluster's blocks) along the chunks
-template <int GP, int WC, int MOST, int STAGES>
-__global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
+template <int GP, int WC, int STAGES>
+__global__ void __launch_bounds__(OUT_WARPS * 32, 5) moe_out_kernel(const __grid_constant__ MoeParams p, int cluster)
 {
     constexpr int KW = OUT_WARPS / WC, WIDE = 8 * NT, COLS = WC * WIDE, THREADS = OUT_WARPS * 32;
     using S = Stage<NT, GP>;
@@ -705,7 +461,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const int rank = cluster > 1 ? (int)cluster_ctarank() : 0;
     const int64_t b0 = (int64_t)(blockIdx.x / cluster) * COLS, c0 = b0 + warp % WC * WIDE;
-    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES), one = p.odd ? 0x08080808u : 0u;
+    const uint32_t ring = smem_u32(smem) + (uint32_t)(warp * STAGES * S::BYTES);
     // [OUT_WARPS][T][WIDE]; the warp's own
     float *sums = reinterpret_cast<float *>(smem + OUT_WARPS * STAGES * S::BYTES), *mine = sums + warp * p.T * WIDE;
     for (int i = lane; i < p.T * WIDE; i += 32) mine[i] = 0.f;
@@ -743,25 +499,25 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
     grid_launch_dependents();
 
     Members g = {};
-    Sources<MOST> from;
-    Digits<MOST> d = {};
+    Sources<1> from;
+    Digits<1> d = {};
     int cg = q0 / chunks, cc = q0 - cg * chunks;                // of the chunk at hand
     auto rows_of = [&](int i) {
         g = members_of(p.w, i);
         d = {};
 #pragma unroll
-        for (int m = 0; m < MOST; ++m) {
+        for (int m = 0; m < 1; ++m) {
             const int r = 4 * m + (n >> 1);
             const int slot = r < g.n ? g.slot(r) : -1;
             if (slot < 0) from.set(m, nullptr, nullptr);
-            else from.set(m, p.w.mid_digits + (int64_t)slot * chunks * 512, p.w.mid_step + (int64_t)slot * chunks);
+            else from.set(m, p.w.mid_rows + (int64_t)slot * chunks * 512, p.w.mid_step + (int64_t)slot * chunks);
         }
     };
     if (q0 < q1) {
         rows_of(cg);
         from.load(cc, d);
     }
-    DsqPair total[MOST][NT][2] = {};
+    DsqPair total[1][NT][2] = {};
     // what a lane's digits n & 1 and (n & 1) + 2 stand for, in steps
     const float high = n & 1 ? 0x1p-8f : 1.f, low = n & 1 ? 0x1p-24f : 0x1p-16f;
 #pragma unroll 1
@@ -770,19 +526,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
         __syncwarp();
         issue(i + STAGES - 1);
         const uint32_t at = ring + (uint32_t)((i - q0) % STAGES * S::BYTES);
-        if constexpr (MOST == 2) {
-            if (g.n <= 4) {
-                Digits<1> d1;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) d1.x[0][q] = d.x[0][q];
-                d1.step[0] = d.step[0];
-                multiply_digits<1, NT, GP>(at, one, d1, reinterpret_cast<DsqPair (&)[1][NT][2]>(total));
-            } else {
-                multiply_digits<2, NT, GP>(at, one, d, total);
-            }
-        } else {
-            multiply_digits<1, NT, GP>(at, one, d, total);
-        }
+        multiply_digits<1, NT, GP>(at, d, total);
         if (++cc < chunks && i + 1 < q1) {
             from.load(cc, d);
             if (cc + 1 < chunks && i + 2 < q1) from.touch(cc + 1);
@@ -790,7 +534,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
         }
         // the group's sums to the tokens' rows, one slot after the other (two may be the same token's)
 #pragma unroll
-        for (int m = 0; m < MOST; ++m) {
+        for (int m = 0; m < 1; ++m) {
             if (4 * m >= g.n) break;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -848,7 +592,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
     }
     if (cluster > 1) cluster_sync_all();
     else __syncthreads();
-    const float unit = dsq_value_unit<DSQ_I8>(p.odd);
+    const float unit = dsq_value_unit<DSQ_I8>(1);
     for (int e = rank * THREADS + threadIdx.x; e < p.T * COLS; e += cluster * THREADS) {
         float s = 0.f;
         if (cluster == 1) s = sums[e];
@@ -875,8 +619,7 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, MOST == 1 ? 5 : 3) moe_out_ker
 }
 
 // ---- host ------------------------------------------------------------------------------------
-template <int MOST> constexpr int IN_STAGES = MOST == 1 ? 3 : 4;
-constexpr int OUT_STAGES = 4;
+constexpr int IN_STAGES = 3, OUT_STAGES = 4, IN_SIDE = 2, OUT_SIDE = 1;     // warps side by side
 
 template <int XT, int GP> int launch_prepare(const MoeParams &p, cudaStream_t s)
 {
@@ -884,52 +627,57 @@ template <int XT, int GP> int launch_prepare(const MoeParams &p, cudaStream_t s)
     return dsq_launch(moe_prepare_kernel<XT, GP == 4>, dim3(blocks), dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int XT, int GP, int WC, int MOST> int launch_in(const MoeParams &p, cudaStream_t s)
+template <int GP> int launch_in(const MoeParams &p, cudaStream_t s)
 {
-    constexpr int bytes = In<XT, GP, WC, MOST, IN_STAGES<MOST>>::BYTES;
-    static_assert(bytes <= (MOST == 1 ? 74 : 112) * 1024, "shared memory");
+    constexpr int bytes = In<GP, IN_SIDE, IN_STAGES>::BYTES, cols = IN_SIDE * 16;
+    static_assert(bytes <= 74 * 1024, "shared memory");
     static std::atomic<unsigned long long> configured{0};
-    const auto kernel = moe_in_kernel<XT, GP, WC, MOST, IN_STAGES<MOST>>;
+    const auto kernel = moe_in_kernel<GP, IN_SIDE, IN_STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, bytes, &configured);
     if (st) return st;
     // (to the end of the last chunk: zeros)
-    const dim3 grid((unsigned)((p.chunks_out * 128 + WC * 16 - 1) / (WC * 16)), (unsigned)(p.slots < p.E ? p.slots : p.E));
+    const dim3 grid((unsigned)((p.chunks_out * 128 + cols - 1) / cols), (unsigned)(p.slots < p.E ? p.slots : p.E));
     return dsq_launch(kernel, grid, dim3(IN_WARPS * 32), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
 }
 
-template <int GP, int WC, int MOST> int launch_out(const MoeParams &p, cudaStream_t s)
+template <int GP> int launch_out(const MoeParams &p, cudaStream_t s)
 {
-    constexpr int ring = OUT_WARPS * OUT_STAGES * Stage<NT, GP>::BYTES, row = OUT_WARPS * 8 * NT * 4, cols = WC * 8 * NT;
+    constexpr int ring = OUT_WARPS * OUT_STAGES * Stage<NT, GP>::BYTES, row = OUT_WARPS * 8 * NT * 4, cols = OUT_SIDE * 8 * NT;
     static_assert(ring + PASS_TOKENS * row <= 200 * 1024, "shared memory");
     static std::atomic<unsigned long long> configured{0};
-    const auto kernel = moe_out_kernel<GP, WC, MOST, OUT_STAGES>;
+    const auto kernel = moe_out_kernel<GP, OUT_SIDE, OUT_STAGES>;
     const int st = dsq_allow_smem((const void *)kernel, ring + PASS_TOKENS * row, &configured);
     if (st) return st;
     const int tiles = (p.H + cols - 1) / cols, sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148;
-    int cluster = 1;
-    while (cluster < 8 && tiles * cluster * 2 <= (MOST == 1 ? 4 : 3) * sms) cluster *= 2;
+    int cluster = 4 * sms / tiles;
+    cluster = cluster < 1 ? 1 : cluster > 8 ? 8 : cluster;
     return dsq_launch(kernel, dim3((unsigned)(tiles * cluster)), dim3(OUT_WARPS * 32), (size_t)(ring + p.T * row), s,
                       dsq_launch_hooks().pdl, cluster, p, cluster);
 }
 
-template <int XT, int GP> int pick_in(const MoeParams &p, cudaStream_t s)
+template <int XT, int GP> int run_in(const MoeParams &p, cudaStream_t s)
 {
     const int st = launch_prepare<XT, GP>(p, s);
-    if (st) return st;
-    return p.rows == 4 ? launch_in<XT, GP, 2, 1>(p, s) : launch_in<XT, GP, 4, 2>(p, s);
+    return st ? st : launch_in<GP>(p, s);
 }
-template <int GP> int pick_out(const MoeParams &p, cudaStream_t s)
+template <int GP> int run_out(const MoeParams &p, cudaStream_t s)
 {
     const int st = dsq_launch(moe_mid_kernel<GP == 4>, dim3((p.slots * p.chunks_out + PREPARE_WARPS - 1) / PREPARE_WARPS),
                               dim3(PREPARE_WARPS * 32), 0, s, dsq_launch_hooks().pdl, 0, p);
-    if (st) return st;
-    return p.rows == 4 ? launch_out<GP, 1, 1>(p, s) : launch_out<GP, 4, 2>(p, s);
+    return st ? st : launch_out<GP>(p, s);
+}
+int run_digits(const MoeParams &p, int x_type, int gp_in, int gp_out, cudaStream_t s)
+{
+    int st;
+    if (x_type == DSQ_BF16) st = gp_in == 4 ? run_in<DSQ_BF16, 4>(p, s) : gp_in == 2 ? run_in<DSQ_BF16, 2>(p, s) : run_in<DSQ_BF16, 1>(p, s);
+    else st = gp_in == 4 ? run_in<DSQ_F16, 4>(p, s) : gp_in == 2 ? run_in<DSQ_F16, 2>(p, s) : run_in<DSQ_F16, 1>(p, s);
+    return st ? st : gp_out == 4 ? run_out<4>(p, s) : gp_out == 2 ? run_out<2>(p, s) : run_out<1>(p, s);
 }
 
 int chunks_of(int64_t K) { return (int)((K + 127) / 128); }
 
-// Lays the workspace out behind its first bytes; returns its size.
-size_t lay_out(Work &w, char *base, int T, int slots, int chunks_in, int chunks_out)
+// Lays the workspace out behind its first bytes, for either form; returns its size.
+size_t lay_out(Work &w, char *base, int T, int slots, int H, int chunks_in, int chunks_out)
 {
     size_t at = DSQ_WS_BYTES;
     auto take = [&](size_t bytes) {
@@ -937,14 +685,15 @@ size_t lay_out(Work &w, char *base, int T, int slots, int chunks_in, int chunks_
         at += (bytes + 255) / 256 * 256;
         return p;
     };
+    const size_t mid = (size_t)slots * chunks_out * 512, part = (size_t)slots * H * 4;
     w.groups = (int *)take(4);
     w.group = (Group *)take((size_t)slots * sizeof(Group));
-    w.lost = (uint8_t *)take((size_t)T * chunks_in);
     w.x_step = (float *)take((size_t)T * chunks_in * 4);
     w.mid_step = (float *)take((size_t)slots * chunks_out * 4);
-    w.x_digits = (uint8_t *)take((size_t)T * chunks_in * 512);
-    w.mid_digits = (uint8_t *)take((size_t)slots * chunks_out * 512);
-    w.mid = (float *)take((size_t)slots * chunks_out * 512);
+    w.x = (uint8_t *)take((size_t)T * chunks_in * 512);
+    w.mid_rows = (uint8_t *)take((size_t)slots * chunks_out * 512);
+    w.mid = (float *)take(mid > part ? mid : part);
+    w.part = w.mid;
     return at;
 }
 
@@ -980,7 +729,7 @@ size_t dsq_moe_workspace_bytes(int64_t T, int64_t H, int64_t I, int k)
     if (T <= 0 || H <= 0 || H > DSQ_GROUPS_MAX_K || I <= 0 || I > DSQ_GROUPS_MAX_K || k <= 0 || k > MAX_TOP) return DSQ_WS_BYTES;
     const int tokens = (int)(T < PASS_TOKENS ? T : PASS_TOKENS);
     Work w;
-    return lay_out(w, nullptr, tokens, tokens * k, chunks_of(H), chunks_of(I));
+    return lay_out(w, nullptr, tokens, tokens * k, (int)H, chunks_of(H), chunks_of(I));
 }
 
 int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *weights, const void *W_in,
@@ -1020,19 +769,17 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
     for (int64_t t = 0; t < T; t += PASS_TOKENS) {
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
-        // Groups of four where few experts can be expected to have more; else of eight, whose warps lie side by side and
-        // share the rows of digits in L1.
-        p.rows = p.T <= 4 || p.slots <= 3 * p.E ? 4 : 8;
-        lay_out(p.w, (char *)workspace, p.T, p.slots, p.chunks_in, p.chunks_out);
+        // Digits where few experts can be expected to have more than four slots, and where no code is 0 (see above).  On 16 bits
+        // mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.
+        const bool digits = p.odd && (p.T <= 4 || p.slots <= 3 * p.E);
+        p.split = !digits && y_type != DSQ_BF16;
+        p.rows = digits ? 4 : p.split || p.slots <= 5 * p.E ? 8 : 16;
+        lay_out(p.w, (char *)workspace, p.T, p.slots, p.H, p.chunks_in, p.chunks_out);
         p.X = (const uint8_t *)X + t * H * 2;
         p.ids = ids + t * k; p.weights = weights + t * k;
         p.residual = residual ? (const char *)residual + t * H * y_size : nullptr;
         p.Y = (char *)Y + t * H * y_size;
-        if (x_type == DSQ_BF16)
-            st = gp_in == 4 ? pick_in<DSQ_BF16, 4>(p, s) : gp_in == 2 ? pick_in<DSQ_BF16, 2>(p, s) : pick_in<DSQ_BF16, 1>(p, s);
-        else
-            st = gp_in == 4 ? pick_in<DSQ_F16, 4>(p, s) : gp_in == 2 ? pick_in<DSQ_F16, 2>(p, s) : pick_in<DSQ_F16, 1>(p, s);
-        if (!st) st = gp_out == 4 ? pick_out<4>(p, s) : gp_out == 2 ? pick_out<2>(p, s) : pick_out<1>(p, s);
+        st = digits ? run_digits(p, x_type, gp_in, gp_out, s) : run_wide(p, x_type, gp_in, gp_out, s);
         if (st) return st;
     }
     return DSQ_OK;

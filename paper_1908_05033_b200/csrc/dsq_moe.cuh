@@ -1,0 +1,158 @@
+// What the kernels for layers of experts share (dsq_moe.cu: groups of up to four slots, on digits of 8 bits;
+// dsq_moe_wide.cu: of up to sixteen, on 16 bits).
+#pragma once
+
+#include "dsq_groups.h"
+#include "dsq_pairs.cuh"
+#include "dsq_ptx.cuh"
+#include "dsq_tc_host.h"
+#include "dsq_types.cuh"
+#include "dsq_wgemm_group.cuh"
+
+namespace dsq_moe {
+
+using namespace dsq_ptx;
+
+constexpr int PASS_TOKENS = 64, MAX_TOP = 32, MAX_EXPERTS = 1024;      // tokens of a pass over the weights
+
+// ---- slots by expert
+// a group as the kernels read it, in one access
+struct alignas(64) Group {
+    int expert, n, unused[2];
+    uint16_t slot[16];
+};
+// what lies in the workspace
+struct Work {
+    int *groups;                      // how many
+    Group *group;                     // by expert, the slots of an expert in their order
+    // digits: [T][chunks_in], [slots][chunks_out], what the highest digit stands for; 16 bits: [slots], what 1 stands for
+    float *x_step, *mid_step;
+    // digits: [T][chunks_in][512], [slots][chunks_out][512]; 16 bits: [T][chunks_in][256], [slots or 2 slots][chunks_out][256]
+    uint8_t *x, *mid_rows;
+    float *mid;                       // [slots][128 chunks_out]
+    float *part;                      // 16 bits: [slots][H], what a slot adds to its token (where mid was)
+};
+struct MoeParams {
+    Work w;
+    const uint8_t *X, *W_in, *W_out;
+    const float *s_in, *s_out, *weights;
+    const int32_t *ids;
+    const void *residual;
+    void *Y;
+    int T, H, I, E, k, slots;
+    int pitch_in, pitch_out;                 // bytes of a row of codes
+    int chunks_in, chunks_out;               // of 128 codes in a row
+    int groups_in, groups_out;               // scales of a row
+    uint32_t units_in, units_in_inv, units_out, units_out_inv;
+    int odd, act, y_type;
+    int rows;                                // slots of a group: 4 (digits), 8 or 16 (16 bits)
+    int split;                               // 16 bits: mid as two numbers
+};
+__device__ __forceinline__ uint4 load_16(const void *p)
+{
+    uint4 r;
+    asm volatile("ld.global.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p));
+    return r;
+}
+
+// Sorts the slots whose expert there is, and cuts them into groups.  A block.
+struct Sorting { int count[MAX_EXPERTS], group[MAX_EXPERTS]; };
+__device__ __forceinline__ void sort_slots(const MoeParams &p, Sorting &s)
+{
+    const int lane = threadIdx.x & 31, E = p.E, n = p.slots, rows = p.rows, shift = rows == 16 ? 4 : rows == 8 ? 3 : 2;
+    for (int e = threadIdx.x; e < E; e += blockDim.x) s.count[e] = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < n; i += blockDim.x) {
+        const int id = p.ids[i];
+        if (id >= 0 && id < E) atomicAdd(&s.count[id], 1);
+    }
+    __syncthreads();
+    if (threadIdx.x >= 32) return;
+    int groups = 0;                   // so far
+    for (int e0 = 0; e0 < E; e0 += 32) {
+        const int e = e0 + lane, count = e < E ? s.count[e] : 0, parts = (count + rows - 1) >> shift;
+        int b = parts;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(~0u, b, o);
+            if (lane >= o) b += v;
+        }
+        const int g = groups + b - parts;
+        if (e < E) {
+            s.count[e] = 0;
+            s.group[e] = g;
+        }
+        for (int i = 0; i < parts; ++i) {
+            p.w.group[g + i].expert = e;
+            p.w.group[g + i].n = min(rows, count - i * rows);
+        }
+        groups += __shfl_sync(~0u, b, 31);
+    }
+    if (lane == 0) *p.w.groups = groups;
+    __syncwarp();
+    for (int i0 = 0; i0 < n; i0 += 32) {
+        int id = i0 + lane < n ? p.ids[i0 + lane] : -1;
+        if (id < 0 || id >= E) id = -1;
+        const uint32_t same = __match_any_sync(~0u, id);
+        const int at = id >= 0 ? s.count[id] : 0;
+        __syncwarp();
+        if (id >= 0) {
+            const int pos = at + __popc(same & ((1u << lane) - 1));
+            p.w.group[s.group[id] + (pos >> shift)].slot[pos & (rows - 1)] = (uint16_t)(i0 + lane);
+            if (lane == 31 - __clz(same)) s.count[id] = at + __popc(same);
+        }
+        __syncwarp();
+    }
+}
+
+constexpr int NT = 4;                 // tiles of eight columns that a warp has
+
+// ---- products ------------------------------------------------------------------------------
+// group of scales of a unit (dsq_wgemm_group.cuh)
+__device__ __forceinline__ int scale_of(uint32_t unit, uint32_t units, uint32_t inv)
+{
+    return units == 1 ? (int)unit : (int)__umulhi(unit, inv);
+}
+
+__device__ __forceinline__ void cp_async_4(uint32_t dst, const void *src, uint32_t src_bytes)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(src_bytes) : "memory");
+}
+
+// Codes of 8 NT columns and the scales of a chunk's 4 / GP units, as dsq_wgemm_group.cu keeps them.
+template <int NT, int GP> struct Stage {
+    static constexpr int W_BYTES = NT * 512, S_BYTES = (4 / GP) * NT * 32, BYTES = W_BYTES + S_BYTES;
+};
+
+// A warp's copies of codes and scales, chunk by chunk.  (Columns behind the last are the last: their sums are not used.)
+template <int NT, int GP> struct Copies {
+    const uint8_t *w[NT];             // 16-byte piece j of this lane's columns, from the first chunk on
+    const float *scale;               // of the column whose scales this lane copies
+    __device__ __forceinline__ void operator()(uint32_t at, int chunk, int pitch, int64_t rows, int groups, uint32_t units, uint32_t inv) const
+    {
+        const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+        const uint32_t to = at + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
+        const int64_t from = chunk * 64;
+        const uint32_t bytes = chunk * 64 + 16 * j < pitch ? 16u : 0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) cp_async_16(to + t * 512, bytes ? w[t] + from : w[t], bytes);
+#pragma unroll
+        for (int u = 0; u < 4 / GP; ++u) {
+            const int g = scale_of((uint32_t)(chunk * (4 / GP) + u), units, inv);
+            cp_async_4(at + Stage<NT, GP>::W_BYTES + u * NT * 32 + lane * 4, scale + (g < groups ? g * rows : 0), g < groups ? 4u : 0u);
+        }
+    }
+};
+static_assert(8 * NT == 32, "a lane a column's scales");
+
+__device__ __forceinline__ float activated(float g, int act)
+{
+    if (act == DSQ_SILU) return g / (1.f + expf(-g));
+    const float u = 0.7978845608028654f * __fmaf_rn(0.044715f * g * g, g, g);
+    return 0.5f * g * (1.f + tanhf(u));
+}
+
+// The same layer on 16 bits; arguments validated, p.w laid out for it.  gp: pieces of 32 codes that no group's end cuts.
+DSQ_HIDDEN int run_wide(const MoeParams &p, int x_type, int gp_in, int gp_out, cudaStream_t s);
+
+}  // namespace dsq_moe
