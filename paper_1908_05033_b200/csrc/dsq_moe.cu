@@ -344,7 +344,7 @@ template <int GP, int WC, int STAGES> struct In {
     uint8_t *smem;
     int warp, lane, n, j, wk, c0, turns, to_turn, issued;
     uint32_t ring;
-    Copies<NT, GP> copies;
+    Copies<NT, GP, STAGES> copies;
 
     __device__ __forceinline__ In(const MoeParams &p_, const Members &g_, uint8_t *smem_) : p(p_), g(g_), smem(smem_)
     {
@@ -357,14 +357,13 @@ template <int GP, int WC, int STAGES> struct In {
         // columns 0 .. 15 are the gate's, 16 .. 31 the other half's
         auto row = [&](int c) { return (int64_t)g.expert * 2 * p.I + min(c0 + (c & 15), p.I - 1) + (c < 16 ? 0 : p.I); };
 #pragma unroll
-        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_in + row(8 * t + n) * p.pitch_in + 16 * j;
+        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_in + row(8 * t + n) * p.pitch_in;
         copies.scale = p.s_in + row(lane);
+        copies.start(ring, wk, KW);
     }
     __device__ __forceinline__ void issue()
     {
-        if (issued < turns)
-            copies(ring + (uint32_t)(issued % STAGES * S::BYTES), wk + issued * KW, p.pitch_in, (int64_t)p.E * 2 * p.I, p.groups_in,
-                   p.units_in, p.units_in_inv);
+        if (issued < turns) copies.next(p.pitch_in, (int64_t)p.E * 2 * p.I, p.groups_in, p.units_in, p.units_in_inv);
         ++issued;
         cp_async_commit();
     }
@@ -472,26 +471,30 @@ __global__ void __launch_bounds__(OUT_WARPS * 32, 5) moe_out_kernel(const __grid
     const int64_t all = (int64_t)groups * chunks;
     const int share = rank * KW + warp / WC, shares = cluster * KW;
     const int q0 = (int)(all * share / shares), q1 = (int)(all * (share + 1) / shares);
-    int ig = q0 / chunks, ic = q0 - ig * chunks;                // of the next copy
-    Copies<NT, GP> copies;
+    int ig = q0 / chunks;                                       // group of the next copy
+    Copies<NT, GP, STAGES> copies;
     auto columns_of = [&](int i) {
         const int64_t row0 = (int64_t)p.w.group[i].expert * p.H;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_out + (row0 + min(c0 + 8 * t + n, (int64_t)p.H - 1)) * p.pitch_out + 16 * j;
+        for (int t = 0; t < NT; ++t) copies.w[t] = p.W_out + (row0 + min(c0 + 8 * t + n, (int64_t)p.H - 1)) * p.pitch_out;
         copies.scale = p.s_out + row0 + min(c0 + lane, (int64_t)p.H - 1);
     };
     auto issue = [&](int i) {
         if (i < q1) {
-            copies(ring + (uint32_t)((i - q0) % STAGES * S::BYTES), ic, p.pitch_out, (int64_t)p.E * p.H, p.groups_out, p.units_out,
-                   p.units_out_inv);
-            if (++ic == chunks) {
-                ic = 0;
-                if (i + 1 < q1) columns_of(++ig);
+            copies.next(p.pitch_out, (int64_t)p.E * p.H, p.groups_out, p.units_out, p.units_out_inv);
+            if (copies.chunk == chunks && i + 1 < q1) {
+                const uint32_t to = copies.to;
+                columns_of(++ig);
+                copies.start(ring, 0, 1);
+                copies.to = to;
             }
         }
         cp_async_commit();
     };
-    if (q0 < q1) columns_of(ig);
+    if (q0 < q1) {
+        columns_of(ig);
+        copies.start(ring, q0 - ig * chunks, 1);
+    }
 #pragma unroll
     for (int s = 0; s < STAGES - 1; ++s) issue(q0 + s);
     __syncwarp();

@@ -124,23 +124,38 @@ template <int NT, int GP> struct Stage {
     static constexpr int W_BYTES = NT * 512, S_BYTES = (4 / GP) * NT * 32, BYTES = W_BYTES + S_BYTES;
 };
 
-// A warp's copies of codes and scales, chunk by chunk.  (Columns behind the last are the last: their sums are not used.)
-template <int NT, int GP> struct Copies {
-    const uint8_t *w[NT];             // 16-byte piece j of this lane's columns, from the first chunk on
+// A warp's copies of codes and scales, every `by`-th chunk from `first` on, to the places of a ring of STAGES in turn.
+// (Columns behind the last are the last: their sums are not used.  A copy of 0 bytes reads nothing, wherever it points.)
+template <int NT, int GP, int STAGES> struct Copies {
+    const uint8_t *w[NT];             // 16-byte piece j of this lane's columns, of the next chunk
     const float *scale;               // of the column whose scales this lane copies
-    __device__ __forceinline__ void operator()(uint32_t at, int chunk, int pitch, int64_t rows, int groups, uint32_t units, uint32_t inv) const
+    uint32_t to, to_first, to_scale;  // places in shared memory; the scales' behind the codes'
+    int chunk, by;
+    __device__ __forceinline__ void start(uint32_t ring, int first, int by_)
     {
         const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
-        const uint32_t to = at + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
-        const int64_t from = chunk * 64;
-        const uint32_t bytes = chunk * 64 + 16 * j < pitch ? 16u : 0u;
+        to = to_first = ring + n * 64 + ((j ^ (n >> 1)) & 3) * 16;
+        to_scale = Stage<NT, GP>::W_BYTES + lane * 4 - (n * 64 + ((j ^ (n >> 1)) & 3) * 16);
+        chunk = first;
+        by = by_;
 #pragma unroll
-        for (int t = 0; t < NT; ++t) cp_async_16(to + t * 512, bytes ? w[t] + from : w[t], bytes);
+        for (int t = 0; t < NT; ++t) w[t] += first * 64 + 16 * j;
+    }
+    __device__ __forceinline__ void next(int pitch, int64_t rows, int groups, uint32_t units, uint32_t inv)
+    {
+        const uint32_t bytes = chunk * 64 + 16 * (int)(threadIdx.x & 3) < pitch ? 16u : 0u;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            cp_async_16(to + t * 512, w[t], bytes);
+            w[t] += by * 64;
+        }
 #pragma unroll
         for (int u = 0; u < 4 / GP; ++u) {
             const int g = scale_of((uint32_t)(chunk * (4 / GP) + u), units, inv);
-            cp_async_4(at + Stage<NT, GP>::W_BYTES + u * NT * 32 + lane * 4, scale + (g < groups ? g * rows : 0), g < groups ? 4u : 0u);
+            cp_async_4(to + to_scale + u * NT * 32, scale + (int64_t)g * rows, g < groups ? 4u : 0u);
         }
+        chunk += by;
+        to = to == to_first + (STAGES - 1) * Stage<NT, GP>::BYTES ? to_first : to + Stage<NT, GP>::BYTES;
     }
 };
 static_assert(8 * NT == 32, "a lane a column's scales");

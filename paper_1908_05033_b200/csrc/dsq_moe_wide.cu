@@ -192,7 +192,7 @@ template <bool OUT, int XT, int GP> struct Wide {
     uint8_t *smem;
     int expert, slots, warp, lane, n, j, wk, c0, chunks, turns, issued;
     uint32_t ring;
-    Copies<NT, GP> copies;
+    Copies<NT, GP, STAGES> copies;
 
     __device__ __forceinline__ Wide(const MoeParams &p_, const Group *group_, int expert_, int slots_, uint8_t *smem_)
         : p(p_), group(group_), smem(smem_), expert(expert_), slots(slots_)
@@ -212,15 +212,15 @@ template <bool OUT, int XT, int GP> struct Wide {
         };
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            copies.w[t] = (OUT ? p.W_out : p.W_in) + row(8 * t + n) * (OUT ? p.pitch_out : p.pitch_in) + 16 * j;
+            copies.w[t] = (OUT ? p.W_out : p.W_in) + row(8 * t + n) * (OUT ? p.pitch_out : p.pitch_in);
         copies.scale = (OUT ? p.s_out : p.s_in) + row(lane);
+        copies.start(ring, wk, KW);
     }
     __device__ __forceinline__ void issue()
     {
         if (issued < turns) {
-            const uint32_t at = ring + (uint32_t)(issued % STAGES * S::BYTES);
-            if (OUT) copies(at, wk + issued * KW, p.pitch_out, (int64_t)p.E * p.H, p.groups_out, p.units_out, p.units_out_inv);
-            else copies(at, wk + issued * KW, p.pitch_in, (int64_t)p.E * 2 * p.I, p.groups_in, p.units_in, p.units_in_inv);
+            if (OUT) copies.next(p.pitch_out, (int64_t)p.E * p.H, p.groups_out, p.units_out, p.units_out_inv);
+            else copies.next(p.pitch_in, (int64_t)p.E * 2 * p.I, p.groups_in, p.units_in, p.units_in_inv);
         }
         ++issued;
         cp_async_commit();
