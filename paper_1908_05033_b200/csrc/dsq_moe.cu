@@ -48,6 +48,11 @@ __device__ __forceinline__ uint32_t order_of(float v)
     return v != v ? 0u : (int)u < 0 ? ~u : u | 0x80000000u;
 }
 
+__device__ __forceinline__ float value_of(uint32_t o)
+{
+    return __uint_as_float(o == 0u ? 0x7FC00000u : (int)o < 0 ? o & 0x7FFFFFFFu : ~o);
+}
+
 template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const RouteParams p)
 {
     const int lane = threadIdx.x & 31;
@@ -85,7 +90,7 @@ template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const R
         }
         last = __reduce_max_sync(~0u, best);
         last_at = (int)__reduce_min_sync(~0u, best == last ? (uint32_t)at : (uint32_t)p.E);
-        const float value = row[last_at];
+        const float value = value_of(last);
         if (s == 0) first = value;
         if (lane == s) {
             mine = value;
@@ -218,15 +223,13 @@ __device__ __forceinline__ void mma_i8(int (&d)[4], const uint32_t (&a)[4], uint
         : "+r"(d[0]), "+r"(d[1]), "+r"(d[2]), "+r"(d[3])
         : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// The same on sums of 1.5 2^23 as binary32 keeps it: a sum below 2^22 (128 codes of 128 at most, digits of 128: 2^21)
-// is then a binary32 number, 1.5 2^23 and itself.
-constexpr float MAGIC = 12582912.f;
+// the same on sums of zero
 __device__ __forceinline__ void mma_i8_first(int (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1)
 {
     asm("mma.sync.aligned.m16n8k32.row.col.s32.s8.s8.s32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
         "{%8, %9}, {%10, %10, %10, %10};"
         : "=r"(d[0]), "=r"(d[1]), "=r"(d[2]), "=r"(d[3])
-        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0x4B400000));
+        : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "r"(0));
 }
 
 // What a lane has of a chunk's rows, a tile being four slots: digits n & 1 and (n & 1) + 2 of slot n / 2, and the step.
@@ -314,15 +317,13 @@ __device__ __forceinline__ void multiply_digits(uint32_t at, const Digits<TILES>
                 for (int s = 0; s < SIDE; ++s) {
                     const int t = t0 + s;
                     const uint2 sv = lds_64(as + (q / GP * NT * 8 + 8 * t + 2 * j) * 4);
-                    const DsqPair scales = dsq_pair_of(__uint_as_float(sv.x), __uint_as_float(sv.y)), less = dsq_pair_of(-MAGIC, -MAGIC);
+                    const DsqPair scales = dsq_pair_of(__uint_as_float(sv.x), __uint_as_float(sv.y));
 #pragma unroll
                     for (int m = 0; m < TILES; ++m) {
                         const DsqPair by = dsq_pair_mul(scales, dsq_pair_of(r.step[m], r.step[m]));
 #pragma unroll
                         for (int e = 0; e < 2; ++e)
-                            total[m][t][e] = dsq_pair_fma(
-                                dsq_pair_add(dsq_pair_of(__int_as_float(acc[s][m][2 * e]), __int_as_float(acc[s][m][2 * e + 1])), less), by,
-                                total[m][t][e]);
+                            total[m][t][e] = dsq_pair_fma(dsq_pair_of((float)acc[s][m][2 * e], (float)acc[s][m][2 * e + 1]), by, total[m][t][e]);
                     }
                 }
             }

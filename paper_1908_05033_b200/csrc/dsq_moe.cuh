@@ -60,6 +60,31 @@ struct Sorting { int count[MAX_EXPERTS], group[MAX_EXPERTS]; };
 __device__ __forceinline__ void sort_slots(const MoeParams &p, Sorting &s)
 {
     const int lane = threadIdx.x & 31, E = p.E, n = p.slots, rows = p.rows, shift = rows == 16 ? 4 : rows == 8 ? 3 : 2;
+    if (n <= 32) {
+        // A slot a lane: groups in the order of their first slots, unless an expert has more than one.
+        if (threadIdx.x < 32) {
+            int id = lane < n ? p.ids[lane] : -1;
+            if (id < 0 || id >= E) id = -1;
+            const uint32_t same = __match_any_sync(~0u, id), before = same & ((1u << lane) - 1);
+            const uint32_t firsts = __ballot_sync(~0u, id >= 0 && before == 0u);
+            if (!__any_sync(~0u, id >= 0 && __popc(same) > rows)) {
+                if (id >= 0) {
+                    Group *g = p.w.group + __popc(firsts & ((1u << (__ffs(same) - 1)) - 1));
+                    g->slot[__popc(before)] = (uint16_t)lane;
+                    if (before == 0u) {
+                        g->expert = id;
+                        g->n = __popc(same);
+                    }
+                }
+                if (lane == 0) *p.w.groups = __popc(firsts);
+                s.group[0] = -1;
+            } else {
+                s.group[0] = 0;
+            }
+        }
+        __syncthreads();
+        if (s.group[0] < 0) return;
+    }
     for (int e = threadIdx.x; e < E; e += blockDim.x) s.count[e] = 0;
     __syncthreads();
     for (int i = threadIdx.x; i < n; i += blockDim.x) {
