@@ -777,6 +777,7 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
         // mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.
         const bool digits = p.odd && (p.T <= 4 || p.slots <= 3 * p.E);
         p.split = !digits && y_type != DSQ_BF16;
+        p.scaled = !digits && p.odd && x_type == DSQ_BF16;
         p.rows = digits ? 4 : p.split || p.slots <= 5 * p.E ? 8 : 16;
         lay_out(p.w, (char *)workspace, p.T, p.slots, p.H, p.chunks_in, p.chunks_out);
         p.X = (const uint8_t *)X + t * H * 2;

@@ -25,7 +25,7 @@ struct alignas(64) Group {
 struct Work {
     int *groups;                      // how many
     Group *group;                     // by expert, the slots of an expert in their order
-    // digits: [T][chunks_in], [slots][chunks_out], what the highest digit stands for; 16 bits: [slots], what 1 stands for
+    // digits: [T][chunks_in], [slots][chunks_out], what the highest digit stands for; 16 bits: [T], [slots], what 1 stands for
     float *x_step, *mid_step;
     // digits: [T][chunks_in][512], [slots][chunks_out][512]; 16 bits: [T][chunks_in][256], [slots or 2 slots][chunks_out][256]
     uint8_t *x, *mid_rows;
@@ -46,7 +46,7 @@ struct MoeParams {
     uint32_t units_in, units_in_inv, units_out, units_out_inv;
     int odd, act, y_type;
     int rows;                                // slots of a group: 4 (digits), 8 or 16 (16 bits)
-    int split;                               // 16 bits: mid as two numbers
+    int split, scaled;                       // 16 bits: mid as two numbers; x, in bf16, as fp16 times a power of two
 };
 __device__ __forceinline__ uint4 load_16(const void *p)
 {

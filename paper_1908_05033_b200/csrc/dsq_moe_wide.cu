@@ -50,11 +50,65 @@ template <bool WHOLE> __global__ void __launch_bounds__(PREPARE_WARPS * 32) moe_
     else *reinterpret_cast<uint2 *>(to) = make_uint2(__byte_perm(v.x, o.x, 0x5410), __byte_perm(v.x, o.x, 0x7632));
 }
 
+// The power of two that brings the largest of a row below 2^15 (the smallest numbers' rows as far as binary32 has
+// powers of two), and what 1 stands for then; a block has the largest of each thread's elements, and whether one is
+// infinite or NaN.
+__device__ __forceinline__ float block_scale(float m, bool bad, float *step)
+{
+    __shared__ float most[8];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
+    if ((threadIdx.x & 31) == 0) most[threadIdx.x >> 5] = m;
+    bad = __syncthreads_or(bad);
+#pragma unroll
+    for (int w = 0; w < 8; ++w) m = fmaxf(m, most[w]);
+    const int e = (int)(__float_as_uint(m) >> 23), up = min(141 - e, 126);
+    if (threadIdx.x == 0) *step = __uint_as_float(bad ? 0x7FC00000u : (uint32_t)(127 - up) << 23);
+    return __uint_as_float((uint32_t)(127 + up) << 23);
+}
+
+// the same of bf16 as fp16 (scaled): block 1 + t has token t
+template <bool WHOLE> __global__ void __launch_bounds__(256) moe_wide_prepare_scaled_kernel(const __grid_constant__ MoeParams p)
+{
+    __shared__ Sorting sorting;
+    grid_dependency_wait();
+    grid_launch_dependents();
+    if (blockIdx.x == 0) {
+        sort_slots(p, sorting);
+        return;
+    }
+    const int t = blockIdx.x - 1, words = p.chunks_in * 16;
+    const uint4 *row = reinterpret_cast<const uint4 *>(p.X + (int64_t)t * p.H * 2);
+    float m = 0.f;
+    bool bad = false;
+    for (int i = threadIdx.x; 8 * i < p.H; i += 256) {
+        float f[8];
+        dsq_unpack8(dsq_load8(reinterpret_cast<const __nv_bfloat16 *>(row + i)), f);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m = fmaxf(m, fabsf(f[e]));
+            bad = bad || !(fabsf(f[e]) <= 3.402823466e38f);
+        }
+    }
+    const float by = block_scale(m, bad, p.w.x_step + t);
+    for (int i = threadIdx.x; i < words; i += 256) {
+        float f[8] = {};
+        if (8 * i < p.H) dsq_unpack8(dsq_load8(reinterpret_cast<const __nv_bfloat16 *>(row + i)), f);
+        uint32_t v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const __half2 h = __floats2half2_rn(f[k] * by, f[k + 4] * by);
+            v[k] = *reinterpret_cast<const uint32_t *>(&h);
+        }
+        *reinterpret_cast<uint4 *>(p.w.x + ((int64_t)t * p.chunks_in + (i >> 4)) * 256 + place_of<WHOLE>(i & 15)) =
+            make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+
 // mid's rows, a block a slot (of slots without an expert: of whatever lies there)
 template <bool WHOLE> __global__ void __launch_bounds__(256) moe_wide_mid_kernel(const __grid_constant__ MoeParams p)
 {
-    __shared__ float most[8];
-    const int slot = blockIdx.x, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int slot = blockIdx.x;
     grid_dependency_wait();
     grid_launch_dependents();
     const float *mid = p.w.mid + (int64_t)slot * p.chunks_out * 128;
@@ -70,16 +124,7 @@ template <bool WHOLE> __global__ void __launch_bounds__(256) moe_wide_mid_kernel
             bad = bad || !(fabsf(f[e]) <= 3.402823466e38f);
         }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(~0u, m, o));
-    if (lane == 0) most[warp] = m;
-    bad = __syncthreads_or(bad);
-#pragma unroll
-    for (int w = 0; w < 8; ++w) m = fmaxf(m, most[w]);
-    // 2^up brings the largest below 2^15 (the smallest numbers' rows as far as binary32 has powers of two)
-    const int e = (int)(__float_as_uint(m) >> 23), up = min(141 - e, 126);
-    const float by = __uint_as_float((uint32_t)(127 + up) << 23);
-    if (threadIdx.x == 0) p.w.mid_step[slot] = bad ? __uint_as_float(0x7FC00000u) : __uint_as_float((uint32_t)(127 - up) << 23);
+    const float by = block_scale(m, bad, p.w.mid_step + slot);
     uint8_t *rows = p.w.mid_rows + (int64_t)slot * p.chunks_out * 256 * (p.split ? 2 : 1);
     for (int i = threadIdx.x; i < words; i += 256) {
         const float4 a = reinterpret_cast<const float4 *>(mid)[2 * i], b = reinterpret_cast<const float4 *>(mid)[2 * i + 1];
@@ -129,12 +174,42 @@ template <int XT> __device__ __forceinline__ void mma_first(float (&d)[4], const
             : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
 }
 
+// A word of codes as operands' pairs: of elements i and i + 4 each.  For fp16 two of the four fields lie in the
+// mantissa at once, at its bits 1 to 4 and 5 to 8 of 32 and 2: two shifts instead of four (10 operations a word; bf16 has no
+// room for a second field: 12).
+template <int XT> struct Unpack {
+    uint32_t base;
+    __device__ __forceinline__ Unpack(int odd) : base(dsq_value_base<XT>(odd)) {}
+    __device__ __forceinline__ void operator()(uint32_t w, uint32_t (&v)[4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = dsq_value_pair<XT>(w, i, base);
+    }
+};
+template <> struct Unpack<DSQ_F16> {
+    uint32_t low, high;               // 32 and 2, and 7.5 / 16 or 8 / 16 beside
+    __device__ __forceinline__ Unpack(int odd) : low(odd ? 0x500F500Fu : 0x50105010u), high(odd ? 0x40F040F0u : 0x41004100u) {}
+    __device__ __forceinline__ void operator()(uint32_t w, uint32_t (&v)[4]) const
+    {
+        const uint32_t y[2] = {w << 1, w >> 7};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t mask = i & 1 ? 0x01E001E0u : 0x001E001Eu, flip = i & 1 ? 0x41004100u : 0x50105010u;
+            const uint32_t less = i & 1 ? high : low;
+            uint32_t f;
+            asm("lop3.b32 %0, %1, %2, %3, 0x6a;" : "=r"(f) : "r"(y[i >> 1]), "r"(mask), "r"(flip));
+            const __half2 r = __hsub2(*reinterpret_cast<const __half2 *>(&f), *reinterpret_cast<const __half2 *>(&less));
+            v[i] = *reinterpret_cast<const uint32_t *>(&r);
+        }
+    }
+};
+
 // What a lane has of a chunk's rows: of each tile of eight slots the elements of slot n beside its own words of codes.
 template <int TILES> struct Elements { uint4 x[TILES][4]; };
 
 // total[h][m] += scale (sum of v x) of a chunk: rows n and n + 8 of half h of the 32 columns, slots 2 j and 2 j + 1 of tile m
 template <int XT, int TILES, int GP>
-__device__ __forceinline__ void multiply(uint32_t at, uint32_t base, const Elements<TILES> &r, DsqPair (&total)[2][TILES][2])
+__device__ __forceinline__ void multiply(uint32_t at, const Unpack<XT> &unpack, const Elements<TILES> &r, DsqPair (&total)[2][TILES][2])
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES + n * 4;
@@ -157,9 +232,12 @@ __device__ __forceinline__ void multiply(uint32_t at, uint32_t base, const Eleme
         for (int q = 0; q < 4; ++q) {
             uint32_t a[2][4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int s = 0; s < 2; ++s) {
+                uint32_t v[4];
+                unpack(w[s][q], v);
 #pragma unroll
-                for (int s = 0; s < 2; ++s) a[i >> 1][(i & 1) * 2 + s] = dsq_value_pair<XT>(w[s][q], i, base);
+                for (int i = 0; i < 4; ++i) a[i >> 1][(i & 1) * 2 + s] = v[i];
+            }
 #pragma unroll
             for (int s = 0; s < 2; ++s)
 #pragma unroll
@@ -228,7 +306,7 @@ template <bool OUT, int XT, int GP> struct Wide {
 
     template <int TILES> __device__ __forceinline__ void run()
     {
-        const uint32_t base = dsq_value_base<XT>(p.odd);
+        const Unpack<XT> unpack(p.odd);
         const bool split = OUT && p.split;
         const uint8_t *x[TILES];
         Elements<TILES> r = {};
@@ -268,7 +346,7 @@ template <bool OUT, int XT, int GP> struct Wide {
             cp_async_wait<STAGES - 2>();
             __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
             issue();
-            multiply<XT, TILES, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), base, r, total);
+            multiply<XT, TILES, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), unpack, r, total);
             if (i + 1 < turns) load(wk + (i + 1) * KW);
             if (i + 2 < turns) touch(wk + (i + 2) * KW);
         }
@@ -305,8 +383,10 @@ template <bool OUT, int XT, int GP> struct Wide {
                 const int s = e / (WC * 16), c = e % (WC * 16), col = blockIdx.x * WC * 16 + c;
                 if (col >= chunks_of_mid()) continue;
                 // (columns behind the last are zeros up to the end of the chunk)
-                const float gate = sum(c >> 4, 0, c & 15, s) * unit, up = sum(c >> 4, 1, c & 15, s) * unit;
-                p.w.mid[(int64_t)group->slot[s] * chunks_of_mid() + col] = col < p.I ? activated(gate, p.act) * up : 0.f;
+                const int slot = group->slot[s];
+                const float of_x = p.scaled ? unit * p.w.x_step[slot / p.k] : unit;
+                const float gate = sum(c >> 4, 0, c & 15, s) * of_x, up = sum(c >> 4, 1, c & 15, s) * of_x;
+                p.w.mid[(int64_t)slot * chunks_of_mid() + col] = col < p.I ? activated(gate, p.act) * up : 0.f;
             }
         }
         __syncthreads();
@@ -399,10 +479,15 @@ template <class T> int combine(const MoeParams &p, cudaStream_t s)
 
 int dsq_moe::run_wide(const MoeParams &p, int x_type, int gp_in, int gp_out, cudaStream_t s)
 {
-    const int pdl = dsq_launch_hooks().pdl, blocks = 1 + (p.T * p.chunks_in + PREPARE_WARPS - 1) / PREPARE_WARPS;
-    int st = dsq_launch(gp_in == 4 ? moe_wide_prepare_kernel<true> : moe_wide_prepare_kernel<false>, dim3(blocks), dim3(PREPARE_WARPS * 32),
+    const int pdl = dsq_launch_hooks().pdl;
+    int st;
+    if (p.scaled)
+        st = dsq_launch(gp_in == 4 ? moe_wide_prepare_scaled_kernel<true> : moe_wide_prepare_scaled_kernel<false>, dim3(1 + p.T), dim3(256),
                         0, s, pdl, 0, p);
-    if (!st) st = x_type == DSQ_BF16 ? pick<false, DSQ_BF16>(p, gp_in, s) : pick<false, DSQ_F16>(p, gp_in, s);
+    else
+        st = dsq_launch(gp_in == 4 ? moe_wide_prepare_kernel<true> : moe_wide_prepare_kernel<false>,
+                        dim3(1 + (p.T * p.chunks_in + PREPARE_WARPS - 1) / PREPARE_WARPS), dim3(PREPARE_WARPS * 32), 0, s, pdl, 0, p);
+    if (!st) st = x_type == DSQ_BF16 && !p.scaled ? pick<false, DSQ_BF16>(p, gp_in, s) : pick<false, DSQ_F16>(p, gp_in, s);
     if (!st) st = dsq_launch(gp_out == 4 ? moe_wide_mid_kernel<true> : moe_wide_mid_kernel<false>, dim3(p.slots), dim3(256), 0, s, pdl, 0, p);
     if (!st) st = pick<true, DSQ_F16>(p, gp_out, s);
     if (!st)
