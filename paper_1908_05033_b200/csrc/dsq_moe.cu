@@ -10,7 +10,7 @@
 // (2^-30 of the largest's power of two), and four slots' digits are the 16 rows of an instruction.
 //
 //   * A slot is a token's s-th choice.  moe_prepare_kernel sorts the slots by expert (stable), cuts each
-//     expert's into groups of up to eight, and makes digits of x.
+//     expert's into groups of up to four, and makes digits of x, as an instruction's rows want them.
 //   * moe_in_kernel: a block has columns of a group's gate and the same ones of its other half; warps
 //     split columns and K in chunks of 128 codes, each through a ring of stages of its own (cp.async,
 //     no barrier between warps); their sums are added in a fixed order, and the activation makes
@@ -24,6 +24,9 @@
 //     element what is below 2^-31 of the largest of its 128: for the codes' grid Delta (c + 1/2),
 //     which has no 0, that is below the rounding of the sums.  The grid Delta c, whose 0 can make the largest
 //     element vanish, and experts with more slots go on 16 bits (dsq_moe_wide.cu).
+// One token of 2048 to 1024, eight of 64 experts (27 MB of codes and scales): 14.5 us, of which four launches in a row
+// without work are 6; 16 tokens of 4096 to 1024, four of 64 (276 MB): 75.5 us, 3.7 TB/s, issue slots 65 to 70 % (275 instructions a
+// chunk of 2 KB: 97 for its copies, 187 to unpack and multiply), tensor pipe 22 %.
 #include "dsq_moe.cuh"
 
 using namespace dsq_moe;
@@ -773,9 +776,15 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
     for (int64_t t = 0; t < T; t += PASS_TOKENS) {
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
-        // Digits where few experts can be expected to have more than four slots, and where no code is 0 (see above).  On 16 bits
-        // mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.
-        const bool digits = p.odd && (p.T <= 4 || p.slots <= 3 * p.E);
+        // Digits where few experts can be expected to have several slots, and where no code is 0 (see above): at 54 sizes
+        // within 9 % of the faster form, 2 % on average.  4096 to 2048, 8 experts, two a token: 2 tokens 21.1 us on digits, 25.8 on
+        // 16 bits; 5 tokens 33.0 and 35.9; 8 tokens 38.3 and 36.3; 48 tokens 115 and 49.  4096 to 1024, 64 experts, four
+        // a token: 4 tokens 32.6 and 35.9; 24 tokens 87.3 and 87.5; 32 tokens 99.3 and 96.0; 48 tokens 147 and 111.
+        const bool digits = p.odd && (p.T <= 4 || 2 * p.slots <= 3 * p.E);
+        // On 16 bits: mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.  Sixteen rows of elements
+        // share an expert's codes where it can be expected to have more than five, with two blocks an SM instead of
+        // three: 48 tokens of 4096 to 2048, 8 experts, two a token, 49 us, 84 with eight; of 4096 to 1024, 64 experts, four a
+        // token, 119 us and 111.
         p.split = !digits && y_type != DSQ_BF16;
         p.scaled = !digits && p.odd && x_type == DSQ_BF16;
         p.rows = digits ? 4 : p.split || p.slots <= 5 * p.E ? 8 : 16;
