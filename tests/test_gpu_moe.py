@@ -58,7 +58,7 @@ class Layer:
         H, I, k = self.x.shape[1], self.I, self.ids.shape[1]
         # (a pass takes 64 tokens: the first ones say more than the last few)
         few = min(len(self.x), 64)
-        narrow = w_offset == 0.5 and (few <= 4 or few * k <= 3 * self.E) and len(self.x) <= 64
+        narrow = w_offset == 0.5 and (few <= 4 or 2 * few * k <= 3 * self.E) and len(self.x) <= 64
         eps_mid = 20 * U + (0 if narrow else 2.0 ** -11 if y.dtype == torch.bfloat16 else 2.0 ** -22)
         ref, bound = moe.layer(self.x.double().numpy(), self.ids, self.w, self.c_in, self.s_in, self.c_out, self.s_out,
                                self.E, I, self.group, kind, w_offset, self.residual.double().numpy() if residual else None,
@@ -159,6 +159,30 @@ def test_outliers(dsq, T, t, off):
         a.s_in *= 1e-3
         a.weights[1] = torch.from_numpy(a.s_in).cuda()
         a.check(a.run(dsq, out_dtype=torch.float32, residual=None), residual=False)
+
+
+@pytest.mark.parametrize("t", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("off", [0.5, 0.0])
+@pytest.mark.parametrize("T", [3, 30])
+def test_powers_of_two(dsq, T, off, t):
+    """Rows far from 1 (of fp16 and the smallest of bf16: with elements below the type's normal numbers), and one of zeros."""
+    for e in (-126, -60, 100) if t == torch.bfloat16 else (-14, -8, 10):
+        a = Layer(dsq, T, 328, 64, 3, 2, 64, t=t, seed=7)
+        a.x = (a.x.double() * 2.0 ** e).to(t)
+        a.x[2] = 0
+        a.s_in = (a.s_in * 2.0 ** -e).astype(np.float32)
+        a.weights[1] = torch.from_numpy(a.s_in).cuda()
+        a.check(a.run(dsq, w_offset=off, residual=None, out_dtype=torch.float32), w_offset=off, residual=False)
+
+
+@pytest.mark.parametrize("T", [3, 30])
+def test_outliers_of_bf16(dsq, T):
+    """One element of a row 2^40 above the others: those still count to 2^-30 of it."""
+    a = Layer(dsq, T, 512, 96, 3, 2, 64, seed=8)
+    a.x[:, 5] = 2.0 ** 40
+    a.s_in *= np.float32(2.0 ** -36)
+    a.weights[1] = torch.from_numpy(a.s_in).cuda()
+    a.check(a.run(dsq, out_dtype=torch.float32, residual=None), residual=False)
 
 
 def test_large_values(dsq):
