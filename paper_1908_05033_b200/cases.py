@@ -10,6 +10,11 @@
     python -m paper_1908_05033_b200.cases normbwd --m 8192 --size 4096
     python -m paper_1908_05033_b200.cases groups --n 16384 --k 4096 --group 128
     python -m paper_1908_05033_b200.cases glinear --m 64 --size 8192 --group 128 --type bf16
+    python -m paper_1908_05033_b200.cases heads --m 16384 --size 128         (m tokens, 32 + 8 heads)
+    python -m paper_1908_05033_b200.cases headsbwd --m 8192 --size 128
+    python -m paper_1908_05033_b200.cases moe --m 16 --n 1024 --k 4096 --experts 64 --top 4
+    python -m paper_1908_05033_b200.cases logprob --m 4096 --k 128000 --top 5
+    python -m paper_1908_05033_b200.cases logprobbwd --m 1024 --k 128000
 
 Each runs the named kernel `--iters` times on seeded synthetic inputs (an L2
 flush between launches) and prints the median CUDA-event time with the
@@ -45,13 +50,16 @@ def _timeit(fn, iters, flush):
 def main(argv=None):
     ap = argparse.ArgumentParser()
     ap.add_argument("case", choices=["gemm", "bgemm", "wgemm", "conv", "quant", "dw", "soft",
-                                     "norm", "normbwd", "groups", "glinear"])
+                                     "norm", "normbwd", "groups", "glinear",
+                                     "heads", "headsbwd", "moe", "logprob", "logprobbwd"])
     ap.add_argument("--size", type=int, default=4096)
     ap.add_argument("--m", type=int, default=0, help="rows of a GEMM's result (0: --size)")
     ap.add_argument("--n", type=int, default=0, help="its columns")
     ap.add_argument("--k", type=int, default=0, help="its inner extent")
     ap.add_argument("--bits", type=int, default=4)
     ap.add_argument("--group", type=int, default=128, help="weights that share a scale")
+    ap.add_argument("--experts", type=int, default=64)
+    ap.add_argument("--top", type=int, default=4, help="experts of a token, alternatives of a row of logits")
     ap.add_argument("--type", choices=["f32", "bf16", "f16", "i8"], default="bf16", help="rows of norm and glinear")
     ap.add_argument("--iters", type=int, default=5)
     ap.add_argument("--cin", type=int, default=64)
@@ -151,6 +159,48 @@ def main(argv=None):
                                                        out_dtype=torch.bfloat16, out=Y), a.iters, flush)
         out.update(size=[m, n, k], group=a.group, ms=ms, gbs=(W.numel() + 4 * sc.numel()) / (ms * 1e-3) / 1e9,
                    tflops=2.0 * m * n * k / (ms * 1e-3) / 1e12, all_ms=all_ms)
+    elif a.case in ("heads", "headsbwd"):
+        # m tokens of 32 heads of q and 8 of k, --size elements each
+        t = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[a.type]
+        q, kk, gq, gk = (torch.randn((m, h, a.size), device=dev, generator=gen).to(t) for h in (32, 8, 32, 8))
+        w = torch.rand(a.size, device=dev, generator=gen) + 0.5
+        pos = torch.arange(m, device=dev)
+        freq = 10000.0 ** (-torch.arange(0, a.size, 2, device=dev).float() / a.size)
+        if a.case == "heads":
+            ms, all_ms = _timeit(lambda: B.dsq_headnorm_fwd(q, kk, pos, freq, w, w), a.iters, flush)
+        else:
+            ms, all_ms = _timeit(lambda: B.dsq_headnorm_bwd(gq, gk, q, kk, pos, freq, w, w), a.iters, flush)
+        nbytes = (q.numel() + kk.numel()) * q.element_size() * (2 if a.case == "heads" else 3)
+        out.update(size=[m, 32, 8, a.size], ms=ms, gbs=nbytes / (ms * 1e-3) / 1e9, all_ms=all_ms)
+    elif a.case == "moe":
+        # m tokens of k elements through experts of n
+        X = torch.randn((m, k), device=dev, generator=gen).to(torch.float16 if a.type == "f16" else torch.bfloat16)
+        logits = torch.randn((m, a.experts), device=dev, generator=gen)
+        ids, weights = B.dsq_moe_route(logits, a.top)
+        w_in, w_out = (torch.randint(0, 256, (rows, B.dsq_row_pitch(c, 4)), dtype=torch.uint8, device=dev, generator=gen)
+                       for rows, c in ((a.experts * 2 * n, k), (a.experts * k, n)))
+        s_in, s_out = (torch.rand((B.dsq_group_count(c, a.group), rows), device=dev, generator=gen) * 0.01
+                       for rows, c in ((a.experts * 2 * n, k), (a.experts * k, n)))
+        mws = torch.empty(B.dsq_moe_workspace_bytes(m, k, n, a.top), dtype=torch.uint8, device=dev)
+        ms, all_ms = _timeit(lambda: B.dsq_moe_group(X, ids, weights, w_in, s_in, w_out, s_out, a.experts, n, 4, a.group,
+                                                     residual=X, ws=mws), a.iters, flush)
+        used = ids.unique().numel()
+        nbytes = used * (w_in.numel() + w_out.numel() + 4 * (s_in.numel() + s_out.numel())) / a.experts
+        out.update(size=[m, k, n], experts=a.experts, top=a.top, used=used, ms=ms, gbs=nbytes / (ms * 1e-3) / 1e9,
+                   all_ms=all_ms)
+    elif a.case in ("logprob", "logprobbwd"):
+        # m rows of k logits
+        t = {"f32": torch.float32, "bf16": torch.bfloat16, "f16": torch.float16}[a.type]
+        logits = torch.randn((m, k), device=dev, generator=gen).to(t)
+        ids = torch.randint(0, k, (m,), device=dev, generator=gen)
+        lse, g = B.dsq_logprob_fwd(logits, ids)[2], torch.ones(m, device=dev)
+        nbytes = logits.numel() * logits.element_size()
+        if a.case == "logprob":
+            ms, all_ms = _timeit(lambda: B.dsq_logprob_fwd(logits, ids, top=a.top), a.iters, flush)
+        else:
+            nbytes *= 2
+            ms, all_ms = _timeit(lambda: B.dsq_logprob_bwd(logits, ids, lse, g), a.iters, flush)
+        out.update(size=[m, k], ms=ms, gbs=nbytes / (ms * 1e-3) / 1e9, all_ms=all_ms)
     elif a.case == "conv":
         shape = (a.batch, a.hw, a.hw, a.cin)
         pitch = B.dsq_row_pitch(a.cin, bits)
