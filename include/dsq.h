@@ -415,7 +415,8 @@ int dsq_rmsnorm_bwd(const void *grad_y, const void *grad_h, const void *h,
  *   positions  int64 [axes][tokens] (one position a token, or one for time, height and width ...)
  *   inv_freq   fp32 [rot_dim / 2]
  *   axis       uint8 [rot_dim / 2], below axes (a pair with another one is NaN); NULL: all 0
- * Angles are formed and reduced in binary64, cosines and sines are binary32. */
+ * Angles are formed and reduced in binary64, cosines and sines are binary32; an angle of 2^50 or more, which binary64
+ * does not hold to a part of a turn, makes its pair NaN. */
 typedef struct dsq_rotary_t {
     const int64_t *positions;
     const float *inv_freq;

@@ -55,14 +55,16 @@ struct Params {
     float eps, inv_d;
 };
 
-// Cosine and sine of pos f: the angle and what it is beyond a whole number of quarter turns in binary64 (that number
-// below 2^51), then the two series at most pi / 4 away from 0, whose first terms left out are below 2^-29.
+// Cosine and sine of pos f: the angle and what it is beyond a whole number of quarter turns in binary64 (below 2^50, else
+// NaN: binary64 has no fourth of a turn left then), then the two series at most pi / 4 away from 0, whose first terms left out are
+// below 2^-29.
 __device__ __forceinline__ float2 turn_of(int64_t pos, float f)
 {
     constexpr double WHOLE = 6755399441055744.0;              // 1.5 2^52: the sum's low bits are the whole number
     const double a = (double)pos * (double)f, k1 = fma(a, 0.6366197723675814, WHOLE), k = k1 - WHOLE;
     // pi / 2 in two parts
-    const float r = (float)fma(-k, 6.123233995736766e-17, fma(-k, 1.5707963267948966, a));
+    float r = (float)fma(-k, 6.123233995736766e-17, fma(-k, 1.5707963267948966, a));
+    if (!(fabs(a) < 1125899906842624.0)) r = __int_as_float(0x7FC00000);
     const int q = __double2loint(k1) & 3;
     const float x = r * r;
     float c = __fmaf_rn(x, -1.f / 3628800.f, 1.f / 40320.f);

@@ -10,7 +10,7 @@
 //     block joins the parts.  A thread keeps m, s and t of its elements in one pass; four vectors are
 //     on their way together.  The exponents are powers of two, x c - M with c = scale log2 e and M = m c as
 //     binary32 rounds it: one fused operation, the rounding of M being the same in s, t and the target's
-//     exponent.  Four instructions an element in all; where an element is -infinity, or M is large enough for its
+//     exponent.  Four instructions an element for the three; where an element is -infinity, or M is large enough for its
 //     rounding to matter, (x - m) c instead, held above -1000 (six).
 //   * Alternatives: a thread leaves the largest element of each turn of its loop in shared memory.  Fours of
 //     threads form groups; the top-th of the groups' largest elements bounds from below what can be among the

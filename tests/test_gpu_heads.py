@@ -199,6 +199,21 @@ def test_far_positions(dsq):
     assert np.all(np.abs(N(y.double()) - heads.turn(np.ones((6, 1, D)), a)) <= tol)
 
 
+def test_angles_beyond_binary64_are_nan(dsq):
+    """2^50 - 3 is an angle, 2^50 and the ends of the range are none; the elements that are not turned stay."""
+    x = torch.randn(6, 2, 64, device="cuda")
+    top = 2 ** 63 - 1
+    pos = torch.tensor([2 ** 50 - 3, -(2 ** 50) + 3, 2 ** 50, -(2 ** 50), top, -top - 1])
+    freq = torch.ones(16)
+    freq[1] = 0.0
+    y, _ = dsq.dsq_headnorm_fwd(x, None, pos.cuda(), freq.cuda(), norm=False)
+    check_forward(y[:2], x[:2].cpu(), None, heads.angles(pos[:2].numpy(), freq.numpy()), 0.0, False, torch.float32, norm=False)
+    turned = torch.ones(64, dtype=torch.bool)
+    turned[32:] = False
+    turned[[1, 17]] = False
+    assert y[2:][..., turned].isnan().all() and torch.equal(y[2:][..., ~turned], x[2:][..., ~turned])
+
+
 def test_axis_out_of_range_is_nan(dsq):
     x, freq = torch.ones(2, 3, 32), torch.ones(16)
     axis = torch.zeros(16, dtype=torch.uint8)
