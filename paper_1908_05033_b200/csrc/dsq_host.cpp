@@ -810,8 +810,9 @@ PyObject *logprob_fwd(PyObject *, PyObject *const *a, Py_ssize_t n)
         if (targets) logp = new_tensor({M}, at::kFloat, x);
         if (as_bool(a[4])) entropy = new_tensor({M}, at::kFloat, x);
         if (top > 0) {
-            ids = new_tensor({M, top}, at::kLong, x);
-            top_logp = new_tensor({M, top}, at::kFloat, x);
+            const int64_t room = std::min<int64_t>(top, 64);           // (more than 32 are refused)
+            ids = new_tensor({M, room}, at::kLong, x);
+            top_logp = new_tensor({M, room}, at::kFloat, x);
         }
         check(enqueue([&](void *s) {
                   return dsq_logprob_fwd(x.data_ptr(), row_stride(x), M, x.size(1), type_code(x.scalar_type()),
@@ -864,7 +865,8 @@ PyObject *moe_route(PyObject *, PyObject *const *a, Py_ssize_t n)
         const int64_t k = as_int(a[1]);
         const bool renormalise = as_bool(a[2]);
         want(k >= 0 && k <= 1 << 20, "k: want a number of experts");
-        at::Tensor ids = new_tensor({x.size(0), k}, at::kInt, x), weights = new_tensor({x.size(0), k}, at::kFloat, x);
+        const int64_t room = std::min<int64_t>(k, 64);                 // (more than 32 are refused)
+        at::Tensor ids = new_tensor({x.size(0), room}, at::kInt, x), weights = new_tensor({x.size(0), room}, at::kFloat, x);
         check(enqueue([&](void *s) {
                   return dsq_moe_route((const float *)x.data_ptr(), x.size(0), x.size(1), (int)k, renormalise,
                                        (int32_t *)ids.data_ptr(), (float *)weights.data_ptr(), s);

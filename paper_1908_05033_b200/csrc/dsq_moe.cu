@@ -643,7 +643,7 @@ template <int GP> int launch_in(const MoeParams &p, cudaStream_t s)
     const int st = dsq_allow_smem((const void *)kernel, bytes, &configured);
     if (st) return st;
     // (to the end of the last chunk: zeros)
-    const dim3 grid((unsigned)((p.chunks_out * 128 + cols - 1) / cols), (unsigned)(p.slots < p.E ? p.slots : p.E));
+    const dim3 grid((unsigned)((p.chunks_out * 128 + cols - 1) / cols), (unsigned)p.groups_most());
     return dsq_launch(kernel, grid, dim3(IN_WARPS * 32), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
 }
 

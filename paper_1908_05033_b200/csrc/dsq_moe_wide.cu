@@ -464,7 +464,7 @@ template <bool OUT, int XT, int GP, int MOST> int launch(const MoeParams &p, cud
     if (st) return st;
     // (of mid to the end of the last chunk: zeros)
     const int columns = OUT ? p.H : p.chunks_out * 128;
-    const dim3 grid((unsigned)((columns + cols - 1) / cols), (unsigned)(p.slots < p.E ? p.slots : p.E));
+    const dim3 grid((unsigned)((columns + cols - 1) / cols), (unsigned)p.groups_most());
     return dsq_launch(kernel, grid, dim3(THREADS), (size_t)bytes, s, dsq_launch_hooks().pdl, 0, p);
 }
 template <bool OUT, int XT> int pick(const MoeParams &p, int gp, cudaStream_t s)
