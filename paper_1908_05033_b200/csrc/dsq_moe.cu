@@ -24,8 +24,8 @@
 //     element what is below 2^-31 of the largest of its 128: for the codes' grid Delta (c + 1/2),
 //     which has no 0, that is below the rounding of the sums.  The grid Delta c, whose 0 can make the largest
 //     element vanish, and experts with more slots go on 16 bits (dsq_moe_wide.cu).
-// One token of 2048 to 1024, eight of 64 experts (27 MB of codes and scales): 14.5 us, of which four launches in a row
-// without work are 6; 16 tokens of 4096 to 1024, four of 64 (276 MB): 75.5 us, 3.7 TB/s, issue slots 65 to 70 % (275 instructions a
+// One token of 2048 to 1024, eight of 64 experts (27 MB of codes and scales): 13.6 us, of which four launches in a row
+// without work are 6 (14.4 where the first product's copies wait for the groups that the kernel ahead writes); 16 tokens of 4096 to 1024, four of 64 (276 MB): 75 us, 3.7 TB/s, issue slots 65 to 70 % (275 instructions a
 // chunk of 2 KB: 97 for its copies, 187 to unpack and multiply), tensor pipe 22 %.
 #include "dsq_moe.cuh"
 
@@ -124,6 +124,18 @@ struct Members {
     {
         const uint32_t w = r & 2 ? slots.y : slots.x;
         return (int)(r & 1 ? w >> 16 : w & 0xFFFFu);
+    }
+    // of slots as bits, four at most
+    __device__ __forceinline__ void set(uint32_t bits)
+    {
+        n = __popc(bits);
+        uint32_t at[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            at[i] = bits ? (uint32_t)__ffs(bits) - 1 : 0u;
+            bits &= bits - 1;
+        }
+        slots = make_uint2(at[0] | at[1] << 16, at[2] | at[3] << 16);
     }
 };
 __device__ __forceinline__ Members members_of(const Work &w, int i)
@@ -441,16 +453,43 @@ template <int GP, int WC, int STAGES>
 __global__ void __launch_bounds__(IN_WARPS * 32, 3) moe_in_kernel(const __grid_constant__ MoeParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    grid_dependency_wait();
-    grid_launch_dependents();
-    // (what is there of a group that is not is not used)
-    Members g = members_of(p.w, blockIdx.y);
-    const int groups = *p.w.groups;
+    // Where there are few slots their groups follow from the ids, which are older than the kernel ahead: the first codes are
+    // on their way while that makes digits of x.
+    Members g;
+    int groups = -1;
+    if (p.slots <= 32) {
+        const Few few(p);
+        if (few.fit) {
+            groups = few.groups();
+            if ((int)blockIdx.y < groups) {
+                uint32_t slots;
+                few.group(blockIdx.y, g.expert, slots);
+                g.set(slots);
+            }
+        }
+    }
+    bool waited = groups < 0;
+    if (waited) {
+        grid_dependency_wait();
+        grid_launch_dependents();
+        // (what is there of a group that is not is not used)
+        g = members_of(p.w, blockIdx.y);
+        groups = *p.w.groups;
+    }
     for (int i = blockIdx.y; i < groups; i += gridDim.y, g = members_of(p.w, min(i, groups - 1))) {
         In<GP, WC, STAGES> in(p, g, smem);
 #pragma unroll
         for (int s = 0; s < STAGES - 1; ++s) in.issue();
+        if (!waited) {
+            grid_dependency_wait();
+            grid_launch_dependents();
+            waited = true;
+        }
         in.run();
+    }
+    if (!waited) {
+        grid_dependency_wait();
+        grid_launch_dependents();
     }
 }
 

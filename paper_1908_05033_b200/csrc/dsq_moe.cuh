@@ -58,32 +58,52 @@ __device__ __forceinline__ uint4 load_16(const void *p)
     return r;
 }
 
+// Up to 32 slots, one a lane of a warp: groups in the order of their first slots, unless an expert has more than one.
+struct Few {
+    int id;                           // of the lane's slot, -1: none
+    uint32_t same, firsts;            // lanes of this lane's expert; the first lane of each expert
+    bool fit;                         // no expert has more than one group
+    __device__ __forceinline__ explicit Few(const MoeParams &p)
+    {
+        const int lane = threadIdx.x & 31;
+        id = lane < p.slots ? p.ids[lane] : -1;
+        if (id < 0 || id >= p.E) id = -1;
+        same = __match_any_sync(~0u, id);
+        firsts = __ballot_sync(~0u, id >= 0 && (same & below()) == 0u);
+        fit = !__any_sync(~0u, id >= 0 && __popc(same) > p.rows);
+    }
+    __device__ __forceinline__ static uint32_t below() { return (1u << (threadIdx.x & 31)) - 1; }
+    __device__ __forceinline__ int groups() const { return __popc(firsts); }
+    // group i (there is one): its expert, its slots as bits
+    __device__ __forceinline__ void group(int i, int &expert, uint32_t &slots) const
+    {
+        const uint32_t of = __ballot_sync(~0u, (firsts >> (threadIdx.x & 31) & 1) && __popc(firsts & below()) == i);
+        expert = __shfl_sync(~0u, id, __ffs(of) - 1);
+        slots = __shfl_sync(~0u, same, __ffs(of) - 1);
+    }
+};
+
 // Sorts the slots whose expert there is, and cuts them into groups.  A block.
 struct Sorting { int count[MAX_EXPERTS], group[MAX_EXPERTS]; };
 __device__ __forceinline__ void sort_slots(const MoeParams &p, Sorting &s)
 {
     const int lane = threadIdx.x & 31, E = p.E, n = p.slots, rows = p.rows, shift = rows == 16 ? 4 : rows == 8 ? 3 : 2;
     if (n <= 32) {
-        // A slot a lane: groups in the order of their first slots, unless an expert has more than one.
         if (threadIdx.x < 32) {
-            int id = lane < n ? p.ids[lane] : -1;
-            if (id < 0 || id >= E) id = -1;
-            const uint32_t same = __match_any_sync(~0u, id), before = same & ((1u << lane) - 1);
-            const uint32_t firsts = __ballot_sync(~0u, id >= 0 && before == 0u);
-            if (!__any_sync(~0u, id >= 0 && __popc(same) > rows)) {
-                if (id >= 0) {
-                    Group *g = p.w.group + __popc(firsts & ((1u << (__ffs(same) - 1)) - 1));
-                    g->slot[__popc(before)] = (uint16_t)lane;
-                    if (before == 0u) {
-                        g->expert = id;
-                        g->n = __popc(same);
+            const Few few(p);
+            if (few.fit) {
+                const int before = __popc(few.same & Few::below());
+                if (few.id >= 0) {
+                    Group *g = p.w.group + __popc(few.firsts & ((1u << (__ffs(few.same) - 1)) - 1));
+                    g->slot[before] = (uint16_t)lane;
+                    if (before == 0) {
+                        g->expert = few.id;
+                        g->n = __popc(few.same);
                     }
                 }
-                if (lane == 0) *p.w.groups = __popc(firsts);
-                s.group[0] = -1;
-            } else {
-                s.group[0] = 0;
+                if (lane == 0) *p.w.groups = few.groups();
             }
+            if (lane == 0) s.group[0] = few.fit ? -1 : 0;
         }
         __syncthreads();
         if (s.group[0] < 0) return;

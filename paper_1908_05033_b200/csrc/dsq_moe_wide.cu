@@ -402,13 +402,30 @@ template <bool OUT, int XT, int GP, int MOST>
 __global__ void __launch_bounds__(THREADS, MOST == 1 ? 3 : 2) moe_wide_kernel(const __grid_constant__ MoeParams p)
 {
     extern __shared__ __align__(128) uint8_t smem[];
-    if (!OUT) grid_dependency_wait();
-    // (the second product: slots, codes and scales are older than the kernel ahead, moe_wide_mid_kernel)
-    const uint4 first = load_16(p.w.group + blockIdx.y);       // (what is there of a group that is not is not used)
-    const int groups = *p.w.groups;
-    int expert = (int)first.x, slots = (int)first.y;
-    bool waited = !OUT;
-    if (!OUT) grid_launch_dependents();
+    // (the second product: slots, codes and scales are older than the kernel ahead, moe_wide_mid_kernel; the first: ids,
+    // which say what groups of few slots there are)
+    int expert = 0, slots = 0, groups = -1;
+    bool waited = false;
+    if (!OUT && p.slots <= 32) {
+        const Few few(p);
+        if (few.fit) {
+            groups = few.groups();
+            uint32_t of = 0u;
+            if ((int)blockIdx.y < groups) few.group(blockIdx.y, expert, of);
+            slots = __popc(of);
+        }
+    }
+    if (groups < 0) {
+        if (!OUT) {
+            grid_dependency_wait();
+            grid_launch_dependents();
+            waited = true;
+        }
+        const uint4 first = load_16(p.w.group + blockIdx.y);   // (what is there of a group that is not is not used)
+        groups = *p.w.groups;
+        expert = (int)first.x;
+        slots = (int)first.y;
+    }
     for (int i = blockIdx.y; i < groups; i += gridDim.y) {
         if (i != (int)blockIdx.y) {
             expert = p.w.group[i].expert;
