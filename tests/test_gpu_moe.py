@@ -194,6 +194,43 @@ def test_large_values(dsq):
     a.check(a.run(dsq))
 
 
+@pytest.mark.parametrize("T,off", [(1, 0.5), (8, 0.5), (8, 0.0), (40, 0.5)])
+def test_ids_and_weights_written_right_ahead(dsq, T, off):
+    """A step that writes the router's logits, codes and scales before each call: nothing of the step before is used."""
+    a, b = (Layer(dsq, T, 256, 128, 6, 2, 64, seed=s) for s in (9, 10))
+    g = torch.Generator().manual_seed(T)
+    logits = [torch.randn(T, 6, generator=g).cuda() for _ in range(2)]
+    x = [v.x.cuda() for v in (a, b)]
+    expected = []
+    for i, v in enumerate((a, b)):
+        ids, w = dsq.dsq_moe_route(logits[i], 2)
+        expected.append(dsq.dsq_moe_group(x[i], ids, w, *v.weights, w_offset=off))
+        torch.cuda.synchronize()
+    now = [v.clone() for v in a.weights[:4]]
+    z, X = logits[0].clone(), x[0].clone()
+    ws = torch.empty(dsq.dsq_moe_workspace_bytes(T, 256, 128, 2), dtype=torch.uint8, device="cuda")
+    out = [torch.empty_like(x[0]) for _ in range(8)]
+
+    def steps():
+        for i in range(8):
+            for to, of in zip(now, (a, b)[i % 2].weights):
+                to.copy_(of)
+            z.copy_(logits[i % 2])
+            X.copy_(x[i % 2])
+            ids, w = dsq.dsq_moe_route(z, 2)
+            dsq.dsq_moe_group(X, ids, w, *now, *a.weights[4:], w_offset=off, out=out[i], ws=ws)
+
+    steps()
+    assert all(torch.equal(o, expected[i % 2]) for i, o in enumerate(out))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        steps()
+    for o in out:
+        o.zero_()
+    graph.replay()
+    assert all(torch.equal(o, expected[i % 2]) for i, o in enumerate(out))
+
+
 @pytest.mark.parametrize("E", [1, 5, 64, 65, 256, 300, 2000])
 @pytest.mark.parametrize("renormalise", [True, False])
 def test_route(dsq, E, renormalise):
