@@ -816,9 +816,9 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
         // Digits where few experts can be expected to have several slots, and where no code is 0 (see above): at 54 sizes
-        // within 9 % of the faster form, 2 % on average.  4096 to 2048, 8 experts, two a token: 2 tokens 21.1 us on digits, 25.8 on
-        // 16 bits; 5 tokens 33.0 and 35.9; 8 tokens 38.3 and 36.3; 48 tokens 115 and 49.  4096 to 1024, 64 experts, four
-        // a token: 4 tokens 32.6 and 35.9; 24 tokens 87.3 and 87.5; 32 tokens 99.3 and 96.0; 48 tokens 147 and 111.
+        // within 11 % of the faster form, 1 % on average.  4096 to 2048, 8 experts, two a token: 2 tokens 19.9 us on digits, 24.7 on
+        // 16 bits; 5 tokens 32.0 and 34.8; 8 tokens 36.8 and 35.6; 48 tokens 107 and 49.  4096 to 1024, 64 experts, four
+        // a token: 4 tokens 32.0 and 34.7; 24 tokens 85.6 and 87.7; 32 tokens 97.5 and 95.6; 48 tokens 145 and 111.
         const bool digits = p.odd && (p.T <= 4 || 2 * p.slots <= 3 * p.E);
         // On 16 bits: mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.  Sixteen rows of elements
         // share an expert's codes where it can be expected to have more than five, with two blocks an SM instead of
