@@ -816,17 +816,15 @@ int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *we
         p.T = (int)(T - t < PASS_TOKENS ? T - t : PASS_TOKENS);
         p.slots = p.T * k;
         // Digits where few experts can be expected to have several slots, and where no code is 0 (see above): at 54 sizes
-        // within 11 % of the faster form, 1 % on average.  4096 to 2048, 8 experts, two a token: 2 tokens 19.9 us on digits, 24.7 on
-        // 16 bits; 5 tokens 32.0 and 34.8; 8 tokens 36.8 and 35.6; 48 tokens 107 and 49.  4096 to 1024, 64 experts, four
-        // a token: 4 tokens 32.0 and 34.7; 24 tokens 85.6 and 87.7; 32 tokens 97.5 and 95.6; 48 tokens 145 and 111.
+        // within 14 % of the faster form, 1.5 % on average.  4096 to 2048, 8 experts, two a token: 2 tokens 20.1 us on digits, 26.8 on
+        // 16 bits; 5 tokens 32.7 and 36.2; 8 tokens 36.2 and 36.8; 48 tokens 107 and 56.  4096 to 1024, 64 experts, four
+        // a token: 4 tokens 32.1 and 35.4; 24 tokens 85.7 and 91.4; 32 tokens 97.6 and 100.2; 48 tokens 145 and 117.
         const bool digits = p.odd && (p.T <= 4 || 2 * p.slots <= 3 * p.E);
-        // On 16 bits: mid is one fp16 number where y is bf16 (2^-12 beside y's 2^-9), else two.  Sixteen rows of elements
-        // share an expert's codes where it can be expected to have more than five, with two blocks an SM instead of
-        // three: 48 tokens of 4096 to 2048, 8 experts, two a token, 49 us, 84 with eight; of 4096 to 1024, 64 experts, four a
-        // token, 119 us and 111.
-        p.split = !digits && y_type != DSQ_BF16;
+        // On 16 bits sixteen slots share an expert's codes where it can be expected to have more than five, with two blocks an SM
+        // instead of three: 48 tokens of 4096 to 2048, 8 experts, two a token, 56 us, 71 with eight; of 4096 to 1024, 64
+        // experts, four a token, 129 us and 117.
         p.scaled = !digits && p.odd && x_type == DSQ_BF16;
-        p.rows = digits ? 4 : p.split || p.slots <= 5 * p.E ? 8 : 16;
+        p.rows = digits ? 4 : p.slots <= 5 * p.E ? 8 : 16;
         lay_out(p.w, (char *)workspace, p.T, p.slots, p.H, p.chunks_in, p.chunks_out);
         p.X = (const uint8_t *)X + t * H * 2;
         p.ids = ids + t * k; p.weights = weights + t * k;

@@ -27,7 +27,7 @@ struct Work {
     Group *group;                     // by expert, the slots of an expert in their order
     // digits: [T][chunks_in], [slots][chunks_out], what the highest digit stands for; 16 bits: [T], [slots], what 1 stands for
     float *x_step, *mid_step;
-    // digits: [T][chunks_in][512], [slots][chunks_out][512]; 16 bits: [T][chunks_in][256], [slots or 2 slots][chunks_out][256]
+    // digits: [T][chunks_in][512], [slots][chunks_out][512]; 16 bits: [T][chunks_in][256], [slots][chunks_out][512]
     uint8_t *x, *mid_rows;
     float *mid;                       // [slots][128 chunks_out]
     float *part;                      // 16 bits: [slots][H], what a slot adds to its token (where mid was)
@@ -46,7 +46,7 @@ struct MoeParams {
     uint32_t units_in, units_in_inv, units_out, units_out_inv;
     int odd, act, y_type;
     int rows;                                // slots of a group: 4 (digits), 8 or 16 (16 bits)
-    int split, scaled;                       // 16 bits: mid as two numbers; x, in bf16, as fp16 times a power of two
+    int scaled;                              // 16 bits: x, in bf16, as fp16 times a power of two
     // No call has more groups: blocks are launched for so many (as many as experts, each taking several groups in turn where
     // all tokens go to few experts: 64 tokens, one expert of 2048 to 768, 69 us, with all at once 23; three of 11, 75 and 55).
     int groups_most() const { const int most = E + slots / rows; return slots < most ? slots : most; }

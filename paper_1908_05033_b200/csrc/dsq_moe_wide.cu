@@ -8,13 +8,16 @@
 //     operand's order: products are exact and added in binary32.  Rows of bf16 go as fp16 times a power of two where no code is
 //     0: exact down to 2^-32 of a token's largest element, off by 2^-41 of it below, far below the sums' rounding
 //     (16 tokens of 4096 to 1024, four of 64 experts: 81 us with twelve operations a word, 73.6 with ten).
-//   * mid, in binary32 first, goes as fp16 on a power of two of its own for each slot, its largest below 2^15: 11 bits
-//     where y is bf16 (8 bits), as two numbers and 22 bits where y is more.
+//   * mid, in binary32 first, goes as two fp16 numbers, 22 bits, on a power of two of its own for each slot, its largest below
+//     2^15; they are two rows of elements, so that four slots fill an instruction's columns there.  (One number, 11 bits, is 16 us
+//     faster below, but Y then shows its rounding wherever a residual takes most of the sum away, and other numbers of tokens in a
+//     call, which go on digits, change Y by as much.)
 //   * moe_wide_kernel does both products: a block has 4 warps side by side on 32 columns each (16 of gate and
 //     other half; or 32 of y) and 2 along K; the warps' sums are added in a fixed order.  What each slot adds to its
 //     token goes to the workspace, moe_combine_kernel adds it slot by slot.
-// 64 tokens of 4096 to 2048, four of 32 experts (429 MB of codes and scales): 134 us, 3.2 TB/s: issue slots 50 to 55 %, with
-// four warps a scheduler (registers) that wait for copies and for one another; 3.5 waves of blocks.
+// 64 tokens of 4096 to 2048, four of 32 experts (429 MB of codes and scales): 150 us, 2.9 TB/s.  No unit is saturated (issue slots
+// 53 % and 40 %, tensor pipe 26 % and 30 %, DRAM 42 % and 25 % of the two products): four warps a scheduler (128 registers)
+// do not cover the loads of their rows from L1 and the chains of products; without those loads the second product takes two thirds.
 #include "dsq_moe.cuh"
 
 using namespace dsq_moe;
@@ -129,7 +132,7 @@ template <bool WHOLE> __global__ void __launch_bounds__(256) moe_wide_mid_kernel
         }
     }
     const float by = block_scale(m, bad, p.w.mid_step + slot);
-    uint8_t *rows = p.w.mid_rows + (int64_t)slot * p.chunks_out * 256 * (p.split ? 2 : 1);
+    uint8_t *rows = p.w.mid_rows + (int64_t)slot * p.chunks_out * 512;
     for (int i = threadIdx.x; i < words; i += 256) {
         const float4 a = reinterpret_cast<const float4 *>(mid)[2 * i], b = reinterpret_cast<const float4 *>(mid)[2 * i + 1];
         const float f[4][2] = {{a.x, b.x}, {a.y, b.y}, {a.z, b.z}, {a.w, b.w}};
@@ -143,9 +146,11 @@ template <bool WHOLE> __global__ void __launch_bounds__(256) moe_wide_mid_kernel
             hi[k] = *reinterpret_cast<const uint32_t *>(&h);
             lo[k] = *reinterpret_cast<const uint32_t *>(&l);
         }
-        uint8_t *to = rows + (int64_t)(i >> 4) * 256 + place_of<WHOLE>(i & 15);
+        // (a line for the words of four lanes: 64 bytes of first numbers, 64 of second ones)
+        const int place = place_of<WHOLE>(i & 15);
+        uint8_t *to = rows + (int64_t)(i >> 4) * 512 + (place >> 6) * 128 + (place & 63);
         *reinterpret_cast<uint4 *>(to) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-        if (p.split) *reinterpret_cast<uint4 *>(to + (int64_t)p.chunks_out * 256) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+        *reinterpret_cast<uint4 *>(to + 64) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
     }
 }
 
@@ -263,7 +268,58 @@ __device__ __forceinline__ void multiply(uint32_t at, const Unpack<XT> &unpack, 
     }
 }
 
-// TILES: of eight rows of elements (slots; OUT and p.split: a slot's two numbers)
+// The same of slots whose elements are two numbers each, the first in row 2 i of a tile of four slots, the second in row 2 i + 1: a lane
+// has both sums of slot j, and adds them.  Elements come word by word, one ahead: pieces[q & 1] has those of word q when
+// its turn comes, fetch(q, to) brings those of word q (4: the next chunk's word 0).
+template <int TILES> struct Piece { uint4 x[TILES]; };
+template <int XT, int TILES, int GP, class F>
+__device__ __forceinline__ void multiply_both(uint32_t at, const Unpack<XT> &unpack, Piece<TILES> (&pieces)[2], DsqPair (&total)[2][TILES], F fetch)
+{
+    const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
+    const uint32_t as = at + Stage<NT, GP>::W_BYTES + n * 4;
+    uint32_t w[4][4];
+    if (GP == 4) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const uint4 v = lds_128(at + t * 512 + n * 64 + ((j ^ (n >> 1)) & 3) * 16);
+            w[t][0] = v.x; w[t][1] = v.y; w[t][2] = v.z; w[t][3] = v.w;
+        }
+    }
+    float acc[2][TILES][4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        fetch(q + 1, pieces[(q + 1) & 1]);
+        const Piece<TILES> &r = pieces[q & 1];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t a[2][4];
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                uint32_t v[4];
+                if (GP != 4) w[2 * h + s][q] = lds_32(at + (2 * h + s) * 512 + n * 64 + ((q ^ (n >> 1)) & 3) * 16 + 4 * j);
+                unpack(w[2 * h + s][q], v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) a[i >> 1][(i & 1) * 2 + s] = v[i];
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s)
+#pragma unroll
+                for (int m = 0; m < TILES; ++m) {
+                    const uint32_t b0 = s ? r.x[m].z : r.x[m].x, b1 = s ? r.x[m].w : r.x[m].y;
+                    if (q % GP == 0 && s == 0) mma_first<XT>(acc[h][m], a[s], b0, b1);
+                    else mma<XT>(acc[h][m], a[s], b0, b1);
+                }
+            if (q % GP == GP - 1) {
+                const uint32_t from = as + (q / GP * NT * 8 + 16 * h) * 4;
+                const DsqPair scales = dsq_pair_of(__uint_as_float(lds_32(from)), __uint_as_float(lds_32(from + 32)));
+#pragma unroll
+                for (int m = 0; m < TILES; ++m)
+                    total[h][m] = dsq_pair_fma(dsq_pair_of(acc[h][m][0] + acc[h][m][1], acc[h][m][2] + acc[h][m][3]), scales, total[h][m]);
+            }
+        }
+    }
+}
+
 template <bool OUT, int XT, int GP> struct Wide {
     using S = Stage<NT, GP>;
     static constexpr int RING = WARPS * STAGES * S::BYTES, SUMS = WARPS * 2 * 2 * 512;
@@ -308,22 +364,39 @@ template <bool OUT, int XT, int GP> struct Wide {
         cp_async_commit();
     }
 
-    template <int TILES> __device__ __forceinline__ void run()
+    // this warp's turns: codes of each as they come
+    template <class F> __device__ __forceinline__ void each_turn(F f)
+    {
+#pragma unroll 1
+        for (int i = 0; i < turns; ++i) {
+            cp_async_wait<STAGES - 2>();
+            __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
+            issue();
+            f(i, ring + (uint32_t)(i % STAGES * S::BYTES));
+        }
+        cp_async_wait<0>();
+        __syncthreads();
+    }
+    // (a line a lane into L1, ahead of the loads, which would wait for L2 with every register taken; rows of `lines` lines a chunk)
+    template <int TILES> __device__ __forceinline__ void touch(const uint8_t *(&x)[TILES], int chunk, int lines) const
+    {
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+            if (x[m] && j < lines) {
+                uint32_t none;
+                asm volatile("ld.global.u32 %0, [%1];" : "=r"(none) : "l"(x[m] + (int64_t)chunk * 128 * lines + j * 112));
+            }
+    }
+
+    // the first product of up to 8 TILES slots
+    template <int TILES> __device__ __forceinline__ void run_in()
     {
         const Unpack<XT> unpack(p.odd);
-        const bool split = OUT && p.split;
         const uint8_t *x[TILES];
         Elements<TILES> r = {};
 #pragma unroll
-        for (int m = 0; m < TILES; ++m) {
-            const int i = 8 * m + n, of = split ? i >> 1 : i;
-            x[m] = nullptr;
-            if (of < slots) {
-                const int slot = group->slot[of];
-                if (OUT) x[m] = p.w.mid_rows + (int64_t)(split ? 2 * slot + (i & 1) : slot) * chunks * 256 + 16 * j;
-                else x[m] = p.w.x + (int64_t)(slot / p.k) * chunks * 256 + 16 * j;
-            }
-        }
+        for (int m = 0; m < TILES; ++m)
+            x[m] = 8 * m + n < slots ? p.w.x + (int64_t)(group->slot[8 * m + n] / p.k) * chunks * 256 + 16 * j : nullptr;
         // (rows of no slot stay zeros)
         auto load = [&](int chunk) {
 #pragma unroll
@@ -333,30 +406,15 @@ template <bool OUT, int XT, int GP> struct Wide {
                     for (int q = 0; q < 4; ++q) r.x[m][q] = load_16(x[m] + (int64_t)chunk * 256 + 64 * q);
                 }
         };
-        // (a line a lane into L1, ahead of the loads, which would wait for L2 with every register taken)
-        auto touch = [&](int chunk) {
-#pragma unroll
-            for (int m = 0; m < TILES; ++m)
-                if (x[m] && j < 2) {
-                    uint32_t none;
-                    asm volatile("ld.global.u32 %0, [%1];" : "=r"(none) : "l"(x[m] + (int64_t)chunk * 256 + j * 112));
-                }
-        };
         if (turns > 0) load(wk);
-        if (turns > 1) touch(wk + KW);
+        if (turns > 1) touch(x, wk + KW, 2);
         DsqPair total[2][TILES][2] = {};
-#pragma unroll 1
-        for (int i = 0; i < turns; ++i) {
-            cp_async_wait<STAGES - 2>();
-            __syncwarp();             // every lane's copies of this stage are here, and the last stage has been read
-            issue();
-            multiply<XT, TILES, GP>(ring + (uint32_t)(i % STAGES * S::BYTES), unpack, r, total);
+        each_turn([&](int i, uint32_t at) {
+            multiply<XT, TILES, GP>(at, unpack, r, total);
             if (i + 1 < turns) load(wk + (i + 1) * KW);
-            if (i + 2 < turns) touch(wk + (i + 2) * KW);
-        }
+            if (i + 2 < turns) touch(x, wk + (i + 2) * KW, 2);
+        });
         // the warps' sums, added in a fixed order
-        cp_async_wait<0>();
-        __syncthreads();
         ulonglong2 *part = reinterpret_cast<ulonglong2 *>(smem);       // [WARPS][2][TILES][32]
 #pragma unroll
         for (int h = 0; h < 2; ++h)
@@ -366,7 +424,7 @@ template <bool OUT, int XT, int GP> struct Wide {
         __syncthreads();
         const float unit = dsq_value_unit<XT>(p.odd);
         const float *sums = reinterpret_cast<const float *>(smem);
-        // the sum of row i of elements and column c of half h of the wc-th warp's
+        // the sum of slot i and column c of half h of the wc-th warp's
         auto sum = [&](int wc, int h, int c, int i) {
             const int at = ((h * TILES + (i >> 3)) * 32 + (c & 7) * 4 + ((i & 7) >> 1)) * 4 + 2 * (c >> 3) + (i & 1);
             float v = 0.f;
@@ -374,30 +432,68 @@ template <bool OUT, int XT, int GP> struct Wide {
             for (int w = 0; w < KW; ++w) v += sums[(w * WC + wc) * 2 * TILES * 128 + at];
             return v;
         };
-        if (OUT) {
-            for (int e = threadIdx.x; e < slots * WC * 32; e += THREADS) {
-                const int s = e / (WC * 32), c = e % (WC * 32), col = blockIdx.x * WC * 32 + c, wc = c >> 5, h = c >> 4 & 1;
-                if (col >= p.H) continue;
-                const float v = split ? sum(wc, h, c & 15, 2 * s) + sum(wc, h, c & 15, 2 * s + 1) : sum(wc, h, c & 15, s);
-                const int slot = group->slot[s];
-                p.w.part[(int64_t)slot * p.H + col] = v * unit * p.w.mid_step[slot] * p.weights[slot];
-            }
-        } else {
-            for (int e = threadIdx.x; e < slots * WC * 16; e += THREADS) {
-                const int s = e / (WC * 16), c = e % (WC * 16), col = blockIdx.x * WC * 16 + c;
-                if (col >= chunks_of_mid()) continue;
-                // (columns behind the last are zeros up to the end of the chunk)
-                const int slot = group->slot[s];
-                const float of_x = p.scaled ? unit * p.w.x_step[slot / p.k] : unit;
-                const float gate = sum(c >> 4, 0, c & 15, s) * of_x, up = sum(c >> 4, 1, c & 15, s) * of_x;
-                p.w.mid[(int64_t)slot * chunks_of_mid() + col] = col < p.I ? activated(gate, p.act) * up : 0.f;
-            }
+        for (int e = threadIdx.x; e < slots * WC * 16; e += THREADS) {
+            const int s = e / (WC * 16), c = e % (WC * 16), col = blockIdx.x * WC * 16 + c;
+            if (col >= chunks_of_mid()) continue;
+            // (columns behind the last are zeros up to the end of the chunk)
+            const int slot = group->slot[s];
+            const float of_x = p.scaled ? unit * p.w.x_step[slot / p.k] : unit;
+            const float gate = sum(c >> 4, 0, c & 15, s) * of_x, up = sum(c >> 4, 1, c & 15, s) * of_x;
+            p.w.mid[(int64_t)slot * chunks_of_mid() + col] = col < p.I ? activated(gate, p.act) * up : 0.f;
+        }
+        __syncthreads();
+    }
+
+    // the second product of up to 4 TILES slots
+    template <int TILES> __device__ __forceinline__ void run_out()
+    {
+        const Unpack<XT> unpack(p.odd);
+        const uint8_t *x[TILES];
+        Piece<TILES> pieces[2] = {};
+#pragma unroll
+        for (int m = 0; m < TILES; ++m)
+            x[m] = 4 * m + (n >> 1) < slots ? p.w.mid_rows + (int64_t)group->slot[4 * m + (n >> 1)] * chunks * 512 + 64 * (n & 1) + 16 * j : nullptr;
+        // (rows of no slot stay zeros)
+        auto fetch = [&](int chunk, int q, Piece<TILES> &to) {
+#pragma unroll
+            for (int m = 0; m < TILES; ++m)
+                if (x[m]) to.x[m] = load_16(x[m] + (int64_t)chunk * 512 + 128 * q);
+        };
+        if (turns > 0) fetch(wk, 0, pieces[0]);
+        if (turns > 1) touch(x, wk + KW, 4);
+        DsqPair total[2][TILES] = {};
+        each_turn([&](int i, uint32_t at) {
+            multiply_both<XT, TILES, GP>(at, unpack, pieces, total, [&](int q, Piece<TILES> &to) {
+                if (q < 4) fetch(wk + i * KW, q, to);
+                else if (i + 1 < turns) fetch(wk + (i + 1) * KW, 0, to);
+            });
+            if (i + 2 < turns) touch(x, wk + (i + 2) * KW, 4);
+        });
+        // the warps' sums, added in a fixed order
+        DsqPair *part = reinterpret_cast<DsqPair *>(smem);             // [WARPS][2][TILES][32]
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int m = 0; m < TILES; ++m) part[((warp * 2 + h) * TILES + m) * 32 + lane] = total[h][m];
+        __syncthreads();
+        const float unit = dsq_value_unit<XT>(p.odd);
+        const float *sums = reinterpret_cast<const float *>(smem);
+        for (int e = threadIdx.x; e < slots * WC * 32; e += THREADS) {
+            const int s = e / (WC * 32), c = e % (WC * 32), col = blockIdx.x * WC * 32 + c, wc = c >> 5, h = c >> 4 & 1;
+            if (col >= p.H) continue;
+            const int at = ((h * TILES + (s >> 2)) * 32 + (c & 7) * 4 + (s & 3)) * 2 + (c >> 3 & 1);
+            float v = 0.f;
+#pragma unroll
+            for (int w = 0; w < KW; ++w) v += sums[(w * WC + wc) * 2 * TILES * 64 + at];
+            const int slot = group->slot[s];
+            p.w.part[(int64_t)slot * p.H + col] = v * unit * p.w.mid_step[slot] * p.weights[slot];
         }
         __syncthreads();
     }
     __device__ __forceinline__ int chunks_of_mid() const { return p.chunks_out * 128; }
 };
 
+// MOST: eights of slots of a group
 template <bool OUT, int XT, int GP, int MOST>
 __global__ void __launch_bounds__(THREADS, MOST == 1 ? 3 : 2) moe_wide_kernel(const __grid_constant__ MoeParams p)
 {
@@ -439,8 +535,15 @@ __global__ void __launch_bounds__(THREADS, MOST == 1 ? 3 : 2) moe_wide_kernel(co
             grid_launch_dependents();
             waited = true;
         }
-        if (MOST == 1 || (OUT && p.split ? 2 : 1) * slots <= 8) w.template run<1>();
-        else w.template run<MOST>();
+        if (OUT) {
+            if (slots <= 4) w.template run_out<1>();
+            else if (MOST == 1 || slots <= 8) w.template run_out<2>();
+            else if (slots <= 12) w.template run_out<3>();
+            else w.template run_out<4>();
+        } else {
+            if (MOST == 1 || slots <= 8) w.template run_in<1>();
+            else w.template run_in<2>();
+        }
     }
     if (!waited) {
         grid_dependency_wait();
@@ -486,7 +589,7 @@ template <bool OUT, int XT, int GP, int MOST> int launch(const MoeParams &p, cud
 }
 template <bool OUT, int XT> int pick(const MoeParams &p, int gp, cudaStream_t s)
 {
-    if ((OUT && p.split ? 2 : 1) * p.rows == 8)
+    if (p.rows == 8)
         return gp == 4 ? launch<OUT, XT, 4, 1>(p, s) : gp == 2 ? launch<OUT, XT, 2, 1>(p, s) : launch<OUT, XT, 1, 1>(p, s);
     return gp == 4 ? launch<OUT, XT, 4, 2>(p, s) : gp == 2 ? launch<OUT, XT, 2, 2>(p, s) : launch<OUT, XT, 1, 2>(p, s);
 }
