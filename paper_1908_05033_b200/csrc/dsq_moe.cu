@@ -100,18 +100,18 @@ template <int ITEMS> __global__ void __launch_bounds__(128) route_kernel(const R
             my_id = last_at;
         }
     }
-    // (of a row of nothing but -infinity: 0)
-    const bool none = first == __uint_as_float(0xFF800000u);
-    float e = lane < p.k ? expf(mine - first) : 0.f, sum = e;
+    // (where the largest is -infinity: less 0, which leaves sums of 0, or of a NaN below it)
+    const float base = first == __uint_as_float(0xFF800000u) ? 0.f : first;
+    float e = lane < p.k ? expf(mine - base) : 0.f, sum = e;
     if (!p.renormalise) {
         sum = 0.f;
-        for (int i = lane; i < p.E; i += 32) sum += expf(row[i] - first);
+        for (int i = lane; i < p.E; i += 32) sum += expf(row[i] - base);
     }
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(~0u, sum, o);
     if (lane < p.k) {
         p.ids[t * p.k + lane] = my_id;
-        p.weights[t * p.k + lane] = none ? 0.f : e / sum;
+        p.weights[t * p.k + lane] = sum == 0.f ? 0.f : e / sum;
     }
 }
 
