@@ -474,7 +474,7 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
  * and the `top` largest of a row in order, equal ones by index, the lowest first.
  *   dtype     DSQ_F32, DSQ_BF16 or DSQ_F16
  *   targets   int64 [M] (needed for logp): a negative one is none (logp 0), one of V or more gives NaN
- *   scale     positive and finite (an inverse temperature), DSQ_ERR_RANGE otherwise
+ *   scale     positive, at most 2^127 (an inverse temperature), DSQ_ERR_RANGE otherwise
  *   top       0 to 32 (DSQ_ERR_UNSUPPORTED beyond) and at most V; 0 just where top_ids and top_logp
  *             are NULL (DSQ_ERR_SHAPE)
  *   logp, entropy, lse  fp32 [M], top_ids int64 [M][top], top_logp fp32 [M][top]: any may be NULL

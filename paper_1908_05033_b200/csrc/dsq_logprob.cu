@@ -36,6 +36,8 @@ constexpr int SLOTS = 16, HITS = 512;      // turns that are told apart, and how
 constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 // 2^x of what is lower is zero
 constexpr float NOTHING = -1000.f;
+// times log2 e it is finite
+constexpr float MAX_SCALE = 0x1p127f;
 // M is taken below this: its rounding is at most 2^-8 then
 constexpr float FAR = 65536.f;
 
@@ -644,7 +646,7 @@ int check_rows(int64_t M, int64_t V, int64_t ld, int dtype, float scale)
     if (!dsq_is_float_type(dtype)) return DSQ_ERR_UNSUPPORTED;
     if (M <= 0 || V <= 0 || ld < V) return DSQ_ERR_SHAPE;
     if (V > 1 << 30 || M > 1 << 28) return DSQ_ERR_SIZE;
-    if (!dsq_finite(scale) || scale <= 0.f) return DSQ_ERR_RANGE;
+    if (!(scale > 0.f && scale <= MAX_SCALE)) return DSQ_ERR_RANGE;
     return DSQ_OK;
 }
 
