@@ -453,7 +453,8 @@ int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
  *   grad_weight  fp32 [head_dim] or NULL
  *   workspace    dsq_headnorm_bwd_workspace_bytes(head_dim) bytes (DSQ_ERR_SIZE otherwise); not
  *                needed without grad_weight.  Scratch: calls that may overlap must not share it.
- * Sums are binary32 in a fixed order: the same call gives the same bits on the same GPU. */
+ * Sums are binary32 in a fixed order: the same call gives the same bits on the same GPU.  Heads whose squares or
+ * whose products with grad_y leave binary32's range are done in binary64. */
 typedef struct dsq_heads_grad_t {
     const void *grad_y, *x;
     const float *weight;

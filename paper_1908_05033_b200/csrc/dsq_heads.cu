@@ -155,6 +155,9 @@ template <int L> __device__ __forceinline__ float lanes_sum(float v, int lanes)
 }
 // squares, and what is divided by their root, are inside binary32's range
 __device__ __forceinline__ bool in_range(float mean) { return mean > 1e-28f && mean < 1e36f; }
+// Backwards, too, the products of the gradient and x: c is their mean over the root.  (Finite sums leave every product finite; what
+// products lose below 2^-149 is, times rstd below 10^4, below the rounding of gradients from 2^-108 on.)
+__device__ __forceinline__ bool in_range(float mean, float c) { return mean > 1e-8f && mean < 1e36f && fabsf(c) < 1e36f; }
 
 // A head whose squares are not: by a whole warp in binary64, element by element.  `sums`: the warp's
 // sums of the weight's gradient.  Every pair is read and written by one lane.
@@ -560,14 +563,14 @@ __global__ void __launch_bounds__(BLOCK, 2 * U * VEC > 16 ? 2 : BACK_BLOCKS) hea
                 }
                 const float sum = lanes_sum<L_>(sum_of(sum2), lanes), dot = lanes_sum<L_>(sum_of(dot2), lanes);
                 const float mean = __fmaf_rn(sum, p.inv_d, p.eps), rstd = rsqrtf(mean);
-                const bool bad = on && !in_range(mean);
+                const float c = dot * rstd * p.inv_d;
+                const bool bad = on && !in_range(mean, c);
                 if (bad) {
                     if (lane == 0) bad_heads[(at.head - at.begin) >> 5] |= 1u << ((at.head - at.begin) & 31);
                     any = true;
                     on = false;
                 }
                 if (on) {
-                    const float c = dot * rstd * p.inv_d;
                     const DsqPair r = dsq_pair_of(rstd, rstd), less = dsq_pair_of(-c, -c);
 #pragma unroll
                     for (int k = 0; k < L::P; ++k) {
