@@ -707,14 +707,15 @@ template <class T, int VEC, int U, bool INTER, int L, bool BACK> int launch(Para
     const int pdl = dsq_launch_hooks().pdl;
     const int64_t sms = dsq_sm_count() > 0 ? dsq_sm_count() : 148, per_block = BLOCK / p.lanes;
     if constexpr (!BACK) {
-        // heads enough for the teams of a warp to share a token's
+        // heads enough for the teams of a warp to share a token's (a lane has more units just where 32 are too few)
+        constexpr bool TEAMS = VEC == 1 ? U <= 2 : U == 1;
         const int heads = p.t[0].heads + p.t[1].heads;
-        const bool warp = p.lanes < 32 && heads >= 2 * (32 / p.lanes);
+        const bool warp = TEAMS && p.lanes < 32 && heads >= 2 * (32 / p.lanes);
         const int64_t items = warp ? BLOCK / 32 : per_block;
         set_parts(p.t[0], p.tokens, heads, sms * 5 * items, warp ? 32 / p.lanes : 1, (int)per_block);
         const int64_t blocks = (p.tokens * p.t[0].parts + items - 1) / items;
         if (blocks > 0x7FFFFFFF) return DSQ_ERR_SIZE;
-        const auto kernel = warp ? heads_fwd_kernel<T, VEC, U, INTER, L, true> : heads_fwd_kernel<T, VEC, U, INTER, L, false>;
+        const auto kernel = warp ? heads_fwd_kernel<T, VEC, U, INTER, L, TEAMS> : heads_fwd_kernel<T, VEC, U, INTER, L, false>;
         return dsq_launch(kernel, dim3((unsigned)blocks), dim3(BLOCK), 0, s, pdl, 0, p);
     } else {
         // what is resident together, shared among q and k as their tokens' costs are (set_parts)
