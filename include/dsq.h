@@ -483,7 +483,8 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
  * lse -infinity, entropy 0 and log probabilities -infinity.  A NaN or +infinity makes its row's numbers
  * NaN; top_ids takes NaN to be below all.  Arithmetic is binary32.  Data need the alignment of their
  * elements only (this and the next function).  V at most 2^30, M at most 2^28 (DSQ_ERR_SIZE).
- * HBM-bound: the logits are read once. */
+ * HBM-bound: the logits are read once; a row that is one value for the most part is read again up to where `top` of it
+ * are found, one whose largest elements are many, different and all in the same few vectors of a block's turns up to `top` times. */
 int dsq_logprob_fwd(const void *logits, int64_t ld, int64_t M, int64_t V, int dtype,
                     const int64_t *targets, float scale, int top, float *logp,
                     float *entropy, float *lse, int64_t *top_ids, float *top_logp,

@@ -16,7 +16,11 @@
 //     threads form groups; the top-th of the groups' largest elements bounds from below what can be among the
 //     first `top`, and only turns whose largest is above the bound are read again (from L2), by as many threads as
 //     they have vectors; what passes goes to shared memory, where ranks are counted.  Order and ties are those of
-//     (value, lowest index), as one 64-bit key.
+//     (value, lowest index), as one 64-bit key.  Where the bound is the value of most elements (a mask that leaves fewer groups than
+//     `top` anything) the elements above it are collected alone and its lowest indices fill up behind them, in a scan that ends
+//     with the turn that has enough: 2048 rows of 128000 bf16 with three left, 20 alternatives, 152 us (111 without a
+//     mask; the largest `top` times one after the other 3790).  That is left for rows whose large elements are many,
+//     different and all with the same few threads.
 //   4096 rows of 128000 bf16 with five alternatives: 198 us, 5.3 TB/s (issue slots 60 %, nine instructions an element in
 //   all); without alternatives or with 32000 columns what follows a row's pass weighs more (56 us, 4.6 TB/s).  One row: 9.5 us, a
 //   chain of a load, three barriers, a second load of a few vectors and the cluster's exchange.
@@ -202,6 +206,127 @@ template <int THREADS, class F> __device__ __forceinline__ void ranked(const uns
 __device__ __forceinline__ void st_cluster_64(uint32_t addr, unsigned long long v)
 {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
+}
+
+// What a block has of a row for its alternatives.
+template <class T> struct Part {
+    Cut<T> cut;
+    int v0, v1, singles;              // its vectors, how many single elements
+    int turns, per_slot;
+    const float *slot_most;
+    uint32_t *hit;
+    unsigned long long *found;
+    int *hits, *count;
+};
+
+// The vectors of the turns whose largest element passes, f(element, index) for each, a thread a vector; f(...) for the single ones
+// too.  False where there are more turns than there is room for.  (*hits and *count are 0, and every thread knows.)
+template <class T, int THREADS, class P, class F>
+__device__ __forceinline__ bool look_again(const Part<T> &a, P passes, F f)
+{
+    constexpr int VEC = vec_of<T>();
+    const int tid = threadIdx.x;
+    if (tid < a.singles) f(dsq_to_f32(a.cut.row[a.cut.single(tid)]), a.cut.single(tid));
+    for (int i = 0; i * a.per_slot < a.turns; ++i) {
+        if (a.v0 + i * a.per_slot * AHEAD * THREADS + tid >= a.v1) break;
+        if (!passes(a.slot_most[i * THREADS + tid])) continue;
+        const int at = atomicAdd(a.hits, 1);
+        if (at < HITS) a.hit[at] = (uint32_t)tid | (uint32_t)i << 16;
+    }
+    __syncthreads();
+    const int per_hit = a.per_slot * AHEAD, n_hits = *a.hits;
+    if (n_hits > HITS) return false;
+    for (int64_t w = tid; w < (int64_t)n_hits * per_hit; w += THREADS) {
+        const int h = (int)(w / per_hit), k = (int)(w - (int64_t)h * per_hit);
+        const int64_t v = a.v0 + ((int64_t)(a.hit[h] >> 16) * per_hit + k) * THREADS + (a.hit[h] & 0xFFFFu);
+        if (v >= a.v1) continue;
+        float e[VEC];
+        values<T>(load_16(a.cut.row + a.cut.head + v * VEC), e);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) f(e[i], a.cut.index((int)v) + i);
+    }
+    return true;
+}
+
+// The first `top` where most elements are equal to the bound (a mask's value; a row of one value): those above it, of
+// which there are fewer, and behind them the lowest indices of equal ones, in one scan that ends with the turn that has enough.
+// `masked`: the bound is LOWEST or below, and behind LOWEST come -infinity and NaN.  *count: of the candidates in `found`,
+// beyond ROOM where there is no room for those above.
+template <class T, int THREADS> __device__ __forceinline__ void take_equal(const Part<T> &a, int top, float least, bool masked)
+{
+    constexpr int VEC = vec_of<T>();
+    const int tid = threadIdx.x, lane = tid & 31;
+    const float none = __uint_as_float(0xFF800000u);
+    if (masked) {
+        // (a slot's largest tells whether LOWEST is a mask; single ones of it between larger elements are found with these)
+        bool low = false;
+        for (int i = 0; i * a.per_slot < a.turns; ++i) {
+            if (a.v0 + i * a.per_slot * AHEAD * THREADS + tid >= a.v1) break;
+            low = low || a.slot_most[i * THREADS + tid] == LOWEST;
+        }
+        least = __syncthreads_or(low) ? LOWEST : none;
+    }
+    __syncthreads();                                           // (*hits and *count have been read)
+    if (tid == 0) *a.hits = *a.count = 0;
+    __syncthreads();
+    auto add = [&](float v, int index) {
+        const int at = atomicAdd(a.count, 1);
+        if (at < ROOM) a.found[at] = key_of(v, index);
+    };
+    const bool room = look_again<T, THREADS>(a, [&](float most) { return most > least; }, [&](float v, int index) {
+        if (v > least) add(v, index);
+    });
+    __syncthreads();
+    if (!room) {
+        if (tid == 0) *a.count = ROOM + 1;
+        __syncthreads();
+        return;
+    }
+    int have = *a.count;
+    for (;;) {                                                 // least: NaN in the end
+        __syncthreads();                                       // (everybody has read *count)
+        if (have >= top) return;
+        auto equal = [&](float v) { return least != least ? v != v : v == least; };
+        auto single = [&](int from, int to) {
+            if (tid >= from && tid < to) {
+                const float v = dsq_to_f32(a.cut.row[a.cut.single(tid)]);
+                if (equal(v)) add(v, a.cut.single(tid));
+            }
+            __syncthreads();
+            have = *a.count;
+            __syncthreads();
+        };
+        if (a.singles > 0) single(0, a.cut.head);
+        for (int v0 = a.v0; v0 < a.v1 && have < top; v0 += THREADS) {
+            float e[VEC];
+            uint32_t mine = 0u;
+            if (v0 + tid < a.v1) {
+                values<T>(load_16(a.cut.row + a.cut.head + (int64_t)(v0 + tid) * VEC), e);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) mine |= equal(e[i]) ? 1u << i : 0u;
+            }
+            // the warp's first ones, as many as are still wanted
+            int before = __popc(mine);
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(~0u, before, o);
+                if (lane >= o) before += v;
+            }
+            const int wanted = min(__shfl_sync(~0u, before, 31), top - have);
+            before -= __popc(mine);
+            int at = 0;
+            if (lane == 0 && wanted > 0) at = atomicAdd(a.count, wanted);
+            at = __shfl_sync(~0u, at, 0);
+            for (; mine && before < wanted; mine &= mine - 1, ++before)
+                a.found[at + before] = key_of(least, a.cut.index(v0 + tid) + __ffs(mine) - 1);
+            __syncthreads();
+            have = *a.count;
+            __syncthreads();
+        }
+        if (a.singles > 0 && have < top) single(a.cut.head, a.singles);
+        if (!masked || least != least) return;
+        least = least == LOWEST ? none : __uint_as_float(0x7FC00000u);
+    }
 }
 
 template <class T, bool TOP, int THREADS>
@@ -398,37 +523,23 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
         }
         __syncthreads();
         const unsigned long long bound = bound_key;
-        auto keep = [&](float v, int index) {
-            const unsigned long long key = key_of(v, index);
-            if (key < bound) return;
-            const int at = atomicAdd(&count, 1);
-            if (at < ROOM) found[at] = key;
-        };
-        if (tid < singles) keep(dsq_to_f32(cut.row[cut.single(tid)]), cut.single(tid));
-        // turns that may have some, and their vectors, a thread each
-        const bool any_value = bound >> 32 == 0ull;
+        const Part<T> part = {cut, v0, v1, singles, turns, per_slot, slot_most, hit, found, &hits, &count};
+        // turns that may have some, and their vectors, a thread each (no bound: all)
+        const bool masked = bound != 0ull && bound >> 32 == 0ull;
         const float least = value_of(bound);
-        for (int i = 0; i * per_slot < turns; ++i) {
-            if (v0 + i * per_slot * AHEAD * THREADS + tid >= v1) break;
-            if (!any_value && !(slot_most[i * THREADS + tid] >= least)) continue;
-            const int at = atomicAdd(&hits, 1);
-            if (at < HITS) hit[at] = (uint32_t)tid | (uint32_t)i << 16;
+        bool room = false;
+        if (!masked) {
+            room = look_again<T, THREADS>(part, [&](float most) { return bound == 0ull || most >= least; }, [&](float v, int index) {
+                const unsigned long long key = key_of(v, index);
+                if (key < bound) return;
+                const int at = atomicAdd(&count, 1);
+                if (at < ROOM) found[at] = key;
+            });
+            __syncthreads();
+            room = room && count <= ROOM;
         }
-        __syncthreads();
-        const int per_hit = per_slot * AHEAD, n_hits = hits;
-        if (n_hits > HITS) {
-            if (tid == 0) count = ROOM + 1;                    // (more than there is room for)
-        } else {
-            for (int64_t w = tid; w < (int64_t)n_hits * per_hit; w += THREADS) {
-                const int h = (int)(w / per_hit), k = (int)(w - (int64_t)h * per_hit);
-                const int64_t v = v0 + ((int64_t)(hit[h] >> 16) * per_hit + k) * THREADS + (hit[h] & 0xFFFFu);
-                if (v >= v1) continue;
-                float f[VEC];
-                values<T>(load_16(vecs + v * VEC), f);
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) keep(f[i], cut.index((int)v) + i);
-            }
-        }
+        if (!room && bound != 0ull) take_equal<T, THREADS>(part, p.top, least, masked);
+        else if (!room && tid == 0) count = ROOM + 1;
     }
     __syncthreads();
     if (p.cluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
@@ -460,7 +571,7 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) logprob_fwd_kernel(co
                 if (at < p.top) put(at, key);
             });
         } else {
-            // More than there is room for (many large elements, and all with the same few threads): one after
+            // More than there is room for (many different large elements, and all with the same few threads): one after
             // the other, the largest below the one before.
             unsigned long long last = ~0ull;
             for (int i = 0; i < p.top; ++i) {
