@@ -532,8 +532,9 @@ typedef enum dsq_activation { DSQ_SILU = 0, DSQ_GELU_TANH = 1 } dsq_activation;
  * Made for few tokens: up to 64 share a pass over the weights of the experts they chose; more take several.
  * Sums are binary32 in a fixed order: the same call gives the same bits on the same GPU.  x and mid are
  * kept to 2^-31 of the power of two above the largest of their 128 neighbours where a call has few slots for its
- * experts; else x to 2^-40 of the token's largest (exact as DSQ_F16, and with w_offset = 0), mid to 22 bits.  Y is rounded once.  A token with a NaN or an infinity is NaN and does not touch the
- * others.
+ * experts; else x to 2^-39 of the token's largest (exact as DSQ_F16, and with w_offset = 0), mid to 22 bits of itself or
+ * 2^-39 of the largest beside it, both to 2^-151 where that is more.  Y is rounded once.  A token with a NaN or an
+ * infinity is NaN and does not touch the others.
  * k at most 32, E at most 1024, H and I at most 2^20, T at most 2^20 (DSQ_ERR_SIZE). */
 size_t dsq_moe_workspace_bytes(int64_t T, int64_t H, int64_t I, int k);
 int dsq_moe_group(const void *X, int x_type, const int32_t *ids, const float *weights,

@@ -6,7 +6,7 @@
 //     (half the registers of digits) and sums of 16 columns by 8 slots in four registers.
 //   * Codes become bf16 or fp16 pairs, x is rearranged once, so that 16 bytes are a word's elements in the
 //     operand's order: products are exact and added in binary32.  Rows of bf16 go as fp16 times a power of two where no code is
-//     0: exact down to 2^-32 of a token's largest element, off by 2^-41 of it below, far below the sums' rounding
+//     0: exact down to 2^-31 of a token's largest element, off by 2^-39 of it (or 2^-151) below, far below the sums' rounding
 //     (16 tokens of 4096 to 1024, four of 64 experts: 81 us with twelve operations a word, 73.6 with ten).
 //   * mid, in binary32 first, goes as two fp16 numbers, 22 bits, on a power of two of its own for each slot, its largest below
 //     2^15; they are two rows of elements, so that four slots fill an instruction's columns there.  (One number, 11 bits, is 16 us
