@@ -9,14 +9,14 @@
 //     0: exact down to 2^-31 of a token's largest element, off by 2^-39 of it (or 2^-151) below, far below the sums' rounding
 //     (16 tokens of 4096 to 1024, four of 64 experts: 81 us with twelve operations a word, 73.6 with ten).
 //   * mid, in binary32 first, goes as two fp16 numbers, 22 bits, on a power of two of its own for each slot, its largest below
-//     2^15; they are two rows of elements, so that four slots fill an instruction's columns there.  (One number, 11 bits, is 16 us
+//     2^15; they are two rows of elements, so that four slots fill an instruction's columns there.  (One number, 11 bits, is 12 us
 //     faster below, but Y then shows its rounding wherever a residual takes most of the sum away, and other numbers of tokens in a
 //     call, which go on digits, change Y by as much.)
 //   * moe_wide_kernel does both products: a block has 4 warps side by side on 32 columns each (16 of gate and
 //     other half; or 32 of y) and 2 along K; the warps' sums are added in a fixed order.  What each slot adds to its
 //     token goes to the workspace, moe_combine_kernel adds it slot by slot.
-// 64 tokens of 4096 to 2048, four of 32 experts (429 MB of codes and scales): 150 us, 2.9 TB/s.  No unit is saturated (issue slots
-// 53 % and 40 %, tensor pipe 26 % and 30 %, DRAM 42 % and 25 % of the two products): four warps a scheduler (128 registers)
+// 64 tokens of 4096 to 2048, four of 32 experts (429 MB of codes and scales): 146 us, 2.9 TB/s.  No unit is saturated (issue slots
+// 53 % and 41 %, tensor pipe 32 % and 34 %, DRAM 42 % and 28 % in the two products): four warps a scheduler (128 registers)
 // do not cover the loads of their rows from L1 and the chains of products; without those loads the second product takes two thirds.
 #include "dsq_moe.cuh"
 
@@ -269,11 +269,11 @@ __device__ __forceinline__ void multiply(uint32_t at, const Unpack<XT> &unpack, 
 }
 
 // The same of slots whose elements are two numbers each, the first in row 2 i of a tile of four slots, the second in row 2 i + 1: a lane
-// has both sums of slot j, and adds them.  Elements come word by word, one ahead: pieces[q & 1] has those of word q when
-// its turn comes, fetch(q, to) brings those of word q (4: the next chunk's word 0).
+// has both sums of slot j, and adds them.  Elements come word by word, WORDS (2 or 4) less one ahead: pieces[q % WORDS] has those of
+// word q when its turn comes, fetch(q, to) brings those of word q (from 4 on the next chunk's).
 template <int TILES> struct Piece { uint4 x[TILES]; };
-template <int XT, int TILES, int GP, class F>
-__device__ __forceinline__ void multiply_both(uint32_t at, const Unpack<XT> &unpack, Piece<TILES> (&pieces)[2], DsqPair (&total)[2][TILES], F fetch)
+template <int XT, int TILES, int GP, int WORDS, class F>
+__device__ __forceinline__ void multiply_both(uint32_t at, const Unpack<XT> &unpack, Piece<TILES> (&pieces)[WORDS], DsqPair (&total)[2][TILES], F fetch)
 {
     const int lane = threadIdx.x & 31, n = lane >> 2, j = lane & 3;
     const uint32_t as = at + Stage<NT, GP>::W_BYTES + n * 4;
@@ -288,8 +288,8 @@ __device__ __forceinline__ void multiply_both(uint32_t at, const Unpack<XT> &unp
     float acc[2][TILES][4];
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
-        fetch(q + 1, pieces[(q + 1) & 1]);
-        const Piece<TILES> &r = pieces[q & 1];
+        fetch(q + WORDS - 1, pieces[(q + WORDS - 1) % WORDS]);
+        const Piece<TILES> &r = pieces[q % WORDS];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             uint32_t a[2][4];
@@ -444,12 +444,12 @@ template <bool OUT, int XT, int GP> struct Wide {
         __syncthreads();
     }
 
-    // the second product of up to 4 TILES slots
-    template <int TILES> __device__ __forceinline__ void run_out()
+    // the second product of up to 4 TILES slots, WORDS words of elements on their way
+    template <int TILES, int WORDS> __device__ __forceinline__ void run_out()
     {
         const Unpack<XT> unpack(p.odd);
         const uint8_t *x[TILES];
-        Piece<TILES> pieces[2] = {};
+        Piece<TILES> pieces[WORDS] = {};
 #pragma unroll
         for (int m = 0; m < TILES; ++m)
             x[m] = 4 * m + (n >> 1) < slots ? p.w.mid_rows + (int64_t)group->slot[4 * m + (n >> 1)] * chunks * 512 + 64 * (n & 1) + 16 * j : nullptr;
@@ -459,13 +459,16 @@ template <bool OUT, int XT, int GP> struct Wide {
             for (int m = 0; m < TILES; ++m)
                 if (x[m]) to.x[m] = load_16(x[m] + (int64_t)chunk * 512 + 128 * q);
         };
-        if (turns > 0) fetch(wk, 0, pieces[0]);
+        if (turns > 0) {
+#pragma unroll
+            for (int q = 0; q < WORDS - 1; ++q) fetch(wk, q, pieces[q]);
+        }
         if (turns > 1) touch(x, wk + KW, 4);
         DsqPair total[2][TILES] = {};
         each_turn([&](int i, uint32_t at) {
-            multiply_both<XT, TILES, GP>(at, unpack, pieces, total, [&](int q, Piece<TILES> &to) {
+            multiply_both<XT, TILES, GP, WORDS>(at, unpack, pieces, total, [&](int q, Piece<TILES> &to) {
                 if (q < 4) fetch(wk + i * KW, q, to);
-                else if (i + 1 < turns) fetch(wk + (i + 1) * KW, 0, to);
+                else if (i + 1 < turns) fetch(wk + (i + 1) * KW, q - 4, to);
             });
             if (i + 2 < turns) touch(x, wk + (i + 2) * KW, 4);
         });
@@ -536,10 +539,12 @@ __global__ void __launch_bounds__(THREADS, MOST == 1 ? 3 : 2) moe_wide_kernel(co
             waited = true;
         }
         if (OUT) {
-            if (slots <= 4) w.template run_out<1>();
-            else if (MOST == 1 || slots <= 8) w.template run_out<2>();
-            else if (slots <= 12) w.template run_out<3>();
-            else w.template run_out<4>();
+            // (as many words ahead as there are registers for)
+            if (slots <= 4) w.template run_out<1, 4>();
+            else if (MOST == 1) w.template run_out<2, 2>();
+            else if (slots <= 8) w.template run_out<2, 4>();
+            else if (slots <= 12) w.template run_out<3, 2>();
+            else w.template run_out<4, 2>();
         } else {
             if (MOST == 1 || slots <= 8) w.template run_in<1>();
             else w.template run_in<2>();
