@@ -21,10 +21,12 @@
 //     with the turn that has enough: 2048 rows of 128000 bf16 with three left, 20 alternatives, 152 us (111 without a
 //     mask; the largest `top` times one after the other 3790).  That is left for rows whose large elements are many,
 //     different and all with the same few threads.
-//   4096 rows of 128000 bf16 with five alternatives: 198 us, 5.3 TB/s (issue slots 60 %, nine instructions an element in
-//   all); without alternatives or with 32000 columns what follows a row's pass weighs more (56 us, 4.6 TB/s).  One row: 9.5 us, a
-//   chain of a load, three barriers, a second load of a few vectors and the cluster's exchange.
-//   * Backwards: a block takes a piece of a row, reads it and writes it.  2048 rows of 128000 bf16: 158 us, 6.6 TB/s.
+//   4096 rows of 128000 bf16 with five alternatives: 222 us, 4.7 TB/s (197 where the same rows come again and L2 has some of
+//   them): nothing is saturated (issue slots 63 %, DRAM 53 %), blocks between their passes and a last wave that is not
+//   full; without alternatives 161.  Fewer rows more so: 1024 57 us, 300 32, 75 to 148 13.5.  One row: 9.6 us, a chain of a
+//   load, three barriers, a second load of a few vectors and the cluster's exchange.
+//   * Backwards: a block takes a piece of a row, reads it and writes it.  2048 rows of 128000 bf16: 175 us, 6.0 TB/s (158 where
+//   the same rows come again: L2).
 #include "dsq_launch.h"
 #include "dsq_pairs.cuh"
 #include "dsq_ptx.cuh"

@@ -24,9 +24,11 @@
 //     element what is below 2^-31 of the largest of its 128: for the codes' grid Delta (c + 1/2),
 //     which has no 0, that is below the rounding of the sums.  The grid Delta c, whose 0 can make the largest
 //     element vanish, and experts with more slots go on 16 bits (dsq_moe_wide.cu).
-// One token of 2048 to 1024, eight of 64 experts (27 MB of codes and scales): 13.6 us, of which four launches in a row
-// without work are 6 (14.4 where the first product's copies wait for the groups that the kernel ahead writes); 16 tokens of 4096 to 1024, four of 64 (276 MB): 75 us, 3.7 TB/s, issue slots 65 to 70 % (275 instructions a
-// chunk of 2 KB: 97 for its copies, 187 to unpack and multiply), tensor pipe 22 %.
+// One token of 2048 to 1024, eight of 64 experts (27 MB of codes and scales): 14 us, of which four launches in a row
+// without work are 6 (14.4 against 13.6 where the first product's copies wait for the groups that the kernel ahead writes).  16
+// tokens of 4096 to 1024, four of 64 (276 MB): 72 us, 3.8 TB/s; no unit is saturated (issue slots 56 % and 45 %, tensor pipe
+// 27 % and 18 %, DRAM 52 % and 37 % in the two products): warps wait for digits from L1, for copies and for one another's
+// instructions (275 a chunk of 2 KB: 97 for its copies, 187 to unpack and multiply).
 #include "dsq_moe.cuh"
 
 using namespace dsq_moe;
