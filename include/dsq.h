@@ -441,7 +441,8 @@ typedef struct dsq_heads_t {
  * eps = 0 gives zeros; a NaN or an infinity stays in its head.  Data need the alignment of their
  * elements only (this and the next function; 16 bytes and strides that are multiples of 16 bytes
  * are the fast case).  head_dim even, at most 512; heads at most 4096 (DSQ_ERR_SIZE); heads of y that
- * overlap: DSQ_ERR_SHAPE; weight with norm = 0, odd head_dim: DSQ_ERR_UNSUPPORTED.  HBM-bound. */
+ * overlap: DSQ_ERR_SHAPE (q's and k's where they begin together; further in that is the caller's care);
+ * weight with norm = 0, odd head_dim: DSQ_ERR_UNSUPPORTED.  HBM-bound. */
 int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
                      const dsq_rotary_t *rotary, int norm, float eps, int dtype,
                      void *stream);

@@ -823,7 +823,7 @@ int dsq_headnorm_fwd(const dsq_heads_t *q, const dsq_heads_t *k, int64_t tokens,
         if (st) return st;
         if (h->weight && !norm) return DSQ_ERR_UNSUPPORTED;
         if (!aligned_to(h->x, size) || !aligned_to(h->y, size) || !aligned_to(h->weight, 4)) return DSQ_ERR_ALIGN;
-        if (!apart(tokens, h->heads, h->y_token, h->y_head, p.D)) return DSQ_ERR_SHAPE;
+        if (!apart(tokens, h->heads, h->y_token, h->y_head, p.D) || (i && h->y == q->y)) return DSQ_ERR_SHAPE;
         Tensor &t = p.t[i];
         t.x = h->x; t.y = h->y; t.w = h->weight;
         t.x_token = h->x_token; t.x_head = h->x_head; t.y_token = h->y_token; t.y_head = h->y_head;
@@ -870,7 +870,7 @@ int dsq_headnorm_bwd(const dsq_heads_grad_t *q, const dsq_heads_grad_t *k, int64
         if (!aligned_to(h->grad_y, size) || !aligned_to(h->x, size) || !aligned_to(h->grad_x, size) ||
             !aligned_to(h->weight, 4) || !aligned_to(h->grad_weight, 4))
             return DSQ_ERR_ALIGN;
-        if (!apart(tokens, h->heads, h->gx_token, h->gx_head, p.D)) return DSQ_ERR_SHAPE;
+        if (!apart(tokens, h->heads, h->gx_token, h->gx_head, p.D) || (i && h->grad_x == q->grad_x)) return DSQ_ERR_SHAPE;
         Tensor &t = p.t[i];
         t.gy = h->grad_y; t.x = h->x; t.y = h->grad_x; t.w = h->weight;
         t.g_token = h->gy_token; t.g_head = h->gy_head;
