@@ -103,7 +103,6 @@ def test_gradients_whose_products_leave_binary32(dsq, D, hq, hk, size, of_g, eps
     x, g = rng.normal(size=(9, hq + hk, D)), rng.normal(size=(9, hq + hk, D))
     x[4], g[4] = x[4] * size, g[4] * of_g                       # beside ordinary ones
     x[8, hq], g[8, hq] = x[8, hq] * size, g[8, hq] * of_g
-    # (a rounding of grad_w is one of its largest term's: ordinary tokens alone are looked at in a second call)
     x, g = torch.from_numpy(x).float(), torch.from_numpy(g).float()
     pos, freq = torch.arange(9), torch.rand(D // 2, generator=torch.Generator().manual_seed(D))
     w = [torch.from_numpy(1 + 0.2 * rng.normal(size=D)).float() for _ in range(2)]
